@@ -413,6 +413,152 @@ CAWN_API int cawn_phase_accumulate_fwd_static(const cawn_params *params,
                                               uint32_t *device_status,
                                               void *cuda_stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Operators that stand next to the phase accumulation in a layer.  (Not in the paper, which
+ * names dropout on the layer's output only.)  The library's rules hold: caller-owned device
+ * memory, asynchronous on the given stream, everything validated before anything is launched,
+ * 64-bit offsets throughout.  Sequence arrays are float, or bfloat16 with CAWN_FLAG_INPUT_BF16 |
+ * CAWN_FLAG_OUTPUT_BF16 (these come together or not at all; other flags are refused); every
+ * sum, statistic, state and parameter is float.  All array pointers must be 16-byte aligned.
+ * None of these calls keeps anything between calls: a workspace needs no initialisation, and
+ * one workspace serves one call at a time.  Results are bitwise repeatable (no atomics).
+ * ------------------------------------------------------------------------------------------ */
+
+/*
+ * Gated delta rule: per value head a matrix state that decays, and that a new key corrects
+ * towards its value instead of adding to it.
+ *   S_t = e^{g_t} S_{t-1} + u_t k_t^T
+ *   u_t = beta_t (v_t - e^{g_t} S_{t-1} k_t)          S_{-1} = state_in (0 when NULL)
+ *   o_t = scale S_t q_t                               state_out = S_{L-1}
+ * Shapes.  q, k [B, L, Hk, Dk]; v, o [B, L, Hv, Dv]; g, beta [B, L, Hv] float, dense; states
+ * [B, Hv, Dv, Dk] float, dense.  Value head h reads key head h / (Hv/Hk).  The rows of one time step
+ * (all heads) are contiguous; consecutive steps lie *_stride elements apart (0 = dense) and batches
+ * L times that, so that q, k, v may be slices of one projection's output.
+ * g is the log decay, at most 0: e^{g} in [0, 1]; -infinity forgets the state (a packed document's
+ * first token).  beta is usually in [0, 1]; the recurrence is stable while beta |k|^2 < 2, which the
+ * caller sees to (unit keys).
+ * Limits: Hv a multiple of Hk, Dk and Dv multiples of 8 up to 128, strides multiples of 8 elements,
+ * B * Hv <= 65535 * 64.
+ */
+typedef struct cawn_delta_params {
+    uint32_t struct_size;
+    int32_t  B;              /* batch >= 1                                                       */
+    int64_t  L;              /* time steps of this call, >= 0, any value                         */
+    int32_t  Hk, Hv;         /* key / query heads, value heads                                   */
+    int32_t  Dk, Dv;         /* widths of a key / query and of a value                           */
+    float    scale;          /* of the read-out, usually Dk^-1/2                                 */
+    uint32_t flags;          /* 0, or CAWN_FLAG_INPUT_BF16 | CAWN_FLAG_OUTPUT_BF16: q, k, v, o and
+                                their gradients are bfloat16                                     */
+    int64_t  q_stride, k_stride, v_stride, o_stride;   /* elements from one time step to the next; 0 = dense */
+} cawn_delta_params;
+
+enum { CAWN_DELTA_FWD = 0, CAWN_DELTA_BWD = 1 };    /* `op` of cawn_delta_rule_workspace_bytes */
+
+/* Host-only size query for cawn_delta_rule_fwd / _bwd. */
+CAWN_API int cawn_delta_rule_workspace_bytes(const cawn_delta_params *params, int op, size_t *bytes);
+
+/*
+ * Forward for prompts and training.  state_in NULL = zero; state_out NULL = not wanted, may alias
+ * state_in.  o may not alias an input.  Short calls run the recurrence token by token, longer ones
+ * chunk by chunk, and with few heads the time axis is cut into segments that run side by side.
+ * With bfloat16 storage o is rounded once from a sum whose factors (state, corrections, scores) were
+ * rounded to bfloat16; the state and everything that feeds it keep 16 or more mantissa bits.
+ */
+CAWN_API int cawn_delta_rule_fwd(const cawn_delta_params *params,
+                                 const void *q, const void *k, const void *v,
+                                 const float *g, const float *beta, const float *state_in,
+                                 void *o, float *state_out,
+                                 void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * The same operation token by token in float32, for decoding: one token (or a few, e.g. a draft
+ * that is checked) with the state read and written once.  No workspace.  Any L; meant for short ones.
+ */
+CAWN_API int cawn_delta_rule_step(const cawn_delta_params *params,
+                                  const void *q, const void *k, const void *v,
+                                  const float *g, const float *beta, const float *state_in,
+                                  void *o, float *state_out, void *cuda_stream);
+
+/*
+ * Backward.  Everything is recomputed from the forward's inputs (nothing is saved by the forward).
+ * grad_o [B, L, Hv, Dv] (o_stride).  grad_state_out: gradient of state_out or NULL (= 0).
+ * grad_q, grad_k [B, L, Hk, Dk] (summed over the value heads that share them), grad_v [B, L, Hv, Dv]:
+ * dense, the type of the inputs.  grad_g, grad_beta [B, L, Hv] float.  grad_state_in: float or NULL.
+ * Outputs may not alias inputs or each other.
+ */
+CAWN_API int cawn_delta_rule_bwd(const cawn_delta_params *params,
+                                 const void *q, const void *k, const void *v,
+                                 const float *g, const float *beta, const float *state_in,
+                                 const void *grad_o, const float *grad_state_out,
+                                 void *grad_q, void *grad_k, void *grad_v,
+                                 float *grad_g, float *grad_beta, float *grad_state_in,
+                                 void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Group norm with an activation, channels last: x [N, G*M], statistics over the M channels of each
+ * position's group (never over positions, so a causal layer stays causal).
+ *   xh = (x - mean) / sqrt(var + eps)      CAWN_NORM_RMS: xh = x / sqrt(mean(x^2) + eps)
+ *   z  = xh * weight + bias                [G*M] float each, NULL = 1 and 0
+ *   y  = z | z sigmoid(z) | z * gate * sigmoid(gate)          by `act`
+ * Heads of a mixer are groups; the rms form with weight = M^-1/2 makes unit queries and keys.
+ * x, gate: rows x_stride / gate_stride elements apart (0 = dense).  y and gradients: dense.
+ * y may alias x or gate when that one is dense.
+ */
+enum { CAWN_NORM_ACT_NONE = 0, CAWN_NORM_ACT_SILU = 1, CAWN_NORM_ACT_GATE = 2 };
+
+typedef struct cawn_norm_params {
+    uint32_t struct_size;
+    int32_t  G;              /* groups >= 1                                                      */
+    int64_t  N;              /* positions >= 0                                                   */
+    int32_t  M;              /* channels of a group, 1..4096                                     */
+    int32_t  act;            /* CAWN_NORM_ACT_*                                                  */
+    float    eps;            /* >= 0                                                             */
+    int32_t  rms;            /* 0: mean and variance, 1: mean square only                        */
+    uint32_t flags;          /* 0, or CAWN_FLAG_INPUT_BF16 | CAWN_FLAG_OUTPUT_BF16               */
+    uint32_t reserved;       /* 0                                                                */
+    int64_t  x_stride, gate_stride;
+} cawn_norm_params;
+
+CAWN_API int cawn_group_norm_fwd(const cawn_norm_params *params, const void *x,
+                                 const float *weight, const float *bias, const void *gate,
+                                 void *y, void *cuda_stream);
+
+/* Host-only size query for cawn_group_norm_bwd. */
+CAWN_API int cawn_group_norm_workspace_bytes(const cawn_norm_params *params, size_t *bytes);
+
+/* Backward: grad_y [N, G*M] dense -> grad_x; grad_gate (required with CAWN_NORM_ACT_GATE, NULL
+ * otherwise), grad_weight, grad_bias [G*M] float or NULL.  The statistics are recomputed from x.
+ * grad_x may alias grad_y.  The workspace is used for grad_weight and grad_bias only and may be NULL
+ * when neither is wanted. */
+CAWN_API int cawn_group_norm_bwd(const cawn_norm_params *params, const void *x,
+                                 const float *weight, const float *bias, const void *gate,
+                                 const void *grad_y, void *grad_x, void *grad_gate,
+                                 float *grad_weight, float *grad_bias,
+                                 void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Dropout whose mask is never stored, with the sum that usually follows:
+ *   y_i = residual_i + (keep_i ? x_i / P(keep) : 0)       residual NULL = 0
+ * keep_i: 16 random bits of element i are at least T = round(p * 65536).  The bits are those of
+ * Philox4x32-10 (Salmon, Moraes, Dror, Shaw: "Parallel random numbers: as easy as 1, 2, 3", 2011)
+ * with key `seed` and counter (i / 8, offset): word (i % 8) / 2, its low half for even i.  P(keep) =
+ * 1 - T / 65536 exactly, so the expectation of y is exact for every p.  The gradient with respect to
+ * x is the same call on grad_y with the same seed and offset and no residual.
+ * offset_device: device pointer to one uint64 that is added to `offset`, or NULL: a CUDA graph that
+ * is replayed gets a new mask by writing it.  y may alias x or residual.
+ */
+typedef struct cawn_dropout_params {
+    uint32_t struct_size;
+    float    p;              /* in [0, 1); T is at most 65535                                    */
+    int64_t  n;              /* elements >= 0                                                    */
+    uint64_t seed, offset;
+    uint32_t flags;          /* 0, or CAWN_FLAG_INPUT_BF16 | CAWN_FLAG_OUTPUT_BF16               */
+    uint32_t reserved;       /* 0                                                                */
+} cawn_dropout_params;
+
+CAWN_API int cawn_dropout(const cawn_dropout_params *params, const void *x, const void *residual,
+                          void *y, const uint64_t *offset_device, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

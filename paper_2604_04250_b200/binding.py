@@ -33,6 +33,8 @@ CAWN_FLAG_OUTPUT_BF16 = 16
 
 CAWN_OP_FWD, CAWN_OP_BWD_SAVED, CAWN_OP_BWD_PUSHES, CAWN_OP_STATE, CAWN_OP_FWD_HOST, CAWN_OP_MIXING_BWD = range(6)
 CAWN_SAVED_STATES, CAWN_SAVED_PUSHES = 0, 1
+CAWN_DELTA_FWD, CAWN_DELTA_BWD = 0, 1
+CAWN_NORM_ACT_NONE, CAWN_NORM_ACT_SILU, CAWN_NORM_ACT_GATE = range(3)
 
 EXPORTS = (
     "cawn_status_string", "cawn_workspace_bytes", "cawn_workspace_init",
@@ -40,6 +42,8 @@ EXPORTS = (
     "cawn_poll_status", "cawn_phase_accumulate_fwd_host", "cawn_phase_accumulate_fwd_static",
     "cawn_phase_accumulate_bwd_dynamic", "cawn_mixing_bwd", "cawn_phase_accumulate_fwd_ear",
     "cawn_workspace_set_wait_hook", "cawn_mixing_bwd_dynamic",
+    "cawn_delta_rule_workspace_bytes", "cawn_delta_rule_fwd", "cawn_delta_rule_step", "cawn_delta_rule_bwd",
+    "cawn_group_norm_fwd", "cawn_group_norm_workspace_bytes", "cawn_group_norm_bwd", "cawn_dropout",
 )
 
 
@@ -56,6 +60,52 @@ class cawn_params(ctypes.Structure):
         ("grad_clamp_abs", ctypes.c_float),
         ("conv_k", ctypes.c_int32),
         ("flags", ctypes.c_uint32),
+    ]
+
+
+class cawn_delta_params(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("B", ctypes.c_int32),
+        ("L", ctypes.c_int64),
+        ("Hk", ctypes.c_int32),
+        ("Hv", ctypes.c_int32),
+        ("Dk", ctypes.c_int32),
+        ("Dv", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("flags", ctypes.c_uint32),
+        ("q_stride", ctypes.c_int64),
+        ("k_stride", ctypes.c_int64),
+        ("v_stride", ctypes.c_int64),
+        ("o_stride", ctypes.c_int64),
+    ]
+
+
+class cawn_norm_params(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("G", ctypes.c_int32),
+        ("N", ctypes.c_int64),
+        ("M", ctypes.c_int32),
+        ("act", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("rms", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+        ("reserved", ctypes.c_uint32),
+        ("x_stride", ctypes.c_int64),
+        ("gate_stride", ctypes.c_int64),
+    ]
+
+
+class cawn_dropout_params(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("p", ctypes.c_float),
+        ("n", ctypes.c_int64),
+        ("seed", ctypes.c_uint64),
+        ("offset", ctypes.c_uint64),
+        ("flags", ctypes.c_uint32),
+        ("reserved", ctypes.c_uint32),
     ]
 
 
@@ -94,6 +144,15 @@ def lib():
         L.cawn_workspace_set_wait_hook.argtypes = [vp, ctypes.c_int, ctypes.c_uint, vp]
         L.cawn_phase_accumulate_fwd_host.argtypes = [pp, vp, fp, fp, vp, vp, vp, vp, vp, sz, vp]
         L.cawn_phase_accumulate_fwd_static.argtypes = [pp, vp, fp, fp, vp, vp, vp, vp, vp, vp]
+        dp, np_, op = ctypes.POINTER(cawn_delta_params), ctypes.POINTER(cawn_norm_params), ctypes.POINTER(cawn_dropout_params)
+        L.cawn_delta_rule_workspace_bytes.argtypes = [dp, ctypes.c_int, ctypes.POINTER(sz)]
+        L.cawn_delta_rule_fwd.argtypes = [dp, vp, vp, vp, fp, fp, fp, vp, fp, vp, sz, vp]
+        L.cawn_delta_rule_step.argtypes = [dp, vp, vp, vp, fp, fp, fp, vp, fp, vp]
+        L.cawn_delta_rule_bwd.argtypes = [dp, vp, vp, vp, fp, fp, fp, vp, fp, vp, vp, vp, fp, fp, fp, vp, sz, vp]
+        L.cawn_group_norm_fwd.argtypes = [np_, vp, fp, fp, vp, vp, vp]
+        L.cawn_group_norm_workspace_bytes.argtypes = [np_, ctypes.POINTER(sz)]
+        L.cawn_group_norm_bwd.argtypes = [np_, vp, fp, fp, vp, vp, vp, vp, fp, fp, vp, sz, vp]
+        L.cawn_dropout.argtypes = [op, vp, vp, vp, vp, vp]
         for name in EXPORTS:
             if name != "cawn_status_string":
                 getattr(L, name).restype = ctypes.c_int
@@ -246,3 +305,84 @@ def cawn_mixing_bwd(params, h, conv_w, gamma, theta, grad_y, grad_h, workspace, 
         _dp(state_in), _dp(grad_y), _dp(grad_state_out), _dp(grad_h), _dp(grad_conv_w), _dp(grad_conv_bias),
         _dp(grad_gamma), _dp(grad_theta), _dp(grad_state_in), _dp(workspace),
         workspace.numel() * workspace.element_size(), _stream(stream)), "cawn_mixing_bwd")
+
+
+# ---- operators next to the phase accumulation in a layer
+
+def make_delta_params(B, L, Hk, Hv, Dk, Dv, scale=None, flags=0, q_stride=0, k_stride=0, v_stride=0, o_stride=0):
+    return cawn_delta_params(ctypes.sizeof(cawn_delta_params), B, L, Hk, Hv, Dk, Dv,
+                             Dk ** -0.5 if scale is None else scale, flags, q_stride, k_stride, v_stride, o_stride)
+
+
+def cawn_delta_rule_workspace_bytes(params, op):
+    n = ctypes.c_size_t(0)
+    _check(lib().cawn_delta_rule_workspace_bytes(ctypes.byref(params), op, ctypes.byref(n)),
+           "cawn_delta_rule_workspace_bytes")
+    return n.value
+
+
+def _plain_workspace(n, device):
+    import torch
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def new_delta_workspace(params, op, device="cuda"):
+    """Allocate (with torch, as plain device memory) a workspace for CAWN_DELTA_FWD or CAWN_DELTA_BWD."""
+    return _plain_workspace(cawn_delta_rule_workspace_bytes(params, op), device)
+
+
+def cawn_delta_rule_fwd(params, q, k, v, g, beta, o, workspace, state_in=None, state_out=None, stream=None):
+    _check(lib().cawn_delta_rule_fwd(
+        ctypes.byref(params), _dp(q), _dp(k), _dp(v), _dp(g), _dp(beta), _dp(state_in), _dp(o), _dp(state_out),
+        _dp(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "cawn_delta_rule_fwd")
+
+
+def cawn_delta_rule_step(params, q, k, v, g, beta, o, state_in=None, state_out=None, stream=None):
+    _check(lib().cawn_delta_rule_step(
+        ctypes.byref(params), _dp(q), _dp(k), _dp(v), _dp(g), _dp(beta), _dp(state_in), _dp(o), _dp(state_out),
+        _stream(stream)), "cawn_delta_rule_step")
+
+
+def cawn_delta_rule_bwd(params, q, k, v, g, beta, grad_o, grad_q, grad_k, grad_v, grad_g, grad_beta, workspace,
+                        state_in=None, grad_state_out=None, grad_state_in=None, stream=None):
+    _check(lib().cawn_delta_rule_bwd(
+        ctypes.byref(params), _dp(q), _dp(k), _dp(v), _dp(g), _dp(beta), _dp(state_in), _dp(grad_o),
+        _dp(grad_state_out), _dp(grad_q), _dp(grad_k), _dp(grad_v), _dp(grad_g), _dp(grad_beta), _dp(grad_state_in),
+        _dp(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "cawn_delta_rule_bwd")
+
+
+def make_norm_params(N, G, M, eps=1e-5, act=CAWN_NORM_ACT_NONE, rms=False, flags=0, x_stride=0, gate_stride=0):
+    return cawn_norm_params(ctypes.sizeof(cawn_norm_params), G, N, M, act, eps, int(rms), flags, 0, x_stride, gate_stride)
+
+
+def cawn_group_norm_workspace_bytes(params):
+    n = ctypes.c_size_t(0)
+    _check(lib().cawn_group_norm_workspace_bytes(ctypes.byref(params), ctypes.byref(n)), "cawn_group_norm_workspace_bytes")
+    return n.value
+
+
+def new_norm_workspace(params, device="cuda"):
+    """Allocate (with torch, as plain device memory) a workspace for cawn_group_norm_bwd."""
+    return _plain_workspace(cawn_group_norm_workspace_bytes(params), device)
+
+
+def cawn_group_norm_fwd(params, x, y, weight=None, bias=None, gate=None, stream=None):
+    _check(lib().cawn_group_norm_fwd(ctypes.byref(params), _dp(x), _dp(weight), _dp(bias), _dp(gate), _dp(y),
+                                     _stream(stream)), "cawn_group_norm_fwd")
+
+
+def cawn_group_norm_bwd(params, x, grad_y, grad_x, workspace=None, weight=None, bias=None, gate=None, grad_gate=None,
+                        grad_weight=None, grad_bias=None, stream=None):
+    n = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().cawn_group_norm_bwd(
+        ctypes.byref(params), _dp(x), _dp(weight), _dp(bias), _dp(gate), _dp(grad_y), _dp(grad_x), _dp(grad_gate),
+        _dp(grad_weight), _dp(grad_bias), _dp(workspace), n, _stream(stream)), "cawn_group_norm_bwd")
+
+
+def make_dropout_params(n, p, seed, offset=0, flags=0):
+    return cawn_dropout_params(ctypes.sizeof(cawn_dropout_params), p, n, seed, offset, flags, 0)
+
+
+def cawn_dropout(params, x, y, residual=None, offset_device=None, stream=None):
+    _check(lib().cawn_dropout(ctypes.byref(params), _dp(x), _dp(residual), _dp(y), _dp(offset_device), _stream(stream)),
+           "cawn_dropout")

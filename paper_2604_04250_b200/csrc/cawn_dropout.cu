@@ -1,0 +1,103 @@
+// Dropout from a counter-based generator, added to a residual.
+//
+// Mathematics: y = residual + keep * x / P(keep), keep decided by 16 bits of Philox4x32-10 (Salmon et
+// al. 2011) per element.  One generator call gives 128 bits, so it serves 8 elements: one 16-byte word
+// of bfloat16, two of float.  Whoever recomputes the mask (the backward) needs the seed and the offset only.
+#include "cawn_ops.cuh"
+
+#include <math.h>
+
+namespace cawn {
+namespace {
+
+struct DropoutParams {
+    const void *x, *residual;
+    void *y;
+    const unsigned long long *offset_device;
+    long long n;
+    unsigned long long offset;
+    unsigned k0, k1, drop;       // an element is dropped when its 16 bits are below `drop`
+    float scale;                 // 1 / P(keep)
+};
+
+// Philox4x32-10: multipliers and Weyl increments as published.
+__device__ __forceinline__ uint4 philox(uint4 c, unsigned k0, unsigned k1)
+{
+#pragma unroll
+    for (int r = 0; r < 10; r++) {
+        const unsigned h0 = __umulhi(0xD2511F53u, c.x), l0 = 0xD2511F53u * c.x;
+        const unsigned h1 = __umulhi(0xCD9E8D57u, c.z), l1 = 0xCD9E8D57u * c.z;
+        c = make_uint4(h1 ^ c.y ^ k0, l1, h0 ^ c.w ^ k1, l0);
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return c;
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) dropout_kernel(const DropoutParams P)
+{
+    const long long block = (long long)blockIdx.x * blockDim.x + threadIdx.x, at = block * 8;
+    if (at >= P.n) return;
+    const unsigned long long off = P.offset + (P.offset_device != nullptr ? *P.offset_device : 0ull);
+    const T *x = static_cast<const T *>(P.x) + at;
+    const T *res = P.residual != nullptr ? static_cast<const T *>(P.residual) + at : nullptr;
+    T *y = static_cast<T *>(P.y) + at;
+    const int m = P.n - at < 8 ? (int)(P.n - at) : 8;
+    float f[8], a[8] = {};
+    if (m == 8) {
+        load_vec(f, x);
+        if (res != nullptr) load_vec(a, res);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            f[i] = i < m ? widen(x[i]) : 0.f;
+            if (res != nullptr && i < m) a[i] = widen(res[i]);
+        }
+    }
+    const uint4 c = philox(make_uint4((unsigned)block, (unsigned)((unsigned long long)block >> 32), (unsigned)off, (unsigned)(off >> 32)),
+                           P.k0, P.k1);
+    const unsigned w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const unsigned bits = i % 2 == 0 ? w[i / 2] & 0xffffu : w[i / 2] >> 16;
+        // a select, not a product with 0: what is dropped may be an infinity or NaN
+        f[i] = (bits >= P.drop ? f[i] * P.scale : 0.f) + a[i];
+    }
+    if (m == 8) {
+        store_vec(y, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (i < m) y[i] = narrow<T>(f[i]);
+    }
+}
+
+}  // namespace
+}  // namespace cawn
+
+extern "C" int cawn_dropout(const cawn_dropout_params *params, const void *x, const void *residual, void *y,
+                            const uint64_t *offset_device, void *cuda_stream)
+{
+    using namespace cawn;
+    if (params == nullptr) return CAWN_ERR_NULL_POINTER;
+    if (params->struct_size != sizeof(cawn_dropout_params)) return CAWN_ERR_INVALID_ARG;
+    if (params->n < 0 || !(params->p >= 0.f && params->p < 1.f) || params->reserved != 0 || !storage_flags_ok(params->flags))
+        return CAWN_ERR_INVALID_ARG;
+    if (params->n == 0) return CAWN_OK;
+    if (x == nullptr || y == nullptr) return CAWN_ERR_NULL_POINTER;
+    if (!all_aligned16(x, residual, y) || (reinterpret_cast<uintptr_t>(offset_device) & 7) != 0) return CAWN_ERR_MISALIGNED;
+    const long long blocks = ((params->n - 1) / 8 + 256) / 256;
+    if (blocks > 0x7fffffffll) return CAWN_ERR_UNSUPPORTED;
+    DropoutParams P = {};
+    P.x = x; P.residual = residual; P.y = y;
+    P.offset_device = reinterpret_cast<const unsigned long long *>(offset_device);
+    P.n = params->n; P.offset = params->offset;
+    P.k0 = (unsigned)params->seed; P.k1 = (unsigned)(params->seed >> 32);
+    const long drop = lround((double)params->p * 65536.0);
+    P.drop = (unsigned)(drop > 65535 ? 65535 : drop);
+    P.scale = (float)(65536.0 / (65536.0 - (double)P.drop));
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const bool half = params->flags != 0;
+    return status_of(launch(half ? dropout_kernel<bf16> : dropout_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, st, P));
+}

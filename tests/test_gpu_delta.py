@@ -1,0 +1,196 @@
+"""Gated delta rule against its definition in 64 bits.
+
+Tolerances (relative 2-norm).  float storage and states: products run on pairs of bfloat16 (16 mantissa
+bits, 2^-17 per rounding, a handful of roundings in a row) or on floats: 1e-5.  bfloat16 outputs: one
+storage rounding (at most 2^-8 of a value, 1.7e-3 of the norm) beside up to three factors rounded alike
+whose errors add up like independent ones: 5e-3.
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_04250_b200 import binding as cb
+from delta_ref import close, delta_inputs, delta_rule, flags_of
+
+pytestmark = pytest.mark.gpu
+
+TOL = {torch.float32: 1e-5, torch.bfloat16: 5e-3}
+STATE_TOL = 1e-5
+
+
+def params(d, scale=None, **kw):
+    B, L, Hv, Dv = d["v"].shape
+    return cb.make_delta_params(B, L, d["q"].shape[2], Hv, d["q"].shape[3], Dv, scale=scale, flags=flags_of(d["v"].dtype), **kw)
+
+
+def forward(d, form, with_state=True, in_place=False, prm=None, cuda=None):
+    c = cuda or {n: t.cuda() for n, t in d.items()}
+    prm = prm or params(d)
+    o = torch.full_like(d["v"], float("nan")).cuda()
+    si = c["state_in"].clone() if with_state else None
+    so = si if in_place else torch.full_like(c["state_in"], float("nan"))
+    if form == "step":
+        cb.cawn_delta_rule_step(prm, c["q"], c["k"], c["v"], c["g"], c["beta"], o, state_in=si, state_out=so)
+    else:
+        ws = cb.new_delta_workspace(prm, cb.CAWN_DELTA_FWD)
+        ws.fill_(0xFF)                                   # NaN patterns: nothing may be read before it is written
+        cb.cawn_delta_rule_fwd(prm, c["q"], c["k"], c["v"], c["g"], c["beta"], o, ws, state_in=si, state_out=so)
+    return o, so
+
+
+def reference(d, with_state=True):
+    w = {n: t.double() for n, t in d.items()}
+    return delta_rule(w["q"], w["k"], w["v"], w["g"], w["beta"], d["q"].shape[3] ** -0.5,
+                      w["state_in"] if with_state else torch.zeros_like(w["state_in"]))
+
+
+SHAPES = [  # B, L, Hk, Hv, Dk, Dv
+    (1, 1, 1, 1, 64, 64), (2, 2, 1, 3, 64, 64), (1, 7, 2, 2, 128, 128), (3, 15, 1, 1, 8, 8), (1, 63, 2, 4, 40, 24),
+    (1, 64, 1, 1, 64, 64), (2, 65, 2, 2, 64, 128), (1, 127, 3, 3, 96, 80), (2, 130, 1, 2, 128, 64), (1, 200, 2, 2, 16, 120),
+    (1, 321, 4, 4, 64, 64), (5, 129, 2, 6, 72, 56),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("form", ["step", "chunk"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_forward(shape, form, dtype):
+    d = delta_inputs(*shape, dtype, seed=sum(shape))
+    o, so = forward(d, form)
+    want_o, want_s = reference(d)
+    close(o, want_o, TOL[dtype], "o")
+    close(so, want_s, STATE_TOL, "state")
+
+
+@pytest.mark.parametrize("form", ["step", "chunk"])
+def test_no_state_in_and_in_place(form):
+    d = delta_inputs(2, 150, 2, 2, 64, 64, torch.float32, seed=5)
+    o, so = forward(d, form, with_state=False)
+    want_o, want_s = reference(d, with_state=False)
+    close(o, want_o, 1e-5)
+    close(so, want_s, 1e-5)
+    o1, s1 = forward(d, form)
+    o2, s2 = forward(d, form, in_place=True)
+    assert torch.equal(o1, o2) and torch.equal(s1, s2)
+
+
+@pytest.mark.parametrize("form", ["step", "chunk"])
+def test_no_tokens_hand_the_state_on(form):
+    d = delta_inputs(2, 0, 1, 2, 64, 64, torch.float32, seed=6)
+    _, so = forward(d, form)
+    assert torch.equal(so.cpu(), d["state_in"])
+    _, so = forward(d, form, with_state=False)
+    assert (so == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("form", ["step", "chunk"])
+def test_slices_of_one_projection(form, dtype):
+    """q, k, v side by side in one array, o in a wider one whose other columns stay as they are."""
+    B, L, Hk, Hv, Dk, Dv = 2, 99, 2, 4, 64, 72
+    d = delta_inputs(B, L, Hk, Hv, Dk, Dv, dtype, seed=7)
+    w = torch.cat([d["q"].flatten(2), d["k"].flatten(2), d["v"].flatten(2)], -1).cuda()
+    c = {n: t.cuda() for n, t in d.items()}
+    c["q"], c["k"], c["v"] = (x.unflatten(-1, s) for x, s in zip(w.split([Hk * Dk, Hk * Dk, Hv * Dv], -1), [(Hk, Dk), (Hk, Dk), (Hv, Dv)]))
+    out = torch.full((B, L, Hv * Dv + 16), 7.0, dtype=dtype, device="cuda")
+    prm = params(d, q_stride=w.shape[-1], k_stride=w.shape[-1], v_stride=w.shape[-1], o_stride=out.shape[-1])
+    so = torch.empty_like(c["state_in"])
+    view = out[..., 8:-8]
+    args = (prm, c["q"], c["k"], c["v"], c["g"], c["beta"], view)
+    if form == "step":
+        cb.cawn_delta_rule_step(*args, state_in=c["state_in"], state_out=so)
+    else:
+        cb.cawn_delta_rule_fwd(*args, cb.new_delta_workspace(prm, cb.CAWN_DELTA_FWD), state_in=c["state_in"], state_out=so)
+    want_o, want_s = reference(d)
+    close(view.unflatten(-1, (Hv, Dv)), want_o, TOL[dtype])
+    close(so, want_s, STATE_TOL)
+    assert (out[..., :8] == 7).all() and (out[..., -8:] == 7).all()
+
+
+@pytest.mark.parametrize("form", ["step", "chunk"])
+def test_state_passing_across_calls(form):
+    """A prompt in two calls, of which the second goes token by token, equals one call."""
+    d = delta_inputs(2, 203, 2, 2, 64, 64, torch.float32, seed=8)
+    want_o, want_s = reference(d)
+    first = {n: (t[:, :170].contiguous() if t.dim() > 2 and t.shape[1] == 203 else t) for n, t in d.items()}
+    rest = {n: (t[:, 170:].contiguous() if t.dim() > 2 and t.shape[1] == 203 else t) for n, t in d.items()}
+    o1, s1 = forward(first, form)
+    rest["state_in"] = s1.cpu()
+    o2, s2 = forward(rest, "step")
+    close(torch.cat([o1, o2], 1), want_o, 1e-5)
+    close(s2, want_s, 1e-5)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("form", ["step", "chunk"])
+def test_repeated_tokens(form, dtype):
+    """One key over and over with beta = 1 and next to no decay: the chunk's triangular system is the
+    all-ones triangle, whose powers grow like binomials (a power series for its inverse would fail)."""
+    d = delta_inputs(1, 192, 1, 2, 64, 64, dtype, seed=9)
+    d["k"] = d["k"][:, :1].expand_as(d["k"]).contiguous()
+    k = d["k"].double()
+    d["g"] = torch.full_like(d["g"], -1e-4)
+    d["beta"] = torch.ones_like(d["beta"]) / k.square().sum(-1).max().float()
+    o, so = forward(d, form)
+    want_o, want_s = reference(d)
+    close(o, want_o, TOL[dtype])
+    close(so, want_s, STATE_TOL)
+
+
+@pytest.mark.parametrize("form", ["step", "chunk"])
+def test_forgetting_and_strong_decay(form):
+    """-infinity as log decay starts over (the state before it leaves no trace); very strong and zero
+    decays, beta 0 and beta 2 in one call."""
+    d = delta_inputs(1, 200, 2, 2, 64, 64, torch.float32, seed=10)
+    d["g"][:, 70] = -float("inf")
+    d["g"][:, 71] = -float("inf")
+    d["g"][:, 100:110] = -90.0
+    d["g"][:, 110:120] = -1000.0
+    d["g"][:, 120:130] = 0.0
+    d["beta"][:, 130:140] = 0.0
+    d["beta"][:, 140:145] = 1.9
+    o, so = forward(d, form)
+    want_o, want_s = reference(d)
+    close(o, want_o, 1e-5)
+    close(so, want_s, 1e-5)
+    late = {n: (t[:, 70:].contiguous() if t.dim() > 2 and t.shape[1] == 200 else t) for n, t in d.items()}
+    o2, s2 = forward(late, form)
+    close(o2, want_o[:, 70:], 1e-5)
+    close(s2, want_s, 1e-5)
+
+
+def test_bad_values_stay_in_their_stream():
+    """NaN and infinity in one batch row's value leave the other rows alone and are not hidden."""
+    d = delta_inputs(3, 130, 1, 1, 64, 64, torch.float32, seed=11)
+    clean, _ = forward(d, "chunk")
+    d["v"][1, 40, 0, 3] = float("nan")
+    d["g"][2, 90] = float("nan")
+    o, so = forward(d, "chunk")
+    assert torch.equal(o[0], clean[0])
+    assert torch.isnan(o[1, 40:, 0, 3]).all() and torch.equal(o[1, :, 0, 4:], clean[1, :, 0, 4:])
+    assert torch.isnan(o[2, 90:]).all() and torch.isnan(so[2]).all()
+
+
+@pytest.mark.parametrize("form", ["step", "chunk"])
+def test_runs_on_another_stream_and_in_a_graph(form):
+    d = delta_inputs(2, 140, 2, 2, 64, 64, torch.bfloat16, seed=12)
+    want, want_s = forward(d, form)
+    c = {n: t.cuda() for n, t in d.items()}
+    prm = params(d)
+    o, so = torch.empty_like(want), torch.empty_like(want_s)
+    ws = cb.new_delta_workspace(prm, cb.CAWN_DELTA_FWD)
+    call = {"step": lambda: cb.cawn_delta_rule_step(prm, c["q"], c["k"], c["v"], c["g"], c["beta"], o, state_in=c["state_in"], state_out=so),
+            "chunk": lambda: cb.cawn_delta_rule_fwd(prm, c["q"], c["k"], c["v"], c["g"], c["beta"], o, ws, state_in=c["state_in"], state_out=so)}[form]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    side.synchronize()
+    assert torch.equal(o, want) and torch.equal(so, want_s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    o.zero_(), so.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(o, want) and torch.equal(so, want_s)

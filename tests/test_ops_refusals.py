@@ -1,0 +1,133 @@
+"""What the operators next to the scan refuse, on the host and before anything is launched (the
+addresses are fake and never dereferenced)."""
+import ctypes
+
+import pytest
+
+import __graft_entry__ as entry
+from paper_2604_04250_b200 import binding as cb
+
+A = 0x10000
+N = ctypes.c_size_t()
+ref = ctypes.byref
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    entry.build()
+
+
+def test_struct_layouts():
+    assert ctypes.sizeof(cb.cawn_delta_params) == 72 and cb.cawn_delta_params.q_stride.offset == 40
+    assert ctypes.sizeof(cb.cawn_norm_params) == 56 and cb.cawn_norm_params.x_stride.offset == 40
+    assert ctypes.sizeof(cb.cawn_dropout_params) == 40 and cb.cawn_dropout_params.seed.offset == 16
+
+
+def fwd(prm, q=A, ws=A, n=1 << 40, **kw):
+    a = dict(k=A, v=A, g=A, beta=A, state_in=None, o=A, state_out=None)
+    a.update(kw)
+    return cb.lib().cawn_delta_rule_fwd(None if prm is None else ref(prm), q, a["k"], a["v"], a["g"], a["beta"], a["state_in"], a["o"], a["state_out"], ws, n, None)
+
+
+def step(prm, q=A, **kw):
+    a = dict(k=A, v=A, g=A, beta=A, state_in=None, o=A, state_out=None)
+    a.update(kw)
+    return cb.lib().cawn_delta_rule_step(None if prm is None else ref(prm), q, a["k"], a["v"], a["g"], a["beta"], a["state_in"], a["o"], a["state_out"], None)
+
+
+def bwd(prm, ws=A, n=1 << 40, **kw):
+    names = ["q", "k", "v", "g", "beta", "state_in", "grad_o", "grad_state_out", "grad_q", "grad_k", "grad_v", "grad_g", "grad_beta", "grad_state_in"]
+    return cb.lib().cawn_delta_rule_bwd(None if prm is None else ref(prm), *[kw.get(x, None if "state" in x else A) for x in names], ws, n, None)
+
+
+def delta(B=2, L=200, Hk=2, Hv=4, Dk=64, Dv=64, **kw):
+    return cb.make_delta_params(B, L, Hk, Hv, Dk, Dv, **kw)
+
+
+INVALID = [dict(B=0), dict(L=-1), dict(Hk=0), dict(Hv=3), dict(Hv=0), dict(Dk=0), dict(flags=cb.CAWN_FLAG_INPUT_BF16), dict(flags=1 << 9),
+           dict(q_stride=64), dict(v_stride=300), dict(o_stride=255), dict(k_stride=132), dict(q_stride=-128)]
+UNSUPPORTED = [dict(Dk=60), dict(Dv=136), dict(Dk=256), dict(Dv=4), dict(B=1 << 22, Hv=4), dict(L=1 << 60)]
+
+
+@pytest.mark.parametrize("call", [fwd, step, bwd])
+def test_delta_rule_refusals(call):
+    assert call(None) == cb.CAWN_ERR_NULL_POINTER
+    bad = delta()
+    bad.struct_size = 64
+    assert call(bad) == cb.CAWN_ERR_INVALID_ARG
+    for kw in INVALID:
+        assert call(delta(**kw)) == cb.CAWN_ERR_INVALID_ARG, kw
+    for kw in UNSUPPORTED:
+        assert call(delta(**kw)) == cb.CAWN_ERR_UNSUPPORTED, kw
+    for name in ("q", "k", "v", "g", "beta"):
+        assert call(delta(), **{name: None}) == cb.CAWN_ERR_NULL_POINTER, name
+        assert call(delta(), **{name: A + 8}) == cb.CAWN_ERR_MISALIGNED, name
+
+
+def test_delta_rule_workspace():
+    size = lambda prm, op: cb.cawn_delta_rule_workspace_bytes(prm, op)
+    for op in (cb.CAWN_DELTA_FWD, cb.CAWN_DELTA_BWD):
+        assert size(delta(L=0), op) >= 0
+        assert size(delta(L=300), op) <= size(delta(L=3000), op)
+        assert size(delta(L=3000), op) > 0
+    lib = cb.lib()
+    assert lib.cawn_delta_rule_workspace_bytes(ref(delta()), 2, ref(N)) == cb.CAWN_ERR_INVALID_ARG
+    assert lib.cawn_delta_rule_workspace_bytes(ref(delta()), 0, None) == cb.CAWN_ERR_NULL_POINTER
+    assert lib.cawn_delta_rule_workspace_bytes(ref(delta(Dk=60)), 0, ref(N)) == cb.CAWN_ERR_UNSUPPORTED
+    long = delta(L=4000)
+    assert fwd(long, n=256) == cb.CAWN_ERR_WORKSPACE_TOO_SMALL
+    assert fwd(long, ws=None) == cb.CAWN_ERR_NULL_POINTER
+    assert fwd(long, ws=A + 4) == cb.CAWN_ERR_MISALIGNED
+    assert bwd(long, n=256) == cb.CAWN_ERR_WORKSPACE_TOO_SMALL
+    assert bwd(long, ws=None) == cb.CAWN_ERR_NULL_POINTER
+
+
+def test_delta_rule_backward_pointers():
+    for name in ("grad_o", "grad_q", "grad_k", "grad_v", "grad_g", "grad_beta"):
+        assert bwd(delta(), **{name: None}) == cb.CAWN_ERR_NULL_POINTER, name
+    for name in ("grad_q", "grad_state_out", "grad_state_in", "state_in"):
+        assert bwd(delta(), **{name: A + 2}) == cb.CAWN_ERR_MISALIGNED, name
+
+
+def norm(prm, x=A, gate=None, y=A, w=None):
+    return cb.lib().cawn_group_norm_fwd(None if prm is None else ref(prm), x, w, None, gate, y, None)
+
+
+def norm_bwd(prm, x=A, gate=None, gy=A, gx=A, gg=None, gw=None, ws=None, n=0):
+    return cb.lib().cawn_group_norm_bwd(ref(prm), x, None, None, gate, gy, gx, gg, gw, None, ws, n, None)
+
+
+def test_group_norm_refusals():
+    make = cb.make_norm_params
+    assert norm(None) == cb.CAWN_ERR_NULL_POINTER
+    for prm in (make(-1, 1, 8), make(1, 0, 8), make(1, 1, 0), make(1, 1, 8, eps=-1.0), make(1, 1, 8, eps=float("nan")), make(1, 1, 8, act=3),
+                make(1, 1, 8, flags=cb.CAWN_FLAG_OUTPUT_BF16), make(1, 2, 8, x_stride=15), make(1, 2, 8, gate_stride=3)):
+        assert norm(prm) == cb.CAWN_ERR_INVALID_ARG
+        assert norm_bwd(prm) == cb.CAWN_ERR_INVALID_ARG
+    for prm in (make(1, 1, 4097), make(1 << 40, 1, 8), make(1, 65536, 8)):
+        assert norm(prm) == cb.CAWN_ERR_UNSUPPORTED
+    ok, gated = make(4, 2, 8), make(4, 2, 8, act=cb.CAWN_NORM_ACT_GATE)
+    assert norm(ok, x=None) == cb.CAWN_ERR_NULL_POINTER and norm(ok, y=None) == cb.CAWN_ERR_NULL_POINTER
+    assert norm(gated) == cb.CAWN_ERR_NULL_POINTER
+    assert norm(ok, x=A + 4) == cb.CAWN_ERR_MISALIGNED and norm(ok, w=A + 4) == cb.CAWN_ERR_MISALIGNED
+    assert norm_bwd(gated, gate=A) == cb.CAWN_ERR_NULL_POINTER
+    assert norm_bwd(ok, gg=A) == cb.CAWN_ERR_INVALID_ARG
+    assert norm_bwd(ok, gw=A) == cb.CAWN_ERR_NULL_POINTER
+    assert norm_bwd(ok, gw=A, ws=A, n=16) == cb.CAWN_ERR_WORKSPACE_TOO_SMALL
+    bad = make(4, 2, 8)
+    bad.struct_size = 1
+    assert norm(bad) == cb.CAWN_ERR_INVALID_ARG
+    assert cb.lib().cawn_group_norm_workspace_bytes(ref(ok), None) == cb.CAWN_ERR_NULL_POINTER
+
+
+def test_dropout_refusals():
+    make = cb.make_dropout_params
+    f = lambda prm, x=A, r=None, y=A, d=None: cb.lib().cawn_dropout(None if prm is None else ref(prm), x, r, y, d, None)
+    assert f(None) == cb.CAWN_ERR_NULL_POINTER
+    for prm in (make(-1, 0.1, 0), make(8, 1.0, 0), make(8, -0.1, 0), make(8, float("nan"), 0), make(8, 0.1, 0, flags=cb.CAWN_FLAG_INPUT_BF16)):
+        assert f(prm) == cb.CAWN_ERR_INVALID_ARG
+    ok = make(8, 0.1, 0)
+    assert f(ok, x=None) == cb.CAWN_ERR_NULL_POINTER and f(ok, y=None) == cb.CAWN_ERR_NULL_POINTER
+    assert f(ok, r=A + 2) == cb.CAWN_ERR_MISALIGNED and f(ok, d=A + 4) == cb.CAWN_ERR_MISALIGNED
+    assert f(make(1 << 50, 0.1, 0)) == cb.CAWN_ERR_UNSUPPORTED
+    assert f(make(0, 0.1, 0), x=None) == cb.CAWN_OK
