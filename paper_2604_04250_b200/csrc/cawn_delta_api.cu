@@ -1,5 +1,5 @@
 // Gated delta rule: entry points and argument checks.
-#include "cawn_delta.cuh"
+#include "cawn_delta_chunk.cuh"
 
 namespace cawn {
 namespace {
@@ -46,8 +46,91 @@ int pass_state(const cawn_delta_params *p, const float *from, float *to, cudaStr
     return status_of(from != nullptr ? cudaMemcpyAsync(to, from, bytes, cudaMemcpyDeviceToDevice, st) : cudaMemsetAsync(to, 0, bytes, st));
 }
 
+// Calls of up to this many tokens run token by token.
+constexpr int kStepTokens = 16;
+
+// The workspace, front to back; sizes in bytes, every part a multiple of 256.
+struct Plan {
+    int dk, terms, chunks, vblocks, segs, seg_chunks;    // terms: of an input
+    size_t q, k, v, go;                  // three bfloat16 terms each, float storage only
+    size_t coef, tri, p, r, s0;
+    size_t seg_state, seg_map;
+    size_t total;
+};
+
+inline size_t part(double bytes) { return ((size_t)bytes + 255) / 256 * 256; }
+
+Plan plan_of(const cawn_delta_params *p, bool backward)
+{
+    Plan w = {};
+    w.dk = p->Dk <= 64 ? 64 : 128;
+    w.terms = p->flags != 0 ? 1 : 3;
+    const double nt = w.terms == 1 ? 2 : 3;      // terms of what is computed
+    w.chunks = (int)((p->L + kC - 1) / kC);
+    w.vblocks = (p->Dv + kC - 1) / kC;
+    w.segs = 1;
+    w.seg_chunks = w.chunks;
+    const size_t nc = (size_t)p->B * p->Hv * w.chunks, rows = (size_t)p->B * p->L;
+    if (w.terms == 3) {
+        w.q = part((double)rows * p->Hk * p->Dk * 6);
+        w.k = w.q;
+        w.v = part((double)rows * p->Hv * p->Dv * 6);
+        w.go = backward ? w.v : 0;
+    }
+    w.coef = part((double)nc * kCoef * kC * 4);
+    w.tri = part((double)nc * nt * kTile * 2);
+    w.p = w.tri;
+    if (backward) {
+        w.r = part((double)nc * w.vblocks * nt * kTile * 2);
+        w.s0 = part((double)nc * w.vblocks * nt * kC * w.dk * 2);
+    }
+    w.total = w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + 2 * (w.r + w.s0) + 2 * w.seg_state + w.seg_map;
+    return w;
+}
+
+// Chunk kernels number chunks of heads in one grid dimension.
+bool chunks_fit(const cawn_delta_params *p) { return (double)p->B * p->Hv * ((double)p->L / kC + 1.0) < 2147483647.0; }
+
+struct Carver {
+    char *at;
+    template <class T> T *take(size_t bytes)
+    {
+        T *p = reinterpret_cast<T *>(at);
+        at += bytes;
+        return p;
+    }
+};
+
+// One sequence array as bfloat16 terms: itself, or (float storage) split into the workspace.
+int terms_of(Terms &t, const void *src, long long stride, long long rows, long long L, int width, int terms, size_t bytes, Carver &ws, cudaStream_t st)
+{
+    if (terms == 1) {
+        t = {static_cast<const bf16 *>(src), 0, stride, stride * L};
+        return CAWN_OK;
+    }
+    bf16 *dst = ws.take<bf16>(bytes);
+    t = {dst, rows * width, width, (long long)width * L};
+    return status_of(launch_delta_split(static_cast<const float *>(src), dst, t.plane, rows, width, stride, st));
+}
+
+int chunk_params(ChunkParams &C, const cawn_delta_params *p, const DeltaParams &D, const Plan &w, Carver &ws, cudaStream_t st)
+{
+    C.g = D.g; C.beta = D.beta; C.state_in = D.state_in;
+    C.L = p->L; C.B = p->B; C.Hk = p->Hk; C.Hv = p->Hv; C.Dk = p->Dk; C.Dv = p->Dv; C.scale = p->scale;
+    C.chunks = w.chunks; C.vblocks = w.vblocks; C.segs = w.segs; C.seg_chunks = w.seg_chunks;
+    const long long rows = (long long)p->B * p->L;
+    int rc = terms_of(C.q, D.q, D.q_stride, rows, p->L, p->Hk * p->Dk, w.terms, w.q, ws, st);
+    if (rc == CAWN_OK) rc = terms_of(C.k, D.k, D.k_stride, rows, p->L, p->Hk * p->Dk, w.terms, w.k, ws, st);
+    if (rc == CAWN_OK) rc = terms_of(C.v, D.v, D.v_stride, rows, p->L, p->Hv * p->Dv, w.terms, w.v, ws, st);
+    C.coef = ws.take<float>(w.coef);
+    C.tri = ws.take<bf16>(w.tri);
+    C.p = ws.take<bf16>(w.p);
+    return rc;
+}
+
 }  // namespace
 }  // namespace cawn
+
 
 extern "C" int cawn_delta_rule_step(const cawn_delta_params *params, const void *q, const void *k, const void *v, const float *g,
                                     const float *beta, const float *state_in, void *o, float *state_out, void *cuda_stream)
@@ -71,7 +154,8 @@ extern "C" int cawn_delta_rule_workspace_bytes(const cawn_delta_params *params, 
     if (rc != CAWN_OK) return rc;
     if (op != CAWN_DELTA_FWD && op != CAWN_DELTA_BWD) return CAWN_ERR_INVALID_ARG;
     if (bytes == nullptr) return CAWN_ERR_NULL_POINTER;
-    *bytes = 0;
+    if (!chunks_fit(params)) return CAWN_ERR_UNSUPPORTED;
+    *bytes = plan_of(params, op == CAWN_DELTA_BWD).total;
     return CAWN_OK;
 }
 
@@ -79,8 +163,26 @@ extern "C" int cawn_delta_rule_fwd(const cawn_delta_params *params, const void *
                                    const float *beta, const float *state_in, void *o, float *state_out, void *workspace,
                                    size_t workspace_bytes, void *cuda_stream)
 {
-    (void)workspace; (void)workspace_bytes;
-    return cawn_delta_rule_step(params, q, k, v, g, beta, state_in, o, state_out, cuda_stream);
+    using namespace cawn;
+    int rc = check(params);
+    if (rc != CAWN_OK) return rc;
+    if (params->L <= kStepTokens) return cawn_delta_rule_step(params, q, k, v, g, beta, state_in, o, state_out, cuda_stream);
+    if (!chunks_fit(params)) return CAWN_ERR_UNSUPPORTED;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (q == nullptr || k == nullptr || v == nullptr || g == nullptr || beta == nullptr || o == nullptr || workspace == nullptr)
+        return CAWN_ERR_NULL_POINTER;
+    if (!all_aligned16(q, k, v, g, beta, state_in, o, state_out, workspace)) return CAWN_ERR_MISALIGNED;
+    const Plan w = plan_of(params, false);
+    if (workspace_bytes < w.total) return CAWN_ERR_WORKSPACE_TOO_SMALL;
+    const DeltaParams D = fill(params, q, k, v, g, beta, state_in);
+    ChunkParams C = {};
+    Carver ws = {static_cast<char *>(workspace)};
+    rc = chunk_params(C, params, D, w, ws, st);
+    if (rc != CAWN_OK) return rc;
+    C.o = o; C.state_out = state_out; C.o_stride_t = D.o_stride; C.o_stride_b = D.o_stride * params->L;
+    cudaError_t e = launch_delta_prep(C, w.dk, w.terms, st);
+    if (e == cudaSuccess) e = launch_delta_scan(C, w.dk, w.terms, false, st);
+    return status_of(e);
 }
 
 extern "C" int cawn_delta_rule_bwd(const cawn_delta_params *, const void *, const void *, const void *, const float *, const float *,

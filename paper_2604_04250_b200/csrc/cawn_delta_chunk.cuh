@@ -1,0 +1,197 @@
+// Gated delta rule, chunk form: matrix fragments, tiles and the workspace shared by its kernels.
+//
+// Mathematics of a chunk of 64 tokens (G = running sum of g inside the chunk, Gam_ij = e^{G_i - G_j},
+// S0 the state before it, states written [value, key]):
+//   At_ij = Gam_ij k_i.k_j (i > j)           T = (I + At diag(beta))^{-1}, unit lower triangular
+//   r = T (V - e^G K S0^T),  u = beta r       P_ij = scale Gam_ij q_i.k_j (i >= j)
+//   O = scale e^G Q S0^T + P u               S = e^{G_C} S0 + sum_j e^{G_C - G_j} u_j k_j^T
+//
+// Precision.  Products run on the tensor cores with bfloat16 factors and float sums; a float factor enters
+// as a sum of bfloat16 terms (8 mantissa bits each).  With bfloat16 storage inputs are exact as one term
+// and everything computed takes two (16 bits; measured error of the state 5e-6); with float storage
+// everything takes three, inputs by a pass of their own (two terms were at 8e-6, too near to what a user
+// of float expects).  NP: terms of inputs (1 or 3), NT: terms of computed factors (2 or 3).
+//
+// Layout.  Sequential kernels work on transposed chunks: a warp owns 16 rows of values v and all keys,
+// so that every product of the chain (state x keys, triangle, update) has the previous result as its
+// left factor.  The accumulator layout of mma.m16n8k16 is the layout of its left operand, so the chain
+// stays in registers, with no barrier and no shared-memory round trip between its products; the right
+// factors (K, Q, T, P tiles) are the same for all warps and come from shared memory.
+#pragma once
+#include "cawn_delta.cuh"
+
+namespace cawn {
+
+constexpr int kC = 64;                  // tokens of a chunk
+constexpr int kPad = 8;                 // bfloat16 of padding per shared row: ldmatrix reads 8 rows without conflicts
+constexpr int kTile = kC * kC;          // elements of a 64 x 64 tile in the workspace
+constexpr int kLd = kC + kPad;
+constexpr int kCoef = 5;                // floats per token: e^G, e^{G_C - G}, beta, G (high, low part)
+enum { COEF_EG = 0, COEF_LEFT = 1, COEF_BETA = 2, COEF_GHI = 3, COEF_GLO = 4 };
+
+// One input array as NP bfloat16 terms, `plane` elements apart; strides in elements.
+struct Terms {
+    const bf16 *at;
+    long long plane, stride_t, stride_b;
+};
+
+// Everything the chunk kernels share.  nc = bh * chunks + c numbers chunks of value heads; tiles and
+// coefficients of the workspace are dense over nc.
+struct ChunkParams {
+    Terms q, k, v, go;
+    const float *g, *beta;
+    float *coef;                        // [nc][kCoef][64]
+    bf16 *tri;                          // [nc][NT][64 j][64 i]: T transposed, blocks on and below T's diagonal
+    bf16 *p;                            // [nc][NT][64 i][64 j]: P, blocks on and below the diagonal
+    bf16 *r, *rb;                       // backward: [nc][vblocks][NT][64 t][64 v]
+    bf16 *s0, *ds;                      // backward: [nc][vblocks][NT][64 v][DK]
+    const float *state_in;              // [bh][Dv][Dk], may be NULL
+    float *state_out;
+    void *o;                            // forward output; backward: grad_v
+    void *gq, *gk;
+    float *gg, *gbeta;
+    long long L, o_stride_t, o_stride_b;
+    // time segments: start states per segment, local end states, transitions
+    float *seg_start, *seg_end, *seg_map;   // [bh][segs][Dv][Dk], same, [bh][segs][Dk][Dk]
+    int segs, seg_chunks;
+    int B, Hk, Hv, Dk, Dv, chunks, vblocks;
+    float scale;
+};
+
+__device__ __forceinline__ unsigned smem_addr(const void *p) { return (unsigned)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void cp16(unsigned dst, const void *src, bool ok)
+{
+    const int n = ok ? 16 : 0;          // 0 bytes read: the 16 bytes in shared memory become zero
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
+
+// ROWS x COLS tile into shared rows of COLS + kPad; rows and columns past the valid ones become zero.
+template <int ROWS, int COLS, int THREADS>
+__device__ __forceinline__ void load_tile(bf16 *dst, const bf16 *src, long long stride, int rows, int cols)
+{
+    const unsigned base = smem_addr(dst);
+#pragma unroll
+    for (int i = threadIdx.x; i < ROWS * (COLS / 8); i += THREADS) {
+        const int r = i / (COLS / 8), c = i % (COLS / 8) * 8;
+        const bool ok = r < rows && c < cols;
+        cp16(base + (r * (COLS + kPad) + c) * 2, ok ? src + r * stride + c : src, ok);
+    }
+}
+
+__device__ __forceinline__ void ldsm(unsigned (&r)[4], unsigned addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm_t(unsigned (&r)[4], unsigned addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void stsm_t(unsigned addr, unsigned a, unsigned b, unsigned c, unsigned d)
+{
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};"
+                 :: "r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void mma(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// This lane's row address inside a 16 x 16 block at (row, col) of a tile with rows of `ld` elements.
+// NK: rows are the n index of a right factor (or the k index of a transposed left one), KN: rows are the
+// k index of a right factor read transposed, or the m index of a left factor.
+__device__ __forceinline__ unsigned at_nk(unsigned base, int ld, int row, int col)
+{
+    const int l = threadIdx.x % 32;
+    return base + ((row + l % 8 + l / 16 * 8) * ld + col + l / 8 % 2 * 8) * 2;
+}
+__device__ __forceinline__ unsigned at_kn(unsigned base, int ld, int row, int col)
+{
+    const int l = threadIdx.x % 32;
+    return base + ((row + l % 8 + l / 8 % 2 * 8) * ld + col + l / 16 * 8) * 2;
+}
+
+// x, y as N bfloat16 terms of falling size, packed; N = 1 rounds
+template <int N> __device__ __forceinline__ void split(float x, float y, unsigned (&w)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        w[i] = pack_bf16(x, y);
+        x -= __uint_as_float(w[i] << 16);
+        y -= __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ float2 unpack(unsigned w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+
+// Accumulators of two neighbouring 16 x 8 tiles as N terms of the left operand of the next product.
+template <int N> __device__ __forceinline__ void as_left(const float (&c0)[4], const float (&c1)[4], unsigned (&a)[N][4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        unsigned w[N];
+        split(e < 2 ? c0[2 * e] : c1[2 * e - 4], e < 2 ? c0[2 * e + 1] : c1[2 * e - 3], w);
+#pragma unroll
+        for (int i = 0; i < N; i++) a[i][e] = w[i];
+    }
+}
+
+// The first N terms
+template <int N, int M> __device__ __forceinline__ const unsigned (&leading(const unsigned (&a)[M][4]))[N][4]
+{
+    static_assert(N <= M, "no more terms than there are");
+    return reinterpret_cast<const unsigned (&)[N][4]>(a);
+}
+
+// Left operand of AP terms from shared planes `plane` elements apart (TRANS: stored [k][m], at_nk; else at_kn).
+template <int AP, bool TRANS> __device__ __forceinline__ void load_left(unsigned (&a)[AP][4], unsigned addr, int plane)
+{
+#pragma unroll
+    for (int i = 0; i < AP; i++)
+        if (TRANS) ldsm_t(a[i], addr + i * plane * 2); else ldsm(a[i], addr + i * plane * 2);
+}
+
+// Two 16 x 8 tiles += left (AP terms) x right (BP terms in shared planes `plane` elements apart); TRANS as
+// ldsm_t.  Pairs of terms beyond the precision of the longer operand are left out: 2 x 2 terms take three
+// products, 3 x 3 six.
+template <int AP, int BP, bool TRANS>
+__device__ __forceinline__ void product(float (&c0)[4], float (&c1)[4], const unsigned (&a)[AP][4], unsigned addr, int plane)
+{
+    constexpr int ORDER = AP > BP ? AP : BP;
+#pragma unroll
+    for (int j = 0; j < BP; j++) {
+        unsigned b[4];
+        if (TRANS) ldsm_t(b, addr + j * plane * 2); else ldsm(b, addr + j * plane * 2);
+#pragma unroll
+        for (int i = 0; i < AP; i++)
+            if (i + j < ORDER) {
+                mma(c0, a[i], b[0], b[1]);
+                mma(c1, a[i], b[2], b[3]);
+            }
+    }
+}
+
+// Value head's place
+__device__ __forceinline__ long long q_base(const ChunkParams &P, const Terms &t, int bh, long long t0)
+{
+    return (bh / P.Hv) * t.stride_b + t0 * t.stride_t + (long long)(bh % P.Hv / (P.Hv / P.Hk)) * P.Dk;
+}
+__device__ __forceinline__ long long v_base(const ChunkParams &P, const Terms &t, int bh, long long t0)
+{
+    return (bh / P.Hv) * t.stride_b + t0 * t.stride_t + (long long)(bh % P.Hv) * P.Dv;
+}
+
+// terms: NP
+cudaError_t launch_delta_split(const float *src, bf16 *dst, long long plane, long long rows, int width, long long stride, cudaStream_t st);
+cudaError_t launch_delta_prep(const ChunkParams &P, int dk, int terms, cudaStream_t st);
+// forward over the chunks: outputs (or, for the backward, what it needs to keep: `save`)
+cudaError_t launch_delta_scan(const ChunkParams &P, int dk, int terms, bool save, cudaStream_t st);
+cudaError_t launch_delta_reverse(const ChunkParams &P, int dk, int terms, cudaStream_t st);
+cudaError_t launch_delta_grads(const ChunkParams &P, int dk, int terms, cudaStream_t st);
+
+}  // namespace cawn

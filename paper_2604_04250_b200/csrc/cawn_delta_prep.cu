@@ -1,0 +1,213 @@
+// Gated delta rule, chunk form: what a chunk needs that does not depend on the state.  All chunks of all
+// heads at once: decays, the scores P, and the inverse T of the chunk's triangle.
+//
+// The inverse: 16 x 16 blocks on the diagonal by substitution in float (a lane per column), the blocks
+// below from T_IJ = -T_II sum_K A_IK T_KJ on the tensor cores, a block column per warp with the
+// intermediate blocks in registers.  Substitution is stable for every triangle whose inverse is moderate;
+// a power series of A is not (equal keys give binomial coefficients).
+#include "cawn_delta_chunk.cuh"
+
+namespace cawn {
+namespace {
+
+template <int DK, int NP> struct PrepSmem {
+    static constexpr int NT = NP == 1 ? 2 : 3;
+    bf16 q[NP][kC * (DK + kPad)], k[NP][kC * (DK + kPad)];
+    bf16 a[NT][kC * kLd];               // A = At diag(beta), terms
+    bf16 d[NT][4][16 * 24];             // inverses of the diagonal blocks, terms
+    float diag[4][16][20];              // diagonal blocks of A
+    float ghi[kC], glo[kC], beta[kC];
+};
+
+template <int DK, int NP>
+__global__ void __launch_bounds__(128) delta_prep_kernel(const ChunkParams P)
+{
+    extern __shared__ __align__(16) unsigned char raw[];
+    auto &sm = *reinterpret_cast<PrepSmem<DK, NP> *>(raw);
+    constexpr int ld = DK + kPad, NT = NP == 1 ? 2 : 3;
+    const long long nc = blockIdx.x;
+    const int bh = (int)(nc / P.chunks), c = (int)(nc % P.chunks);
+    const long long t0 = (long long)c * kC;
+    const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
+    const int lane = threadIdx.x % 32, w = threadIdx.x / 32, gr = lane / 4, tc = lane % 4 * 2;
+
+#pragma unroll
+    for (int i = 0; i < NP; i++) {
+        load_tile<kC, DK, 128>(sm.k[i], P.k.at + i * P.k.plane + q_base(P, P.k, bh, t0), P.k.stride_t, rows, P.Dk);
+        load_tile<kC, DK, 128>(sm.q[i], P.q.at + i * P.q.plane + q_base(P, P.q, bh, t0), P.q.stride_t, rows, P.Dk);
+    }
+    cp_commit();
+
+    if (w == 0) {
+        // Running sum in double: differences G_i - G_j of strong decays keep their accuracy.  Below
+        // -200 every decay is zero in float, and so is every product with one: the clamp changes no
+        // result and keeps -infinity out of the differences.
+        const long long at = ((long long)(bh / P.Hv) * P.L + t0) * P.Hv + bh % P.Hv;
+        double sum[2];
+        float bt[2];
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            const int t = lane * 2 + e;
+            const float g = t < rows ? P.g[at + (long long)t * P.Hv] : 0.f;
+            bt[e] = t < rows ? P.beta[at + (long long)t * P.Hv] : 0.f;
+            sum[e] = g < -200.f ? -200.0 : (double)g;
+        }
+        sum[1] += sum[0];
+        double run = sum[1];
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const double other = __shfl_up_sync(0xffffffffu, run, o);
+            if (lane >= o) run += other;
+        }
+        const double before = run - sum[1];
+        sum[0] += before;
+        sum[1] += before;
+        const double last = __shfl_sync(0xffffffffu, sum[1], 31);
+        float *coef = P.coef + nc * (kCoef * kC);
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            const int t = lane * 2 + e;
+            const float hi = (float)sum[e], lo = (float)(sum[e] - (double)hi);
+            sm.ghi[t] = hi; sm.glo[t] = lo; sm.beta[t] = bt[e];
+            coef[COEF_EG * kC + t] = expf(hi) * (1.f + lo);
+            coef[COEF_LEFT * kC + t] = expf((float)(last - sum[e]));
+            coef[COEF_BETA * kC + t] = bt[e];
+            coef[COEF_GHI * kC + t] = hi;
+            coef[COEF_GLO * kC + t] = lo;
+        }
+    }
+    cp_wait<0>();
+    __syncthreads();
+
+    // 16 rows i per warp, blocks j <= i
+    float kk[8][4] = {}, qk[8][4] = {};
+    const unsigned ks = smem_addr(sm.k[0]), qs = smem_addr(sm.q[0]);
+#pragma unroll
+    for (int d = 0; d < DK; d += 16) {
+        unsigned ka[NP][4], qa[NP][4];
+        load_left<NP, false>(ka, at_kn(ks, ld, 16 * w, d), kC * ld);
+        load_left<NP, false>(qa, at_kn(qs, ld, 16 * w, d), kC * ld);
+#pragma unroll
+        for (int nb = 0; nb < 4; nb++)
+            if (nb <= w) {
+                product<NP, NP, false>(kk[2 * nb], kk[2 * nb + 1], ka, at_nk(ks, ld, 16 * nb, d), kC * ld);
+                product<NP, NP, false>(qk[2 * nb], qk[2 * nb + 1], qa, at_nk(ks, ld, 16 * nb, d), kC * ld);
+            }
+    }
+    bf16 *pt = P.p + nc * NT * kTile;
+#pragma unroll
+    for (int n = 0; n < 8; n++) {
+        if (n / 2 > w) continue;
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+            const int i = 16 * w + gr + 8 * half, j = 8 * n + tc;
+            float a[2], p[2];
+#pragma unroll
+            for (int e = 0; e < 2; e++) {
+                const bool low = i >= j + e;
+                const float gam = low ? expf((sm.ghi[i] - sm.ghi[j + e]) + (sm.glo[i] - sm.glo[j + e])) : 0.f;
+                p[e] = low ? P.scale * gam * qk[n][2 * half + e] : 0.f;
+                a[e] = i > j + e ? gam * kk[n][2 * half + e] * sm.beta[j + e] : 0.f;
+            }
+            unsigned pw[NT], aw[NT];
+            split(p[0], p[1], pw);
+            split(a[0], a[1], aw);
+#pragma unroll
+            for (int m = 0; m < NT; m++) {
+                *reinterpret_cast<unsigned *>(pt + m * kTile + i * kC + j) = pw[m];
+                *reinterpret_cast<unsigned *>(&sm.a[m][i * kLd + j]) = aw[m];
+            }
+            if (n / 2 == w) *reinterpret_cast<float2 *>(&sm.diag[w][i - 16 * w][j - 16 * w]) = make_float2(a[0], a[1]);
+        }
+    }
+    __syncwarp();
+    // inverse of this warp's diagonal block, lane = column
+    if (lane < 16) {
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            float s = i == lane ? 1.f : 0.f;
+#pragma unroll
+            for (int l = 0; l < i; l++) s = fmaf(-sm.diag[w][i][l], x[l], s);
+            x[i] = s;
+            float rest = s;
+#pragma unroll
+            for (int m = 0; m < NT; m++) {
+                const bf16 term = __float2bfloat16_rn(rest);
+                sm.d[m][w][i * 24 + lane] = term;
+                rest -= __bfloat162float(term);
+            }
+        }
+    }
+    __syncthreads();
+
+    // block column J = w: left operands hold T_KJ transposed
+    bf16 *tri = P.tri + nc * NT * kTile;
+    const unsigned as = smem_addr(sm.a[0]), dsm = smem_addr(sm.d[0][0]);
+    unsigned tw[4][NT][4];
+    load_left<NT, true>(tw[0], at_nk(dsm + w * 16 * 24 * 2, 24, 0, 0), 4 * 16 * 24);
+#pragma unroll
+    for (int step = 0; step < 4; step++) {
+        const int I = w + step;
+        if (I >= 4) break;
+        if (step > 0) {
+            float y[2][4] = {}, z[2][4] = {};
+#pragma unroll
+            for (int m = 0; m < step; m++)
+                product<NT, NT, false>(y[0], y[1], tw[m], at_nk(as, kLd, 16 * I, 16 * (w + m)), kC * kLd);
+            unsigned yw[NT][4];
+            as_left(y[0], y[1], yw);
+            product<NT, NT, false>(z[0], z[1], yw, at_nk(dsm + I * 16 * 24 * 2, 24, 0, 0), 4 * 16 * 24);
+#pragma unroll
+            for (int e = 0; e < 4; e++) { z[0][e] = -z[0][e]; z[1][e] = -z[1][e]; }
+            as_left(z[0], z[1], tw[step]);
+        }
+        // rows j = 16 w + (gr, gr + 8), columns i = 16 I + tc (+8)
+        bf16 *dst = tri + (16 * w + gr) * kC + 16 * I + tc;
+#pragma unroll
+        for (int m = 0; m < NT; m++)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                *reinterpret_cast<unsigned *>(dst + m * kTile + (e & 1) * 8 * kC + (e >> 1) * 8) = tw[step][m][e];
+    }
+}
+
+// float array -> three bfloat16 terms, dense rows of `width` (a multiple of 8) elements
+__global__ void __launch_bounds__(256) delta_split_kernel(const float *src, bf16 *dst, long long plane, long long words, int width8, long long stride)
+{
+    const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= words) return;
+    const long long row = i / width8;
+    const int col = (int)(i - row * width8) * 8;
+    float f[8];
+    load_vec(f, src + row * stride + col);
+    unsigned w[4][3];
+#pragma unroll
+    for (int e = 0; e < 4; e++) split(f[2 * e], f[2 * e + 1], w[e]);
+#pragma unroll
+    for (int m = 0; m < 3; m++) *reinterpret_cast<uint4 *>(dst + m * plane + i * 8) = make_uint4(w[0][m], w[1][m], w[2][m], w[3][m]);
+}
+
+template <int DK, int NP> cudaError_t prep(const ChunkParams &P, cudaStream_t st)
+{
+    const size_t smem = sizeof(PrepSmem<DK, NP>);
+    const cudaError_t e = cudaFuncSetAttribute(delta_prep_kernel<DK, NP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    return launch(delta_prep_kernel<DK, NP>, dim3((unsigned)(P.B * P.Hv * (long long)P.chunks)), dim3(128), smem, st, P);
+}
+
+}  // namespace
+
+cudaError_t launch_delta_prep(const ChunkParams &P, int dk, int terms, cudaStream_t st)
+{
+    if (dk == 64) return terms == 1 ? prep<64, 1>(P, st) : prep<64, 3>(P, st);
+    return terms == 1 ? prep<128, 1>(P, st) : prep<128, 3>(P, st);
+}
+
+cudaError_t launch_delta_split(const float *src, bf16 *dst, long long plane, long long rows, int width, long long stride, cudaStream_t st)
+{
+    const long long words = rows * (width / 8);
+    return launch(delta_split_kernel, dim3((unsigned)((words + 255) / 256)), dim3(256), 0, st, src, dst, plane, words, width / 8, stride);
+}
+
+}  // namespace cawn

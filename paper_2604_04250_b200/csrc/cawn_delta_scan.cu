@@ -1,0 +1,289 @@
+// Gated delta rule, chunk form: the walk over a head's chunks.
+//
+// Per chunk and warp (16 value rows, transposed products; see cawn_delta_chunk.cuh):
+//   X = S K^T,  R = V^T - e^G X,  r = R T^T,  u = beta r,  O = scale e^G S Q^T + u P^T,
+//   S <- e^{G_C} S + (e^{G_C - G} u) K
+// Bound: the chain of these products, chunk after chunk.  It needs no barrier but the one per chunk that
+// hands over the next tiles, which cp.async brings in while the current chunk is computed.
+//
+// Few heads leave SMs idle while the chain is long, so the time axis is cut into segments: a chunk acts on
+// a state row s as s <- s M + l, so a first pass computes each segment's M (the same walk over the rows
+// of the identity with V = 0) and l (from a zero state); a small kernel chains them to every segment's
+// start state, and the output pass runs all segments side by side.
+#include "cawn_delta_chunk.cuh"
+
+#include <type_traits>
+
+namespace cawn {
+namespace {
+
+enum { MODE_OUT, MODE_SAVE, MODE_SUMMARY };
+
+template <int DK, int NP, int MODE> struct ScanStage {
+    bf16 k[NP][kC * (DK + kPad)];
+    bf16 q[MODE == MODE_OUT ? NP : 0][kC * (DK + kPad)];
+    bf16 tri[NP == 1 ? 2 : 3][kC * kLd];
+    bf16 p[MODE == MODE_OUT ? NP : 0][kC * kLd];
+    bf16 v[NP][kC * kLd];
+    float coef[3][kC];
+};
+// two where they fit, so that the next chunk's tiles arrive during the current one
+template <int DK, int NP, int MODE> constexpr int kScanStages = sizeof(ScanStage<DK, NP, MODE>) * 2 <= 227 * 1024 ? 2 : 1;
+
+template <int DK, int NP, int MODE>
+__device__ __forceinline__ void scan_load(const ChunkParams &P, ScanStage<DK, NP, MODE> &st, int bh, int c, int vb, int vcols)
+{
+    constexpr int NT = NP == 1 ? 2 : 3;
+    const long long t0 = (long long)c * kC, nc = (long long)bh * P.chunks + c;
+    const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
+#pragma unroll
+    for (int i = 0; i < NP; i++) {
+        load_tile<kC, DK, 128>(st.k[i], P.k.at + i * P.k.plane + q_base(P, P.k, bh, t0), P.k.stride_t, rows, P.Dk);
+        load_tile<kC, kC, 128>(st.v[i], P.v.at + i * P.v.plane + (vcols > 0 ? v_base(P, P.v, bh, t0) + vb * kC : 0), P.v.stride_t, rows, vcols);
+        if constexpr (MODE == MODE_OUT) {
+            load_tile<kC, DK, 128>(st.q[i], P.q.at + i * P.q.plane + q_base(P, P.q, bh, t0), P.q.stride_t, rows, P.Dk);
+            load_tile<kC, kC, 128>(st.p[i], P.p + (nc * NT + i) * kTile, kC, kC, kC);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NT; i++) load_tile<kC, kC, 128>(st.tri[i], P.tri + (nc * NT + i) * kTile, kC, kC, kC);
+    if (threadIdx.x < 48)
+        cp16(smem_addr(&st.coef[0][0]) + threadIdx.x * 16, P.coef + nc * (kCoef * kC) + threadIdx.x * 4, true);
+    cp_commit();
+}
+
+template <int DK, int NP, int MODE, class T>
+__global__ void __launch_bounds__(128) delta_scan_kernel(const ChunkParams P)
+{
+    constexpr int STAGES = kScanStages<DK, NP, MODE>, ld = DK + kPad, NT = NP == 1 ? 2 : 3;
+    extern __shared__ __align__(16) unsigned char raw[];
+    auto *stages = reinterpret_cast<ScanStage<DK, NP, MODE> *>(raw);
+    const int bh = blockIdx.x, vb = blockIdx.y, seg = blockIdx.z;
+    const int lane = threadIdx.x % 32, w = threadIdx.x / 32, gr = lane / 4, tc = lane % 4 * 2;
+    const bool ident = MODE == MODE_SUMMARY && vb >= P.vblocks;     // rows of the identity instead of values
+    const int r0 = (ident ? vb - P.vblocks : vb) * kC;              // first value (or identity) row of the block
+    const int vcols = ident ? 0 : (P.Dv - r0 < kC ? P.Dv - r0 : kC);
+    const int rlim = ident ? P.Dk : P.Dv;                           // rows that exist
+    const int row[2] = {r0 + 16 * w + gr, r0 + 16 * w + gr + 8};
+    const int c0 = seg * P.seg_chunks, c1 = c0 + P.seg_chunks < P.chunks ? c0 + P.seg_chunks : P.chunks;
+
+    scan_load<DK, NP, MODE>(P, stages[0], bh, c0, vb, vcols);
+
+    // state rows row[0], row[1]; columns 8 n + tc, +1 of tile n
+    float S[DK / 8][4];
+    const float *from = nullptr;
+    if (MODE != MODE_SUMMARY)
+        from = P.segs > 1 ? P.seg_start + ((long long)bh * P.segs + seg) * P.Dv * P.Dk
+                          : (P.state_in != nullptr ? P.state_in + (long long)bh * P.Dv * P.Dk : nullptr);
+#pragma unroll
+    for (int n = 0; n < DK / 8; n++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            float2 x = make_float2(0.f, 0.f);
+            const int col = 8 * n + tc;
+            if (ident) x = make_float2(row[h] == col ? 1.f : 0.f, row[h] == col + 1 ? 1.f : 0.f);
+            else if (from != nullptr && row[h] < P.Dv && col < P.Dk) x = *reinterpret_cast<const float2 *>(from + (long long)row[h] * P.Dk + col);
+            S[n][2 * h] = x.x;
+            S[n][2 * h + 1] = x.y;
+        }
+
+    for (int c = c0; c < c1; c++) {
+        auto &st = stages[(c - c0) % STAGES];
+        if (STAGES == 2 && c + 1 < c1) {
+            scan_load<DK, NP, MODE>(P, stages[(c - c0 + 1) % STAGES], bh, c + 1, vb, vcols);
+            cp_wait<1>();
+        } else {
+            cp_wait<0>();
+        }
+        __syncthreads();
+        const long long t0 = (long long)c * kC, nc = (long long)bh * P.chunks + c;
+        const unsigned ks = smem_addr(st.k[0]), ts = smem_addr(st.tri[0]), vs = smem_addr(st.v[0]);
+
+        if (MODE == MODE_SAVE) {
+            bf16 *dst = P.s0 + (nc * P.vblocks + vb) * (NT * kC * DK);
+#pragma unroll
+            for (int n = 0; n < DK / 8; n++)
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    unsigned x[NT];
+                    split(S[n][2 * h], S[n][2 * h + 1], x);
+#pragma unroll
+                    for (int i = 0; i < NT; i++)
+                        *reinterpret_cast<unsigned *>(dst + i * (kC * DK) + (row[h] - r0) * DK + 8 * n + tc) = x[i];
+                }
+        }
+        // X = S K^T, Y = S Q^T
+        float X[8][4] = {}, Y[MODE == MODE_OUT ? 8 : 1][4] = {};
+#pragma unroll
+        for (int d = 0; d < DK / 16; d++) {
+            unsigned s[NT][4];
+            as_left(S[2 * d], S[2 * d + 1], s);
+#pragma unroll
+            for (int nb = 0; nb < 4; nb++) {
+                product<NT, NP, false>(X[2 * nb], X[2 * nb + 1], s, at_nk(ks, ld, 16 * nb, 16 * d), kC * ld);
+                if constexpr (MODE == MODE_OUT)     // bfloat16 results: one term of the state is enough
+                    product<NP, NP, false>(Y[2 * nb], Y[2 * nb + 1], leading<NP>(s), at_nk(smem_addr(st.q[0]), ld, 16 * nb, 16 * d), kC * ld);
+            }
+        }
+        // R = V^T - e^G X; the read-out's first part gets its factor
+#pragma unroll
+        for (int nb = 0; nb < 4; nb++) {
+            unsigned vf[NP][4];
+            if (vcols > 0) load_left<NP, true>(vf, at_nk(vs, kLd, 16 * nb, 16 * w), kC * kLd);
+#pragma unroll
+            for (int m = 0; m < 2; m++) {
+                const int n = 2 * nb + m;
+                const float2 eg = *reinterpret_cast<const float2 *>(&st.coef[COEF_EG][8 * n + tc]);
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    float2 x = make_float2(0.f, 0.f);
+                    if (vcols > 0) {
+#pragma unroll
+                        for (int i = NP - 1; i >= 0; i--) {
+                            const float2 y = unpack(vf[i][2 * m + h]);
+                            x.x += y.x;
+                            x.y += y.y;
+                        }
+                    }
+                    X[n][2 * h] = fmaf(-eg.x, X[n][2 * h], x.x);
+                    X[n][2 * h + 1] = fmaf(-eg.y, X[n][2 * h + 1], x.y);
+                    if (MODE == MODE_OUT) {
+                        Y[n][2 * h] *= P.scale * eg.x;
+                        Y[n][2 * h + 1] *= P.scale * eg.y;
+                    }
+                }
+            }
+        }
+        // r = R T^T: tokens t of the result from block t' on
+        float r[8][4] = {};
+#pragma unroll
+        for (int tb = 0; tb < 4; tb++) {
+            unsigned x[NT][4];
+            as_left(X[2 * tb], X[2 * tb + 1], x);
+#pragma unroll
+            for (int nb = tb; nb < 4; nb++)
+                product<NT, NT, true>(r[2 * nb], r[2 * nb + 1], x, at_kn(ts, kLd, 16 * tb, 16 * nb), kC * kLd);
+        }
+        if (MODE == MODE_SAVE) {
+            // r, token rows of 64 values: transposed through this warp's own columns of the V tile
+            bf16 *dst = P.r + (nc * P.vblocks + vb) * (NT * kTile);
+#pragma unroll
+            for (int term = 0; term < NT; term++) {
+                __syncwarp();
+#pragma unroll
+                for (int nb = 0; nb < 4; nb++) {
+                    unsigned x[NT][4];
+                    as_left(r[2 * nb], r[2 * nb + 1], x);
+                    stsm_t(at_nk(vs, kLd, 16 * nb, 16 * w), x[term][0], x[term][1], x[term][2], x[term][3]);
+                }
+                __syncwarp();
+#pragma unroll
+                for (int i = lane; i < 128; i += 32)
+                    *reinterpret_cast<uint4 *>(dst + term * kTile + i / 2 * kC + 16 * w + i % 2 * 8) =
+                        *reinterpret_cast<const uint4 *>(&st.v[0][i / 2 * kLd + 16 * w + i % 2 * 8]);
+            }
+        }
+        // u = beta r
+#pragma unroll
+        for (int n = 0; n < 8; n++) {
+            const float2 bt = *reinterpret_cast<const float2 *>(&st.coef[COEF_BETA][8 * n + tc]);
+            r[n][0] *= bt.x; r[n][1] *= bt.y; r[n][2] *= bt.x; r[n][3] *= bt.y;
+        }
+        if constexpr (MODE == MODE_OUT) {
+            const unsigned ps = smem_addr(st.p[0]);
+#pragma unroll
+            for (int tb = 0; tb < 4; tb++) {
+                unsigned u[NP][4];
+                as_left(r[2 * tb], r[2 * tb + 1], u);
+#pragma unroll
+                for (int nb = tb; nb < 4; nb++)
+                    product<NP, NP, false>(Y[2 * nb], Y[2 * nb + 1], u, at_nk(ps, kLd, 16 * nb, 16 * tb), kC * kLd);
+            }
+            T *o = static_cast<T *>(P.o) + (bh / P.Hv) * P.o_stride_b + t0 * P.o_stride_t + (long long)(bh % P.Hv) * P.Dv + r0;
+            const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
+            if constexpr (sizeof(T) == 2) {
+                __syncwarp();
+#pragma unroll
+                for (int nb = 0; nb < 4; nb++)
+                    stsm_t(at_nk(vs, kLd, 16 * nb, 16 * w), pack_bf16(Y[2 * nb][0], Y[2 * nb][1]), pack_bf16(Y[2 * nb][2], Y[2 * nb][3]),
+                           pack_bf16(Y[2 * nb + 1][0], Y[2 * nb + 1][1]), pack_bf16(Y[2 * nb + 1][2], Y[2 * nb + 1][3]));
+                __syncwarp();
+#pragma unroll
+                for (int i = lane; i < 128; i += 32) {
+                    const int t = i / 2, v = 16 * w + i % 2 * 8;
+                    if (t < rows && v < vcols)
+                        *reinterpret_cast<uint4 *>(o + t * P.o_stride_t + v) = *reinterpret_cast<const uint4 *>(&st.v[0][t * kLd + v]);
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < 8; n++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const int t = 8 * n + tc + (e & 1), v = 16 * w + gr + (e >> 1) * 8;
+                        if (t < rows && v < vcols) o[t * P.o_stride_t + v] = narrow<T>(Y[n][e]);
+                    }
+            }
+        }
+        // S <- e^{G_C} S + (e^{G_C - G} u) K
+        const float eC = st.coef[COEF_EG][kC - 1];
+#pragma unroll
+        for (int n = 0; n < DK / 8; n++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) S[n][e] *= eC;
+#pragma unroll
+        for (int tb = 0; tb < 4; tb++) {
+#pragma unroll
+            for (int m = 0; m < 2; m++) {
+                const float2 lf = *reinterpret_cast<const float2 *>(&st.coef[COEF_LEFT][16 * tb + 8 * m + tc]);
+                float (&x)[4] = r[2 * tb + m];
+                x[0] *= lf.x; x[1] *= lf.y; x[2] *= lf.x; x[3] *= lf.y;
+            }
+            unsigned u[NT][4];
+            as_left(r[2 * tb], r[2 * tb + 1], u);
+#pragma unroll
+            for (int nb = 0; nb < DK / 16; nb++)
+                product<NT, NP, true>(S[2 * nb], S[2 * nb + 1], u, at_kn(ks, ld, 16 * tb, 16 * nb), kC * ld);
+        }
+        __syncthreads();        // the tiles are free
+        if (STAGES == 1 && c + 1 < c1) scan_load<DK, NP, MODE>(P, stages[0], bh, c + 1, vb, vcols);
+    }
+
+    float *to = nullptr;
+    if (MODE == MODE_SUMMARY)
+        to = ident ? P.seg_map + ((long long)bh * P.segs + seg) * P.Dk * P.Dk : P.seg_end + ((long long)bh * P.segs + seg) * P.Dv * P.Dk;
+    else if (P.state_out != nullptr && seg == P.segs - 1)
+        to = P.state_out + (long long)bh * P.Dv * P.Dk;
+    if (to != nullptr) {
+#pragma unroll
+        for (int n = 0; n < DK / 8; n++)
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+                if (row[h] < rlim && 8 * n + tc < P.Dk)
+                    *reinterpret_cast<float2 *>(to + (long long)row[h] * P.Dk + 8 * n + tc) = make_float2(S[n][2 * h], S[n][2 * h + 1]);
+    }
+}
+
+template <int DK, int NP, int MODE> cudaError_t scan(const ChunkParams &P, int row_blocks, int segs, cudaStream_t st)
+{
+    using T = typename std::conditional<NP == 1, bf16, float>::type;
+    const size_t smem = sizeof(ScanStage<DK, NP, MODE>) * kScanStages<DK, NP, MODE>;
+    auto *kernel = delta_scan_kernel<DK, NP, MODE, T>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    return launch(kernel, dim3((unsigned)(P.B * P.Hv), row_blocks, segs), dim3(128), smem, st, P);
+}
+
+template <int DK, int NP> cudaError_t run(const ChunkParams &P, bool save, cudaStream_t st)
+{
+    return save ? scan<DK, NP, MODE_SAVE>(P, P.vblocks, P.segs, st) : scan<DK, NP, MODE_OUT>(P, P.vblocks, P.segs, st);
+}
+
+}  // namespace
+
+cudaError_t launch_delta_scan(const ChunkParams &P, int dk, int terms, bool save, cudaStream_t st)
+{
+    if (dk == 64) return terms == 1 ? run<64, 1>(P, save, st) : run<64, 3>(P, save, st);
+    return terms == 1 ? run<128, 1>(P, save, st) : run<128, 3>(P, save, st);
+}
+
+}  // namespace cawn
