@@ -311,7 +311,7 @@ def cawn_mixing_bwd(params, h, conv_w, gamma, theta, grad_y, grad_h, workspace, 
 
 def make_delta_params(B, L, Hk, Hv, Dk, Dv, scale=None, flags=0, q_stride=0, k_stride=0, v_stride=0, o_stride=0):
     return cawn_delta_params(ctypes.sizeof(cawn_delta_params), B, L, Hk, Hv, Dk, Dv,
-                             Dk ** -0.5 if scale is None else scale, flags, q_stride, k_stride, v_stride, o_stride)
+                             max(Dk, 1) ** -0.5 if scale is None else scale, flags, q_stride, k_stride, v_stride, o_stride)
 
 
 def cawn_delta_rule_workspace_bytes(params, op):

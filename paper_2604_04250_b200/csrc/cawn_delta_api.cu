@@ -53,7 +53,7 @@ constexpr int kStepTokens = 16;
 struct Plan {
     int dk, terms, chunks, vblocks, segs, seg_chunks;    // terms: of an input
     size_t q, k, v, go;                  // three bfloat16 terms each, float storage only
-    size_t coef, tri, p, r, s0;
+    size_t coef, tri, p, r, rb, s0, dots;
     size_t seg_state, seg_map;
     size_t total;
 };
@@ -81,10 +81,12 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
     w.tri = part((double)nc * nt * kTile * 2);
     w.p = w.tri;
     if (backward) {
-        w.r = part((double)nc * w.vblocks * nt * kTile * 2);
+        w.r = part((double)nc * w.vblocks * 3 * kTile * 2);
+        w.rb = part((double)nc * w.vblocks * nt * kTile * 2);
         w.s0 = part((double)nc * w.vblocks * nt * kC * w.dk * 2);
     }
-    w.total = w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + 2 * (w.r + w.s0) + 2 * w.seg_state + w.seg_map;
+    if (backward) w.dots = part((double)nc * w.vblocks * 4 * 2 * kC * 4);
+    w.total = w.dots + w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + w.r + w.rb + 2 * w.s0 + 2 * w.seg_state + w.seg_map;
     return w;
 }
 
@@ -185,9 +187,47 @@ extern "C" int cawn_delta_rule_fwd(const cawn_delta_params *params, const void *
     return status_of(e);
 }
 
-extern "C" int cawn_delta_rule_bwd(const cawn_delta_params *, const void *, const void *, const void *, const float *, const float *,
-                                   const float *, const void *, const float *, void *, void *, void *, float *, float *, float *,
-                                   void *, size_t, void *)
+extern "C" int cawn_delta_rule_bwd(const cawn_delta_params *params, const void *q, const void *k, const void *v, const float *g,
+                                   const float *beta, const float *state_in, const void *grad_o, const float *grad_state_out,
+                                   void *grad_q, void *grad_k, void *grad_v, float *grad_g, float *grad_beta, float *grad_state_in,
+                                   void *workspace, size_t workspace_bytes, void *cuda_stream)
 {
-    return CAWN_ERR_UNSUPPORTED;
+    using namespace cawn;
+    int rc = check(params);
+    if (rc != CAWN_OK) return rc;
+    if (!chunks_fit(params)) return CAWN_ERR_UNSUPPORTED;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (!all_aligned16(q, k, v, g, beta, state_in, grad_o, grad_state_out, grad_q, grad_k, grad_v, grad_g, grad_beta, grad_state_in, workspace))
+        return CAWN_ERR_MISALIGNED;
+    if (params->L == 0) return pass_state(params, grad_state_out, grad_state_in, st);
+    if (q == nullptr || k == nullptr || v == nullptr || g == nullptr || beta == nullptr || grad_o == nullptr || grad_q == nullptr ||
+        grad_k == nullptr || grad_v == nullptr || grad_g == nullptr || grad_beta == nullptr || workspace == nullptr)
+        return CAWN_ERR_NULL_POINTER;
+    const Plan w = plan_of(params, true);
+    if (workspace_bytes < w.total) return CAWN_ERR_WORKSPACE_TOO_SMALL;
+    const DeltaParams D = fill(params, q, k, v, g, beta, state_in);
+    ChunkParams C = {};
+    Carver ws = {static_cast<char *>(workspace)};
+    rc = chunk_params(C, params, D, w, ws, st);
+    if (rc == CAWN_OK)
+        rc = terms_of(C.go, grad_o, D.o_stride, (long long)params->B * params->L, params->L, params->Hv * params->Dv, w.terms, w.go, ws, st);
+    if (rc != CAWN_OK) return rc;
+    C.r = ws.take<bf16>(w.r);
+    C.s0 = ws.take<bf16>(w.s0);
+    C.rb = ws.take<bf16>(w.rb);
+    C.ds = ws.take<bf16>(w.s0);
+    C.dots = ws.take<float>(w.dots);
+    // the forward's walk, for the states and corrections
+    cudaError_t e = launch_delta_prep(C, w.dk, w.terms, st);
+    if (e == cudaSuccess) e = launch_delta_scan(C, w.dk, w.terms, true, st);
+    // the reverse walk: its "state" is the adjoint, its output the gradient of v
+    C.state_in = grad_state_out;
+    C.state_out = grad_state_in;
+    C.o = grad_v;
+    C.o_stride_t = (long long)params->Hv * params->Dv;
+    C.o_stride_b = C.o_stride_t * params->L;
+    if (e == cudaSuccess) e = launch_delta_reverse(C, w.dk, w.terms, st);
+    C.gq = grad_q; C.gk = grad_k; C.gg = grad_g; C.gbeta = grad_beta;
+    if (e == cudaSuccess) e = launch_delta_grads(C, w.dk, w.terms, st);
+    return status_of(e);
 }

@@ -41,10 +41,12 @@ struct ChunkParams {
     Terms q, k, v, go;
     const float *g, *beta;
     float *coef;                        // [nc][kCoef][64]
-    bf16 *tri;                          // [nc][NT][64 j][64 i]: T transposed, blocks on and below T's diagonal
+    bf16 *tri;                          // [nc][NT][64 j][64 i]: T - I transposed, blocks on and below T's diagonal
     bf16 *p;                            // [nc][NT][64 i][64 j]: P, blocks on and below the diagonal
-    bf16 *r, *rb;                       // backward: [nc][vblocks][NT][64 t][64 v]
+    bf16 *r;                            // backward: [nc][vblocks][3][64 t][64 v]
+    bf16 *rb;                           // backward: [nc][vblocks][NT][64 t][64 v]
     bf16 *s0, *ds;                      // backward: [nc][vblocks][NT][64 v][DK]
+    float *dots;                        // backward: [nc][4 vblocks][2][64], r.(..) per 16 values
     const float *state_in;              // [bh][Dv][Dk], may be NULL
     float *state_out;
     void *o;                            // forward output; backward: grad_v
@@ -128,6 +130,19 @@ template <int N> __device__ __forceinline__ void split(float x, float y, unsigne
     }
 }
 __device__ __forceinline__ float2 unpack(unsigned w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+
+// The value pair that the terms of word e of a fragment stand for
+template <int N> __device__ __forceinline__ float2 sum_terms(const unsigned (&a)[N][4], int e)
+{
+    float2 x = unpack(a[N - 1][e]);
+#pragma unroll
+    for (int i = N - 2; i >= 0; i--) {
+        const float2 y = unpack(a[i][e]);
+        x.x += y.x;
+        x.y += y.y;
+    }
+    return x;
+}
 
 // Accumulators of two neighbouring 16 x 8 tiles as N terms of the left operand of the next product.
 template <int N> __device__ __forceinline__ void as_left(const float (&c0)[4], const float (&c1)[4], unsigned (&a)[N][4])

@@ -162,13 +162,26 @@ __global__ void __launch_bounds__(128) delta_prep_kernel(const ChunkParams P)
             for (int e = 0; e < 4; e++) { z[0][e] = -z[0][e]; z[1][e] = -z[1][e]; }
             as_left(z[0], z[1], tw[step]);
         }
-        // rows j = 16 w + (gr, gr + 8), columns i = 16 I + tc (+8)
+        // rows j = 16 w + (gr, gr + 8), columns i = 16 I + tc (+8); the identity is left out: who uses T adds its
+        // factor in float, which keeps that part of the product exact
+        unsigned out[NT][4];
+#pragma unroll
+        for (int m = 0; m < NT; m++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                out[m][e] = tw[step][m][e];
+                // words 0 and 3 of a diagonal block hold the diagonal: element tc == gr low half, tc + 1 == gr high
+                if (step == 0 && (e == 0 || e == 3)) {
+                    if (tc == gr) out[m][e] &= 0xffff0000u;
+                    if (tc + 1 == gr) out[m][e] &= 0x0000ffffu;
+                }
+            }
         bf16 *dst = tri + (16 * w + gr) * kC + 16 * I + tc;
 #pragma unroll
         for (int m = 0; m < NT; m++)
 #pragma unroll
             for (int e = 0; e < 4; e++)
-                *reinterpret_cast<unsigned *>(dst + m * kTile + (e & 1) * 8 * kC + (e >> 1) * 8) = tw[step][m][e];
+                *reinterpret_cast<unsigned *>(dst + m * kTile + (e & 1) * 8 * kC + (e >> 1) * 8) = out[m][e];
     }
 }
 

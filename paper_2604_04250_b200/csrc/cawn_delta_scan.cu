@@ -136,15 +136,7 @@ __global__ void __launch_bounds__(128) delta_scan_kernel(const ChunkParams P)
                 const float2 eg = *reinterpret_cast<const float2 *>(&st.coef[COEF_EG][8 * n + tc]);
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
-                    float2 x = make_float2(0.f, 0.f);
-                    if (vcols > 0) {
-#pragma unroll
-                        for (int i = NP - 1; i >= 0; i--) {
-                            const float2 y = unpack(vf[i][2 * m + h]);
-                            x.x += y.x;
-                            x.y += y.y;
-                        }
-                    }
+                    const float2 x = vcols > 0 ? sum_terms(vf, 2 * m + h) : make_float2(0.f, 0.f);
                     X[n][2 * h] = fmaf(-eg.x, X[n][2 * h], x.x);
                     X[n][2 * h + 1] = fmaf(-eg.y, X[n][2 * h + 1], x.y);
                     if (MODE == MODE_OUT) {
@@ -154,8 +146,12 @@ __global__ void __launch_bounds__(128) delta_scan_kernel(const ChunkParams P)
                 }
             }
         }
-        // r = R T^T: tokens t of the result from block t' on
-        float r[8][4] = {};
+        // r = R + R (T - I)^T: tokens t of the result from block t' on
+        float r[8][4];
+#pragma unroll
+        for (int n = 0; n < 8; n++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) r[n][e] = X[n][e];
 #pragma unroll
         for (int tb = 0; tb < 4; tb++) {
             unsigned x[NT][4];
@@ -166,13 +162,13 @@ __global__ void __launch_bounds__(128) delta_scan_kernel(const ChunkParams P)
         }
         if (MODE == MODE_SAVE) {
             // r, token rows of 64 values: transposed through this warp's own columns of the V tile
-            bf16 *dst = P.r + (nc * P.vblocks + vb) * (NT * kTile);
+            bf16 *dst = P.r + (nc * P.vblocks + vb) * (3 * kTile);
 #pragma unroll
-            for (int term = 0; term < NT; term++) {
+            for (int term = 0; term < 3; term++) {
                 __syncwarp();
 #pragma unroll
                 for (int nb = 0; nb < 4; nb++) {
-                    unsigned x[NT][4];
+                    unsigned x[3][4];
                     as_left(r[2 * nb], r[2 * nb + 1], x);
                     stsm_t(at_nk(vs, kLd, 16 * nb, 16 * w), x[term][0], x[term][1], x[term][2], x[term][3]);
                 }
@@ -224,12 +220,11 @@ __global__ void __launch_bounds__(128) delta_scan_kernel(const ChunkParams P)
                     }
             }
         }
-        // S <- e^{G_C} S + (e^{G_C - G} u) K
+        // S <- e^{G_C} S + (e^{G_C - G} u) K.  The update is summed from zero and added once: the tensor
+        // core's running sum drops low bits at every step, always towards zero, which on a state that lives
+        // for many chunks would add up.
         const float eC = st.coef[COEF_EG][kC - 1];
-#pragma unroll
-        for (int n = 0; n < DK / 8; n++)
-#pragma unroll
-            for (int e = 0; e < 4; e++) S[n][e] *= eC;
+        unsigned u[4][NT][4];
 #pragma unroll
         for (int tb = 0; tb < 4; tb++) {
 #pragma unroll
@@ -238,11 +233,18 @@ __global__ void __launch_bounds__(128) delta_scan_kernel(const ChunkParams P)
                 float (&x)[4] = r[2 * tb + m];
                 x[0] *= lf.x; x[1] *= lf.y; x[2] *= lf.x; x[3] *= lf.y;
             }
-            unsigned u[NT][4];
-            as_left(r[2 * tb], r[2 * tb + 1], u);
+            as_left(r[2 * tb], r[2 * tb + 1], u[tb]);
+        }
 #pragma unroll
-            for (int nb = 0; nb < DK / 16; nb++)
-                product<NT, NP, true>(S[2 * nb], S[2 * nb + 1], u, at_kn(ks, ld, 16 * tb, 16 * nb), kC * ld);
+        for (int nb = 0; nb < DK / 16; nb++) {
+            float x[2][4] = {};
+#pragma unroll
+            for (int tb = 0; tb < 4; tb++) product<NT, NP, true>(x[0], x[1], u[tb], at_kn(ks, ld, 16 * tb, 16 * nb), kC * ld);
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                S[2 * nb][e] = fmaf(eC, S[2 * nb][e], x[0][e]);
+                S[2 * nb + 1][e] = fmaf(eC, S[2 * nb + 1][e], x[1][e]);
+            }
         }
         __syncthreads();        // the tiles are free
         if (STAGES == 1 && c + 1 < c1) scan_load<DK, NP, MODE>(P, stages[0], bh, c + 1, vb, vcols);

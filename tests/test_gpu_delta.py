@@ -194,3 +194,139 @@ def test_runs_on_another_stream_and_in_a_graph(form):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(o, want) and torch.equal(so, want_s)
+
+
+# ------------------------------------------------------------------------------------ backward
+
+def backward(d, prm=None, cuda=None, with_states=True):
+    c = cuda or {n: t.cuda() for n, t in d.items()}
+    prm = prm or params(d)
+    nan = lambda t: torch.full(t.shape, float("nan"), dtype=t.dtype, device="cuda")
+    out = {n: nan(d[n]) for n in ("q", "k", "v", "g", "beta")}
+    gsi = nan(d["state_in"]) if with_states else None
+    ws = cb.new_delta_workspace(prm, cb.CAWN_DELTA_BWD)
+    ws.fill_(0xFF)
+    cb.cawn_delta_rule_bwd(prm, c["q"], c["k"], c["v"], c["g"], c["beta"], c["grad_o"], out["q"], out["k"], out["v"], out["g"], out["beta"], ws,
+                           state_in=c["state_in"] if with_states else None, grad_state_out=c["grad_state_out"] if with_states else None, grad_state_in=gsi)
+    if with_states:
+        out["state_in"] = gsi
+    return out
+
+
+def loss64(w, scale):
+    o, s = delta_rule(w["q"], w["k"], w["v"], w["g"], w["beta"], scale, w["state_in"])
+    return (o * w["grad_o"]).sum() + (s * w["grad_state_out"]).sum()
+
+
+def reference_grads(d, with_states=True):
+    w = {n: t.double() for n, t in d.items()}
+    if not with_states:
+        w["state_in"], w["grad_state_out"] = torch.zeros_like(w["state_in"]), torch.zeros_like(w["state_in"])
+    names = ["q", "k", "v", "g", "beta"] + (["state_in"] if with_states else [])
+    for n in names:
+        w[n].requires_grad_()
+    return dict(zip(names, torch.autograd.grad(loss64(w, d["q"].shape[3] ** -0.5), [w[n] for n in names])))
+
+
+def check_grads(got, want, dtype):
+    for n in want:
+        close(got[n], want[n], TOL[dtype] if n in "qkv" else STATE_TOL, "grad_" + n)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_backward(shape, dtype):
+    d = delta_inputs(*shape, dtype, seed=sum(shape) + 1)
+    check_grads(backward(d), reference_grads(d), dtype)
+
+
+def test_backward_without_states():
+    d = delta_inputs(2, 100, 1, 2, 64, 64, torch.float32, seed=20)
+    check_grads(backward(d, with_states=False), reference_grads(d, with_states=False), torch.float32)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_backward_of_slices(dtype):
+    """q, k, v and grad_o with strides; gradients dense."""
+    B, L, Hk, Hv, Dk, Dv = 2, 99, 2, 4, 64, 72
+    d = delta_inputs(B, L, Hk, Hv, Dk, Dv, dtype, seed=21)
+    c = {n: t.cuda() for n, t in d.items()}
+    w = torch.cat([c["q"].flatten(2), c["k"].flatten(2), c["v"].flatten(2), c["grad_o"].flatten(2)], -1)
+    parts = w.split([Hk * Dk, Hk * Dk, Hv * Dv, Hv * Dv], -1)
+    for n, x in zip(("q", "k", "v", "grad_o"), parts):
+        c[n] = x
+    s = w.shape[-1]
+    prm = params(d, q_stride=s, k_stride=s, v_stride=s, o_stride=s)
+    check_grads(backward(d, prm, c), reference_grads(d), dtype)
+
+
+def test_backward_of_shared_heads_sums_them():
+    """Hv / Hk value heads on one key head: the same gradients as with the key head written out per value
+    head, summed."""
+    d = delta_inputs(1, 150, 1, 3, 64, 64, torch.float32, seed=22)
+    wide = dict(d)
+    wide["q"], wide["k"] = d["q"].repeat_interleave(3, 2), d["k"].repeat_interleave(3, 2)
+    a, b = backward(d), backward(wide)
+    for n in ("q", "k"):
+        close(a[n], b[n].double().sum(2, keepdim=True), 1e-6)
+    for n in ("v", "g", "beta", "state_in"):
+        assert torch.equal(a[n], b[n])
+
+
+def test_backward_forgetting_and_repeated_tokens():
+    d = delta_inputs(1, 170, 1, 2, 64, 64, torch.float32, seed=23)
+    d["k"][:, 20:60] = d["k"][:, 20:21]
+    d["g"][:, 64:110] = -1e-4
+    d["g"][:, 70] = -float("inf")
+    d["g"][:, 120:130] = -60.0
+    d["beta"][:, 30:40] = 0.0
+    d["beta"][:, 90:100] = 1.0
+    got = backward(d)
+    want = reference_grads(d)
+    assert (got["g"][:, 70] == 0).all()                 # nothing before it reaches past it
+    check_grads(got, want, torch.float32)
+
+
+def test_backward_against_differences():
+    """Directional derivatives of the 64-bit loss.  Central differences with h = 1e-5 are good to about
+    1e-8 of the gradient's size; the kernel's own 1e-5 dominates."""
+    d = delta_inputs(1, 90, 1, 2, 64, 64, torch.float32, seed=24)
+    got = backward(d)
+    rng = torch.Generator().manual_seed(240)
+    for n, grad in got.items():
+        way = torch.randn(d[n].shape, generator=rng).double()
+        def loss(h):
+            w = {m: t.double() for m, t in d.items()}
+            w[n] = w[n] + h * way
+            return loss64(w, 64 ** -0.5)
+        slope = (loss(1e-5) - loss(-1e-5)) / 2e-5
+        g = grad.double().cpu()
+        assert abs((g * way).sum() - slope) <= 1e-5 * g.norm() * way.norm(), n
+
+
+def test_backward_is_repeatable_and_runs_in_a_graph():
+    d = delta_inputs(2, 200, 2, 4, 64, 64, torch.bfloat16, seed=25)
+    want = backward(d)
+    again = backward(d)
+    assert all(torch.equal(want[n], again[n]) for n in want)
+    c = {n: t.cuda() for n, t in d.items()}
+    prm = params(d)
+    out = {n: torch.empty_like(want[n]) for n in want}
+    ws = cb.new_delta_workspace(prm, cb.CAWN_DELTA_BWD)
+    call = lambda: cb.cawn_delta_rule_bwd(prm, c["q"], c["k"], c["v"], c["g"], c["beta"], c["grad_o"], out["q"], out["k"], out["v"], out["g"], out["beta"],
+                                          ws, state_in=c["state_in"], grad_state_out=c["grad_state_out"], grad_state_in=out["state_in"])
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for t in out.values():
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(want[n], out[n]) for n in want)
+
+
+def test_backward_without_tokens():
+    d = delta_inputs(2, 0, 1, 1, 64, 64, torch.float32, seed=26)
+    got = backward(d)
+    assert torch.equal(got["state_in"].cpu(), d["grad_state_out"])
