@@ -53,7 +53,8 @@ constexpr int kStepTokens = 16;
 struct Plan {
     int dk, terms, chunks, vblocks, segs, seg_chunks;    // terms: of an input
     size_t q, k, v, go;                  // three bfloat16 terms each, float storage only
-    size_t coef, tri, p, r, rb, s0, dots;
+    size_t coef, tri, p;
+    size_t u, s0, rf, sf, od, ds, rbt, rd, sd;   // backward
     size_t seg_state, seg_map;
     size_t total;
 };
@@ -81,12 +82,19 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
     w.tri = part((double)nc * nt * kTile * 2);
     w.p = w.tri;
     if (backward) {
-        w.r = part((double)nc * w.vblocks * 3 * kTile * 2);
-        w.rb = part((double)nc * w.vblocks * nt * kTile * 2);
-        w.s0 = part((double)nc * w.vblocks * nt * kC * w.dk * 2);
+        const double nv = (double)nc * w.vblocks, ends = (double)p->B * p->Hv * w.vblocks;
+        w.u = part(nv * w.terms * kTile * 2);
+        w.s0 = part(nv * w.terms * kC * w.dk * 2);
+        w.ds = w.s0;
+        w.rf = part(nv * kTile * 4);
+        w.sf = part((nv + ends) * kC * w.dk * 4);
+        w.od = part(nv * 4 * kC * 4);
+        w.rd = 2 * w.od;
+        w.sd = part(nv * 4 * 4);
+        w.rbt = w.terms == 3 ? w.v : 0;
     }
-    if (backward) w.dots = part((double)nc * w.vblocks * 4 * 2 * kC * 4);
-    w.total = w.dots + w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + w.r + w.rb + 2 * w.s0 + 2 * w.seg_state + w.seg_map;
+    w.total = w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + w.u + w.s0 + w.ds + w.rf + w.sf + w.od + w.rd + w.sd + w.rbt +
+              2 * w.seg_state + w.seg_map;
     return w;
 }
 
@@ -212,11 +220,17 @@ extern "C" int cawn_delta_rule_bwd(const cawn_delta_params *params, const void *
     if (rc == CAWN_OK)
         rc = terms_of(C.go, grad_o, D.o_stride, (long long)params->B * params->L, params->L, params->Hv * params->Dv, w.terms, w.go, ws, st);
     if (rc != CAWN_OK) return rc;
-    C.r = ws.take<bf16>(w.r);
+    C.u = ws.take<bf16>(w.u);
     C.s0 = ws.take<bf16>(w.s0);
-    C.rb = ws.take<bf16>(w.rb);
-    C.ds = ws.take<bf16>(w.s0);
-    C.dots = ws.take<float>(w.dots);
+    C.ds = ws.take<bf16>(w.ds);
+    C.rf = ws.take<float4>(w.rf);
+    C.sf = ws.take<float4>(w.sf);
+    C.od = ws.take<float>(w.od);
+    C.rd = ws.take<float>(w.rd);
+    C.sd = ws.take<float>(w.sd);
+    C.rbt = ws.take<bf16>(w.rbt);
+    const long long vo = (long long)params->Hv * params->Dv;
+    C.rb = {w.terms == 1 ? static_cast<const bf16 *>(grad_v) : C.rbt, (long long)params->B * params->L * vo, vo, vo * params->L};
     // the forward's walk, for the states and corrections
     cudaError_t e = launch_delta_prep(C, w.dk, w.terms, st);
     if (e == cudaSuccess) e = launch_delta_scan(C, w.dk, w.terms, true, st);
@@ -224,8 +238,6 @@ extern "C" int cawn_delta_rule_bwd(const cawn_delta_params *params, const void *
     C.state_in = grad_state_out;
     C.state_out = grad_state_in;
     C.o = grad_v;
-    C.o_stride_t = (long long)params->Hv * params->Dv;
-    C.o_stride_b = C.o_stride_t * params->L;
     if (e == cudaSuccess) e = launch_delta_reverse(C, w.dk, w.terms, st);
     C.gq = grad_q; C.gk = grad_k; C.gg = grad_g; C.gbeta = grad_beta;
     if (e == cudaSuccess) e = launch_delta_grads(C, w.dk, w.terms, st);

@@ -7,10 +7,11 @@
 //   O = scale e^G Q S0^T + P u               S = e^{G_C} S0 + sum_j e^{G_C - G_j} u_j k_j^T
 //
 // Precision.  Products run on the tensor cores with bfloat16 factors and float sums; a float factor enters
-// as a sum of bfloat16 terms (8 mantissa bits each).  With bfloat16 storage inputs are exact as one term
-// and everything computed takes two (16 bits; measured error of the state 5e-6); with float storage
-// everything takes three, inputs by a pass of their own (two terms were at 8e-6, too near to what a user
-// of float expects).  NP: terms of inputs (1 or 3), NT: terms of computed factors (2 or 3).
+// as a sum of bfloat16 terms (8 mantissa bits each).  With bfloat16 storage inputs are exact as one term, T
+// and P take two, the state, its update and everything behind a float result three; with float storage
+// everything takes three, inputs by a pass of their own.  (With two terms throughout, the state was off by
+// 5e-6 and the gradient of g by up to 2e-5, too near to or past what a user of float expects.)  NP: terms of
+// inputs (1 or 3), NT: terms of T and P (2 or 3).
 //
 // Layout.  Sequential kernels work on transposed chunks: a warp owns 16 rows of values v and all keys,
 // so that every product of the chain (state x keys, triangle, update) has the previous result as its
@@ -26,7 +27,7 @@ constexpr int kC = 64;                  // tokens of a chunk
 constexpr int kPad = 8;                 // bfloat16 of padding per shared row: ldmatrix reads 8 rows without conflicts
 constexpr int kTile = kC * kC;          // elements of a 64 x 64 tile in the workspace
 constexpr int kLd = kC + kPad;
-constexpr int kCoef = 5;                // floats per token: e^G, e^{G_C - G}, beta, G (high, low part)
+constexpr int kCoef = 5;                // floats per token: e^G, e^{G_C - G}, beta, log2(e) G (high, low part)
 enum { COEF_EG = 0, COEF_LEFT = 1, COEF_BETA = 2, COEF_GHI = 3, COEF_GLO = 4 };
 
 // One input array as NP bfloat16 terms, `plane` elements apart; strides in elements.
@@ -35,18 +36,26 @@ struct Terms {
     long long plane, stride_t, stride_b;
 };
 
-// Everything the chunk kernels share.  nc = bh * chunks + c numbers chunks of value heads; tiles and
-// coefficients of the workspace are dense over nc.
+// Everything the chunk kernels share.  nc = bh * chunks + c numbers chunks of value heads, nv = nc * vblocks +
+// vb their blocks of 64 values; tiles and coefficients of the workspace are dense over these.
 struct ChunkParams {
     Terms q, k, v, go;
+    Terms rb;                           // gradients kernel: rb, which is dV (bfloat16) or its terms
     const float *g, *beta;
     float *coef;                        // [nc][kCoef][64]
     bf16 *tri;                          // [nc][NT][64 j][64 i]: T - I transposed, blocks on and below T's diagonal
     bf16 *p;                            // [nc][NT][64 i][64 j]: P, blocks on and below the diagonal
-    bf16 *r;                            // backward: [nc][vblocks][3][64 t][64 v]
-    bf16 *rb;                           // backward: [nc][vblocks][NT][64 t][64 v]
-    bf16 *s0, *ds;                      // backward: [nc][vblocks][NT][64 v][DK]
-    float *dots;                        // backward: [nc][4 vblocks][2][64], r.(..) per 16 values
+    // kept by the forward's walk for the backward
+    bf16 *u;                            // [nv][NP][64 t][64 v]
+    bf16 *s0;                           // [nv][NP][64 v][DK]: state before the chunk
+    float4 *rf, *sf;                    // [nv][4 warps][8 or DK/8 tiles][32 lanes]: r and the state before the chunk in float,
+                                        // as the walks' accumulators hold them
+    float *od;                          // [nv][4][64]: dO.o over 16 values
+    // kept by the reverse walk
+    bf16 *ds;                           // [nv][NP][64 v][DK]: adjoint of the state after the chunk
+    bf16 *rbt;                          // [NP] terms of rb, float storage only, laid out like v
+    float *rd;                          // [nv][4][2][64]: rb.r and rb.v over 16 values
+    float *sd;                          // [nv][4]: <state after the chunk, its adjoint> over 16 values
     const float *state_in;              // [bh][Dv][Dk], may be NULL
     float *state_out;
     void *o;                            // forward output; backward: grad_v
@@ -74,14 +83,21 @@ template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.as
 template <int ROWS, int COLS, int THREADS>
 __device__ __forceinline__ void load_tile(bf16 *dst, const bf16 *src, long long stride, int rows, int cols)
 {
-    const unsigned base = smem_addr(dst);
+    static_assert(THREADS % (COLS / 8) == 0 && ROWS % (THREADS / (COLS / 8)) == 0, "whole passes");
+    constexpr int STEP = THREADS / (COLS / 8);
+    const int tid = threadIdx.x % THREADS, r = tid / (COLS / 8), c = tid % (COLS / 8) * 8;
+    unsigned to = smem_addr(dst) + (r * (COLS + kPad) + c) * 2;
+    const bf16 *from = src + r * stride + c;
 #pragma unroll
-    for (int i = threadIdx.x; i < ROWS * (COLS / 8); i += THREADS) {
-        const int r = i / (COLS / 8), c = i % (COLS / 8) * 8;
-        const bool ok = r < rows && c < cols;
-        cp16(base + (r * (COLS + kPad) + c) * 2, ok ? src + r * stride + c : src, ok);
+    for (int i = 0; i < ROWS / STEP; i++) {
+        const bool ok = r + i * STEP < rows && c < cols;
+        cp16(to, ok ? from : src, ok);
+        to += STEP * (COLS + kPad) * 2;
+        from += STEP * stride;
     }
 }
+// A dense 64 x 64 tile of the workspace
+template <int THREADS> __device__ __forceinline__ void load_dense(bf16 *dst, const bf16 *src) { load_tile<kC, kC, THREADS>(dst, src, kC, kC, kC); }
 
 __device__ __forceinline__ void ldsm(unsigned (&r)[4], unsigned addr)
 {
@@ -100,7 +116,7 @@ __device__ __forceinline__ void stsm_t(unsigned addr, unsigned a, unsigned b, un
 }
 __device__ __forceinline__ void mma(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -119,14 +135,93 @@ __device__ __forceinline__ unsigned at_kn(unsigned base, int ld, int row, int co
     return base + ((row + l % 8 + l / 8 % 2 * 8) * ld + col + l / 16 * 8) * 2;
 }
 
+// A pair of floats in one 64-bit register: the accumulators' neighbours are handled two at a time.
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 pair(float x, float y)
+{
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ f32x2 pair(float2 v) { return pair(v.x, v.y); }
+__device__ __forceinline__ float2 halves(f32x2 v)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
+{
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+// rows h = 0, 1 of an accumulator tile, times / plus pairs
+__device__ __forceinline__ void scale_row(float (&c)[4], int h, f32x2 f)
+{
+    const float2 v = halves(mul2(pair(c[2 * h], c[2 * h + 1]), f));
+    c[2 * h] = v.x;
+    c[2 * h + 1] = v.y;
+}
+// c row h <- a * (c row h) + b
+__device__ __forceinline__ void fma_row(float (&c)[4], int h, f32x2 a, f32x2 b)
+{
+    const float2 v = halves(fma2(a, pair(c[2 * h], c[2 * h + 1]), b));
+    c[2 * h] = v.x;
+    c[2 * h + 1] = v.y;
+}
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// Barriers of the walks: four consumer warps, one producer warp.
+constexpr int kWalkThreads = 160;
+__device__ __forceinline__ void bar_sync(int id) { asm volatile("bar.sync %0, %1;" :: "r"(id), "n"(kWalkThreads) : "memory"); }
+__device__ __forceinline__ void bar_arrive(int id) { asm volatile("bar.arrive %0, %1;" :: "r"(id), "n"(kWalkThreads) : "memory"); }
+
+// Sums over the eight lanes that share a column pair, for N pairs of each of the eight tiles; lane row gr
+// ends with the sums of tile gr in v[0].
+template <int N> __device__ __forceinline__ void column_sums(float (&v)[8][N])
+{
+    const int gr = threadIdx.x % 32 / 4;
+#pragma unroll
+    for (int bit = 4; bit > 0; bit /= 2)
+#pragma unroll
+        for (int n = 0; n < bit; n++)
+#pragma unroll
+            for (int e = 0; e < N; e++) {
+                const bool up = (gr & bit) != 0;
+                const float keep = up ? v[n + bit][e] : v[n][e], send = up ? v[n][e] : v[n + bit][e];
+                v[n][e] = keep + __shfl_xor_sync(0xffffffffu, send, bit * 4);
+            }
+}
+
 // x, y as N bfloat16 terms of falling size, packed; N = 1 rounds
 template <int N> __device__ __forceinline__ void split(float x, float y, unsigned (&w)[N])
 {
+    f32x2 rest = pair(x, y);
 #pragma unroll
     for (int i = 0; i < N; i++) {
-        w[i] = pack_bf16(x, y);
-        x -= __uint_as_float(w[i] << 16);
-        y -= __uint_as_float(w[i] & 0xffff0000u);
+        const float2 v = halves(rest);
+        w[i] = pack_bf16(v.x, v.y);
+        if (i + 1 < N)
+            rest = fma2(pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)), pair(-1.f, -1.f), rest);
     }
 }
 __device__ __forceinline__ float2 unpack(unsigned w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }

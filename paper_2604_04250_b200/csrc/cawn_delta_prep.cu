@@ -39,7 +39,8 @@ __global__ void __launch_bounds__(128) delta_prep_kernel(const ChunkParams P)
     cp_commit();
 
     if (w == 0) {
-        // Running sum in double: differences G_i - G_j of strong decays keep their accuracy.  Below
+        // Running sum in double, in units of log 2: differences G_i - G_j of strong decays keep their
+        // accuracy, and one instruction turns them into decays.  Below
         // -200 every decay is zero in float, and so is every product with one: the clamp changes no
         // result and keeps -infinity out of the differences.
         const long long at = ((long long)(bh / P.Hv) * P.L + t0) * P.Hv + bh % P.Hv;
@@ -49,8 +50,10 @@ __global__ void __launch_bounds__(128) delta_prep_kernel(const ChunkParams P)
         for (int e = 0; e < 2; e++) {
             const int t = lane * 2 + e;
             const float g = t < rows ? P.g[at + (long long)t * P.Hv] : 0.f;
-            bt[e] = t < rows ? P.beta[at + (long long)t * P.Hv] : 0.f;
-            sum[e] = g < -200.f ? -200.0 : (double)g;
+            const float x = t < rows ? P.beta[at + (long long)t * P.Hv] : 1.f;
+            // the backward divides by beta; 2^-100 in place of 0 changes nothing that float could show
+            bt[e] = fabsf(x) < 0x1p-100f ? copysignf(0x1p-100f, x) : x;
+            sum[e] = (g < -200.f ? -200.0 : (double)g) * 1.4426950408889634;
         }
         sum[1] += sum[0];
         double run = sum[1];
@@ -69,8 +72,8 @@ __global__ void __launch_bounds__(128) delta_prep_kernel(const ChunkParams P)
             const int t = lane * 2 + e;
             const float hi = (float)sum[e], lo = (float)(sum[e] - (double)hi);
             sm.ghi[t] = hi; sm.glo[t] = lo; sm.beta[t] = bt[e];
-            coef[COEF_EG * kC + t] = expf(hi) * (1.f + lo);
-            coef[COEF_LEFT * kC + t] = expf((float)(last - sum[e]));
+            coef[COEF_EG * kC + t] = exp2_fast(hi) * fmaf(lo, 0.69314718f, 1.f);
+            coef[COEF_LEFT * kC + t] = exp2_fast((float)(last - sum[e]));
             coef[COEF_BETA * kC + t] = bt[e];
             coef[COEF_GHI * kC + t] = hi;
             coef[COEF_GLO * kC + t] = lo;
@@ -105,7 +108,7 @@ __global__ void __launch_bounds__(128) delta_prep_kernel(const ChunkParams P)
 #pragma unroll
             for (int e = 0; e < 2; e++) {
                 const bool low = i >= j + e;
-                const float gam = low ? expf((sm.ghi[i] - sm.ghi[j + e]) + (sm.glo[i] - sm.glo[j + e])) : 0.f;
+                const float gam = low ? exp2_fast((sm.ghi[i] - sm.ghi[j + e]) + (sm.glo[i] - sm.glo[j + e])) : 0.f;
                 p[e] = low ? P.scale * gam * qk[n][2 * half + e] : 0.f;
                 a[e] = i > j + e ? gam * kk[n][2 * half + e] * sm.beta[j + e] : 0.f;
             }
