@@ -69,8 +69,18 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
     const double nt = w.terms == 1 ? 2 : 3;      // terms of what is computed
     w.chunks = (int)((p->L + kC - 1) / kC);
     w.vblocks = (p->Dv + kC - 1) / kC;
-    w.segs = 1;
-    w.seg_chunks = w.chunks;
+    // Time segments where the heads alone leave SMs without a block: they cost a second walk over values and keys,
+    // so fewer than three do not pay.
+    const int64_t blocks = (int64_t)p->B * p->Hv * w.vblocks, room = (int64_t)sm_count() * (w.dk == 64 && w.terms == 1 && !backward ? 2 : 1);
+    int64_t segs = 3 * blocks <= sm_count() ? room / blocks : 1;
+    if (segs > w.chunks / 4) segs = w.chunks / 4;
+    if (segs < 3) segs = 1;
+    w.seg_chunks = (int)((w.chunks + segs - 1) / segs);
+    w.segs = w.chunks > 0 ? (w.chunks + w.seg_chunks - 1) / w.seg_chunks : 1;
+    if (w.segs > 1) {
+        w.seg_state = part((double)p->B * p->Hv * w.segs * p->Dv * p->Dk * 4);
+        w.seg_map = part((double)p->B * p->Hv * w.segs * p->Dk * p->Dk * 4);
+    }
     const size_t nc = (size_t)p->B * p->Hv * w.chunks, rows = (size_t)p->B * p->L;
     if (w.terms == 3) {
         w.q = part((double)rows * p->Hk * p->Dk * 6);
@@ -135,6 +145,9 @@ int chunk_params(ChunkParams &C, const cawn_delta_params *p, const DeltaParams &
     C.coef = ws.take<float>(w.coef);
     C.tri = ws.take<bf16>(w.tri);
     C.p = ws.take<bf16>(w.p);
+    C.seg_start = ws.take<float>(w.seg_state);
+    C.seg_end = ws.take<float>(w.seg_state);
+    C.seg_map = ws.take<float>(w.seg_map);
     return rc;
 }
 

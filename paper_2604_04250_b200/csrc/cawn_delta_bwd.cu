@@ -57,7 +57,8 @@ __device__ __forceinline__ void rev_load(const ChunkParams &P, RevStage<DK, NP> 
     cp_commit();
 }
 
-template <int DK, int NP, class T>
+// SUMMARY: only the adjoint that a segment's own outputs send to its start.
+template <int DK, int NP, bool SUMMARY, class T>
 __global__ void __launch_bounds__(kWalkThreads, 1) delta_reverse_kernel(const ChunkParams P)
 {
     constexpr int STAGES = kRevStages<DK, NP>, ld = DK + kPad, NT = NP == 1 ? 2 : 3;
@@ -81,8 +82,9 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_reverse_kernel(const Ch
 
     const int row[2] = {r0 + 16 * w + gr, r0 + 16 * w + gr + 8};
     float D[DK / 8][4];
-    const float *from = P.segs > 1 ? P.seg_start + ((long long)bh * P.segs + seg) * P.Dv * P.Dk
-                                   : (P.state_in != nullptr ? P.state_in + (long long)bh * P.Dv * P.Dk : nullptr);
+    const float *from = SUMMARY ? nullptr
+                        : P.segs > 1 ? P.seg_start + ((long long)bh * P.segs + seg) * P.Dv * P.Dk
+                                     : (P.state_in != nullptr ? P.state_in + (long long)bh * P.Dv * P.Dk : nullptr);
 #pragma unroll
     for (int n = 0; n < DK / 8; n++)
 #pragma unroll
@@ -102,7 +104,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_reverse_kernel(const Ch
         const unsigned gs = smem_addr(st.go[0]), vs = smem_addr(st.v[0]);
 
         // <state after the chunk, D>; D for the chunk's own gradients
-        {
+        if constexpr (!SUMMARY) {
             const long long after = c + 1 < P.chunks ? nc + 1 : (long long)P.B * P.Hv * P.chunks + bh;
             const float4 *sf = P.sf + ((after * P.vblocks + vb) * 4 + w) * (DK / 8 * 32) + lane;
             bf16 *dst = P.ds + nv * (NP * kC * DK) + (16 * w + gr) * DK + tc;
@@ -125,7 +127,8 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_reverse_kernel(const Ch
         }
         float4 rf[8];               // r, fetched long before its use
 #pragma unroll
-        for (int n = 0; n < 8; n++) rf[n] = P.rf[((nv * 4 + w) * 8 + n) * 32 + lane];
+        for (int n = 0; n < 8; n++)
+            if (!SUMMARY) rf[n] = P.rf[((nv * 4 + w) * 8 + n) * 32 + lane];
         bar_sync(1 + s);
         // X = e^{G_C - G} (D K^T) + dO^T P
         float X[8][4] = {};
@@ -167,7 +170,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_reverse_kernel(const Ch
             for (int nb = 0; nb <= ib; nb++) product<3, NT, false>(rb[2 * nb], rb[2 * nb + 1], x, at_nk(ts, kLd, 16 * nb, 16 * ib), kC * kLd);
         }
         // rb.r and rb.v over this warp's 16 values
-        {
+        if constexpr (!SUMMARY) {
             float dots[8][4];
 #pragma unroll
             for (int nb = 0; nb < 4; nb++) {
@@ -192,7 +195,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_reverse_kernel(const Ch
         // the rounded value), or its terms for the chunk's gradients
         const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
 #pragma unroll
-        for (int term = 0; term < NP; term++) {
+        for (int term = 0; term < (SUMMARY ? 0 : NP); term++) {
             bf16 *dst = NP == 1 ? static_cast<bf16 *>(P.o) : P.rbt + term * P.rb.plane;
             dst += v_base(P, P.rb, bh, t0) + r0;
             __syncwarp();
@@ -210,7 +213,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_reverse_kernel(const Ch
                     *reinterpret_cast<uint4 *>(dst + t * P.rb.stride_t + v) = *reinterpret_cast<const uint4 *>(&st.v[0][t * kLd + v]);
             }
         }
-        if constexpr (sizeof(T) == 4) {
+        if constexpr (sizeof(T) == 4 && !SUMMARY) {
             T *gv = static_cast<T *>(P.o) + v_base(P, P.rb, bh, t0) + r0;
 #pragma unroll
             for (int n = 0; n < 8; n++)
@@ -258,8 +261,9 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_reverse_kernel(const Ch
         }
         if (c - STAGES >= c0) bar_arrive(3 + s);
     }
-    if (P.state_out != nullptr && seg == 0) {
-        float *to = P.state_out + (long long)bh * P.Dv * P.Dk;
+    float *to = SUMMARY ? P.seg_end + ((long long)bh * P.segs + seg) * P.Dv * P.Dk
+                : P.state_out != nullptr && seg == 0 ? P.state_out + (long long)bh * P.Dv * P.Dk : nullptr;
+    if (to != nullptr) {
 #pragma unroll
         for (int n = 0; n < DK / 8; n++)
 #pragma unroll
@@ -474,15 +478,25 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
         }
 }
 
-template <int DK, int NP> cudaError_t reverse(const ChunkParams &P, cudaStream_t st)
+template <int DK, int NP, bool SUMMARY> cudaError_t walk(const ChunkParams &P, cudaStream_t st)
 {
     using T = typename std::conditional<NP == 1, bf16, float>::type;
     const size_t smem = sizeof(RevStage<DK, NP>) * kRevStages<DK, NP>;
     static_assert(sizeof(RevStage<DK, NP>) <= 227 * 1024, "fits an SM");
-    auto *kernel = delta_reverse_kernel<DK, NP, T>;
+    auto *kernel = delta_reverse_kernel<DK, NP, SUMMARY, T>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     return launch(kernel, dim3((unsigned)(P.B * P.Hv), P.vblocks, P.segs), dim3(kWalkThreads), smem, st, P);
+}
+
+template <int DK, int NP> cudaError_t reverse(const ChunkParams &P, cudaStream_t st)
+{
+    if (P.segs > 1) {           // the forward's transitions are still in the workspace
+        cudaError_t e = walk<DK, NP, true>(P, st);
+        if (e == cudaSuccess) e = launch_delta_join(P, DK, true, st);
+        if (e != cudaSuccess) return e;
+    }
+    return walk<DK, NP, false>(P, st);
 }
 
 template <int DK, int NP> cudaError_t grads(const ChunkParams &P, cudaStream_t st)

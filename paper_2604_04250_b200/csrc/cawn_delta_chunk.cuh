@@ -301,6 +301,7 @@ cudaError_t launch_delta_split(const float *src, bf16 *dst, long long plane, lon
 cudaError_t launch_delta_prep(const ChunkParams &P, int dk, int terms, cudaStream_t st);
 // forward over the chunks: outputs (or, for the backward, what it needs to keep: `save`)
 cudaError_t launch_delta_scan(const ChunkParams &P, int dk, int terms, bool save, cudaStream_t st);
+cudaError_t launch_delta_join(const ChunkParams &P, int dk, bool reverse, cudaStream_t st);
 cudaError_t launch_delta_reverse(const ChunkParams &P, int dk, int terms, cudaStream_t st);
 cudaError_t launch_delta_grads(const ChunkParams &P, int dk, int terms, cudaStream_t st);
 

@@ -322,12 +322,85 @@ template <int DK, int NP, int MODE> cudaError_t scan(const ChunkParams &P, int r
     return launch(kernel, dim3((unsigned)(P.B * P.Hv), row_blocks, P.segs), dim3(kWalkThreads), smem, st, P);
 }
 
+// Start states of the segments from their end states and transitions, one segment after the other.  A block has 16
+// rows of one head's state, a thread eight rows of one column; the next transition is on its way (in registers)
+// while the current one is multiplied from shared memory.  Float arithmetic: a few products per segment, once, are
+// not worth the tensor cores.  REVERSE: adjoints, last segment first, with the transposed transitions.
+template <int DK, bool REVERSE>
+__global__ void __launch_bounds__(2 * DK) delta_join_kernel(const ChunkParams P)
+{
+    extern __shared__ __align__(16) float map[];            // [DK][DK + 1], row k: what state column k sends on
+    __shared__ __align__(16) float S[16][DK];
+    constexpr int EACH = DK / 2, LD = DK + 1;               // transition elements per thread
+    const int col = threadIdx.x % DK, half = threadIdx.x / DK, bh = blockIdx.x, r0 = blockIdx.y * 16 + 8 * half;
+    const long long rows = (long long)P.Dv * P.Dk;
+    const bool in = col < P.Dk;
+    float s[8], end[8], m[EACH];
+    auto fetch = [&](int n) {
+        const long long seg = (long long)bh * P.segs + (REVERSE ? P.segs - 1 - n : n);
+        const float *from = P.seg_map + seg * P.Dk * P.Dk;
+#pragma unroll
+        for (int i = 0; i < EACH; i++) {
+            const int k = 2 * i + half;
+            m[i] = in && k < P.Dk ? from[(long long)k * P.Dk + col] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) end[i] = in && r0 + i < P.Dv ? P.seg_end[seg * rows + (long long)(r0 + i) * P.Dk + col] : 0.f;
+    };
+#pragma unroll
+    for (int i = 0; i < 8; i++) s[i] = in && r0 + i < P.Dv && P.state_in != nullptr ? P.state_in[bh * rows + (long long)(r0 + i) * P.Dk + col] : 0.f;
+    fetch(0);
+    for (int n = 0; n < P.segs; n++) {
+        const long long seg = (long long)bh * P.segs + (REVERSE ? P.segs - 1 - n : n);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            if (in && r0 + i < P.Dv) P.seg_start[seg * rows + (long long)(r0 + i) * P.Dk + col] = s[i];
+            S[8 * half + i][col] = s[i];
+            s[i] = end[i];
+        }
+        if (n + 1 == P.segs) break;
+#pragma unroll
+        for (int i = 0; i < EACH; i++) map[REVERSE ? col * LD + 2 * i + half : (2 * i + half) * LD + col] = m[i];
+        __syncthreads();
+        fetch(n + 1);
+#pragma unroll 4
+        for (int k = 0; k < DK; k += 4) {
+            const float a = map[k * LD + col], b = map[(k + 1) * LD + col], c = map[(k + 2) * LD + col], d = map[(k + 3) * LD + col];
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float4 x = *reinterpret_cast<const float4 *>(&S[8 * half + i][k]);
+                s[i] = fmaf(x.x, a, fmaf(x.y, b, fmaf(x.z, c, fmaf(x.w, d, s[i]))));
+            }
+        }
+        __syncthreads();
+    }
+}
+
+template <int DK, bool REVERSE> cudaError_t join1(const ChunkParams &P, cudaStream_t st)
+{
+    const size_t smem = DK * (DK + 1) * sizeof(float);
+    const cudaError_t e = cudaFuncSetAttribute(delta_join_kernel<DK, REVERSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    return launch(delta_join_kernel<DK, REVERSE>, dim3((unsigned)(P.B * P.Hv), (P.Dv + 15) / 16), dim3(2 * DK), smem, st, P);
+}
+template <int DK> cudaError_t join(const ChunkParams &P, bool reverse, cudaStream_t st) { return reverse ? join1<DK, true>(P, st) : join1<DK, false>(P, st); }
+
 template <int DK, int NP> cudaError_t run(const ChunkParams &P, bool save, cudaStream_t st)
 {
+    if (P.segs > 1) {
+        cudaError_t e = scan<DK, NP, MODE_SUMMARY>(P, P.vblocks + (P.Dk + kC - 1) / kC, st);
+        if (e == cudaSuccess) e = join<DK>(P, false, st);
+        if (e != cudaSuccess) return e;
+    }
     return save ? scan<DK, NP, MODE_SAVE>(P, P.vblocks, st) : scan<DK, NP, MODE_OUT>(P, P.vblocks, st);
 }
 
 }  // namespace
+
+cudaError_t launch_delta_join(const ChunkParams &P, int dk, bool reverse, cudaStream_t st)
+{
+    return dk == 64 ? join<64>(P, reverse, st) : join<128>(P, reverse, st);
+}
 
 cudaError_t launch_delta_scan(const ChunkParams &P, int dk, int terms, bool save, cudaStream_t st)
 {

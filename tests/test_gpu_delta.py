@@ -196,6 +196,17 @@ def test_runs_on_another_stream_and_in_a_graph(form):
     assert torch.equal(o, want) and torch.equal(so, want_s)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(1, 1500, 1, 1, 64, 64), (1, 2100, 2, 4, 128, 72), (2, 769, 1, 2, 40, 128)], ids=str)
+def test_long_and_few_heads(shape, dtype):
+    """Cut into time segments that run side by side."""
+    d = delta_inputs(*shape, dtype, seed=sum(shape))
+    o, so = forward(d, "chunk")
+    want_o, want_s = reference(d)
+    close(o, want_o, TOL[dtype], "o")
+    close(so, want_s, STATE_TOL, "state")
+
+
 # ------------------------------------------------------------------------------------ backward
 
 def backward(d, prm=None, cuda=None, with_states=True):
@@ -236,6 +247,13 @@ def check_grads(got, want, dtype):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
 def test_backward(shape, dtype):
+    d = delta_inputs(*shape, dtype, seed=sum(shape) + 1)
+    check_grads(backward(d), reference_grads(d), dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(1, 1100, 1, 1, 64, 64), (1, 900, 1, 2, 128, 72)], ids=str)
+def test_backward_long_and_few_heads(shape, dtype):
     d = delta_inputs(*shape, dtype, seed=sum(shape) + 1)
     check_grads(backward(d), reference_grads(d), dtype)
 
