@@ -71,8 +71,9 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
     w.vblocks = (p->Dv + kC - 1) / kC;
     // Time segments where the heads alone leave SMs without a block: they cost a second walk over values and keys,
     // so fewer than three do not pay.
-    const int64_t blocks = (int64_t)p->B * p->Hv * w.vblocks, room = (int64_t)sm_count() * (w.dk == 64 && w.terms == 1 && !backward ? 2 : 1);
-    int64_t segs = 3 * blocks <= sm_count() ? room / blocks : 1;
+    const int vw = 16 * (w.terms == 1 ? kRowGroups<1> : kRowGroups<3>);
+    const int64_t blocks = (int64_t)p->B * p->Hv * ((p->Dv + vw - 1) / vw);
+    int64_t segs = sm_count() / blocks;
     if (segs > w.chunks / 4) segs = w.chunks / 4;
     if (segs < 3) segs = 1;
     w.seg_chunks = (int)((w.chunks + segs - 1) / segs);

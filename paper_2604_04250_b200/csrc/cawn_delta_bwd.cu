@@ -4,8 +4,7 @@
 // With D the adjoint of the state after a chunk, P as in the forward, T the inverse triangle:
 //   dU = P^T dO + e^{G_C - G} (K D^T),   rb = T^T (beta dU),   dV = rb
 //   D <- e^{G_C} D + (scale e^G dO)^T Q - (e^G rb)^T K
-// is the reverse walk (delta_reverse_kernel: transposed like the forward's, a warp owns 16 value rows,
-// products chained in registers).  The rest of dQ and dK is local to a chunk (delta_grads_kernel):
+// is the reverse walk (delta_reverse_kernel: laid out like the forward's).  The rest of dQ and dK is local to a chunk (delta_grads_kernel):
 //   dP_ij = scale Gam_ij dO_i.u_j (i >= j),   E_ij = -Gam_ij rb_i.u_j (i > j)
 //   dQ = scale e^G dO S0 + dP K
 //   dK = dP^T Q + e^{G_C - G} u D - e^G rb S0 + (E + E^T) K
@@ -25,61 +24,156 @@ namespace {
 // ------------------------------------------------------------------------------ reverse walk
 
 template <int DK, int NP> struct RevStage {
-    static constexpr int NT = NP == 1 ? 2 : 3;
-    bf16 k[NP][kC * (DK + kPad)], q[NP][kC * (DK + kPad)];
-    bf16 tri[NT][kC * kLd], p[NT][kC * kLd];
-    bf16 go[NP][kC * kLd], v[NP][kC * kLd];
+    static constexpr int NT = NP == 1 ? 2 : 3, VLD = 16 * kRowGroups<NP> + kPad;
+    bf16 k[NP][kC * (DK + kPad)], tri[NT][kC * kLd], v[NP][kC * VLD];
     float coef[kCoef][kC];
 };
-template <int DK, int NP> constexpr int kRevStages = sizeof(RevStage<DK, NP>) * 2 <= 227 * 1024 ? 2 : 1;
+template <int DK, int NP> struct RevSide {
+    static constexpr int NT = NP == 1 ? 2 : 3, VLD = 16 * kRowGroups<NP> + kPad;
+    bf16 q[NP][kC * (DK + kPad)], p[NT][kC * kLd], go[NP][kC * VLD];
+    float coef[kCoef][kC];
+};
+// From side to chain warp, as accumulators: dO^T P and (scale e^G dO)^T Q.
+template <int DK> struct RevSwap {
+    float4 u[8 * 32], d[DK / 8 * 32];
+};
+template <int DK, int NP> struct RevPlan {
+    static constexpr int RG = kRowGroups<NP>, threads = 64 * RG;
+    static constexpr size_t chain = sizeof(RevStage<DK, NP>), side = sizeof(RevSide<DK, NP>), swap = sizeof(RevSwap<DK>) * RG;
+    static constexpr Stages n = fit_stages(chain, side, swap);
+    static constexpr size_t smem = chain * n.chain + side * n.side + swap * n.swap;
+    static_assert(smem <= 227 * 1024, "fits an SM");
+};
 
 template <int DK, int NP>
-__device__ __forceinline__ void rev_load(const ChunkParams &P, RevStage<DK, NP> &st, int bh, int c, int vb, int vcols)
+__device__ __forceinline__ void rev_load(const ChunkParams &P, RevStage<DK, NP> &st, int bh, int c, int v0, int vcols)
 {
-    constexpr int NT = NP == 1 ? 2 : 3;
+    constexpr int NT = NP == 1 ? 2 : 3, TH = 32 * kRowGroups<NP>, VW = 16 * kRowGroups<NP>;
     const long long t0 = (long long)c * kC, nc = (long long)bh * P.chunks + c;
-    const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC, lane = threadIdx.x % 32;
+    const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
 #pragma unroll
     for (int i = 0; i < NP; i++) {
-        load_tile<kC, DK, 32>(st.k[i], P.k.at + i * P.k.plane + q_base(P, P.k, bh, t0), P.k.stride_t, rows, P.Dk);
-        load_tile<kC, kC, 32>(st.go[i], P.go.at + i * P.go.plane + v_base(P, P.go, bh, t0) + vb * kC, P.go.stride_t, rows, vcols);
-        load_tile<kC, DK, 32>(st.q[i], P.q.at + i * P.q.plane + q_base(P, P.q, bh, t0), P.q.stride_t, rows, P.Dk);
-        load_tile<kC, kC, 32>(st.v[i], P.v.at + i * P.v.plane + v_base(P, P.v, bh, t0) + vb * kC, P.v.stride_t, rows, vcols);
+        load_tile<kC, DK, TH>(st.k[i], P.k.at + i * P.k.plane + q_base(P, P.k, bh, t0), P.k.stride_t, rows, P.Dk);
+        load_tile<kC, VW, TH>(st.v[i], P.v.at + i * P.v.plane + v_base(P, P.v, bh, t0) + v0, P.v.stride_t, rows, vcols);
     }
 #pragma unroll
-    for (int i = 0; i < NT; i++) {
-        load_dense<32>(st.tri[i], P.tri + (nc * NT + i) * kTile);
-        load_dense<32>(st.p[i], P.p + (nc * NT + i) * kTile);
+    for (int i = 0; i < NT; i++) load_dense<TH>(st.tri[i], P.tri + (nc * NT + i) * kTile);
+    for (int i = threadIdx.x % TH; i < kCoef * kC / 4; i += TH) cp16(smem_addr(&st.coef[0][0]) + i * 16, P.coef + nc * (kCoef * kC) + i * 4, true);
+    cp_commit();
+}
+template <int DK, int NP>
+__device__ __forceinline__ void rev_side_load(const ChunkParams &P, RevSide<DK, NP> &st, int bh, int c, int v0, int vcols)
+{
+    constexpr int NT = NP == 1 ? 2 : 3, TH = 32 * kRowGroups<NP>, VW = 16 * kRowGroups<NP>;
+    const long long t0 = (long long)c * kC, nc = (long long)bh * P.chunks + c;
+    const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
+#pragma unroll
+    for (int i = 0; i < NP; i++) {
+        load_tile<kC, DK, TH>(st.q[i], P.q.at + i * P.q.plane + q_base(P, P.q, bh, t0), P.q.stride_t, rows, P.Dk);
+        load_tile<kC, VW, TH>(st.go[i], P.go.at + i * P.go.plane + v_base(P, P.go, bh, t0) + v0, P.go.stride_t, rows, vcols);
     }
 #pragma unroll
-    for (int i = 0; i < 3; i++)
-        if (i * 32 + lane < kCoef * kC / 4) cp16(smem_addr(&st.coef[0][0]) + (i * 32 + lane) * 16, P.coef + nc * (kCoef * kC) + (i * 32 + lane) * 4, true);
+    for (int i = 0; i < NT; i++) load_dense<TH>(st.p[i], P.p + (nc * NT + i) * kTile);
+    for (int i = threadIdx.x % TH; i < kCoef * kC / 4; i += TH) cp16(smem_addr(&st.coef[0][0]) + i * 16, P.coef + nc * (kCoef * kC) + i * 4, true);
     cp_commit();
 }
 
 // SUMMARY: only the adjoint that a segment's own outputs send to its start.
 template <int DK, int NP, bool SUMMARY, class T>
-__global__ void __launch_bounds__(kWalkThreads, 1) delta_reverse_kernel(const ChunkParams P)
+__global__ void __launch_bounds__((RevPlan<DK, NP>::threads), 1) delta_reverse_kernel(const ChunkParams P)
 {
-    constexpr int STAGES = kRevStages<DK, NP>, ld = DK + kPad, NT = NP == 1 ? 2 : 3;
+    using Plan = RevPlan<DK, NP>;
+    constexpr int ld = DK + kPad, NT = NP == 1 ? 2 : 3, RG = Plan::RG, VW = 16 * RG, VLD = VW + kPad, CS = Plan::n.chain, SS = Plan::n.side, WS = Plan::n.swap;
+    constexpr int PAIR = 64 * RG, ONE = 32 * RG;
     extern __shared__ __align__(16) unsigned char raw[];
     auto *stages = reinterpret_cast<RevStage<DK, NP> *>(raw);
-    const int bh = blockIdx.x, vb = blockIdx.y, seg = blockIdx.z;
-    const int lane = threadIdx.x % 32, w = threadIdx.x / 32, gr = lane / 4, tc = lane % 4 * 2;
-    const int r0 = vb * kC, vcols = P.Dv - r0 < kC ? P.Dv - r0 : kC;
-    const int c0 = seg * P.seg_chunks, c1 = c0 + P.seg_chunks < P.chunks ? c0 + P.seg_chunks : P.chunks;
+    auto *tiles = reinterpret_cast<RevSide<DK, NP> *>(raw + Plan::chain * CS);
+    auto *swaps = reinterpret_cast<RevSwap<DK> *>(raw + Plan::chain * CS + Plan::side * SS);
+    const int bh = blockIdx.x, seg = blockIdx.z;
+    const int r0 = blockIdx.y * VW, vcols = P.Dv - r0 < VW ? P.Dv - r0 : VW;
+    const int c0 = seg * P.seg_chunks, c1 = c0 + P.seg_chunks < P.chunks ? c0 + P.seg_chunks : P.chunks, count = c1 - c0;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, w = warp % RG, gr = lane / 4, tc = lane % 4 * 2;
+    const int w4 = (r0 / 16 + w) % 4;
 
-    if (w == 4) {               // producer, as in the forward's walk
-        for (int c = c1 - 1; c >= c0; c--) {
-            const int s = (c1 - 1 - c) % STAGES;
-            if (c1 - 1 - c >= STAGES) bar_sync(3 + s);
-            rev_load<DK, NP>(P, stages[s], bh, c, vb, vcols);
-            cp_wait<0>();
-            bar_arrive(1 + s);
+    if (warp >= RG) {       // -------------------------------------------------- side warps: tiles, and what does not need D
+        rev_side_load<DK, NP>(P, tiles[0], bh, c1 - 1, r0, vcols);
+        rev_load<DK, NP>(P, stages[0], bh, c1 - 1, r0, vcols);
+        for (int i = 0; i < count; i++) {
+            const int c = c1 - 1 - i, cs = i % CS, par = i % WS;
+            auto &st = tiles[i % SS];
+            auto &sw = swaps[par * RG + w];
+            const unsigned qs = smem_addr(st.q[0]), ps = smem_addr(st.p[0]), gs = smem_addr(st.go[0]);
+            // The side's tiles of this chunk were asked for before the chain's (SS = 2), which may still be on
+            // their way until the chain is about to need them.
+            if (SS == 2 && CS == 2) cp_wait<1>(); else cp_wait<0>();
+            bar_sync(BAR_SIDE, ONE);            // the tiles are here, and the previous chunk's are done with
+            if (SS == 2) {
+                if (i + 1 < count) rev_side_load<DK, NP>(P, tiles[(i + 1) % SS], bh, c - 1, r0, vcols);
+                else cp_commit();               // an empty group keeps the count
+            }
+            // dO^T P
+            float U[8][4] = {};
+            triangle<NP, NT, true, true>(U,
+                [&](unsigned (&a)[NP][4], int ib) { load_left<NP, true>(a, at_nk(gs, VLD, 16 * ib, 16 * w), kC * VLD); },
+                [&](int ib, int nb) { return at_kn(ps, kLd, 16 * ib, 16 * nb); }, kC * kLd);
+            if (CS == 2 || i == 0) {            // the chain's tiles
+                if (SS == 2) cp_wait<1>(); else cp_wait<0>();
+                bar_arrive(BAR_FULL + cs, PAIR);
+            }
+            // (scale e^G dO)^T Q
+            unsigned a[4][3][4];
+#pragma unroll
+            for (int tb = 0; tb < 4; tb++) {
+                unsigned x[NP][4];
+                load_left<NP, true>(x, at_nk(gs, VLD, 16 * tb, 16 * w), kC * VLD);
+                float y[2][4];
+#pragma unroll
+                for (int m = 0; m < 2; m++) {
+                    const float2 e = *reinterpret_cast<const float2 *>(&st.coef[COEF_EG][16 * tb + 8 * m + tc]);
+                    const f32x2 plus = pair(P.scale * e.x, P.scale * e.y);
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        const float2 z = halves(mul2(plus, pair(sum_terms(x, 2 * m + h))));
+                        y[m][2 * h] = z.x;
+                        y[m][2 * h + 1] = z.y;
+                    }
+                }
+                as_left(y[0], y[1], a[tb]);
+            }
+            float D[DK / 8][4] = {};
+#pragma unroll
+            for (int tb = 0; tb < 4; tb++)
+#pragma unroll
+                for (int nb = 0; nb < DK / 16; nb += 2) {
+                    unsigned b[2][NP][4];
+#pragma unroll
+                    for (int k = 0; k < 2; k++) load_right<NP, true>(b[k], at_kn(qs, ld, 16 * tb, 16 * (nb + k)), kC * ld);
+                    multiply<3, NP, 2>(reinterpret_cast<float (&)[4][4]>(D[2 * nb]), a[tb], b);
+                }
+            if (i >= WS) bar_sync(BAR_FREE + par, PAIR);
+#pragma unroll
+            for (int n = 0; n < 8; n++) sw.u[n * 32 + lane] = make_float4(U[n][0], U[n][1], U[n][2], U[n][3]);
+#pragma unroll
+            for (int n = 0; n < DK / 8; n++) sw.d[n * 32 + lane] = make_float4(D[n][0], D[n][1], D[n][2], D[n][3]);
+            bar_arrive(BAR_READY + par, PAIR);
+            if (i + 1 < count) {                // the chain's next tiles
+                const int ns = (i + 1) % CS;
+                if (i + 1 >= CS) bar_sync(BAR_EMPTY + ns, PAIR);
+                rev_load<DK, NP>(P, stages[ns], bh, c - 1, r0, vcols);
+                if (CS == 1) {
+                    cp_wait<0>();
+                    bar_arrive(BAR_FULL, PAIR);
+                }
+                if (SS == 1) {
+                    bar_sync(BAR_SIDE, ONE);
+                    rev_side_load<DK, NP>(P, tiles[0], bh, c - 1, r0, vcols);
+                }
+            }
         }
         return;
     }
 
+    // -------------------------------------------------------------------------- chain warps
     const int row[2] = {r0 + 16 * w + gr, r0 + 16 * w + gr + 8};
     float D[DK / 8][4];
     const float *from = SUMMARY ? nullptr
@@ -96,18 +190,18 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_reverse_kernel(const Ch
             D[n][2 * h + 1] = x.y;
         }
 
-    for (int c = c1 - 1; c >= c0; c--) {
-        const int s = (c1 - 1 - c) % STAGES;
+    for (int i = 0; i < count; i++) {
+        const int c = c1 - 1 - i, s = i % CS, par = i % WS;
         auto &st = stages[s];
-        const long long t0 = (long long)c * kC, nc = (long long)bh * P.chunks + c, nv = nc * P.vblocks + vb;
-        const unsigned ks = smem_addr(st.k[0]), qs = smem_addr(st.q[0]), ts = smem_addr(st.tri[0]), ps = smem_addr(st.p[0]);
-        const unsigned gs = smem_addr(st.go[0]), vs = smem_addr(st.v[0]);
+        const auto &sw = swaps[par * RG + w];
+        const long long t0 = (long long)c * kC, nc = (long long)bh * P.chunks + c, nv = nc * P.vblocks + r0 / kC;
+        const unsigned ks = smem_addr(st.k[0]), ts = smem_addr(st.tri[0]), vs = smem_addr(st.v[0]);
 
         // <state after the chunk, D>; D for the chunk's own gradients
         if constexpr (!SUMMARY) {
             const long long after = c + 1 < P.chunks ? nc + 1 : (long long)P.B * P.Hv * P.chunks + bh;
-            const float4 *sf = P.sf + ((after * P.vblocks + vb) * 4 + w) * (DK / 8 * 32) + lane;
-            bf16 *dst = P.ds + nv * (NP * kC * DK) + (16 * w + gr) * DK + tc;
+            const float4 *sf = P.sf + ((after * P.vblocks + r0 / kC) * 4 + w4) * (DK / 8 * 32) + lane;
+            bf16 *dst = P.ds + nv * (NP * kC * DK) + (16 * w4 + gr) * DK + tc;
             float dot = 0.f;
 #pragma unroll
             for (int n = 0; n < DK / 8; n++) {
@@ -118,148 +212,132 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_reverse_kernel(const Ch
                     unsigned y[NP];
                     split(D[n][2 * h], D[n][2 * h + 1], y);
 #pragma unroll
-                    for (int i = 0; i < NP; i++) *reinterpret_cast<unsigned *>(dst + i * (kC * DK) + 8 * h * DK + 8 * n) = y[i];
+                    for (int j = 0; j < NP; j++) *reinterpret_cast<unsigned *>(dst + j * (kC * DK) + 8 * h * DK + 8 * n) = y[j];
                 }
             }
 #pragma unroll
             for (int o = 16; o > 0; o /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-            if (lane == 0) P.sd[nv * 4 + w] = dot;
+            if (lane == 0) P.sd[nv * 4 + w4] = dot;
         }
-        float4 rf[8];               // r, fetched long before its use
-#pragma unroll
-        for (int n = 0; n < 8; n++)
-            if (!SUMMARY) rf[n] = P.rf[((nv * 4 + w) * 8 + n) * 32 + lane];
-        bar_sync(1 + s);
-        // X = e^{G_C - G} (D K^T) + dO^T P
+        bar_sync(BAR_FULL + s, PAIR);
+        // X = beta (e^{G_C - G} (D K^T) + dO^T P)
         float X[8][4] = {};
 #pragma unroll
         for (int d = 0; d < DK / 16; d++) {
-            unsigned x[3][4];
-            as_left(D[2 * d], D[2 * d + 1], x);
+            unsigned a[3][4], b[4][NP][4];
 #pragma unroll
-            for (int nb = 0; nb < 4; nb++) product<3, NP, false>(X[2 * nb], X[2 * nb + 1], x, at_nk(ks, ld, 16 * nb, 16 * d), kC * ld);
+            for (int j = 0; j < 4; j++) load_right<NP, false>(b[j], at_nk(ks, ld, 16 * j, 16 * d), kC * ld);
+            as_left(D[2 * d], D[2 * d + 1], a);
+            multiply<3, NP, 4>(X, a, b);
         }
-#pragma unroll
-        for (int n = 0; n < 8; n++) {
-            const f32x2 lf = pair(*reinterpret_cast<const float2 *>(&st.coef[COEF_LEFT][8 * n + tc]));
-            scale_row(X[n], 0, lf);
-            scale_row(X[n], 1, lf);
-        }
-#pragma unroll
-        for (int ib = 0; ib < 4; ib++) {
-            unsigned x[NP][4];
-            load_left<NP, true>(x, at_nk(gs, kLd, 16 * ib, 16 * w), kC * kLd);
-#pragma unroll
-            for (int nb = 0; nb <= ib; nb++) product<NP, NT, true>(X[2 * nb], X[2 * nb + 1], x, at_kn(ps, kLd, 16 * ib, 16 * nb), kC * kLd);
-        }
-        // rb = (I + (T - I)^T) (beta dU)
+        bar_sync(BAR_READY + par, PAIR);
         float rb[8][4];
 #pragma unroll
         for (int n = 0; n < 8; n++) {
-            const f32x2 bt = pair(*reinterpret_cast<const float2 *>(&st.coef[COEF_BETA][8 * n + tc]));
+            const int t = 8 * n + tc;
+            const f32x2 lf = pair(*reinterpret_cast<const float2 *>(&st.coef[COEF_LEFT][t])), bt = pair(*reinterpret_cast<const float2 *>(&st.coef[COEF_BETA][t]));
+            const float4 u = sw.u[n * 32 + lane];
+            fma_row(X[n], 0, lf, pair(u.x, u.y));
+            fma_row(X[n], 1, lf, pair(u.z, u.w));
             scale_row(X[n], 0, bt);
             scale_row(X[n], 1, bt);
 #pragma unroll
             for (int e = 0; e < 4; e++) rb[n][e] = X[n][e];
         }
-#pragma unroll
-        for (int ib = 0; ib < 4; ib++) {
-            unsigned x[3][4];
-            as_left(X[2 * ib], X[2 * ib + 1], x);
-#pragma unroll
-            for (int nb = 0; nb <= ib; nb++) product<3, NT, false>(rb[2 * nb], rb[2 * nb + 1], x, at_nk(ts, kLd, 16 * nb, 16 * ib), kC * kLd);
-        }
-        // rb.r and rb.v over this warp's 16 values
+        // rb = X + (T - I)^T X
+        triangle<3, NT, false, true>(rb, [&](unsigned (&a)[3][4], int ib) { as_left(X[2 * ib], X[2 * ib + 1], a); },
+                                     [&](int ib, int nb) { return at_nk(ts, kLd, 16 * nb, 16 * ib); }, kC * kLd);
         if constexpr (!SUMMARY) {
+            // rb.r and rb.v over this row group's 16 values
             float dots[8][4];
 #pragma unroll
             for (int nb = 0; nb < 4; nb++) {
                 unsigned x[NP][4];
-                load_left<NP, true>(x, at_nk(vs, kLd, 16 * nb, 16 * w), kC * kLd);
+                load_left<NP, true>(x, at_nk(vs, VLD, 16 * nb, 16 * w), kC * VLD);
 #pragma unroll
                 for (int m = 0; m < 2; m++) {
                     const int n = 2 * nb + m;
+                    const float4 r = P.rf[((nv * 4 + w4) * 8 + n) * 32 + lane];
                     const float2 a = sum_terms(x, 2 * m), b = sum_terms(x, 2 * m + 1);
-                    dots[n][0] = fmaf(rb[n][0], rf[n].x, rb[n][2] * rf[n].z);
-                    dots[n][1] = fmaf(rb[n][1], rf[n].y, rb[n][3] * rf[n].w);
+                    dots[n][0] = fmaf(rb[n][0], r.x, rb[n][2] * r.z);
+                    dots[n][1] = fmaf(rb[n][1], r.y, rb[n][3] * r.w);
                     dots[n][2] = fmaf(rb[n][0], a.x, rb[n][2] * b.x);
                     dots[n][3] = fmaf(rb[n][1], a.y, rb[n][3] * b.y);
                 }
             }
             column_sums(dots);
-            float *to = P.rd + (nv * 4 + w) * (2 * kC) + 8 * gr + tc;
+            float *to = P.rd + (nv * 4 + w4) * (2 * kC) + 8 * gr + tc;
             *reinterpret_cast<float2 *>(to) = make_float2(dots[0][0], dots[0][1]);
             *reinterpret_cast<float2 *>(to + kC) = make_float2(dots[0][2], dots[0][3]);
-        }
-        // rb as token rows, through this warp's own columns of the V tile: dV (bfloat16: the first term is
-        // the rounded value), or its terms for the chunk's gradients
-        const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
+            // rb as token rows, through this warp's own part of the V tile: dV (bfloat16: the first term is the
+            // rounded value), or its terms for the chunk's gradients
+            const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
 #pragma unroll
-        for (int term = 0; term < (SUMMARY ? 0 : NP); term++) {
-            bf16 *dst = NP == 1 ? static_cast<bf16 *>(P.o) : P.rbt + term * P.rb.plane;
-            dst += v_base(P, P.rb, bh, t0) + r0;
-            __syncwarp();
+            for (int term = 0; term < NP; term++) {
+                bf16 *dst = NP == 1 ? static_cast<bf16 *>(P.o) : P.rbt + term * P.rb.plane;
+                dst += v_base(P, P.rb, bh, t0) + r0;
+                __syncwarp();
 #pragma unroll
-            for (int nb = 0; nb < 4; nb++) {
-                unsigned x[NP][4];
-                as_left(rb[2 * nb], rb[2 * nb + 1], x);
-                stsm_t(at_nk(vs, kLd, 16 * nb, 16 * w), x[term][0], x[term][1], x[term][2], x[term][3]);
-            }
-            __syncwarp();
-#pragma unroll
-            for (int i = lane; i < 128; i += 32) {
-                const int t = i / 2, v = 16 * w + i % 2 * 8;
-                if (t < rows && v < vcols)
-                    *reinterpret_cast<uint4 *>(dst + t * P.rb.stride_t + v) = *reinterpret_cast<const uint4 *>(&st.v[0][t * kLd + v]);
-            }
-        }
-        if constexpr (sizeof(T) == 4 && !SUMMARY) {
-            T *gv = static_cast<T *>(P.o) + v_base(P, P.rb, bh, t0) + r0;
-#pragma unroll
-            for (int n = 0; n < 8; n++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const int t = 8 * n + tc + (e & 1), v = 16 * w + gr + (e >> 1) * 8;
-                    if (t < rows && v < vcols) gv[t * P.rb.stride_t + v] = narrow<T>(rb[n][e]);
+                for (int nb = 0; nb < 4; nb++) {
+                    unsigned x[NP][4];
+                    as_left(rb[2 * nb], rb[2 * nb + 1], x);
+                    stsm_t(at_nk(vs, VLD, 16 * nb, 16 * w), x[term][0], x[term][1], x[term][2], x[term][3]);
                 }
+                __syncwarp();
+#pragma unroll
+                for (int j = lane; j < 128; j += 32) {
+                    const int t = j / 2, v = 16 * w + j % 2 * 8;
+                    if (t < rows && v < vcols)
+                        *reinterpret_cast<uint4 *>(dst + t * P.rb.stride_t + v) = *reinterpret_cast<const uint4 *>(&st.v[0][t * VLD + v]);
+                }
+            }
+            if constexpr (sizeof(T) == 4) {
+                T *gv = static_cast<T *>(P.o) + v_base(P, P.rb, bh, t0) + r0;
+#pragma unroll
+                for (int n = 0; n < 8; n++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const int t = 8 * n + tc + (e & 1), v = 16 * w + gr + (e >> 1) * 8;
+                        if (t < rows && v < vcols) gv[t * P.rb.stride_t + v] = narrow<T>(rb[n][e]);
+                    }
+            }
         }
-        // D <- e^{G_C} D + (scale e^G dO)^T Q - (e^G rb)^T K, the update summed from zero as in the forward
+        // D <- e^{G_C} D + (scale e^G dO)^T Q - (e^G rb)^T K, the update summed apart as in the forward
         const float eC = st.coef[COEF_EG][kC - 1];
-        unsigned a[4][3][4], f[4][3][4];
+        unsigned f[4][3][4];
 #pragma unroll
         for (int tb = 0; tb < 4; tb++) {
-            unsigned x[NP][4];
-            load_left<NP, true>(x, at_nk(gs, kLd, 16 * tb, 16 * w), kC * kLd);
-            float y[2][4];
 #pragma unroll
             for (int m = 0; m < 2; m++) {
                 const float2 e = *reinterpret_cast<const float2 *>(&st.coef[COEF_EG][16 * tb + 8 * m + tc]);
-                const f32x2 plus = pair(P.scale * e.x, P.scale * e.y), minus = pair(-e.x, -e.y);
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    const float2 z = halves(mul2(plus, pair(sum_terms(x, 2 * m + h))));
-                    y[m][2 * h] = z.x;
-                    y[m][2 * h + 1] = z.y;
-                    scale_row(rb[2 * tb + m], h, minus);
-                }
+                const f32x2 minus = pair(-e.x, -e.y);
+                scale_row(rb[2 * tb + m], 0, minus);
+                scale_row(rb[2 * tb + m], 1, minus);
             }
-            as_left(y[0], y[1], a[tb]);
             as_left(rb[2 * tb], rb[2 * tb + 1], f[tb]);
         }
 #pragma unroll
-        for (int nb = 0; nb < DK / 16; nb++) {
-            float x[2][4] = {};
+        for (int nb = 0; nb < DK / 16; nb += 2) {
+            float x[4][4];
 #pragma unroll
-            for (int tb = 0; tb < 4; tb++) {
-                product<3, NP, true>(x[0], x[1], a[tb], at_kn(qs, ld, 16 * tb, 16 * nb), kC * ld);
-                product<3, NP, true>(x[0], x[1], f[tb], at_kn(ks, ld, 16 * tb, 16 * nb), kC * ld);
+            for (int m = 0; m < 4; m++) {
+                const float4 d = sw.d[(2 * nb + m) * 32 + lane];
+                x[m][0] = d.x; x[m][1] = d.y; x[m][2] = d.z; x[m][3] = d.w;
             }
 #pragma unroll
-            for (int m = 0; m < 2; m++)
+            for (int tb = 0; tb < 4; tb++) {
+                unsigned b[2][NP][4];
+#pragma unroll
+                for (int k = 0; k < 2; k++) load_right<NP, true>(b[k], at_kn(ks, ld, 16 * tb, 16 * (nb + k)), kC * ld);
+                multiply<3, NP, 2>(x, f[tb], b);
+            }
+#pragma unroll
+            for (int m = 0; m < 4; m++)
 #pragma unroll
                 for (int h = 0; h < 2; h++) fma_row(D[2 * nb + m], h, pair(eC, eC), pair(x[m][2 * h], x[m][2 * h + 1]));
         }
-        if (c - STAGES >= c0) bar_arrive(3 + s);
+        if (i + WS < count) bar_arrive(BAR_FREE + par, PAIR);
+        if (i + CS < count) bar_arrive(BAR_EMPTY + s, PAIR);
     }
     float *to = SUMMARY ? P.seg_end + ((long long)bh * P.segs + seg) * P.Dv * P.Dk
                 : P.state_out != nullptr && seg == 0 ? P.state_out + (long long)bh * P.Dv * P.Dk : nullptr;
@@ -334,9 +412,9 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
             for (int i = 0; i < NP; i++) {
                 load_tile<kC, VW, 256>(sm.v.go[i], P.go.at + i * P.go.plane + v_base(P, P.go, bh, t0) + v0, P.go.stride_t, rows, vcols);
                 load_tile<kC, VW, 256>(sm.v.rb[i], P.rb.at + i * P.rb.plane + v_base(P, P.rb, bh, t0) + v0, P.rb.stride_t, rows, vcols);
-                load_tile<kC, VW, 256>(sm.v.u[i], P.u + (nv * NP + i) * kTile + in, kC, kC, VW);
-                load_tile<VW, DK, 256>(sm.v.s0[i], P.s0 + (nv * NP + i) * (kC * DK) + in * DK, DK, VW, DK);
-                load_tile<VW, DK, 256>(sm.v.ds[i], P.ds + (nv * NP + i) * (kC * DK) + in * DK, DK, VW, DK);
+                load_tile<kC, VW, 256>(sm.v.u[i], P.u + (nv * NP + i) * kTile + in, kC, kC, vcols);
+                load_tile<VW, DK, 256>(sm.v.s0[i], P.s0 + (nv * NP + i) * (kC * DK) + in * DK, DK, vcols, DK);
+                load_tile<VW, DK, 256>(sm.v.ds[i], P.ds + (nv * NP + i) * (kC * DK) + in * DK, DK, vcols, DK);
             }
             cp_commit();
             cp_wait<0>();
@@ -432,11 +510,12 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
         if (warp == 0) {
             float dG[2], end = 0.f;
             const long long at = ((long long)b * P.L + t0) * P.Hv + bh % P.Hv;
+            const long long g0 = nc * P.vblocks * 4, g1 = g0 + (P.Dv + 15) / 16;       // row groups of this chunk
 #pragma unroll
             for (int e = 0; e < 2; e++) {
                 const int t = 2 * lane + e;
                 float od = 0.f, rr = 0.f, rv = 0.f;
-                for (long long i = nc * P.vblocks * 4; i < (nc + 1) * P.vblocks * 4; i++) {
+                for (long long i = g0; i < g1; i++) {
                     od += P.od[i * kC + t];
                     rr += P.rd[i * (2 * kC) + t];
                     rv += P.rd[i * (2 * kC) + kC + t];
@@ -444,7 +523,7 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
                 dG[e] = od - rv;
                 if (t < rows) P.gbeta[at + (long long)t * P.Hv] = rr / sm.coef[COEF_BETA][t];
             }
-            for (long long i = nc * P.vblocks * 4; i < (nc + 1) * P.vblocks * 4; i++) end += P.sd[i];
+            for (long long i = g0; i < g1; i++) end += P.sd[i];
             float run = dG[0] + dG[1];      // suffix sums
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
@@ -481,12 +560,12 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
 template <int DK, int NP, bool SUMMARY> cudaError_t walk(const ChunkParams &P, cudaStream_t st)
 {
     using T = typename std::conditional<NP == 1, bf16, float>::type;
-    const size_t smem = sizeof(RevStage<DK, NP>) * kRevStages<DK, NP>;
-    static_assert(sizeof(RevStage<DK, NP>) <= 227 * 1024, "fits an SM");
+    using Plan = RevPlan<DK, NP>;
     auto *kernel = delta_reverse_kernel<DK, NP, SUMMARY, T>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan::smem);
     if (e != cudaSuccess) return e;
-    return launch(kernel, dim3((unsigned)(P.B * P.Hv), P.vblocks, P.segs), dim3(kWalkThreads), smem, st, P);
+    constexpr int VW = 16 * Plan::RG;
+    return launch(kernel, dim3((unsigned)(P.B * P.Hv), (P.Dv + VW - 1) / VW, P.segs), dim3(Plan::threads), Plan::smem, st, P);
 }
 
 template <int DK, int NP> cudaError_t reverse(const ChunkParams &P, cudaStream_t st)

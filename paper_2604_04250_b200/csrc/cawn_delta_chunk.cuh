@@ -13,11 +13,14 @@
 // 5e-6 and the gradient of g by up to 2e-5, too near to or past what a user of float expects.)  NP: terms of
 // inputs (1 or 3), NT: terms of T and P (2 or 3).
 //
-// Layout.  Sequential kernels work on transposed chunks: a warp owns 16 rows of values v and all keys,
-// so that every product of the chain (state x keys, triangle, update) has the previous result as its
-// left factor.  The accumulator layout of mma.m16n8k16 is the layout of its left operand, so the chain
-// stays in registers, with no barrier and no shared-memory round trip between its products; the right
-// factors (K, Q, T, P tiles) are the same for all warps and come from shared memory.
+// Layout of the walks.  They work on transposed chunks: a row group is 16 rows of values against all keys and
+// tokens, so that every product of the chain (state x keys, triangle, update) has the previous result as its left
+// factor.  The accumulator layout of mma.m16n8k16 is the layout of that operand: the chain stays in one warp's
+// registers.  The right factors (K, Q, T, P tiles) come from shared memory.  Two kinds of warps:
+// chain warps do what the next chunk waits for; side warps, one per chain warp on the same scheduler, fetch
+// all tiles (cp.async) and do what hangs off the chain (the forward's outputs) or can be done ahead of it (the
+// backward's terms without D), which fills the chain's waits.  (Two warps sharing a row group's chain were slower: handing
+// fragments over doubled the shared-memory traffic.)
 #pragma once
 #include "cawn_delta.cuh"
 
@@ -190,13 +193,43 @@ __device__ __forceinline__ float exp2_fast(float x)
     return r;
 }
 
-// Barriers of the walks: four consumer warps, one producer warp.
-constexpr int kWalkThreads = 160;
-__device__ __forceinline__ void bar_sync(int id) { asm volatile("bar.sync %0, %1;" :: "r"(id), "n"(kWalkThreads) : "memory"); }
-__device__ __forceinline__ void bar_arrive(int id) { asm volatile("bar.arrive %0, %1;" :: "r"(id), "n"(kWalkThreads) : "memory"); }
+// Barriers of the walks, `threads` of both sides together: chain tiles are here / free again, what passes between chain
+// and side is here / free again, and one among the side warps.
+enum { BAR_FULL = 1, BAR_EMPTY = 3, BAR_READY = 5, BAR_FREE = 7, BAR_SIDE = 9 };    // the first four: + stage or parity
+__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" :: "r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ void bar_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" :: "r"(id), "r"(threads) : "memory"); }
 
-// Sums over the eight lanes that share a column pair, for N pairs of each of the eight tiles; lane row gr
-// ends with the sums of tile gr in v[0].
+// Row groups of a block: float storage has three times the tiles, so half the row groups fit.
+template <int NP> constexpr int kRowGroups = NP == 1 ? 4 : 2;
+
+// Stages of the chain's and the side's tiles and of what they exchange: as many as fit.
+struct Stages { int chain, side, swap; };
+constexpr Stages fit_stages(size_t chain, size_t side, size_t swap)
+{
+    const size_t room = 227 * 1024;
+    if (2 * (chain + side + swap) <= room) return {2, 2, 2};
+    if (2 * chain + side + 2 * swap <= room) return {2, 1, 2};
+    if (2 * chain + side + swap <= room) return {2, 1, 1};
+    return {1, 1, 1};
+}
+
+// Fragments handed from warp to warp: N terms of left operand number i.
+template <int N> __device__ __forceinline__ void put_left(uint4 *buf, int i, const unsigned (&a)[N][4])
+{
+#pragma unroll
+    for (int t = 0; t < N; t++) buf[(i * N + t) * 32 + threadIdx.x % 32] = make_uint4(a[t][0], a[t][1], a[t][2], a[t][3]);
+}
+template <int N> __device__ __forceinline__ void get_left(unsigned (&a)[N][4], const uint4 *buf, int i)
+{
+#pragma unroll
+    for (int t = 0; t < N; t++) {
+        const uint4 v = buf[(i * N + t) * 32 + threadIdx.x % 32];
+        a[t][0] = v.x; a[t][1] = v.y; a[t][2] = v.z; a[t][3] = v.w;
+    }
+}
+
+// Sums over the eight lanes that share a column pair, for N values of each of eight tiles; lane row gr ends with the
+// sums of tile gr in v[0].
 template <int N> __device__ __forceinline__ void column_sums(float (&v)[8][N])
 {
     const int gr = threadIdx.x % 32 / 4;
@@ -266,23 +299,76 @@ template <int AP, bool TRANS> __device__ __forceinline__ void load_left(unsigned
         if (TRANS) ldsm_t(a[i], addr + i * plane * 2); else ldsm(a[i], addr + i * plane * 2);
 }
 
-// Two 16 x 8 tiles += left (AP terms) x right (BP terms in shared planes `plane` elements apart); TRANS as
-// ldsm_t.  Pairs of terms beyond the precision of the longer operand are left out: 2 x 2 terms take three
-// products, 3 x 3 six.
+// Right operand of a 16 x 16 block, BP terms in shared planes `plane` elements apart; TRANS as ldsm_t.
+template <int BP, bool TRANS> __device__ __forceinline__ void load_right(unsigned (&b)[BP][4], unsigned addr, int plane)
+{
+#pragma unroll
+    for (int j = 0; j < BP; j++)
+        if (TRANS) ldsm_t(b[j], addr + j * plane * 2); else ldsm(b[j], addr + j * plane * 2);
+}
+
+// Tiles 2 i, 2 i + 1 += left (AP terms) x right block i (BP terms), N blocks.  Pairs of terms
+// beyond the precision of the longer operand are left out: 2 x 2 terms take three products, 3 x 3 six.  Blocks
+// are the inner loop: a product waits 21 cycles for the sum before it but issues every 8.
+template <int AP, int BP, int N>
+__device__ __forceinline__ void multiply(float (&c)[2 * N][4], const unsigned (&a)[AP][4], const unsigned (&b)[N][BP][4])
+{
+    constexpr int ORDER = AP > BP ? AP : BP;
+#pragma unroll
+    for (int j = 0; j < BP; j++)
+#pragma unroll
+        for (int i = 0; i < AP; i++)
+            if (i + j < ORDER)
+#pragma unroll
+                for (int n = 0; n < N; n++) {
+                    mma(c[2 * n], a[i], b[n][j][0], b[n][j][1]);
+                    mma(c[2 * n + 1], a[i], b[n][j][2], b[n][j][3]);
+                }
+}
+
+// One block at a time
 template <int AP, int BP, bool TRANS>
 __device__ __forceinline__ void product(float (&c0)[4], float (&c1)[4], const unsigned (&a)[AP][4], unsigned addr, int plane)
 {
     constexpr int ORDER = AP > BP ? AP : BP;
+    unsigned b[BP][4];
+    load_right<BP, TRANS>(b, addr, plane);
 #pragma unroll
-    for (int j = 0; j < BP; j++) {
-        unsigned b[4];
-        if (TRANS) ldsm_t(b, addr + j * plane * 2); else ldsm(b, addr + j * plane * 2);
+    for (int j = 0; j < BP; j++)
 #pragma unroll
         for (int i = 0; i < AP; i++)
             if (i + j < ORDER) {
-                mma(c0, a[i], b[0], b[1]);
-                mma(c1, a[i], b[2], b[3]);
+                mma(c0, a[i], b[j][0], b[j][1]);
+                mma(c1, a[i], b[j][2], b[j][3]);
             }
+}
+
+// C (token tiles of 8, in 16-row blocks) += chain of 16-token blocks A_b x right blocks, on and below the triangle's
+// diagonal: C block n takes A blocks b <= n (UPPER: b >= n).  `left(a, b)` loads or makes A_b, `at(b, n)` is the
+// address of the right block.  Two C blocks at a time, so that four sums are under way.
+template <int AP, int BP, bool TRANS, bool UPPER, class Left, class At>
+__device__ __forceinline__ void triangle(float (&c)[8][4], Left left, At at, int plane)
+{
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int b = UPPER ? 3 - i : i;
+        unsigned a[AP][4];
+        left(a, b);
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+            // the pair of C blocks j, j + 1
+            const bool first = UPPER ? j <= b : j >= b, second = UPPER ? j + 1 <= b : j + 1 >= b;
+            if (first && second) {
+                unsigned r[2][BP][4];
+                load_right<BP, TRANS>(r[0], at(b, j), plane);
+                load_right<BP, TRANS>(r[1], at(b, j + 1), plane);
+                multiply<AP, BP, 2>(reinterpret_cast<float (&)[4][4]>(c[2 * j]), a, r);
+            } else if (first) {
+                product<AP, BP, TRANS>(c[2 * j], c[2 * j + 1], a, at(b, j), plane);
+            } else if (second) {
+                product<AP, BP, TRANS>(c[2 * j + 2], c[2 * j + 3], a, at(b, j + 1), plane);
+            }
+        }
     }
 }
 

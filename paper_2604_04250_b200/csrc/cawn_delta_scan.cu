@@ -3,10 +3,8 @@
 // Per chunk and warp (16 value rows, transposed products; see cawn_delta_chunk.cuh):
 //   X = S K^T,  R = V^T - e^G X,  r = R T^T,  u = beta r,  O = scale e^G S Q^T + u P^T,
 //   S <- e^{G_C} S + (e^{G_C - G} u) K
-// Bound: the chain of these products, chunk after chunk, and the instructions between them (with one
-// warp per scheduler, every one costs).  So the four warps that compute do nothing else: a fifth fetches the
-// next chunk's tiles with cp.async while the current one is computed, and hands them over with a barrier;
-// arithmetic between the products runs on pairs of floats.
+// Bound: the chain of these products, chunk after chunk, on the tensor pipes of the SMs that have a head.  The
+// chain's warps do nothing else; side warps make the outputs from the state and the corrections handed to them.
 //
 // Few heads leave SMs idle while the chain is long, so the time axis is cut into segments: a chunk acts on
 // a state row s as s <- s M + l, so a first pass computes each segment's M (the same walk over the rows
@@ -23,75 +21,260 @@ namespace {
 // SUMMARY: end states and transitions of segments only.
 enum { MODE_OUT, MODE_SAVE, MODE_SUMMARY };
 
-template <int DK, int NP, int MODE> struct ScanStage {
-    static constexpr int NT = NP == 1 ? 2 : 3;
-    bf16 k[NP][kC * (DK + kPad)];
-    bf16 q[MODE == MODE_SUMMARY ? 0 : NP][kC * (DK + kPad)];
-    bf16 tri[NT][kC * kLd];
-    bf16 p[MODE == MODE_OUT ? NP : MODE == MODE_SAVE ? NT : 0][kC * kLd];
-    bf16 v[NP][kC * kLd];
-    bf16 go[MODE == MODE_SAVE ? NP : 0][kC * kLd];
+template <int DK, int NP> struct ScanStage {
+    static constexpr int NT = NP == 1 ? 2 : 3, VLD = 16 * kRowGroups<NP> + kPad;
+    bf16 k[NP][kC * (DK + kPad)], tri[NT][kC * kLd], v[NP][kC * VLD];
     float coef[kCoef][kC];
 };
-// two where they fit, so that the next chunk's tiles arrive during the current one
-template <int DK, int NP, int MODE> constexpr int kScanStages = sizeof(ScanStage<DK, NP, MODE>) * 2 <= 227 * 1024 ? 2 : 1;
-template <int DK, int NP, int MODE> constexpr int kScanBlocks = DK == 64 && NP == 1 && MODE != MODE_SAVE ? 2 : 1;   // per SM
+template <int DK, int NP, int MODE> struct ScanSide {
+    static constexpr int NB = MODE == MODE_SAVE && NP == 1 ? 2 : NP, VLD = 16 * kRowGroups<NP> + kPad;   // NB: terms of P
+    bf16 q[NP][kC * (DK + kPad)], p[NB][kC * kLd];
+    bf16 t[MODE == MODE_SAVE ? NP : 1][kC * VLD];      // dO, and the way out for token rows
+    float coef[kCoef][kC];
+};
+// From chain to side warp: terms of the state and of u, or (SAVE) the state and r as accumulators.
+template <int DK, int NP, int MODE> struct ScanSwap {
+    uint4 s[MODE == MODE_OUT ? NP * DK / 16 * 32 : DK / 8 * 32], u[MODE == MODE_OUT ? NP * 4 * 32 : 8 * 32];
+};
 
-template <int DK, int NP, int MODE>
-__device__ __forceinline__ void scan_load(const ChunkParams &P, ScanStage<DK, NP, MODE> &st, int bh, int c, int vb, int vcols)
+template <int DK, int NP, int MODE> struct ScanPlan {
+    static constexpr int RG = kRowGroups<NP>;
+    static constexpr bool SIDE = MODE != MODE_SUMMARY;
+    static constexpr size_t chain = sizeof(ScanStage<DK, NP>), side = SIDE ? sizeof(ScanSide<DK, NP, MODE>) : 0;
+    static constexpr size_t swap = SIDE ? sizeof(ScanSwap<DK, NP, MODE>) * RG : 0;
+    static constexpr Stages n = fit_stages(chain, side, swap);
+    static constexpr size_t smem = chain * n.chain + side * n.side + swap * n.swap;
+    static constexpr int threads = 64 * RG;         // chain warps, then side warps (without outputs they only fetch)
+    static_assert(smem <= 227 * 1024, "fits an SM");
+};
+
+template <int DK, int NP>
+__device__ __forceinline__ void scan_load(const ChunkParams &P, ScanStage<DK, NP> &st, int bh, int c, int v0, int vcols)
 {
-    constexpr int NT = NP == 1 ? 2 : 3;
+    constexpr int NT = NP == 1 ? 2 : 3, TH = 32 * kRowGroups<NP>, VW = 16 * kRowGroups<NP>;
     const long long t0 = (long long)c * kC, nc = (long long)bh * P.chunks + c;
-    const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC, lane = threadIdx.x % 32;
+    const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
 #pragma unroll
     for (int i = 0; i < NP; i++) {
-        load_tile<kC, DK, 32>(st.k[i], P.k.at + i * P.k.plane + q_base(P, P.k, bh, t0), P.k.stride_t, rows, P.Dk);
-        if (vcols > 0) load_tile<kC, kC, 32>(st.v[i], P.v.at + i * P.v.plane + v_base(P, P.v, bh, t0) + vb * kC, P.v.stride_t, rows, vcols);
-        if constexpr (MODE != MODE_SUMMARY)
-            load_tile<kC, DK, 32>(st.q[i], P.q.at + i * P.q.plane + q_base(P, P.q, bh, t0), P.q.stride_t, rows, P.Dk);
+        load_tile<kC, DK, TH>(st.k[i], P.k.at + i * P.k.plane + q_base(P, P.k, bh, t0), P.k.stride_t, rows, P.Dk);
+        if (vcols > 0) load_tile<kC, VW, TH>(st.v[i], P.v.at + i * P.v.plane + v_base(P, P.v, bh, t0) + v0, P.v.stride_t, rows, vcols);
+    }
+#pragma unroll
+    for (int i = 0; i < NT; i++) load_dense<TH>(st.tri[i], P.tri + (nc * NT + i) * kTile);
+    for (int i = threadIdx.x % TH; i < kCoef * kC / 4; i += TH) cp16(smem_addr(&st.coef[0][0]) + i * 16, P.coef + nc * (kCoef * kC) + i * 4, true);
+    cp_commit();
+}
+
+template <int DK, int NP, int MODE>
+__device__ __forceinline__ void side_load(const ChunkParams &P, ScanSide<DK, NP, MODE> &st, int bh, int c, int v0, int vcols)
+{
+    constexpr int NT = NP == 1 ? 2 : 3, TH = 32 * kRowGroups<NP>, VW = 16 * kRowGroups<NP>;
+    const long long t0 = (long long)c * kC, nc = (long long)bh * P.chunks + c;
+    const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
+#pragma unroll
+    for (int i = 0; i < NP; i++) {
+        load_tile<kC, DK, TH>(st.q[i], P.q.at + i * P.q.plane + q_base(P, P.q, bh, t0), P.q.stride_t, rows, P.Dk);
         if constexpr (MODE == MODE_SAVE)
-            load_tile<kC, kC, 32>(st.go[i], P.go.at + i * P.go.plane + v_base(P, P.go, bh, t0) + vb * kC, P.go.stride_t, rows, vcols);
-        if constexpr (MODE == MODE_OUT) load_dense<32>(st.p[i], P.p + (nc * NT + i) * kTile);
+            load_tile<kC, VW, TH>(st.t[i], P.go.at + i * P.go.plane + v_base(P, P.go, bh, t0) + v0, P.go.stride_t, rows, vcols);
     }
 #pragma unroll
-    for (int i = 0; i < NT; i++) {
-        load_dense<32>(st.tri[i], P.tri + (nc * NT + i) * kTile);
-        if constexpr (MODE == MODE_SAVE) load_dense<32>(st.p[i], P.p + (nc * NT + i) * kTile);
-    }
-#pragma unroll
-    for (int i = 0; i < 3; i++)
-        if (i * 32 + lane < kCoef * kC / 4) cp16(smem_addr(&st.coef[0][0]) + (i * 32 + lane) * 16, P.coef + nc * (kCoef * kC) + (i * 32 + lane) * 4, true);
+    for (int i = 0; i < ScanSide<DK, NP, MODE>::NB; i++) load_dense<TH>(st.p[i], P.p + (nc * NT + i) * kTile);
+    for (int i = threadIdx.x % TH; i < kCoef * kC / 4; i += TH) cp16(smem_addr(&st.coef[0][0]) + i * 16, P.coef + nc * (kCoef * kC) + i * 4, true);
     cp_commit();
 }
 
 template <int DK, int NP, int MODE, class T>
-__global__ void __launch_bounds__(kWalkThreads, (kScanBlocks<DK, NP, MODE>)) delta_scan_kernel(const ChunkParams P)
+__global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_scan_kernel(const ChunkParams P)
 {
-    constexpr int STAGES = kScanStages<DK, NP, MODE>, ld = DK + kPad, NT = NP == 1 ? 2 : 3;
-    // Terms of the walk's own factors: three for the state and its update, three for R and in the output's
-    // sum where the backward's dots need them, else NT and the terms of the output's type.
-    constexpr int NR = MODE == MODE_SAVE ? 3 : NT, NO = MODE == MODE_SAVE ? 3 : NP, NB = MODE == MODE_SAVE ? NT : NP;
+    using Plan = ScanPlan<DK, NP, MODE>;
+    using Side = ScanSide<DK, NP, MODE>;
+    using Swap = ScanSwap<DK, NP, MODE>;
+    constexpr int ld = DK + kPad, NT = NP == 1 ? 2 : 3, RG = Plan::RG, VW = 16 * RG, VLD = VW + kPad, CS = Plan::n.chain, SS = Plan::n.side, WS = Plan::n.swap;
+    constexpr int PAIR = 64 * RG, ONE = 32 * RG;
     extern __shared__ __align__(16) unsigned char raw[];
-    auto *stages = reinterpret_cast<ScanStage<DK, NP, MODE> *>(raw);
-    const int bh = blockIdx.x, vb = blockIdx.y, seg = blockIdx.z;
-    const int lane = threadIdx.x % 32, w = threadIdx.x / 32, gr = lane / 4, tc = lane % 4 * 2;
-    const bool ident = MODE == MODE_SUMMARY && vb >= P.vblocks;     // rows of the identity instead of values
-    const int r0 = (ident ? vb - P.vblocks : vb) * kC;              // first value (or identity) row of the block
-    const int vcols = ident ? 0 : (P.Dv - r0 < kC ? P.Dv - r0 : kC);
+    auto *stages = reinterpret_cast<ScanStage<DK, NP> *>(raw);
+    const int bh = blockIdx.x, seg = blockIdx.z;
+    const int vblks = (P.Dv + VW - 1) / VW;
+    const bool ident = MODE == MODE_SUMMARY && (int)blockIdx.y >= vblks;        // rows of the identity instead of values
+    const int r0 = ((int)blockIdx.y - (ident ? vblks : 0)) * VW;                // first value (or identity) row of the block
+    const int vcols = ident ? 0 : (P.Dv - r0 < VW ? P.Dv - r0 : VW);
     const int c0 = seg * P.seg_chunks, c1 = c0 + P.seg_chunks < P.chunks ? c0 + P.seg_chunks : P.chunks;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, w = warp % RG, gr = lane / 4, tc = lane % 4 * 2;
+    const int w4 = (r0 / 16 + w) % 4;                                           // row group inside its block of 64 values
 
-    if (w == 4) {               // producer: barrier 1 + s: stage s is full, 3 + s: stage s is free again
+    if (!Plan::SIDE && warp >= RG) {            // fetch only
         for (int c = c0; c < c1; c++) {
-            const int s = (c - c0) % STAGES;
-            if (c - c0 >= STAGES) bar_sync(3 + s);
-            scan_load<DK, NP, MODE>(P, stages[s], bh, c, vb, vcols);
+            const int s = (c - c0) % CS;
+            if (c - c0 >= CS) bar_sync(BAR_EMPTY + s, PAIR);
+            scan_load<DK, NP>(P, stages[s], bh, c, r0, vcols);
             cp_wait<0>();
-            bar_arrive(1 + s);
+            bar_arrive(BAR_FULL + s, PAIR);
+        }
+        return;
+    }
+    if constexpr (Plan::SIDE) if (warp >= RG) { // ---------------------------- side warps: tiles, and outputs or dO.o
+        constexpr int NO = MODE == MODE_SAVE ? 3 : NP, NB = Side::NB;     // terms of the state and of u, of P
+        auto *tiles = reinterpret_cast<Side *>(raw + Plan::chain * CS);
+        scan_load<DK, NP>(P, stages[0], bh, c0, r0, vcols);
+        cp_wait<0>();
+        bar_arrive(BAR_FULL, PAIR);
+        side_load<DK, NP, MODE>(P, tiles[0], bh, c0, r0, vcols);
+        if (CS == 2 && c0 + 1 < c1) scan_load<DK, NP>(P, stages[1], bh, c0 + 1, r0, vcols);
+        else cp_commit();
+        for (int c = c0; c < c1; c++) {
+            const int s = (c - c0) % SS, cs = (c - c0) % CS, par = (c - c0) % WS;
+            auto &st = tiles[s];
+            const Swap &sw = reinterpret_cast<const Swap *>(raw + Plan::chain * CS + Plan::side * SS)[par * RG + w];
+            const long long t0 = (long long)c * kC, nv = ((long long)bh * P.chunks + c) * P.vblocks + r0 / kC;
+            const unsigned qs = smem_addr(st.q[0]), ps = smem_addr(st.p[0]), os = smem_addr(st.t[0]);
+            // The side's tiles of this chunk were asked for before the chain's next ones, which may still be on
+            // their way until the chain is about to need them.
+            if (SS == 2 && CS == 2) cp_wait<1>(); else cp_wait<0>();
+            bar_sync(BAR_SIDE, ONE);            // the tiles are here, and the previous chunk's are done with
+            if (SS == 2) {
+                if (c + 1 < c1) side_load<DK, NP, MODE>(P, tiles[(c + 1 - c0) % SS], bh, c + 1, r0, vcols);
+                else cp_commit();               // an empty group keeps the count
+            }
+            bar_sync(BAR_READY + par, PAIR);
+            float S[MODE == MODE_SAVE ? DK / 8 : 1][4], r[MODE == MODE_SAVE ? 8 : 1][4];
+            if constexpr (MODE == MODE_SAVE) {
+#pragma unroll
+                for (int n = 0; n < DK / 8; n++) {
+                    const float4 x = reinterpret_cast<const float4 *>(sw.s)[n * 32 + lane];
+                    S[n][0] = x.x; S[n][1] = x.y; S[n][2] = x.z; S[n][3] = x.w;
+                    P.sf[((nv * 4 + w4) * (DK / 8) + n) * 32 + lane] = x;
+                }
+#pragma unroll
+                for (int n = 0; n < 8; n++) {
+                    const float4 x = reinterpret_cast<const float4 *>(sw.u)[n * 32 + lane];
+                    r[n][0] = x.x; r[n][1] = x.y; r[n][2] = x.z; r[n][3] = x.w;
+                    P.rf[((nv * 4 + w4) * 8 + n) * 32 + lane] = x;
+                }
+            }
+            // Y = scale e^G S Q^T + u P^T
+            float Y[8][4] = {};
+#pragma unroll
+            for (int d = 0; d < DK / 16; d++) {
+                unsigned a[NO][4], b[4][NP][4];
+                if constexpr (MODE == MODE_SAVE) as_left(S[2 * d], S[2 * d + 1], a);
+                else get_left(a, sw.s, d);
+#pragma unroll
+                for (int i = 0; i < 4; i++) load_right<NP, false>(b[i], at_nk(qs, ld, 16 * i, 16 * d), kC * ld);
+                multiply<NO, NP, 4>(Y, a, b);
+            }
+#pragma unroll
+            for (int n = 0; n < 8; n++) {
+                const int t = 8 * n + tc;
+                const float2 e = *reinterpret_cast<const float2 *>(&st.coef[COEF_EG][t]);
+                const f32x2 f = pair(P.scale * e.x, P.scale * e.y);
+                scale_row(Y[n], 0, f);
+                scale_row(Y[n], 1, f);
+                if constexpr (MODE == MODE_SAVE) {
+                    const f32x2 bt = pair(*reinterpret_cast<const float2 *>(&st.coef[COEF_BETA][t]));
+                    scale_row(r[n], 0, bt);
+                    scale_row(r[n], 1, bt);
+                }
+            }
+            if (CS == 2 && c + 1 < c1) {        // the chain's next tiles
+                if (SS == 2) cp_wait<1>(); else cp_wait<0>();
+                bar_arrive(BAR_FULL + (cs ^ 1), PAIR);
+            }
+            triangle<NO, NB, false, false>(Y,
+                [&](unsigned (&a)[NO][4], int tb) {
+                    if constexpr (MODE == MODE_SAVE) as_left(r[2 * tb], r[2 * tb + 1], a);
+                    else get_left(a, sw.u, tb);
+                },
+                [&](int tb, int nb) { return at_nk(ps, kLd, 16 * nb, 16 * tb); }, kC * kLd);
+            if (c + WS < c1) bar_arrive(BAR_FREE + par, PAIR);
+            if (c + CS >= c1) {
+                cp_commit();
+            } else {                            // the chain's next tiles but CS - 1
+                bar_sync(BAR_EMPTY + cs, PAIR);
+                scan_load<DK, NP>(P, stages[cs], bh, c + CS, r0, vcols);
+                if (CS == 1) {
+                    cp_wait<0>();
+                    bar_arrive(BAR_FULL, PAIR);
+                }
+            }
+            const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
+            if constexpr (MODE == MODE_SAVE) {
+                // dO.o over this row group's 16 values
+                float dots[8][2];
+#pragma unroll
+                for (int nb = 0; nb < 4; nb++) {
+                    unsigned g[NP][4];
+                    load_left<NP, true>(g, at_nk(os, VLD, 16 * nb, 16 * w), kC * VLD);
+#pragma unroll
+                    for (int m = 0; m < 2; m++) {
+                        const int n = 2 * nb + m;
+                        const float2 a = sum_terms(g, 2 * m), b = sum_terms(g, 2 * m + 1);
+                        dots[n][0] = fmaf(Y[n][0], a.x, Y[n][2] * b.x);
+                        dots[n][1] = fmaf(Y[n][1], a.y, Y[n][3] * b.y);
+                    }
+                }
+                column_sums(dots);
+                *reinterpret_cast<float2 *>(P.od + (nv * 4 + w4) * kC + 8 * gr + tc) = make_float2(dots[0][0], dots[0][1]);
+                // the state before the chunk, and u as token rows, in the inputs' terms
+                bf16 *dst = P.s0 + nv * (NP * kC * DK) + (16 * w4 + gr) * DK + tc;
+#pragma unroll
+                for (int n = 0; n < DK / 8; n++)
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        unsigned x[NP];
+                        split(S[n][2 * h], S[n][2 * h + 1], x);
+#pragma unroll
+                        for (int i = 0; i < NP; i++) *reinterpret_cast<unsigned *>(dst + i * (kC * DK) + 8 * h * DK + 8 * n) = x[i];
+                    }
+#pragma unroll
+                for (int term = 0; term < NP; term++) {
+                    __syncwarp();
+#pragma unroll
+                    for (int nb = 0; nb < 4; nb++) {
+                        unsigned x[NP][4];
+                        as_left(r[2 * nb], r[2 * nb + 1], x);
+                        stsm_t(at_nk(os, VLD, 16 * nb, 16 * w), x[term][0], x[term][1], x[term][2], x[term][3]);
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = lane; i < 128; i += 32)
+                        *reinterpret_cast<uint4 *>(P.u + (nv * NP + term) * kTile + i / 2 * kC + 16 * w4 + i % 2 * 8) =
+                            *reinterpret_cast<const uint4 *>(&st.t[0][i / 2 * VLD + 16 * w + i % 2 * 8]);
+                }
+            } else {
+                T *o = static_cast<T *>(P.o) + (bh / P.Hv) * P.o_stride_b + t0 * P.o_stride_t + (long long)(bh % P.Hv) * P.Dv + r0;
+                if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                    for (int nb = 0; nb < 4; nb++)
+                        stsm_t(at_nk(os, VLD, 16 * nb, 16 * w), pack_bf16(Y[2 * nb][0], Y[2 * nb][1]), pack_bf16(Y[2 * nb][2], Y[2 * nb][3]),
+                               pack_bf16(Y[2 * nb + 1][0], Y[2 * nb + 1][1]), pack_bf16(Y[2 * nb + 1][2], Y[2 * nb + 1][3]));
+                    __syncwarp();
+#pragma unroll
+                    for (int i = lane; i < 128; i += 32) {
+                        const int t = i / 2, v = 16 * w + i % 2 * 8;
+                        if (t < rows && v < vcols)
+                            *reinterpret_cast<uint4 *>(o + t * P.o_stride_t + v) = *reinterpret_cast<const uint4 *>(&st.t[0][t * VLD + v]);
+                    }
+                } else {
+#pragma unroll
+                    for (int n = 0; n < 8; n++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            const int t = 8 * n + tc + (e & 1), v = 16 * w + gr + (e >> 1) * 8;
+                            if (t < rows && v < vcols) o[t * P.o_stride_t + v] = narrow<T>(Y[n][e]);
+                        }
+                }
+            }
+            if (SS == 1 && c + 1 < c1) {
+                bar_sync(BAR_SIDE, ONE);
+                side_load<DK, NP, MODE>(P, tiles[0], bh, c + 1, r0, vcols);
+            }
         }
         return;
     }
 
-    const int rlim = ident ? P.Dk : P.Dv;                           // rows that exist
+    // -------------------------------------------------------------------------- chain warps
+    constexpr int NR = MODE == MODE_SAVE ? 3 : NT;          // terms of R: three where the backward's dots need them
+    const int rlim = ident ? P.Dk : P.Dv;                   // rows that exist
     const int row[2] = {r0 + 16 * w + gr, r0 + 16 * w + gr + 8};
     // state rows row[0], row[1]; columns 8 n + tc, +1 of tile n
     float S[DK / 8][4];
@@ -112,46 +295,34 @@ __global__ void __launch_bounds__(kWalkThreads, (kScanBlocks<DK, NP, MODE>)) del
         }
 
     for (int c = c0; c < c1; c++) {
-        const int s = (c - c0) % STAGES;
+        const int s = (c - c0) % CS, par = (c - c0) % WS;
         auto &st = stages[s];
-        const long long t0 = (long long)c * kC, nv = ((long long)bh * P.chunks + c) * P.vblocks + vb;
+        Swap &sw = reinterpret_cast<Swap *>(raw + Plan::chain * CS + Plan::side * SS)[par * RG + w];
         const unsigned ks = smem_addr(st.k[0]), ts = smem_addr(st.tri[0]), vs = smem_addr(st.v[0]);
 
+        if (Plan::SIDE && c - c0 >= WS) bar_sync(BAR_FREE + par, PAIR);
         if constexpr (MODE == MODE_SAVE) {
-            bf16 *dst = P.s0 + nv * (NP * kC * DK) + (16 * w + gr) * DK + tc;
-            float4 *df = P.sf + (nv * 4 + w) * (DK / 8 * 32) + lane;
 #pragma unroll
-            for (int n = 0; n < DK / 8; n++) {
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    unsigned x[NP];
-                    split(S[n][2 * h], S[n][2 * h + 1], x);
-#pragma unroll
-                    for (int i = 0; i < NP; i++) *reinterpret_cast<unsigned *>(dst + i * (kC * DK) + 8 * h * DK + 8 * n) = x[i];
-                }
-                df[n * 32] = make_float4(S[n][0], S[n][1], S[n][2], S[n][3]);
-            }
+            for (int n = 0; n < DK / 8; n++) reinterpret_cast<float4 *>(sw.s)[n * 32 + lane] = make_float4(S[n][0], S[n][1], S[n][2], S[n][3]);
         }
-        bar_sync(1 + s);
-        // X = S K^T, Y = S Q^T
-        float X[8][4] = {}, Y[MODE == MODE_SUMMARY ? 1 : 8][4] = {};
+        bar_sync(BAR_FULL + s, PAIR);
+        // X = S K^T
+        float X[8][4] = {};
 #pragma unroll
         for (int d = 0; d < DK / 16; d++) {
-            unsigned a[3][4];
-            as_left(S[2 * d], S[2 * d + 1], a);
+            unsigned a[3][4], b[4][NP][4];
 #pragma unroll
-            for (int nb = 0; nb < 4; nb++) {
-                product<3, NP, false>(X[2 * nb], X[2 * nb + 1], a, at_nk(ks, ld, 16 * nb, 16 * d), kC * ld);
-                if constexpr (MODE != MODE_SUMMARY)     // bfloat16 results: one term of the state is enough
-                    product<NO, NP, false>(Y[2 * nb], Y[2 * nb + 1], leading<NO>(a), at_nk(smem_addr(st.q[0]), ld, 16 * nb, 16 * d), kC * ld);
-            }
+            for (int i = 0; i < 4; i++) load_right<NP, false>(b[i], at_nk(ks, ld, 16 * i, 16 * d), kC * ld);
+            as_left(S[2 * d], S[2 * d + 1], a);
+            if constexpr (MODE == MODE_OUT) put_left(sw.s, d, leading<NP>(a));
+            multiply<3, NP, 4>(X, a, b);
         }
-        // R = V^T - e^G X (into X and as the start of r); the read-out's first part gets its factor
+        // R = V^T - e^G X (in X, and the start of r)
         float r[8][4];
 #pragma unroll
         for (int nb = 0; nb < 4; nb++) {
             unsigned vf[NP][4] = {};
-            if (vcols > 0) load_left<NP, true>(vf, at_nk(vs, kLd, 16 * nb, 16 * w), kC * kLd);
+            if (vcols > 0) load_left<NP, true>(vf, at_nk(vs, VLD, 16 * nb, 16 * w), kC * VLD);
 #pragma unroll
             for (int m = 0; m < 2; m++) {
                 const int n = 2 * nb + m;
@@ -159,108 +330,33 @@ __global__ void __launch_bounds__(kWalkThreads, (kScanBlocks<DK, NP, MODE>)) del
                 const f32x2 minus = pair(-e.x, -e.y);
 #pragma unroll
                 for (int h = 0; h < 2; h++) fma_row(X[n], h, minus, pair(sum_terms(vf, 2 * m + h)));
-                if constexpr (MODE != MODE_SUMMARY) {
-                    const f32x2 f = pair(P.scale * e.x, P.scale * e.y);
-                    scale_row(Y[n], 0, f);
-                    scale_row(Y[n], 1, f);
-                }
 #pragma unroll
                 for (int i = 0; i < 4; i++) r[n][i] = X[n][i];
             }
         }
         // r = R + R (T - I)^T: tokens t of the result from block t' on
+        triangle<NR, NT, true, false>(r, [&](unsigned (&a)[NR][4], int tb) { as_left(X[2 * tb], X[2 * tb + 1], a); },
+                                      [&](int tb, int nb) { return at_kn(ts, kLd, 16 * tb, 16 * nb); }, kC * kLd);
+        if constexpr (MODE == MODE_SAVE) {
+#pragma unroll
+            for (int n = 0; n < 8; n++) reinterpret_cast<float4 *>(sw.u)[n * 32 + lane] = make_float4(r[n][0], r[n][1], r[n][2], r[n][3]);
+        }
+        // u = beta r, handed over
 #pragma unroll
         for (int tb = 0; tb < 4; tb++) {
-            unsigned a[NR][4];
-            as_left(X[2 * tb], X[2 * tb + 1], a);
 #pragma unroll
-            for (int nb = tb; nb < 4; nb++)
-                product<NR, NT, true>(r[2 * nb], r[2 * nb + 1], a, at_kn(ts, kLd, 16 * tb, 16 * nb), kC * kLd);
-        }
-        if constexpr (MODE == MODE_SAVE) {
-            float4 *df = P.rf + (nv * 4 + w) * (8 * 32) + lane;
-#pragma unroll
-            for (int n = 0; n < 8; n++) df[n * 32] = make_float4(r[n][0], r[n][1], r[n][2], r[n][3]);
-        }
-        // u = beta r
-#pragma unroll
-        for (int n = 0; n < 8; n++) {
-            const f32x2 bt = pair(*reinterpret_cast<const float2 *>(&st.coef[COEF_BETA][8 * n + tc]));
-            scale_row(r[n], 0, bt);
-            scale_row(r[n], 1, bt);
-        }
-        if constexpr (MODE != MODE_SUMMARY) {
-            const unsigned ps = smem_addr(st.p[0]);
-#pragma unroll
-            for (int tb = 0; tb < 4; tb++) {
-                unsigned a[NO][4];
+            for (int m = 0; m < 2; m++) {
+                const f32x2 bt = pair(*reinterpret_cast<const float2 *>(&st.coef[COEF_BETA][16 * tb + 8 * m + tc]));
+                scale_row(r[2 * tb + m], 0, bt);
+                scale_row(r[2 * tb + m], 1, bt);
+            }
+            if constexpr (MODE == MODE_OUT) {
+                unsigned a[NP][4];
                 as_left(r[2 * tb], r[2 * tb + 1], a);
-#pragma unroll
-                for (int nb = tb; nb < 4; nb++)
-                    product<NO, NB, false>(Y[2 * nb], Y[2 * nb + 1], a, at_nk(ps, kLd, 16 * nb, 16 * tb), kC * kLd);
+                put_left(sw.u, tb, a);
             }
         }
-        if constexpr (MODE == MODE_SAVE) {
-            // dO.o over this warp's 16 values
-            float dots[8][2];
-#pragma unroll
-            for (int nb = 0; nb < 4; nb++) {
-                unsigned g[NP][4];
-                load_left<NP, true>(g, at_nk(smem_addr(st.go[0]), kLd, 16 * nb, 16 * w), kC * kLd);
-#pragma unroll
-                for (int m = 0; m < 2; m++) {
-                    const int n = 2 * nb + m;
-                    const float2 a = sum_terms(g, 2 * m), b = sum_terms(g, 2 * m + 1);
-                    dots[n][0] = fmaf(Y[n][0], a.x, Y[n][2] * b.x);
-                    dots[n][1] = fmaf(Y[n][1], a.y, Y[n][3] * b.y);
-                }
-            }
-            column_sums(dots);
-            *reinterpret_cast<float2 *>(P.od + (nv * 4 + w) * kC + 8 * gr + tc) = make_float2(dots[0][0], dots[0][1]);
-            // u as token rows, through this warp's own columns of the V tile
-            bf16 *dst = P.u + nv * (NP * kTile);
-#pragma unroll
-            for (int term = 0; term < NP; term++) {
-                __syncwarp();
-#pragma unroll
-                for (int nb = 0; nb < 4; nb++) {
-                    unsigned x[NP][4];
-                    as_left(r[2 * nb], r[2 * nb + 1], x);
-                    stsm_t(at_nk(vs, kLd, 16 * nb, 16 * w), x[term][0], x[term][1], x[term][2], x[term][3]);
-                }
-                __syncwarp();
-#pragma unroll
-                for (int i = lane; i < 128; i += 32)
-                    *reinterpret_cast<uint4 *>(dst + term * kTile + i / 2 * kC + 16 * w + i % 2 * 8) =
-                        *reinterpret_cast<const uint4 *>(&st.v[0][i / 2 * kLd + 16 * w + i % 2 * 8]);
-            }
-        }
-        if constexpr (MODE == MODE_OUT) {
-            T *o = static_cast<T *>(P.o) + (bh / P.Hv) * P.o_stride_b + t0 * P.o_stride_t + (long long)(bh % P.Hv) * P.Dv + r0;
-            const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
-            if constexpr (sizeof(T) == 2) {
-                __syncwarp();
-#pragma unroll
-                for (int nb = 0; nb < 4; nb++)
-                    stsm_t(at_nk(vs, kLd, 16 * nb, 16 * w), pack_bf16(Y[2 * nb][0], Y[2 * nb][1]), pack_bf16(Y[2 * nb][2], Y[2 * nb][3]),
-                           pack_bf16(Y[2 * nb + 1][0], Y[2 * nb + 1][1]), pack_bf16(Y[2 * nb + 1][2], Y[2 * nb + 1][3]));
-                __syncwarp();
-#pragma unroll
-                for (int i = lane; i < 128; i += 32) {
-                    const int t = i / 2, v = 16 * w + i % 2 * 8;
-                    if (t < rows && v < vcols)
-                        *reinterpret_cast<uint4 *>(o + t * P.o_stride_t + v) = *reinterpret_cast<const uint4 *>(&st.v[0][t * kLd + v]);
-                }
-            } else {
-#pragma unroll
-                for (int n = 0; n < 8; n++)
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const int t = 8 * n + tc + (e & 1), v = 16 * w + gr + (e >> 1) * 8;
-                        if (t < rows && v < vcols) o[t * P.o_stride_t + v] = narrow<T>(Y[n][e]);
-                    }
-            }
-        }
+        if (Plan::SIDE) bar_arrive(BAR_READY + par, PAIR);
         // S <- e^{G_C} S + (e^{G_C - G} u) K.  The update is summed from zero and added once: the tensor
         // core's running sum drops low bits at every step, always towards zero, which on a state that lives
         // for many chunks would add up.
@@ -277,16 +373,21 @@ __global__ void __launch_bounds__(kWalkThreads, (kScanBlocks<DK, NP, MODE>)) del
             as_left(r[2 * tb], r[2 * tb + 1], a[tb]);
         }
 #pragma unroll
-        for (int nb = 0; nb < DK / 16; nb++) {
-            float x[2][4] = {};
+        for (int nb = 0; nb < DK / 16; nb += 2) {
+            float x[4][4] = {};
 #pragma unroll
-            for (int tb = 0; tb < 4; tb++) product<3, NP, true>(x[0], x[1], a[tb], at_kn(ks, ld, 16 * tb, 16 * nb), kC * ld);
+            for (int tb = 0; tb < 4; tb++) {
+                unsigned b[2][NP][4];
 #pragma unroll
-            for (int m = 0; m < 2; m++)
+                for (int i = 0; i < 2; i++) load_right<NP, true>(b[i], at_kn(ks, ld, 16 * tb, 16 * (nb + i)), kC * ld);
+                multiply<3, NP, 2>(x, a[tb], b);
+            }
+#pragma unroll
+            for (int m = 0; m < 4; m++)
 #pragma unroll
                 for (int h = 0; h < 2; h++) fma_row(S[2 * nb + m], h, pair(eC, eC), pair(x[m][2 * h], x[m][2 * h + 1]));
         }
-        if (c + STAGES < c1) bar_arrive(3 + s);
+        if (c + CS < c1) bar_arrive(BAR_EMPTY + s, PAIR);
     }
 
     float *to = nullptr;
@@ -304,71 +405,72 @@ __global__ void __launch_bounds__(kWalkThreads, (kScanBlocks<DK, NP, MODE>)) del
     }
     if constexpr (MODE == MODE_SAVE) {
         // the state after the last chunk, for the reverse walk's <state, adjoint>
-        float4 *df = P.sf + ((((long long)P.B * P.Hv * P.chunks + bh) * P.vblocks + vb) * 4 + w) * (DK / 8 * 32) + lane;
+        const long long nv = ((long long)P.B * P.Hv * P.chunks + bh) * P.vblocks + r0 / kC;
         if (seg == P.segs - 1)
 #pragma unroll
-            for (int n = 0; n < DK / 8; n++) df[n * 32] = make_float4(S[n][0], S[n][1], S[n][2], S[n][3]);
+            for (int n = 0; n < DK / 8; n++) P.sf[((nv * 4 + w4) * (DK / 8) + n) * 32 + lane] = make_float4(S[n][0], S[n][1], S[n][2], S[n][3]);
     }
 }
 
-template <int DK, int NP, int MODE> cudaError_t scan(const ChunkParams &P, int row_blocks, cudaStream_t st)
+template <int DK, int NP, int MODE> cudaError_t scan(const ChunkParams &P, cudaStream_t st)
 {
     using T = typename std::conditional<NP == 1, bf16, float>::type;
-    const size_t smem = sizeof(ScanStage<DK, NP, MODE>) * kScanStages<DK, NP, MODE>;
-    static_assert(sizeof(ScanStage<DK, NP, MODE>) <= 227 * 1024, "fits an SM");
+    using Plan = ScanPlan<DK, NP, MODE>;
     auto *kernel = delta_scan_kernel<DK, NP, MODE, T>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan::smem);
     if (e != cudaSuccess) return e;
-    return launch(kernel, dim3((unsigned)(P.B * P.Hv), row_blocks, P.segs), dim3(kWalkThreads), smem, st, P);
+    constexpr int VW = 16 * Plan::RG;
+    const int blocks = (P.Dv + VW - 1) / VW + (MODE == MODE_SUMMARY ? (P.Dk + VW - 1) / VW : 0);
+    return launch(kernel, dim3((unsigned)(P.B * P.Hv), blocks, P.segs), dim3(Plan::threads), Plan::smem, st, P);
 }
 
 // Start states of the segments from their end states and transitions, one segment after the other.  A block has 16
-// rows of one head's state, a thread eight rows of one column; the next transition is on its way (in registers)
+// rows of one head's state, a thread four rows of one column; the next transition is on its way (in registers)
 // while the current one is multiplied from shared memory.  Float arithmetic: a few products per segment, once, are
 // not worth the tensor cores.  REVERSE: adjoints, last segment first, with the transposed transitions.
 template <int DK, bool REVERSE>
-__global__ void __launch_bounds__(2 * DK) delta_join_kernel(const ChunkParams P)
+__global__ void __launch_bounds__(4 * DK) delta_join_kernel(const ChunkParams P)
 {
     extern __shared__ __align__(16) float map[];            // [DK][DK + 1], row k: what state column k sends on
     __shared__ __align__(16) float S[16][DK];
-    constexpr int EACH = DK / 2, LD = DK + 1;               // transition elements per thread
-    const int col = threadIdx.x % DK, half = threadIdx.x / DK, bh = blockIdx.x, r0 = blockIdx.y * 16 + 8 * half;
+    constexpr int EACH = DK / 4, LD = DK + 1;               // transition elements per thread
+    const int col = threadIdx.x % DK, part = threadIdx.x / DK, bh = blockIdx.x, r0 = blockIdx.y * 16 + 4 * part;
     const long long rows = (long long)P.Dv * P.Dk;
     const bool in = col < P.Dk;
-    float s[8], end[8], m[EACH];
+    float s[4], end[4], m[EACH];
     auto fetch = [&](int n) {
         const long long seg = (long long)bh * P.segs + (REVERSE ? P.segs - 1 - n : n);
         const float *from = P.seg_map + seg * P.Dk * P.Dk;
 #pragma unroll
         for (int i = 0; i < EACH; i++) {
-            const int k = 2 * i + half;
+            const int k = 4 * i + part;
             m[i] = in && k < P.Dk ? from[(long long)k * P.Dk + col] : 0.f;
         }
 #pragma unroll
-        for (int i = 0; i < 8; i++) end[i] = in && r0 + i < P.Dv ? P.seg_end[seg * rows + (long long)(r0 + i) * P.Dk + col] : 0.f;
+        for (int i = 0; i < 4; i++) end[i] = in && r0 + i < P.Dv ? P.seg_end[seg * rows + (long long)(r0 + i) * P.Dk + col] : 0.f;
     };
 #pragma unroll
-    for (int i = 0; i < 8; i++) s[i] = in && r0 + i < P.Dv && P.state_in != nullptr ? P.state_in[bh * rows + (long long)(r0 + i) * P.Dk + col] : 0.f;
+    for (int i = 0; i < 4; i++) s[i] = in && r0 + i < P.Dv && P.state_in != nullptr ? P.state_in[bh * rows + (long long)(r0 + i) * P.Dk + col] : 0.f;
     fetch(0);
     for (int n = 0; n < P.segs; n++) {
         const long long seg = (long long)bh * P.segs + (REVERSE ? P.segs - 1 - n : n);
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
+        for (int i = 0; i < 4; i++) {
             if (in && r0 + i < P.Dv) P.seg_start[seg * rows + (long long)(r0 + i) * P.Dk + col] = s[i];
-            S[8 * half + i][col] = s[i];
+            S[4 * part + i][col] = s[i];
             s[i] = end[i];
         }
         if (n + 1 == P.segs) break;
 #pragma unroll
-        for (int i = 0; i < EACH; i++) map[REVERSE ? col * LD + 2 * i + half : (2 * i + half) * LD + col] = m[i];
+        for (int i = 0; i < EACH; i++) map[REVERSE ? col * LD + 4 * i + part : (4 * i + part) * LD + col] = m[i];
         __syncthreads();
         fetch(n + 1);
 #pragma unroll 4
         for (int k = 0; k < DK; k += 4) {
             const float a = map[k * LD + col], b = map[(k + 1) * LD + col], c = map[(k + 2) * LD + col], d = map[(k + 3) * LD + col];
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float4 x = *reinterpret_cast<const float4 *>(&S[8 * half + i][k]);
+            for (int i = 0; i < 4; i++) {
+                const float4 x = *reinterpret_cast<const float4 *>(&S[4 * part + i][k]);
                 s[i] = fmaf(x.x, a, fmaf(x.y, b, fmaf(x.z, c, fmaf(x.w, d, s[i]))));
             }
         }
@@ -381,18 +483,18 @@ template <int DK, bool REVERSE> cudaError_t join1(const ChunkParams &P, cudaStre
     const size_t smem = DK * (DK + 1) * sizeof(float);
     const cudaError_t e = cudaFuncSetAttribute(delta_join_kernel<DK, REVERSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    return launch(delta_join_kernel<DK, REVERSE>, dim3((unsigned)(P.B * P.Hv), (P.Dv + 15) / 16), dim3(2 * DK), smem, st, P);
+    return launch(delta_join_kernel<DK, REVERSE>, dim3((unsigned)(P.B * P.Hv), (P.Dv + 15) / 16), dim3(4 * DK), smem, st, P);
 }
 template <int DK> cudaError_t join(const ChunkParams &P, bool reverse, cudaStream_t st) { return reverse ? join1<DK, true>(P, st) : join1<DK, false>(P, st); }
 
 template <int DK, int NP> cudaError_t run(const ChunkParams &P, bool save, cudaStream_t st)
 {
     if (P.segs > 1) {
-        cudaError_t e = scan<DK, NP, MODE_SUMMARY>(P, P.vblocks + (P.Dk + kC - 1) / kC, st);
+        cudaError_t e = scan<DK, NP, MODE_SUMMARY>(P, st);
         if (e == cudaSuccess) e = join<DK>(P, false, st);
         if (e != cudaSuccess) return e;
     }
-    return save ? scan<DK, NP, MODE_SAVE>(P, P.vblocks, st) : scan<DK, NP, MODE_OUT>(P, P.vblocks, st);
+    return save ? scan<DK, NP, MODE_SAVE>(P, st) : scan<DK, NP, MODE_OUT>(P, st);
 }
 
 }  // namespace
