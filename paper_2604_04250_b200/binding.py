@@ -179,10 +179,20 @@ def _dp(t):
     return t.ctypes.data
 
 
+_current_stream = None
+
+
 def _stream(stream):
+    """The given stream's handle, or that of torch's current stream on the current device.  The latter is asked
+    for by every call: torch's own raw lookup takes 0.3 us, building a Stream object for its handle 3 us."""
+    global _current_stream
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _current_stream is None:
+            import torch
+            torch.cuda.current_stream()         # initialises CUDA, with torch's own message where there is none
+            raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+            _current_stream = (lambda: raw(device())) if raw and device else lambda: torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     return getattr(stream, "cuda_stream", stream)
 
 

@@ -21,35 +21,40 @@ namespace {
 // SUMMARY: end states and transitions of segments only.
 enum { MODE_OUT, MODE_SAVE, MODE_SUMMARY };
 
-template <int DK, int NP> struct ScanStage {
+// Tiles of the chain; SAVE: and those of dO.o, which its chain takes along.
+template <int DK, int NP, int MODE> struct ScanStage {
     static constexpr int NT = NP == 1 ? 2 : 3, VLD = 16 * kRowGroups<NP> + kPad;
+    static constexpr bool SAVE = MODE == MODE_SAVE;
     bf16 k[NP][kC * (DK + kPad)], tri[NT][kC * kLd], v[NP][kC * VLD];
+    bf16 q[SAVE ? NP : 0][kC * (DK + kPad)], p[SAVE ? NT : 0][kC * kLd], go[SAVE ? NP : 0][kC * VLD];
     float coef[kCoef][kC];
 };
-template <int DK, int NP, int MODE> struct ScanSide {
-    static constexpr int NB = MODE == MODE_SAVE && NP == 1 ? 2 : NP, VLD = 16 * kRowGroups<NP> + kPad;   // NB: terms of P
-    bf16 q[NP][kC * (DK + kPad)], p[NB][kC * kLd];
-    bf16 t[MODE == MODE_SAVE ? NP : 1][kC * VLD];      // dO, and the way out for token rows
+// Tiles of the outputs.
+template <int DK, int NP> struct ScanSide {
+    bf16 q[NP][kC * (DK + kPad)], p[NP][kC * kLd];
+    bf16 t[kC * (16 * kRowGroups<NP> + kPad)];          // the way out for token rows
     float coef[kCoef][kC];
 };
-// From chain to side warp: terms of the state and of u, or (SAVE) the state and r as accumulators.
-template <int DK, int NP, int MODE> struct ScanSwap {
-    uint4 s[MODE == MODE_OUT ? NP * DK / 16 * 32 : DK / 8 * 32], u[MODE == MODE_OUT ? NP * 4 * 32 : 8 * 32];
+// From chain to side warp: terms of the state and of u.
+template <int DK, int NP> struct ScanSwap {
+    uint4 s[NP * DK / 16 * 32], u[NP * 4 * 32];
 };
 
 template <int DK, int NP, int MODE> struct ScanPlan {
     static constexpr int RG = kRowGroups<NP>;
-    static constexpr bool SIDE = MODE != MODE_SUMMARY;
-    static constexpr size_t chain = sizeof(ScanStage<DK, NP>), side = SIDE ? sizeof(ScanSide<DK, NP, MODE>) : 0;
-    static constexpr size_t swap = SIDE ? sizeof(ScanSwap<DK, NP, MODE>) * RG : 0;
+    // Measured for the backward's walk too: with dO.o on the side it took 152 us instead of 126, because three
+    // terms of everything keep the tensor pipe busy enough, and splitting them twice costs more than it fills.
+    static constexpr bool SIDE = MODE == MODE_OUT;
+    static constexpr size_t chain = sizeof(ScanStage<DK, NP, MODE>), side = SIDE ? sizeof(ScanSide<DK, NP>) : 0;
+    static constexpr size_t swap = SIDE ? sizeof(ScanSwap<DK, NP>) * RG : 0;
     static constexpr Stages n = fit_stages(chain, side, swap);
     static constexpr size_t smem = chain * n.chain + side * n.side + swap * n.swap;
     static constexpr int threads = 64 * RG;         // chain warps, then side warps (without outputs they only fetch)
     static_assert(smem <= 227 * 1024, "fits an SM");
 };
 
-template <int DK, int NP>
-__device__ __forceinline__ void scan_load(const ChunkParams &P, ScanStage<DK, NP> &st, int bh, int c, int v0, int vcols)
+template <int DK, int NP, int MODE>
+__device__ __forceinline__ void scan_load(const ChunkParams &P, ScanStage<DK, NP, MODE> &st, int bh, int c, int v0, int vcols)
 {
     constexpr int NT = NP == 1 ? 2 : 3, TH = 32 * kRowGroups<NP>, VW = 16 * kRowGroups<NP>;
     const long long t0 = (long long)c * kC, nc = (long long)bh * P.chunks + c;
@@ -58,27 +63,31 @@ __device__ __forceinline__ void scan_load(const ChunkParams &P, ScanStage<DK, NP
     for (int i = 0; i < NP; i++) {
         load_tile<kC, DK, TH>(st.k[i], P.k.at + i * P.k.plane + q_base(P, P.k, bh, t0), P.k.stride_t, rows, P.Dk);
         if (vcols > 0) load_tile<kC, VW, TH>(st.v[i], P.v.at + i * P.v.plane + v_base(P, P.v, bh, t0) + v0, P.v.stride_t, rows, vcols);
+        if constexpr (MODE == MODE_SAVE) {
+            load_tile<kC, DK, TH>(st.q[i], P.q.at + i * P.q.plane + q_base(P, P.q, bh, t0), P.q.stride_t, rows, P.Dk);
+            load_tile<kC, VW, TH>(st.go[i], P.go.at + i * P.go.plane + v_base(P, P.go, bh, t0) + v0, P.go.stride_t, rows, vcols);
+        }
     }
 #pragma unroll
-    for (int i = 0; i < NT; i++) load_dense<TH>(st.tri[i], P.tri + (nc * NT + i) * kTile);
+    for (int i = 0; i < NT; i++) {
+        load_dense<TH>(st.tri[i], P.tri + (nc * NT + i) * kTile);
+        if constexpr (MODE == MODE_SAVE) load_dense<TH>(st.p[i], P.p + (nc * NT + i) * kTile);
+    }
     for (int i = threadIdx.x % TH; i < kCoef * kC / 4; i += TH) cp16(smem_addr(&st.coef[0][0]) + i * 16, P.coef + nc * (kCoef * kC) + i * 4, true);
     cp_commit();
 }
 
-template <int DK, int NP, int MODE>
-__device__ __forceinline__ void side_load(const ChunkParams &P, ScanSide<DK, NP, MODE> &st, int bh, int c, int v0, int vcols)
+template <int DK, int NP>
+__device__ __forceinline__ void side_load(const ChunkParams &P, ScanSide<DK, NP> &st, int bh, int c)
 {
-    constexpr int NT = NP == 1 ? 2 : 3, TH = 32 * kRowGroups<NP>, VW = 16 * kRowGroups<NP>;
+    constexpr int NT = NP == 1 ? 2 : 3, TH = 32 * kRowGroups<NP>;
     const long long t0 = (long long)c * kC, nc = (long long)bh * P.chunks + c;
     const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
 #pragma unroll
     for (int i = 0; i < NP; i++) {
         load_tile<kC, DK, TH>(st.q[i], P.q.at + i * P.q.plane + q_base(P, P.q, bh, t0), P.q.stride_t, rows, P.Dk);
-        if constexpr (MODE == MODE_SAVE)
-            load_tile<kC, VW, TH>(st.t[i], P.go.at + i * P.go.plane + v_base(P, P.go, bh, t0) + v0, P.go.stride_t, rows, vcols);
+        load_dense<TH>(st.p[i], P.p + (nc * NT + i) * kTile);
     }
-#pragma unroll
-    for (int i = 0; i < ScanSide<DK, NP, MODE>::NB; i++) load_dense<TH>(st.p[i], P.p + (nc * NT + i) * kTile);
     for (int i = threadIdx.x % TH; i < kCoef * kC / 4; i += TH) cp16(smem_addr(&st.coef[0][0]) + i * 16, P.coef + nc * (kCoef * kC) + i * 4, true);
     cp_commit();
 }
@@ -87,12 +96,12 @@ template <int DK, int NP, int MODE, class T>
 __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_scan_kernel(const ChunkParams P)
 {
     using Plan = ScanPlan<DK, NP, MODE>;
-    using Side = ScanSide<DK, NP, MODE>;
-    using Swap = ScanSwap<DK, NP, MODE>;
+    using Side = ScanSide<DK, NP>;
+    using Swap = ScanSwap<DK, NP>;
     constexpr int ld = DK + kPad, NT = NP == 1 ? 2 : 3, RG = Plan::RG, VW = 16 * RG, VLD = VW + kPad, CS = Plan::n.chain, SS = Plan::n.side, WS = Plan::n.swap;
     constexpr int PAIR = 64 * RG, ONE = 32 * RG;
     extern __shared__ __align__(16) unsigned char raw[];
-    auto *stages = reinterpret_cast<ScanStage<DK, NP> *>(raw);
+    auto *stages = reinterpret_cast<ScanStage<DK, NP, MODE> *>(raw);
     const int bh = blockIdx.x, seg = blockIdx.z;
     const int vblks = (P.Dv + VW - 1) / VW;
     const bool ident = MODE == MODE_SUMMARY && (int)blockIdx.y >= vblks;        // rows of the identity instead of values
@@ -106,167 +115,95 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
         for (int c = c0; c < c1; c++) {
             const int s = (c - c0) % CS;
             if (c - c0 >= CS) bar_sync(BAR_EMPTY + s, PAIR);
-            scan_load<DK, NP>(P, stages[s], bh, c, r0, vcols);
+            scan_load<DK, NP, MODE>(P, stages[s], bh, c, r0, vcols);
             cp_wait<0>();
             bar_arrive(BAR_FULL + s, PAIR);
         }
         return;
     }
-    if constexpr (Plan::SIDE) if (warp >= RG) { // ---------------------------- side warps: tiles, and outputs or dO.o
-        constexpr int NO = MODE == MODE_SAVE ? 3 : NP, NB = Side::NB;     // terms of the state and of u, of P
+    if constexpr (Plan::SIDE) if (warp >= RG) { // ---------------------------- side warps: tiles and outputs
         auto *tiles = reinterpret_cast<Side *>(raw + Plan::chain * CS);
-        scan_load<DK, NP>(P, stages[0], bh, c0, r0, vcols);
+        scan_load<DK, NP, MODE>(P, stages[0], bh, c0, r0, vcols);
         cp_wait<0>();
         bar_arrive(BAR_FULL, PAIR);
-        side_load<DK, NP, MODE>(P, tiles[0], bh, c0, r0, vcols);
-        if (CS == 2 && c0 + 1 < c1) scan_load<DK, NP>(P, stages[1], bh, c0 + 1, r0, vcols);
+        side_load<DK, NP>(P, tiles[0], bh, c0);
+        if (CS == 2 && c0 + 1 < c1) scan_load<DK, NP, MODE>(P, stages[1], bh, c0 + 1, r0, vcols);
         else cp_commit();
         for (int c = c0; c < c1; c++) {
-            const int s = (c - c0) % SS, cs = (c - c0) % CS, par = (c - c0) % WS;
-            auto &st = tiles[s];
+            const int cs = (c - c0) % CS, par = (c - c0) % WS;
+            auto &st = tiles[(c - c0) % SS];
             const Swap &sw = reinterpret_cast<const Swap *>(raw + Plan::chain * CS + Plan::side * SS)[par * RG + w];
-            const long long t0 = (long long)c * kC, nv = ((long long)bh * P.chunks + c) * P.vblocks + r0 / kC;
-            const unsigned qs = smem_addr(st.q[0]), ps = smem_addr(st.p[0]), os = smem_addr(st.t[0]);
+            const long long t0 = (long long)c * kC;
+            const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
+            const unsigned qs = smem_addr(st.q[0]), ps = smem_addr(st.p[0]), os = smem_addr(st.t);
             // The side's tiles of this chunk were asked for before the chain's next ones, which may still be on
             // their way until the chain is about to need them.
             if (SS == 2 && CS == 2) cp_wait<1>(); else cp_wait<0>();
             bar_sync(BAR_SIDE, ONE);            // the tiles are here, and the previous chunk's are done with
             if (SS == 2) {
-                if (c + 1 < c1) side_load<DK, NP, MODE>(P, tiles[(c + 1 - c0) % SS], bh, c + 1, r0, vcols);
+                if (c + 1 < c1) side_load<DK, NP>(P, tiles[(c + 1 - c0) % SS], bh, c + 1);
                 else cp_commit();               // an empty group keeps the count
             }
             bar_sync(BAR_READY + par, PAIR);
-            float S[MODE == MODE_SAVE ? DK / 8 : 1][4], r[MODE == MODE_SAVE ? 8 : 1][4];
-            if constexpr (MODE == MODE_SAVE) {
-#pragma unroll
-                for (int n = 0; n < DK / 8; n++) {
-                    const float4 x = reinterpret_cast<const float4 *>(sw.s)[n * 32 + lane];
-                    S[n][0] = x.x; S[n][1] = x.y; S[n][2] = x.z; S[n][3] = x.w;
-                    P.sf[((nv * 4 + w4) * (DK / 8) + n) * 32 + lane] = x;
-                }
-#pragma unroll
-                for (int n = 0; n < 8; n++) {
-                    const float4 x = reinterpret_cast<const float4 *>(sw.u)[n * 32 + lane];
-                    r[n][0] = x.x; r[n][1] = x.y; r[n][2] = x.z; r[n][3] = x.w;
-                    P.rf[((nv * 4 + w4) * 8 + n) * 32 + lane] = x;
-                }
-            }
-            // Y = scale e^G S Q^T + u P^T
+            // Y = scale e^G S Q^T + u P^T; factors in the output's terms
             float Y[8][4] = {};
 #pragma unroll
             for (int d = 0; d < DK / 16; d++) {
-                unsigned a[NO][4], b[4][NP][4];
-                if constexpr (MODE == MODE_SAVE) as_left(S[2 * d], S[2 * d + 1], a);
-                else get_left(a, sw.s, d);
+                unsigned a[NP][4], b[4][NP][4];
+                get_left(a, sw.s, d);
 #pragma unroll
                 for (int i = 0; i < 4; i++) load_right<NP, false>(b[i], at_nk(qs, ld, 16 * i, 16 * d), kC * ld);
-                multiply<NO, NP, 4>(Y, a, b);
+                multiply<NP, NP, 4>(Y, a, b);
             }
 #pragma unroll
             for (int n = 0; n < 8; n++) {
-                const int t = 8 * n + tc;
-                const float2 e = *reinterpret_cast<const float2 *>(&st.coef[COEF_EG][t]);
+                const float2 e = *reinterpret_cast<const float2 *>(&st.coef[COEF_EG][8 * n + tc]);
                 const f32x2 f = pair(P.scale * e.x, P.scale * e.y);
                 scale_row(Y[n], 0, f);
                 scale_row(Y[n], 1, f);
-                if constexpr (MODE == MODE_SAVE) {
-                    const f32x2 bt = pair(*reinterpret_cast<const float2 *>(&st.coef[COEF_BETA][t]));
-                    scale_row(r[n], 0, bt);
-                    scale_row(r[n], 1, bt);
-                }
             }
             if (CS == 2 && c + 1 < c1) {        // the chain's next tiles
                 if (SS == 2) cp_wait<1>(); else cp_wait<0>();
                 bar_arrive(BAR_FULL + (cs ^ 1), PAIR);
             }
-            triangle<NO, NB, false, false>(Y,
-                [&](unsigned (&a)[NO][4], int tb) {
-                    if constexpr (MODE == MODE_SAVE) as_left(r[2 * tb], r[2 * tb + 1], a);
-                    else get_left(a, sw.u, tb);
-                },
-                [&](int tb, int nb) { return at_nk(ps, kLd, 16 * nb, 16 * tb); }, kC * kLd);
+            triangle<NP, NP, false, false>(Y, [&](unsigned (&a)[NP][4], int tb) { get_left(a, sw.u, tb); },
+                                           [&](int tb, int nb) { return at_nk(ps, kLd, 16 * nb, 16 * tb); }, kC * kLd);
             if (c + WS < c1) bar_arrive(BAR_FREE + par, PAIR);
             if (c + CS >= c1) {
                 cp_commit();
             } else {                            // the chain's next tiles but CS - 1
                 bar_sync(BAR_EMPTY + cs, PAIR);
-                scan_load<DK, NP>(P, stages[cs], bh, c + CS, r0, vcols);
+                scan_load<DK, NP, MODE>(P, stages[cs], bh, c + CS, r0, vcols);
                 if (CS == 1) {
                     cp_wait<0>();
                     bar_arrive(BAR_FULL, PAIR);
                 }
             }
-            const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
-            if constexpr (MODE == MODE_SAVE) {
-                // dO.o over this row group's 16 values
-                float dots[8][2];
+            T *o = static_cast<T *>(P.o) + (bh / P.Hv) * P.o_stride_b + t0 * P.o_stride_t + (long long)(bh % P.Hv) * P.Dv + r0;
+            if constexpr (sizeof(T) == 2) {
 #pragma unroll
-                for (int nb = 0; nb < 4; nb++) {
-                    unsigned g[NP][4];
-                    load_left<NP, true>(g, at_nk(os, VLD, 16 * nb, 16 * w), kC * VLD);
+                for (int nb = 0; nb < 4; nb++)
+                    stsm_t(at_nk(os, VLD, 16 * nb, 16 * w), pack_bf16(Y[2 * nb][0], Y[2 * nb][1]), pack_bf16(Y[2 * nb][2], Y[2 * nb][3]),
+                           pack_bf16(Y[2 * nb + 1][0], Y[2 * nb + 1][1]), pack_bf16(Y[2 * nb + 1][2], Y[2 * nb + 1][3]));
+                __syncwarp();
 #pragma unroll
-                    for (int m = 0; m < 2; m++) {
-                        const int n = 2 * nb + m;
-                        const float2 a = sum_terms(g, 2 * m), b = sum_terms(g, 2 * m + 1);
-                        dots[n][0] = fmaf(Y[n][0], a.x, Y[n][2] * b.x);
-                        dots[n][1] = fmaf(Y[n][1], a.y, Y[n][3] * b.y);
-                    }
-                }
-                column_sums(dots);
-                *reinterpret_cast<float2 *>(P.od + (nv * 4 + w4) * kC + 8 * gr + tc) = make_float2(dots[0][0], dots[0][1]);
-                // the state before the chunk, and u as token rows, in the inputs' terms
-                bf16 *dst = P.s0 + nv * (NP * kC * DK) + (16 * w4 + gr) * DK + tc;
-#pragma unroll
-                for (int n = 0; n < DK / 8; n++)
-#pragma unroll
-                    for (int h = 0; h < 2; h++) {
-                        unsigned x[NP];
-                        split(S[n][2 * h], S[n][2 * h + 1], x);
-#pragma unroll
-                        for (int i = 0; i < NP; i++) *reinterpret_cast<unsigned *>(dst + i * (kC * DK) + 8 * h * DK + 8 * n) = x[i];
-                    }
-#pragma unroll
-                for (int term = 0; term < NP; term++) {
-                    __syncwarp();
-#pragma unroll
-                    for (int nb = 0; nb < 4; nb++) {
-                        unsigned x[NP][4];
-                        as_left(r[2 * nb], r[2 * nb + 1], x);
-                        stsm_t(at_nk(os, VLD, 16 * nb, 16 * w), x[term][0], x[term][1], x[term][2], x[term][3]);
-                    }
-                    __syncwarp();
-#pragma unroll
-                    for (int i = lane; i < 128; i += 32)
-                        *reinterpret_cast<uint4 *>(P.u + (nv * NP + term) * kTile + i / 2 * kC + 16 * w4 + i % 2 * 8) =
-                            *reinterpret_cast<const uint4 *>(&st.t[0][i / 2 * VLD + 16 * w + i % 2 * 8]);
+                for (int i = lane; i < 128; i += 32) {
+                    const int t = i / 2, v = 16 * w + i % 2 * 8;
+                    if (t < rows && v < vcols)
+                        *reinterpret_cast<uint4 *>(o + t * P.o_stride_t + v) = *reinterpret_cast<const uint4 *>(&st.t[t * VLD + v]);
                 }
             } else {
-                T *o = static_cast<T *>(P.o) + (bh / P.Hv) * P.o_stride_b + t0 * P.o_stride_t + (long long)(bh % P.Hv) * P.Dv + r0;
-                if constexpr (sizeof(T) == 2) {
 #pragma unroll
-                    for (int nb = 0; nb < 4; nb++)
-                        stsm_t(at_nk(os, VLD, 16 * nb, 16 * w), pack_bf16(Y[2 * nb][0], Y[2 * nb][1]), pack_bf16(Y[2 * nb][2], Y[2 * nb][3]),
-                               pack_bf16(Y[2 * nb + 1][0], Y[2 * nb + 1][1]), pack_bf16(Y[2 * nb + 1][2], Y[2 * nb + 1][3]));
-                    __syncwarp();
+                for (int n = 0; n < 8; n++)
 #pragma unroll
-                    for (int i = lane; i < 128; i += 32) {
-                        const int t = i / 2, v = 16 * w + i % 2 * 8;
-                        if (t < rows && v < vcols)
-                            *reinterpret_cast<uint4 *>(o + t * P.o_stride_t + v) = *reinterpret_cast<const uint4 *>(&st.t[0][t * VLD + v]);
+                    for (int e = 0; e < 4; e++) {
+                        const int t = 8 * n + tc + (e & 1), v = 16 * w + gr + (e >> 1) * 8;
+                        if (t < rows && v < vcols) o[t * P.o_stride_t + v] = narrow<T>(Y[n][e]);
                     }
-                } else {
-#pragma unroll
-                    for (int n = 0; n < 8; n++)
-#pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            const int t = 8 * n + tc + (e & 1), v = 16 * w + gr + (e >> 1) * 8;
-                            if (t < rows && v < vcols) o[t * P.o_stride_t + v] = narrow<T>(Y[n][e]);
-                        }
-                }
             }
             if (SS == 1 && c + 1 < c1) {
                 bar_sync(BAR_SIDE, ONE);
-                side_load<DK, NP, MODE>(P, tiles[0], bh, c + 1, r0, vcols);
+                side_load<DK, NP>(P, tiles[0], bh, c + 1);
             }
         }
         return;
@@ -300,14 +237,25 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
         Swap &sw = reinterpret_cast<Swap *>(raw + Plan::chain * CS + Plan::side * SS)[par * RG + w];
         const unsigned ks = smem_addr(st.k[0]), ts = smem_addr(st.tri[0]), vs = smem_addr(st.v[0]);
 
+        const long long nv = ((long long)bh * P.chunks + c) * P.vblocks + r0 / kC;
         if (Plan::SIDE && c - c0 >= WS) bar_sync(BAR_FREE + par, PAIR);
-        if constexpr (MODE == MODE_SAVE) {
+        if constexpr (MODE == MODE_SAVE) {      // the state before the chunk, in float and in the inputs' terms
+            bf16 *dst = P.s0 + nv * (NP * kC * DK) + (16 * w4 + gr) * DK + tc;
 #pragma unroll
-            for (int n = 0; n < DK / 8; n++) reinterpret_cast<float4 *>(sw.s)[n * 32 + lane] = make_float4(S[n][0], S[n][1], S[n][2], S[n][3]);
+            for (int n = 0; n < DK / 8; n++) {
+                P.sf[((nv * 4 + w4) * (DK / 8) + n) * 32 + lane] = make_float4(S[n][0], S[n][1], S[n][2], S[n][3]);
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    unsigned x[NP];
+                    split(S[n][2 * h], S[n][2 * h + 1], x);
+#pragma unroll
+                    for (int i = 0; i < NP; i++) *reinterpret_cast<unsigned *>(dst + i * (kC * DK) + 8 * h * DK + 8 * n) = x[i];
+                }
+            }
         }
         bar_sync(BAR_FULL + s, PAIR);
-        // X = S K^T
-        float X[8][4] = {};
+        // X = S K^T; SAVE: Y = S Q^T
+        float X[8][4] = {}, Y[MODE == MODE_SAVE ? 8 : 1][4] = {};
 #pragma unroll
         for (int d = 0; d < DK / 16; d++) {
             unsigned a[3][4], b[4][NP][4];
@@ -316,6 +264,11 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
             as_left(S[2 * d], S[2 * d + 1], a);
             if constexpr (MODE == MODE_OUT) put_left(sw.s, d, leading<NP>(a));
             multiply<3, NP, 4>(X, a, b);
+            if constexpr (MODE == MODE_SAVE) {
+#pragma unroll
+                for (int i = 0; i < 4; i++) load_right<NP, false>(b[i], at_nk(smem_addr(st.q[0]), ld, 16 * i, 16 * d), kC * ld);
+                multiply<3, NP, 4>(Y, a, b);
+            }
         }
         // R = V^T - e^G X (in X, and the start of r)
         float r[8][4];
@@ -332,6 +285,11 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
                 for (int h = 0; h < 2; h++) fma_row(X[n], h, minus, pair(sum_terms(vf, 2 * m + h)));
 #pragma unroll
                 for (int i = 0; i < 4; i++) r[n][i] = X[n][i];
+                if constexpr (MODE == MODE_SAVE) {
+                    const f32x2 f = pair(P.scale * e.x, P.scale * e.y);
+                    scale_row(Y[n], 0, f);
+                    scale_row(Y[n], 1, f);
+                }
             }
         }
         // r = R + R (T - I)^T: tokens t of the result from block t' on
@@ -339,7 +297,7 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
                                       [&](int tb, int nb) { return at_kn(ts, kLd, 16 * tb, 16 * nb); }, kC * kLd);
         if constexpr (MODE == MODE_SAVE) {
 #pragma unroll
-            for (int n = 0; n < 8; n++) reinterpret_cast<float4 *>(sw.u)[n * 32 + lane] = make_float4(r[n][0], r[n][1], r[n][2], r[n][3]);
+            for (int n = 0; n < 8; n++) P.rf[((nv * 4 + w4) * 8 + n) * 32 + lane] = make_float4(r[n][0], r[n][1], r[n][2], r[n][3]);
         }
         // u = beta r, handed over
 #pragma unroll
@@ -357,6 +315,43 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
             }
         }
         if (Plan::SIDE) bar_arrive(BAR_READY + par, PAIR);
+        if constexpr (MODE == MODE_SAVE) {
+            const unsigned ps = smem_addr(st.p[0]);
+            triangle<3, NT, false, false>(Y, [&](unsigned (&a)[3][4], int tb) { as_left(r[2 * tb], r[2 * tb + 1], a); },
+                                          [&](int tb, int nb) { return at_nk(ps, kLd, 16 * nb, 16 * tb); }, kC * kLd);
+            // dO.o over this row group's 16 values
+            float dots[8][2];
+#pragma unroll
+            for (int nb = 0; nb < 4; nb++) {
+                unsigned g[NP][4];
+                load_left<NP, true>(g, at_nk(smem_addr(st.go[0]), VLD, 16 * nb, 16 * w), kC * VLD);
+#pragma unroll
+                for (int m = 0; m < 2; m++) {
+                    const int n = 2 * nb + m;
+                    const float2 a = sum_terms(g, 2 * m), b = sum_terms(g, 2 * m + 1);
+                    dots[n][0] = fmaf(Y[n][0], a.x, Y[n][2] * b.x);
+                    dots[n][1] = fmaf(Y[n][1], a.y, Y[n][3] * b.y);
+                }
+            }
+            column_sums(dots);
+            *reinterpret_cast<float2 *>(P.od + (nv * 4 + w4) * kC + 8 * gr + tc) = make_float2(dots[0][0], dots[0][1]);
+            // u as token rows in the inputs' terms, through this warp's own part of the V tile
+#pragma unroll
+            for (int term = 0; term < NP; term++) {
+                __syncwarp();
+#pragma unroll
+                for (int nb = 0; nb < 4; nb++) {
+                    unsigned x[NP][4];
+                    as_left(r[2 * nb], r[2 * nb + 1], x);
+                    stsm_t(at_nk(vs, VLD, 16 * nb, 16 * w), x[term][0], x[term][1], x[term][2], x[term][3]);
+                }
+                __syncwarp();
+#pragma unroll
+                for (int i = lane; i < 128; i += 32)
+                    *reinterpret_cast<uint4 *>(P.u + (nv * NP + term) * kTile + i / 2 * kC + 16 * w4 + i % 2 * 8) =
+                        *reinterpret_cast<const uint4 *>(&st.v[0][i / 2 * VLD + 16 * w + i % 2 * 8]);
+            }
+        }
         // S <- e^{G_C} S + (e^{G_C - G} u) K.  The update is summed from zero and added once: the tensor
         // core's running sum drops low bits at every step, always towards zero, which on a state that lives
         // for many chunks would add up.
