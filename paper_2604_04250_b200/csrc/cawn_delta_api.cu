@@ -139,6 +139,7 @@ int chunk_params(ChunkParams &C, const cawn_delta_params *p, const DeltaParams &
     C.g = D.g; C.beta = D.beta; C.state_in = D.state_in;
     C.L = p->L; C.B = p->B; C.Hk = p->Hk; C.Hv = p->Hv; C.Dk = p->Dk; C.Dv = p->Dv; C.scale = p->scale;
     C.chunks = w.chunks; C.vblocks = w.vblocks; C.segs = w.segs; C.seg_chunks = w.seg_chunks;
+    C.p_terms = w.terms == 3 ? 3 : w.rf > 0 ? 2 : 1;    // bfloat16 outputs take one, the backward's dots two
     const long long rows = (long long)p->B * p->L;
     int rc = terms_of(C.q, D.q, D.q_stride, rows, p->L, p->Hk * p->Dk, w.terms, w.q, ws, st);
     if (rc == CAWN_OK) rc = terms_of(C.k, D.k, D.k_stride, rows, p->L, p->Hk * p->Dk, w.terms, w.k, ws, st);

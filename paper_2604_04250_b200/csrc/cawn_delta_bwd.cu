@@ -30,7 +30,7 @@ template <int DK, int NP> struct RevStage {
 };
 // No side warps: measured with dO^T P and (scale e^G dO)^T Q made ahead on the side, 160 us instead of 149.
 template <int DK, int NP> struct RevPlan {
-    static constexpr int RG = kRowGroups<NP>, threads = 64 * RG;        // walking and fetching warps
+    static constexpr int RG = kRowGroups<NP>, threads = 32 * (RG + kFetch<NP>);        // walking and fetching warps
     static constexpr int stages = fit_stages(sizeof(RevStage<DK, NP>), 0, 0).chain;
     static constexpr size_t smem = sizeof(RevStage<DK, NP>) * stages;
     static_assert(smem <= 227 * 1024, "fits an SM");
@@ -39,7 +39,7 @@ template <int DK, int NP> struct RevPlan {
 template <int DK, int NP>
 __device__ __forceinline__ void rev_load(const ChunkParams &P, RevStage<DK, NP> &st, int bh, int c, int v0, int vcols)
 {
-    constexpr int NT = NP == 1 ? 2 : 3, TH = 32 * kRowGroups<NP>, VW = 16 * kRowGroups<NP>;
+    constexpr int NT = NP == 1 ? 2 : 3, TH = 32 * kFetch<NP>, VW = 16 * kRowGroups<NP>;
     const long long t0 = (long long)c * kC, nc = (long long)bh * P.chunks + c;
     const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
 #pragma unroll
@@ -63,7 +63,7 @@ template <int DK, int NP, bool SUMMARY, class T>
 __global__ void __launch_bounds__((RevPlan<DK, NP>::threads), 1) delta_reverse_kernel(const ChunkParams P)
 {
     using Plan = RevPlan<DK, NP>;
-    constexpr int ld = DK + kPad, NT = NP == 1 ? 2 : 3, RG = Plan::RG, VW = 16 * RG, VLD = VW + kPad, CS = Plan::stages, PAIR = 64 * RG;
+    constexpr int ld = DK + kPad, NT = NP == 1 ? 2 : 3, RG = Plan::RG, VW = 16 * RG, VLD = VW + kPad, CS = Plan::stages, PAIR = Plan::threads;
     extern __shared__ __align__(16) unsigned char raw[];
     auto *stages = reinterpret_cast<RevStage<DK, NP> *>(raw);
     const int bh = blockIdx.x, seg = blockIdx.z;

@@ -69,6 +69,7 @@ struct ChunkParams {
     float *seg_start, *seg_end, *seg_map;   // [bh][segs][Dv][Dk], same, [bh][segs][Dk][Dk]
     int segs, seg_chunks;
     int B, Hk, Hv, Dk, Dv, chunks, vblocks;
+    int p_terms;                        // terms of P that the walk will read
     float scale;
 };
 
@@ -201,6 +202,9 @@ __device__ __forceinline__ void bar_arrive(int id, int threads) { asm volatile("
 
 // Row groups of a block: float storage has three times the tiles, so half the row groups fit.
 template <int NP> constexpr int kRowGroups = NP == 1 ? 4 : 2;
+
+// Warps that fetch tiles where there are no side warps to do it.
+template <int NP> constexpr int kFetch = NP == 1 ? 1 : 4;
 
 // Stages of the chain's and the side's tiles and of what they exchange: as many as fit.
 struct Stages { int chain, side, swap; };

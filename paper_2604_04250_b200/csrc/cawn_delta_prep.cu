@@ -1,6 +1,8 @@
 // Gated delta rule, chunk form: what a chunk needs that does not depend on the state.  All chunks of all
 // heads at once: decays, the scores P, and the inverse T of the chunk's triangle.
 //
+// Bound: instructions and their latency (exponentials, splitting, substitution), so many small blocks per SM: six,
+// which is why A reuses the tiles' shared memory.
 // The inverse: 16 x 16 blocks on the diagonal by substitution in float (a lane per column), the blocks
 // below from T_IJ = -T_II sum_K A_IK T_KJ on the tensor cores, a block column per warp with the
 // intermediate blocks in registers.  Substitution is stable for every triangle whose inverse is moderate;
@@ -12,15 +14,19 @@ namespace {
 
 template <int DK, int NP> struct PrepSmem {
     static constexpr int NT = NP == 1 ? 2 : 3;
-    bf16 q[NP][kC * (DK + kPad)], k[NP][kC * (DK + kPad)];
-    bf16 a[NT][kC * kLd];               // A = At diag(beta), terms
+    union {
+        struct { bf16 q[NP][kC * (DK + kPad)], k[NP][kC * (DK + kPad)]; };
+        bf16 a[NT][kC * kLd];           // A = At diag(beta), terms: takes the tiles' place once the scores are made
+    };
     bf16 d[NT][4][16 * 24];             // inverses of the diagonal blocks, terms
     float diag[4][16][20];              // diagonal blocks of A
     float ghi[kC], glo[kC], beta[kC];
 };
 
+// Each of the four warps owns the 8-row blocks w and 7 - w: below the diagonal that is nine 8 x 8 blocks for
+// everyone.  (With 16 adjacent rows the last warp had four times the first one's exponentials.)
 template <int DK, int NP>
-__global__ void __launch_bounds__(128) delta_prep_kernel(const ChunkParams P)
+__global__ void __launch_bounds__(128, (DK == 64 && NP == 1 ? 6 : 1)) delta_prep_kernel(const ChunkParams P)
 {
     extern __shared__ __align__(16) unsigned char raw[];
     auto &sm = *reinterpret_cast<PrepSmem<DK, NP> *>(raw);
@@ -82,58 +88,66 @@ __global__ void __launch_bounds__(128) delta_prep_kernel(const ChunkParams P)
     cp_wait<0>();
     __syncthreads();
 
-    // 16 rows i per warp, blocks j <= i
+    // rows 8 w + gr and 8 (7 - w) + gr against column blocks 0 .. 7 - w
     float kk[8][4] = {}, qk[8][4] = {};
     const unsigned ks = smem_addr(sm.k[0]), qs = smem_addr(sm.q[0]);
+    const int left = (lane / 8 % 2 == 0 ? 8 * w : 8 * (7 - w)) + lane % 8;      // this lane's row address of a left operand
 #pragma unroll
     for (int d = 0; d < DK; d += 16) {
         unsigned ka[NP][4], qa[NP][4];
-        load_left<NP, false>(ka, at_kn(ks, ld, 16 * w, d), kC * ld);
-        load_left<NP, false>(qa, at_kn(qs, ld, 16 * w, d), kC * ld);
+        load_left<NP, false>(ka, ks + (left * ld + d + lane / 16 * 8) * 2, kC * ld);
+        load_left<NP, false>(qa, qs + (left * ld + d + lane / 16 * 8) * 2, kC * ld);
 #pragma unroll
         for (int nb = 0; nb < 4; nb++)
-            if (nb <= w) {
+            if (2 * nb <= 7 - w) {
                 product<NP, NP, false>(kk[2 * nb], kk[2 * nb + 1], ka, at_nk(ks, ld, 16 * nb, d), kC * ld);
                 product<NP, NP, false>(qk[2 * nb], qk[2 * nb + 1], qa, at_nk(ks, ld, 16 * nb, d), kC * ld);
             }
     }
+    __syncthreads();                    // A takes the place of the tiles
     bf16 *pt = P.p + nc * NT * kTile;
 #pragma unroll
-    for (int n = 0; n < 8; n++) {
-        if (n / 2 > w) continue;
+    for (int half = 0; half < 2; half++) {
+        const int block = half == 0 ? w : 7 - w, i = 8 * block + gr;
+        const float ghi = sm.ghi[i], glo = sm.glo[i];
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-            const int i = 16 * w + gr + 8 * half, j = 8 * n + tc;
-            float a[2], p[2];
-#pragma unroll
-            for (int e = 0; e < 2; e++) {
-                const bool low = i >= j + e;
-                const float gam = low ? exp2_fast((sm.ghi[i] - sm.ghi[j + e]) + (sm.glo[i] - sm.glo[j + e])) : 0.f;
-                p[e] = low ? P.scale * gam * qk[n][2 * half + e] : 0.f;
-                a[e] = i > j + e ? gam * kk[n][2 * half + e] * sm.beta[j + e] : 0.f;
-            }
+        for (int n = 0; n < 8; n++) {
+            // whole 16 x 16 blocks on and below the diagonal are read later: the block's upper half as zeros
+            if (n / 2 > block / 2) continue;
+            const int j = 8 * n + tc;
+            const float2 jhi = *reinterpret_cast<const float2 *>(&sm.ghi[j]), jlo = *reinterpret_cast<const float2 *>(&sm.glo[j]);
+            const float2 bt = *reinterpret_cast<const float2 *>(&sm.beta[j]);
+            const float g0 = exp2_fast((ghi - jhi.x) + (glo - jlo.x)), g1 = exp2_fast((ghi - jhi.y) + (glo - jlo.y));
+            const float p0 = i >= j ? P.scale * g0 * qk[n][2 * half] : 0.f, p1 = i >= j + 1 ? P.scale * g1 * qk[n][2 * half + 1] : 0.f;
+            const float a0 = i > j ? g0 * kk[n][2 * half] * bt.x : 0.f, a1 = i > j + 1 ? g1 * kk[n][2 * half + 1] * bt.y : 0.f;
             unsigned pw[NT], aw[NT];
-            split(p[0], p[1], pw);
-            split(a[0], a[1], aw);
+            split(p0, p1, pw);
+            split(a0, a1, aw);
 #pragma unroll
             for (int m = 0; m < NT; m++) {
-                *reinterpret_cast<unsigned *>(pt + m * kTile + i * kC + j) = pw[m];
+                if (m < P.p_terms) *reinterpret_cast<unsigned *>(pt + m * kTile + i * kC + j) = pw[m];
                 *reinterpret_cast<unsigned *>(&sm.a[m][i * kLd + j]) = aw[m];
             }
-            if (n / 2 == w) *reinterpret_cast<float2 *>(&sm.diag[w][i - 16 * w][j - 16 * w]) = make_float2(a[0], a[1]);
+            if (n / 2 == block / 2) *reinterpret_cast<float2 *>(&sm.diag[block / 2][i % 16][j % 16]) = make_float2(a0, a1);
         }
     }
-    __syncwarp();
-    // inverse of this warp's diagonal block, lane = column
+    __syncthreads();
+    // inverse of diagonal block w, lane = column; two sums, so that the chain of products is half as long
     if (lane < 16) {
         float x[16];
 #pragma unroll
         for (int i = 0; i < 16; i++) {
-            float s = i == lane ? 1.f : 0.f;
+            float s = i == lane ? 1.f : 0.f, s1 = 0.f;
 #pragma unroll
-            for (int l = 0; l < i; l++) s = fmaf(-sm.diag[w][i][l], x[l], s);
-            x[i] = s;
-            float rest = s;
+            for (int l = 0; l < i; l += 4) {
+                const float4 v = *reinterpret_cast<const float4 *>(&sm.diag[w][i][l]);
+                s = fmaf(-v.x, x[l], s);
+                if (l + 1 < i) s1 = fmaf(-v.y, x[l + 1], s1);
+                if (l + 2 < i) s = fmaf(-v.z, x[l + 2], s);
+                if (l + 3 < i) s1 = fmaf(-v.w, x[l + 3], s1);
+            }
+            x[i] = s + s1;
+            float rest = x[i];
 #pragma unroll
             for (int m = 0; m < NT; m++) {
                 const bf16 term = __float2bfloat16_rn(rest);

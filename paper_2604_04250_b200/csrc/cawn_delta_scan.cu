@@ -49,14 +49,14 @@ template <int DK, int NP, int MODE> struct ScanPlan {
     static constexpr size_t swap = SIDE ? sizeof(ScanSwap<DK, NP>) * RG : 0;
     static constexpr Stages n = fit_stages(chain, side, swap);
     static constexpr size_t smem = chain * n.chain + side * n.side + swap * n.swap;
-    static constexpr int threads = 64 * RG;         // chain warps, then side warps (without outputs they only fetch)
+    static constexpr int fetch = SIDE ? RG : kFetch<NP>, threads = 32 * (RG + fetch);       // chain warps, then side or fetching warps
     static_assert(smem <= 227 * 1024, "fits an SM");
 };
 
 template <int DK, int NP, int MODE>
 __device__ __forceinline__ void scan_load(const ChunkParams &P, ScanStage<DK, NP, MODE> &st, int bh, int c, int v0, int vcols)
 {
-    constexpr int NT = NP == 1 ? 2 : 3, TH = 32 * kRowGroups<NP>, VW = 16 * kRowGroups<NP>;
+    constexpr int NT = NP == 1 ? 2 : 3, TH = 32 * ScanPlan<DK, NP, MODE>::fetch, VW = 16 * kRowGroups<NP>;
     const long long t0 = (long long)c * kC, nc = (long long)bh * P.chunks + c;
     const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
 #pragma unroll
@@ -99,7 +99,7 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
     using Side = ScanSide<DK, NP>;
     using Swap = ScanSwap<DK, NP>;
     constexpr int ld = DK + kPad, NT = NP == 1 ? 2 : 3, RG = Plan::RG, VW = 16 * RG, VLD = VW + kPad, CS = Plan::n.chain, SS = Plan::n.side, WS = Plan::n.swap;
-    constexpr int PAIR = 64 * RG, ONE = 32 * RG;
+    constexpr int PAIR = Plan::threads, ONE = 32 * RG;
     extern __shared__ __align__(16) unsigned char raw[];
     auto *stages = reinterpret_cast<ScanStage<DK, NP, MODE> *>(raw);
     const int bh = blockIdx.x, seg = blockIdx.z;

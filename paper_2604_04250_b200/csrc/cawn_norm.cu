@@ -36,6 +36,46 @@ template <int LPG> __device__ __forceinline__ float team_sum(float v)
 
 __device__ __forceinline__ float sigmoidf(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
 
+// A row's words as they are stored, so that the next row can be on its way without taking a float register per
+// element; V = 1 keeps the element itself.
+template <class T, int V> struct Word {
+    static constexpr int N = V * (int)sizeof(T) / 16;
+    uint4 w[N];
+    __device__ __forceinline__ void get(const T *p) { for (int i = 0; i < N; i++) w[i] = reinterpret_cast<const uint4 *>(p)[i]; }
+    __device__ __forceinline__ void to(float (&f)[V]) const
+    {
+        const unsigned *u = &w[0].x;
+#pragma unroll
+        for (int i = 0; i < V; i++)
+            f[i] = sizeof(T) == 4 ? __uint_as_float(u[i]) : __uint_as_float(i % 2 == 0 ? u[i / 2] << 16 : u[i / 2] & 0xffff0000u);
+    }
+};
+template <class T> struct Word<T, 1> {
+    T w;
+    __device__ __forceinline__ void get(const T *p) { w = *p; }
+    __device__ __forceinline__ void to(float (&f)[1]) const { f[0] = widen(w); }
+};
+template <class T, int V, int NV>
+__device__ __forceinline__ void fetch_row(Word<T, V> (&r)[NV], const T *row, const int (&ch)[NV], bool live)
+{
+#pragma unroll
+    for (int j = 0; j < NV; j++)
+        if (live && ch[j] >= 0) r[j].get(row + ch[j]);
+}
+template <class T, int V, int NV>
+__device__ __forceinline__ void unpack_row(float (&f)[NV][V], const Word<T, V> (&r)[NV], const int (&ch)[NV], bool live)
+{
+#pragma unroll
+    for (int j = 0; j < NV; j++) {
+        if (live && ch[j] >= 0) {
+            r[j].to(f[j]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; e++) f[j][e] = 0.f;
+        }
+    }
+}
+
 template <class T, int V, int NV>
 __device__ __forceinline__ void load_row(float (&f)[NV][V], const T *row, const int (&ch)[NV], bool live)
 {
@@ -153,13 +193,23 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormParams P)
     const int TY = P.TY, tx = threadIdx.x % P.TX;
     const long long r0 = (long long)blockIdx.x * P.rows_per_block;
     const long long r1 = r0 + P.rows_per_block < P.N ? r0 + P.rows_per_block : P.N;
+    const bool gated = P.act == CAWN_NORM_ACT_GATE;
+    Word<T, V> fw[NV], dw[NV], gw[NV];
+    auto fetch = [&](long long r) {
+        const bool live = r < r1 && ty < TY;
+        fetch_row(fw, static_cast<const T *>(P.x) + r * P.x_stride, ch, live);
+        fetch_row(dw, static_cast<const T *>(P.gy) + r * P.C, ch, live);
+        if (gated) fetch_row(gw, static_cast<const T *>(P.gate) + r * P.gate_stride, ch, live);
+    };
+    fetch(r0 + ty);
     for (long long base = r0; base < r1; base += TY) {
         const long long r = base + ty;
         const bool live = r < r1 && ty < TY;
         float f[NV][V], g[NV][V], d[NV][V];
-        load_row(f, static_cast<const T *>(P.x) + r * P.x_stride, ch, live);
-        load_row(d, static_cast<const T *>(P.gy) + r * P.C, ch, live);
-        if (P.act == CAWN_NORM_ACT_GATE) load_row(g, static_cast<const T *>(P.gate) + r * P.gate_stride, ch, live);
+        unpack_row(f, fw, ch, live);
+        unpack_row(d, dw, ch, live);
+        if (gated) unpack_row(g, gw, ch, live);
+        fetch(r + TY);                  // the next row, while this one is worked on
         const float rstd = normalise<LPG>(f, ch, P);
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -296,22 +346,32 @@ __global__ void __launch_bounds__(kWideThreads) norm_wide_kernel(const NormParam
     }
 }
 
-// Parameter gradients: 32 columns a block, 8 row lanes, doubles, fixed order.
-__global__ void __launch_bounds__(256) norm_sum_kernel(const float *part, int blocks, int C, float *gw, float *gb)
+// Parameter gradients: 32 columns a block, 32 row lanes with two sums each, doubles, fixed order.
+__global__ void __launch_bounds__(1024) norm_sum_kernel(const float *part, int blocks, int C, float *gw, float *gb)
 {
-    __shared__ double sums[8][32];
-    const int col = blockIdx.x * 32 + threadIdx.x % 32, lane = threadIdx.x / 32;
-    double s = 0.0;
-    if (col < 2 * C)
-        for (int i = lane; i < blocks; i += 8) s += (double)part[(size_t)i * 2 * C + col];
-    sums[lane][threadIdx.x % 32] = s;
+    __shared__ double sums[32][33];
+    const int x = threadIdx.x % 32, lane = threadIdx.x / 32, col = blockIdx.x * 32 + x;
+    double s = 0.0, t = 0.0;
+    if (col < 2 * C) {
+        int i = lane;
+        for (; i + 32 < blocks; i += 64) {
+            s += (double)part[(size_t)i * 2 * C + col];
+            t += (double)part[(size_t)(i + 32) * 2 * C + col];
+        }
+        if (i < blocks) s += (double)part[(size_t)i * 2 * C + col];
+    }
+    sums[lane][x] = s + t;
     __syncthreads();
-    if (lane == 0 && col < 2 * C) {
-        for (int i = 1; i < 8; i++) s += sums[i][threadIdx.x];
-        if (col < C) {
-            if (gw != nullptr) gw[col] = (float)s;
+    // a warp per column: lane x holds row lane x of column `lane`
+    s = sums[x][lane];
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+    const int mine = blockIdx.x * 32 + lane;
+    if (x == 0 && mine < 2 * C) {
+        if (mine < C) {
+            if (gw != nullptr) gw[mine] = (float)s;
         } else if (gb != nullptr) {
-            gb[col - C] = (float)s;
+            gb[mine - C] = (float)s;
         }
     }
 }
@@ -483,5 +543,5 @@ extern "C" int cawn_group_norm_bwd(const cawn_norm_params *params, const void *x
     P.part = sums ? static_cast<float *>(workspace) : nullptr;
     const int first = run(params, c, P, true, st);
     if (first != CAWN_OK || !sums) return first;
-    return status_of(launch(norm_sum_kernel, dim3((2 * C + 31) / 32), dim3(256), 0, st, (const float *)P.part, c.bx, C, grad_weight, grad_bias));
+    return status_of(launch(norm_sum_kernel, dim3((2 * C + 31) / 32), dim3(1024), 0, st, (const float *)P.part, c.bx, C, grad_weight, grad_bias));
 }
