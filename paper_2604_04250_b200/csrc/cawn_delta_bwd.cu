@@ -289,6 +289,7 @@ template <int DK, int NP> struct GradSmem {
         } m;
     };
     float coef[kCoef][kC];
+    float dots[8][3][kC];                   // per 16 values: dO.o, rb.r, rb.v (up to 128 values)
 };
 
 template <int DK, int NP, class T>
@@ -322,6 +323,12 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
         const long long nc = (long long)bh * P.chunks + c;
         if (threadIdx.x < kCoef * 16)
             cp16(smem_addr(&sm.coef[0][0]) + threadIdx.x * 16, P.coef + nc * (kCoef * kC) + threadIdx.x * 4, true);
+        const int groups = (P.Dv + 15) / 16;                // row groups of the walks
+        const long long g0 = nc * P.vblocks * 4;
+        for (int i = threadIdx.x; i < groups * 48; i += 256) {
+            const int g = i / 48, x = i % 48 * 4;
+            cp16(smem_addr(&sm.dots[g][0][0]) + x * 4, x < kC ? P.od + (g0 + g) * kC + x : P.rd + (g0 + g) * (2 * kC) + x - kC, true);
+        }
         float X[8][4] = {};                 // dO.u or rb.u, then dP or E
         for (int v0 = 0; v0 < P.Dv; v0 += VW) {
             const int vcols = P.Dv - v0 < VW ? P.Dv - v0 : VW, in = v0 % kC;
@@ -428,20 +435,21 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
         if (warp == 0) {
             float dG[2], end = 0.f;
             const long long at = ((long long)b * P.L + t0) * P.Hv + bh % P.Hv;
-            const long long g0 = nc * P.vblocks * 4, g1 = g0 + (P.Dv + 15) / 16;       // row groups of this chunk
+            for (int i = lane; i < groups; i += 32) end += P.sd[g0 + i];
+#pragma unroll
+            for (int o = 16; o > 0; o /= 2) end += __shfl_xor_sync(0xffffffffu, end, o);
 #pragma unroll
             for (int e = 0; e < 2; e++) {
                 const int t = 2 * lane + e;
                 float od = 0.f, rr = 0.f, rv = 0.f;
-                for (long long i = g0; i < g1; i++) {
-                    od += P.od[i * kC + t];
-                    rr += P.rd[i * (2 * kC) + t];
-                    rv += P.rd[i * (2 * kC) + kC + t];
+                for (int i = 0; i < groups; i++) {
+                    od += sm.dots[i][0][t];
+                    rr += sm.dots[i][1][t];
+                    rv += sm.dots[i][2][t];
                 }
                 dG[e] = od - rv;
                 if (t < rows) P.gbeta[at + (long long)t * P.Hv] = rr / sm.coef[COEF_BETA][t];
             }
-            for (long long i = g0; i < g1; i++) end += P.sd[i];
             float run = dG[0] + dG[1];      // suffix sums
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {

@@ -138,7 +138,7 @@ __device__ __forceinline__ void my_place(const NormParams &P, int &ty, int (&ch)
 }
 
 template <class T, int LPG, int V, int NV>
-__global__ void __launch_bounds__(512) norm_fwd_kernel(const NormParams P)
+__global__ void __launch_bounds__(256) norm_fwd_kernel(const NormParams P)
 {
     int ty, ch[NV];
     float w[NV][V], b[NV][V];
@@ -184,9 +184,10 @@ __device__ __forceinline__ float act_backward(int act, float dy, float z, float 
 }
 
 template <class T, int LPG, int V, int NV>
-__global__ void __launch_bounds__(512) norm_bwd_kernel(const NormParams P)
+__global__ void __launch_bounds__(256) norm_bwd_kernel(const NormParams P)
 {
-    extern __shared__ float fold[];          // [2][TX * NV * V] per row lane, folded pairwise
+    constexpr int AHEAD = NV * V <= 8 ? 2 : 1;      // rows on their way: what registers allow
+    extern __shared__ float fold[];                 // [2][TX * NV * V]
     int ty, ch[NV];
     float w[NV][V], b[NV][V], sw[NV][V] = {}, sb[NV][V] = {};
     my_place<LPG>(P, ty, ch, w, b);
@@ -194,22 +195,20 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormParams P)
     const long long r0 = (long long)blockIdx.x * P.rows_per_block;
     const long long r1 = r0 + P.rows_per_block < P.N ? r0 + P.rows_per_block : P.N;
     const bool gated = P.act == CAWN_NORM_ACT_GATE;
-    Word<T, V> fw[NV], dw[NV], gw[NV];
-    auto fetch = [&](long long r) {
+    struct Row { Word<T, V> f[NV], d[NV], g[NV]; };
+    auto fetch = [&](Row &w, long long r) {
         const bool live = r < r1 && ty < TY;
-        fetch_row(fw, static_cast<const T *>(P.x) + r * P.x_stride, ch, live);
-        fetch_row(dw, static_cast<const T *>(P.gy) + r * P.C, ch, live);
-        if (gated) fetch_row(gw, static_cast<const T *>(P.gate) + r * P.gate_stride, ch, live);
+        fetch_row(w.f, static_cast<const T *>(P.x) + r * P.x_stride, ch, live);
+        fetch_row(w.d, static_cast<const T *>(P.gy) + r * P.C, ch, live);
+        if (gated) fetch_row(w.g, static_cast<const T *>(P.gate) + r * P.gate_stride, ch, live);
     };
-    fetch(r0 + ty);
-    for (long long base = r0; base < r1; base += TY) {
-        const long long r = base + ty;
+    auto work = [&](Row &row, long long r) {
         const bool live = r < r1 && ty < TY;
         float f[NV][V], g[NV][V], d[NV][V];
-        unpack_row(f, fw, ch, live);
-        unpack_row(d, dw, ch, live);
-        if (gated) unpack_row(g, gw, ch, live);
-        fetch(r + TY);                  // the next row, while this one is worked on
+        unpack_row(f, row.f, ch, live);
+        unpack_row(d, row.d, ch, live);
+        if (gated) unpack_row(g, row.g, ch, live);
+        fetch(row, r + AHEAD * TY);     // a later row, while this one is worked on
         const float rstd = normalise<LPG>(f, ch, P);
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -238,7 +237,14 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormParams P)
                 if (P.act == CAWN_NORM_ACT_GATE) store_vec(static_cast<T *>(P.ggate) + r * P.C + ch[j], g[j]);
             }
         }
-    }
+    };
+    Row row[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; i++) fetch(row[i], r0 + ty + i * TY);
+    // the bound is the block's, not the row's: whole warps stay in the loop for the shuffles
+    for (long long base = r0; base < r1; base += AHEAD * TY)
+#pragma unroll
+        for (int i = 0; i < AHEAD; i++) work(row[i], base + ty + i * TY);
     if (P.part == nullptr) return;
     // row lanes fold their sums one after the other in a fixed order: shared memory holds one row
     for (int turn = 0; turn < TY; turn++) {
@@ -383,6 +389,8 @@ struct Cut {
     long long rows;
 };
 
+inline int threads_of(const Cut &c) { return (c.TX * c.TY + 31) / 32 * 32; }
+
 Cut cut_of(const cawn_norm_params *p, bool backward)
 {
     Cut c = {};
@@ -410,11 +418,16 @@ Cut cut_of(const cawn_norm_params *p, bool backward)
     c.TX = slots < 256 ? (int)slots : 256;
     c.by = (int)((slots + c.TX - 1) / c.TX);
     c.TY = c.TX >= 256 ? 1 : 256 / c.TX;
-    // forward: four rows a thread once there are enough rows to fill the GPU with that; backward: two
-    // blocks per SM walk all rows, so that few partial rows are left to sum
+    // forward: four rows a thread once there are enough rows to fill the GPU with that; backward: as many blocks
+    // as are resident at once by the registers a thread takes (by elements held), so that no second, mostly
+    // empty wave follows and few partial rows are left to sum
     int64_t bx;
     if (backward) {
-        bx = ((int64_t)sms * 4 + c.by - 1) / c.by;
+        const int held = c.nv * c.v, regs = held <= 1 ? 40 : held <= 4 ? 72 : held <= 8 ? 112 : held <= 16 ? 168 : 255;
+        int64_t each = 65536 / (regs * (int64_t)threads_of(c));
+        if (each > 8) each = 8;
+        if (each < 1) each = 1;
+        bx = sms * each / c.by;
     } else {
         const int64_t each = p->N * c.by >= (int64_t)sms * c.TY * 32 ? 4 : 1;
         bx = (p->N + c.TY * each - 1) / (c.TY * each);
@@ -483,7 +496,7 @@ int run(const cawn_norm_params *p, const Cut &c, const NormParams &P, bool bwd, 
     }
     Kernel<float, 1> k = half ? (c.v == 1 ? pick<bf16, 1>(c, bwd) : pick<bf16, 8>(c, bwd))
                               : (c.v == 1 ? pick<float, 1>(c, bwd) : pick<float, 4>(c, bwd));
-    const int threads = (c.TX * c.TY + 31) / 32 * 32;
+    const int threads = threads_of(c);
     const size_t smem = bwd && P.part != nullptr ? (size_t)2 * c.TX * c.nv * c.v * sizeof(float) : 0;
     return status_of(launch(k, dim3(c.bx, c.by), dim3(threads), smem, st, P));
 }
