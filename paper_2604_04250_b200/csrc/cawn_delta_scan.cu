@@ -258,16 +258,17 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
         float X[8][4] = {}, Y[MODE == MODE_SAVE ? 8 : 1][4] = {};
 #pragma unroll
         for (int d = 0; d < DK / 16; d++) {
-            unsigned a[3][4], b[4][NP][4];
+            constexpr int NS = MODE == MODE_SAVE || NP == 3 ? 3 : 2;
+            unsigned a[NS][4], b[4][NP][4];
 #pragma unroll
             for (int i = 0; i < 4; i++) load_right<NP, false>(b[i], at_nk(ks, ld, 16 * i, 16 * d), kC * ld);
             as_left(S[2 * d], S[2 * d + 1], a);
             if constexpr (MODE == MODE_OUT) put_left(sw.s, d, leading<NP>(a));
-            multiply<3, NP, 4>(X, a, b);
+            multiply<NS, NP, 4>(X, a, b);
             if constexpr (MODE == MODE_SAVE) {
 #pragma unroll
                 for (int i = 0; i < 4; i++) load_right<NP, false>(b[i], at_nk(smem_addr(st.q[0]), ld, 16 * i, 16 * d), kC * ld);
-                multiply<3, NP, 4>(Y, a, b);
+                multiply<NS, NP, 4>(Y, a, b);
             }
         }
         // R = V^T - e^G X (in X, and the start of r)
