@@ -25,8 +25,12 @@ namespace {
 
 template <int DK, int NP> struct RevStage {
     static constexpr int NT = NP == 1 ? 2 : 3, VLD = 16 * kRowGroups<NP> + kPad;
+    // r and the state come with the tiles, except where that would leave room for one stage only: asked for by the
+    // walk itself they cost it a trip to L2 each.
+    static constexpr bool FLOATS = DK == 64 || NP == 3;
     bf16 k[NP][kC * (DK + kPad)], q[NP][kC * (DK + kPad)], tri[NT][kC * kLd], p[NT][kC * kLd], go[NP][kC * VLD], v[NP][kC * VLD];
     float coef[kCoef][kC];
+    float4 rf[FLOATS ? kRowGroups<NP> * 8 * 32 : 0], sf[FLOATS ? kRowGroups<NP> * (DK / 8) * 32 : 0];
 };
 // No side warps: measured with dO^T P and (scale e^G dO)^T Q made ahead on the side, 160 us instead of 149.
 template <int DK, int NP> struct RevPlan {
@@ -37,7 +41,7 @@ template <int DK, int NP> struct RevPlan {
 };
 
 template <int DK, int NP>
-__device__ __forceinline__ void rev_load(const ChunkParams &P, RevStage<DK, NP> &st, int bh, int c, int v0, int vcols)
+__device__ __forceinline__ void rev_load(const ChunkParams &P, RevStage<DK, NP> &st, int bh, int c, int v0, int vcols, bool floats)
 {
     constexpr int NT = NP == 1 ? 2 : 3, TH = 32 * kFetch<NP>, VW = 16 * kRowGroups<NP>;
     const long long t0 = (long long)c * kC, nc = (long long)bh * P.chunks + c;
@@ -55,6 +59,14 @@ __device__ __forceinline__ void rev_load(const ChunkParams &P, RevStage<DK, NP> 
         load_dense<TH>(st.p[i], P.p + (nc * NT + i) * kTile);
     }
     for (int i = threadIdx.x % TH; i < kCoef * kC / 4; i += TH) cp16(smem_addr(&st.coef[0][0]) + i * 16, P.coef + nc * (kCoef * kC) + i * 4, true);
+    if constexpr (RevStage<DK, NP>::FLOATS) {
+        if (floats) {           // this block's row groups lie one after the other
+            const long long after = c + 1 < P.chunks ? nc + 1 : (long long)P.B * P.Hv * P.chunks + bh, g = v0 / 16 % 4;
+            const float4 *rf = P.rf + ((nc * P.vblocks + v0 / kC) * 4 + g) * (8 * 32), *sf = P.sf + ((after * P.vblocks + v0 / kC) * 4 + g) * (DK / 8 * 32);
+            for (int i = threadIdx.x % TH; i < kRowGroups<NP> * 8 * 32; i += TH) cp16(smem_addr(st.rf) + i * 16, rf + i, true);
+            for (int i = threadIdx.x % TH; i < kRowGroups<NP> * (DK / 8) * 32; i += TH) cp16(smem_addr(st.sf) + i * 16, sf + i, true);
+        }
+    }
     cp_commit();
 }
 
@@ -76,7 +88,7 @@ __global__ void __launch_bounds__((RevPlan<DK, NP>::threads), 1) delta_reverse_k
         for (int i = 0; i < count; i++) {
             const int s = i % CS;
             if (i >= CS) bar_sync(BAR_EMPTY + s, PAIR);
-            rev_load<DK, NP>(P, stages[s], bh, c1 - 1 - i, r0, vcols);
+            rev_load<DK, NP>(P, stages[s], bh, c1 - 1 - i, r0, vcols, !SUMMARY);
             cp_wait<0>();
             bar_arrive(BAR_FULL + s, PAIR);
         }
@@ -106,16 +118,11 @@ __global__ void __launch_bounds__((RevPlan<DK, NP>::threads), 1) delta_reverse_k
         const unsigned ks = smem_addr(st.k[0]), qs = smem_addr(st.q[0]), ts = smem_addr(st.tri[0]), ps = smem_addr(st.p[0]);
         const unsigned gs = smem_addr(st.go[0]), vs = smem_addr(st.v[0]);
 
-        // <state after the chunk, D>; D for the chunk's own gradients
+        // D for the chunk's own gradients
         if constexpr (!SUMMARY) {
-            const long long after = c + 1 < P.chunks ? nc + 1 : (long long)P.B * P.Hv * P.chunks + bh;
-            const float4 *sf = P.sf + ((after * P.vblocks + r0 / kC) * 4 + w4) * (DK / 8 * 32) + lane;
             bf16 *dst = P.ds + nv * (NP * kC * DK) + (16 * w4 + gr) * DK + tc;
-            float dot = 0.f;
 #pragma unroll
-            for (int n = 0; n < DK / 8; n++) {
-                const float4 x = sf[n * 32];
-                dot = fmaf(D[n][0], x.x, fmaf(D[n][1], x.y, fmaf(D[n][2], x.z, fmaf(D[n][3], x.w, dot))));
+            for (int n = 0; n < DK / 8; n++)
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
                     unsigned y[NP];
@@ -123,12 +130,23 @@ __global__ void __launch_bounds__((RevPlan<DK, NP>::threads), 1) delta_reverse_k
 #pragma unroll
                     for (int j = 0; j < NP; j++) *reinterpret_cast<unsigned *>(dst + j * (kC * DK) + 8 * h * DK + 8 * n) = y[j];
                 }
+        }
+        bar_sync(BAR_FULL + s, PAIR);
+        // <state after the chunk, D>
+        if constexpr (!SUMMARY) {
+            const long long after = c + 1 < P.chunks ? nc + 1 : (long long)P.B * P.Hv * P.chunks + bh;
+            const float4 *sf = RevStage<DK, NP>::FLOATS ? st.sf + w * (DK / 8 * 32) + lane
+                                                        : P.sf + ((after * P.vblocks + r0 / kC) * 4 + w4) * (DK / 8 * 32) + lane;
+            float dot = 0.f;
+#pragma unroll
+            for (int n = 0; n < DK / 8; n++) {
+                const float4 x = sf[n * 32];
+                dot = fmaf(D[n][0], x.x, fmaf(D[n][1], x.y, fmaf(D[n][2], x.z, fmaf(D[n][3], x.w, dot))));
             }
 #pragma unroll
             for (int o = 16; o > 0; o /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, o);
             if (lane == 0) P.sd[nv * 4 + w4] = dot;
         }
-        bar_sync(BAR_FULL + s, PAIR);
         // X = beta (e^{G_C - G} (D K^T) + dO^T P)
         float X[8][4] = {};
 #pragma unroll
@@ -169,7 +187,7 @@ __global__ void __launch_bounds__((RevPlan<DK, NP>::threads), 1) delta_reverse_k
 #pragma unroll
                 for (int m = 0; m < 2; m++) {
                     const int n = 2 * nb + m;
-                    const float4 r = P.rf[((nv * 4 + w4) * 8 + n) * 32 + lane];
+                    const float4 r = RevStage<DK, NP>::FLOATS ? st.rf[(w * 8 + n) * 32 + lane] : P.rf[((nv * 4 + w4) * 8 + n) * 32 + lane];
                     const float2 a = sum_terms(x, 2 * m), b = sum_terms(x, 2 * m + 1);
                     dots[n][0] = fmaf(rb[n][0], r.x, rb[n][2] * r.z);
                     dots[n][1] = fmaf(rb[n][1], r.y, rb[n][3] * r.w);
