@@ -139,39 +139,6 @@ __device__ __forceinline__ unsigned at_kn(unsigned base, int ld, int row, int co
     return base + ((row + l % 8 + l / 8 % 2 * 8) * ld + col + l / 16 * 8) * 2;
 }
 
-// A pair of floats in one 64-bit register: the accumulators' neighbours are handled two at a time.
-using f32x2 = unsigned long long;
-__device__ __forceinline__ f32x2 pair(float x, float y)
-{
-    f32x2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ f32x2 pair(float2 v) { return pair(v.x, v.y); }
-__device__ __forceinline__ float2 halves(f32x2 v)
-{
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
-{
-    f32x2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
-{
-    f32x2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
-{
-    f32x2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
 // rows h = 0, 1 of an accumulator tile, times / plus pairs
 __device__ __forceinline__ void scale_row(float (&c)[4], int h, f32x2 f)
 {
@@ -185,13 +152,6 @@ __device__ __forceinline__ void fma_row(float (&c)[4], int h, f32x2 a, f32x2 b)
     const float2 v = halves(fma2(a, pair(c[2 * h], c[2 * h + 1]), b));
     c[2 * h] = v.x;
     c[2 * h + 1] = v.y;
-}
-
-__device__ __forceinline__ float exp2_fast(float x)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
 }
 
 // Barriers of the walks, `threads` of both sides together: chain tiles are here / free again, what passes between chain

@@ -101,6 +101,23 @@ def test_norm_many_rows_and_repeatable():
     assert all(torch.equal(a, b) for a, b in zip(*got))
 
 
+@pytest.mark.parametrize("act", sorted(ACTS))
+def test_norm_without_eps(act):
+    """eps = 0 and a row count that leaves row lanes of the last block without a row."""
+    d, _ = norm_case(13, 3, 32, torch.float32, act, seed=8)
+    prm = cb.make_norm_params(13, 3, 32, eps=0.0, act=ACTS[act])
+    c = {n: on_gpu(t) for n, t in d.items()}
+    gx, gw, gb = torch.empty_like(c["x"]), torch.empty_like(c["w"]), torch.empty_like(c["b"])
+    gg = torch.empty_like(c["x"]) if act == "gate" else None
+    cb.cawn_group_norm_bwd(prm, c["x"], c["gy"], gx, cb.new_norm_workspace(prm), weight=c["w"], bias=c["b"], gate=c["gate"], grad_gate=gg, grad_weight=gw, grad_bias=gb)
+    w = {n: (t.double().requires_grad_() if t is not None else None) for n, t in d.items()}
+    want = group_norm(w["x"], 3, 0.0, False, w["w"], w["b"], ACTS[act], w["gate"])
+    wx, ww, wb = torch.autograd.grad(want, [w["x"], w["w"], w["b"]], d["gy"].double())
+    close(gx, wx, 2e-6)
+    close(gw, ww, SUM_TOL)
+    close(gb, wb, SUM_TOL)
+
+
 def test_norm_constant_row_and_bad_row():
     """A row without variance gives the bias (rms form excepted); NaN and infinity stay in their group."""
     d, prm = norm_case(3, 2, 64, torch.float32, "none", seed=5)
