@@ -54,7 +54,7 @@ struct Plan {
     int dk, terms, chunks, vblocks, segs, seg_chunks;    // terms: of an input
     size_t q, k, v, go;                  // three bfloat16 terms each, float storage only
     size_t coef, tri, p;
-    size_t u, s0, rf, sf, od, ds, rbt, rd, sd;   // backward
+    size_t rf, sf, od;                   // backward: rf also for rb, sf for the adjoints, od for rb.v
     size_t seg_state, seg_map;
     size_t total;
 };
@@ -72,7 +72,7 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
     // Time segments where the heads alone leave SMs without a block: they cost a second walk over values and keys,
     // so fewer than three do not pay.
     const int vw = 16 * (w.terms == 1 ? kRowGroups<1> : kRowGroups<3>);
-    const int64_t blocks = (int64_t)p->B * p->Hv * ((p->Dv + vw - 1) / vw);
+    const int64_t blocks = (int64_t)p->B * p->Hv * ((p->Dv + vw - 1) / vw) * (backward ? 2 : 1);
     int64_t segs = sm_count() / blocks;
     if (segs > w.chunks / 4) segs = w.chunks / 4;
     if (segs < 3) segs = 1;
@@ -94,18 +94,11 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
     w.p = w.tri;
     if (backward) {
         const double nv = (double)nc * w.vblocks, ends = (double)p->B * p->Hv * w.vblocks;
-        w.u = part(nv * w.terms * kTile * 2);
-        w.s0 = part(nv * w.terms * kC * w.dk * 2);
-        w.ds = w.s0;
         w.rf = part(nv * kTile * 4);
         w.sf = part((nv + ends) * kC * w.dk * 4);
         w.od = part(nv * 4 * kC * 4);
-        w.rd = 2 * w.od;
-        w.sd = part(nv * 4 * 4);
-        w.rbt = w.terms == 3 ? w.v : 0;
     }
-    w.total = w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + w.u + w.s0 + w.ds + w.rf + w.sf + w.od + w.rd + w.sd + w.rbt +
-              2 * w.seg_state + w.seg_map;
+    w.total = w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + 2 * (w.rf + w.sf + w.od) + (backward ? 4 : 2) * w.seg_state + w.seg_map;
     return w;
 }
 
@@ -206,7 +199,7 @@ extern "C" int cawn_delta_rule_fwd(const cawn_delta_params *params, const void *
     if (rc != CAWN_OK) return rc;
     C.o = o; C.state_out = state_out; C.o_stride_t = D.o_stride; C.o_stride_b = D.o_stride * params->L;
     cudaError_t e = launch_delta_prep(C, w.dk, w.terms, st);
-    if (e == cudaSuccess) e = launch_delta_scan(C, w.dk, w.terms, false, st);
+    if (e == cudaSuccess) e = launch_delta_scan(C, w.dk, w.terms, st);
     return status_of(e);
 }
 
@@ -235,26 +228,21 @@ extern "C" int cawn_delta_rule_bwd(const cawn_delta_params *params, const void *
     if (rc == CAWN_OK)
         rc = terms_of(C.go, grad_o, D.o_stride, (long long)params->B * params->L, params->L, params->Hv * params->Dv, w.terms, w.go, ws, st);
     if (rc != CAWN_OK) return rc;
-    C.u = ws.take<bf16>(w.u);
-    C.s0 = ws.take<bf16>(w.s0);
-    C.ds = ws.take<bf16>(w.ds);
     C.rf = ws.take<float4>(w.rf);
+    C.rbf = ws.take<float4>(w.rf);
     C.sf = ws.take<float4>(w.sf);
+    C.df = ws.take<float4>(w.sf);
     C.od = ws.take<float>(w.od);
-    C.rd = ws.take<float>(w.rd);
-    C.sd = ws.take<float>(w.sd);
-    C.rbt = ws.take<bf16>(w.rbt);
-    const long long vo = (long long)params->Hv * params->Dv;
-    C.rb = {w.terms == 1 ? static_cast<const bf16 *>(grad_v) : C.rbt, (long long)params->B * params->L * vo, vo, vo * params->L};
-    // the forward's walk, for the states and corrections
-    cudaError_t e = launch_delta_prep(C, w.dk, w.terms, st);
-    if (e == cudaSuccess) e = launch_delta_scan(C, w.dk, w.terms, true, st);
-    // the reverse walk: its "state" is the adjoint, its output the gradient of v
-    C.state_in = grad_state_out;
-    C.state_out = grad_state_in;
+    C.rv = ws.take<float>(w.od);
+    C.adj_start = ws.take<float>(w.seg_state);
+    C.adj_end = ws.take<float>(w.seg_state);
+    C.adj_in = grad_state_out; C.adj_out = grad_state_in;
     C.o = grad_v;
-    if (e == cudaSuccess) e = launch_delta_reverse(C, w.dk, w.terms, st);
+    C.o_stride_t = (long long)params->Hv * params->Dv;
+    C.o_stride_b = C.o_stride_t * params->L;
     C.gq = grad_q; C.gk = grad_k; C.gg = grad_g; C.gbeta = grad_beta;
+    cudaError_t e = launch_delta_prep(C, w.dk, w.terms, st);
+    if (e == cudaSuccess) e = launch_delta_walks(C, w.dk, w.terms, st);
     if (e == cudaSuccess) e = launch_delta_grads(C, w.dk, w.terms, st);
     return status_of(e);
 }

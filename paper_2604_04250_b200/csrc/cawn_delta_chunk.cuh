@@ -43,30 +43,26 @@ struct Terms {
 // vb their blocks of 64 values; tiles and coefficients of the workspace are dense over these.
 struct ChunkParams {
     Terms q, k, v, go;
-    Terms rb;                           // gradients kernel: rb, which is dV (bfloat16) or its terms
     const float *g, *beta;
     float *coef;                        // [nc][kCoef][64]
     bf16 *tri;                          // [nc][NT][64 j][64 i]: T - I transposed, blocks on and below T's diagonal
     bf16 *p;                            // [nc][NT][64 i][64 j]: P, blocks on and below the diagonal
-    // kept by the forward's walk for the backward
-    bf16 *u;                            // [nv][NP][64 t][64 v]
-    bf16 *s0;                           // [nv][NP][64 v][DK]: state before the chunk
-    float4 *rf, *sf;                    // [nv][4 warps][8 or DK/8 tiles][32 lanes]: r and the state before the chunk in float,
-                                        // as the walks' accumulators hold them
-    float *od;                          // [nv][4][64]: dO.o over 16 values
-    // kept by the reverse walk
-    bf16 *ds;                           // [nv][NP][64 v][DK]: adjoint of the state after the chunk
-    bf16 *rbt;                          // [NP] terms of rb, float storage only, laid out like v
-    float *rd;                          // [nv][4][2][64]: rb.r and rb.v over 16 values
-    float *sd;                          // [nv][4]: <state after the chunk, its adjoint> over 16 values
+    // The backward's walks leave accumulators as they hold them, [nv][4 row groups][tiles of 8 columns][32 lanes]: r
+    // and the state before the chunk (sf has a further end state per head), rb and the adjoint of the state after
+    // the chunk.
+    float4 *rf, *sf, *rbf, *df;
+    float *od, *rv;                     // [nv][4][64]: dO.o and rb.v over 16 values
     const float *state_in;              // [bh][Dv][Dk], may be NULL
     float *state_out;
+    const float *adj_in;                // gradient of state_out, may be NULL
+    float *adj_out;                     // gradient of state_in, may be NULL
     void *o;                            // forward output; backward: grad_v
     void *gq, *gk;
     float *gg, *gbeta;
     long long L, o_stride_t, o_stride_b;
-    // time segments: start states per segment, local end states, transitions
+    // time segments: start states per segment, local end states, transitions; adjoints likewise, from the end
     float *seg_start, *seg_end, *seg_map;   // [bh][segs][Dv][Dk], same, [bh][segs][Dk][Dk]
+    float *adj_start, *adj_end;
     int segs, seg_chunks;
     int B, Hk, Hv, Dk, Dv, chunks, vblocks;
     int p_terms;                        // terms of P that the walk will read
@@ -162,9 +158,6 @@ __device__ __forceinline__ void bar_arrive(int id, int threads) { asm volatile("
 
 // Row groups of a block: float storage has three times the tiles, so half the row groups fit.
 template <int NP> constexpr int kRowGroups = NP == 1 ? 4 : 2;
-
-// Warps that fetch tiles where there are no side warps to do it.
-template <int NP> constexpr int kFetch = NP == 1 ? 1 : 4;
 
 // Stages of the chain's and the side's tiles and of what they exchange: as many as fit.
 struct Stages { int chain, side, swap; };
@@ -336,6 +329,105 @@ __device__ __forceinline__ void triangle(float (&c)[8][4], Left left, At at, int
     }
 }
 
+// ------------------------------------------------------------------------------------ steps shared by the walks
+// X (8 token tiles) += rows of a state (NS terms) x K^T or Q^T (tile with rows of tokens)
+template <int NS, int NP, int DK> __device__ __forceinline__ void rows_times(float (&X)[8][4], const float (&S)[DK / 8][4], unsigned tile)
+{
+#pragma unroll
+    for (int d = 0; d < DK / 16; d++) {
+        unsigned a[NS][4], b[4][NP][4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) load_right<NP, false>(b[i], at_nk(tile, DK + kPad, 16 * i, 16 * d), kC * (DK + kPad));
+        as_left(S[2 * d], S[2 * d + 1], a);
+        multiply<NS, NP, 4>(X, a, b);
+    }
+}
+// x (tiles 2 nb .. 2 nb + 3 of a state's columns) += left x K or Q, token block by token block
+template <int NP, int DK> __device__ __forceinline__ void columns_times(float (&x)[4][4], const unsigned (&a)[4][3][4], unsigned tile, int nb)
+{
+#pragma unroll
+    for (int tb = 0; tb < 4; tb++) {
+        unsigned b[2][NP][4];
+#pragma unroll
+        for (int i = 0; i < 2; i++) load_right<NP, true>(b[i], at_kn(tile, DK + kPad, 16 * tb, 16 * (nb + i)), kC * (DK + kPad));
+        multiply<3, NP, 2>(x, a[tb], b);
+    }
+}
+// every token's column of tiles times its coefficient (row `which` of coef)
+__device__ __forceinline__ void scale_tokens(float (&x)[8][4], const float (*coef)[kC], int which, float sign = 1.f)
+{
+    const int tc = threadIdx.x % 4 * 2;
+#pragma unroll
+    for (int n = 0; n < 8; n++) {
+        const float2 f = *reinterpret_cast<const float2 *>(&coef[which][8 * n + tc]);
+        const f32x2 g = sign == 1.f ? pair(f) : pair(sign * f.x, sign * f.y);
+        scale_row(x[n], 0, g);
+        scale_row(x[n], 1, g);
+    }
+}
+// R = V^T - e^G X, V a tile with rows of tokens, `addr` this row group's block of it
+template <int NP> __device__ __forceinline__ void residual(float (&X)[8][4], const float (*coef)[kC], unsigned tile, int vld, int col, bool values)
+{
+    const int tc = threadIdx.x % 4 * 2;
+#pragma unroll
+    for (int nb = 0; nb < 4; nb++) {
+        unsigned v[NP][4] = {};
+        if (values) load_left<NP, true>(v, at_nk(tile, vld, 16 * nb, col), kC * vld);
+#pragma unroll
+        for (int m = 0; m < 2; m++) {
+            const float2 e = *reinterpret_cast<const float2 *>(&coef[COEF_EG][16 * nb + 8 * m + tc]);
+#pragma unroll
+            for (int h = 0; h < 2; h++) fma_row(X[2 * nb + m], h, pair(-e.x, -e.y), pair(sum_terms(v, 2 * m + h)));
+        }
+    }
+}
+// sum over this thread's rows of x times a value tile with rows of tokens (dO or V)
+template <int NP> __device__ __forceinline__ void dots_with(float (&dots)[8][2], const float (&x)[8][4], unsigned tile, int vld, int col)
+{
+#pragma unroll
+    for (int nb = 0; nb < 4; nb++) {
+        unsigned v[NP][4];
+        load_left<NP, true>(v, at_nk(tile, vld, 16 * nb, col), kC * vld);
+#pragma unroll
+        for (int m = 0; m < 2; m++) {
+            const int n = 2 * nb + m;
+            const float2 a = sum_terms(v, 2 * m), b = sum_terms(v, 2 * m + 1);
+            dots[n][0] = fmaf(x[n][0], a.x, x[n][2] * b.x);
+            dots[n][1] = fmaf(x[n][1], a.y, x[n][3] * b.y);
+        }
+    }
+}
+// state rows r, r + 8 (r = this thread's) from / to [Dv][Dk] floats
+template <int DK> __device__ __forceinline__ void load_state(float (&S)[DK / 8][4], const float *from, int r, int rows, int Dk)
+{
+    const int tc = threadIdx.x % 4 * 2;
+#pragma unroll
+    for (int n = 0; n < DK / 8; n++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            float2 x = make_float2(0.f, 0.f);
+            if (from != nullptr && r + 8 * h < rows && 8 * n + tc < Dk) x = *reinterpret_cast<const float2 *>(from + (long long)(r + 8 * h) * Dk + 8 * n + tc);
+            S[n][2 * h] = x.x;
+            S[n][2 * h + 1] = x.y;
+        }
+}
+template <int DK> __device__ __forceinline__ void store_state(float *to, const float (&S)[DK / 8][4], int r, int rows, int Dk)
+{
+    const int tc = threadIdx.x % 4 * 2;
+#pragma unroll
+    for (int n = 0; n < DK / 8; n++)
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+            if (r + 8 * h < rows && 8 * n + tc < Dk)
+                *reinterpret_cast<float2 *>(to + (long long)(r + 8 * h) * Dk + 8 * n + tc) = make_float2(S[n][2 * h], S[n][2 * h + 1]);
+}
+// accumulator tiles to / from the walks' arrays
+template <int N> __device__ __forceinline__ void store_tiles(float4 *to, const float (&x)[N][4])
+{
+#pragma unroll
+    for (int n = 0; n < N; n++) to[n * 32 + threadIdx.x % 32] = make_float4(x[n][0], x[n][1], x[n][2], x[n][3]);
+}
+
 // Value head's place
 __device__ __forceinline__ long long q_base(const ChunkParams &P, const Terms &t, int bh, long long t0)
 {
@@ -349,10 +441,12 @@ __device__ __forceinline__ long long v_base(const ChunkParams &P, const Terms &t
 // terms: NP
 cudaError_t launch_delta_split(const float *src, bf16 *dst, long long plane, long long rows, int width, long long stride, cudaStream_t st);
 cudaError_t launch_delta_prep(const ChunkParams &P, int dk, int terms, cudaStream_t st);
-// forward over the chunks: outputs (or, for the backward, what it needs to keep: `save`)
-cudaError_t launch_delta_scan(const ChunkParams &P, int dk, int terms, bool save, cudaStream_t st);
-cudaError_t launch_delta_join(const ChunkParams &P, int dk, bool reverse, cudaStream_t st);
-cudaError_t launch_delta_reverse(const ChunkParams &P, int dk, int terms, cudaStream_t st);
+// forward over the chunks: outputs and end state
+cudaError_t launch_delta_scan(const ChunkParams &P, int dk, int terms, cudaStream_t st);
+// start states of time segments (and of the adjoint's) from what the summaries left
+cudaError_t launch_delta_join(const ChunkParams &P, int dk, bool adjoint, cudaStream_t st);
+// backward: the forward's walk and the reverse one, then what is local to a chunk
+cudaError_t launch_delta_walks(const ChunkParams &P, int dk, int terms, cudaStream_t st);
 cudaError_t launch_delta_grads(const ChunkParams &P, int dk, int terms, cudaStream_t st);
 
 }  // namespace cawn

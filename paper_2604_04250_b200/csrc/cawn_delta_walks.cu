@@ -1,0 +1,368 @@
+// Gated delta rule, chunk form: the backward's two walks, side by side.
+//
+// The forward's walk again, for what the gradients need of it,
+//   X = S K^T,  R = V^T - e^G X,  r = R T^T,  u = beta r,  o = scale e^G S Q^T + u P^T,  S <- e^{G_C} S + (e^{G_C - G} u) K,
+// and the reverse walk, with D the adjoint of the state after a chunk,
+//   dU = P^T dO + e^{G_C - G} (K D^T),   rb = T^T (beta dU),   D <- e^{G_C} D + (scale e^G dO)^T Q - (e^G rb)^T K.
+// Neither needs the other: one launch runs both, a block per head, 16 * row groups of values and direction.
+// Bound: each walk is a chain of products and of the instructions between them that leaves its scheduler waiting
+// half of the time, so two blocks share an SM where registers and shared memory allow (64 keys, bfloat16): the
+// two directions of 96 heads together take what either took alone before.  For that a block has its four chain
+// warps only, which also fetch: tiles that a chunk starts with are double-buffered, those that it needs later are
+// asked for when it starts.
+#include "cawn_delta_chunk.cuh"
+
+#include <type_traits>
+
+namespace cawn {
+namespace {
+
+template <int DK, int NP> struct WalkTiles {
+    static constexpr int NT = NP == 1 ? 2 : 3, VLD = 16 * kRowGroups<NP> + kPad;
+    using Keys = bf16[NP][kC * (DK + kPad)];
+    using Values = bf16[NP][kC * VLD];
+    using Square = bf16[NT][kC * kLd];
+    struct FwdEarly { Keys k, q; Values v; float coef[kCoef][kC]; };
+    struct FwdLate { Square tri, p; Values go; };
+    struct RevEarly { Keys k; Values go; Square p; float coef[kCoef][kC]; };
+    struct RevLate { Keys q; Square tri; Values v; };
+};
+template <int DK, int NP> struct WalkPlan {
+    using Tiles = WalkTiles<DK, NP>;
+    static constexpr int RG = kRowGroups<NP>, VW = 16 * RG;
+    static constexpr int threads = NP == 1 ? 32 * RG : 128;     // float storage: two more warps that fetch
+    static constexpr size_t max(size_t a, size_t b) { return a > b ? a : b; }
+    static constexpr size_t early = max(sizeof(typename Tiles::FwdEarly), sizeof(typename Tiles::RevEarly));
+    static constexpr size_t late = max(sizeof(typename Tiles::FwdLate), sizeof(typename Tiles::RevLate));
+    static constexpr int stages = 2 * early + late <= 227 * 1024 ? 2 : 1;
+    static constexpr size_t smem = stages * early + late;
+    static constexpr int blocks = 2 * (smem + 1024) <= 228 * 1024 ? 2 : 1;      // per SM
+    static_assert(smem <= 227 * 1024, "fits an SM");
+};
+
+template <int DK, int NP> struct Fetch {
+    using Plan = WalkPlan<DK, NP>;
+    static constexpr int TH = Plan::threads, NT = Plan::Tiles::NT, VW = Plan::VW;
+    const ChunkParams &P;
+    int bh, v0, vcols;
+    __device__ __forceinline__ int rows(int c) const { return P.L - (long long)c * kC < kC ? (int)(P.L - (long long)c * kC) : kC; }
+    __device__ __forceinline__ void keys(typename Plan::Tiles::Keys &to, const Terms &t, int c) const
+    {
+#pragma unroll
+        for (int i = 0; i < NP; i++) load_tile<kC, DK, TH>(to[i], t.at + i * t.plane + q_base(P, t, bh, (long long)c * kC), t.stride_t, rows(c), P.Dk);
+    }
+    __device__ __forceinline__ void values(typename Plan::Tiles::Values &to, const Terms &t, int c) const
+    {
+#pragma unroll
+        for (int i = 0; i < NP; i++) load_tile<kC, VW, TH>(to[i], t.at + i * t.plane + v_base(P, t, bh, (long long)c * kC) + v0, t.stride_t, rows(c), vcols);
+    }
+    __device__ __forceinline__ void square(typename Plan::Tiles::Square &to, const bf16 *from, int c) const
+    {
+#pragma unroll
+        for (int i = 0; i < NT; i++) load_dense<TH>(to[i], from + (((long long)bh * P.chunks + c) * NT + i) * kTile);
+    }
+    __device__ __forceinline__ void coef(float (&to)[kCoef][kC], int c) const
+    {
+        if (threadIdx.x < kCoef * kC / 4)
+            cp16(smem_addr(&to[0][0]) + threadIdx.x * 16, P.coef + ((long long)bh * P.chunks + c) * (kCoef * kC) + threadIdx.x * 4, true);
+    }
+};
+static_assert(kCoef * kC / 4 <= 128, "one word per thread");
+
+// A walk's chunk: wait for the early tiles, ask for the late ones and for the next chunk's early ones.
+// `load_early(i)`, `load_late(i)`: tiles of the i-th chunk of the walk.
+template <int STAGES, class Early, class Late> __device__ __forceinline__ void begin_chunk(int i, int count, Early load_early, Late load_late)
+{
+    if (STAGES == 1 && i > 0) __syncthreads();      // everyone is done with the one set there is
+    if (STAGES == 1 || i == 0) {
+        load_early(i);
+        cp_commit();
+    }
+    cp_wait<0>();
+    __syncthreads();            // the early tiles are here, and everyone is done with the chunk before
+    load_late(i);
+    cp_commit();
+    if (STAGES == 2) {
+        if (i + 1 < count) load_early(i + 1);
+        cp_commit();            // possibly empty, which keeps the count
+    }
+}
+template <int STAGES> __device__ __forceinline__ void late_tiles()
+{
+    if (STAGES == 2) cp_wait<1>(); else cp_wait<0>();
+    __syncthreads();
+}
+
+// SUMMARY: what a segment's own tokens leave at its end (forward; with the transitions, which are the walk of the
+// identity's rows with V = 0) or send to its start (reverse).
+template <int DK, int NP, bool SUMMARY>
+__device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char *raw, int block)
+{
+    using Plan = WalkPlan<DK, NP>;
+    using Early = typename Plan::Tiles::FwdEarly;
+    constexpr int NT = Plan::Tiles::NT, VW = Plan::VW, VLD = Plan::Tiles::VLD, STAGES = Plan::stages;
+    auto stage = [&](int i) -> Early & { return *reinterpret_cast<Early *>(raw + (i % STAGES) * Plan::early); };
+    auto &late = *reinterpret_cast<typename Plan::Tiles::FwdLate *>(raw + STAGES * Plan::early);
+    const int bh = blockIdx.x, seg = blockIdx.z, vblks = (P.Dv + VW - 1) / VW;
+    const bool ident = SUMMARY && block >= vblks;
+    const int r0 = (block - (ident ? vblks : 0)) * VW, vcols = ident ? 0 : (P.Dv - r0 < VW ? P.Dv - r0 : VW);
+    const int c0 = seg * P.seg_chunks, c1 = c0 + P.seg_chunks < P.chunks ? c0 + P.seg_chunks : P.chunks, count = c1 - c0;
+    const int lane = threadIdx.x % 32, w = threadIdx.x / 32, gr = lane / 4, tc = lane % 4 * 2, w4 = (r0 / 16 + w) % 4;
+    const bool walks = w < Plan::RG;
+    const int row = r0 + 16 * w + gr;
+    const Fetch<DK, NP> fetch = {P, bh, r0, vcols};
+    auto load_early = [&](int i) {
+        Early &e = stage(i);
+        fetch.keys(e.k, P.k, c0 + i);
+        if (vcols > 0) fetch.values(e.v, P.v, c0 + i);
+        if (!SUMMARY) fetch.keys(e.q, P.q, c0 + i);
+        fetch.coef(e.coef, c0 + i);
+    };
+    auto load_late = [&](int i) {
+        fetch.square(late.tri, P.tri, c0 + i);
+        if (!SUMMARY) {
+            fetch.square(late.p, P.p, c0 + i);
+            fetch.values(late.go, P.go, c0 + i);
+        }
+    };
+    float S[DK / 8][4];
+    if (ident) {
+#pragma unroll
+        for (int n = 0; n < DK / 8; n++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) S[n][e] = row + e / 2 * 8 == 8 * n + tc + e % 2 ? 1.f : 0.f;
+    } else {
+        const float *from = SUMMARY ? nullptr
+                            : P.segs > 1 ? P.seg_start + ((long long)bh * P.segs + seg) * P.Dv * P.Dk
+                                         : (P.state_in != nullptr ? P.state_in + (long long)bh * P.Dv * P.Dk : nullptr);
+        load_state<DK>(S, from, walks ? row : P.Dv, P.Dv, P.Dk);
+    }
+    for (int i = 0; i < count; i++) {
+        begin_chunk<STAGES>(i, count, load_early, load_late);
+        const long long g = (((long long)bh * P.chunks + c0 + i) * P.vblocks + r0 / kC) * 4 + w4;       // row group in the arrays
+        Early &e = stage(i);
+        const unsigned ks = smem_addr(e.k[0]);
+        float X[8][4] = {}, Y[SUMMARY ? 1 : 8][4] = {};
+        if (walks) {
+            rows_times<3, NP, DK>(X, S, ks);
+            if constexpr (!SUMMARY) {
+                store_tiles(P.sf + g * (DK / 8 * 32), S);
+                rows_times<3, NP, DK>(Y, S, smem_addr(e.q[0]));
+                scale_tokens(Y, e.coef, COEF_EG, P.scale);
+            }
+            residual<NP>(X, e.coef, smem_addr(e.v[0]), VLD, 16 * w, vcols > 0);
+        }
+        late_tiles<STAGES>();
+        if (!walks) continue;
+        float r[8][4];
+#pragma unroll
+        for (int n = 0; n < 8; n++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) r[n][j] = X[n][j];
+        triangle<3, NT, true, false>(r, [&](unsigned (&a)[3][4], int tb) { as_left(X[2 * tb], X[2 * tb + 1], a); },
+                                     [&](int tb, int nb) { return at_kn(smem_addr(late.tri[0]), kLd, 16 * tb, 16 * nb); }, kC * kLd);
+        if constexpr (!SUMMARY) store_tiles(P.rf + g * (8 * 32), r);
+        scale_tokens(r, e.coef, COEF_BETA);
+        if constexpr (!SUMMARY) {
+            triangle<3, NT, false, false>(Y, [&](unsigned (&a)[3][4], int tb) { as_left(r[2 * tb], r[2 * tb + 1], a); },
+                                          [&](int tb, int nb) { return at_nk(smem_addr(late.p[0]), kLd, 16 * nb, 16 * tb); }, kC * kLd);
+            float dots[8][2];
+            dots_with<NP>(dots, Y, smem_addr(late.go[0]), VLD, 16 * w);
+            column_sums(dots);
+            *reinterpret_cast<float2 *>(P.od + g * kC + 8 * gr + tc) = make_float2(dots[0][0], dots[0][1]);
+        }
+        // the update is summed from zero and added once, as in the forward
+        const float eC = e.coef[COEF_EG][kC - 1];
+        scale_tokens(r, e.coef, COEF_LEFT);
+        unsigned a[4][3][4];
+#pragma unroll
+        for (int tb = 0; tb < 4; tb++) as_left(r[2 * tb], r[2 * tb + 1], a[tb]);
+#pragma unroll
+        for (int nb = 0; nb < DK / 16; nb += 2) {
+            float x[4][4] = {};
+            columns_times<NP, DK>(x, a, ks, nb);
+#pragma unroll
+            for (int m = 0; m < 4; m++)
+#pragma unroll
+                for (int h = 0; h < 2; h++) fma_row(S[2 * nb + m], h, pair(eC, eC), pair(x[m][2 * h], x[m][2 * h + 1]));
+        }
+    }
+    if (!walks) return;
+    if constexpr (SUMMARY) {
+        if (ident) store_state<DK>(P.seg_map + ((long long)bh * P.segs + seg) * P.Dk * P.Dk, S, row, P.Dk, P.Dk);
+        else store_state<DK>(P.seg_end + ((long long)bh * P.segs + seg) * P.Dv * P.Dk, S, row, P.Dv, P.Dk);
+    } else if (seg == P.segs - 1) {         // behind the last chunk's, a state per head
+        const long long g = (((long long)P.B * P.Hv * P.chunks + bh) * P.vblocks + r0 / kC) * 4 + w4;
+        store_tiles(P.sf + g * (DK / 8 * 32), S);
+    }
+}
+
+template <int DK, int NP, bool SUMMARY, class T>
+__device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char *raw, int block)
+{
+    using Plan = WalkPlan<DK, NP>;
+    using Early = typename Plan::Tiles::RevEarly;
+    constexpr int NT = Plan::Tiles::NT, VW = Plan::VW, VLD = Plan::Tiles::VLD, STAGES = Plan::stages;
+    auto stage = [&](int i) -> Early & { return *reinterpret_cast<Early *>(raw + (i % STAGES) * Plan::early); };
+    auto &late = *reinterpret_cast<typename Plan::Tiles::RevLate *>(raw + STAGES * Plan::early);
+    const int bh = blockIdx.x, seg = blockIdx.z, r0 = block * VW, vcols = P.Dv - r0 < VW ? P.Dv - r0 : VW;
+    const int c0 = seg * P.seg_chunks, c1 = c0 + P.seg_chunks < P.chunks ? c0 + P.seg_chunks : P.chunks, count = c1 - c0;
+    const int lane = threadIdx.x % 32, w = threadIdx.x / 32, gr = lane / 4, tc = lane % 4 * 2, w4 = (r0 / 16 + w) % 4;
+    const bool walks = w < Plan::RG;
+    const int row = r0 + 16 * w + gr;
+    const Fetch<DK, NP> fetch = {P, bh, r0, vcols};
+    auto load_early = [&](int i) {
+        Early &e = stage(i);
+        fetch.keys(e.k, P.k, c1 - 1 - i);
+        fetch.values(e.go, P.go, c1 - 1 - i);
+        fetch.square(e.p, P.p, c1 - 1 - i);
+        fetch.coef(e.coef, c1 - 1 - i);
+    };
+    auto load_late = [&](int i) {
+        fetch.square(late.tri, P.tri, c1 - 1 - i);
+        fetch.keys(late.q, P.q, c1 - 1 - i);
+        if (!SUMMARY) fetch.values(late.v, P.v, c1 - 1 - i);
+    };
+    float D[DK / 8][4];
+    const float *from = SUMMARY ? nullptr
+                        : P.segs > 1 ? P.adj_start + ((long long)bh * P.segs + seg) * P.Dv * P.Dk
+                                     : (P.adj_in != nullptr ? P.adj_in + (long long)bh * P.Dv * P.Dk : nullptr);
+    load_state<DK>(D, from, walks ? row : P.Dv, P.Dv, P.Dk);
+
+    for (int i = 0; i < count; i++) {
+        begin_chunk<STAGES>(i, count, load_early, load_late);
+        const int c = c1 - 1 - i;
+        const long long t0 = (long long)c * kC, g = (((long long)bh * P.chunks + c) * P.vblocks + r0 / kC) * 4 + w4;
+        Early &e = stage(i);
+        const unsigned ks = smem_addr(e.k[0]), gs = smem_addr(e.go[0]);
+        // X = beta (e^{G_C - G} (D K^T) + dO^T P)
+        float X[8][4] = {};
+        if (walks) {
+            rows_times<3, NP, DK>(X, D, ks);
+            if constexpr (!SUMMARY) store_tiles(P.df + g * (DK / 8 * 32), D);
+            scale_tokens(X, e.coef, COEF_LEFT);
+            triangle<NP, NT, true, true>(X, [&](unsigned (&a)[NP][4], int ib) { load_left<NP, true>(a, at_nk(gs, VLD, 16 * ib, 16 * w), kC * VLD); },
+                                         [&](int ib, int nb) { return at_kn(smem_addr(e.p[0]), kLd, 16 * ib, 16 * nb); }, kC * kLd);
+            scale_tokens(X, e.coef, COEF_BETA);
+        }
+        late_tiles<STAGES>();
+        if (!walks) continue;
+        const unsigned qs = smem_addr(late.q[0]), vs = smem_addr(late.v[0]);
+        // rb = X + (T - I)^T X
+        float rb[8][4];
+#pragma unroll
+        for (int n = 0; n < 8; n++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) rb[n][j] = X[n][j];
+        triangle<3, NT, false, true>(rb, [&](unsigned (&a)[3][4], int ib) { as_left(X[2 * ib], X[2 * ib + 1], a); },
+                                     [&](int ib, int nb) { return at_nk(smem_addr(late.tri[0]), kLd, 16 * nb, 16 * ib); }, kC * kLd);
+        if constexpr (!SUMMARY) {
+            store_tiles(P.rbf + g * (8 * 32), rb);
+            float dots[8][2];
+            dots_with<NP>(dots, rb, vs, VLD, 16 * w);
+            column_sums(dots);
+            *reinterpret_cast<float2 *>(P.rv + g * kC + 8 * gr + tc) = make_float2(dots[0][0], dots[0][1]);
+            // dV = rb
+            const int rows = fetch.rows(c);
+            T *gv = static_cast<T *>(P.o) + (bh / P.Hv) * P.o_stride_b + t0 * P.o_stride_t + (long long)(bh % P.Hv) * P.Dv + r0;
+            if constexpr (sizeof(T) == 2) {         // as token rows, through this warp's own part of the V tile
+                __syncwarp();
+#pragma unroll
+                for (int nb = 0; nb < 4; nb++)
+                    stsm_t(at_nk(vs, VLD, 16 * nb, 16 * w), pack_bf16(rb[2 * nb][0], rb[2 * nb][1]), pack_bf16(rb[2 * nb][2], rb[2 * nb][3]),
+                           pack_bf16(rb[2 * nb + 1][0], rb[2 * nb + 1][1]), pack_bf16(rb[2 * nb + 1][2], rb[2 * nb + 1][3]));
+                __syncwarp();
+#pragma unroll
+                for (int j = lane; j < 128; j += 32) {
+                    const int t = j / 2, v = 16 * w + j % 2 * 8;
+                    if (t < rows && v < vcols) *reinterpret_cast<uint4 *>(gv + t * P.o_stride_t + v) = *reinterpret_cast<const uint4 *>(&late.v[0][t * VLD + v]);
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < 8; n++)
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        const int t = 8 * n + tc + (j & 1), v = 16 * w + gr + (j >> 1) * 8;
+                        if (t < rows && v < vcols) gv[t * P.o_stride_t + v] = narrow<T>(rb[n][j]);
+                    }
+            }
+        }
+        // D <- e^{G_C} D + (scale e^G dO)^T Q - (e^G rb)^T K, the update summed from zero
+        const float eC = e.coef[COEF_EG][kC - 1];
+        scale_tokens(rb, e.coef, COEF_EG, -1.f);
+        unsigned a[4][3][4], f[4][3][4];
+#pragma unroll
+        for (int tb = 0; tb < 4; tb++) {
+            unsigned x[NP][4];
+            load_left<NP, true>(x, at_nk(gs, VLD, 16 * tb, 16 * w), kC * VLD);
+            float y[2][4];
+#pragma unroll
+            for (int m = 0; m < 2; m++) {
+                const float2 eg = *reinterpret_cast<const float2 *>(&e.coef[COEF_EG][16 * tb + 8 * m + tc]);
+                const f32x2 plus = pair(P.scale * eg.x, P.scale * eg.y);
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const float2 z = halves(mul2(plus, pair(sum_terms(x, 2 * m + h))));
+                    y[m][2 * h] = z.x;
+                    y[m][2 * h + 1] = z.y;
+                }
+            }
+            as_left(y[0], y[1], a[tb]);
+            as_left(rb[2 * tb], rb[2 * tb + 1], f[tb]);
+        }
+#pragma unroll
+        for (int nb = 0; nb < DK / 16; nb += 2) {
+            float x[4][4] = {};
+            columns_times<NP, DK>(x, a, qs, nb);
+            columns_times<NP, DK>(x, f, ks, nb);
+#pragma unroll
+            for (int m = 0; m < 4; m++)
+#pragma unroll
+                for (int h = 0; h < 2; h++) fma_row(D[2 * nb + m], h, pair(eC, eC), pair(x[m][2 * h], x[m][2 * h + 1]));
+        }
+    }
+    if (!walks) return;
+    float *to = SUMMARY ? P.adj_end + ((long long)bh * P.segs + seg) * P.Dv * P.Dk
+                : P.adj_out != nullptr && seg == 0 ? P.adj_out + (long long)bh * P.Dv * P.Dk : nullptr;
+    if (to != nullptr) store_state<DK>(to, D, row, P.Dv, P.Dk);
+}
+
+template <int DK, int NP, bool SUMMARY, class T>
+__global__ void __launch_bounds__((WalkPlan<DK, NP>::threads), (WalkPlan<DK, NP>::blocks)) delta_walks_kernel(const ChunkParams P)
+{
+    extern __shared__ __align__(16) unsigned char raw[];
+    const int back = (P.Dv + WalkPlan<DK, NP>::VW - 1) / WalkPlan<DK, NP>::VW;      // the reverse walk's blocks come first
+    if ((int)blockIdx.y < back) reverse_walk<DK, NP, SUMMARY, T>(P, raw, blockIdx.y);
+    else forward_walk<DK, NP, SUMMARY>(P, raw, blockIdx.y - back);
+}
+
+template <int DK, int NP, bool SUMMARY> cudaError_t walks(const ChunkParams &P, cudaStream_t st)
+{
+    using T = typename std::conditional<NP == 1, bf16, float>::type;
+    using Plan = WalkPlan<DK, NP>;
+    auto *kernel = delta_walks_kernel<DK, NP, SUMMARY, T>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan::smem);
+    if (e != cudaSuccess) return e;
+    const int vblks = (P.Dv + Plan::VW - 1) / Plan::VW, ident = SUMMARY ? (P.Dk + Plan::VW - 1) / Plan::VW : 0;
+    return launch(kernel, dim3((unsigned)(P.B * P.Hv), 2 * vblks + ident, P.segs), dim3(Plan::threads), Plan::smem, st, P);
+}
+
+template <int DK, int NP> cudaError_t run(const ChunkParams &P, cudaStream_t st)
+{
+    if (P.segs > 1) {
+        cudaError_t e = walks<DK, NP, true>(P, st);
+        if (e == cudaSuccess) e = launch_delta_join(P, DK, true, st);
+        if (e != cudaSuccess) return e;
+    }
+    return walks<DK, NP, false>(P, st);
+}
+
+}  // namespace
+
+cudaError_t launch_delta_walks(const ChunkParams &P, int dk, int terms, cudaStream_t st)
+{
+    if (dk == 64) return terms == 1 ? run<64, 1>(P, st) : run<64, 3>(P, st);
+    return terms == 1 ? run<128, 1>(P, st) : run<128, 3>(P, st);
+}
+
+}  // namespace cawn
