@@ -109,53 +109,40 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
             // The walks' accumulators of this warp's row group: r and rb (first four warps), states and D (the others).
             const long long g = g0 + v0 / 16 + w;
             const bool mine = w < VW / 16 && v0 + 16 * w < P.Dv;
-            float r[8][4], rb[8][4];
-            if (mine && qside) {
-#pragma unroll
-                for (int n = 0; n < 8; n++) {
-                    get_tile(r[n], P.rf + (g * 8 + n) * 32 + lane);
-                    get_tile(rb[n], P.rbf + (g * 8 + n) * 32 + lane);
-                }
-            }
             cp_wait<0>();
             __syncthreads();                // coefficients are here
             if (w < VW / 16 && qside) {
-                if (mine) {
-                    float dots[8][2];
+                float dots[8][2];
 #pragma unroll
-                    for (int n = 0; n < 8; n++) {
-                        dots[n][0] = fmaf(r[n][0], rb[n][0], r[n][2] * rb[n][2]);
-                        dots[n][1] = fmaf(r[n][1], rb[n][1], r[n][3] * rb[n][3]);
+                for (int n = 0; n < 8; n++) {
+                    float r[1][4] = {}, rb[1][4] = {};
+                    if (mine) {
+                        get_tile(r[0], P.rf + (g * 8 + n) * 32 + lane);
+                        get_tile(rb[0], P.rbf + (g * 8 + n) * 32 + lane);
                     }
-                    column_sums(dots);
-                    *reinterpret_cast<float2 *>(&sm.dots[v0 / 16 + w][2][8 * gr + tc]) = make_float2(dots[0][0], dots[0][1]);
-                    scale_tokens(r, sm.coef, COEF_BETA);
-                } else {
-#pragma unroll
-                    for (int n = 0; n < 8; n++)
-#pragma unroll
-                        for (int e = 0; e < 4; e++) r[n][e] = rb[n][e] = 0.f;
+                    dots[n][0] = fmaf(r[0][0], rb[0][0], r[0][2] * rb[0][2]);
+                    dots[n][1] = fmaf(r[0][1], rb[0][1], r[0][3] * rb[0][3]);
+                    const f32x2 bt = pair(*reinterpret_cast<const float2 *>(&sm.coef[COEF_BETA][8 * n + tc]));
+                    scale_row(r[0], 0, bt);
+                    scale_row(r[0], 1, bt);
+                    rows_to_tile<NP>(sm.v.u[0] + 8 * n, VW * kLd, kLd, 16 * w + gr, r);
+                    rows_to_tile<NP>(sm.v.rb[0] + 8 * n, VW * kLd, kLd, 16 * w + gr, rb);
                 }
-                rows_to_tile<NP>(sm.v.u[0], VW * kLd, kLd, 16 * w + gr, r);
-                rows_to_tile<NP>(sm.v.rb[0], VW * kLd, kLd, 16 * w + gr, rb);
+                column_sums(dots);
+                if (mine) *reinterpret_cast<float2 *>(&sm.dots[v0 / 16 + w][2][8 * gr + tc]) = make_float2(dots[0][0], dots[0][1]);
             } else if (w < VW / 16) {
                 const long long next = c + 1 < P.chunks ? g + P.vblocks * 4 : ((long long)P.B * P.Hv * P.chunks + bh) * P.vblocks * 4 + v0 / 16 + w;
                 float dot = 0.f;
 #pragma unroll
-                for (int n = 0; n < DK / 8; n += 4) {
-                    float s0[4][4] = {}, d[4][4] = {}, s1[4][4] = {};
+                for (int n = 0; n < DK / 8; n++) {
+                    float s0[1][4] = {}, d[1][4] = {}, s1[4] = {};
                     if (mine) {
-#pragma unroll
-                        for (int m = 0; m < 4; m++) {
-                            get_tile(s0[m], P.sf + (g * (DK / 8) + n + m) * 32 + lane);
-                            get_tile(d[m], P.df + (g * (DK / 8) + n + m) * 32 + lane);
-                            get_tile(s1[m], P.sf + (next * (DK / 8) + n + m) * 32 + lane);
-                        }
+                        get_tile(s0[0], P.sf + (g * (DK / 8) + n) * 32 + lane);
+                        get_tile(d[0], P.df + (g * (DK / 8) + n) * 32 + lane);
+                        get_tile(s1, P.sf + (next * (DK / 8) + n) * 32 + lane);
                     }
 #pragma unroll
-                    for (int m = 0; m < 4; m++)
-#pragma unroll
-                        for (int e = 0; e < 4; e++) dot = fmaf(s1[m][e], d[m][e], dot);
+                    for (int e = 0; e < 4; e++) dot = fmaf(s1[e], d[0][e], dot);
                     rows_to_tile<NP>(sm.v.s0[0] + 8 * n, VW * ld, ld, 16 * w + gr, s0);
                     rows_to_tile<NP>(sm.v.ds[0] + 8 * n, VW * ld, ld, 16 * w + gr, d);
                 }

@@ -31,11 +31,11 @@ template <int DK, int NP> struct WalkPlan {
     using Tiles = WalkTiles<DK, NP>;
     static constexpr int RG = kRowGroups<NP>, VW = 16 * RG;
     static constexpr int threads = NP == 1 ? 32 * RG : 128;     // float storage: two more warps that fetch
-    static constexpr size_t max(size_t a, size_t b) { return a > b ? a : b; }
-    static constexpr size_t early = max(sizeof(typename Tiles::FwdEarly), sizeof(typename Tiles::RevEarly));
-    static constexpr size_t late = max(sizeof(typename Tiles::FwdLate), sizeof(typename Tiles::RevLate));
-    static constexpr int stages = 2 * early + late <= 227 * 1024 ? 2 : 1;
-    static constexpr size_t smem = stages * early + late;
+    static constexpr size_t fe = sizeof(typename Tiles::FwdEarly), fl = sizeof(typename Tiles::FwdLate);
+    static constexpr size_t re = sizeof(typename Tiles::RevEarly), rl = sizeof(typename Tiles::RevLate);
+    static constexpr size_t need(int stages) { return stages * fe + fl > stages * re + rl ? stages * fe + fl : stages * re + rl; }
+    static constexpr int stages = need(2) <= 227 * 1024 ? 2 : 1;
+    static constexpr size_t smem = need(stages);
     static constexpr int blocks = 2 * (smem + 1024) <= 228 * 1024 ? 2 : 1;      // per SM
     static_assert(smem <= 227 * 1024, "fits an SM");
 };
@@ -101,8 +101,8 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
     using Plan = WalkPlan<DK, NP>;
     using Early = typename Plan::Tiles::FwdEarly;
     constexpr int NT = Plan::Tiles::NT, VW = Plan::VW, VLD = Plan::Tiles::VLD, STAGES = Plan::stages;
-    auto stage = [&](int i) -> Early & { return *reinterpret_cast<Early *>(raw + (i % STAGES) * Plan::early); };
-    auto &late = *reinterpret_cast<typename Plan::Tiles::FwdLate *>(raw + STAGES * Plan::early);
+    auto stage = [&](int i) -> Early & { return reinterpret_cast<Early *>(raw)[i % STAGES]; };
+    auto &late = *reinterpret_cast<typename Plan::Tiles::FwdLate *>(raw + STAGES * sizeof(Early));
     const int bh = blockIdx.x, seg = blockIdx.z, vblks = (P.Dv + VW - 1) / VW;
     const bool ident = SUMMARY && block >= vblks;
     const int r0 = (block - (ident ? vblks : 0)) * VW, vcols = ident ? 0 : (P.Dv - r0 < VW ? P.Dv - r0 : VW);
@@ -203,8 +203,8 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
     using Plan = WalkPlan<DK, NP>;
     using Early = typename Plan::Tiles::RevEarly;
     constexpr int NT = Plan::Tiles::NT, VW = Plan::VW, VLD = Plan::Tiles::VLD, STAGES = Plan::stages;
-    auto stage = [&](int i) -> Early & { return *reinterpret_cast<Early *>(raw + (i % STAGES) * Plan::early); };
-    auto &late = *reinterpret_cast<typename Plan::Tiles::RevLate *>(raw + STAGES * Plan::early);
+    auto stage = [&](int i) -> Early & { return reinterpret_cast<Early *>(raw)[i % STAGES]; };
+    auto &late = *reinterpret_cast<typename Plan::Tiles::RevLate *>(raw + STAGES * sizeof(Early));
     const int bh = blockIdx.x, seg = blockIdx.z, r0 = block * VW, vcols = P.Dv - r0 < VW ? P.Dv - r0 : VW;
     const int c0 = seg * P.seg_chunks, c1 = c0 + P.seg_chunks < P.chunks ? c0 + P.seg_chunks : P.chunks, count = c1 - c0;
     const int lane = threadIdx.x % 32, w = threadIdx.x / 32, gr = lane / 4, tc = lane % 4 * 2, w4 = (r0 / 16 + w) % 4;
