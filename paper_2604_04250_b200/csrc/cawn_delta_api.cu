@@ -54,7 +54,7 @@ struct Plan {
     int dk, terms, chunks, vblocks, segs, seg_chunks;    // terms: of an input
     size_t q, k, v, go;                  // three bfloat16 terms each, float storage only
     size_t coef, tri, p;
-    size_t rf, sf, od;                   // backward: rf also for rb, sf for the adjoints, od for rb.v
+    size_t rf, sf, od, u, s0, rbt;      // backward: rf also for rb, sf and s0 for the adjoints, od for rb.v
     size_t seg_state, seg_map;
     size_t total;
 };
@@ -97,8 +97,11 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
         w.rf = part(nv * kTile * 4);
         w.sf = part((nv + ends) * kC * w.dk * 4);
         w.od = part(nv * 4 * kC * 4);
+        w.u = part(nv * w.terms * kTile * 2);
+        w.s0 = part(nv * w.terms * kC * w.dk * 2);
+        w.rbt = w.terms == 3 ? w.v : 0;
     }
-    w.total = w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + 2 * (w.rf + w.sf + w.od) + (backward ? 4 : 2) * w.seg_state + w.seg_map;
+    w.total = w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + 2 * (w.rf + w.sf + w.od + w.s0) + w.u + w.rbt + (backward ? 4 : 2) * w.seg_state + w.seg_map;
     return w;
 }
 
@@ -237,9 +240,13 @@ extern "C" int cawn_delta_rule_bwd(const cawn_delta_params *params, const void *
     C.adj_start = ws.take<float>(w.seg_state);
     C.adj_end = ws.take<float>(w.seg_state);
     C.adj_in = grad_state_out; C.adj_out = grad_state_in;
+    C.u = ws.take<bf16>(w.u);
+    C.s0 = ws.take<bf16>(w.s0);
+    C.ds = ws.take<bf16>(w.s0);
+    C.rbt = ws.take<bf16>(w.rbt);
     C.o = grad_v;
-    C.o_stride_t = (long long)params->Hv * params->Dv;
-    C.o_stride_b = C.o_stride_t * params->L;
+    const long long vo = (long long)params->Hv * params->Dv;
+    C.rb = {w.terms == 1 ? static_cast<const bf16 *>(grad_v) : C.rbt, (long long)params->B * params->L * vo, vo, vo * params->L};
     C.gq = grad_q; C.gk = grad_k; C.gg = grad_g; C.gbeta = grad_beta;
     cudaError_t e = launch_delta_prep(C, w.dk, w.terms, st);
     if (e == cudaSuccess) e = launch_delta_walks(C, w.dk, w.terms, st);

@@ -29,8 +29,7 @@ template <int DK, int NP> struct GradSmem {
     bf16 q[NP][kC * (DK + kPad)], k[NP][kC * (DK + kPad)];
     union {
         struct {
-            bf16 go[NP][kC * (VW + kPad)];
-            bf16 u[NP][VW * kLd], rb[NP][VW * kLd];         // rows of values, as the walks hold them
+            bf16 go[NP][kC * (VW + kPad)], u[NP][kC * (VW + kPad)], rb[NP][kC * (VW + kPad)];
             bf16 s0[NP][VW * (DK + kPad)], ds[NP][VW * (DK + kPad)];
         } v;
         struct {
@@ -41,26 +40,6 @@ template <int DK, int NP> struct GradSmem {
     float dots[8][3][kC];                   // per 16 values: dO.o, rb.v, rb.r (up to 128 values)
     float sd[8];                            // per 16 values: <state after the chunk, D>
 };
-
-// A row group's accumulators as rows of values in shared memory: N tiles of 8 columns, rows of `ld` elements.
-template <int NP, int N> __device__ __forceinline__ void rows_to_tile(bf16 *tile, int plane, int ld, int row, const float (&x)[N][4])
-{
-    const int tc = threadIdx.x % 4 * 2;
-#pragma unroll
-    for (int n = 0; n < N; n++)
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            unsigned y[NP];
-            split(x[n][2 * h], x[n][2 * h + 1], y);
-#pragma unroll
-            for (int i = 0; i < NP; i++) *reinterpret_cast<unsigned *>(tile + i * plane + (row + 8 * h) * ld + 8 * n + tc) = y[i];
-        }
-}
-__device__ __forceinline__ void get_tile(float (&x)[4], const float4 *from)
-{
-    const float4 v = __ldg(from);
-    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-}
 
 template <int DK, int NP, class T>
 __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grads_kernel(const ChunkParams P)
@@ -74,8 +53,8 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
     const long long t0 = (long long)c * kC;
     const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
     const unsigned qs = smem_addr(sm.q[0]), ks = smem_addr(sm.k[0]);
-    const unsigned gos = smem_addr(sm.v.go[0]), us = smem_addr(sm.v.u[0]), rbs = smem_addr(sm.v.rb[0]);
-    const unsigned s0s = smem_addr(sm.v.s0[0]), dss = smem_addr(sm.v.ds[0]);
+    const unsigned us = smem_addr(sm.v.u[0]), s0s = smem_addr(sm.v.s0[0]), dss = smem_addr(sm.v.ds[0]);
+    const unsigned mine = qside ? smem_addr(sm.v.go[0]) : smem_addr(sm.v.rb[0]);
     const unsigned dps = smem_addr(sm.m.dp[0]), es = smem_addr(sm.m.e[0]);
 
 #pragma unroll
@@ -84,6 +63,35 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
         load_tile<kC, DK, 256>(sm.k[i], P.k.at + i * P.k.plane + q_base(P, P.k, b * P.Hv + hk * rep, t0), P.k.stride_t, rows, P.Dk);
     }
     cp_commit();
+
+    // rb.r per token (first four warps) and <state after the chunk, D> (the others), per row group of the walks.
+    auto dots_of_walks = [&](int bh, long long nc, int groups) {
+        for (int at = w; at < groups; at += 4) {
+            const long long g = nc * P.vblocks * 4 + at;
+            if (qside) {
+                float dots[8][2];
+#pragma unroll
+                for (int n = 0; n < 8; n++) {
+                    const float4 r = __ldg(P.rf + (g * 8 + n) * 32 + lane), rb = __ldg(P.rbf + (g * 8 + n) * 32 + lane);
+                    dots[n][0] = fmaf(r.x, rb.x, r.z * rb.z);
+                    dots[n][1] = fmaf(r.y, rb.y, r.w * rb.w);
+                }
+                column_sums(dots);
+                *reinterpret_cast<float2 *>(&sm.dots[at][2][8 * gr + tc]) = make_float2(dots[0][0], dots[0][1]);
+            } else {
+                const long long next = c + 1 < P.chunks ? g + P.vblocks * 4 : ((long long)P.B * P.Hv * P.chunks + bh) * P.vblocks * 4 + at;
+                float dot = 0.f;
+#pragma unroll
+                for (int n = 0; n < DK / 8; n++) {
+                    const float4 s = __ldg(P.sf + (next * (DK / 8) + n) * 32 + lane), d = __ldg(P.df + (g * (DK / 8) + n) * 32 + lane);
+                    dot = fmaf(s.x, d.x, fmaf(s.y, d.y, fmaf(s.z, d.z, fmaf(s.w, d.w, dot))));
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                if (lane == 0) sm.sd[at] = dot;
+            }
+        }
+    };
 
     float acc[2 * ND][4] = {};              // dQ or dK rows of this warp, over the heads that share them
     const int i0 = 16 * w + gr;             // rows i0 and i0 + 8
@@ -101,65 +109,28 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
         }
         float X[8][4] = {};                 // dO.u or rb.u, then dP or E
         for (int v0 = 0; v0 < P.Dv; v0 += VW) {
-            const int vcols = P.Dv - v0 < VW ? P.Dv - v0 : VW;
+            const int vcols = P.Dv - v0 < VW ? P.Dv - v0 : VW, in = v0 % kC;
+            const long long nv = nc * P.vblocks + v0 / kC;
 #pragma unroll
-            for (int i = 0; i < NP; i++)
+            for (int i = 0; i < NP; i++) {
                 load_tile<kC, VW, 256>(sm.v.go[i], P.go.at + i * P.go.plane + v_base(P, P.go, bh, t0) + v0, P.go.stride_t, rows, vcols);
-            cp_commit();
-            // The walks' accumulators of this warp's row group: r and rb (first four warps), states and D (the others).
-            const long long g = g0 + v0 / 16 + w;
-            const bool mine = w < VW / 16 && v0 + 16 * w < P.Dv;
-            cp_wait<0>();
-            __syncthreads();                // coefficients are here
-            if (w < VW / 16 && qside) {
-                float dots[8][2];
-#pragma unroll
-                for (int n = 0; n < 8; n++) {
-                    float r[1][4] = {}, rb[1][4] = {};
-                    if (mine) {
-                        get_tile(r[0], P.rf + (g * 8 + n) * 32 + lane);
-                        get_tile(rb[0], P.rbf + (g * 8 + n) * 32 + lane);
-                    }
-                    dots[n][0] = fmaf(r[0][0], rb[0][0], r[0][2] * rb[0][2]);
-                    dots[n][1] = fmaf(r[0][1], rb[0][1], r[0][3] * rb[0][3]);
-                    const f32x2 bt = pair(*reinterpret_cast<const float2 *>(&sm.coef[COEF_BETA][8 * n + tc]));
-                    scale_row(r[0], 0, bt);
-                    scale_row(r[0], 1, bt);
-                    rows_to_tile<NP>(sm.v.u[0] + 8 * n, VW * kLd, kLd, 16 * w + gr, r);
-                    rows_to_tile<NP>(sm.v.rb[0] + 8 * n, VW * kLd, kLd, 16 * w + gr, rb);
-                }
-                column_sums(dots);
-                if (mine) *reinterpret_cast<float2 *>(&sm.dots[v0 / 16 + w][2][8 * gr + tc]) = make_float2(dots[0][0], dots[0][1]);
-            } else if (w < VW / 16) {
-                const long long next = c + 1 < P.chunks ? g + P.vblocks * 4 : ((long long)P.B * P.Hv * P.chunks + bh) * P.vblocks * 4 + v0 / 16 + w;
-                float dot = 0.f;
-#pragma unroll
-                for (int n = 0; n < DK / 8; n++) {
-                    float s0[1][4] = {}, d[1][4] = {}, s1[4] = {};
-                    if (mine) {
-                        get_tile(s0[0], P.sf + (g * (DK / 8) + n) * 32 + lane);
-                        get_tile(d[0], P.df + (g * (DK / 8) + n) * 32 + lane);
-                        get_tile(s1, P.sf + (next * (DK / 8) + n) * 32 + lane);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; e++) dot = fmaf(s1[e], d[0][e], dot);
-                    rows_to_tile<NP>(sm.v.s0[0] + 8 * n, VW * ld, ld, 16 * w + gr, s0);
-                    rows_to_tile<NP>(sm.v.ds[0] + 8 * n, VW * ld, ld, 16 * w + gr, d);
-                }
-#pragma unroll
-                for (int o = 16; o > 0; o /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-                if (lane == 0) sm.sd[v0 / 16 + w] = dot;
+                load_tile<kC, VW, 256>(sm.v.rb[i], P.rb.at + i * P.rb.plane + v_base(P, P.rb, bh, t0) + v0, P.rb.stride_t, rows, vcols);
+                load_tile<kC, VW, 256>(sm.v.u[i], P.u + (nv * NP + i) * kTile + in, kC, kC, vcols);
+                load_tile<VW, DK, 256>(sm.v.s0[i], P.s0 + (nv * NP + i) * (kC * DK) + in * DK, DK, vcols, DK);
+                load_tile<VW, DK, 256>(sm.v.ds[i], P.ds + (nv * NP + i) * (kC * DK) + in * DK, DK, vcols, DK);
             }
+            cp_commit();
+            if (v0 == 0) dots_of_walks(bh, nc, groups);         // while the tiles are on their way
+            cp_wait<0>();
             __syncthreads();
 
             unsigned a[VW / 16][NP][4];     // rows of dO or rb
 #pragma unroll
             for (int d = 0; d < VW / 16; d++) {
-                if (qside) load_left<NP, false>(a[d], at_kn(gos, ldv, 16 * w, 16 * d), kC * ldv);
-                else load_left<NP, true>(a[d], at_nk(rbs, kLd, 16 * d, 16 * w), VW * kLd);
+                load_left<NP, false>(a[d], at_kn(mine, ldv, 16 * w, 16 * d), kC * ldv);
 #pragma unroll
                 for (int nb = 0; nb < 4; nb++)
-                    if (nb <= w) product<NP, NP, true>(X[2 * nb], X[2 * nb + 1], a[d], at_kn(us, kLd, 16 * d, 16 * nb), VW * kLd);
+                    if (nb <= w) product<NP, NP, false>(X[2 * nb], X[2 * nb + 1], a[d], at_nk(us, ldv, 16 * nb, 16 * d), kC * ldv);
             }
             // times S0: the state's part of dQ, or minus the read-out's part of dK
             const float sign = qside ? P.scale : -1.f;
@@ -177,7 +148,7 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
             if (!qside) {                   // e^{G_C - G} u D
                 const float g[2] = {sm.coef[COEF_LEFT][i0], sm.coef[COEF_LEFT][i0 + 8]};
 #pragma unroll
-                for (int d = 0; d < VW / 16; d++) load_left<NP, true>(a[d], at_nk(us, kLd, 16 * d, 16 * w), VW * kLd);
+                for (int d = 0; d < VW / 16; d++) load_left<NP, false>(a[d], at_kn(us, ldv, 16 * w, 16 * d), kC * ldv);
 #pragma unroll
                 for (int nb = 0; nb < ND; nb++) {
                     float x[2][4] = {};

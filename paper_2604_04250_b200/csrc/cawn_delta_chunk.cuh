@@ -51,6 +51,10 @@ struct ChunkParams {
     // and the state before the chunk (sf has a further end state per head), rb and the adjoint of the state after
     // the chunk.
     float4 *rf, *sf, *rbf, *df;
+    // and, in the inputs' terms, what the chunk-local products take: u as token rows, both states as value rows
+    bf16 *u, *s0, *ds;                  // [nv][NP][64 t][64 v], [nv][NP][64 v][DK] twice
+    bf16 *rbt;                          // [NP] terms of rb, float storage only, laid out like v
+    Terms rb;                           // rb: dV itself (bfloat16), or its terms
     float *od, *rv;                     // [nv][4][64]: dO.o and rb.v over 16 values
     const float *state_in;              // [bh][Dv][Dk], may be NULL
     float *state_out;
@@ -421,7 +425,21 @@ template <int DK> __device__ __forceinline__ void store_state(float *to, const f
             if (r + 8 * h < rows && 8 * n + tc < Dk)
                 *reinterpret_cast<float2 *>(to + (long long)(r + 8 * h) * Dk + 8 * n + tc) = make_float2(S[n][2 * h], S[n][2 * h + 1]);
 }
-// accumulator tiles to / from the walks' arrays
+// a state's rows in NP terms, rows of DK elements
+template <int NP, int DK> __device__ __forceinline__ void store_rows(bf16 *to, const float (&S)[DK / 8][4])
+{
+    to += threadIdx.x % 32 / 4 * DK + threadIdx.x % 4 * 2;
+#pragma unroll
+    for (int n = 0; n < DK / 8; n++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            unsigned x[NP];
+            split(S[n][2 * h], S[n][2 * h + 1], x);
+#pragma unroll
+            for (int i = 0; i < NP; i++) *reinterpret_cast<unsigned *>(to + i * (kC * DK) + 8 * h * DK + 8 * n) = x[i];
+        }
+}
+// accumulator tiles to the walks' arrays
 template <int N> __device__ __forceinline__ void store_tiles(float4 *to, const float (&x)[N][4])
 {
 #pragma unroll

@@ -139,7 +139,7 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
     }
     for (int i = 0; i < count; i++) {
         begin_chunk<STAGES>(i, count, load_early, load_late);
-        const long long g = (((long long)bh * P.chunks + c0 + i) * P.vblocks + r0 / kC) * 4 + w4;       // row group in the arrays
+        const long long nv = ((long long)bh * P.chunks + c0 + i) * P.vblocks + r0 / kC, g = nv * 4 + w4;        // row group in the arrays
         Early &e = stage(i);
         const unsigned ks = smem_addr(e.k[0]);
         float X[8][4] = {}, Y[SUMMARY ? 1 : 8][4] = {};
@@ -147,6 +147,7 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
             rows_times<3, NP, DK>(X, S, ks);
             if constexpr (!SUMMARY) {
                 store_tiles(P.sf + g * (DK / 8 * 32), S);
+                store_rows<NP, DK>(P.s0 + nv * (NP * kC * DK) + 16 * w4 * DK, S);
                 rows_times<3, NP, DK>(Y, S, smem_addr(e.q[0]));
                 scale_tokens(Y, e.coef, COEF_EG, P.scale);
             }
@@ -170,6 +171,23 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
             dots_with<NP>(dots, Y, smem_addr(late.go[0]), VLD, 16 * w);
             column_sums(dots);
             *reinterpret_cast<float2 *>(P.od + g * kC + 8 * gr + tc) = make_float2(dots[0][0], dots[0][1]);
+            // u as token rows, through this warp's own part of the V tile
+            const unsigned vs = smem_addr(e.v[0]);
+#pragma unroll
+            for (int term = 0; term < NP; term++) {
+                __syncwarp();
+#pragma unroll
+                for (int nb = 0; nb < 4; nb++) {
+                    unsigned x[NP][4];
+                    as_left(r[2 * nb], r[2 * nb + 1], x);
+                    stsm_t(at_nk(vs, VLD, 16 * nb, 16 * w), x[term][0], x[term][1], x[term][2], x[term][3]);
+                }
+                __syncwarp();
+#pragma unroll
+                for (int j = lane; j < 128; j += 32)
+                    *reinterpret_cast<uint4 *>(P.u + (nv * NP + term) * kTile + j / 2 * kC + 16 * w4 + j % 2 * 8) =
+                        *reinterpret_cast<const uint4 *>(&e.v[0][j / 2 * VLD + 16 * w + j % 2 * 8]);
+            }
         }
         // the update is summed from zero and added once, as in the forward
         const float eC = e.coef[COEF_EG][kC - 1];
@@ -232,14 +250,17 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
     for (int i = 0; i < count; i++) {
         begin_chunk<STAGES>(i, count, load_early, load_late);
         const int c = c1 - 1 - i;
-        const long long t0 = (long long)c * kC, g = (((long long)bh * P.chunks + c) * P.vblocks + r0 / kC) * 4 + w4;
+        const long long t0 = (long long)c * kC, nv = ((long long)bh * P.chunks + c) * P.vblocks + r0 / kC, g = nv * 4 + w4;
         Early &e = stage(i);
         const unsigned ks = smem_addr(e.k[0]), gs = smem_addr(e.go[0]);
         // X = beta (e^{G_C - G} (D K^T) + dO^T P)
         float X[8][4] = {};
         if (walks) {
             rows_times<3, NP, DK>(X, D, ks);
-            if constexpr (!SUMMARY) store_tiles(P.df + g * (DK / 8 * 32), D);
+            if constexpr (!SUMMARY) {
+                store_tiles(P.df + g * (DK / 8 * 32), D);
+                store_rows<NP, DK>(P.ds + nv * (NP * kC * DK) + 16 * w4 * DK, D);
+            }
             scale_tokens(X, e.coef, COEF_LEFT);
             triangle<NP, NT, true, true>(X, [&](unsigned (&a)[NP][4], int ib) { load_left<NP, true>(a, at_nk(gs, VLD, 16 * ib, 16 * w), kC * VLD); },
                                          [&](int ib, int nb) { return at_kn(smem_addr(e.p[0]), kLd, 16 * ib, 16 * nb); }, kC * kLd);
@@ -262,28 +283,34 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
             dots_with<NP>(dots, rb, vs, VLD, 16 * w);
             column_sums(dots);
             *reinterpret_cast<float2 *>(P.rv + g * kC + 8 * gr + tc) = make_float2(dots[0][0], dots[0][1]);
-            // dV = rb
+            // rb as token rows, through this warp's own part of the V tile: dV (bfloat16: the first term is the
+            // rounded value), or its terms for the chunk's gradients
             const int rows = fetch.rows(c);
-            T *gv = static_cast<T *>(P.o) + (bh / P.Hv) * P.o_stride_b + t0 * P.o_stride_t + (long long)(bh % P.Hv) * P.Dv + r0;
-            if constexpr (sizeof(T) == 2) {         // as token rows, through this warp's own part of the V tile
+#pragma unroll
+            for (int term = 0; term < NP; term++) {
+                bf16 *dst = (NP == 1 ? static_cast<bf16 *>(P.o) : P.rbt + term * P.rb.plane) + v_base(P, P.rb, bh, t0) + r0;
                 __syncwarp();
 #pragma unroll
-                for (int nb = 0; nb < 4; nb++)
-                    stsm_t(at_nk(vs, VLD, 16 * nb, 16 * w), pack_bf16(rb[2 * nb][0], rb[2 * nb][1]), pack_bf16(rb[2 * nb][2], rb[2 * nb][3]),
-                           pack_bf16(rb[2 * nb + 1][0], rb[2 * nb + 1][1]), pack_bf16(rb[2 * nb + 1][2], rb[2 * nb + 1][3]));
+                for (int nb = 0; nb < 4; nb++) {
+                    unsigned x[NP][4];
+                    as_left(rb[2 * nb], rb[2 * nb + 1], x);
+                    stsm_t(at_nk(vs, VLD, 16 * nb, 16 * w), x[term][0], x[term][1], x[term][2], x[term][3]);
+                }
                 __syncwarp();
 #pragma unroll
                 for (int j = lane; j < 128; j += 32) {
                     const int t = j / 2, v = 16 * w + j % 2 * 8;
-                    if (t < rows && v < vcols) *reinterpret_cast<uint4 *>(gv + t * P.o_stride_t + v) = *reinterpret_cast<const uint4 *>(&late.v[0][t * VLD + v]);
+                    if (t < rows && v < vcols) *reinterpret_cast<uint4 *>(dst + t * P.rb.stride_t + v) = *reinterpret_cast<const uint4 *>(&late.v[0][t * VLD + v]);
                 }
-            } else {
+            }
+            if constexpr (sizeof(T) == 4) {
+                T *gv = static_cast<T *>(P.o) + v_base(P, P.rb, bh, t0) + r0;
 #pragma unroll
                 for (int n = 0; n < 8; n++)
 #pragma unroll
                     for (int j = 0; j < 4; j++) {
                         const int t = 8 * n + tc + (j & 1), v = 16 * w + gr + (j >> 1) * 8;
-                        if (t < rows && v < vcols) gv[t * P.o_stride_t + v] = narrow<T>(rb[n][j]);
+                        if (t < rows && v < vcols) gv[t * P.rb.stride_t + v] = narrow<T>(rb[n][j]);
                     }
             }
         }
