@@ -54,7 +54,8 @@ struct Plan {
     int dk, terms, chunks, vblocks, segs, seg_chunks;    // terms: of an input
     size_t q, k, v, go;                  // three bfloat16 terms each, float storage only
     size_t coef, tri, p;
-    size_t rf, sf, od, u, s0, rbt;      // backward: rf also for rb, sf and s0 for the adjoints, od for rb.v
+    size_t rf, sf, od, sd, u, s0, rbt;  // backward: rf also for rb, sf and s0 for the adjoints, od for the other dots
+    bool together;
     size_t seg_state, seg_map;
     size_t total;
 };
@@ -97,11 +98,13 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
         w.rf = part(nv * kTile * 4);
         w.sf = part((nv + ends) * kC * w.dk * 4);
         w.od = part(nv * 4 * kC * 4);
+        w.sd = part(nv * 4 * 4);
+        w.together = w.segs > 1 || blocks <= sm_count();    // both walks' blocks, one per SM
         w.u = part(nv * w.terms * kTile * 2);
         w.s0 = part(nv * w.terms * kC * w.dk * 2);
         w.rbt = w.terms == 3 ? w.v : 0;
     }
-    w.total = w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + 2 * (w.rf + w.sf + w.od + w.s0) + w.u + w.rbt + (backward ? 4 : 2) * w.seg_state + w.seg_map;
+    w.total = w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + 2 * (w.rf + w.sf + w.s0) + 3 * w.od + w.sd + w.u + w.rbt + (backward ? 4 : 2) * w.seg_state + w.seg_map;
     return w;
 }
 
@@ -237,6 +240,9 @@ extern "C" int cawn_delta_rule_bwd(const cawn_delta_params *params, const void *
     C.df = ws.take<float4>(w.sf);
     C.od = ws.take<float>(w.od);
     C.rv = ws.take<float>(w.od);
+    C.rr = ws.take<float>(w.od);
+    C.sd = ws.take<float>(w.sd);
+    C.together = w.together;
     C.adj_start = ws.take<float>(w.seg_state);
     C.adj_end = ws.take<float>(w.seg_state);
     C.adj_in = grad_state_out; C.adj_out = grad_state_in;

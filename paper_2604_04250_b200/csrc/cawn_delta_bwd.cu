@@ -103,9 +103,9 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
             cp16(smem_addr(&sm.coef[0][0]) + threadIdx.x * 16, P.coef + nc * (kCoef * kC) + threadIdx.x * 4, true);
         const int groups = (P.Dv + 15) / 16;                // row groups of the walks
         const long long g0 = nc * P.vblocks * 4;
-        for (int i = threadIdx.x; i < groups * 32; i += 256) {
-            const int at = i / 32, x = i % 32 * 4;
-            cp16(smem_addr(&sm.dots[at][0][0]) + x * 4, (x < kC ? P.od : P.rv) + (g0 + at) * kC + x % kC, true);
+        for (int i = threadIdx.x; i < groups * (P.together ? 32 : 48); i += 256) {
+            const int at = i / 16 % groups, what = i / 16 / groups, x = i % 16 * 4;
+            cp16(smem_addr(&sm.dots[at][what][x]), (what == 0 ? P.od : what == 1 ? P.rv : P.rr) + (g0 + at) * kC + x, true);
         }
         float X[8][4] = {};                 // dO.u or rb.u, then dP or E
         for (int v0 = 0; v0 < P.Dv; v0 += VW) {
@@ -120,7 +120,8 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
                 load_tile<VW, DK, 256>(sm.v.ds[i], P.ds + (nv * NP + i) * (kC * DK) + in * DK, DK, vcols, DK);
             }
             cp_commit();
-            if (v0 == 0) dots_of_walks(bh, nc, groups);         // while the tiles are on their way
+            if (v0 == 0 && P.together) dots_of_walks(bh, nc, groups);       // while the tiles are on their way
+            else if (v0 == 0 && threadIdx.x < groups) sm.sd[threadIdx.x] = P.sd[g0 + threadIdx.x];
             cp_wait<0>();
             __syncthreads();
 

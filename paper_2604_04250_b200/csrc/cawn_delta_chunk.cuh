@@ -55,7 +55,9 @@ struct ChunkParams {
     bf16 *u, *s0, *ds;                  // [nv][NP][64 t][64 v], [nv][NP][64 v][DK] twice
     bf16 *rbt;                          // [NP] terms of rb, float storage only, laid out like v
     Terms rb;                           // rb: dV itself (bfloat16), or its terms
-    float *od, *rv;                     // [nv][4][64]: dO.o and rb.v over 16 values
+    float *od, *rv, *rr;                // [nv][4][64]: dO.o, rb.v and rb.r over 16 values
+    float *sd;                          // [nv][4]: <state after the chunk, its adjoint> over 16 values
+    bool together;                      // the two walks run side by side: rr and sd are made afterwards
     const float *state_in;              // [bh][Dv][Dk], may be NULL
     float *state_out;
     const float *adj_in;                // gradient of state_out, may be NULL
@@ -344,6 +346,22 @@ template <int NS, int NP, int DK> __device__ __forceinline__ void rows_times(flo
         for (int i = 0; i < 4; i++) load_right<NP, false>(b[i], at_nk(tile, DK + kPad, 16 * i, 16 * d), kC * (DK + kPad));
         as_left(S[2 * d], S[2 * d + 1], a);
         multiply<NS, NP, 4>(X, a, b);
+    }
+}
+// the same for two tiles at once: the state is split once
+template <int NS, int NP, int DK>
+__device__ __forceinline__ void rows_times(float (&X)[8][4], float (&Y)[8][4], const float (&S)[DK / 8][4], unsigned tile_x, unsigned tile_y)
+{
+#pragma unroll
+    for (int d = 0; d < DK / 16; d++) {
+        unsigned a[NS][4], b[4][NP][4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) load_right<NP, false>(b[i], at_nk(tile_x, DK + kPad, 16 * i, 16 * d), kC * (DK + kPad));
+        as_left(S[2 * d], S[2 * d + 1], a);
+        multiply<NS, NP, 4>(X, a, b);
+#pragma unroll
+        for (int i = 0; i < 4; i++) load_right<NP, false>(b[i], at_nk(tile_y, DK + kPad, 16 * i, 16 * d), kC * (DK + kPad));
+        multiply<NS, NP, 4>(Y, a, b);
     }
 }
 // x (tiles 2 nb .. 2 nb + 3 of a state's columns) += left x K or Q, token block by token block

@@ -4,12 +4,15 @@
 //   X = S K^T,  R = V^T - e^G X,  r = R T^T,  u = beta r,  o = scale e^G S Q^T + u P^T,  S <- e^{G_C} S + (e^{G_C - G} u) K,
 // and the reverse walk, with D the adjoint of the state after a chunk,
 //   dU = P^T dO + e^{G_C - G} (K D^T),   rb = T^T (beta dU),   D <- e^{G_C} D + (scale e^G dO)^T Q - (e^G rb)^T K.
-// Neither needs the other: one launch runs both, a block per head, 16 * row groups of values and direction.
-// Bound: each walk is a chain of products and of the instructions between them that leaves its scheduler waiting
-// half of the time, so two blocks share an SM where registers and shared memory allow (64 keys, bfloat16): the
-// two directions of 96 heads together take what either took alone before.  For that a block has its four chain
-// warps only, which also fetch: tiles that a chunk starts with are double-buffered, those that it needs later are
-// asked for when it starts.
+// Neither needs the other, except that rb.r and <state, D> are sums over both walks' floats.  Bound: each walk is a
+// chain of products and of the instructions between them, on the SMs that have a head.  So with few heads one launch
+// runs both walks, each on SMs of its own, and those sums are left to the chunk-local kernel (12 heads, float storage:
+// 372 -> 290 us for the whole backward).  With more heads than half the SMs the two would share SMs, which gains
+// next to nothing (96 heads, both on one SM: 231 us, one after the other 2 x 127), so the forward goes first
+// and the reverse walk takes those sums along, with r and the states fetched beside its tiles.
+// A block is 16 * row groups of values of one head and one direction.  Warps of their own fetch the tiles (with the
+// chain warps fetching, either walk of 96 heads took 153 us instead of 127), a chunk ahead where shared memory holds
+// two sets; else the tiles that a chunk starts with come a chunk ahead and the others when it starts.
 #include "cawn_delta_chunk.cuh"
 
 #include <type_traits>
@@ -26,23 +29,27 @@ template <int DK, int NP> struct WalkTiles {
     struct FwdLate { Square tri, p; Values go; };
     struct RevEarly { Keys k; Values go; Square p; float coef[kCoef][kC]; };
     struct RevLate { Keys q; Square tri; Values v; };
+    struct RevFloats : RevLate { float4 r[kRowGroups<NP> * 8 * 32], s[kRowGroups<NP> * (DK / 8) * 32]; };
 };
-template <int DK, int NP> struct WalkPlan {
+// What a launch does: both walks, or one of them (the reverse one with the sums over both).
+enum { BOTH, FORWARD, REVERSE };
+template <int DK, int NP, int WHAT> struct WalkPlan {
     using Tiles = WalkTiles<DK, NP>;
+    using Late = typename std::conditional<WHAT == REVERSE, typename Tiles::RevFloats, typename Tiles::RevLate>::type;
     static constexpr int RG = kRowGroups<NP>, VW = 16 * RG;
-    static constexpr int threads = NP == 1 ? 32 * RG : 128;     // float storage: two more warps that fetch
-    static constexpr size_t fe = sizeof(typename Tiles::FwdEarly), fl = sizeof(typename Tiles::FwdLate);
-    static constexpr size_t re = sizeof(typename Tiles::RevEarly), rl = sizeof(typename Tiles::RevLate);
-    static constexpr size_t need(int stages) { return stages * fe + fl > stages * re + rl ? stages * fe + fl : stages * re + rl; }
-    static constexpr int stages = need(2) <= 227 * 1024 ? 2 : 1;
-    static constexpr size_t smem = need(stages);
-    static constexpr int blocks = 2 * (smem + 1024) <= 228 * 1024 ? 2 : 1;      // per SM
+    static constexpr int fetch = NP == 1 ? 32 : 128, threads = 32 * RG + fetch;
+    static constexpr size_t forward(int early, int late) { return WHAT == REVERSE ? 0 : early * sizeof(typename Tiles::FwdEarly) + late * sizeof(typename Tiles::FwdLate); }
+    static constexpr size_t reverse(int early, int late) { return WHAT == FORWARD ? 0 : early * sizeof(typename Tiles::RevEarly) + late * sizeof(Late); }
+    static constexpr size_t need(int early, int late) { return forward(early, late) > reverse(early, late) ? forward(early, late) : reverse(early, late); }
+    static constexpr size_t room = 227 * 1024;
+    static constexpr int early = need(2, 1) <= room ? 2 : 1, late = need(2, 2) <= room ? 2 : 1;      // sets of each
+    static constexpr size_t smem = need(early, late);
     static_assert(smem <= 227 * 1024, "fits an SM");
 };
 
 template <int DK, int NP> struct Fetch {
-    using Plan = WalkPlan<DK, NP>;
-    static constexpr int TH = Plan::threads, NT = Plan::Tiles::NT, VW = Plan::VW;
+    using Plan = WalkPlan<DK, NP, BOTH>;
+    static constexpr int TH = Plan::fetch, NT = Plan::Tiles::NT, VW = Plan::VW;
     const ChunkParams &P;
     int bh, v0, vcols;
     __device__ __forceinline__ int rows(int c) const { return P.L - (long long)c * kC < kC ? (int)(P.L - (long long)c * kC) : kC; }
@@ -63,46 +70,75 @@ template <int DK, int NP> struct Fetch {
     }
     __device__ __forceinline__ void coef(float (&to)[kCoef][kC], int c) const
     {
-        if (threadIdx.x < kCoef * kC / 4)
-            cp16(smem_addr(&to[0][0]) + threadIdx.x * 16, P.coef + ((long long)bh * P.chunks + c) * (kCoef * kC) + threadIdx.x * 4, true);
+        for (int i = threadIdx.x % TH; i < kCoef * kC / 4; i += TH)
+            cp16(smem_addr(&to[0][0]) + i * 16, P.coef + ((long long)bh * P.chunks + c) * (kCoef * kC) + i * 4, true);
     }
 };
-static_assert(kCoef * kC / 4 <= 128, "one word per thread");
 
-// A walk's chunk: wait for the early tiles, ask for the late ones and for the next chunk's early ones.
-// `load_early(i)`, `load_late(i)`: tiles of the i-th chunk of the walk.
-template <int STAGES, class Early, class Late> __device__ __forceinline__ void begin_chunk(int i, int count, Early load_early, Late load_late)
+// Two sets of everything: the fetching warps run ahead on their own, and the chain warps do not wait for one another.
+// Returns true for the former, which are done.
+template <class Plan, class Early, class Late> __device__ __forceinline__ bool fetch_ahead(bool walks, int count, Early load_early, Late load_late)
 {
-    if (STAGES == 1 && i > 0) __syncthreads();      // everyone is done with the one set there is
-    if (STAGES == 1 || i == 0) {
+    if (Plan::late == 1 || walks) return false;
+    for (int i = 0; i < count; i++) {
+        if (i >= 2) bar_sync(BAR_EMPTY + i % 2, Plan::threads);
         load_early(i);
+        load_late(i);
         cp_commit();
+        cp_wait<0>();
+        bar_arrive(BAR_FULL + i % 2, Plan::threads);
     }
-    cp_wait<0>();
-    __syncthreads();            // the early tiles are here, and everyone is done with the chunk before
+    return true;
+}
+// A walk's chunk: wait for the early tiles; with one late set the fetching warps ask for what the buffers have room
+// for.  `load_early(i)`, `load_late(i)`: tiles of the i-th chunk of the walk.
+template <class Plan, class Early, class Late> __device__ __forceinline__ void begin_chunk(bool walks, int i, int count, Early load_early, Late load_late)
+{
+    if (Plan::late == 2) {
+        bar_sync(BAR_FULL + i % 2, Plan::threads);
+        return;
+    }
+    if (Plan::early == 1 && i > 0) __syncthreads();     // everyone is done with the one set there is
+    if (!walks) {
+        if (Plan::early == 1 || i == 0) {
+            load_early(i);
+            cp_commit();
+        }
+        cp_wait<0>();
+    }
+    __syncthreads();            // the tiles are here, and everyone is done with the chunk before
+    if (walks) return;
     load_late(i);
     cp_commit();
-    if (STAGES == 2) {
+    if (Plan::early == 2) {
         if (i + 1 < count) load_early(i + 1);
         cp_commit();            // possibly empty, which keeps the count
     }
 }
-template <int STAGES> __device__ __forceinline__ void late_tiles()
+template <class Plan> __device__ __forceinline__ void end_chunk(int i, int count)
 {
-    if (STAGES == 2) cp_wait<1>(); else cp_wait<0>();
+    if (Plan::late == 2 && i + 2 < count) bar_arrive(BAR_EMPTY + i % 2, Plan::threads);
+}
+template <class Plan> __device__ __forceinline__ void late_tiles(bool walks)
+{
+    if (Plan::late == 2) return;                        // they came with the early ones
+    if (!walks) {
+        if (Plan::early == 2) cp_wait<1>(); else cp_wait<0>();
+    }
     __syncthreads();
 }
 
 // SUMMARY: what a segment's own tokens leave at its end (forward; with the transitions, which are the walk of the
 // identity's rows with V = 0) or send to its start (reverse).
-template <int DK, int NP, bool SUMMARY>
+template <int DK, int NP, bool SUMMARY, int WHAT>
 __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char *raw, int block)
 {
-    using Plan = WalkPlan<DK, NP>;
+    using Plan = WalkPlan<DK, NP, WHAT>;
     using Early = typename Plan::Tiles::FwdEarly;
-    constexpr int NT = Plan::Tiles::NT, VW = Plan::VW, VLD = Plan::Tiles::VLD, STAGES = Plan::stages;
-    auto stage = [&](int i) -> Early & { return reinterpret_cast<Early *>(raw)[i % STAGES]; };
-    auto &late = *reinterpret_cast<typename Plan::Tiles::FwdLate *>(raw + STAGES * sizeof(Early));
+    constexpr int NT = Plan::Tiles::NT, VW = Plan::VW, VLD = Plan::Tiles::VLD;
+    using Late = typename Plan::Tiles::FwdLate;
+    auto stage = [&](int i) -> Early & { return reinterpret_cast<Early *>(raw)[i % Plan::early]; };
+    auto stage_late = [&](int i) -> Late & { return reinterpret_cast<Late *>(raw + Plan::early * sizeof(Early))[i % Plan::late]; };
     const int bh = blockIdx.x, seg = blockIdx.z, vblks = (P.Dv + VW - 1) / VW;
     const bool ident = SUMMARY && block >= vblks;
     const int r0 = (block - (ident ? vblks : 0)) * VW, vcols = ident ? 0 : (P.Dv - r0 < VW ? P.Dv - r0 : VW);
@@ -119,6 +155,7 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
         fetch.coef(e.coef, c0 + i);
     };
     auto load_late = [&](int i) {
+        Late &late = stage_late(i);
         fetch.square(late.tri, P.tri, c0 + i);
         if (!SUMMARY) {
             fetch.square(late.p, P.p, c0 + i);
@@ -137,23 +174,25 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
                                          : (P.state_in != nullptr ? P.state_in + (long long)bh * P.Dv * P.Dk : nullptr);
         load_state<DK>(S, from, walks ? row : P.Dv, P.Dv, P.Dk);
     }
+    if (fetch_ahead<Plan>(walks, count, load_early, load_late)) return;
     for (int i = 0; i < count; i++) {
-        begin_chunk<STAGES>(i, count, load_early, load_late);
+        begin_chunk<Plan>(walks, i, count, load_early, load_late);
         const long long nv = ((long long)bh * P.chunks + c0 + i) * P.vblocks + r0 / kC, g = nv * 4 + w4;        // row group in the arrays
         Early &e = stage(i);
+        Late &late = stage_late(i);
         const unsigned ks = smem_addr(e.k[0]);
         float X[8][4] = {}, Y[SUMMARY ? 1 : 8][4] = {};
         if (walks) {
-            rows_times<3, NP, DK>(X, S, ks);
+            if constexpr (SUMMARY) rows_times<3, NP, DK>(X, S, ks);
+            else rows_times<3, NP, DK>(X, Y, S, ks, smem_addr(e.q[0]));
             if constexpr (!SUMMARY) {
                 store_tiles(P.sf + g * (DK / 8 * 32), S);
                 store_rows<NP, DK>(P.s0 + nv * (NP * kC * DK) + 16 * w4 * DK, S);
-                rows_times<3, NP, DK>(Y, S, smem_addr(e.q[0]));
                 scale_tokens(Y, e.coef, COEF_EG, P.scale);
             }
             residual<NP>(X, e.coef, smem_addr(e.v[0]), VLD, 16 * w, vcols > 0);
         }
-        late_tiles<STAGES>();
+        late_tiles<Plan>(walks);
         if (!walks) continue;
         float r[8][4];
 #pragma unroll
@@ -204,6 +243,7 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
 #pragma unroll
                 for (int h = 0; h < 2; h++) fma_row(S[2 * nb + m], h, pair(eC, eC), pair(x[m][2 * h], x[m][2 * h + 1]));
         }
+        end_chunk<Plan>(i, count);
     }
     if (!walks) return;
     if constexpr (SUMMARY) {
@@ -215,14 +255,15 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
     }
 }
 
-template <int DK, int NP, bool SUMMARY, class T>
+template <int DK, int NP, bool SUMMARY, int WHAT, class T>
 __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char *raw, int block)
 {
-    using Plan = WalkPlan<DK, NP>;
+    using Plan = WalkPlan<DK, NP, WHAT>;
     using Early = typename Plan::Tiles::RevEarly;
-    constexpr int NT = Plan::Tiles::NT, VW = Plan::VW, VLD = Plan::Tiles::VLD, STAGES = Plan::stages;
-    auto stage = [&](int i) -> Early & { return reinterpret_cast<Early *>(raw)[i % STAGES]; };
-    auto &late = *reinterpret_cast<typename Plan::Tiles::RevLate *>(raw + STAGES * sizeof(Early));
+    constexpr int NT = Plan::Tiles::NT, VW = Plan::VW, VLD = Plan::Tiles::VLD;
+    using Late = typename Plan::Late;
+    auto stage = [&](int i) -> Early & { return reinterpret_cast<Early *>(raw)[i % Plan::early]; };
+    auto stage_late = [&](int i) -> Late & { return reinterpret_cast<Late *>(raw + Plan::early * sizeof(Early))[i % Plan::late]; };
     const int bh = blockIdx.x, seg = blockIdx.z, r0 = block * VW, vcols = P.Dv - r0 < VW ? P.Dv - r0 : VW;
     const int c0 = seg * P.seg_chunks, c1 = c0 + P.seg_chunks < P.chunks ? c0 + P.seg_chunks : P.chunks, count = c1 - c0;
     const int lane = threadIdx.x % 32, w = threadIdx.x / 32, gr = lane / 4, tc = lane % 4 * 2, w4 = (r0 / 16 + w) % 4;
@@ -237,9 +278,17 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
         fetch.coef(e.coef, c1 - 1 - i);
     };
     auto load_late = [&](int i) {
+        Late &late = stage_late(i);
         fetch.square(late.tri, P.tri, c1 - 1 - i);
         fetch.keys(late.q, P.q, c1 - 1 - i);
         if (!SUMMARY) fetch.values(late.v, P.v, c1 - 1 - i);
+        if constexpr (WHAT == REVERSE) {        // this block's row groups lie one after the other
+            const long long here = (long long)bh * P.chunks + c1 - 1 - i, after = c1 - i < P.chunks ? here + 1 : (long long)P.B * P.Hv * P.chunks + bh;
+            const float4 *r = P.rf + ((here * P.vblocks + r0 / kC) * 4 + r0 / 16 % 4) * (8 * 32);
+            const float4 *s = P.sf + ((after * P.vblocks + r0 / kC) * 4 + r0 / 16 % 4) * (DK / 8 * 32);
+            for (int j = threadIdx.x % Plan::fetch; j < Plan::RG * 8 * 32; j += Plan::fetch) cp16(smem_addr(late.r) + j * 16, r + j, true);
+            for (int j = threadIdx.x % Plan::fetch; j < Plan::RG * (DK / 8) * 32; j += Plan::fetch) cp16(smem_addr(late.s) + j * 16, s + j, true);
+        }
     };
     float D[DK / 8][4];
     const float *from = SUMMARY ? nullptr
@@ -247,18 +296,20 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
                                      : (P.adj_in != nullptr ? P.adj_in + (long long)bh * P.Dv * P.Dk : nullptr);
     load_state<DK>(D, from, walks ? row : P.Dv, P.Dv, P.Dk);
 
+    if (fetch_ahead<Plan>(walks, count, load_early, load_late)) return;
     for (int i = 0; i < count; i++) {
-        begin_chunk<STAGES>(i, count, load_early, load_late);
+        begin_chunk<Plan>(walks, i, count, load_early, load_late);
         const int c = c1 - 1 - i;
         const long long t0 = (long long)c * kC, nv = ((long long)bh * P.chunks + c) * P.vblocks + r0 / kC, g = nv * 4 + w4;
         Early &e = stage(i);
+        Late &late = stage_late(i);
         const unsigned ks = smem_addr(e.k[0]), gs = smem_addr(e.go[0]);
         // X = beta (e^{G_C - G} (D K^T) + dO^T P)
         float X[8][4] = {};
         if (walks) {
             rows_times<3, NP, DK>(X, D, ks);
             if constexpr (!SUMMARY) {
-                store_tiles(P.df + g * (DK / 8 * 32), D);
+                if constexpr (WHAT == BOTH) store_tiles(P.df + g * (DK / 8 * 32), D);
                 store_rows<NP, DK>(P.ds + nv * (NP * kC * DK) + 16 * w4 * DK, D);
             }
             scale_tokens(X, e.coef, COEF_LEFT);
@@ -266,7 +317,7 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
                                          [&](int ib, int nb) { return at_kn(smem_addr(e.p[0]), kLd, 16 * ib, 16 * nb); }, kC * kLd);
             scale_tokens(X, e.coef, COEF_BETA);
         }
-        late_tiles<STAGES>();
+        late_tiles<Plan>(walks);
         if (!walks) continue;
         const unsigned qs = smem_addr(late.q[0]), vs = smem_addr(late.v[0]);
         // rb = X + (T - I)^T X
@@ -277,8 +328,27 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
             for (int j = 0; j < 4; j++) rb[n][j] = X[n][j];
         triangle<3, NT, false, true>(rb, [&](unsigned (&a)[3][4], int ib) { as_left(X[2 * ib], X[2 * ib + 1], a); },
                                      [&](int ib, int nb) { return at_nk(smem_addr(late.tri[0]), kLd, 16 * nb, 16 * ib); }, kC * kLd);
+        if constexpr (WHAT == REVERSE) {
+            float sums[8][2], dot = 0.f;
+#pragma unroll
+            for (int n = 0; n < 8; n++) {
+                const float4 r = late.r[(w * 8 + n) * 32 + lane];
+                sums[n][0] = fmaf(rb[n][0], r.x, rb[n][2] * r.z);
+                sums[n][1] = fmaf(rb[n][1], r.y, rb[n][3] * r.w);
+            }
+            column_sums(sums);
+            *reinterpret_cast<float2 *>(P.rr + g * kC + 8 * gr + tc) = make_float2(sums[0][0], sums[0][1]);
+#pragma unroll
+            for (int n = 0; n < DK / 8; n++) {
+                const float4 s = late.s[(w * (DK / 8) + n) * 32 + lane];
+                dot = fmaf(D[n][0], s.x, fmaf(D[n][1], s.y, fmaf(D[n][2], s.z, fmaf(D[n][3], s.w, dot))));
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+            if (lane == 0) P.sd[g] = dot;
+        }
         if constexpr (!SUMMARY) {
-            store_tiles(P.rbf + g * (8 * 32), rb);
+            if constexpr (WHAT == BOTH) store_tiles(P.rbf + g * (8 * 32), rb);
             float dots[8][2];
             dots_with<NP>(dots, rb, vs, VLD, 16 * w);
             column_sums(dots);
@@ -347,6 +417,7 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
 #pragma unroll
                 for (int h = 0; h < 2; h++) fma_row(D[2 * nb + m], h, pair(eC, eC), pair(x[m][2 * h], x[m][2 * h + 1]));
         }
+        end_chunk<Plan>(i, count);
     }
     if (!walks) return;
     float *to = SUMMARY ? P.adj_end + ((long long)bh * P.segs + seg) * P.Dv * P.Dk
@@ -354,34 +425,39 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
     if (to != nullptr) store_state<DK>(to, D, row, P.Dv, P.Dk);
 }
 
-template <int DK, int NP, bool SUMMARY, class T>
-__global__ void __launch_bounds__((WalkPlan<DK, NP>::threads), (WalkPlan<DK, NP>::blocks)) delta_walks_kernel(const ChunkParams P)
+template <int DK, int NP, bool SUMMARY, int WHAT, class T>
+__global__ void __launch_bounds__((WalkPlan<DK, NP, WHAT>::threads), 1) delta_walks_kernel(const ChunkParams P)
 {
     extern __shared__ __align__(16) unsigned char raw[];
-    const int back = (P.Dv + WalkPlan<DK, NP>::VW - 1) / WalkPlan<DK, NP>::VW;      // the reverse walk's blocks come first
-    if ((int)blockIdx.y < back) reverse_walk<DK, NP, SUMMARY, T>(P, raw, blockIdx.y);
-    else forward_walk<DK, NP, SUMMARY>(P, raw, blockIdx.y - back);
+    constexpr int VW = WalkPlan<DK, NP, WHAT>::VW;
+    const int back = WHAT == FORWARD ? 0 : (P.Dv + VW - 1) / VW;        // the reverse walk's blocks come first
+    if (WHAT != FORWARD && (int)blockIdx.y < back) reverse_walk<DK, NP, SUMMARY, WHAT, T>(P, raw, blockIdx.y);
+    else if (WHAT != REVERSE) forward_walk<DK, NP, SUMMARY, WHAT>(P, raw, blockIdx.y - back);
 }
 
-template <int DK, int NP, bool SUMMARY> cudaError_t walks(const ChunkParams &P, cudaStream_t st)
+template <int DK, int NP, bool SUMMARY, int WHAT> cudaError_t walks(const ChunkParams &P, cudaStream_t st)
 {
     using T = typename std::conditional<NP == 1, bf16, float>::type;
-    using Plan = WalkPlan<DK, NP>;
-    auto *kernel = delta_walks_kernel<DK, NP, SUMMARY, T>;
+    using Plan = WalkPlan<DK, NP, WHAT>;
+    auto *kernel = delta_walks_kernel<DK, NP, SUMMARY, WHAT, T>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan::smem);
     if (e != cudaSuccess) return e;
     const int vblks = (P.Dv + Plan::VW - 1) / Plan::VW, ident = SUMMARY ? (P.Dk + Plan::VW - 1) / Plan::VW : 0;
-    return launch(kernel, dim3((unsigned)(P.B * P.Hv), 2 * vblks + ident, P.segs), dim3(Plan::threads), Plan::smem, st, P);
+    return launch(kernel, dim3((unsigned)(P.B * P.Hv), (WHAT == BOTH ? 2 : 1) * vblks + ident, P.segs), dim3(Plan::threads), Plan::smem, st, P);
 }
 
 template <int DK, int NP> cudaError_t run(const ChunkParams &P, cudaStream_t st)
 {
+    if (!P.together) {
+        const cudaError_t e = walks<DK, NP, false, FORWARD>(P, st);
+        return e == cudaSuccess ? walks<DK, NP, false, REVERSE>(P, st) : e;
+    }
     if (P.segs > 1) {
-        cudaError_t e = walks<DK, NP, true>(P, st);
+        cudaError_t e = walks<DK, NP, true, BOTH>(P, st);
         if (e == cudaSuccess) e = launch_delta_join(P, DK, true, st);
         if (e != cudaSuccess) return e;
     }
-    return walks<DK, NP, false>(P, st);
+    return walks<DK, NP, false, BOTH>(P, st);
 }
 
 }  // namespace
