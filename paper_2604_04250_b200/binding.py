@@ -324,6 +324,29 @@ def make_delta_params(B, L, Hk, Hv, Dk, Dv, scale=None, flags=0, q_stride=0, k_s
                              max(Dk, 1) ** -0.5 if scale is None else scale, flags, q_stride, k_stride, v_stride, o_stride)
 
 
+def _delta_rows(params, q, k, v, o):
+    """The params of a call whose tensors are batched [B, L, ...]: their rows must lie L strides apart from batch to
+    batch.  One token has no step to the next, so torch gives that dimension any stride (that of a slice of a
+    projection, seen as heads, is the slice's width); the step between batches is then the rows' stride."""
+    B, L = params.B, params.L
+    if B == 1 or L < 1:
+        return params
+    mended = None
+    for name, x, heads, width in (("q_stride", q, params.Hk, params.Dk), ("k_stride", k, params.Hk, params.Dk),
+                                  ("v_stride", v, params.Hv, params.Dv), ("o_stride", o, params.Hv, params.Dv)):
+        if not hasattr(x, "stride") or x.dim() < 3 or x.size(0) != B or x.size(1) != L:
+            continue
+        row, batch = getattr(params, name) or heads * width, x.stride(0)
+        if batch == L * row:
+            continue
+        if L > 1:
+            raise ValueError(f"{name} {row}: batches of {L} rows lie {L * row} elements apart, the tensor's {batch}")
+        if mended is None:
+            mended = cawn_delta_params.from_buffer_copy(params)
+        setattr(mended, name, batch)
+    return mended or params
+
+
 def cawn_delta_rule_workspace_bytes(params, op):
     n = ctypes.c_size_t(0)
     _check(lib().cawn_delta_rule_workspace_bytes(ctypes.byref(params), op, ctypes.byref(n)),
@@ -342,12 +365,14 @@ def new_delta_workspace(params, op, device="cuda"):
 
 
 def cawn_delta_rule_fwd(params, q, k, v, g, beta, o, workspace, state_in=None, state_out=None, stream=None):
+    params = _delta_rows(params, q, k, v, o)
     _check(lib().cawn_delta_rule_fwd(
         ctypes.byref(params), _dp(q), _dp(k), _dp(v), _dp(g), _dp(beta), _dp(state_in), _dp(o), _dp(state_out),
         _dp(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "cawn_delta_rule_fwd")
 
 
 def cawn_delta_rule_step(params, q, k, v, g, beta, o, state_in=None, state_out=None, stream=None):
+    params = _delta_rows(params, q, k, v, o)
     _check(lib().cawn_delta_rule_step(
         ctypes.byref(params), _dp(q), _dp(k), _dp(v), _dp(g), _dp(beta), _dp(state_in), _dp(o), _dp(state_out),
         _stream(stream)), "cawn_delta_rule_step")
@@ -355,6 +380,7 @@ def cawn_delta_rule_step(params, q, k, v, g, beta, o, state_in=None, state_out=N
 
 def cawn_delta_rule_bwd(params, q, k, v, g, beta, grad_o, grad_q, grad_k, grad_v, grad_g, grad_beta, workspace,
                         state_in=None, grad_state_out=None, grad_state_in=None, stream=None):
+    params = _delta_rows(params, q, k, v, grad_o)
     _check(lib().cawn_delta_rule_bwd(
         ctypes.byref(params), _dp(q), _dp(k), _dp(v), _dp(g), _dp(beta), _dp(state_in), _dp(grad_o),
         _dp(grad_state_out), _dp(grad_q), _dp(grad_k), _dp(grad_v), _dp(grad_g), _dp(grad_beta), _dp(grad_state_in),

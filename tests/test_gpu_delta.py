@@ -107,6 +107,25 @@ def test_slices_of_one_projection(form, dtype):
     assert (out[..., :8] == 7).all() and (out[..., -8:] == 7).all()
 
 
+@pytest.mark.parametrize("form", ["step", "chunk", "backward"])
+def test_slices_of_one_token_with_the_strides_of_the_heads_view(form):
+    """One token's slice seen as heads: torch gives the time dimension the slice's width as its stride, batches lie
+    the projection's width apart."""
+    B, Hk, Hv, Dk, Dv = 3, 2, 4, 64, 72
+    d = delta_inputs(B, 1, Hk, Hv, Dk, Dv, torch.bfloat16, seed=8)
+    c = {n: t.cuda() for n, t in d.items()}
+    w = torch.cat([c["q"].flatten(2), c["k"].flatten(2), c["v"].flatten(2)], -1)
+    c["q"], c["k"], c["v"] = (x.unflatten(-1, s) for x, s in zip(w.split([Hk * Dk, Hk * Dk, Hv * Dv], -1), [(Hk, Dk), (Hk, Dk), (Hv, Dv)]))
+    assert c["q"].stride(0) == w.shape[-1] and c["q"].stride(1) == Hk * Dk
+    prm = params(d, q_stride=c["q"].stride(1), k_stride=c["k"].stride(1), v_stride=c["v"].stride(1))
+    if form == "backward":
+        return check_grads(backward(d, prm, c), reference_grads(d), torch.bfloat16)
+    o, so = forward(d, form, prm=prm, cuda=c)
+    want_o, want_s = reference(d)
+    close(o, want_o, TOL[torch.bfloat16])
+    close(so, want_s, STATE_TOL)
+
+
 @pytest.mark.parametrize("form", ["step", "chunk"])
 def test_state_passing_across_calls(form):
     """A prompt in two calls, of which the second goes token by token, equals one call."""

@@ -82,6 +82,24 @@ def test_delta_rule_workspace():
     assert bwd(long, ws=None) == cb.CAWN_ERR_NULL_POINTER
 
 
+def test_delta_rule_rows_of_tensors():
+    """Strides against the tensors they are said of: a batch step that is not L rows is refused, and one token's row
+    stride, which torch leaves open, is the batch step."""
+    import torch
+    for L in (1, 5):
+        w = torch.zeros(2, L, 3 * 64)
+        q, k, v = (x.unflatten(-1, (1, 64)) for x in w.split(64, -1))
+        prm = cb.make_delta_params(2, L, 1, 1, 64, 64, q_stride=q.stride(1), k_stride=192, v_stride=v.stride(1))
+        got = cb._delta_rows(prm, q, k, v, torch.zeros(2, L, 1, 64))
+        assert (got.q_stride, got.k_stride, got.v_stride, got.o_stride) == (192, 192, 192, 0)
+        assert prm.q_stride == q.stride(1)              # the caller's own are left alone
+    dense = cb.make_delta_params(2, 5, 1, 1, 64, 64)
+    with pytest.raises(ValueError, match="v_stride"):
+        cb._delta_rows(dense, torch.zeros(2, 5, 1, 64), torch.zeros(2, 5, 1, 64), v, torch.zeros(2, 5, 1, 64))
+    with pytest.raises(ValueError, match="q_stride"):   # the first five tokens of a longer buffer
+        cb._delta_rows(dense, torch.zeros(2, 9, 1, 64)[:, :5], k, v, None)
+
+
 def test_delta_rule_backward_pointers():
     for name in ("grad_o", "grad_q", "grad_k", "grad_v", "grad_g", "grad_beta"):
         assert bwd(delta(), **{name: None}) == cb.CAWN_ERR_NULL_POINTER, name
