@@ -121,35 +121,35 @@ struct Carver {
     }
 };
 
-// One sequence array as bfloat16 terms: itself, or (float storage) split into the workspace.
-int terms_of(Terms &t, const void *src, long long stride, long long rows, long long L, int width, int terms, size_t bytes, Carver &ws, cudaStream_t st)
+// One sequence array as bfloat16 terms: itself, or (float storage) to be split into the workspace.
+Terms terms_of(SplitJobs &jobs, const void *src, long long stride, const cawn_delta_params *p, int width, const Plan &w, size_t bytes, Carver &ws)
 {
-    if (terms == 1) {
-        t = {static_cast<const bf16 *>(src), 0, stride, stride * L};
-        return CAWN_OK;
-    }
+    if (w.terms == 1) return {static_cast<const bf16 *>(src), 0, stride, stride * p->L};
     bf16 *dst = ws.take<bf16>(bytes);
-    t = {dst, rows * width, width, (long long)width * L};
-    return status_of(launch_delta_split(static_cast<const float *>(src), dst, t.plane, rows, width, stride, st));
+    jobs.job[jobs.count++] = {static_cast<const float *>(src), dst, stride, width};
+    return {dst, jobs.rows * width, width, (long long)width * p->L};
 }
 
-int chunk_params(ChunkParams &C, const cawn_delta_params *p, const DeltaParams &D, const Plan &w, Carver &ws, cudaStream_t st)
+// The shared part of both directions' arguments; grad_o NULL in the forward.
+int chunk_params(ChunkParams &C, const cawn_delta_params *p, const DeltaParams &D, const Plan &w, const void *grad_o, Carver &ws, cudaStream_t st)
 {
     C.g = D.g; C.beta = D.beta; C.state_in = D.state_in;
     C.L = p->L; C.B = p->B; C.Hk = p->Hk; C.Hv = p->Hv; C.Dk = p->Dk; C.Dv = p->Dv; C.scale = p->scale;
     C.chunks = w.chunks; C.vblocks = w.vblocks; C.segs = w.segs; C.seg_chunks = w.seg_chunks;
-    C.p_terms = w.terms == 3 ? 3 : w.rf > 0 ? 2 : 1;    // bfloat16 outputs take one, the backward's dots two
-    const long long rows = (long long)p->B * p->L;
-    int rc = terms_of(C.q, D.q, D.q_stride, rows, p->L, p->Hk * p->Dk, w.terms, w.q, ws, st);
-    if (rc == CAWN_OK) rc = terms_of(C.k, D.k, D.k_stride, rows, p->L, p->Hk * p->Dk, w.terms, w.k, ws, st);
-    if (rc == CAWN_OK) rc = terms_of(C.v, D.v, D.v_stride, rows, p->L, p->Hv * p->Dv, w.terms, w.v, ws, st);
+    C.p_terms = w.terms == 3 ? 3 : grad_o != nullptr ? 2 : 1;   // bfloat16 outputs take one, the backward's dots two
+    SplitJobs jobs = {};
+    jobs.rows = (long long)p->B * p->L;
+    C.q = terms_of(jobs, D.q, D.q_stride, p, p->Hk * p->Dk, w, w.q, ws);
+    C.k = terms_of(jobs, D.k, D.k_stride, p, p->Hk * p->Dk, w, w.k, ws);
+    C.v = terms_of(jobs, D.v, D.v_stride, p, p->Hv * p->Dv, w, w.v, ws);
+    if (grad_o != nullptr) C.go = terms_of(jobs, grad_o, D.o_stride, p, p->Hv * p->Dv, w, w.go, ws);
     C.coef = ws.take<float>(w.coef);
     C.tri = ws.take<bf16>(w.tri);
     C.p = ws.take<bf16>(w.p);
     C.seg_start = ws.take<float>(w.seg_state);
     C.seg_end = ws.take<float>(w.seg_state);
     C.seg_map = ws.take<float>(w.seg_map);
-    return rc;
+    return jobs.count == 0 ? CAWN_OK : status_of(launch_delta_split(jobs, st));
 }
 
 }  // namespace
@@ -201,7 +201,7 @@ extern "C" int cawn_delta_rule_fwd(const cawn_delta_params *params, const void *
     const DeltaParams D = fill(params, q, k, v, g, beta, state_in);
     ChunkParams C = {};
     Carver ws = {static_cast<char *>(workspace)};
-    rc = chunk_params(C, params, D, w, ws, st);
+    rc = chunk_params(C, params, D, w, nullptr, ws, st);
     if (rc != CAWN_OK) return rc;
     C.o = o; C.state_out = state_out; C.o_stride_t = D.o_stride; C.o_stride_b = D.o_stride * params->L;
     cudaError_t e = launch_delta_prep(C, w.dk, w.terms, st);
@@ -230,9 +230,7 @@ extern "C" int cawn_delta_rule_bwd(const cawn_delta_params *params, const void *
     const DeltaParams D = fill(params, q, k, v, g, beta, state_in);
     ChunkParams C = {};
     Carver ws = {static_cast<char *>(workspace)};
-    rc = chunk_params(C, params, D, w, ws, st);
-    if (rc == CAWN_OK)
-        rc = terms_of(C.go, grad_o, D.o_stride, (long long)params->B * params->L, params->L, params->Hv * params->Dv, w.terms, w.go, ws, st);
+    rc = chunk_params(C, params, D, w, grad_o, ws, st);
     if (rc != CAWN_OK) return rc;
     C.rf = ws.take<float4>(w.rf);
     C.rbf = ws.take<float4>(w.rf);

@@ -474,8 +474,21 @@ __device__ __forceinline__ long long v_base(const ChunkParams &P, const Terms &t
     return (bh / P.Hv) * t.stride_b + t0 * t.stride_t + (long long)(bh % P.Hv) * P.Dv;
 }
 
+// Float arrays of `rows` rows to split, `stride` elements from row to row; terms go one after the other into dst.
+struct SplitJob {
+    const float *src;
+    bf16 *dst;
+    long long stride;
+    int width;
+};
+struct SplitJobs {
+    SplitJob job[4];
+    long long rows;
+    int count;
+};
+
 // terms: NP
-cudaError_t launch_delta_split(const float *src, bf16 *dst, long long plane, long long rows, int width, long long stride, cudaStream_t st);
+cudaError_t launch_delta_split(const SplitJobs &jobs, cudaStream_t st);
 cudaError_t launch_delta_prep(const ChunkParams &P, int dk, int terms, cudaStream_t st);
 // forward over the chunks: outputs and end state
 cudaError_t launch_delta_scan(const ChunkParams &P, int dk, int terms, cudaStream_t st);

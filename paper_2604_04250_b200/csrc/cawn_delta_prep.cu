@@ -202,20 +202,22 @@ __global__ void __launch_bounds__(128, (DK == 64 && NP == 1 ? 6 : 1)) delta_prep
     }
 }
 
-// float array -> three bfloat16 terms, dense rows of `width` (a multiple of 8) elements
-__global__ void __launch_bounds__(256) delta_split_kernel(const float *src, bf16 *dst, long long plane, long long words, int width8, long long stride)
+// Float arrays -> three bfloat16 terms each, dense rows: one launch for all arrays of a call, an array per grid row.
+__global__ void __launch_bounds__(256) delta_split_kernel(const SplitJobs jobs)
 {
-    const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    const SplitJob &j = jobs.job[blockIdx.y];
+    const int width8 = j.width / 8;
+    const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x, words = jobs.rows * width8;
     if (i >= words) return;
     const long long row = i / width8;
     const int col = (int)(i - row * width8) * 8;
     float f[8];
-    load_vec(f, src + row * stride + col);
+    load_vec(f, j.src + row * j.stride + col);
     unsigned w[4][3];
 #pragma unroll
     for (int e = 0; e < 4; e++) split(f[2 * e], f[2 * e + 1], w[e]);
 #pragma unroll
-    for (int m = 0; m < 3; m++) *reinterpret_cast<uint4 *>(dst + m * plane + i * 8) = make_uint4(w[0][m], w[1][m], w[2][m], w[3][m]);
+    for (int m = 0; m < 3; m++) *reinterpret_cast<uint4 *>(j.dst + m * (words * 8) + i * 8) = make_uint4(w[0][m], w[1][m], w[2][m], w[3][m]);
 }
 
 template <int DK, int NP> cudaError_t prep(const ChunkParams &P, cudaStream_t st)
@@ -234,10 +236,12 @@ cudaError_t launch_delta_prep(const ChunkParams &P, int dk, int terms, cudaStrea
     return terms == 1 ? prep<128, 1>(P, st) : prep<128, 3>(P, st);
 }
 
-cudaError_t launch_delta_split(const float *src, bf16 *dst, long long plane, long long rows, int width, long long stride, cudaStream_t st)
+cudaError_t launch_delta_split(const SplitJobs &jobs, cudaStream_t st)
 {
-    const long long words = rows * (width / 8);
-    return launch(delta_split_kernel, dim3((unsigned)((words + 255) / 256)), dim3(256), 0, st, src, dst, plane, words, width / 8, stride);
+    int width = 0;
+    for (int i = 0; i < jobs.count; i++) width = jobs.job[i].width > width ? jobs.job[i].width : width;
+    const long long words = jobs.rows * (width / 8);
+    return launch(delta_split_kernel, dim3((unsigned)((words + 255) / 256), jobs.count), dim3(256), 0, st, jobs);
 }
 
 }  // namespace cawn
