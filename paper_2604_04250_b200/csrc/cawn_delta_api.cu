@@ -46,8 +46,10 @@ int pass_state(const cawn_delta_params *p, const float *from, float *to, cudaStr
     return status_of(from != nullptr ? cudaMemcpyAsync(to, from, bytes, cudaMemcpyDeviceToDevice, st) : cudaMemsetAsync(to, 0, bytes, st));
 }
 
-// Calls of up to this many tokens run token by token.
-constexpr int kStepTokens = 16;
+// Calls of up to this many tokens run token by token.  Step / chunk, us: bfloat16, 12 heads of 64 x 64, 12 tokens
+// 14 / 15, 16 tokens 16 / 15, 24 tokens 21 / 15; 1024 heads of 128 x 128, 16 tokens 102 / 110.  Float storage, whose
+// chunks multiply three terms: 12 heads, 32 tokens 25 / 28, 64 tokens 43 / 30; 1024 heads, 32 tokens 197 / 359.
+inline int step_tokens(const cawn_delta_params *p) { return p->flags != 0 ? 16 : 32; }
 
 // The workspace, front to back; sizes in bytes, every part a multiple of 256.
 struct Plan {
@@ -70,13 +72,16 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
     const double nt = w.terms == 1 ? 2 : 3;      // terms of what is computed
     w.chunks = (int)((p->L + kC - 1) / kC);
     w.vblocks = (p->Dv + kC - 1) / kC;
-    // Time segments where the heads alone leave SMs without a block: they cost a second walk over values and keys,
-    // so fewer than three do not pay.
+    // Time segments where the heads alone leave SMs without a block.  They cost a second walk over values and keys and
+    // the join, so three pay in a forward for long sequences alone.  Three / one, us, bfloat16 heads of 64 x 64: forward,
+    // 49 / 50 heads x 8192 tokens 329 / 366, 49 heads x 2048 110 / 103, x 1024 69 / 58; backward, 24 / 25 heads x 8192
+    // 603 / 732, 24 heads x 2048 191 / 202, x 1024 120 / 116 (float storage, 12 heads x 1024: 177 / 193).  Four, forward,
+    // 36 / 50 heads x 1024: 56 / 58.
     const int vw = 16 * (w.terms == 1 ? kRowGroups<1> : kRowGroups<3>);
     const int64_t blocks = (int64_t)p->B * p->Hv * ((p->Dv + vw - 1) / vw) * (backward ? 2 : 1);
     int64_t segs = sm_count() / blocks;
     if (segs > w.chunks / 4) segs = w.chunks / 4;
-    if (segs < 3) segs = 1;
+    if (segs < 3 || (segs == 3 && !backward && w.chunks <= 32)) segs = 1;
     w.seg_chunks = (int)((w.chunks + segs - 1) / segs);
     w.segs = w.chunks > 0 ? (w.chunks + w.seg_chunks - 1) / w.seg_chunks : 1;
     if (w.segs > 1) {
@@ -190,7 +195,7 @@ extern "C" int cawn_delta_rule_fwd(const cawn_delta_params *params, const void *
     using namespace cawn;
     int rc = check(params);
     if (rc != CAWN_OK) return rc;
-    if (params->L <= kStepTokens) return cawn_delta_rule_step(params, q, k, v, g, beta, state_in, o, state_out, cuda_stream);
+    if (params->L <= step_tokens(params)) return cawn_delta_rule_step(params, q, k, v, g, beta, state_in, o, state_out, cuda_stream);
     if (!chunks_fit(params)) return CAWN_ERR_UNSUPPORTED;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (q == nullptr || k == nullptr || v == nullptr || g == nullptr || beta == nullptr || o == nullptr || workspace == nullptr)

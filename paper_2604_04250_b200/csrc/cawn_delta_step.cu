@@ -7,21 +7,54 @@
 // call is HBM-bound for a batch and latency-bound for one stream.  A row is dealt to LPR lanes, 8 floats
 // each as two float4 (coalesced, no shared memory); a thread holds R rows so that a batch keeps R * 32
 // bytes per thread in flight, while few rows take R = 1 and spread over more SMs.
+// The 2R dot products are summed over the lanes by halving: each exchange sends half of a lane's partial
+// sums away and keeps the other half, so that 2R - 1 exchanges (and a full one per bit that is left) do
+// what 2R log2(LPR) would, and each lane ends up with one dot product, its row's u or o to compute, and
+// only that row's v to read.  The next token's rows are fetched while this one's are summed.
 #include "cawn_delta.cuh"
 
 namespace cawn {
 namespace {
 
 constexpr int kStepThreads = 128;
+constexpr unsigned kAll = 0xffffffffu;
+
+// Four elements as they are stored, and as two pairs of floats.
+template <class T> struct Four;
+template <> struct Four<float> {
+    float4 w;
+    __device__ f32x2 low() const { return pair(w.x, w.y); }
+    __device__ f32x2 high() const { return pair(w.z, w.w); }
+};
+template <> struct Four<bf16> {
+    uint2 w;
+    __device__ f32x2 low() const { return pair(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u)); }
+    __device__ f32x2 high() const { return pair(__uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u)); }
+};
+template <class T> __device__ __forceinline__ Four<T> four(const T *p, bool in)
+{
+    Four<T> r = {};
+    if (in) r = *reinterpret_cast<const Four<T> *>(p);
+    return r;
+}
+
+// One token as a lane needs it: its columns of key and query, its row's value, decay and step.
+template <class T> struct Token {
+    Four<T> k[2], q[2];
+    float v, g, beta;
+};
 
 template <class T, int LPR, int R>
 __global__ void __launch_bounds__(kStepThreads) delta_step_kernel(const DeltaParams P)
 {
-    constexpr int kRowsWarp = 32 / LPR, kRowsPass = kStepThreads / LPR;
+    constexpr int kRowsWarp = 32 / LPR, kRowsPass = kStepThreads / LPR, kSums = 2 * R, kHolds = LPR / kSums;
+    static_assert(kHolds >= 1, "a dot product per lane");
     const int lane = threadIdx.x % LPR, row0 = blockIdx.y * (kRowsPass * R) + (threadIdx.x / 32) * kRowsWarp + (threadIdx.x % 32) / LPR;
     const int bh = blockIdx.x, b = bh / P.Hv, h = bh % P.Hv, hk = h / (P.Hv / P.Hk);
     const int c0 = lane * 4, c1 = (LPR + lane) * 4;              // this lane's columns: c0..c0+3 and c1..c1+3
     const bool in0 = c0 < P.Dk, in1 = c1 < P.Dk;
+    // after the exchanges this lane holds s.k (lower half of the lanes) or s.q (upper half) of row `mine`
+    const int mine = row0 + (lane / kHolds % R) * kRowsPass;
     const long long srow = (long long)bh * P.Dv * P.Dk;
     const T *q = static_cast<const T *>(P.q) + (long long)b * P.L * P.q_stride + (long long)hk * P.Dk;
     const T *k = static_cast<const T *>(P.k) + (long long)b * P.L * P.k_stride + (long long)hk * P.Dk;
@@ -29,69 +62,79 @@ __global__ void __launch_bounds__(kStepThreads) delta_step_kernel(const DeltaPar
     T *o = static_cast<T *>(P.o) + (long long)b * P.L * P.o_stride + (long long)h * P.Dv;
     const float *g = P.g + (long long)b * P.L * P.Hv + h, *beta = P.beta + (long long)b * P.L * P.Hv + h;
 
-    float s[R][8];
-    int row[R];
+    f32x2 s[R][4];
 #pragma unroll
     for (int i = 0; i < R; i++) {
-        row[i] = row0 + i * kRowsPass;
+        const int row = row0 + i * kRowsPass;
         float4 lo = make_float4(0.f, 0.f, 0.f, 0.f), hi = lo;
-        if (P.state_in != nullptr && row[i] < P.Dv) {
-            const float *src = P.state_in + srow + (long long)row[i] * P.Dk;
+        if (P.state_in != nullptr && row < P.Dv) {
+            const float *src = P.state_in + srow + (long long)row * P.Dk;
             if (in0) lo = *reinterpret_cast<const float4 *>(src + c0);
             if (in1) hi = *reinterpret_cast<const float4 *>(src + c1);
         }
-        s[i][0] = lo.x; s[i][1] = lo.y; s[i][2] = lo.z; s[i][3] = lo.w;
-        s[i][4] = hi.x; s[i][5] = hi.y; s[i][6] = hi.z; s[i][7] = hi.w;
+        s[i][0] = pair(lo.x, lo.y); s[i][1] = pair(lo.z, lo.w);
+        s[i][2] = pair(hi.x, hi.y); s[i][3] = pair(hi.z, hi.w);
     }
+    auto fetch = [&](long long t) {
+        Token<T> x;
+        x.k[0] = four(k + t * P.k_stride + c0, in0); x.k[1] = four(k + t * P.k_stride + c1, in1);
+        x.q[0] = four(q + t * P.q_stride + c0, in0); x.q[1] = four(q + t * P.q_stride + c1, in1);
+        x.v = mine < P.Dv ? widen(v[t * P.v_stride + mine]) : 0.f;
+        x.g = g[t * P.Hv]; x.beta = beta[t * P.Hv];
+        return x;
+    };
+    Token<T> next = fetch(0);
     for (long long t = 0; t < P.L; t++) {
-        float kv[8], qv[8];
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const int c = e < 4 ? c0 + e : c1 + e - 4;
-            const bool in = e < 4 ? in0 : in1;
-            kv[e] = in ? widen(k[t * P.k_stride + c]) : 0.f;
-            qv[e] = in ? widen(q[t * P.q_stride + c]) : 0.f;
-        }
-        const float a = decay_of(g[t * P.Hv]), bt = beta[t * P.Hv];
-        float vv[R];
-#pragma unroll
-        for (int i = 0; i < R; i++) vv[i] = row[i] < P.Dv ? widen(v[t * P.v_stride + row[i]]) : 0.f;
-        float kq = 0.f, sk[R], sq[R];
-#pragma unroll
-        for (int e = 0; e < 8; e++) kq = fmaf(kv[e], qv[e], kq);
+        const Token<T> now = next;
+        if (t + 1 < P.L) next = fetch(t + 1);
+        const f32x2 kv[4] = {now.k[0].low(), now.k[0].high(), now.k[1].low(), now.k[1].high()};
+        const f32x2 qv[4] = {now.q[0].low(), now.q[0].high(), now.q[1].low(), now.q[1].high()};
+        const float a = decay_of(now.g);
+        float sums[kSums];                                       // s.k of the R rows, then s.q
 #pragma unroll
         for (int i = 0; i < R; i++) {
-            sk[i] = 0.f; sq[i] = 0.f;
+            f32x2 sk = mul2(s[i][0], kv[0]), sq = mul2(s[i][0], qv[0]);
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                sk[i] = fmaf(s[i][e], kv[e], sk[i]);
-                sq[i] = fmaf(s[i][e], qv[e], sq[i]);
+            for (int e = 1; e < 4; e++) { sk = fma2(s[i][e], kv[e], sk); sq = fma2(s[i][e], qv[e], sq); }
+            const float2 x = halves(sk), y = halves(sq);
+            sums[i] = x.x + x.y; sums[R + i] = y.x + y.y;
+        }
+        f32x2 both = mul2(kv[0], qv[0]);
+#pragma unroll
+        for (int e = 1; e < 4; e++) both = fma2(kv[e], qv[e], both);
+        float kq = halves(both).x + halves(both).y;
+#pragma unroll
+        for (int m = LPR / 2, n = R; m > 0; m /= 2, n /= 2) {
+            kq += __shfl_xor_sync(kAll, kq, m);
+            if (n == 0) sums[0] += __shfl_xor_sync(kAll, sums[0], m);
+            const bool upper = lane & m;
+#pragma unroll
+            for (int i = 0; i < n; i++) {
+                const float sent = upper ? sums[i] : sums[n + i], kept = upper ? sums[n + i] : sums[i];
+                sums[i] = kept + __shfl_xor_sync(kAll, sent, m);
             }
         }
-#pragma unroll
-        for (int m = LPR / 2; m > 0; m /= 2) {
-            kq += __shfl_xor_sync(0xffffffffu, kq, m);
-#pragma unroll
-            for (int i = 0; i < R; i++) {
-                sk[i] += __shfl_xor_sync(0xffffffffu, sk[i], m);
-                sq[i] += __shfl_xor_sync(0xffffffffu, sq[i], m);
-            }
-        }
+        const float u = now.beta * (now.v - a * sums[0]), u_of_mine = __shfl_xor_sync(kAll, u, LPR / 2);   // u: lower half
+        if (lane >= LPR / 2 && lane % kHolds == 0 && mine < P.Dv)
+            o[t * P.o_stride + mine] = narrow<T>(P.scale * fmaf(u_of_mine, kq, a * sums[0]));
+        const f32x2 aa = pair(a, a);
 #pragma unroll
         for (int i = 0; i < R; i++) {
-            const float u = bt * (vv[i] - a * sk[i]);
+            const float ui = __shfl_sync(kAll, u, i * kHolds, LPR);
+            const f32x2 uu = pair(ui, ui);
 #pragma unroll
-            for (int e = 0; e < 8; e++) s[i][e] = fmaf(u, kv[e], a * s[i][e]);
-            if (lane == 0 && row[i] < P.Dv) o[t * P.o_stride + row[i]] = narrow<T>(P.scale * fmaf(u, kq, a * sq[i]));
+            for (int e = 0; e < 4; e++) s[i][e] = fma2(uu, kv[e], mul2(aa, s[i][e]));
         }
     }
     if (P.state_out == nullptr) return;
 #pragma unroll
     for (int i = 0; i < R; i++) {
-        if (row[i] >= P.Dv) continue;
-        float *dst = P.state_out + srow + (long long)row[i] * P.Dk;
-        if (in0) *reinterpret_cast<float4 *>(dst + c0) = make_float4(s[i][0], s[i][1], s[i][2], s[i][3]);
-        if (in1) *reinterpret_cast<float4 *>(dst + c1) = make_float4(s[i][4], s[i][5], s[i][6], s[i][7]);
+        const int row = row0 + i * kRowsPass;
+        if (row >= P.Dv) continue;
+        float *dst = P.state_out + srow + (long long)row * P.Dk;
+        const float2 w0 = halves(s[i][0]), w1 = halves(s[i][1]), w2 = halves(s[i][2]), w3 = halves(s[i][3]);
+        if (in0) *reinterpret_cast<float4 *>(dst + c0) = make_float4(w0.x, w0.y, w1.x, w1.y);
+        if (in1) *reinterpret_cast<float4 *>(dst + c1) = make_float4(w2.x, w2.y, w3.x, w3.y);
     }
 }
 

@@ -62,6 +62,26 @@ def test_forward(shape, form, dtype):
     close(so, want_s, STATE_TOL, "state")
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(100, 3, 2, 6, 40, 72), (160, 1, 4, 4, 128, 40), (80, 2, 8, 8, 64, 64)], ids=str)
+def test_step_of_many_streams(shape, dtype):
+    d = delta_inputs(*shape, dtype, seed=sum(shape))
+    o, so = forward(d, "step")
+    want_o, want_s = reference(d)
+    close(o, want_o, TOL[dtype])
+    close(so, want_s, STATE_TOL)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("L", [16, 17, 32, 33])
+def test_either_side_of_the_short_calls(L, dtype):
+    d = delta_inputs(2, L, 1, 2, 64, 64, dtype, seed=L)
+    o, so = forward(d, "chunk")
+    want_o, want_s = reference(d)
+    close(o, want_o, TOL[dtype])
+    close(so, want_s, STATE_TOL)
+
+
 @pytest.mark.parametrize("form", ["step", "chunk"])
 def test_no_state_in_and_in_place(form):
     d = delta_inputs(2, 150, 2, 2, 64, 64, torch.float32, seed=5)
