@@ -96,7 +96,7 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
         w.go = backward ? w.v : 0;
     }
     w.coef = part((double)nc * kCoef * kC * 4);
-    w.tri = part((double)nc * nt * kTile * 2);
+    w.tri = part((double)nc * nt * kTri * 2);
     w.p = w.tri;
     if (backward) {
         const double nv = (double)nc * w.vblocks, ends = (double)p->B * p->Hv * w.vblocks;

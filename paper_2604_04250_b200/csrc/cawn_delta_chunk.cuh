@@ -29,6 +29,7 @@ namespace cawn {
 constexpr int kC = 64;                  // tokens of a chunk
 constexpr int kPad = 8;                 // bfloat16 of padding per shared row: ldmatrix reads 8 rows without conflicts
 constexpr int kTile = kC * kC;          // elements of a 64 x 64 tile in the workspace
+constexpr int kTri = 10 * 256;          // of a triangle there: its ten 16 x 16 blocks on and below the diagonal
 constexpr int kLd = kC + kPad;
 constexpr int kCoef = 5;                // floats per token: e^G, e^{G_C - G}, beta, log2(e) G (high, low part)
 enum { COEF_EG = 0, COEF_LEFT = 1, COEF_BETA = 2, COEF_GHI = 3, COEF_GLO = 4 };
@@ -45,8 +46,7 @@ struct ChunkParams {
     Terms q, k, v, go;
     const float *g, *beta;
     float *coef;                        // [nc][kCoef][64]
-    bf16 *tri;                          // [nc][NT][64 j][64 i]: T - I transposed, blocks on and below T's diagonal
-    bf16 *p;                            // [nc][NT][64 i][64 j]: P, blocks on and below the diagonal
+    bf16 *tri, *p;                      // [nc][NT][kTri]: T - I, transposed, and P, see in_triangle
     // The backward's walks leave accumulators as they hold them, [nv][4 row groups][tiles of 8 columns][32 lanes]: r
     // and the state before the chunk (sf has a further end state per head), rb and the adjoint of the state after
     // the chunk.
@@ -102,8 +102,19 @@ __device__ __forceinline__ void load_tile(bf16 *dst, const bf16 *src, long long 
         from += STEP * stride;
     }
 }
-// A dense 64 x 64 tile of the workspace
-template <int THREADS> __device__ __forceinline__ void load_dense(bf16 *dst, const bf16 *src) { load_tile<kC, kC, THREADS>(dst, src, kC, kC, kC); }
+// Where block (I, J), I >= J, of a triangle starts, in the workspace and in shared memory: four blocks of 8 x 8 (half of
+// the row, half of the column), 128 bytes each, which is what a warp holds of an accumulator tile and writes at once,
+// and what one phase of ldmatrix reads.  (As 64 x 64 tiles a warp's words fell on eight rows: those stores took a
+// third of the shared memory pipe's time in the kernel that makes T and P.)
+__host__ __device__ constexpr int in_triangle(int I, int J) { return (I * (I + 1) / 2 + J) * 256; }
+template <int THREADS> __device__ __forceinline__ void load_triangle(bf16 *dst, const bf16 *src)
+{
+    const int tid = threadIdx.x % THREADS;
+    const unsigned to = smem_addr(dst) + tid * 16;
+#pragma unroll
+    for (int i = 0; i < kTri / 8; i += THREADS)
+        if ((kTri / 8) % THREADS == 0 || i + tid < kTri / 8) cp16(to + i * 16, src + (i + tid) * 8, true);
+}
 
 __device__ __forceinline__ void ldsm(unsigned (&r)[4], unsigned addr)
 {
@@ -139,6 +150,14 @@ __device__ __forceinline__ unsigned at_kn(unsigned base, int ld, int row, int co
 {
     const int l = threadIdx.x % 32;
     return base + ((row + l % 8 + l / 8 % 2 * 8) * ld + col + l / 16 * 8) * 2;
+}
+
+// the same for block (I, J) of a triangle
+__device__ __forceinline__ unsigned triangle_nk(unsigned base, int I, int J) { return base + in_triangle(I, J) * 2 + threadIdx.x % 32 * 16; }
+__device__ __forceinline__ unsigned triangle_kn(unsigned base, int I, int J)
+{
+    const int l = threadIdx.x % 32;
+    return base + in_triangle(I, J) * 2 + (l / 8 % 2 * 16 + l / 16 * 8 + l % 8) * 16;
 }
 
 // rows h = 0, 1 of an accumulator tile, times / plus pairs
@@ -310,7 +329,7 @@ __device__ __forceinline__ void product(float (&c0)[4], float (&c1)[4], const un
 // diagonal: C block n takes A blocks b <= n (UPPER: b >= n).  `left(a, b)` loads or makes A_b, `at(b, n)` is the
 // address of the right block.  Two C blocks at a time, so that four sums are under way.
 template <int AP, int BP, bool TRANS, bool UPPER, class Left, class At>
-__device__ __forceinline__ void triangle(float (&c)[8][4], Left left, At at, int plane)
+__device__ __forceinline__ void triangle(float (&c)[8][4], Left left, At at)
 {
 #pragma unroll
     for (int i = 0; i < 4; i++) {
@@ -323,13 +342,13 @@ __device__ __forceinline__ void triangle(float (&c)[8][4], Left left, At at, int
             const bool first = UPPER ? j <= b : j >= b, second = UPPER ? j + 1 <= b : j + 1 >= b;
             if (first && second) {
                 unsigned r[2][BP][4];
-                load_right<BP, TRANS>(r[0], at(b, j), plane);
-                load_right<BP, TRANS>(r[1], at(b, j + 1), plane);
+                load_right<BP, TRANS>(r[0], at(b, j), kTri);
+                load_right<BP, TRANS>(r[1], at(b, j + 1), kTri);
                 multiply<AP, BP, 2>(reinterpret_cast<float (&)[4][4]>(c[2 * j]), a, r);
             } else if (first) {
-                product<AP, BP, TRANS>(c[2 * j], c[2 * j + 1], a, at(b, j), plane);
+                product<AP, BP, TRANS>(c[2 * j], c[2 * j + 1], a, at(b, j), kTri);
             } else if (second) {
-                product<AP, BP, TRANS>(c[2 * j + 2], c[2 * j + 3], a, at(b, j + 1), plane);
+                product<AP, BP, TRANS>(c[2 * j + 2], c[2 * j + 3], a, at(b, j + 1), kTri);
             }
         }
     }

@@ -18,9 +18,9 @@ template <int DK, int NP> struct PrepSmem {
         struct { bf16 q[NP][kC * (DK + kPad)], k[NP][kC * (DK + kPad)]; };
         bf16 a[NT][kC * kLd];           // A = At diag(beta), terms: takes the tiles' place once the scores are made
     };
-    bf16 d[NT][4][16 * 24];             // inverses of the diagonal blocks, terms
+    bf16 d[NT][4][16 * 24];             // inverses of the diagonal blocks, transposed, terms
     float diag[4][16][20];              // diagonal blocks of A
-    float ghi[kC], glo[kC], beta[kC];
+    float nhi[kC], nlo[kC], beta[kC];   // -G in two parts
 };
 
 // Each of the four warps owns the 8-row blocks w and 7 - w: below the diagonal that is nine 8 x 8 blocks for
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(128, (DK == 64 && NP == 1 ? 6 : 1)) delta_prep
         for (int e = 0; e < 2; e++) {
             const int t = lane * 2 + e;
             const float hi = (float)sum[e], lo = (float)(sum[e] - (double)hi);
-            sm.ghi[t] = hi; sm.glo[t] = lo; sm.beta[t] = bt[e];
+            sm.nhi[t] = -hi; sm.nlo[t] = -lo; sm.beta[t] = bt[e];
             coef[COEF_EG * kC + t] = exp2_fast(hi) * fmaf(lo, 0.69314718f, 1.f);
             coef[COEF_LEFT * kC + t] = exp2_fast((float)(last - sum[e]));
             coef[COEF_BETA * kC + t] = bt[e];
@@ -100,35 +100,51 @@ __global__ void __launch_bounds__(128, (DK == 64 && NP == 1 ? 6 : 1)) delta_prep
 #pragma unroll
         for (int nb = 0; nb < 4; nb++)
             if (2 * nb <= 7 - w) {
-                product<NP, NP, false>(kk[2 * nb], kk[2 * nb + 1], ka, at_nk(ks, ld, 16 * nb, d), kC * ld);
-                product<NP, NP, false>(qk[2 * nb], qk[2 * nb + 1], qa, at_nk(ks, ld, 16 * nb, d), kC * ld);
+                unsigned r[1][NP][4];
+                load_right<NP, false>(r[0], at_nk(ks, ld, 16 * nb, d), kC * ld);
+                multiply<NP, NP, 1>(reinterpret_cast<float (&)[2][4]>(kk[2 * nb]), ka, r);
+                multiply<NP, NP, 1>(reinterpret_cast<float (&)[2][4]>(qk[2 * nb]), qa, r);
             }
     }
     __syncthreads();                    // A takes the place of the tiles
-    bf16 *pt = P.p + nc * NT * kTile;
+    bf16 *pt = P.p + nc * NT * kTri;
+    const f32x2 scale = pair(P.scale, P.scale);
+    f32x2 hi[2], lo[2];
 #pragma unroll
     for (int half = 0; half < 2; half++) {
-        const int block = half == 0 ? w : 7 - w, i = 8 * block + gr;
-        const float ghi = sm.ghi[i], glo = sm.glo[i];
+        const int i = 8 * (half == 0 ? w : 7 - w) + gr;
+        hi[half] = pair(-sm.nhi[i], -sm.nhi[i]);
+        lo[half] = pair(-sm.nlo[i], -sm.nlo[i]);
+    }
 #pragma unroll
-        for (int n = 0; n < 8; n++) {
+    for (int n = 0; n < 8; n++) {
+        if (n / 2 > (7 - w) / 2) continue;
+        const int j = 8 * n + tc;
+        const f32x2 jhi = *reinterpret_cast<const f32x2 *>(&sm.nhi[j]), jlo = *reinterpret_cast<const f32x2 *>(&sm.nlo[j]);
+        const f32x2 bt = *reinterpret_cast<const f32x2 *>(&sm.beta[j]);
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+            const int block = half == 0 ? w : 7 - w, i = 8 * block + gr;
             // whole 16 x 16 blocks on and below the diagonal are read later: the block's upper half as zeros
             if (n / 2 > block / 2) continue;
-            const int j = 8 * n + tc;
-            const float2 jhi = *reinterpret_cast<const float2 *>(&sm.ghi[j]), jlo = *reinterpret_cast<const float2 *>(&sm.glo[j]);
-            const float2 bt = *reinterpret_cast<const float2 *>(&sm.beta[j]);
-            const float g0 = exp2_fast((ghi - jhi.x) + (glo - jlo.x)), g1 = exp2_fast((ghi - jhi.y) + (glo - jlo.y));
-            const float p0 = i >= j ? P.scale * g0 * qk[n][2 * half] : 0.f, p1 = i >= j + 1 ? P.scale * g1 * qk[n][2 * half + 1] : 0.f;
-            const float a0 = i > j ? g0 * kk[n][2 * half] * bt.x : 0.f, a1 = i > j + 1 ? g1 * kk[n][2 * half + 1] * bt.y : 0.f;
+            const float2 x = halves(add2(add2(hi[half], jhi), add2(lo[half], jlo)));
+            const f32x2 decay = pair(exp2_fast(x.x), exp2_fast(x.y));
+            float2 p = halves(mul2(mul2(scale, decay), pair(qk[n][2 * half], qk[n][2 * half + 1])));
+            float2 a = halves(mul2(mul2(decay, pair(kk[n][2 * half], kk[n][2 * half + 1])), bt));
+            if (n >= block) {
+                p.x = i >= j ? p.x : 0.f; p.y = i >= j + 1 ? p.y : 0.f;
+                a.x = i > j ? a.x : 0.f; a.y = i > j + 1 ? a.y : 0.f;
+            }
             unsigned pw[NT], aw[NT];
-            split(p0, p1, pw);
-            split(a0, a1, aw);
+            split(p.x, p.y, pw);
+            split(a.x, a.y, aw);
+            const int to = in_triangle(block / 2, n / 2) + (block % 2 * 2 + n % 2) * 64 + lane * 2;
 #pragma unroll
             for (int m = 0; m < NT; m++) {
-                if (m < P.p_terms) *reinterpret_cast<unsigned *>(pt + m * kTile + i * kC + j) = pw[m];
+                if (m < P.p_terms) *reinterpret_cast<unsigned *>(pt + m * kTri + to) = pw[m];
                 *reinterpret_cast<unsigned *>(&sm.a[m][i * kLd + j]) = aw[m];
             }
-            if (n / 2 == block / 2) *reinterpret_cast<float2 *>(&sm.diag[block / 2][i % 16][j % 16]) = make_float2(a0, a1);
+            if (n / 2 == block / 2) *reinterpret_cast<float2 *>(&sm.diag[block / 2][i % 16][j % 16]) = a;
         }
     }
     __syncthreads();
@@ -147,22 +163,23 @@ __global__ void __launch_bounds__(128, (DK == 64 && NP == 1 ? 6 : 1)) delta_prep
                 if (l + 3 < i) s1 = fmaf(-v.w, x[l + 3], s1);
             }
             x[i] = s + s1;
-            float rest = x[i];
+        }
 #pragma unroll
-            for (int m = 0; m < NT; m++) {
-                const bf16 term = __float2bfloat16_rn(rest);
-                sm.d[m][w][i * 24 + lane] = term;
-                rest -= __bfloat162float(term);
-            }
+        for (int i = 0; i < 16; i += 8) {
+            unsigned t[4][NT];
+#pragma unroll
+            for (int e = 0; e < 4; e++) split(x[i + 2 * e], x[i + 2 * e + 1], t[e]);
+#pragma unroll
+            for (int m = 0; m < NT; m++) *reinterpret_cast<uint4 *>(&sm.d[m][w][lane * 24 + i]) = make_uint4(t[0][m], t[1][m], t[2][m], t[3][m]);
         }
     }
     __syncthreads();
 
     // block column J = w: left operands hold T_KJ transposed
-    bf16 *tri = P.tri + nc * NT * kTile;
+    bf16 *tri = P.tri + nc * NT * kTri;
     const unsigned as = smem_addr(sm.a[0]), dsm = smem_addr(sm.d[0][0]);
     unsigned tw[4][NT][4];
-    load_left<NT, true>(tw[0], at_nk(dsm + w * 16 * 24 * 2, 24, 0, 0), 4 * 16 * 24);
+    load_left<NT, false>(tw[0], at_kn(dsm + w * 16 * 24 * 2, 24, 0, 0), 4 * 16 * 24);
 #pragma unroll
     for (int step = 0; step < 4; step++) {
         const int I = w + step;
@@ -174,7 +191,7 @@ __global__ void __launch_bounds__(128, (DK == 64 && NP == 1 ? 6 : 1)) delta_prep
                 product<NT, NT, false>(y[0], y[1], tw[m], at_nk(as, kLd, 16 * I, 16 * (w + m)), kC * kLd);
             unsigned yw[NT][4];
             as_left(y[0], y[1], yw);
-            product<NT, NT, false>(z[0], z[1], yw, at_nk(dsm + I * 16 * 24 * 2, 24, 0, 0), 4 * 16 * 24);
+            product<NT, NT, true>(z[0], z[1], yw, at_kn(dsm + I * 16 * 24 * 2, 24, 0, 0), 4 * 16 * 24);
 #pragma unroll
             for (int e = 0; e < 4; e++) { z[0][e] = -z[0][e]; z[1][e] = -z[1][e]; }
             as_left(z[0], z[1], tw[step]);
@@ -193,12 +210,11 @@ __global__ void __launch_bounds__(128, (DK == 64 && NP == 1 ? 6 : 1)) delta_prep
                     if (tc + 1 == gr) out[m][e] &= 0x0000ffffu;
                 }
             }
-        bf16 *dst = tri + (16 * w + gr) * kC + 16 * I + tc;
+        bf16 *dst = tri + in_triangle(I, w) + lane * 2;
 #pragma unroll
         for (int m = 0; m < NT; m++)
 #pragma unroll
-            for (int e = 0; e < 4; e++)
-                *reinterpret_cast<unsigned *>(dst + m * kTile + (e & 1) * 8 * kC + (e >> 1) * 8) = out[m][e];
+            for (int e = 0; e < 4; e++) *reinterpret_cast<unsigned *>(dst + m * kTri + ((e & 1) * 2 + (e >> 1)) * 64) = out[m][e];
     }
 }
 

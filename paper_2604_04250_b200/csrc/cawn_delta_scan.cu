@@ -23,12 +23,12 @@ enum { MODE_OUT, MODE_SUMMARY };
 // Tiles of the chain.
 template <int DK, int NP> struct ScanStage {
     static constexpr int NT = NP == 1 ? 2 : 3, VLD = 16 * kRowGroups<NP> + kPad;
-    bf16 k[NP][kC * (DK + kPad)], tri[NT][kC * kLd], v[NP][kC * VLD];
+    bf16 k[NP][kC * (DK + kPad)], tri[NT][kTri], v[NP][kC * VLD];
     float coef[kCoef][kC];
 };
 // Tiles of the outputs.
 template <int DK, int NP> struct ScanSide {
-    bf16 q[NP][kC * (DK + kPad)], p[NP][kC * kLd];
+    bf16 q[NP][kC * (DK + kPad)], p[NP][kTri];
     bf16 t[kC * (16 * kRowGroups<NP> + kPad)];          // the way out for token rows
     float coef[kCoef][kC];
 };
@@ -60,7 +60,7 @@ __device__ __forceinline__ void scan_load(const ChunkParams &P, ScanStage<DK, NP
         if (vcols > 0) load_tile<kC, VW, TH>(st.v[i], P.v.at + i * P.v.plane + v_base(P, P.v, bh, t0) + v0, P.v.stride_t, rows, vcols);
     }
 #pragma unroll
-    for (int i = 0; i < NT; i++) load_dense<TH>(st.tri[i], P.tri + (nc * NT + i) * kTile);
+    for (int i = 0; i < NT; i++) load_triangle<TH>(st.tri[i], P.tri + (nc * NT + i) * kTri);
     for (int i = threadIdx.x % TH; i < kCoef * kC / 4; i += TH) cp16(smem_addr(&st.coef[0][0]) + i * 16, P.coef + nc * (kCoef * kC) + i * 4, true);
     cp_commit();
 }
@@ -74,7 +74,7 @@ __device__ __forceinline__ void side_load(const ChunkParams &P, ScanSide<DK, NP>
 #pragma unroll
     for (int i = 0; i < NP; i++) {
         load_tile<kC, DK, TH>(st.q[i], P.q.at + i * P.q.plane + q_base(P, P.q, bh, t0), P.q.stride_t, rows, P.Dk);
-        load_dense<TH>(st.p[i], P.p + (nc * NT + i) * kTile);
+        load_triangle<TH>(st.p[i], P.p + (nc * NT + i) * kTri);
     }
     for (int i = threadIdx.x % TH; i < kCoef * kC / 4; i += TH) cp16(smem_addr(&st.coef[0][0]) + i * 16, P.coef + nc * (kCoef * kC) + i * 4, true);
     cp_commit();
@@ -154,7 +154,7 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
                 bar_arrive(BAR_FULL + (cs ^ 1), PAIR);
             }
             triangle<NP, NP, false, false>(Y, [&](unsigned (&a)[NP][4], int tb) { get_left(a, sw.u, tb); },
-                                           [&](int tb, int nb) { return at_nk(ps, kLd, 16 * nb, 16 * tb); }, kC * kLd);
+                                           [&](int tb, int nb) { return triangle_nk(ps, nb, tb); });
             if (c + WS < c1) bar_arrive(BAR_FREE + par, PAIR);
             if (c + CS >= c1) {
                 cp_commit();
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
 #pragma unroll
             for (int i = 0; i < 4; i++) r[n][i] = X[n][i];
         triangle<NT, NT, true, false>(r, [&](unsigned (&a)[NT][4], int tb) { as_left(X[2 * tb], X[2 * tb + 1], a); },
-                                      [&](int tb, int nb) { return at_kn(ts, kLd, 16 * tb, 16 * nb); }, kC * kLd);
+                                      [&](int tb, int nb) { return triangle_kn(ts, nb, tb); });
         // u = beta r, handed over
         scale_tokens(r, st.coef, COEF_BETA);
         if constexpr (MODE == MODE_OUT) {

@@ -24,11 +24,11 @@ template <int DK, int NP> struct WalkTiles {
     static constexpr int NT = NP == 1 ? 2 : 3, VLD = 16 * kRowGroups<NP> + kPad;
     using Keys = bf16[NP][kC * (DK + kPad)];
     using Values = bf16[NP][kC * VLD];
-    using Square = bf16[NT][kC * kLd];
+    using Triangle = bf16[NT][kTri];
     struct FwdEarly { Keys k, q; Values v; float coef[kCoef][kC]; };
-    struct FwdLate { Square tri, p; Values go; };
-    struct RevEarly { Keys k; Values go; Square p; float coef[kCoef][kC]; };
-    struct RevLate { Keys q; Square tri; Values v; };
+    struct FwdLate { Triangle tri, p; Values go; };
+    struct RevEarly { Keys k; Values go; Triangle p; float coef[kCoef][kC]; };
+    struct RevLate { Keys q; Triangle tri; Values v; };
     struct RevFloats : RevLate { float4 r[kRowGroups<NP> * 8 * 32], s[kRowGroups<NP> * (DK / 8) * 32]; };
 };
 // What a launch does: both walks, or one of them (the reverse one with the sums over both).
@@ -63,10 +63,10 @@ template <int DK, int NP> struct Fetch {
 #pragma unroll
         for (int i = 0; i < NP; i++) load_tile<kC, VW, TH>(to[i], t.at + i * t.plane + v_base(P, t, bh, (long long)c * kC) + v0, t.stride_t, rows(c), vcols);
     }
-    __device__ __forceinline__ void square(typename Plan::Tiles::Square &to, const bf16 *from, int c) const
+    __device__ __forceinline__ void triangle(typename Plan::Tiles::Triangle &to, const bf16 *from, int c) const
     {
 #pragma unroll
-        for (int i = 0; i < NT; i++) load_dense<TH>(to[i], from + (((long long)bh * P.chunks + c) * NT + i) * kTile);
+        for (int i = 0; i < NT; i++) load_triangle<TH>(to[i], from + (((long long)bh * P.chunks + c) * NT + i) * kTri);
     }
     __device__ __forceinline__ void coef(float (&to)[kCoef][kC], int c) const
     {
@@ -79,7 +79,8 @@ template <int DK, int NP> struct Fetch {
 // Returns true for the former, which are done.
 template <class Plan, class Early, class Late> __device__ __forceinline__ bool fetch_ahead(bool walks, int count, Early load_early, Late load_late)
 {
-    if (Plan::late == 1 || walks) return false;
+    if constexpr (Plan::late == 1) return false;
+    if (walks) return false;
     for (int i = 0; i < count; i++) {
         if (i >= 2) bar_sync(BAR_EMPTY + i % 2, Plan::threads);
         load_early(i);
@@ -156,9 +157,9 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
     };
     auto load_late = [&](int i) {
         Late &late = stage_late(i);
-        fetch.square(late.tri, P.tri, c0 + i);
+        fetch.triangle(late.tri, P.tri, c0 + i);
         if (!SUMMARY) {
-            fetch.square(late.p, P.p, c0 + i);
+            fetch.triangle(late.p, P.p, c0 + i);
             fetch.values(late.go, P.go, c0 + i);
         }
     };
@@ -200,12 +201,12 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
 #pragma unroll
             for (int j = 0; j < 4; j++) r[n][j] = X[n][j];
         triangle<3, NT, true, false>(r, [&](unsigned (&a)[3][4], int tb) { as_left(X[2 * tb], X[2 * tb + 1], a); },
-                                     [&](int tb, int nb) { return at_kn(smem_addr(late.tri[0]), kLd, 16 * tb, 16 * nb); }, kC * kLd);
+                                     [&](int tb, int nb) { return triangle_kn(smem_addr(late.tri[0]), nb, tb); });
         if constexpr (!SUMMARY) store_tiles(P.rf + g * (8 * 32), r);
         scale_tokens(r, e.coef, COEF_BETA);
         if constexpr (!SUMMARY) {
             triangle<3, NT, false, false>(Y, [&](unsigned (&a)[3][4], int tb) { as_left(r[2 * tb], r[2 * tb + 1], a); },
-                                          [&](int tb, int nb) { return at_nk(smem_addr(late.p[0]), kLd, 16 * nb, 16 * tb); }, kC * kLd);
+                                          [&](int tb, int nb) { return triangle_nk(smem_addr(late.p[0]), nb, tb); });
             float dots[8][2];
             dots_with<NP>(dots, Y, smem_addr(late.go[0]), VLD, 16 * w);
             column_sums(dots);
@@ -274,12 +275,12 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
         Early &e = stage(i);
         fetch.keys(e.k, P.k, c1 - 1 - i);
         fetch.values(e.go, P.go, c1 - 1 - i);
-        fetch.square(e.p, P.p, c1 - 1 - i);
+        fetch.triangle(e.p, P.p, c1 - 1 - i);
         fetch.coef(e.coef, c1 - 1 - i);
     };
     auto load_late = [&](int i) {
         Late &late = stage_late(i);
-        fetch.square(late.tri, P.tri, c1 - 1 - i);
+        fetch.triangle(late.tri, P.tri, c1 - 1 - i);
         fetch.keys(late.q, P.q, c1 - 1 - i);
         if (!SUMMARY) fetch.values(late.v, P.v, c1 - 1 - i);
         if constexpr (WHAT == REVERSE) {        // this block's row groups lie one after the other
@@ -314,7 +315,7 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
             }
             scale_tokens(X, e.coef, COEF_LEFT);
             triangle<NP, NT, true, true>(X, [&](unsigned (&a)[NP][4], int ib) { load_left<NP, true>(a, at_nk(gs, VLD, 16 * ib, 16 * w), kC * VLD); },
-                                         [&](int ib, int nb) { return at_kn(smem_addr(e.p[0]), kLd, 16 * ib, 16 * nb); }, kC * kLd);
+                                         [&](int ib, int nb) { return triangle_kn(smem_addr(e.p[0]), ib, nb); });
             scale_tokens(X, e.coef, COEF_BETA);
         }
         late_tiles<Plan>(walks);
@@ -327,7 +328,7 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
 #pragma unroll
             for (int j = 0; j < 4; j++) rb[n][j] = X[n][j];
         triangle<3, NT, false, true>(rb, [&](unsigned (&a)[3][4], int ib) { as_left(X[2 * ib], X[2 * ib + 1], a); },
-                                     [&](int ib, int nb) { return at_nk(smem_addr(late.tri[0]), kLd, 16 * nb, 16 * ib); }, kC * kLd);
+                                     [&](int ib, int nb) { return triangle_nk(smem_addr(late.tri[0]), ib, nb); });
         if constexpr (WHAT == REVERSE) {
             float sums[8][2], dot = 0.f;
 #pragma unroll
