@@ -44,6 +44,7 @@ template <int DK, int NP> struct GradSmem {
 template <int DK, int NP, class T>
 __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grads_kernel(const ChunkParams P)
 {
+    follow_previous();
     constexpr int ld = DK + kPad, ND = DK / 16, VW = kGradVW<DK, NP>, ldv = VW + kPad;
     extern __shared__ __align__(16) unsigned char raw[];
     auto &sm = *reinterpret_cast<GradSmem<DK, NP> *>(raw);
@@ -72,7 +73,7 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
                 float dots[8][2];
 #pragma unroll
                 for (int n = 0; n < 8; n++) {
-                    const float4 r = __ldg(P.rf + (g * 8 + n) * 32 + lane), rb = __ldg(P.rbf + (g * 8 + n) * 32 + lane);
+                    const float4 r = P.rf[(g * 8 + n) * 32 + lane], rb = P.rbf[(g * 8 + n) * 32 + lane];
                     dots[n][0] = fmaf(r.x, rb.x, r.z * rb.z);
                     dots[n][1] = fmaf(r.y, rb.y, r.w * rb.w);
                 }
@@ -83,7 +84,7 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
                 float dot = 0.f;
 #pragma unroll
                 for (int n = 0; n < DK / 8; n++) {
-                    const float4 s = __ldg(P.sf + (next * (DK / 8) + n) * 32 + lane), d = __ldg(P.df + (g * (DK / 8) + n) * 32 + lane);
+                    const float4 s = P.sf[(next * (DK / 8) + n) * 32 + lane], d = P.df[(g * (DK / 8) + n) * 32 + lane];
                     dot = fmaf(s.x, d.x, fmaf(s.y, d.y, fmaf(s.z, d.z, fmaf(s.w, d.w, dot))));
                 }
 #pragma unroll

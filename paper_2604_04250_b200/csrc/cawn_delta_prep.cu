@@ -1,8 +1,9 @@
 // Gated delta rule, chunk form: what a chunk needs that does not depend on the state.  All chunks of all
 // heads at once: decays, the scores P, and the inverse T of the chunk's triangle.
 //
-// Bound: instructions and their latency (exponentials, splitting, substitution), so many small blocks per SM: six,
-// which is why A reuses the tiles' shared memory.
+// Bound: instructions and their latency (exponentials, splitting, substitution) and the shared memory pipe, so many
+// small blocks per SM, which is why A reuses the tiles' shared memory: five, at 96 registers (3072 chunks of 64 keys:
+// 35 us; with six, which spill, 39, with four 39).
 // The inverse: 16 x 16 blocks on the diagonal by substitution in float (a lane per column), the blocks
 // below from T_IJ = -T_II sum_K A_IK T_KJ on the tensor cores, a block column per warp with the
 // intermediate blocks in registers.  Substitution is stable for every triangle whose inverse is moderate;
@@ -23,11 +24,12 @@ template <int DK, int NP> struct PrepSmem {
     float nhi[kC], nlo[kC], beta[kC];   // -G in two parts
 };
 
-// Each of the four warps owns the 8-row blocks w and 7 - w: below the diagonal that is nine 8 x 8 blocks for
+// PT: terms of P that are read later.  Each of the four warps owns the 8-row blocks w and 7 - w: below the diagonal that is nine 8 x 8 blocks for
 // everyone.  (With 16 adjacent rows the last warp had four times the first one's exponentials.)
-template <int DK, int NP>
-__global__ void __launch_bounds__(128, (DK == 64 && NP == 1 ? 6 : 1)) delta_prep_kernel(const ChunkParams P)
+template <int DK, int NP, int PT>
+__global__ void __launch_bounds__(128, (DK == 64 && NP == 1 ? 5 : 1)) delta_prep_kernel(const ChunkParams P)
 {
+    follow_previous();
     extern __shared__ __align__(16) unsigned char raw[];
     auto &sm = *reinterpret_cast<PrepSmem<DK, NP> *>(raw);
     constexpr int ld = DK + kPad, NT = NP == 1 ? 2 : 3;
@@ -135,15 +137,14 @@ __global__ void __launch_bounds__(128, (DK == 64 && NP == 1 ? 6 : 1)) delta_prep
                 p.x = i >= j ? p.x : 0.f; p.y = i >= j + 1 ? p.y : 0.f;
                 a.x = i > j ? a.x : 0.f; a.y = i > j + 1 ? a.y : 0.f;
             }
-            unsigned pw[NT], aw[NT];
+            unsigned pw[PT], aw[NT];
             split(p.x, p.y, pw);
             split(a.x, a.y, aw);
             const int to = in_triangle(block / 2, n / 2) + (block % 2 * 2 + n % 2) * 64 + lane * 2;
 #pragma unroll
-            for (int m = 0; m < NT; m++) {
-                if (m < P.p_terms) *reinterpret_cast<unsigned *>(pt + m * kTri + to) = pw[m];
-                *reinterpret_cast<unsigned *>(&sm.a[m][i * kLd + j]) = aw[m];
-            }
+            for (int m = 0; m < PT; m++) *reinterpret_cast<unsigned *>(pt + m * kTri + to) = pw[m];
+#pragma unroll
+            for (int m = 0; m < NT; m++) *reinterpret_cast<unsigned *>(&sm.a[m][i * kLd + j]) = aw[m];
             if (n / 2 == block / 2) *reinterpret_cast<float2 *>(&sm.diag[block / 2][i % 16][j % 16]) = a;
         }
     }
@@ -221,6 +222,7 @@ __global__ void __launch_bounds__(128, (DK == 64 && NP == 1 ? 6 : 1)) delta_prep
 // Float arrays -> three bfloat16 terms each, dense rows: one launch for all arrays of a call, an array per grid row.
 __global__ void __launch_bounds__(256) delta_split_kernel(const SplitJobs jobs)
 {
+    follow_previous();
     const SplitJob &j = jobs.job[blockIdx.y];
     const int width8 = j.width / 8;
     const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x, words = jobs.rows * width8;
@@ -236,20 +238,21 @@ __global__ void __launch_bounds__(256) delta_split_kernel(const SplitJobs jobs)
     for (int m = 0; m < 3; m++) *reinterpret_cast<uint4 *>(j.dst + m * (words * 8) + i * 8) = make_uint4(w[0][m], w[1][m], w[2][m], w[3][m]);
 }
 
-template <int DK, int NP> cudaError_t prep(const ChunkParams &P, cudaStream_t st)
+template <int DK, int NP, int PT> cudaError_t prep(const ChunkParams &P, cudaStream_t st)
 {
     const size_t smem = sizeof(PrepSmem<DK, NP>);
-    const cudaError_t e = cudaFuncSetAttribute(delta_prep_kernel<DK, NP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = cudaFuncSetAttribute(delta_prep_kernel<DK, NP, PT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    return launch(delta_prep_kernel<DK, NP>, dim3((unsigned)(P.B * P.Hv * (long long)P.chunks)), dim3(128), smem, st, P);
+    return launch<true>(delta_prep_kernel<DK, NP, PT>, dim3((unsigned)(P.B * P.Hv * (long long)P.chunks)), dim3(128), smem, st, P);
 }
 
 }  // namespace
 
 cudaError_t launch_delta_prep(const ChunkParams &P, int dk, int terms, cudaStream_t st)
 {
-    if (dk == 64) return terms == 1 ? prep<64, 1>(P, st) : prep<64, 3>(P, st);
-    return terms == 1 ? prep<128, 1>(P, st) : prep<128, 3>(P, st);
+    if (terms == 3) return dk == 64 ? prep<64, 3, 3>(P, st) : prep<128, 3, 3>(P, st);
+    if (P.p_terms == 1) return dk == 64 ? prep<64, 1, 1>(P, st) : prep<128, 1, 1>(P, st);
+    return dk == 64 ? prep<64, 1, 2>(P, st) : prep<128, 1, 2>(P, st);
 }
 
 cudaError_t launch_delta_split(const SplitJobs &jobs, cudaStream_t st)
@@ -257,7 +260,7 @@ cudaError_t launch_delta_split(const SplitJobs &jobs, cudaStream_t st)
     int width = 0;
     for (int i = 0; i < jobs.count; i++) width = jobs.job[i].width > width ? jobs.job[i].width : width;
     const long long words = jobs.rows * (width / 8);
-    return launch(delta_split_kernel, dim3((unsigned)((words + 255) / 256), jobs.count), dim3(256), 0, st, jobs);
+    return launch<true>(delta_split_kernel, dim3((unsigned)((words + 255) / 256), jobs.count), dim3(256), 0, st, jobs);
 }
 
 }  // namespace cawn

@@ -83,6 +83,7 @@ __device__ __forceinline__ void side_load(const ChunkParams &P, ScanSide<DK, NP>
 template <int DK, int NP, int MODE, class T>
 __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_scan_kernel(const ChunkParams P)
 {
+    follow_previous();
     using Plan = ScanPlan<DK, NP, MODE>;
     using Side = ScanSide<DK, NP>;
     using Swap = ScanSwap<DK, NP>;
@@ -289,7 +290,7 @@ template <int DK, int NP, int MODE> cudaError_t scan(const ChunkParams &P, cudaS
     if (e != cudaSuccess) return e;
     constexpr int VW = 16 * Plan::RG;
     const int blocks = (P.Dv + VW - 1) / VW + (MODE == MODE_SUMMARY ? (P.Dk + VW - 1) / VW : 0);
-    return launch(kernel, dim3((unsigned)(P.B * P.Hv), blocks, P.segs), dim3(Plan::threads), Plan::smem, st, P);
+    return launch<true>(kernel, dim3((unsigned)(P.B * P.Hv), blocks, P.segs), dim3(Plan::threads), Plan::smem, st, P);
 }
 
 // Start states of the segments from their end states and transitions, one segment after the other.  A block has 16
@@ -299,6 +300,7 @@ template <int DK, int NP, int MODE> cudaError_t scan(const ChunkParams &P, cudaS
 template <int DK>
 __global__ void __launch_bounds__(4 * DK) delta_join_kernel(const ChunkParams P)
 {
+    follow_previous();
     extern __shared__ __align__(16) float map[];            // [DK][DK + 1], row k: what state column k sends on
     __shared__ __align__(16) float S[16][DK];
     constexpr int EACH = DK / 4, LD = DK + 1;               // transition elements per thread

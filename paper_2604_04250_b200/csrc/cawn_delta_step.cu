@@ -47,6 +47,7 @@ template <class T> struct Token {
 template <class T, int LPR, int R>
 __global__ void __launch_bounds__(kStepThreads) delta_step_kernel(const DeltaParams P)
 {
+    follow_previous();
     constexpr int kRowsWarp = 32 / LPR, kRowsPass = kStepThreads / LPR, kSums = 2 * R, kHolds = LPR / kSums;
     static_assert(kHolds >= 1, "a dot product per lane");
     const int lane = threadIdx.x % LPR, row0 = blockIdx.y * (kRowsPass * R) + (threadIdx.x / 32) * kRowsWarp + (threadIdx.x % 32) / LPR;
@@ -145,8 +146,8 @@ template <class T, int LPR> cudaError_t go(const DeltaParams &P, cudaStream_t st
     const int blocks1 = (P.Dv + pass - 1) / pass, blocks4 = (P.Dv + 4 * pass - 1) / (4 * pass);
     // four rows a thread when that still gives every SM several blocks
     if (heads * blocks4 >= 4ll * sm_count())
-        return launch(delta_step_kernel<T, LPR, 4>, dim3((unsigned)heads, blocks4), dim3(kStepThreads), 0, st, P);
-    return launch(delta_step_kernel<T, LPR, 1>, dim3((unsigned)heads, blocks1), dim3(kStepThreads), 0, st, P);
+        return launch<true>(delta_step_kernel<T, LPR, 4>, dim3((unsigned)heads, blocks4), dim3(kStepThreads), 0, st, P);
+    return launch<true>(delta_step_kernel<T, LPR, 1>, dim3((unsigned)heads, blocks1), dim3(kStepThreads), 0, st, P);
 }
 
 }  // namespace

@@ -429,6 +429,7 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
 template <int DK, int NP, bool SUMMARY, int WHAT, class T>
 __global__ void __launch_bounds__((WalkPlan<DK, NP, WHAT>::threads), 1) delta_walks_kernel(const ChunkParams P)
 {
+    follow_previous();
     extern __shared__ __align__(16) unsigned char raw[];
     constexpr int VW = WalkPlan<DK, NP, WHAT>::VW;
     const int back = WHAT == FORWARD ? 0 : (P.Dv + VW - 1) / VW;        // the reverse walk's blocks come first

@@ -37,6 +37,7 @@ __device__ __forceinline__ uint4 philox(uint4 c, unsigned k0, unsigned k1)
 template <class T>
 __global__ void __launch_bounds__(256) dropout_kernel(const DropoutParams P)
 {
+    follow_previous();
     const long long block = (long long)blockIdx.x * blockDim.x + threadIdx.x, at = block * 8;
     if (at >= P.n) return;
     const unsigned long long off = P.offset + (P.offset_device != nullptr ? *P.offset_device : 0ull);
@@ -99,5 +100,5 @@ extern "C" int cawn_dropout(const cawn_dropout_params *params, const void *x, co
     P.scale = (float)(65536.0 / (65536.0 - (double)P.drop));
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const bool half = params->flags != 0;
-    return status_of(launch(half ? dropout_kernel<bf16> : dropout_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, st, P));
+    return status_of(launch<true>(half ? dropout_kernel<bf16> : dropout_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, st, P));
 }

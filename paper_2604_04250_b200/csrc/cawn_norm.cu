@@ -28,6 +28,7 @@ __device__ __forceinline__ float block_sum(float v, float *red)
 template <class T, bool BWD>
 __global__ void __launch_bounds__(kWideThreads) norm_wide_kernel(const NormParams P)
 {
+    follow_previous();
     __shared__ float red[kWideThreads / 32];
     extern __shared__ float fold[];
     const int c0 = blockIdx.y * P.M;
@@ -91,6 +92,7 @@ __global__ void __launch_bounds__(kWideThreads) norm_wide_kernel(const NormParam
 // Parameter gradients: 32 columns a block, 32 row lanes with two sums each, doubles, fixed order.
 __global__ void __launch_bounds__(1024) norm_sum_kernel(const float *part, int blocks, int C, float *gw, float *gb)
 {
+    follow_previous();
     __shared__ double sums[32][33];
     const int x = threadIdx.x % 32, lane = threadIdx.x / 32, col = blockIdx.x * 32 + x;
     double s = 0.0, t = 0.0;
@@ -150,10 +152,10 @@ int run(const cawn_norm_params *p, const Cut &c, const NormParams &P, bool bwd, 
     if (c.lpg == 0) {
         NormKernel k = half ? (bwd ? norm_wide_kernel<bf16, true> : norm_wide_kernel<bf16, false>)
                             : (bwd ? norm_wide_kernel<float, true> : norm_wide_kernel<float, false>);
-        return status_of(launch(k, dim3(c.bx, c.by), dim3(kWideThreads), sums ? (size_t)2 * P.M * sizeof(float) : 0, st, P));
+        return status_of(launch<true>(k, dim3(c.bx, c.by), dim3(kWideThreads), sums ? (size_t)2 * P.M * sizeof(float) : 0, st, P));
     }
     NormKernel k = bwd ? norm_bwd_pick(c, half, p->act) : norm_fwd_pick(c, half, p->act);
-    return status_of(launch(k, dim3(c.bx, c.by), dim3(threads_of(c)), sums ? (size_t)2 * c.TX * c.nv * c.v * sizeof(float) : 0, st, P));
+    return status_of(launch<true>(k, dim3(c.bx, c.by), dim3(threads_of(c)), sums ? (size_t)2 * c.TX * c.nv * c.v * sizeof(float) : 0, st, P));
 }
 
 }  // namespace
@@ -211,5 +213,5 @@ extern "C" int cawn_group_norm_bwd(const cawn_norm_params *params, const void *x
     P.part = sums ? static_cast<float *>(workspace) : nullptr;
     const int first = run(params, c, P, true, st);
     if (first != CAWN_OK || !sums) return first;
-    return status_of(launch(norm_sum_kernel, dim3((2 * C + 31) / 32), dim3(1024), 0, st, (const float *)P.part, c.bx, C, grad_weight, grad_bias));
+    return status_of(launch<true>(norm_sum_kernel, dim3((2 * C + 31) / 32), dim3(1024), 0, st, (const float *)P.part, c.bx, C, grad_weight, grad_bias));
 }

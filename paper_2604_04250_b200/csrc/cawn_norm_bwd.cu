@@ -10,6 +10,7 @@ namespace {
 template <class T, int LPG, int V, int NV, int ACT>
 __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormParams P)
 {
+    follow_previous();
     using U = typename UnitOf<V>::type;
     constexpr int N = UnitOf<V>::N;
     constexpr bool GATED = ACT == CAWN_NORM_ACT_GATE;
