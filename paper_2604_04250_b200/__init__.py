@@ -1,4 +1,4 @@
-"""B200-native CAWN phase accumulation (sm_100a CUDA behind a C ABI).
+"""B200-native CAWN phase accumulation, and operators for layers around it (sm_100a CUDA behind a C ABI).
 
 Importing the package is cheap and loads nothing native:
 

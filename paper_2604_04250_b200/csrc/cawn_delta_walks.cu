@@ -8,7 +8,7 @@
 // chain of products and of the instructions between them, on the SMs that have a head.  So with few heads one launch
 // runs both walks, each on SMs of its own, and those sums are left to the chunk-local kernel (12 heads, float storage:
 // 372 -> 290 us for the whole backward).  With more heads than half the SMs the two would share SMs, which gains
-// next to nothing (96 heads, both on one SM: 231 us, one after the other 2 x 127), so the forward goes first
+// next to nothing (96 heads, both on one SM: 231 us, one after the other 125 + 130), so the forward goes first
 // and the reverse walk takes those sums along, with r and the states fetched beside its tiles.
 // A block is 16 * row groups of values of one head and one direction.  Warps of their own fetch the tiles (with the
 // chain warps fetching, either walk of 96 heads took 153 us instead of 127), a chunk ahead where shared memory holds
