@@ -58,7 +58,9 @@ struct ChunkParams {
     Terms rb;                           // rb: dV itself (bfloat16), or its terms
     float *od, *rv, *rr;                // [nv][4][64]: dO.o, rb.v and rb.r over 16 values
     float *sd;                          // [nv][4]: <state after the chunk, its adjoint> over 16 values
-    bool together;                      // the two walks run side by side: rr and sd are made afterwards
+    bool together;                      // the two walks ran side by side: rr and sd are made by the chunk-local kernel
+    int rev_first, rev_heads;           // value heads whose reverse walk a launch does
+    int key_first, key_heads;           // and key heads (over all batches) of a launch of the chunk-local kernel
     const float *state_in;              // [bh][Dv][Dk], may be NULL
     float *state_out;
     const float *adj_in;                // gradient of state_out, may be NULL
@@ -515,7 +517,10 @@ cudaError_t launch_delta_scan(const ChunkParams &P, int dk, int terms, cudaStrea
 // start states of time segments (and of the adjoint's) from what the summaries left
 cudaError_t launch_delta_join(const ChunkParams &P, int dk, bool adjoint, cudaStream_t st);
 // backward: the forward's walk and the reverse one, then what is local to a chunk
-cudaError_t launch_delta_walks(const ChunkParams &P, int dk, int terms, cudaStream_t st);
+// What a launch of the backward's walks does: SUMMARY of segments in both directions; BOTH: all forward walks and the
+// reverse ones of rev_heads; FORWARD: the former; REVERSE: the latter, with the sums over both walks (rr, sd).
+enum { WALK_SUMMARY, WALK_BOTH, WALK_FORWARD, WALK_REVERSE };
+cudaError_t launch_delta_walks(const ChunkParams &P, int dk, int terms, int what, cudaStream_t st);
 cudaError_t launch_delta_grads(const ChunkParams &P, int dk, int terms, cudaStream_t st);
 
 }  // namespace cawn

@@ -8,8 +8,10 @@
 // chain of products and of the instructions between them, on the SMs that have a head.  So with few heads one launch
 // runs both walks, each on SMs of its own, and those sums are left to the chunk-local kernel (12 heads, float storage:
 // 372 -> 290 us for the whole backward).  With more heads than half the SMs the two would share SMs, which gains
-// next to nothing (96 heads, both on one SM: 231 us, one after the other 125 + 130), so the forward goes first
-// and the reverse walk takes those sums along, with r and the states fetched beside its tiles.
+// next to nothing (96 heads, both on one SM: 231 us, one after the other 125 + 130), so the forward goes first,
+// on the SMs that it leaves idle the reverse walks of some heads, and the other heads' reverse walks after it, which
+// take those sums along, with r and the states fetched beside their tiles; the SMs that these leave idle make the first
+// heads' gradients (whole backward of 96 heads, 2048 tokens: 407 -> 367 us).
 // A block is 16 * row groups of values of one head and one direction.  Warps of their own fetch the tiles (with the
 // chain warps fetching, either walk of 96 heads took 153 us instead of 127), a chunk ahead where shared memory holds
 // two sets; else the tiles that a chunk starts with come a chunk ahead and the others when it starts.
@@ -132,7 +134,7 @@ template <class Plan> __device__ __forceinline__ void late_tiles(bool walks)
 // SUMMARY: what a segment's own tokens leave at its end (forward; with the transitions, which are the walk of the
 // identity's rows with V = 0) or send to its start (reverse).
 template <int DK, int NP, bool SUMMARY, int WHAT>
-__device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char *raw, int block)
+__device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char *raw, int bh, int block)
 {
     using Plan = WalkPlan<DK, NP, WHAT>;
     using Early = typename Plan::Tiles::FwdEarly;
@@ -140,7 +142,7 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
     using Late = typename Plan::Tiles::FwdLate;
     auto stage = [&](int i) -> Early & { return reinterpret_cast<Early *>(raw)[i % Plan::early]; };
     auto stage_late = [&](int i) -> Late & { return reinterpret_cast<Late *>(raw + Plan::early * sizeof(Early))[i % Plan::late]; };
-    const int bh = blockIdx.x, seg = blockIdx.z, vblks = (P.Dv + VW - 1) / VW;
+    const int seg = blockIdx.z, vblks = (P.Dv + VW - 1) / VW;
     const bool ident = SUMMARY && block >= vblks;
     const int r0 = (block - (ident ? vblks : 0)) * VW, vcols = ident ? 0 : (P.Dv - r0 < VW ? P.Dv - r0 : VW);
     const int c0 = seg * P.seg_chunks, c1 = c0 + P.seg_chunks < P.chunks ? c0 + P.seg_chunks : P.chunks, count = c1 - c0;
@@ -257,7 +259,7 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
 }
 
 template <int DK, int NP, bool SUMMARY, int WHAT, class T>
-__device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char *raw, int block)
+__device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char *raw, int bh, int block)
 {
     using Plan = WalkPlan<DK, NP, WHAT>;
     using Early = typename Plan::Tiles::RevEarly;
@@ -265,7 +267,7 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
     using Late = typename Plan::Late;
     auto stage = [&](int i) -> Early & { return reinterpret_cast<Early *>(raw)[i % Plan::early]; };
     auto stage_late = [&](int i) -> Late & { return reinterpret_cast<Late *>(raw + Plan::early * sizeof(Early))[i % Plan::late]; };
-    const int bh = blockIdx.x, seg = blockIdx.z, r0 = block * VW, vcols = P.Dv - r0 < VW ? P.Dv - r0 : VW;
+    const int seg = blockIdx.z, r0 = block * VW, vcols = P.Dv - r0 < VW ? P.Dv - r0 : VW;
     const int c0 = seg * P.seg_chunks, c1 = c0 + P.seg_chunks < P.chunks ? c0 + P.seg_chunks : P.chunks, count = c1 - c0;
     const int lane = threadIdx.x % 32, w = threadIdx.x / 32, gr = lane / 4, tc = lane % 4 * 2, w4 = (r0 / 16 + w) % 4;
     const bool walks = w < Plan::RG;
@@ -432,9 +434,9 @@ __global__ void __launch_bounds__((WalkPlan<DK, NP, WHAT>::threads), 1) delta_wa
     follow_previous();
     extern __shared__ __align__(16) unsigned char raw[];
     constexpr int VW = WalkPlan<DK, NP, WHAT>::VW;
-    const int back = WHAT == FORWARD ? 0 : (P.Dv + VW - 1) / VW;        // the reverse walk's blocks come first
-    if (WHAT != FORWARD && (int)blockIdx.y < back) reverse_walk<DK, NP, SUMMARY, WHAT, T>(P, raw, blockIdx.y);
-    else if (WHAT != REVERSE) forward_walk<DK, NP, SUMMARY, WHAT>(P, raw, blockIdx.y - back);
+    const int back = WHAT == FORWARD ? 0 : P.rev_heads * ((P.Dv + VW - 1) / VW), at = (int)blockIdx.x - back;    // reverse walks come first
+    if (WHAT != FORWARD && at < 0) reverse_walk<DK, NP, SUMMARY, WHAT, T>(P, raw, P.rev_first + (int)blockIdx.x % P.rev_heads, (int)blockIdx.x / P.rev_heads);
+    else if (WHAT != REVERSE) forward_walk<DK, NP, SUMMARY, WHAT>(P, raw, at % (P.B * P.Hv), at / (P.B * P.Hv));
 }
 
 template <int DK, int NP, bool SUMMARY, int WHAT> cudaError_t walks(const ChunkParams &P, cudaStream_t st)
@@ -445,29 +447,22 @@ template <int DK, int NP, bool SUMMARY, int WHAT> cudaError_t walks(const ChunkP
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan::smem);
     if (e != cudaSuccess) return e;
     const int vblks = (P.Dv + Plan::VW - 1) / Plan::VW, ident = SUMMARY ? (P.Dk + Plan::VW - 1) / Plan::VW : 0;
-    return launch(kernel, dim3((unsigned)(P.B * P.Hv), (WHAT == BOTH ? 2 : 1) * vblks + ident, P.segs), dim3(Plan::threads), Plan::smem, st, P);
+    const unsigned blocks = (WHAT == FORWARD ? 0u : (unsigned)P.rev_heads * vblks) + (WHAT == REVERSE ? 0u : (unsigned)(P.B * P.Hv) * (vblks + ident));
+    return launch(kernel, dim3(blocks, 1, P.segs), dim3(Plan::threads), Plan::smem, st, P);
 }
 
-template <int DK, int NP> cudaError_t run(const ChunkParams &P, cudaStream_t st)
+template <int DK, int NP> cudaError_t run(const ChunkParams &P, int what, cudaStream_t st)
 {
-    if (!P.together) {
-        const cudaError_t e = walks<DK, NP, false, FORWARD>(P, st);
-        return e == cudaSuccess ? walks<DK, NP, false, REVERSE>(P, st) : e;
-    }
-    if (P.segs > 1) {
-        cudaError_t e = walks<DK, NP, true, BOTH>(P, st);
-        if (e == cudaSuccess) e = launch_delta_join(P, DK, true, st);
-        if (e != cudaSuccess) return e;
-    }
-    return walks<DK, NP, false, BOTH>(P, st);
+    return what == WALK_SUMMARY ? walks<DK, NP, true, BOTH>(P, st) : what == WALK_BOTH ? walks<DK, NP, false, BOTH>(P, st)
+         : what == WALK_FORWARD ? walks<DK, NP, false, FORWARD>(P, st) : walks<DK, NP, false, REVERSE>(P, st);
 }
 
 }  // namespace
 
-cudaError_t launch_delta_walks(const ChunkParams &P, int dk, int terms, cudaStream_t st)
+cudaError_t launch_delta_walks(const ChunkParams &P, int dk, int terms, int what, cudaStream_t st)
 {
-    if (dk == 64) return terms == 1 ? run<64, 1>(P, st) : run<64, 3>(P, st);
-    return terms == 1 ? run<128, 1>(P, st) : run<128, 3>(P, st);
+    if (dk == 64) return terms == 1 ? run<64, 1>(P, what, st) : run<64, 3>(P, what, st);
+    return terms == 1 ? run<128, 1>(P, what, st) : run<128, 3>(P, what, st);
 }
 
 }  // namespace cawn

@@ -383,6 +383,45 @@ def test_backward_is_repeatable_and_runs_in_a_graph():
     assert all(torch.equal(want[n], out[n]) for n in want)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(12, 130, 4, 8, 64, 64), (5, 70, 6, 18, 64, 72), (14, 66, 3, 15, 32, 40), (3, 200, 16, 48, 128, 32), (9, 65, 5, 10, 96, 128),
+                                   (12, 961, 4, 8, 16, 8), (5, 1000, 6, 18, 8, 8), (13, 1024, 3, 15, 8, 8), (3, 970, 16, 16, 8, 72)], ids=str)
+def test_backward_of_many_heads(shape, dtype):
+    """More heads than half the SMs, in part more than SMs: some reverse walks run beside the forward ones."""
+    d = delta_inputs(*shape, dtype, seed=sum(shape))
+    check_grads(backward(d), reference_grads(d), dtype)
+
+
+def test_backward_of_many_heads_on_streams_and_in_a_graph():
+    """The call's second stream is forked from and joined into the caller's, also while that one is captured."""
+    d = delta_inputs(12, 1100, 4, 8, 64, 64, torch.bfloat16, seed=27)
+    want = backward(d)
+    c = {n: t.cuda() for n, t in d.items()}
+    prm = params(d)
+    side = torch.cuda.Stream()
+    out = {n: torch.empty_like(want[n]) for n in want}
+    ws = cb.new_delta_workspace(prm, cb.CAWN_DELTA_BWD)
+    call = lambda: cb.cawn_delta_rule_bwd(prm, c["q"], c["k"], c["v"], c["g"], c["beta"], c["grad_o"], out["q"], out["k"], out["v"], out["g"], out["beta"],
+                                          ws, state_in=c["state_in"], grad_state_out=c["grad_state_out"], grad_state_in=out["state_in"])
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            for t in out.values():
+                t.zero_()
+            call()
+            got = {n: t.clone() for n, t in out.items()}
+    side.synchronize()
+    assert all(torch.equal(want[n], got[n]) for n in want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for t in out.values():
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(want[n], out[n]) for n in want)
+
+
 def test_backward_without_tokens():
     d = delta_inputs(2, 0, 1, 1, 64, 64, torch.float32, seed=26)
     got = backward(d)
