@@ -174,9 +174,10 @@ def _dp(t):
     """Device (or host) pointer of a tensor / numpy array / None."""
     if t is None:
         return None
-    if hasattr(t, "data_ptr"):
+    try:
         return t.data_ptr()
-    return t.ctypes.data
+    except AttributeError:
+        return t.ctypes.data
 
 
 _current_stream = None

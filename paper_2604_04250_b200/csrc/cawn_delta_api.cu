@@ -195,6 +195,15 @@ cudaError_t get_aside(Aside **out)
     return cudaSuccess;
 }
 
+// Whether work of `st` may be forked to `other`: not while a capture that `st` does not belong to holds that one.
+bool can_fork(cudaStream_t st, cudaStream_t other)
+{
+    cudaStreamCaptureStatus mine, its;
+    unsigned long long my_id = 0, its_id = 0;
+    if (cudaStreamGetCaptureInfo(st, &mine, &my_id) != cudaSuccess || cudaStreamGetCaptureInfo(other, &its, &its_id) != cudaSuccess) return false;
+    return its == cudaStreamCaptureStatusNone || (mine == cudaStreamCaptureStatusActive && my_id == its_id);
+}
+
 __global__ void nothing_kernel(int) { follow_previous(); }
 
 // The backward behind the preparation.
@@ -211,7 +220,13 @@ cudaError_t walks_and_gradients(ChunkParams &C, const Plan &w, cudaStream_t st)
         if (e == cudaSuccess) e = launch_delta_walks(C, w.dk, w.terms, WALK_BOTH, st);
         return e == cudaSuccess ? launch_delta_grads(C, w.dk, w.terms, st) : e;
     }
-    if (w.first == 0) {
+    std::unique_lock<std::mutex> lock(g_aside_mutex, std::defer_lock);
+    Aside *a = nullptr;
+    if (w.first > 0) {
+        lock.lock();
+        if ((e = get_aside(&a)) != cudaSuccess) return e;
+    }
+    if (a == nullptr || !can_fork(st, a->stream)) {
         e = launch_delta_walks(C, w.dk, w.terms, WALK_FORWARD, st);
         if (e == cudaSuccess) e = launch_delta_walks(C, w.dk, w.terms, WALK_REVERSE, st);
         return e == cudaSuccess ? launch_delta_grads(C, w.dk, w.terms, st) : e;
@@ -220,9 +235,6 @@ cudaError_t walks_and_gradients(ChunkParams &C, const Plan &w, cudaStream_t st)
     ChunkParams first = C;
     first.rev_heads = w.first * rep; first.key_heads = w.first; first.together = true;
     C.rev_first = w.first * rep; C.rev_heads = heads - w.first * rep; C.key_first = w.first; C.key_heads = keys - w.first;
-    std::lock_guard<std::mutex> lock(g_aside_mutex);
-    Aside *a = nullptr;
-    if ((e = get_aside(&a)) != cudaSuccess) return e;
     if ((e = launch_delta_walks(first, w.dk, w.terms, WALK_BOTH, st)) != cudaSuccess) return e;
     if ((e = cudaEventRecord(a->fork, st)) != cudaSuccess) return e;
     if ((e = cudaStreamWaitEvent(a->stream, a->fork, 0)) != cudaSuccess) return e;

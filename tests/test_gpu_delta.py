@@ -422,6 +422,34 @@ def test_backward_of_many_heads_on_streams_and_in_a_graph():
     assert all(torch.equal(want[n], out[n]) for n in want)
 
 
+def test_backward_of_many_heads_while_a_capture_is_open():
+    """A capture that has taken the call's second stream in does not keep another stream from calling."""
+    d = delta_inputs(12, 1100, 4, 8, 16, 16, torch.bfloat16, seed=28)
+    want = backward(d)
+    c = {n: t.cuda() for n, t in d.items()}
+    prm = params(d)
+    outs = [{n: torch.zeros_like(want[n]) for n in want} for _ in range(2)]
+    spaces = [cb.new_delta_workspace(prm, cb.CAWN_DELTA_BWD) for _ in range(2)]
+
+    def call(out, ws):
+        cb.cawn_delta_rule_bwd(prm, c["q"], c["k"], c["v"], c["g"], c["beta"], c["grad_o"], out["q"], out["k"], out["v"], out["g"], out["beta"],
+                               ws, state_in=c["state_in"], grad_state_out=c["grad_state_out"], grad_state_in=out["state_in"])
+
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, capture_error_mode="relaxed"):
+        call(outs[0], spaces[0])
+        with torch.cuda.stream(other):
+            call(outs[1], spaces[1])
+        call(outs[0], spaces[0])
+    graph.replay()
+    torch.cuda.synchronize()
+    for out in outs:
+        for n in want:
+            close(out[n], want[n], 2e-6 if want[n].dtype == torch.float32 else 4e-3, n)      # the sums over both walks in another order
+
+
 def test_backward_without_tokens():
     d = delta_inputs(2, 0, 1, 1, 64, 64, torch.float32, seed=26)
     got = backward(d)
