@@ -13,7 +13,7 @@
 // a state row s as s <- s M + l, so a first pass computes each segment's M (the same walk over the rows
 // of the identity with V = 0) and l (from a zero state); a small kernel chains them to every segment's
 // start state, and the output pass runs all segments side by side.  12 heads x 32768 tokens in 12 segments: 132 us for
-// the first pass, 22 for the chaining, 93 for the outputs; in one segment the walk took 1.5 ms.
+// the first pass, 18 for the chaining, 93 for the outputs; in one segment the walk took 1.5 ms.
 #include "cawn_delta_chunk.cuh"
 
 #include <type_traits>
@@ -298,67 +298,81 @@ template <int DK, int NP, int MODE> cudaError_t scan(const ChunkParams &P, cudaS
 }
 
 // Start states of the segments from their end states and transitions, one segment after the other.  A block has 16
-// rows of one head's state, a thread four rows of one column; the next transition is on its way (in registers)
-// while the current one is multiplied from shared memory.  Float arithmetic: a few products per segment, once, are
-// not worth the tensor cores.  Adjoints (second grid layer): last segment first, with the transposed transitions.
+// rows of one head's state, a thread four rows of one column; the next two transitions are on their way to shared memory
+// while one is multiplied (in registers on the way, and one ahead: 22 us for 12 heads x 12 segments, now 18).  Float
+// arithmetic: a few products per segment, once, are not worth the tensor cores.  Adjoints (second grid layer): last
+// segment first, with the transposed transitions.
+constexpr int kMaps = 3;
+template <int DK> constexpr int kMapLd = DK + 4;         // rows of whole 16-byte words that eight lanes read without conflicts
+
 template <int DK>
 __global__ void __launch_bounds__(4 * DK) delta_join_kernel(const ChunkParams P)
 {
     follow_previous();
-    extern __shared__ __align__(16) float map[];            // [DK][DK + 1], row k: what state column k sends on
-    __shared__ __align__(16) float S[16][DK];
-    constexpr int EACH = DK / 4, LD = DK + 1;               // transition elements per thread
+    extern __shared__ __align__(16) float maps[];           // [kMaps][DK][kMapLd], row k: what state column k sends on
+    __shared__ __align__(16) float S[2][16][DK];
+    constexpr int LD = kMapLd<DK>, WORDS = DK / 4;
     const bool adjoint = blockIdx.z == 1;
     const float *first = adjoint ? P.adj_in : P.state_in, *ends = adjoint ? P.adj_end : P.seg_end;
     float *starts = adjoint ? P.adj_start : P.seg_start;
     const int col = threadIdx.x % DK, part = threadIdx.x / DK, bh = blockIdx.x, r0 = blockIdx.y * 16 + 4 * part;
     const long long rows = (long long)P.Dv * P.Dk;
     const bool in = col < P.Dk;
-    float s[4], end[4], m[EACH];
+    float s[4], end[4];
     auto place = [&](int n) { return (long long)bh * P.segs + (adjoint ? P.segs - 1 - n : n); };
-    auto fetch = [&](int n) {
-        const long long seg = place(n);
-        const float *from = P.seg_map + seg * P.Dk * P.Dk;
+    auto fetch_map = [&](int n) {
+        if (n + 1 < P.segs) {
+            const float *from = P.seg_map + place(n) * P.Dk * P.Dk;
+            const unsigned to = smem_addr(maps + n % kMaps * (DK * LD));
 #pragma unroll
-        for (int i = 0; i < EACH; i++) {
-            const int k = 4 * i + part;
-            m[i] = in && k < P.Dk ? from[(long long)k * P.Dk + col] : 0.f;
+            for (int i = threadIdx.x; i < DK * WORDS; i += 4 * DK) {
+                const int k = i / WORDS, c = i % WORDS * 4;
+                const bool ok = k < P.Dk && c < P.Dk;
+                cp16(to + (k * LD + c) * 4, ok ? from + (long long)k * P.Dk + c : from, ok);
+            }
         }
-#pragma unroll
-        for (int i = 0; i < 4; i++) end[i] = in && r0 + i < P.Dv ? ends[seg * rows + (long long)(r0 + i) * P.Dk + col] : 0.f;
+        cp_commit();                    // possibly empty, which keeps the count
     };
+    auto fetch_end = [&](int n) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) end[i] = in && r0 + i < P.Dv ? ends[place(n) * rows + (long long)(r0 + i) * P.Dk + col] : 0.f;
+    };
+    fetch_map(0);
+    fetch_map(1);
 #pragma unroll
     for (int i = 0; i < 4; i++) s[i] = in && r0 + i < P.Dv && first != nullptr ? first[bh * rows + (long long)(r0 + i) * P.Dk + col] : 0.f;
-    fetch(0);
+    fetch_end(0);
     for (int n = 0; n < P.segs; n++) {
-        const long long seg = place(n);
+        float(&now)[16][DK] = S[n % 2];
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            if (in && r0 + i < P.Dv) starts[seg * rows + (long long)(r0 + i) * P.Dk + col] = s[i];
-            S[4 * part + i][col] = s[i];
+            if (in && r0 + i < P.Dv) starts[place(n) * rows + (long long)(r0 + i) * P.Dk + col] = s[i];
+            now[4 * part + i][col] = s[i];
             s[i] = end[i];
         }
         if (n + 1 == P.segs) break;
-#pragma unroll
-        for (int i = 0; i < EACH; i++) map[adjoint ? col * LD + 4 * i + part : (4 * i + part) * LD + col] = m[i];
-        __syncthreads();
-        fetch(n + 1);
+        cp_wait<1>();
+        __syncthreads();                // this transition and the rows are here, everyone is done with the one before
+        fetch_map(n + 2);
+        fetch_end(n + 1);
+        const float *map = maps + n % kMaps * (DK * LD);
 #pragma unroll 4
         for (int k = 0; k < DK; k += 4) {
-            const float a = map[k * LD + col], b = map[(k + 1) * LD + col], c = map[(k + 2) * LD + col], d = map[(k + 3) * LD + col];
+            float4 m;
+            if (adjoint) m = *reinterpret_cast<const float4 *>(&map[col * LD + k]);
+            else m = make_float4(map[k * LD + col], map[(k + 1) * LD + col], map[(k + 2) * LD + col], map[(k + 3) * LD + col]);
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                const float4 x = *reinterpret_cast<const float4 *>(&S[4 * part + i][k]);
-                s[i] = fmaf(x.x, a, fmaf(x.y, b, fmaf(x.z, c, fmaf(x.w, d, s[i]))));
+                const float4 x = *reinterpret_cast<const float4 *>(&now[4 * part + i][k]);
+                s[i] = fmaf(x.x, m.x, fmaf(x.y, m.y, fmaf(x.z, m.z, fmaf(x.w, m.w, s[i]))));
             }
         }
-        __syncthreads();
     }
 }
 
 template <int DK> cudaError_t join(const ChunkParams &P, bool adjoint, cudaStream_t st)
 {
-    const size_t smem = DK * (DK + 1) * sizeof(float);
+    const size_t smem = kMaps * DK * kMapLd<DK> * sizeof(float);
     const cudaError_t e = cudaFuncSetAttribute(delta_join_kernel<DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     return launch(delta_join_kernel<DK>, dim3((unsigned)(P.B * P.Hv), (P.Dv + 15) / 16, adjoint ? 2 : 1), dim3(4 * DK), smem, st, P);
