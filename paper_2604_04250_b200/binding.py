@@ -342,6 +342,8 @@ def _delta_rows(params, q, k, v, o):
             continue
         if L > 1:
             raise ValueError(f"{name} {row}: batches of {L} rows lie {L * row} elements apart, the tensor's {batch}")
+        if batch < heads * width:           # a tensor expanded over the batch; 0 would say dense in the C call
+            raise ValueError(f"{name}: batches of one row of {heads * width} elements lie {batch} apart")
         if mended is None:
             mended = cawn_delta_params.from_buffer_copy(params)
         setattr(mended, name, batch)

@@ -100,6 +100,17 @@ def test_delta_rule_rows_of_tensors():
         cb._delta_rows(dense, torch.zeros(2, 9, 1, 64)[:, :5], k, v, None)
 
 
+@pytest.mark.parametrize("which", range(4))
+def test_delta_rule_one_token_expanded_over_the_batch(which):
+    """Its batch step is 0, which the C call would take as dense and read (or write) past the one row there is."""
+    import torch
+    x = [torch.zeros(4, 1, 1, 64) for _ in range(4)]
+    cb._delta_rows(cb.make_delta_params(4, 1, 1, 1, 64, 64), *x)
+    x[which] = torch.zeros(1, 1, 1, 64).expand(4, 1, 1, 64)
+    with pytest.raises(ValueError, match="qkvo"[which] + "_stride"):
+        cb._delta_rows(cb.make_delta_params(4, 1, 1, 1, 64, 64), *x)
+
+
 def test_delta_rule_backward_pointers():
     for name in ("grad_o", "grad_q", "grad_k", "grad_v", "grad_g", "grad_beta"):
         assert bwd(delta(), **{name: None}) == cb.CAWN_ERR_NULL_POINTER, name
