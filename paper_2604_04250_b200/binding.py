@@ -325,29 +325,65 @@ def make_delta_params(B, L, Hk, Hv, Dk, Dv, scale=None, flags=0, q_stride=0, k_s
                              max(Dk, 1) ** -0.5 if scale is None else scale, flags, q_stride, k_stride, v_stride, o_stride)
 
 
+def _dense(names, *arrays):
+    """What the kernels take as dense arrays has to be laid out so."""
+    for i, x in enumerate(arrays):
+        if x is not None and not getattr(x, "is_contiguous", _yes)():
+            raise ValueError(f"{names.split()[i]}: strides {tuple(x.stride())} of shape {tuple(x.shape)}, it has to be dense")
+
+
+def _yes():
+    return True
+
+
+def _check_rows(name, x, width, row):
+    """x's elements, in order, have to be rows of `width` neighbours that start `row` apart (the shape may be any that
+    has whole rows: [B, L, H, D], [B, L, H * D], [B * L, H * D])."""
+    if row == width and getattr(x, "is_contiguous", _yes)() or not hasattr(x, "stride"):
+        return
+    shape, strides = x.shape, x.stride()
+    expect, inside = 1, 1               # the step that is due, the elements of a row that the dimensions so far hold
+    for i in range(len(shape) - 1, -1, -1):
+        size = shape[i]
+        if size == 1:
+            continue
+        over = inside * size
+        if strides[i] != expect or (inside < width < over and (over % width != 0 or row != width)):
+            raise ValueError(f"{name} {row}: strides {tuple(strides)} of shape {tuple(shape)}, which are not rows of {width} "
+                             f"elements {row} apart")
+        expect *= size
+        if inside < width:
+            inside = over
+            if inside >= width:
+                expect = row * (inside // width)
+
+
 def _delta_rows(params, q, k, v, o):
-    """The params of a call whose tensors are batched [B, L, ...]: their rows must lie L strides apart from batch to
-    batch.  One token has no step to the next, so torch gives that dimension any stride (that of a slice of a
-    projection, seen as heads, is the slice's width); the step between batches is then the rows' stride."""
-    B, L = params.B, params.L
-    if B == 1 or L < 1:
+    """The params of a call whose tensors are [B, L, ...], their layout checked: rows (all heads of a token) contiguous and
+    *_stride apart, batches L strides apart.  One token has no step to the next, so torch gives that dimension any
+    stride (that of a slice of a projection, seen as heads, is the slice's width); the step between batches is then
+    the rows' stride."""
+    B, L, p = params.B, params.L, params
+    if L < 1:
         return params
-    mended = None
-    for name, x, heads, width in (("q_stride", q, params.Hk, params.Dk), ("k_stride", k, params.Hk, params.Dk),
-                                  ("v_stride", v, params.Hv, params.Dv), ("o_stride", o, params.Hv, params.Dv)):
-        if not hasattr(x, "stride") or x.dim() < 3 or x.size(0) != B or x.size(1) != L:
-            continue
-        row, batch = getattr(params, name) or heads * width, x.stride(0)
-        if batch == L * row:
-            continue
-        if L > 1:
-            raise ValueError(f"{name} {row}: batches of {L} rows lie {L * row} elements apart, the tensor's {batch}")
-        if batch < heads * width:           # a tensor expanded over the batch; 0 would say dense in the C call
-            raise ValueError(f"{name}: batches of one row of {heads * width} elements lie {batch} apart")
-        if mended is None:
-            mended = cawn_delta_params.from_buffer_copy(params)
-        setattr(mended, name, batch)
-    return mended or params
+    qk, vo = p.Hk * p.Dk, p.Hv * p.Dv
+    for name, x, width, row in (("q_stride", q, qk, p.q_stride), ("k_stride", k, qk, p.k_stride),
+                                ("v_stride", v, vo, p.v_stride), ("o_stride", o, vo, p.o_stride)):
+        if row == 0:
+            row = width
+        if L == 1 and B > 1:
+            shape = getattr(x, "shape", ())
+            if len(shape) > 2 and shape[0] == B and shape[1] == 1:
+                batch = x.stride(0)
+                if batch < width:       # a tensor expanded over the batch; 0 would say dense in the C call
+                    raise ValueError(f"{name}: batches of one row of {width} elements lie {batch} apart")
+                if batch != row:
+                    if p is params:
+                        p = cawn_delta_params.from_buffer_copy(params)
+                    setattr(p, name, batch)
+                    row = batch
+        _check_rows(name, x, width, row)
+    return p
 
 
 def cawn_delta_rule_workspace_bytes(params, op):
@@ -368,6 +404,7 @@ def new_delta_workspace(params, op, device="cuda"):
 
 
 def cawn_delta_rule_fwd(params, q, k, v, g, beta, o, workspace, state_in=None, state_out=None, stream=None):
+    _dense("g beta state_in state_out", g, beta, state_in, state_out)
     params = _delta_rows(params, q, k, v, o)
     _check(lib().cawn_delta_rule_fwd(
         ctypes.byref(params), _dp(q), _dp(k), _dp(v), _dp(g), _dp(beta), _dp(state_in), _dp(o), _dp(state_out),
@@ -375,6 +412,7 @@ def cawn_delta_rule_fwd(params, q, k, v, g, beta, o, workspace, state_in=None, s
 
 
 def cawn_delta_rule_step(params, q, k, v, g, beta, o, state_in=None, state_out=None, stream=None):
+    _dense("g beta state_in state_out", g, beta, state_in, state_out)
     params = _delta_rows(params, q, k, v, o)
     _check(lib().cawn_delta_rule_step(
         ctypes.byref(params), _dp(q), _dp(k), _dp(v), _dp(g), _dp(beta), _dp(state_in), _dp(o), _dp(state_out),
@@ -383,6 +421,8 @@ def cawn_delta_rule_step(params, q, k, v, g, beta, o, state_in=None, state_out=N
 
 def cawn_delta_rule_bwd(params, q, k, v, g, beta, grad_o, grad_q, grad_k, grad_v, grad_g, grad_beta, workspace,
                         state_in=None, grad_state_out=None, grad_state_in=None, stream=None):
+    _dense("g beta state_in grad_state_out grad_q grad_k grad_v grad_g grad_beta grad_state_in",
+           g, beta, state_in, grad_state_out, grad_q, grad_k, grad_v, grad_g, grad_beta, grad_state_in)
     params = _delta_rows(params, q, k, v, grad_o)
     _check(lib().cawn_delta_rule_bwd(
         ctypes.byref(params), _dp(q), _dp(k), _dp(v), _dp(g), _dp(beta), _dp(state_in), _dp(grad_o),
@@ -405,13 +445,25 @@ def new_norm_workspace(params, device="cuda"):
     return _plain_workspace(cawn_group_norm_workspace_bytes(params), device)
 
 
+def _norm_rows(params, x, gate):
+    if params.N > 0:
+        width = params.G * params.M
+        _check_rows("x_stride", x, width, params.x_stride or width)
+        if gate is not None:
+            _check_rows("gate_stride", gate, width, params.gate_stride or width)
+
+
 def cawn_group_norm_fwd(params, x, y, weight=None, bias=None, gate=None, stream=None):
+    _dense("y weight bias", y, weight, bias)
+    _norm_rows(params, x, gate)
     _check(lib().cawn_group_norm_fwd(ctypes.byref(params), _dp(x), _dp(weight), _dp(bias), _dp(gate), _dp(y),
                                      _stream(stream)), "cawn_group_norm_fwd")
 
 
 def cawn_group_norm_bwd(params, x, grad_y, grad_x, workspace=None, weight=None, bias=None, gate=None, grad_gate=None,
                         grad_weight=None, grad_bias=None, stream=None):
+    _dense("grad_y grad_x weight bias grad_gate grad_weight grad_bias", grad_y, grad_x, weight, bias, grad_gate, grad_weight, grad_bias)
+    _norm_rows(params, x, gate)
     n = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib().cawn_group_norm_bwd(
         ctypes.byref(params), _dp(x), _dp(weight), _dp(bias), _dp(gate), _dp(grad_y), _dp(grad_x), _dp(grad_gate),
@@ -423,5 +475,6 @@ def make_dropout_params(n, p, seed, offset=0, flags=0):
 
 
 def cawn_dropout(params, x, y, residual=None, offset_device=None, stream=None):
+    _dense("x y residual", x, y, residual)
     _check(lib().cawn_dropout(ctypes.byref(params), _dp(x), _dp(residual), _dp(y), _dp(offset_device), _stream(stream)),
            "cawn_dropout")

@@ -111,6 +111,70 @@ def test_delta_rule_one_token_expanded_over_the_batch(which):
         cb._delta_rows(cb.make_delta_params(4, 1, 1, 1, 64, 64), *x)
 
 
+def test_delta_rule_layouts():
+    """Whatever the batch, rows that are not as the params say and arrays that are not dense are refused."""
+    import torch
+    B, L, H, D = 2, 5, 3, 64
+    dense = lambda B=B: torch.zeros(B, L, H, D)
+    make = lambda B=B, **kw: cb.make_delta_params(B, L, H, H, D, D, **kw)
+    heads_first = torch.zeros(B, H, L, D).transpose(1, 2)                   # its batch step is that of L rows
+    projection = torch.zeros(1, L, 3 * H * D)
+    part = projection.split(H * D, -1)[1].unflatten(-1, (H, D))
+    wide = projection.shape[-1]
+    for i, name in enumerate(("q_stride", "k_stride", "v_stride", "o_stride")):
+        def rows(x, params, B=B):
+            t = [dense(B) for _ in range(4)]
+            t[i] = x
+            return cb._delta_rows(params, *t)
+        rows(dense(), make())
+        rows(dense().flatten(2), make())
+        rows(dense().flatten(0, 1), make())
+        rows(dense().flatten(), make())
+        rows(part, make(1, **{name: wide}), 1)
+        rows(part.flatten(2), make(1, **{name: wide}), 1)
+        rows(part.flatten(0, 1), make(1, **{name: wide}), 1)
+        for x, params, b in ((heads_first, make(), B), (heads_first[:1], make(1), 1), (part, make(1), 1), (part[0], make(1), 1),
+                             (dense(1), make(1, **{name: wide}), 1), (dense(1).flatten(), make(1, **{name: wide}), 1),
+                             (dense().transpose(2, 3).contiguous().transpose(2, 3), make(), B), (dense()[..., ::2].repeat_interleave(2, 3).mT, make(), B),
+                             (torch.zeros(B, 1, H, D).expand(B, L, H, D), make(), B)):
+            with pytest.raises(ValueError, match=name):
+                rows(x, params, b)
+    halves = torch.zeros(B, L, 2 * H).chunk(2, -1)[0]                        # as a projection to decays and betas leaves them
+    # every array of every call is looked at, before anything else
+    calls = {cb.cawn_delta_rule_fwd: ("g", "beta", "state_in", "state_out"), cb.cawn_delta_rule_step: ("g", "beta", "state_in", "state_out"),
+             cb.cawn_delta_rule_bwd: ("g", "beta", "state_in", "grad_state_out", "grad_q", "grad_k", "grad_v", "grad_g", "grad_beta", "grad_state_in")}
+    import inspect
+    for call, names in calls.items():
+        for name in names:
+            kw = {n: dense() for n, p in inspect.signature(call).parameters.items() if p.default is p.empty}
+            kw.update(params=make(), **{name: halves})
+            with pytest.raises(ValueError, match=name):
+                call(**kw)
+
+
+def test_norm_and_dropout_layouts():
+    import torch
+    N, C = 6, 128
+    x, wide = torch.zeros(N, C), torch.zeros(N, 3 * C)[:, C:2 * C]
+    prm, strided = cb.make_norm_params(N, 2, 64), cb.make_norm_params(N, 2, 64, x_stride=3 * C, gate_stride=3 * C)
+    cb._norm_rows(prm, x, x)
+    cb._norm_rows(prm, x.view(2, 3, 2, 64), None)
+    cb._norm_rows(strided, wide, wide.unflatten(0, (2, 3)))
+    for p, a, g, name in ((prm, wide, None, "x_stride"), (prm, x, wide, "gate_stride"), (strided, x, wide, "x_stride"), (strided, wide, x, "gate_stride"),
+                          (prm, torch.zeros(C, N).T, None, "x_stride")):
+        with pytest.raises(ValueError, match=name):
+            cb._norm_rows(p, a, g)
+    for name in ("y", "weight", "bias"):
+        with pytest.raises(ValueError, match=name):
+            cb.cawn_group_norm_fwd(prm, x, **{"y": x, name: wide})
+    for name in ("grad_y", "grad_x", "grad_gate", "grad_weight", "grad_bias", "weight", "bias"):
+        with pytest.raises(ValueError, match=name):
+            cb.cawn_group_norm_bwd(prm, x, **{"grad_y": x, "grad_x": x, name: wide})
+    for name in ("x", "y", "residual"):
+        with pytest.raises(ValueError, match=name):
+            cb.cawn_dropout(cb.make_dropout_params(N * C, 0.1, 0), **{"x": x, "y": x, name: wide})
+
+
 def test_delta_rule_backward_pointers():
     for name in ("grad_o", "grad_q", "grad_k", "grad_v", "grad_g", "grad_beta"):
         assert bwd(delta(), **{name: None}) == cb.CAWN_ERR_NULL_POINTER, name
