@@ -155,7 +155,12 @@ int run(const cawn_norm_params *p, const Cut &c, const NormParams &P, bool bwd, 
         return status_of(launch<true>(k, dim3(c.bx, c.by), dim3(kWideThreads), sums ? (size_t)2 * P.M * sizeof(float) : 0, st, P));
     }
     NormKernel k = bwd ? norm_bwd_pick(c, half, p->act) : norm_fwd_pick(c, half, p->act);
-    return status_of(launch<true>(k, dim3(c.bx, c.by), dim3(threads_of(c)), sums ? (size_t)2 * c.TX * c.nv * c.v * sizeof(float) : 0, st, P));
+    const size_t fold = sums ? (size_t)2 * c.TX * c.nv * c.v * sizeof(float) : 0;     // up to 64 KB: 256 slots of 32 channels
+    if (fold > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)fold);
+        if (e != cudaSuccess) return status_of(e);
+    }
+    return status_of(launch<true>(k, dim3(c.bx, c.by), dim3(threads_of(c)), fold, st, P));
 }
 
 }  // namespace

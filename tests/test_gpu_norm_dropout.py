@@ -82,6 +82,16 @@ def test_norm(shape, act, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("act", sorted(ACTS))
+@pytest.mark.parametrize("shape", [(5, 8, 1024), (3, 7, 520), (40, 9, 768)], ids=str)
+def test_norm_many_wide_groups(shape, act, dtype):
+    """A thread holds 32 channels and a block 224 or 256 threads: the sums of the parameters' gradients take more than
+    the 48 KB of shared memory that a launch gets unasked."""
+    d, prm = norm_case(*shape, dtype, act, seed=sum(shape))
+    check_norm(d, prm, dtype, False, act)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("pad", [0, 8, 3])
 @pytest.mark.parametrize("affine", [True, False])
 def test_norm_rms_strided(affine, pad, dtype):
