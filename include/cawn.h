@@ -74,7 +74,11 @@ enum {
     CAWN_FLAG_RETENTION_DYNAMIC  = 1u << 1, /* gamma_t = sigmoid(gamma_logit[b,t,h] + freq_bias[k]) */
     CAWN_FLAG_INPUT_INDEPENDENT  = 1u << 2, /* forward: the caller vouches that `input`, gamma, theta
                                                (and the conv weights) are not written by the call
-                                               made just before this one on the same stream.  The
+                                               made just before this one on the same stream, nor, where
+                                               that one has this flag too, by the call before it, and so
+                                               on back to and including the last call without it (any
+                                               of the library's calls; other work in between ends the
+                                               chain).  The
                                                kernels are launched so that a call may start while the
                                                previous one drains (programmatic dependent launch);
                                                with this flag the new call also fetches its input rows

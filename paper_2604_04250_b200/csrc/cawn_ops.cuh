@@ -129,10 +129,12 @@ inline cudaError_t launch(void (*kernel)(A...), dim3 grid, dim3 block, size_t sm
     cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = st; cfg.attrs = &attr; cfg.numAttrs = EARLY ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kernel, A(args)...);
 }
+// The wait comes first: a launch behind this one may read before its own wait what the caller says this one does not
+// write (CAWN_FLAG_INPUT_INDEPENDENT), and that has to be complete by then, whoever wrote it.
 __device__ __forceinline__ void follow_previous()
 {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
 // SMs of the current device, read once per device.

@@ -176,8 +176,12 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void *src)
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"(dst), "l"(src) : "memory");
 }
 // Programmatic dependent launch: let the next launch on the stream start filling SMs as soon as
-// every CTA of this one is running, and wait for the previous launch (and its memory) to be
-// complete.  Both are no-ops for a launch made without the programmatic attribute.
+// every CTA of this one has said so, and wait for the previous launch (and its memory) to be
+// complete.  Both are no-ops for a launch made without the programmatic attribute.  The next launch
+// may read its input before its own wait, so a launch that does not do so itself lets it start
+// only after having waited: what was written before this launch is then complete.  One that
+// fetches early lets it start at once, which is why the caller's promise reaches back over
+// consecutive calls with CAWN_FLAG_INPUT_INDEPENDENT.
 __device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_wait_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
@@ -337,6 +341,7 @@ __device__ __forceinline__ void scan_tile(const ScanParams &prm, ScanSmem<T, W, 
     const bool wait_first = KIND == KIND_FUSED && early && prm.first_wave > 0 &&
         (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x >= (unsigned)prm.first_wave;
     if (!early || wait_first) grid_wait_previous();
+    if (!early) grid_launch_dependents();
     // Reverse kinds (they have waited already) and the fused forward: the thread that later builds
     // channel tid's coefficients asks for its gamma and theta now, and thread 0 for the epoch (the
     // fused forward: once it has waited, below), so that the answers travel while the tile's
@@ -1537,7 +1542,7 @@ __global__ void __launch_bounds__(W * 32, MINB) cawn_scan_kernel(const ScanParam
     // (smaller k) always have smaller linear block indices
     const int g = blockIdx.x, b = blockIdx.y;
     const int k = blockIdx.z;                         // tile index along (logical) time
-    grid_launch_dependents();
+    if (!kind_is_bwd(KIND) && prm.early_loads != 0) grid_launch_dependents();
     const bool full = ((long long)(k + 1) * TILE <= prm.L) && (g * 64 + 64 <= prm.C);
     if (full) scan_tile<T, W, KIND, VEC, DYN, true, EAR, IO, MASKED, LATE>(prm, sm, g, b, k);
     else      scan_tile<T, W, KIND, VEC, DYN, false, EAR, IO, MASKED, LATE>(prm, sm, g, b, k);

@@ -158,10 +158,10 @@ __device__ __forceinline__ void seam_rows(const EpilogueParams &ep, int c, int k
 __global__ void __launch_bounds__(kEpiWarps * 32) cawn_bwd_epilogue_kernel(const EpilogueParams ep)
 {
     __shared__ double sh[kEpiWarps * 5 * 32];
-    // launched with programmatic stream serialisation behind the reverse scan: let the launch after
-    // this one start filling SMs, and touch nothing before the scan is complete
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // launched with programmatic stream serialisation behind the reverse scan: touch nothing before the
+    // scan is complete, and only then let the launch after this one start (it may read before its own wait)
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     int blk = blockIdx.x;
     const int C = ep.C, nparts = ep.nparts;

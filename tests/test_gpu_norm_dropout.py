@@ -229,3 +229,44 @@ def test_dropout_counter_beyond_32_bits_of_words():
     y = torch.empty(n, device="cuda")
     cb.cawn_dropout(cb.make_dropout_params(n, 0.5, 1, 1 << 40), torch.ones(n, device="cuda"), y)
     assert np.array_equal((y != 0).cpu().numpy(), philox_bits(n, 1, 1 << 40) >= 32768)
+
+
+@pytest.mark.parametrize("between", ["dropout", "norm", "delta step", "scan"])
+@pytest.mark.parametrize("writer", ["norm", "dropout", "scan"])
+def test_an_independent_input_written_two_calls_before(writer, between):
+    """CAWN_FLAG_INPUT_INDEPENDENT says that the call just before does not write the input.  The one before that may:
+    it has to be complete when the scan fetches its rows."""
+    B, L, C, n = 8, 2048, 768, 4
+    rng = torch.Generator(device="cuda").manual_seed(9)
+    randn = lambda *s: torch.randn(*s, generator=rng, device="cuda")
+    xs = [randn(B * L, 2 * C) for _ in range(n)]
+    gamma, theta = torch.full((C,), 0.9, device="cuda"), torch.rand(C, generator=rng, device="cuda")
+    p, small, y = torch.empty(B, L, C, dtype=torch.complex64, device="cuda"), randn(4096), torch.empty(4096, device="cuda")
+    state, q = torch.zeros(1, 1, 64, 64, device="cuda"), randn(1, 1, 1, 64)
+    one, o = torch.ones(1, 1, 1, device="cuda"), torch.empty(1, 1, 1, 64, device="cuda")
+    little = torch.view_as_complex(randn(1, 64, 64, 2))
+    little_y, little_prm = torch.empty_like(little), cb.make_params(1, 64, 1, 64)
+    little_ws = cb.new_workspace(little_prm, cb.CAWN_OP_FWD)
+    flat, plain = torch.view_as_real(p).view(B * L, 2 * C), cb.make_params(B, L, 12, 64)
+    plain_ws = cb.new_workspace(plain, cb.CAWN_OP_FWD)
+    first = {"norm": lambda x: cb.cawn_group_norm_fwd(cb.make_norm_params(B * L, 1, 2 * C), x, flat),
+             "dropout": lambda x: cb.cawn_dropout(cb.make_dropout_params(x.numel(), 0.1, 3), x, flat),
+             "scan": lambda x: cb.cawn_phase_accumulate_fwd(plain, torch.view_as_complex(x.view(B, L, C, 2)), gamma, theta, p, plain_ws)}[writer]
+    second = {"dropout": lambda: cb.cawn_dropout(cb.make_dropout_params(4096, 0.1, 3), small, y),
+              "norm": lambda: cb.cawn_group_norm_fwd(cb.make_norm_params(64, 1, 64), small, y),
+              "delta step": lambda: cb.cawn_delta_rule_step(cb.make_delta_params(1, 1, 1, 1, 64, 64), q, q, q, -one, one, o, state, state),
+              "scan": lambda: cb.cawn_phase_accumulate_fwd(little_prm, little, gamma[:64], theta[:64], little_y, little_ws)}[between]
+    outs = []
+    for flags in (0, cb.CAWN_FLAG_INPUT_INDEPENDENT):
+        prm = cb.make_params(B, L, 12, 64, flags=flags)
+        ws, ys = cb.new_workspace(prm, cb.CAWN_OP_FWD), [torch.empty_like(p) for _ in range(n)]
+        torch.cuda.synchronize()
+        for i in range(n):
+            first(xs[i])
+            second()
+            cb.cawn_phase_accumulate_fwd(prm, p, gamma, theta, ys[i], ws)
+            torch.cuda.synchronize()
+        assert cb.cawn_poll_status(ws) == 0
+        outs.append(ys)
+    for a, b in zip(*outs):
+        assert torch.equal(torch.view_as_real(a), torch.view_as_real(b))
