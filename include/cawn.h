@@ -530,7 +530,7 @@ CAWN_API int cawn_group_norm_fwd(const cawn_norm_params *params, const void *x,
                                  const float *weight, const float *bias, const void *gate,
                                  void *y, void *cuda_stream);
 
-/* Host-only size query for cawn_group_norm_bwd. */
+/* Host-only size query for cawn_group_norm_bwd; enough for every N up to the given one. */
 CAWN_API int cawn_group_norm_workspace_bytes(const cawn_norm_params *params, size_t *bytes);
 
 /* Backward: grad_y [N, G*M] dense -> grad_x; grad_gate (required with CAWN_NORM_ACT_GATE, NULL

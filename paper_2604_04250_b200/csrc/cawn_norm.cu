@@ -187,7 +187,7 @@ extern "C" int cawn_group_norm_workspace_bytes(const cawn_norm_params *params, s
     const int rc = check(params);
     if (rc != CAWN_OK) return rc;
     if (bytes == nullptr) return CAWN_ERR_NULL_POINTER;
-    *bytes = (size_t)cut_of(params, true).bx * 2 * params->G * params->M * sizeof(float);
+    *bytes = (size_t)cut_of(params, true).most * 2 * params->G * params->M * sizeof(float);
     return CAWN_OK;
 }
 

@@ -33,6 +33,7 @@ struct NormParams {
 // (lpg = 0: the wide kernel), TX column slots x TY row lanes per block, `bx` blocks along the rows.
 struct Cut {
     int v, lpg, nv, TX, TY, bx, by;
+    int most;                    // bx at most, for this or any smaller N: what a workspace is sized for
     long long rows;
 };
 
@@ -58,6 +59,7 @@ inline Cut cut_of(const cawn_norm_params *p, bool backward)
         const int64_t want = backward ? (int64_t)sms * 4 / p->G + 1 : p->N;
         c.bx = (int)(p->N < want ? p->N : want < 65535 * 16 ? want : 65535 * 16);
         if (c.bx < 1) c.bx = 1;
+        c.most = c.bx;
         c.rows = (p->N + c.bx - 1) / c.bx;
         return c;
     }
@@ -82,6 +84,7 @@ inline Cut cut_of(const cawn_norm_params *p, bool backward)
     const int64_t most = (p->N + c.TY - 1) / c.TY;
     if (bx > most) bx = most;
     if (bx < 1) bx = 1;
+    c.most = (int)bx;            // whole turns of the row lanes below can take fewer blocks for more rows
     c.rows = (p->N + bx - 1) / bx;
     c.rows = (c.rows + c.TY - 1) / c.TY * c.TY;
     c.bx = (int)((p->N + c.rows - 1) / (c.rows > 0 ? c.rows : 1));

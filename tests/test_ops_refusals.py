@@ -213,6 +213,14 @@ def test_group_norm_refusals():
     assert cb.lib().cawn_group_norm_workspace_bytes(ref(ok), None) == cb.CAWN_ERR_NULL_POINTER
 
 
+@pytest.mark.parametrize("flags", [0, cb.CAWN_FLAG_INPUT_BF16 | cb.CAWN_FLAG_OUTPUT_BF16])
+@pytest.mark.parametrize("G, M", [(12, 64), (1, 768), (3, 37), (8, 1024), (40, 16), (2, 4096), (5, 2000)])
+def test_group_norm_workspace_of_the_largest_call_serves_all(G, M, flags):
+    """The size never falls as the call grows, and is what a call of its own takes."""
+    sizes = [cb.cawn_group_norm_workspace_bytes(cb.make_norm_params(N, G, M, flags=flags)) for N in [*range(3000), *range(3000, 200000, 997)]]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+
+
 def test_dropout_refusals():
     make = cb.make_dropout_params
     f = lambda prm, x=A, r=None, y=A, d=None: cb.lib().cawn_dropout(None if prm is None else ref(prm), x, r, y, d, None)
