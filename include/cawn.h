@@ -458,7 +458,7 @@ typedef struct cawn_delta_params {
 
 enum { CAWN_DELTA_FWD = 0, CAWN_DELTA_BWD = 1 };    /* `op` of cawn_delta_rule_workspace_bytes */
 
-/* Host-only size query for cawn_delta_rule_fwd / _bwd. */
+/* Host-only size query for cawn_delta_rule_fwd / _bwd; enough for every B and L up to the given ones. */
 CAWN_API int cawn_delta_rule_workspace_bytes(const cawn_delta_params *params, int op, size_t *bytes);
 
 /*

@@ -87,9 +87,13 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
     if (segs < 3 || (segs == 3 && !backward && w.chunks <= 32)) segs = 1;
     w.seg_chunks = (int)((w.chunks + segs - 1) / segs);
     w.segs = w.chunks > 0 ? (w.chunks + w.seg_chunks - 1) / w.seg_chunks : 1;
-    if (w.segs > 1) {
-        w.seg_state = part((double)p->B * p->Hv * w.segs * p->Dv * p->Dk * 4);
-        w.seg_map = part((double)p->B * p->Hv * w.segs * p->Dk * p->Dk * 4);
+    // Room for as many segments as this call or any shorter or smaller one has over all its heads, so that a workspace
+    // for the largest call serves them all: one block a segment at least, four chunks in each.
+    int64_t most = (int64_t)p->B * p->Hv * (w.chunks / 4);
+    if (most > sm_count() / (backward ? 2 : 1)) most = sm_count() / (backward ? 2 : 1);
+    if (w.chunks / 4 >= 3) {
+        w.seg_state = part((double)most * p->Dv * p->Dk * 4);
+        w.seg_map = part((double)most * p->Dk * p->Dk * 4);
     }
     const size_t nc = (size_t)p->B * p->Hv * w.chunks, rows = (size_t)p->B * p->L;
     if (w.terms == 3) {
@@ -277,7 +281,7 @@ extern "C" int cawn_delta_rule_workspace_bytes(const cawn_delta_params *params, 
     if (op != CAWN_DELTA_FWD && op != CAWN_DELTA_BWD) return CAWN_ERR_INVALID_ARG;
     if (bytes == nullptr) return CAWN_ERR_NULL_POINTER;
     if (!chunks_fit(params)) return CAWN_ERR_UNSUPPORTED;
-    *bytes = plan_of(params, op == CAWN_DELTA_BWD).total;
+    *bytes = params->L == 0 ? 0 : plan_of(params, op == CAWN_DELTA_BWD).total;
     return CAWN_OK;
 }
 

@@ -82,6 +82,20 @@ def test_delta_rule_workspace():
     assert bwd(long, ws=None) == cb.CAWN_ERR_NULL_POINTER
 
 
+@pytest.mark.parametrize("op", [cb.CAWN_DELTA_FWD, cb.CAWN_DELTA_BWD])
+@pytest.mark.parametrize("flags", [0, cb.CAWN_FLAG_INPUT_BF16 | cb.CAWN_FLAG_OUTPUT_BF16])
+@pytest.mark.parametrize("Hk, Hv, Dk, Dv", [(12, 12, 64, 64), (1, 1, 128, 128), (2, 6, 128, 64), (1, 3, 40, 72), (4, 8, 64, 96)])
+def test_delta_rule_workspace_of_the_largest_call_serves_all(Hk, Hv, Dk, Dv, flags, op):
+    """The size never falls as the call grows, in length or in batch."""
+    lengths, batches = [*range(0, 4100, 41), *range(4100, 40000, 1013)], [1, 2, 3, 4, 5, 8, 12, 13, 25, 40, 96]
+    sizes = [[cb.cawn_delta_rule_workspace_bytes(cb.make_delta_params(B, L, Hk, Hv, Dk, Dv, flags=flags), op) for L in lengths] for B in batches]
+    for row in sizes:
+        assert all(a <= b for a, b in zip(row, row[1:]))
+    for one, more in zip(sizes, sizes[1:]):
+        assert all(a <= b for a, b in zip(one, more))
+    assert all(row[0] == 0 for row in sizes)                # no tokens, nothing kept
+
+
 def test_delta_rule_rows_of_tensors():
     """Strides against the tensors they are said of: a batch step that is not L rows is refused, and one token's row
     stride, which torch leaves open, is the batch step."""
