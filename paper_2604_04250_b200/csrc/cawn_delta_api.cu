@@ -58,7 +58,7 @@ struct Plan {
     int dk, terms, chunks, vblocks, segs, seg_chunks;    // terms: of an input
     size_t q, k, v, go;                  // three bfloat16 terms each, float storage only
     size_t coef, tri, p;
-    size_t rf, sf, od, sd, u, s0, rbt;  // backward: rf also for rb, sf and s0 for the adjoints, od for the other dots
+    size_t r, s0, rbt;                  // backward: s0 also for the adjoints
     bool together;                      // backward: both walks of all heads in one launch
     int first;                          // else: key heads whose reverse walk runs beside the forward ones
     size_t seg_state, seg_map;
@@ -106,11 +106,10 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
     w.tri = part((double)nc * nt * kTri * 2);
     w.p = w.tri;
     if (backward) {
-        const double nv = (double)nc * w.vblocks, ends = (double)p->B * p->Hv * w.vblocks;
-        w.rf = part(nv * kTile * 4);
-        w.sf = part((nv + ends) * kC * w.dk * 4);
-        w.od = part(nv * 4 * kC * 4);
-        w.sd = part(nv * 4 * 4);
+        const double nv = (double)nc * w.vblocks;
+        w.r = part(nv * nt * kTile * 2);
+        w.s0 = part(nv * nt * kC * w.dk * 2);
+        w.rbt = w.terms == 3 ? w.v : part((double)rows * p->Hv * p->Dv * 2);     // bfloat16: the first of two terms is dV
         // Both walks in one launch where their blocks take an SM each.  Else the forward walks go first, and with them as
         // many reverse ones as the SMs that they leave idle in their last turn can take, where that is a quarter or
         // more and the walks are long.  Without / with, us, bfloat16 heads of 64 x 64: 96 heads (52 at once) x 2048
@@ -120,11 +119,8 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
         const int64_t one = blocks / 2, each = one / (p->B * p->Hk), idle = (one + sm_count() - 1) / sm_count() * sm_count() - one;
         const int64_t first = idle / each;
         if (!w.together && w.chunks >= 16 && first * 4 >= (int64_t)p->B * p->Hk) w.first = (int)first;
-        w.u = part(nv * w.terms * kTile * 2);
-        w.s0 = part(nv * w.terms * kC * w.dk * 2);
-        w.rbt = w.terms == 3 ? w.v : 0;
     }
-    w.total = w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + 2 * (w.rf + w.sf + w.s0) + 3 * w.od + w.sd + w.u + w.rbt + (backward ? 4 : 2) * w.seg_state + w.seg_map;
+    w.total = w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + w.r + 2 * w.s0 + w.rbt + (backward ? 4 : 2) * w.seg_state + w.seg_map;
     return w;
 }
 
@@ -214,16 +210,21 @@ __global__ void nothing_kernel(int) { follow_previous(); }
 cudaError_t walks_and_gradients(ChunkParams &C, const Plan &w, cudaStream_t st)
 {
     const int heads = C.B * C.Hv, keys = C.B * C.Hk, rep = C.Hv / C.Hk;
-    C.rev_first = 0; C.rev_heads = heads; C.key_first = 0; C.key_heads = keys; C.together = w.together;
+    C.fwd_heads = heads; C.rev_first = 0; C.rev_heads = heads; C.key_first = 0; C.key_heads = keys;
     cudaError_t e = cudaSuccess;
     if (w.together) {
         if (w.segs > 1) {
-            e = launch_delta_walks(C, w.dk, w.terms, WALK_SUMMARY, st);
+            e = launch_delta_walks(C, w.dk, w.terms, true, st);
             if (e == cudaSuccess) e = launch_delta_join(C, w.dk, true, st);
         }
-        if (e == cudaSuccess) e = launch_delta_walks(C, w.dk, w.terms, WALK_BOTH, st);
+        if (e == cudaSuccess) e = launch_delta_walks(C, w.dk, w.terms, false, st);
         return e == cudaSuccess ? launch_delta_grads(C, w.dk, w.terms, st) : e;
     }
+    // Forward walks and the first heads' reverse ones, then the other heads' reverse walks.
+    ChunkParams first = C;
+    first.rev_heads = w.first * rep; first.key_heads = w.first;
+    C.fwd_heads = 0; C.rev_first = w.first * rep; C.rev_heads = heads - w.first * rep;
+    if ((e = launch_delta_walks(first, w.dk, w.terms, false, st)) != cudaSuccess) return e;
     std::unique_lock<std::mutex> lock(g_aside_mutex, std::defer_lock);
     Aside *a = nullptr;
     if (w.first > 0) {
@@ -231,20 +232,16 @@ cudaError_t walks_and_gradients(ChunkParams &C, const Plan &w, cudaStream_t st)
         if ((e = get_aside(&a)) != cudaSuccess) return e;
     }
     if (a == nullptr || !can_fork(st, a->stream)) {
-        e = launch_delta_walks(C, w.dk, w.terms, WALK_FORWARD, st);
-        if (e == cudaSuccess) e = launch_delta_walks(C, w.dk, w.terms, WALK_REVERSE, st);
+        e = launch_delta_walks(C, w.dk, w.terms, false, st);
         return e == cudaSuccess ? launch_delta_grads(C, w.dk, w.terms, st) : e;
     }
-    // The first heads' reverse walks run beside the forward ones, their gradients beside the other heads' reverse walks.
-    ChunkParams first = C;
-    first.rev_heads = w.first * rep; first.key_heads = w.first; first.together = true;
-    C.rev_first = w.first * rep; C.rev_heads = heads - w.first * rep; C.key_first = w.first; C.key_heads = keys - w.first;
-    if ((e = launch_delta_walks(first, w.dk, w.terms, WALK_BOTH, st)) != cudaSuccess) return e;
+    // The first heads' gradients run beside the other heads' reverse walks.
+    C.key_first = w.first; C.key_heads = keys - w.first;
     if ((e = cudaEventRecord(a->fork, st)) != cudaSuccess) return e;
     if ((e = cudaStreamWaitEvent(a->stream, a->fork, 0)) != cudaSuccess) return e;
     // The walks have to get their SMs first: behind the many small blocks of the gradients they would start late.  So the
     // second stream begins with a kernel of nothing (a call by itself: 407 us with it, 496 without).
-    const cudaError_t reverse = launch_delta_walks(C, w.dk, w.terms, WALK_REVERSE, st);
+    const cudaError_t reverse = launch_delta_walks(C, w.dk, w.terms, false, st);
     cudaError_t aside = launch(nothing_kernel, dim3(1), dim3(32), 0, a->stream, 0);
     if (aside == cudaSuccess) aside = launch_delta_grads(first, w.dk, w.terms, a->stream);
     // joined whatever became of the launches
@@ -334,24 +331,16 @@ extern "C" int cawn_delta_rule_bwd(const cawn_delta_params *params, const void *
     Carver ws = {static_cast<char *>(workspace)};
     rc = chunk_params(C, params, D, w, grad_o, ws, st);
     if (rc != CAWN_OK) return rc;
-    C.rf = ws.take<float4>(w.rf);
-    C.rbf = ws.take<float4>(w.rf);
-    C.sf = ws.take<float4>(w.sf);
-    C.df = ws.take<float4>(w.sf);
-    C.od = ws.take<float>(w.od);
-    C.rv = ws.take<float>(w.od);
-    C.rr = ws.take<float>(w.od);
-    C.sd = ws.take<float>(w.sd);
     C.adj_start = ws.take<float>(w.seg_state);
     C.adj_end = ws.take<float>(w.seg_state);
     C.adj_in = grad_state_out; C.adj_out = grad_state_in;
-    C.u = ws.take<bf16>(w.u);
+    C.r = ws.take<bf16>(w.r);
     C.s0 = ws.take<bf16>(w.s0);
     C.ds = ws.take<bf16>(w.s0);
     C.rbt = ws.take<bf16>(w.rbt);
     C.o = grad_v;
     const long long vo = (long long)params->Hv * params->Dv;
-    C.rb = {w.terms == 1 ? static_cast<const bf16 *>(grad_v) : C.rbt, (long long)params->B * params->L * vo, vo, vo * params->L};
+    C.rb = {nullptr, (long long)params->B * params->L * vo, vo, vo * params->L};
     C.gq = grad_q; C.gk = grad_k; C.gg = grad_g; C.gbeta = grad_beta;
     cudaError_t e = launch_delta_prep(C, w.dk, w.terms, st);
     if (e == cudaSuccess) e = walks_and_gradients(C, w, st);

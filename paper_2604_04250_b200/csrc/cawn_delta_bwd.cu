@@ -1,18 +1,20 @@
 // Gated delta rule, chunk form: the gradients that are local to a chunk, from what the two walks left.
 //
-//   dP_ij = scale Gam_ij dO_i.u_j (i >= j),   E_ij = -Gam_ij rb_i.u_j (i > j)
+//   dP_ij = scale Gam_ij beta_j dO_i.r_j (i >= j),   E_ij = -Gam_ij beta_j rb_i.r_j (i > j)
 //   dQ = scale e^G dO S0 + dP K
-//   dK = dP^T Q + e^{G_C - G} u D - e^G rb S0 + (E + E^T) K
-// The gradients of beta and g are dots of the walks' float accumulators.  rb is beta times the adjoint of u, so
-// dbeta_t = rb_t.r_t / beta_t.  For g: in terms of e^{-G} S the decays appear in o_t as a factor e^{G_t} and in v_t
-// as a factor e^{-G_t} only, so with G over the whole sequence
-//   dL/dG_t = dO_t.o_t - dV_t.v_t,   dg_t = sum_{s >= t} dL/dG_s,
-// taken chunk by chunk: what lies behind the chunk's end is <state, D> there.  Sums of 64 terms, nothing
-// accumulates along the sequence.
+//   dK = dP^T Q + e^{G_C - G} u D - e^G rb S0 + (E + E^T) K,   u = beta r
+// rb is beta times the adjoint of u, so dbeta_t = rb_t.r_t / beta_t.  For g: the decay of token t is a factor of what
+// passes from a token j < t (or from S0) to a token i >= t (or to the chunk's end), so with
+//   W_ij = dP_ij q_i.k_j + E_ij k_i.k_j,   a_i = e^G_i (scale q_i.(dO_i S0) - k_i.(rb_i S0)),   z_j = e^{G_C - G_j} k_j.(u_j D)
+//   dg_t = sum_{j < t <= i} W_ij + sum_{i >= t} a_i + sum_{j < t} z_j + e^{G_C} <S0, D>,
+// in which every term carries the decay: no two large ones cancel, and a token's gradient is as small as its decay is
+// strong.  (As a suffix sum of dO.o - dV.v, which is cheaper, terms of order one cancelled: heads with g = -8 were off by
+// 7e-3 of their gradient, with g = -12 by half of it.)
+//
+// Precision: with bfloat16 storage r, rb and both states come in two terms and pairs of those take all four products.
 //
 // Bound: instructions and the trip to memory at the start of a block; all chunks of all key heads at once, two
-// blocks per SM (3072 chunks of 64 keys and values, bfloat16: 112 us; the scheduler issues in 34% of the cycles,
-// 128 registers x 256 threads leave no room for a third block).
+// blocks per SM of 64 keys and values in bfloat16, whose 128 registers a thread leave no room for a third.
 #include "cawn_delta_chunk.cuh"
 
 #include <type_traits>
@@ -21,42 +23,165 @@ namespace cawn {
 namespace {
 
 // Eight warps: the first four own 16 query rows each (dP, dQ), the others 16 key rows (E, dK).  Values pass in
-// blocks of VW: 64, or 32 where three terms of 128 keys leave room for no more.  All factors take the terms
-// of the inputs: what is computed here is rounded to the inputs' type anyway.
+// blocks of VW: 64, or 32 where three terms of 128 keys leave room for no more.
 template <int DK, int NP> constexpr int kGradVW = NP == 3 && DK == 128 ? 32 : 64;
 
 template <int DK, int NP> struct GradSmem {
-    static constexpr int VW = kGradVW<DK, NP>;
+    static constexpr int NT = NP == 1 ? 2 : 3, VW = kGradVW<DK, NP>, LDV = VW + kPad;
     bf16 q[NP][kC * (DK + kPad)], k[NP][kC * (DK + kPad)];
     union {
         struct {
-            bf16 go[NP][kC * (VW + kPad)], u[NP][kC * (VW + kPad)], rb[NP][kC * (VW + kPad)];
-            bf16 s0[NP][VW * (DK + kPad)], ds[NP][VW * (DK + kPad)];
+            bf16 go[NP][kC * LDV], r[NT][kC * LDV], rb[NT][kC * LDV];
+            bf16 s0[NT][VW * (DK + kPad)], ds[NT][VW * (DK + kPad)];
         } v;
         struct {
-            bf16 dp[NP][kC * kLd], e[NP][kC * kLd];
+            bf16 dp[NT][kC * kLd], e[NT][kC * kLd];
         } m;
     };
     float coef[kCoef][kC];
-    float dots[8][3][kC];                   // per 16 values: dO.o, rb.v, rb.r (up to 128 values)
-    float sd[8];                            // per 16 values: <state after the chunk, D>
+    float pairs[8][kC];                     // per warp: its rows' part of the sum over pairs
+    float dots[3][kC];                      // a of the query rows, a of the key rows, z
+    float ends[8];                          // per warp: its part of <S0, D>
 };
+enum { DOTS_Q = 0, DOTS_K = 1, DOTS_Z = 2 };
+
+// Sum over the four lanes that share a row
+__device__ __forceinline__ float row_sum(float v)
+{
+    v += __shfl_xor_sync(0xffffffffu, v, 1);
+    return v + __shfl_xor_sync(0xffffffffu, v, 2);
+}
+// acc += f (by row half) x; dots += the same times this thread's places of a tile (NP planes, its row i0 at `rows`)
+template <int DK, int NP>
+__device__ __forceinline__ void add_rows(float (&acc)[DK / 8][4], int nb, const float (&x)[2][4], const float (&f)[2], float (&dots)[2], const bf16 *rows)
+{
+    constexpr int ld = DK + kPad;
+#pragma unroll
+    for (int m = 0; m < 2; m++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const float y0 = f[h] * x[m][2 * h], y1 = f[h] * x[m][2 * h + 1];
+            acc[2 * nb + m][2 * h] += y0;
+            acc[2 * nb + m][2 * h + 1] += y1;
+            float2 own = unpack(*reinterpret_cast<const unsigned *>(rows + 8 * h * ld + 16 * nb + 8 * m));
+#pragma unroll
+            for (int i = 1; i < NP; i++) {
+                const float2 more = unpack(*reinterpret_cast<const unsigned *>(rows + i * (kC * ld) + 8 * h * ld + 16 * nb + 8 * m));
+                own.x += more.x;
+                own.y += more.y;
+            }
+            dots[h] = fmaf(y0, own.x, fmaf(y1, own.y, dots[h]));
+        }
+}
+
+// acc += f rows (NA terms, at `left`) x state, and their dots with the tile at `rows`.  Two column blocks at a time: the left
+// factors are read again for each two, which leaves the registers to the sums.
+template <int DK, int NP, int NA>
+__device__ __forceinline__ void times_state(float (&acc)[DK / 8][4], unsigned left, unsigned state, const float (&f)[2], float (&dots)[2], const bf16 *rows)
+{
+    using Smem = GradSmem<DK, NP>;
+    constexpr int NT = Smem::NT, MORE = NA == 2 ? 1 : 0, VW = Smem::VW, ldv = Smem::LDV, ld = DK + kPad;
+    const int w = threadIdx.x / 32 % 4;
+#pragma unroll
+    for (int nb = 0; nb < DK / 16; nb += 2) {
+        float x[2][2][4] = {};
+#pragma unroll
+        for (int d = 0; d < VW / 16; d++) {
+            unsigned a[NA][4];
+            load_left<NA, false>(a, at_kn(left, ldv, 16 * w, 16 * d), kC * ldv);
+#pragma unroll
+            for (int i = 0; i < 2; i++) product<NA, NT, true, MORE>(x[i][0], x[i][1], a, at_kn(state, ld, 16 * d, 16 * (nb + i)), VW * ld);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; i++) add_rows<DK, NP>(acc, nb + i, x[i], f, dots, rows);
+    }
+}
+
+// A side's products with a block of values: X += rows r^T; acc += f rows S0 and (key side) e^{G_C - G} u D; a and z.
+template <int DK, int NP, bool QSIDE>
+__device__ __forceinline__ void with_values(const GradSmem<DK, NP> &sm, float (&X)[8][4], float (&acc)[DK / 8][4], float (&a_dots)[2], float (&z_dots)[2], float scale)
+{
+    using Smem = GradSmem<DK, NP>;
+    constexpr int NT = Smem::NT, NA = QSIDE ? NP : NT, MORE = NT == 2 ? 1 : 0, VW = Smem::VW, ldv = Smem::LDV, ld = DK + kPad;
+    const int w = threadIdx.x / 32 % 4, gr = threadIdx.x % 32 / 4, tc = threadIdx.x % 4 * 2, i0 = 16 * w + gr;
+    const unsigned mine = QSIDE ? smem_addr(sm.v.go[0]) : smem_addr(sm.v.rb[0]), rs = smem_addr(sm.v.r[0]);
+    const bf16 *rows = (QSIDE ? sm.q[0] : sm.k[0]) + i0 * ld + tc;
+    const float sign = QSIDE ? scale : -1.f;
+    const float f[2] = {sign * sm.coef[COEF_EG][i0], sign * sm.coef[COEF_EG][i0 + 8]};
+#pragma unroll
+    for (int d = 0; d < VW / 16; d++) {
+        unsigned a[NA][4];
+        load_left<NA, false>(a, at_kn(mine, ldv, 16 * w, 16 * d), kC * ldv);
+#pragma unroll
+        for (int nb = 0; nb < 4; nb++)
+            if (nb <= w) product<NA, NT, false, NA == 2 ? MORE : 0>(X[2 * nb], X[2 * nb + 1], a, at_nk(rs, ldv, 16 * nb, 16 * d), kC * ldv);
+    }
+    times_state<DK, NP, NA>(acc, mine, smem_addr(sm.v.s0[0]), f, a_dots, rows);
+    if constexpr (!QSIDE) {
+        const float g[2] = {sm.coef[COEF_LEFT][i0] * sm.coef[COEF_BETA][i0], sm.coef[COEF_LEFT][i0 + 8] * sm.coef[COEF_BETA][i0 + 8]};
+        times_state<DK, NP, NT>(acc, rs, smem_addr(sm.v.ds[0]), g, z_dots, rows);
+    }
+}
+
+// For every token t: the sum over this warp's rows i >= t and all j < t of X_ij times rows' scores with the keys.  A row's
+// sums over j < t are a running sum without what lies at t (which may be larger than all of it).
+template <int DK, int NP>
+__device__ __forceinline__ void sum_pairs(const float (&X)[8][4], unsigned rows, unsigned keys, float *to)
+{
+    constexpr int ld = DK + kPad;
+    const int lane = threadIdx.x % 32, w = threadIdx.x / 32 % 4, gr = lane / 4, tc = lane % 4 * 2, i0 = 16 * w + gr;
+    float run[2] = {0.f, 0.f}, sums[8][2];
+#pragma unroll
+    for (int nb = 0; nb < 4; nb++) {
+        float s[2][4] = {};
+        if (nb <= w) {
+#pragma unroll
+            for (int d = 0; d < DK / 16; d++) {
+                unsigned a[NP][4];
+                load_left<NP, false>(a, at_kn(rows, ld, 16 * w, 16 * d), kC * ld);
+                product<NP, NP, false>(s[0], s[1], a, at_nk(keys, ld, 16 * nb, 16 * d), kC * ld);
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < 2; m++) {
+            const int n = 2 * nb + m, t = 8 * n + tc;
+            sums[n][0] = sums[n][1] = 0.f;
+            if (nb > w) continue;
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const int i = i0 + 8 * h;
+                const float w0 = X[n][2 * h] * s[m][2 * h], w1 = X[n][2 * h + 1] * s[m][2 * h + 1];
+                float upto = w0 + w1;
+#pragma unroll
+                for (int o = 1; o < 4; o *= 2) {
+                    const float other = __shfl_up_sync(0xffffffffu, upto, o, 4);
+                    if (lane % 4 >= o) upto += other;
+                }
+                const float left = __shfl_up_sync(0xffffffffu, upto, 1, 4), before = run[h] + (lane % 4 > 0 ? left : 0.f);
+                if (t <= i) sums[n][0] += before;
+                if (t + 1 <= i) sums[n][1] += before + w0;
+                run[h] += __shfl_sync(0xffffffffu, upto, 3, 4);
+            }
+        }
+    }
+    column_sums(sums);
+    *reinterpret_cast<float2 *>(to + 8 * gr + tc) = make_float2(sums[0][0], sums[0][1]);
+}
 
 template <int DK, int NP, class T>
 __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grads_kernel(const ChunkParams P)
 {
     follow_previous();
-    constexpr int ld = DK + kPad, ND = DK / 16, VW = kGradVW<DK, NP>, ldv = VW + kPad;
+    using Smem = GradSmem<DK, NP>;
+    constexpr int ld = DK + kPad, ND = DK / 16, VW = Smem::VW, NT = Smem::NT;
     extern __shared__ __align__(16) unsigned char raw[];
-    auto &sm = *reinterpret_cast<GradSmem<DK, NP> *>(raw);
+    auto &sm = *reinterpret_cast<Smem *>(raw);
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, w = warp % 4, gr = lane / 4, tc = lane % 4 * 2;
     const bool qside = warp < 4;
     const int c = (int)(blockIdx.x % P.chunks), bk = P.key_first + (int)(blockIdx.x / P.chunks), b = bk / P.Hk, hk = bk % P.Hk, rep = P.Hv / P.Hk;
     const long long t0 = (long long)c * kC;
     const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
     const unsigned qs = smem_addr(sm.q[0]), ks = smem_addr(sm.k[0]);
-    const unsigned us = smem_addr(sm.v.u[0]), s0s = smem_addr(sm.v.s0[0]), dss = smem_addr(sm.v.ds[0]);
-    const unsigned mine = qside ? smem_addr(sm.v.go[0]) : smem_addr(sm.v.rb[0]);
     const unsigned dps = smem_addr(sm.m.dp[0]), es = smem_addr(sm.m.e[0]);
 
 #pragma unroll
@@ -66,101 +191,46 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
     }
     cp_commit();
 
-    // rb.r per token (first four warps) and <state after the chunk, D> (the others), per row group of the walks.
-    auto dots_of_walks = [&](int bh, long long nc, int groups) {
-        for (int at = w; at < groups; at += 4) {
-            const long long g = nc * P.vblocks * 4 + at;
-            if (qside) {
-                float dots[8][2];
-#pragma unroll
-                for (int n = 0; n < 8; n++) {
-                    const float4 r = P.rf[(g * 8 + n) * 32 + lane], rb = P.rbf[(g * 8 + n) * 32 + lane];
-                    dots[n][0] = fmaf(r.x, rb.x, r.z * rb.z);
-                    dots[n][1] = fmaf(r.y, rb.y, r.w * rb.w);
-                }
-                column_sums(dots);
-                *reinterpret_cast<float2 *>(&sm.dots[at][2][8 * gr + tc]) = make_float2(dots[0][0], dots[0][1]);
-            } else {
-                const long long next = c + 1 < P.chunks ? g + P.vblocks * 4 : ((long long)P.B * P.Hv * P.chunks + bh) * P.vblocks * 4 + at;
-                float dot = 0.f;
-#pragma unroll
-                for (int n = 0; n < DK / 8; n++) {
-                    const float4 s = P.sf[(next * (DK / 8) + n) * 32 + lane], d = P.df[(g * (DK / 8) + n) * 32 + lane];
-                    dot = fmaf(s.x, d.x, fmaf(s.y, d.y, fmaf(s.z, d.z, fmaf(s.w, d.w, dot))));
-                }
-#pragma unroll
-                for (int o = 16; o > 0; o /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-                if (lane == 0) sm.sd[at] = dot;
-            }
-        }
-    };
-
     float acc[2 * ND][4] = {};              // dQ or dK rows of this warp, over the heads that share them
     const int i0 = 16 * w + gr;             // rows i0 and i0 + 8
 
     for (int hv = 0; hv < rep; hv++) {
         const int bh = b * P.Hv + hk * rep + hv;
-        const long long nc = (long long)bh * P.chunks + c;
+        const long long nc = (long long)bh * P.chunks + c, at = ((long long)b * P.L + t0) * P.Hv + bh % P.Hv;
         if (threadIdx.x < kCoef * 16)
             cp16(smem_addr(&sm.coef[0][0]) + threadIdx.x * 16, P.coef + nc * (kCoef * kC) + threadIdx.x * 4, true);
-        const int groups = (P.Dv + 15) / 16;                // row groups of the walks
-        const long long g0 = nc * P.vblocks * 4;
-        for (int i = threadIdx.x; i < groups * (P.together ? 32 : 48); i += 256) {
-            const int at = i / 16 % groups, what = i / 16 / groups, x = i % 16 * 4;
-            cp16(smem_addr(&sm.dots[at][what][x]), (what == 0 ? P.od : what == 1 ? P.rv : P.rr) + (g0 + at) * kC + x, true);
-        }
-        float X[8][4] = {};                 // dO.u or rb.u, then dP or E
+        float X[8][4] = {};                 // dO.r or rb.r, then dP or E
+        float a_dots[2] = {0.f, 0.f}, z_dots[2] = {0.f, 0.f}, end = 0.f;
         for (int v0 = 0; v0 < P.Dv; v0 += VW) {
             const int vcols = P.Dv - v0 < VW ? P.Dv - v0 : VW, in = v0 % kC;
-            const long long nv = nc * P.vblocks + v0 / kC;
+            const long long nv = nc * P.vblocks + v0 / kC, here = v_base(P, P.rb, bh, t0) + v0;
 #pragma unroll
-            for (int i = 0; i < NP; i++) {
-                load_tile<kC, VW, 256>(sm.v.go[i], P.go.at + i * P.go.plane + v_base(P, P.go, bh, t0) + v0, P.go.stride_t, rows, vcols);
-                load_tile<kC, VW, 256>(sm.v.rb[i], P.rb.at + i * P.rb.plane + v_base(P, P.rb, bh, t0) + v0, P.rb.stride_t, rows, vcols);
-                load_tile<kC, VW, 256>(sm.v.u[i], P.u + (nv * NP + i) * kTile + in, kC, kC, vcols);
-                load_tile<VW, DK, 256>(sm.v.s0[i], P.s0 + (nv * NP + i) * (kC * DK) + in * DK, DK, vcols, DK);
-                load_tile<VW, DK, 256>(sm.v.ds[i], P.ds + (nv * NP + i) * (kC * DK) + in * DK, DK, vcols, DK);
+            for (int i = 0; i < NP; i++) load_tile<kC, VW, 256>(sm.v.go[i], P.go.at + i * P.go.plane + v_base(P, P.go, bh, t0) + v0, P.go.stride_t, rows, vcols);
+#pragma unroll
+            for (int i = 0; i < NT; i++) {
+                const bf16 *rb = NP == 1 && i == 0 ? static_cast<const bf16 *>(P.o) : P.rbt + (i - (NP == 1 ? 1 : 0)) * P.rb.plane;
+                load_tile<kC, VW, 256>(sm.v.rb[i], rb + here, P.rb.stride_t, rows, vcols);
+                load_tile<kC, VW, 256>(sm.v.r[i], P.r + (nv * NT + i) * kTile + in, kC, kC, vcols);
+                load_tile<VW, DK, 256>(sm.v.s0[i], P.s0 + (nv * NT + i) * (kC * DK) + in * DK, DK, vcols, DK);
+                load_tile<VW, DK, 256>(sm.v.ds[i], P.ds + (nv * NT + i) * (kC * DK) + in * DK, DK, vcols, DK);
             }
             cp_commit();
-            if (v0 == 0 && P.together) dots_of_walks(bh, nc, groups);       // while the tiles are on their way
-            else if (v0 == 0 && threadIdx.x < groups) sm.sd[threadIdx.x] = P.sd[g0 + threadIdx.x];
             cp_wait<0>();
             __syncthreads();
-
-            unsigned a[VW / 16][NP][4];     // rows of dO or rb
+            if (qside) with_values<DK, NP, true>(sm, X, acc, a_dots, z_dots, P.scale);
+            else with_values<DK, NP, false>(sm, X, acc, a_dots, z_dots, P.scale);
+            for (int i = threadIdx.x; i < VW * (DK / 8); i += 256) {        // <S0, D>
+                const int place = i / (DK / 8) * ld + i % (DK / 8) * 8;
+                unsigned s[NT][4], d[NT][4];
 #pragma unroll
-            for (int d = 0; d < VW / 16; d++) {
-                load_left<NP, false>(a[d], at_kn(mine, ldv, 16 * w, 16 * d), kC * ldv);
+                for (int n = 0; n < NT; n++) {
+                    *reinterpret_cast<uint4 *>(s[n]) = *reinterpret_cast<const uint4 *>(&sm.v.s0[n][place]);
+                    *reinterpret_cast<uint4 *>(d[n]) = *reinterpret_cast<const uint4 *>(&sm.v.ds[n][place]);
+                }
 #pragma unroll
-                for (int nb = 0; nb < 4; nb++)
-                    if (nb <= w) product<NP, NP, false>(X[2 * nb], X[2 * nb + 1], a[d], at_nk(us, ldv, 16 * nb, 16 * d), kC * ldv);
-            }
-            // times S0: the state's part of dQ, or minus the read-out's part of dK
-            const float sign = qside ? P.scale : -1.f;
-            const float f[2] = {sign * sm.coef[COEF_EG][i0], sign * sm.coef[COEF_EG][i0 + 8]};
-#pragma unroll
-            for (int nb = 0; nb < ND; nb++) {
-                float x[2][4] = {};
-#pragma unroll
-                for (int d = 0; d < VW / 16; d++) product<NP, NP, true>(x[0], x[1], a[d], at_kn(s0s, ld, 16 * d, 16 * nb), VW * ld);
-#pragma unroll
-                for (int m = 0; m < 2; m++)
-#pragma unroll
-                    for (int e = 0; e < 4; e++) acc[2 * nb + m][e] = fmaf(f[e >> 1], x[m][e], acc[2 * nb + m][e]);
-            }
-            if (!qside) {                   // e^{G_C - G} u D
-                const float g[2] = {sm.coef[COEF_LEFT][i0], sm.coef[COEF_LEFT][i0 + 8]};
-#pragma unroll
-                for (int d = 0; d < VW / 16; d++) load_left<NP, false>(a[d], at_kn(us, ldv, 16 * w, 16 * d), kC * ldv);
-#pragma unroll
-                for (int nb = 0; nb < ND; nb++) {
-                    float x[2][4] = {};
-#pragma unroll
-                    for (int d = 0; d < VW / 16; d++) product<NP, NP, true>(x[0], x[1], a[d], at_kn(dss, ld, 16 * d, 16 * nb), VW * ld);
-#pragma unroll
-                    for (int m = 0; m < 2; m++)
-#pragma unroll
-                        for (int e = 0; e < 4; e++) acc[2 * nb + m][e] = fmaf(g[e >> 1], x[m][e], acc[2 * nb + m][e]);
+                for (int e = 0; e < 4; e++) {
+                    const float2 x = sum_terms(s, e), y = sum_terms(d, e);
+                    end = fmaf(x.x, y.x, fmaf(x.y, y.y, end));
                 }
             }
             __syncthreads();        // the value tiles are free
@@ -177,16 +247,28 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
                 float x[2];
 #pragma unroll
                 for (int e = 0; e < 2; e++) {
+                    if (!qside && i == j + e && i < rows) P.gbeta[at + (long long)i * P.Hv] = X[n][2 * h + e] / sm.coef[COEF_BETA][i];
                     const bool on = n / 2 <= w && (qside ? i >= j + e : i > j + e);
-                    x[e] = on ? sign * X[n][2 * h + e] * exp2_fast((sm.coef[COEF_GHI][i] - sm.coef[COEF_GHI][j + e]) +
-                                                                   (sm.coef[COEF_GLO][i] - sm.coef[COEF_GLO][j + e])) : 0.f;
+                    x[e] = on ? sign * sm.coef[COEF_BETA][j + e] * X[n][2 * h + e] *
+                                    exp2_fast((sm.coef[COEF_GHI][i] - sm.coef[COEF_GHI][j + e]) + (sm.coef[COEF_GLO][i] - sm.coef[COEF_GLO][j + e])) : 0.f;
                     X[n][2 * h + e] = x[e];
                 }
-                unsigned y[NP];
+                unsigned y[NT];
                 split(x[0], x[1], y);
 #pragma unroll
-                for (int m = 0; m < NP; m++) *reinterpret_cast<unsigned *>(tile + m * (kC * kLd) + i * kLd + j) = y[m];
+                for (int m = 0; m < NT; m++) *reinterpret_cast<unsigned *>(tile + m * (kC * kLd) + i * kLd + j) = y[m];
             }
+        // what the gradients of g are summed from
+        sum_pairs<DK, NP>(X, qside ? qs : ks, ks, sm.pairs[warp]);
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const float a = row_sum(a_dots[h]), z = row_sum(z_dots[h]);
+            if (tc == 0) sm.dots[qside ? DOTS_Q : DOTS_K][i0 + 8 * h] = a;
+            if (tc == 0 && !qside) sm.dots[DOTS_Z][i0 + 8 * h] = z;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o /= 2) end += __shfl_xor_sync(0xffffffffu, end, o);
+        if (lane == 0) sm.ends[warp] = end;
         __syncthreads();
 
         // dQ += dP K;  dK += E K + E^T K + dP^T Q, each head's sum from zero
@@ -195,16 +277,16 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
             float x[2][4] = {};
 #pragma unroll
             for (int jb = 0; jb < 4; jb++) {
-                unsigned a[NP][4];
+                unsigned a[NT][4];
                 if (jb <= w) {
                     as_left(X[2 * jb], X[2 * jb + 1], a);
-                    product<NP, NP, true>(x[0], x[1], a, at_kn(ks, ld, 16 * jb, 16 * nb), kC * ld);
+                    product<NT, NP, true>(x[0], x[1], a, at_kn(ks, ld, 16 * jb, 16 * nb), kC * ld);
                 }
                 if (!qside && jb >= w) {
-                    load_left<NP, true>(a, at_nk(es, kLd, 16 * jb, 16 * w), kC * kLd);
-                    product<NP, NP, true>(x[0], x[1], a, at_kn(ks, ld, 16 * jb, 16 * nb), kC * ld);
-                    load_left<NP, true>(a, at_nk(dps, kLd, 16 * jb, 16 * w), kC * kLd);
-                    product<NP, NP, true>(x[0], x[1], a, at_kn(qs, ld, 16 * jb, 16 * nb), kC * ld);
+                    load_left<NT, true>(a, at_nk(es, kLd, 16 * jb, 16 * w), kC * kLd);
+                    product<NT, NP, true>(x[0], x[1], a, at_kn(ks, ld, 16 * jb, 16 * nb), kC * ld);
+                    load_left<NT, true>(a, at_nk(dps, kLd, 16 * jb, 16 * w), kC * kLd);
+                    product<NT, NP, true>(x[0], x[1], a, at_kn(qs, ld, 16 * jb, 16 * nb), kC * ld);
                 }
             }
 #pragma unroll
@@ -213,37 +295,34 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
                 acc[2 * nb + 1][e] += x[1][e];
             }
         }
-        // decays and betas: one warp, two tokens a lane
+        // decays: one warp, two tokens a lane; sums over later tokens (a) and earlier ones (z) without subtractions
         if (warp == 0) {
-            float dG[2], end = 0.f;
-            const long long at = ((long long)b * P.L + t0) * P.Hv + bh % P.Hv;
-            for (int i = 0; i < groups; i++) end += sm.sd[i];
+            float pairs[2] = {0.f, 0.f}, a[2], z[2], state = 0.f;
+            for (int i = 0; i < 8; i++) state += sm.ends[i];
+            state *= sm.coef[COEF_EG][kC - 1];
 #pragma unroll
             for (int e = 0; e < 2; e++) {
                 const int t = 2 * lane + e;
-                float od = 0.f, rr = 0.f, rv = 0.f;
-                for (int i = 0; i < groups; i++) {
-                    od += sm.dots[i][0][t];
-                    rv += sm.dots[i][1][t];
-                    rr += sm.dots[i][2][t];
-                }
-                dG[e] = od - rv;
-                if (t < rows) P.gbeta[at + (long long)t * P.Hv] = rr / sm.coef[COEF_BETA][t];
+                for (int i = 0; i < 8; i++) pairs[e] += sm.pairs[i][t];
+                a[e] = sm.dots[DOTS_Q][t] + sm.dots[DOTS_K][t];
+                z[e] = sm.dots[DOTS_Z][t];
             }
-            float run = dG[0] + dG[1];      // suffix sums
+            float after = a[0] + a[1], before = z[0] + z[1];
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
-                const float other = __shfl_down_sync(0xffffffffu, run, o);
-                if (lane + o < 32) run += other;
+                const float x = __shfl_down_sync(0xffffffffu, after, o), y = __shfl_up_sync(0xffffffffu, before, o);
+                if (lane + o < 32) after += x;
+                if (lane >= o) before += y;
             }
+            after = __shfl_down_sync(0xffffffffu, after, 1);
+            before = __shfl_up_sync(0xffffffffu, before, 1);
+            if (lane == 31) after = 0.f;
+            if (lane == 0) before = 0.f;
 #pragma unroll
             for (int e = 0; e < 2; e++) {
                 const int t = 2 * lane + e;
-                if (t < rows) {
-                    const long long to = at + (long long)t * P.Hv;
-                    // a decay that is zero in float passes nothing on, and its derivative is zero
-                    P.gg[to] = P.g[to] < -104.f ? 0.f : run - (e == 1 ? dG[0] : 0.f) + end;
-                }
+                const float late = e == 0 ? a[0] + (a[1] + after) : a[1] + after, early = e == 0 ? before : before + z[0];
+                if (t < rows) P.gg[at + (long long)t * P.Hv] = pairs[e] + (late + early) + state;
             }
         }
         if (hv + 1 < rep) __syncthreads();      // tiles and coefficients are free for the next head

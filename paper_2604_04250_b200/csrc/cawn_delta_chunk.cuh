@@ -9,9 +9,10 @@
 // Precision.  Products run on the tensor cores with bfloat16 factors and float sums; a float factor enters
 // as a sum of bfloat16 terms (8 mantissa bits each).  NP: terms of inputs, NT: terms of T and P.
 // bfloat16 storage: inputs are exact as one term (NP 1), T and P take two (NT 2; the forward's P one), the state and R
-// as factors of the chain two in the forward and three in the backward, the state's update three.  What ends in a
-// bfloat16 output (state, u and P as factors of o; u, the states and the products' weights as factors of dq, dk)
-// is rounded to one term: o, dq, dk are off by 3e-3 of their norm where the rounding of the result alone makes 1.7e-3.
+// as factors of the chain two in the forward and three in the backward, the state's update three.  The factors of dq, dk
+// and the gradients of g and beta (r, rb, both states, the products' weights) take two, and pairs of those all
+// four products: dq and dk are rounded once, the gradients of g and beta off by 3e-6 .. 8e-6 of their norm.  State, u and
+// P as factors of o are rounded to one term: o is off by 3e-3 where the rounding of the result alone makes 1.7e-3.
 // Float storage: three terms everywhere (NP = NT = 3), inputs by a pass of their own: 1e-6 .. 3e-6.
 // (With two terms throughout the state was off by 5e-6 and the gradient of g by up to 2e-5.)
 //
@@ -48,18 +49,13 @@ struct ChunkParams {
     const float *g, *beta;
     float *coef;                        // [nc][kCoef][64]
     bf16 *tri, *p;                      // [nc][NT][kTri]: T - I, transposed, and P, see in_triangle
-    // The backward's walks leave accumulators as they hold them, [nv][4 row groups][tiles of 8 columns][32 lanes]: r
-    // and the state before the chunk (sf has a further end state per head), rb and the adjoint of the state after
-    // the chunk.
-    float4 *rf, *sf, *rbf, *df;
-    // and, in the inputs' terms, what the chunk-local products take: u as token rows, both states as value rows
-    bf16 *u, *s0, *ds;                  // [nv][NP][64 t][64 v], [nv][NP][64 v][DK] twice
-    bf16 *rbt;                          // [NP] terms of rb, float storage only, laid out like v
-    Terms rb;                           // rb: dV itself (bfloat16), or its terms
-    float *od, *rv, *rr;                // [nv][4][64]: dO.o, rb.v and rb.r over 16 values
-    float *sd;                          // [nv][4]: <state after the chunk, its adjoint> over 16 values
-    bool together;                      // the two walks ran side by side: rr and sd are made by the chunk-local kernel
-    int rev_first, rev_heads;           // value heads whose reverse walk a launch does
+    // What the backward's walks leave for the chunk-local products, NT terms each: r as token rows, the state before the
+    // chunk and the adjoint of the one after it as value rows
+    bf16 *r, *s0, *ds;                  // [nv][NT][64 t][64 v], [nv][NT][64 v][DK] twice
+    bf16 *rbt;                          // and rb, laid out like v; with bfloat16 storage the first term is dV itself (o)
+    Terms rb;                           // its plane and strides
+    int fwd_heads;                      // value heads whose forward walk a launch does: all or none
+    int rev_first, rev_heads;           // and those whose reverse walk it does
     int key_first, key_heads;           // and key heads (over all batches) of a launch of the chunk-local kernel
     const float *state_in;              // [bh][Dv][Dk], may be NULL
     float *state_out;
@@ -293,7 +289,8 @@ template <int BP, bool TRANS> __device__ __forceinline__ void load_right(unsigne
 }
 
 // Tiles 2 i, 2 i + 1 += left (AP terms) x right block i (BP terms), N blocks.  Pairs of terms
-// beyond the precision of the longer operand are left out: 2 x 2 terms take three products, 3 x 3 six.  Blocks
+// beyond the precision of the longer operand are left out: 2 x 2 terms take three products, 3 x 3 six (MORE: pairs of
+// so many further orders are taken).  Blocks
 // are the inner loop: a product waits 21 cycles for the sum before it but issues every 8.
 template <int AP, int BP, int N>
 __device__ __forceinline__ void multiply(float (&c)[2 * N][4], const unsigned (&a)[AP][4], const unsigned (&b)[N][BP][4])
@@ -312,10 +309,10 @@ __device__ __forceinline__ void multiply(float (&c)[2 * N][4], const unsigned (&
 }
 
 // One block at a time
-template <int AP, int BP, bool TRANS>
+template <int AP, int BP, bool TRANS, int MORE = 0>
 __device__ __forceinline__ void product(float (&c0)[4], float (&c1)[4], const unsigned (&a)[AP][4], unsigned addr, int plane)
 {
-    constexpr int ORDER = AP > BP ? AP : BP;
+    constexpr int ORDER = (AP > BP ? AP : BP) + MORE;
     unsigned b[BP][4];
     load_right<BP, TRANS>(b, addr, plane);
 #pragma unroll
@@ -370,22 +367,6 @@ template <int NS, int NP, int DK> __device__ __forceinline__ void rows_times(flo
         multiply<NS, NP, 4>(X, a, b);
     }
 }
-// the same for two tiles at once: the state is split once
-template <int NS, int NP, int DK>
-__device__ __forceinline__ void rows_times(float (&X)[8][4], float (&Y)[8][4], const float (&S)[DK / 8][4], unsigned tile_x, unsigned tile_y)
-{
-#pragma unroll
-    for (int d = 0; d < DK / 16; d++) {
-        unsigned a[NS][4], b[4][NP][4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) load_right<NP, false>(b[i], at_nk(tile_x, DK + kPad, 16 * i, 16 * d), kC * (DK + kPad));
-        as_left(S[2 * d], S[2 * d + 1], a);
-        multiply<NS, NP, 4>(X, a, b);
-#pragma unroll
-        for (int i = 0; i < 4; i++) load_right<NP, false>(b[i], at_nk(tile_y, DK + kPad, 16 * i, 16 * d), kC * (DK + kPad));
-        multiply<NS, NP, 4>(Y, a, b);
-    }
-}
 // x (tiles 2 nb .. 2 nb + 3 of a state's columns) += left x K or Q, token block by token block
 template <int NP, int DK> __device__ __forceinline__ void columns_times(float (&x)[4][4], const unsigned (&a)[4][3][4], unsigned tile, int nb)
 {
@@ -422,22 +403,6 @@ template <int NP> __device__ __forceinline__ void residual(float (&X)[8][4], con
             const float2 e = *reinterpret_cast<const float2 *>(&coef[COEF_EG][16 * nb + 8 * m + tc]);
 #pragma unroll
             for (int h = 0; h < 2; h++) fma_row(X[2 * nb + m], h, pair(-e.x, -e.y), pair(sum_terms(v, 2 * m + h)));
-        }
-    }
-}
-// sum over this thread's rows of x times a value tile with rows of tokens (dO or V)
-template <int NP> __device__ __forceinline__ void dots_with(float (&dots)[8][2], const float (&x)[8][4], unsigned tile, int vld, int col)
-{
-#pragma unroll
-    for (int nb = 0; nb < 4; nb++) {
-        unsigned v[NP][4];
-        load_left<NP, true>(v, at_nk(tile, vld, 16 * nb, col), kC * vld);
-#pragma unroll
-        for (int m = 0; m < 2; m++) {
-            const int n = 2 * nb + m;
-            const float2 a = sum_terms(v, 2 * m), b = sum_terms(v, 2 * m + 1);
-            dots[n][0] = fmaf(x[n][0], a.x, x[n][2] * b.x);
-            dots[n][1] = fmaf(x[n][1], a.y, x[n][3] * b.y);
         }
     }
 }
@@ -479,13 +444,6 @@ template <int NP, int DK> __device__ __forceinline__ void store_rows(bf16 *to, c
             for (int i = 0; i < NP; i++) *reinterpret_cast<unsigned *>(to + i * (kC * DK) + 8 * h * DK + 8 * n) = x[i];
         }
 }
-// accumulator tiles to the walks' arrays
-template <int N> __device__ __forceinline__ void store_tiles(float4 *to, const float (&x)[N][4])
-{
-#pragma unroll
-    for (int n = 0; n < N; n++) to[n * 32 + threadIdx.x % 32] = make_float4(x[n][0], x[n][1], x[n][2], x[n][3]);
-}
-
 // Value head's place
 __device__ __forceinline__ long long q_base(const ChunkParams &P, const Terms &t, int bh, long long t0)
 {
@@ -517,10 +475,8 @@ cudaError_t launch_delta_scan(const ChunkParams &P, int dk, int terms, cudaStrea
 // start states of time segments (and of the adjoint's) from what the summaries left
 cudaError_t launch_delta_join(const ChunkParams &P, int dk, bool adjoint, cudaStream_t st);
 // backward: the forward's walk and the reverse one, then what is local to a chunk
-// What a launch of the backward's walks does: SUMMARY of segments in both directions; BOTH: all forward walks and the
-// reverse ones of rev_heads; FORWARD: the former; REVERSE: the latter, with the sums over both walks (rr, sd).
-enum { WALK_SUMMARY, WALK_BOTH, WALK_FORWARD, WALK_REVERSE };
-cudaError_t launch_delta_walks(const ChunkParams &P, int dk, int terms, int what, cudaStream_t st);
+// The backward's walks: of fwd_heads and of rev_heads; `summary`: of segments, in both directions.
+cudaError_t launch_delta_walks(const ChunkParams &P, int dk, int terms, bool summary, cudaStream_t st);
 cudaError_t launch_delta_grads(const ChunkParams &P, int dk, int terms, cudaStream_t st);
 
 }  // namespace cawn

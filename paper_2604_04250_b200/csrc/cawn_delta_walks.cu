@@ -1,17 +1,15 @@
 // Gated delta rule, chunk form: the backward's two walks, side by side.
 //
 // The forward's walk again, for what the gradients need of it,
-//   X = S K^T,  R = V^T - e^G X,  r = R T^T,  u = beta r,  o = scale e^G S Q^T + u P^T,  S <- e^{G_C} S + (e^{G_C - G} u) K,
+//   X = S K^T,  R = V^T - e^G X,  r = R T^T,  u = beta r,  S <- e^{G_C} S + (e^{G_C - G} u) K,
 // and the reverse walk, with D the adjoint of the state after a chunk,
 //   dU = P^T dO + e^{G_C - G} (K D^T),   rb = T^T (beta dU),   D <- e^{G_C} D + (scale e^G dO)^T Q - (e^G rb)^T K.
-// Neither needs the other, except that rb.r and <state, D> are sums over both walks' floats.  Bound: each walk is a
-// chain of products and of the instructions between them, on the SMs that have a head.  So with few heads one launch
-// runs both walks, each on SMs of its own, and those sums are left to the chunk-local kernel (12 heads, float storage:
-// 372 -> 290 us for the whole backward).  With more heads than half the SMs the two would share SMs, which gains
-// next to nothing (96 heads, both on one SM: 231 us, one after the other 125 + 130), so the forward goes first,
-// on the SMs that it leaves idle the reverse walks of some heads, and the other heads' reverse walks after it, which
-// take those sums along, with r and the states fetched beside their tiles; the SMs that these leave idle make the first
-// heads' gradients (whole backward of 96 heads, 2048 tokens: 407 -> 367 us).
+// Neither needs the other, and all sums over both are left to the chunk-local kernel.  They leave r, rb and both states
+// in bfloat16 terms.  Bound: each walk is a chain of products and of the instructions between them, on the SMs that
+// have a head.  So with few heads one launch runs both walks, each on SMs of its own.  With more heads than half the
+// SMs the two would share SMs, which gains next to nothing (96 heads, both on one SM: 231 us, one after the other 125 +
+// 130), so the forward goes first, on the SMs that it leaves idle the reverse walks of some heads, and the other heads'
+// reverse walks after it.
 // A block is 16 * row groups of values of one head and one direction.  Warps of their own fetch the tiles (with the
 // chain warps fetching, either walk of 96 heads took 153 us instead of 127), a chunk ahead where shared memory holds
 // two sets; else the tiles that a chunk starts with come a chunk ahead and the others when it starts.
@@ -27,30 +25,29 @@ template <int DK, int NP> struct WalkTiles {
     using Keys = bf16[NP][kC * (DK + kPad)];
     using Values = bf16[NP][kC * VLD];
     using Triangle = bf16[NT][kTri];
-    struct FwdEarly { Keys k, q; Values v; float coef[kCoef][kC]; };
-    struct FwdLate { Triangle tri, p; Values go; };
+    struct FwdEarly { Keys k; Values v; float coef[kCoef][kC]; };
+    struct FwdLate { Triangle tri; };
     struct RevEarly { Keys k; Values go; Triangle p; float coef[kCoef][kC]; };
-    struct RevLate { Keys q; Triangle tri; Values v; };
-    struct RevFloats : RevLate { float4 r[kRowGroups<NP> * 8 * 32], s[kRowGroups<NP> * (DK / 8) * 32]; };
+    struct RevLate { Keys q; Triangle tri; bf16 way[kC * VLD]; };       // way: on which rb leaves as token rows
 };
-// What a launch does: both walks, or one of them (the reverse one with the sums over both).
-enum { BOTH, FORWARD, REVERSE };
-template <int DK, int NP, int WHAT> struct WalkPlan {
+template <int DK, int NP> struct WalkPlan {
     using Tiles = WalkTiles<DK, NP>;
-    using Late = typename std::conditional<WHAT == REVERSE, typename Tiles::RevFloats, typename Tiles::RevLate>::type;
     static constexpr int RG = kRowGroups<NP>, VW = 16 * RG;
     static constexpr int fetch = NP == 1 ? 32 : 128, threads = 32 * RG + fetch;
-    static constexpr size_t forward(int early, int late) { return WHAT == REVERSE ? 0 : early * sizeof(typename Tiles::FwdEarly) + late * sizeof(typename Tiles::FwdLate); }
-    static constexpr size_t reverse(int early, int late) { return WHAT == FORWARD ? 0 : early * sizeof(typename Tiles::RevEarly) + late * sizeof(Late); }
-    static constexpr size_t need(int early, int late) { return forward(early, late) > reverse(early, late) ? forward(early, late) : reverse(early, late); }
+    static constexpr size_t need(int early, int late)
+    {
+        const size_t fwd = early * sizeof(typename Tiles::FwdEarly) + late * sizeof(typename Tiles::FwdLate);
+        const size_t rev = early * sizeof(typename Tiles::RevEarly) + late * sizeof(typename Tiles::RevLate);
+        return fwd > rev ? fwd : rev;
+    }
     static constexpr size_t room = 227 * 1024;
     static constexpr int early = need(2, 1) <= room ? 2 : 1, late = need(2, 2) <= room ? 2 : 1;      // sets of each
     static constexpr size_t smem = need(early, late);
-    static_assert(smem <= 227 * 1024, "fits an SM");
+    static_assert(smem <= room, "fits an SM");
 };
 
 template <int DK, int NP> struct Fetch {
-    using Plan = WalkPlan<DK, NP, BOTH>;
+    using Plan = WalkPlan<DK, NP>;
     static constexpr int TH = Plan::fetch, NT = Plan::Tiles::NT, VW = Plan::VW;
     const ChunkParams &P;
     int bh, v0, vcols;
@@ -131,15 +128,36 @@ template <class Plan> __device__ __forceinline__ void late_tiles(bool walks)
     __syncthreads();
 }
 
+// A thread's accumulators as token rows of 16 values per warp: through shared memory (`way`, this warp's own columns), in
+// N terms; `put(term, t, from)`: eight values of token t.
+template <int N, class Put> __device__ __forceinline__ void token_rows(const float (&x)[8][4], bf16 *way, int ld, int col, Put put)
+{
+    const int lane = threadIdx.x % 32;
+    const unsigned to = smem_addr(way);
+#pragma unroll
+    for (int term = 0; term < N; term++) {
+        __syncwarp();
+#pragma unroll
+        for (int nb = 0; nb < 4; nb++) {
+            unsigned w[N][4];
+            as_left(x[2 * nb], x[2 * nb + 1], w);
+            stsm_t(at_nk(to, ld, 16 * nb, col), w[term][0], w[term][1], w[term][2], w[term][3]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int j = lane; j < 128; j += 32) put(term, j / 2, j % 2 * 8, *reinterpret_cast<const uint4 *>(&way[j / 2 * ld + col + j % 2 * 8]));
+    }
+}
+
 // SUMMARY: what a segment's own tokens leave at its end (forward; with the transitions, which are the walk of the
 // identity's rows with V = 0) or send to its start (reverse).
-template <int DK, int NP, bool SUMMARY, int WHAT>
+template <int DK, int NP, bool SUMMARY>
 __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char *raw, int bh, int block)
 {
-    using Plan = WalkPlan<DK, NP, WHAT>;
+    using Plan = WalkPlan<DK, NP>;
     using Early = typename Plan::Tiles::FwdEarly;
-    constexpr int NT = Plan::Tiles::NT, VW = Plan::VW, VLD = Plan::Tiles::VLD;
     using Late = typename Plan::Tiles::FwdLate;
+    constexpr int NT = Plan::Tiles::NT, VW = Plan::VW, VLD = Plan::Tiles::VLD;
     auto stage = [&](int i) -> Early & { return reinterpret_cast<Early *>(raw)[i % Plan::early]; };
     auto stage_late = [&](int i) -> Late & { return reinterpret_cast<Late *>(raw + Plan::early * sizeof(Early))[i % Plan::late]; };
     const int seg = blockIdx.z, vblks = (P.Dv + VW - 1) / VW;
@@ -154,17 +172,9 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
         Early &e = stage(i);
         fetch.keys(e.k, P.k, c0 + i);
         if (vcols > 0) fetch.values(e.v, P.v, c0 + i);
-        if (!SUMMARY) fetch.keys(e.q, P.q, c0 + i);
         fetch.coef(e.coef, c0 + i);
     };
-    auto load_late = [&](int i) {
-        Late &late = stage_late(i);
-        fetch.triangle(late.tri, P.tri, c0 + i);
-        if (!SUMMARY) {
-            fetch.triangle(late.p, P.p, c0 + i);
-            fetch.values(late.go, P.go, c0 + i);
-        }
-    };
+    auto load_late = [&](int i) { fetch.triangle(stage_late(i).tri, P.tri, c0 + i); };
     float S[DK / 8][4];
     if (ident) {
 #pragma unroll
@@ -180,19 +190,14 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
     if (fetch_ahead<Plan>(walks, count, load_early, load_late)) return;
     for (int i = 0; i < count; i++) {
         begin_chunk<Plan>(walks, i, count, load_early, load_late);
-        const long long nv = ((long long)bh * P.chunks + c0 + i) * P.vblocks + r0 / kC, g = nv * 4 + w4;        // row group in the arrays
+        const long long nv = ((long long)bh * P.chunks + c0 + i) * P.vblocks + r0 / kC;
         Early &e = stage(i);
         Late &late = stage_late(i);
         const unsigned ks = smem_addr(e.k[0]);
-        float X[8][4] = {}, Y[SUMMARY ? 1 : 8][4] = {};
+        float X[8][4] = {};
         if (walks) {
-            if constexpr (SUMMARY) rows_times<3, NP, DK>(X, S, ks);
-            else rows_times<3, NP, DK>(X, Y, S, ks, smem_addr(e.q[0]));
-            if constexpr (!SUMMARY) {
-                store_tiles(P.sf + g * (DK / 8 * 32), S);
-                store_rows<NP, DK>(P.s0 + nv * (NP * kC * DK) + 16 * w4 * DK, S);
-                scale_tokens(Y, e.coef, COEF_EG, P.scale);
-            }
+            rows_times<3, NP, DK>(X, S, ks);
+            if constexpr (!SUMMARY) store_rows<NT, DK>(P.s0 + nv * (NT * kC * DK) + 16 * w4 * DK, S);
             residual<NP>(X, e.coef, smem_addr(e.v[0]), VLD, 16 * w, vcols > 0);
         }
         late_tiles<Plan>(walks);
@@ -204,33 +209,11 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
             for (int j = 0; j < 4; j++) r[n][j] = X[n][j];
         triangle<3, NT, true, false>(r, [&](unsigned (&a)[3][4], int tb) { as_left(X[2 * tb], X[2 * tb + 1], a); },
                                      [&](int tb, int nb) { return triangle_kn(smem_addr(late.tri[0]), nb, tb); });
-        if constexpr (!SUMMARY) store_tiles(P.rf + g * (8 * 32), r);
+        if constexpr (!SUMMARY)             // by way of this warp's own part of the V tile, which is done with
+            token_rows<NT>(r, e.v[0], VLD, 16 * w, [&](int term, int t, int v, uint4 x) {
+                *reinterpret_cast<uint4 *>(P.r + (nv * NT + term) * kTile + t * kC + 16 * w4 + v) = x;
+            });
         scale_tokens(r, e.coef, COEF_BETA);
-        if constexpr (!SUMMARY) {
-            triangle<3, NT, false, false>(Y, [&](unsigned (&a)[3][4], int tb) { as_left(r[2 * tb], r[2 * tb + 1], a); },
-                                          [&](int tb, int nb) { return triangle_nk(smem_addr(late.p[0]), nb, tb); });
-            float dots[8][2];
-            dots_with<NP>(dots, Y, smem_addr(late.go[0]), VLD, 16 * w);
-            column_sums(dots);
-            *reinterpret_cast<float2 *>(P.od + g * kC + 8 * gr + tc) = make_float2(dots[0][0], dots[0][1]);
-            // u as token rows, through this warp's own part of the V tile
-            const unsigned vs = smem_addr(e.v[0]);
-#pragma unroll
-            for (int term = 0; term < NP; term++) {
-                __syncwarp();
-#pragma unroll
-                for (int nb = 0; nb < 4; nb++) {
-                    unsigned x[NP][4];
-                    as_left(r[2 * nb], r[2 * nb + 1], x);
-                    stsm_t(at_nk(vs, VLD, 16 * nb, 16 * w), x[term][0], x[term][1], x[term][2], x[term][3]);
-                }
-                __syncwarp();
-#pragma unroll
-                for (int j = lane; j < 128; j += 32)
-                    *reinterpret_cast<uint4 *>(P.u + (nv * NP + term) * kTile + j / 2 * kC + 16 * w4 + j % 2 * 8) =
-                        *reinterpret_cast<const uint4 *>(&e.v[0][j / 2 * VLD + 16 * w + j % 2 * 8]);
-            }
-        }
         // the update is summed from zero and added once, as in the forward
         const float eC = e.coef[COEF_EG][kC - 1];
         scale_tokens(r, e.coef, COEF_LEFT);
@@ -248,23 +231,18 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
         }
         end_chunk<Plan>(i, count);
     }
-    if (!walks) return;
-    if constexpr (SUMMARY) {
-        if (ident) store_state<DK>(P.seg_map + ((long long)bh * P.segs + seg) * P.Dk * P.Dk, S, row, P.Dk, P.Dk);
-        else store_state<DK>(P.seg_end + ((long long)bh * P.segs + seg) * P.Dv * P.Dk, S, row, P.Dv, P.Dk);
-    } else if (seg == P.segs - 1) {         // behind the last chunk's, a state per head
-        const long long g = (((long long)P.B * P.Hv * P.chunks + bh) * P.vblocks + r0 / kC) * 4 + w4;
-        store_tiles(P.sf + g * (DK / 8 * 32), S);
-    }
+    if (!SUMMARY || !walks) return;
+    if (ident) store_state<DK>(P.seg_map + ((long long)bh * P.segs + seg) * P.Dk * P.Dk, S, row, P.Dk, P.Dk);
+    else store_state<DK>(P.seg_end + ((long long)bh * P.segs + seg) * P.Dv * P.Dk, S, row, P.Dv, P.Dk);
 }
 
-template <int DK, int NP, bool SUMMARY, int WHAT, class T>
+template <int DK, int NP, bool SUMMARY, class T>
 __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char *raw, int bh, int block)
 {
-    using Plan = WalkPlan<DK, NP, WHAT>;
+    using Plan = WalkPlan<DK, NP>;
     using Early = typename Plan::Tiles::RevEarly;
+    using Late = typename Plan::Tiles::RevLate;
     constexpr int NT = Plan::Tiles::NT, VW = Plan::VW, VLD = Plan::Tiles::VLD;
-    using Late = typename Plan::Late;
     auto stage = [&](int i) -> Early & { return reinterpret_cast<Early *>(raw)[i % Plan::early]; };
     auto stage_late = [&](int i) -> Late & { return reinterpret_cast<Late *>(raw + Plan::early * sizeof(Early))[i % Plan::late]; };
     const int seg = blockIdx.z, r0 = block * VW, vcols = P.Dv - r0 < VW ? P.Dv - r0 : VW;
@@ -284,14 +262,6 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
         Late &late = stage_late(i);
         fetch.triangle(late.tri, P.tri, c1 - 1 - i);
         fetch.keys(late.q, P.q, c1 - 1 - i);
-        if (!SUMMARY) fetch.values(late.v, P.v, c1 - 1 - i);
-        if constexpr (WHAT == REVERSE) {        // this block's row groups lie one after the other
-            const long long here = (long long)bh * P.chunks + c1 - 1 - i, after = c1 - i < P.chunks ? here + 1 : (long long)P.B * P.Hv * P.chunks + bh;
-            const float4 *r = P.rf + ((here * P.vblocks + r0 / kC) * 4 + r0 / 16 % 4) * (8 * 32);
-            const float4 *s = P.sf + ((after * P.vblocks + r0 / kC) * 4 + r0 / 16 % 4) * (DK / 8 * 32);
-            for (int j = threadIdx.x % Plan::fetch; j < Plan::RG * 8 * 32; j += Plan::fetch) cp16(smem_addr(late.r) + j * 16, r + j, true);
-            for (int j = threadIdx.x % Plan::fetch; j < Plan::RG * (DK / 8) * 32; j += Plan::fetch) cp16(smem_addr(late.s) + j * 16, s + j, true);
-        }
     };
     float D[DK / 8][4];
     const float *from = SUMMARY ? nullptr
@@ -303,7 +273,7 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
     for (int i = 0; i < count; i++) {
         begin_chunk<Plan>(walks, i, count, load_early, load_late);
         const int c = c1 - 1 - i;
-        const long long t0 = (long long)c * kC, nv = ((long long)bh * P.chunks + c) * P.vblocks + r0 / kC, g = nv * 4 + w4;
+        const long long t0 = (long long)c * kC, nv = ((long long)bh * P.chunks + c) * P.vblocks + r0 / kC;
         Early &e = stage(i);
         Late &late = stage_late(i);
         const unsigned ks = smem_addr(e.k[0]), gs = smem_addr(e.go[0]);
@@ -311,10 +281,7 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
         float X[8][4] = {};
         if (walks) {
             rows_times<3, NP, DK>(X, D, ks);
-            if constexpr (!SUMMARY) {
-                if constexpr (WHAT == BOTH) store_tiles(P.df + g * (DK / 8 * 32), D);
-                store_rows<NP, DK>(P.ds + nv * (NP * kC * DK) + 16 * w4 * DK, D);
-            }
+            if constexpr (!SUMMARY) store_rows<NT, DK>(P.ds + nv * (NT * kC * DK) + 16 * w4 * DK, D);
             scale_tokens(X, e.coef, COEF_LEFT);
             triangle<NP, NT, true, true>(X, [&](unsigned (&a)[NP][4], int ib) { load_left<NP, true>(a, at_nk(gs, VLD, 16 * ib, 16 * w), kC * VLD); },
                                          [&](int ib, int nb) { return triangle_kn(smem_addr(e.p[0]), ib, nb); });
@@ -322,7 +289,7 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
         }
         late_tiles<Plan>(walks);
         if (!walks) continue;
-        const unsigned qs = smem_addr(late.q[0]), vs = smem_addr(late.v[0]);
+        const unsigned qs = smem_addr(late.q[0]);
         // rb = X + (T - I)^T X
         float rb[8][4];
 #pragma unroll
@@ -331,53 +298,16 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
             for (int j = 0; j < 4; j++) rb[n][j] = X[n][j];
         triangle<3, NT, false, true>(rb, [&](unsigned (&a)[3][4], int ib) { as_left(X[2 * ib], X[2 * ib + 1], a); },
                                      [&](int ib, int nb) { return triangle_nk(smem_addr(late.tri[0]), ib, nb); });
-        if constexpr (WHAT == REVERSE) {
-            float sums[8][2], dot = 0.f;
-#pragma unroll
-            for (int n = 0; n < 8; n++) {
-                const float4 r = late.r[(w * 8 + n) * 32 + lane];
-                sums[n][0] = fmaf(rb[n][0], r.x, rb[n][2] * r.z);
-                sums[n][1] = fmaf(rb[n][1], r.y, rb[n][3] * r.w);
-            }
-            column_sums(sums);
-            *reinterpret_cast<float2 *>(P.rr + g * kC + 8 * gr + tc) = make_float2(sums[0][0], sums[0][1]);
-#pragma unroll
-            for (int n = 0; n < DK / 8; n++) {
-                const float4 s = late.s[(w * (DK / 8) + n) * 32 + lane];
-                dot = fmaf(D[n][0], s.x, fmaf(D[n][1], s.y, fmaf(D[n][2], s.z, fmaf(D[n][3], s.w, dot))));
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-            if (lane == 0) P.sd[g] = dot;
-        }
         if constexpr (!SUMMARY) {
-            if constexpr (WHAT == BOTH) store_tiles(P.rbf + g * (8 * 32), rb);
-            float dots[8][2];
-            dots_with<NP>(dots, rb, vs, VLD, 16 * w);
-            column_sums(dots);
-            *reinterpret_cast<float2 *>(P.rv + g * kC + 8 * gr + tc) = make_float2(dots[0][0], dots[0][1]);
-            // rb as token rows, through this warp's own part of the V tile: dV (bfloat16: the first term is the
-            // rounded value), or its terms for the chunk's gradients
+            // dV (bfloat16: its first term, the rounded value), and the terms that the chunk's gradients take
             const int rows = fetch.rows(c);
-#pragma unroll
-            for (int term = 0; term < NP; term++) {
-                bf16 *dst = (NP == 1 ? static_cast<bf16 *>(P.o) : P.rbt + term * P.rb.plane) + v_base(P, P.rb, bh, t0) + r0;
-                __syncwarp();
-#pragma unroll
-                for (int nb = 0; nb < 4; nb++) {
-                    unsigned x[NP][4];
-                    as_left(rb[2 * nb], rb[2 * nb + 1], x);
-                    stsm_t(at_nk(vs, VLD, 16 * nb, 16 * w), x[term][0], x[term][1], x[term][2], x[term][3]);
-                }
-                __syncwarp();
-#pragma unroll
-                for (int j = lane; j < 128; j += 32) {
-                    const int t = j / 2, v = 16 * w + j % 2 * 8;
-                    if (t < rows && v < vcols) *reinterpret_cast<uint4 *>(dst + t * P.rb.stride_t + v) = *reinterpret_cast<const uint4 *>(&late.v[0][t * VLD + v]);
-                }
-            }
+            const long long here = v_base(P, P.rb, bh, t0) + r0;
+            token_rows<NT>(rb, late.way, VLD, 16 * w, [&](int term, int t, int v, uint4 x) {
+                bf16 *to = (NP == 1 && term == 0 ? static_cast<bf16 *>(P.o) : P.rbt + (term - (NP == 1 ? 1 : 0)) * P.rb.plane) + here;
+                if (t < rows && 16 * w + v < vcols) *reinterpret_cast<uint4 *>(to + t * P.rb.stride_t + 16 * w + v) = x;
+            });
             if constexpr (sizeof(T) == 4) {
-                T *gv = static_cast<T *>(P.o) + v_base(P, P.rb, bh, t0) + r0;
+                T *gv = static_cast<T *>(P.o) + here;
 #pragma unroll
                 for (int n = 0; n < 8; n++)
 #pragma unroll
@@ -428,41 +358,37 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
     if (to != nullptr) store_state<DK>(to, D, row, P.Dv, P.Dk);
 }
 
-template <int DK, int NP, bool SUMMARY, int WHAT, class T>
-__global__ void __launch_bounds__((WalkPlan<DK, NP, WHAT>::threads), 1) delta_walks_kernel(const ChunkParams P)
+template <int DK, int NP, bool SUMMARY, class T>
+__global__ void __launch_bounds__((WalkPlan<DK, NP>::threads), 1) delta_walks_kernel(const ChunkParams P)
 {
     follow_previous();
     extern __shared__ __align__(16) unsigned char raw[];
-    constexpr int VW = WalkPlan<DK, NP, WHAT>::VW;
-    const int back = WHAT == FORWARD ? 0 : P.rev_heads * ((P.Dv + VW - 1) / VW), at = (int)blockIdx.x - back;    // reverse walks come first
-    if (WHAT != FORWARD && at < 0) reverse_walk<DK, NP, SUMMARY, WHAT, T>(P, raw, P.rev_first + (int)blockIdx.x % P.rev_heads, (int)blockIdx.x / P.rev_heads);
-    else if (WHAT != REVERSE) forward_walk<DK, NP, SUMMARY, WHAT>(P, raw, at % (P.B * P.Hv), at / (P.B * P.Hv));
+    constexpr int VW = WalkPlan<DK, NP>::VW;
+    const int back = P.rev_heads * ((P.Dv + VW - 1) / VW), at = (int)blockIdx.x - back;     // reverse walks come first
+    if (at < 0) reverse_walk<DK, NP, SUMMARY, T>(P, raw, P.rev_first + (int)blockIdx.x % P.rev_heads, (int)blockIdx.x / P.rev_heads);
+    else forward_walk<DK, NP, SUMMARY>(P, raw, at % P.fwd_heads, at / P.fwd_heads);
 }
 
-template <int DK, int NP, bool SUMMARY, int WHAT> cudaError_t walks(const ChunkParams &P, cudaStream_t st)
+template <int DK, int NP, bool SUMMARY> cudaError_t walks(const ChunkParams &P, cudaStream_t st)
 {
     using T = typename std::conditional<NP == 1, bf16, float>::type;
-    using Plan = WalkPlan<DK, NP, WHAT>;
-    auto *kernel = delta_walks_kernel<DK, NP, SUMMARY, WHAT, T>;
+    using Plan = WalkPlan<DK, NP>;
+    auto *kernel = delta_walks_kernel<DK, NP, SUMMARY, T>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan::smem);
     if (e != cudaSuccess) return e;
     const int vblks = (P.Dv + Plan::VW - 1) / Plan::VW, ident = SUMMARY ? (P.Dk + Plan::VW - 1) / Plan::VW : 0;
-    const unsigned blocks = (WHAT == FORWARD ? 0u : (unsigned)P.rev_heads * vblks) + (WHAT == REVERSE ? 0u : (unsigned)(P.B * P.Hv) * (vblks + ident));
+    const unsigned blocks = (unsigned)P.rev_heads * vblks + (unsigned)P.fwd_heads * (vblks + ident);
     return launch(kernel, dim3(blocks, 1, P.segs), dim3(Plan::threads), Plan::smem, st, P);
-}
-
-template <int DK, int NP> cudaError_t run(const ChunkParams &P, int what, cudaStream_t st)
-{
-    return what == WALK_SUMMARY ? walks<DK, NP, true, BOTH>(P, st) : what == WALK_BOTH ? walks<DK, NP, false, BOTH>(P, st)
-         : what == WALK_FORWARD ? walks<DK, NP, false, FORWARD>(P, st) : walks<DK, NP, false, REVERSE>(P, st);
 }
 
 }  // namespace
 
-cudaError_t launch_delta_walks(const ChunkParams &P, int dk, int terms, int what, cudaStream_t st)
+cudaError_t launch_delta_walks(const ChunkParams &P, int dk, int terms, bool summary, cudaStream_t st)
 {
-    if (dk == 64) return terms == 1 ? run<64, 1>(P, what, st) : run<64, 3>(P, what, st);
-    return terms == 1 ? run<128, 1>(P, what, st) : run<128, 3>(P, what, st);
+    if (dk == 64) return terms == 1 ? (summary ? walks<64, 1, true>(P, st) : walks<64, 1, false>(P, st))
+                                    : (summary ? walks<64, 3, true>(P, st) : walks<64, 3, false>(P, st));
+    return terms == 1 ? (summary ? walks<128, 1, true>(P, st) : walks<128, 1, false>(P, st))
+                      : (summary ? walks<128, 3, true>(P, st) : walks<128, 3, false>(P, st));
 }
 
 }  // namespace cawn

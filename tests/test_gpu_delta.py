@@ -454,3 +454,35 @@ def test_backward_without_tokens():
     d = delta_inputs(2, 0, 1, 1, 64, 64, torch.float32, seed=26)
     got = backward(d)
     assert torch.equal(got["state_in"].cpu(), d["grad_state_out"])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(1, 150, 1, 4, 64, 64), (2, 70, 2, 4, 128, 40), (1, 1100, 1, 4, 64, 64)], ids=str)
+def test_backward_of_heads_with_short_memory(shape, dtype):
+    """One strong decay per head: its gradient carries the factor e^g, and is held to its own size head by head."""
+    d = delta_inputs(*shape, dtype, seed=30)
+    for h, g in enumerate((-4.0, -8.0, -12.0, -20.0)):
+        d["g"][:, :, h] = g
+    got, want = backward(d)["g"], reference_grads(d)["g"]
+    for h in range(4):
+        close(got[:, :, h], want[:, :, h], STATE_TOL, h)
+
+
+def overwritten(dtype, L=150, size=50.0):
+    """A state much larger than the values, which the first tokens overwrite: what is read later is a difference of
+    large numbers."""
+    d = delta_inputs(1, L, 1, 2, 16, 24, dtype, seed=31)
+    d["k"] = torch.eye(16)[torch.arange(L) % 16][None, :, None].to(dtype).contiguous()
+    d["g"], d["beta"] = torch.zeros_like(d["g"]), torch.ones_like(d["beta"])
+    d["state_in"] *= 2 * size
+    return d
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_backward_of_an_overwritten_state(dtype):
+    """Factors of 16 mantissa bits leave 50 x 2^-17 of a few products, 1e-3, beside the rounding of the results (of 8 bits:
+    a tenth and more); float storage, with 24 bits, 50 x 1e-5."""
+    d = overwritten(dtype)
+    got, want = backward(d), reference_grads(d)
+    for n in "qkv":
+        close(got[n][:, 16:], want[n][:, 16:], 5e-3 if dtype == torch.bfloat16 else 5e-4, n)
