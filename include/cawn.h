@@ -489,9 +489,6 @@ CAWN_API int cawn_delta_rule_step(const cawn_delta_params *params,
  * grad_q, grad_k [B, L, Hk, Dk] (summed over the value heads that share them), grad_v [B, L, Hv, Dv]:
  * dense, the type of the inputs.  grad_g, grad_beta [B, L, Hv] float.  grad_state_in: float or NULL.
  * Outputs may not alias inputs or each other.
- * With many heads part of the work runs on a stream of the library, forked from and joined back into
- * cuda_stream (also while that is captured; if a capture of another stream holds it, everything runs on
- * cuda_stream, and the sums of grad_g and grad_beta may be taken in another order).
  */
 CAWN_API int cawn_delta_rule_bwd(const cawn_delta_params *params,
                                  const void *q, const void *k, const void *v,

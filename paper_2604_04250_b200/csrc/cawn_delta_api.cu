@@ -1,8 +1,6 @@
 // Gated delta rule: entry points and argument checks.
 #include "cawn_delta_chunk.cuh"
 
-#include <mutex>
-
 namespace cawn {
 namespace {
 
@@ -59,8 +57,6 @@ struct Plan {
     size_t q, k, v, go;                  // three bfloat16 terms each, float storage only
     size_t coef, tri, p;
     size_t r, s0, rbt;                  // backward: s0 also for the adjoints
-    bool together;                      // backward: both walks of all heads in one launch
-    int first;                          // else: key heads whose reverse walk runs beside the forward ones
     size_t seg_state, seg_map;
     size_t total;
 };
@@ -110,15 +106,6 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
         w.r = part(nv * nt * kTile * 2);
         w.s0 = part(nv * nt * kC * w.dk * 2);
         w.rbt = w.terms == 3 ? w.v : part((double)rows * p->Hv * p->Dv * 2);     // bfloat16: the first of two terms is dV
-        // Both walks in one launch where their blocks take an SM each.  Else the forward walks go first, and with them as
-        // many reverse ones as the SMs that they leave idle in their last turn can take, where that is a quarter or
-        // more and the walks are long.  Without / with, us, bfloat16 heads of 64 x 64: 96 heads (52 at once) x 2048
-        // tokens 413 / 369, x 512 126 / 129; 110 (38) x 2048 435 / 403; 128 (20) x 1024 247 / 248; 160 (136) x 2048
-        // 751 / 598, x 256 124 / 121; 192 (104) x 256 130 / 135; float storage, 64 (10) x 2048 783 / 803.
-        w.together = w.segs > 1 || blocks <= sm_count();
-        const int64_t one = blocks / 2, each = one / (p->B * p->Hk), idle = (one + sm_count() - 1) / sm_count() * sm_count() - one;
-        const int64_t first = idle / each;
-        if (!w.together && w.chunks >= 16 && first * 4 >= (int64_t)p->B * p->Hk) w.first = (int)first;
     }
     w.total = w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + w.r + 2 * w.s0 + w.rbt + (backward ? 4 : 2) * w.seg_state + w.seg_map;
     return w;
@@ -166,89 +153,6 @@ int chunk_params(ChunkParams &C, const cawn_delta_params *p, const DeltaParams &
     C.seg_end = ws.take<float>(w.seg_state);
     C.seg_map = ws.take<float>(w.seg_map);
     return jobs.count == 0 ? CAWN_OK : status_of(launch_delta_split(jobs, st));
-}
-
-// A second stream, for work of a call beside its own, one per device, created on first use and kept; calls that use it
-// hold the mutex while they record and wait for its events.
-struct Aside {
-    cudaStream_t stream;
-    cudaEvent_t fork, done;
-    bool ready;
-};
-std::mutex g_aside_mutex;
-Aside g_aside[64];
-
-cudaError_t get_aside(Aside **out)
-{
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-    Aside &a = g_aside[dev];
-    if (!a.ready) {
-        if ((e = cudaStreamCreateWithFlags(&a.stream, cudaStreamNonBlocking)) != cudaSuccess) return e;
-        if ((e = cudaEventCreateWithFlags(&a.fork, cudaEventDisableTiming)) != cudaSuccess) return e;
-        if ((e = cudaEventCreateWithFlags(&a.done, cudaEventDisableTiming)) != cudaSuccess) return e;
-        a.ready = true;
-    }
-    *out = &a;
-    return cudaSuccess;
-}
-
-// Whether work of `st` may be forked to `other`: not while a capture that `st` does not belong to holds that one.
-bool can_fork(cudaStream_t st, cudaStream_t other)
-{
-    cudaStreamCaptureStatus mine, its;
-    unsigned long long my_id = 0, its_id = 0;
-    if (cudaStreamGetCaptureInfo(st, &mine, &my_id) != cudaSuccess || cudaStreamGetCaptureInfo(other, &its, &its_id) != cudaSuccess) return false;
-    return its == cudaStreamCaptureStatusNone || (mine == cudaStreamCaptureStatusActive && my_id == its_id);
-}
-
-__global__ void nothing_kernel(int) { follow_previous(); }
-
-// The backward behind the preparation.
-cudaError_t walks_and_gradients(ChunkParams &C, const Plan &w, cudaStream_t st)
-{
-    const int heads = C.B * C.Hv, keys = C.B * C.Hk, rep = C.Hv / C.Hk;
-    C.fwd_heads = heads; C.rev_first = 0; C.rev_heads = heads; C.key_first = 0; C.key_heads = keys;
-    cudaError_t e = cudaSuccess;
-    if (w.together) {
-        if (w.segs > 1) {
-            e = launch_delta_walks(C, w.dk, w.terms, true, st);
-            if (e == cudaSuccess) e = launch_delta_join(C, w.dk, true, st);
-        }
-        if (e == cudaSuccess) e = launch_delta_walks(C, w.dk, w.terms, false, st);
-        return e == cudaSuccess ? launch_delta_grads(C, w.dk, w.terms, st) : e;
-    }
-    // Forward walks and the first heads' reverse ones, then the other heads' reverse walks.
-    ChunkParams first = C;
-    first.rev_heads = w.first * rep; first.key_heads = w.first;
-    C.fwd_heads = 0; C.rev_first = w.first * rep; C.rev_heads = heads - w.first * rep;
-    if ((e = launch_delta_walks(first, w.dk, w.terms, false, st)) != cudaSuccess) return e;
-    std::unique_lock<std::mutex> lock(g_aside_mutex, std::defer_lock);
-    Aside *a = nullptr;
-    if (w.first > 0) {
-        lock.lock();
-        if ((e = get_aside(&a)) != cudaSuccess) return e;
-    }
-    if (a == nullptr || !can_fork(st, a->stream)) {
-        e = launch_delta_walks(C, w.dk, w.terms, false, st);
-        return e == cudaSuccess ? launch_delta_grads(C, w.dk, w.terms, st) : e;
-    }
-    // The first heads' gradients run beside the other heads' reverse walks.
-    C.key_first = w.first; C.key_heads = keys - w.first;
-    if ((e = cudaEventRecord(a->fork, st)) != cudaSuccess) return e;
-    if ((e = cudaStreamWaitEvent(a->stream, a->fork, 0)) != cudaSuccess) return e;
-    // The walks have to get their SMs first: behind the many small blocks of the gradients they would start late.  So the
-    // second stream begins with a kernel of nothing (a call by itself: 407 us with it, 496 without).
-    const cudaError_t reverse = launch_delta_walks(C, w.dk, w.terms, false, st);
-    cudaError_t aside = launch(nothing_kernel, dim3(1), dim3(32), 0, a->stream, 0);
-    if (aside == cudaSuccess) aside = launch_delta_grads(first, w.dk, w.terms, a->stream);
-    // joined whatever became of the launches
-    if ((e = cudaEventRecord(a->done, a->stream)) != cudaSuccess) return e;
-    if ((e = cudaStreamWaitEvent(st, a->done, 0)) != cudaSuccess) return e;
-    if (reverse != cudaSuccess || aside != cudaSuccess) return reverse != cudaSuccess ? reverse : aside;
-    return launch_delta_grads(C, w.dk, w.terms, st);
 }
 
 }  // namespace
@@ -343,6 +247,11 @@ extern "C" int cawn_delta_rule_bwd(const cawn_delta_params *params, const void *
     C.rb = {nullptr, (long long)params->B * params->L * vo, vo, vo * params->L};
     C.gq = grad_q; C.gk = grad_k; C.gg = grad_g; C.gbeta = grad_beta;
     cudaError_t e = launch_delta_prep(C, w.dk, w.terms, st);
-    if (e == cudaSuccess) e = walks_and_gradients(C, w, st);
+    if (e == cudaSuccess && w.segs > 1) {
+        e = launch_delta_walks(C, w.dk, w.terms, true, st);
+        if (e == cudaSuccess) e = launch_delta_join(C, w.dk, true, st);
+    }
+    if (e == cudaSuccess) e = launch_delta_walks(C, w.dk, w.terms, false, st);
+    if (e == cudaSuccess) e = launch_delta_grads(C, w.dk, w.terms, st);
     return status_of(e);
 }

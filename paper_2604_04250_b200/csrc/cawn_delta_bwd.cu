@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
     auto &sm = *reinterpret_cast<Smem *>(raw);
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, w = warp % 4, gr = lane / 4, tc = lane % 4 * 2;
     const bool qside = warp < 4;
-    const int c = (int)(blockIdx.x % P.chunks), bk = P.key_first + (int)(blockIdx.x / P.chunks), b = bk / P.Hk, hk = bk % P.Hk, rep = P.Hv / P.Hk;
+    const int c = (int)(blockIdx.x % P.chunks), bk = (int)(blockIdx.x / P.chunks), b = bk / P.Hk, hk = bk % P.Hk, rep = P.Hv / P.Hk;
     const long long t0 = (long long)c * kC;
     const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
     const unsigned qs = smem_addr(sm.q[0]), ks = smem_addr(sm.k[0]);
@@ -350,7 +350,7 @@ template <int DK, int NP> cudaError_t grads(const ChunkParams &P, cudaStream_t s
     auto *kernel = delta_grads_kernel<DK, NP, T>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    return launch(kernel, dim3((unsigned)(P.key_heads * (long long)P.chunks)), dim3(256), smem, st, P);
+    return launch(kernel, dim3((unsigned)(P.B * P.Hk * (long long)P.chunks)), dim3(256), smem, st, P);
 }
 
 }  // namespace

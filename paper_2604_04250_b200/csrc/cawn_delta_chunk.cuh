@@ -54,9 +54,6 @@ struct ChunkParams {
     bf16 *r, *s0, *ds;                  // [nv][NT][64 t][64 v], [nv][NT][64 v][DK] twice
     bf16 *rbt;                          // and rb, laid out like v; with bfloat16 storage the first term is dV itself (o)
     Terms rb;                           // its plane and strides
-    int fwd_heads;                      // value heads whose forward walk a launch does: all or none
-    int rev_first, rev_heads;           // and those whose reverse walk it does
-    int key_first, key_heads;           // and key heads (over all batches) of a launch of the chunk-local kernel
     const float *state_in;              // [bh][Dv][Dk], may be NULL
     float *state_out;
     const float *adj_in;                // gradient of state_out, may be NULL
@@ -475,7 +472,7 @@ cudaError_t launch_delta_scan(const ChunkParams &P, int dk, int terms, cudaStrea
 // start states of time segments (and of the adjoint's) from what the summaries left
 cudaError_t launch_delta_join(const ChunkParams &P, int dk, bool adjoint, cudaStream_t st);
 // backward: the forward's walk and the reverse one, then what is local to a chunk
-// The backward's walks: of fwd_heads and of rev_heads; `summary`: of segments, in both directions.
+// the backward's walks, in both directions; `summary`: of segments
 cudaError_t launch_delta_walks(const ChunkParams &P, int dk, int terms, bool summary, cudaStream_t st);
 cudaError_t launch_delta_grads(const ChunkParams &P, int dk, int terms, cudaStream_t st);
 

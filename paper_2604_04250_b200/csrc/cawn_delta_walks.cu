@@ -6,10 +6,8 @@
 //   dU = P^T dO + e^{G_C - G} (K D^T),   rb = T^T (beta dU),   D <- e^{G_C} D + (scale e^G dO)^T Q - (e^G rb)^T K.
 // Neither needs the other, and all sums over both are left to the chunk-local kernel.  They leave r, rb and both states
 // in bfloat16 terms.  Bound: each walk is a chain of products and of the instructions between them, on the SMs that
-// have a head.  So with few heads one launch runs both walks, each on SMs of its own.  With more heads than half the
-// SMs the two would share SMs, which gains next to nothing (96 heads, both on one SM: 231 us, one after the other 125 +
-// 130), so the forward goes first, on the SMs that it leaves idle the reverse walks of some heads, and the other heads'
-// reverse walks after it.
+// have a head.  One launch runs both, the reverse ones, which take longer, first: with few heads each walk has an SM of
+// its own, with many the forward walks fill the SMs that the reverse ones leave or come free first.
 // A block is 16 * row groups of values of one head and one direction.  Warps of their own fetch the tiles (with the
 // chain warps fetching, either walk of 96 heads took 153 us instead of 127), a chunk ahead where shared memory holds
 // two sets; else the tiles that a chunk starts with come a chunk ahead and the others when it starts.
@@ -364,9 +362,9 @@ __global__ void __launch_bounds__((WalkPlan<DK, NP>::threads), 1) delta_walks_ke
     follow_previous();
     extern __shared__ __align__(16) unsigned char raw[];
     constexpr int VW = WalkPlan<DK, NP>::VW;
-    const int back = P.rev_heads * ((P.Dv + VW - 1) / VW), at = (int)blockIdx.x - back;     // reverse walks come first
-    if (at < 0) reverse_walk<DK, NP, SUMMARY, T>(P, raw, P.rev_first + (int)blockIdx.x % P.rev_heads, (int)blockIdx.x / P.rev_heads);
-    else forward_walk<DK, NP, SUMMARY>(P, raw, at % P.fwd_heads, at / P.fwd_heads);
+    const int heads = P.B * P.Hv, back = heads * ((P.Dv + VW - 1) / VW), at = (int)blockIdx.x - back;       // reverse walks come first
+    if (at < 0) reverse_walk<DK, NP, SUMMARY, T>(P, raw, (int)blockIdx.x % heads, (int)blockIdx.x / heads);
+    else forward_walk<DK, NP, SUMMARY>(P, raw, at % heads, at / heads);
 }
 
 template <int DK, int NP, bool SUMMARY> cudaError_t walks(const ChunkParams &P, cudaStream_t st)
@@ -377,7 +375,7 @@ template <int DK, int NP, bool SUMMARY> cudaError_t walks(const ChunkParams &P, 
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan::smem);
     if (e != cudaSuccess) return e;
     const int vblks = (P.Dv + Plan::VW - 1) / Plan::VW, ident = SUMMARY ? (P.Dk + Plan::VW - 1) / Plan::VW : 0;
-    const unsigned blocks = (unsigned)P.rev_heads * vblks + (unsigned)P.fwd_heads * (vblks + ident);
+    const unsigned blocks = (unsigned)(P.B * P.Hv) * (2 * vblks + ident);
     return launch(kernel, dim3(blocks, 1, P.segs), dim3(Plan::threads), Plan::smem, st, P);
 }
 

@@ -486,3 +486,32 @@ def test_backward_of_an_overwritten_state(dtype):
     got, want = backward(d), reference_grads(d)
     for n in "qkv":
         close(got[n][:, 16:], want[n][:, 16:], 5e-3 if dtype == torch.bfloat16 else 5e-4, n)
+
+
+def test_backward_of_many_heads_does_not_wait_for_another_stream():
+    """Work of one caller's stream stays on it: a call behind a stream that is held up does not hold up another's."""
+    d = delta_inputs(12, 1100, 4, 8, 16, 16, torch.bfloat16, seed=32)
+    c = {n: t.cuda() for n, t in d.items()}
+    prm = params(d)
+    outs = [{n: torch.empty_like(c[n]) for n in ("q", "k", "v", "g", "beta")} for _ in range(2)]
+    spaces = [cb.new_delta_workspace(prm, cb.CAWN_DELTA_BWD) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+
+    def call(i):
+        o = outs[i]
+        cb.cawn_delta_rule_bwd(prm, c["q"], c["k"], c["v"], c["g"], c["beta"], c["grad_o"], o["q"], o["k"], o["v"], o["g"], o["beta"], spaces[i],
+                               state_in=c["state_in"], stream=streams[i])
+
+    call(0), call(1)                                # first use, before anything is held up
+    torch.cuda.synchronize()
+    with torch.cuda.stream(streams[0]):
+        torch.cuda._sleep(1 << 30)                  # half a second
+    call(0)
+    held = torch.cuda.Event()
+    held.record(streams[0])
+    call(1)
+    streams[1].synchronize()
+    assert not held.query()
+    torch.cuda.synchronize()
+    for n in outs[0]:
+        assert torch.equal(outs[0][n], outs[1][n])
