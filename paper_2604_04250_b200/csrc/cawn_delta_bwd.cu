@@ -42,6 +42,7 @@ template <int DK, int NP> struct GradSmem {
     float pairs[8][kC];                     // per warp: its rows' part of the sum over pairs
     float dots[3][kC];                      // a of the query rows, a of the key rows, z
     float ends[8];                          // per warp: its part of <S0, D>
+    float4 handed[4][4][32];                // from a query warp to its key warp: accumulators of two column blocks
 };
 enum { DOTS_Q = 0, DOTS_K = 1, DOTS_Z = 2 };
 
@@ -51,106 +52,155 @@ __device__ __forceinline__ float row_sum(float v)
     v += __shfl_xor_sync(0xffffffffu, v, 1);
     return v + __shfl_xor_sync(0xffffffffu, v, 2);
 }
-// acc += f (by row half) x; dots += the same times this thread's places of a tile (NP planes, its row i0 at `rows`)
-template <int DK, int NP>
-__device__ __forceinline__ void add_rows(float (&acc)[DK / 8][4], int nb, const float (&x)[2][4], const float (&f)[2], float (&dots)[2], const bf16 *rows)
-{
-    constexpr int ld = DK + kPad;
-#pragma unroll
-    for (int m = 0; m < 2; m++)
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const float y0 = f[h] * x[m][2 * h], y1 = f[h] * x[m][2 * h + 1];
-            acc[2 * nb + m][2 * h] += y0;
-            acc[2 * nb + m][2 * h + 1] += y1;
-            float2 own = unpack(*reinterpret_cast<const unsigned *>(rows + 8 * h * ld + 16 * nb + 8 * m));
-#pragma unroll
-            for (int i = 1; i < NP; i++) {
-                const float2 more = unpack(*reinterpret_cast<const unsigned *>(rows + i * (kC * ld) + 8 * h * ld + 16 * nb + 8 * m));
-                own.x += more.x;
-                own.y += more.y;
-            }
-            dots[h] = fmaf(y0, own.x, fmaf(y1, own.y, dots[h]));
-        }
-}
-
-// acc += f rows (NA terms, at `left`) x state, and their dots with the tile at `rows`.  Two column blocks at a time: the left
-// factors are read again for each two, which leaves the registers to the sums.
+// x (column blocks nb, nb + 1 of a side's rows) = f (by row half) rows (NA terms, at `left`) x state; dots += x times this
+// thread's places of a tile (NP planes, its row i0 at `own`).  Two column blocks at a time: the left factors are read
+// again for each two, which leaves the registers to the sums.
 template <int DK, int NP, int NA>
-__device__ __forceinline__ void times_state(float (&acc)[DK / 8][4], unsigned left, unsigned state, const float (&f)[2], float (&dots)[2], const bf16 *rows)
+__device__ __forceinline__ void times_state(float (&x)[4][4], int nb, unsigned left, unsigned state, const f32x2 (&f)[2], f32x2 (&dots)[2], const bf16 *own)
 {
     using Smem = GradSmem<DK, NP>;
     constexpr int NT = Smem::NT, MORE = NA == 2 ? 1 : 0, VW = Smem::VW, ldv = Smem::LDV, ld = DK + kPad;
     const int w = threadIdx.x / 32 % 4;
 #pragma unroll
-    for (int nb = 0; nb < DK / 16; nb += 2) {
-        float x[2][2][4] = {};
+    for (int n = 0; n < 4; n++)
 #pragma unroll
-        for (int d = 0; d < VW / 16; d++) {
-            unsigned a[NA][4];
-            load_left<NA, false>(a, at_kn(left, ldv, 16 * w, 16 * d), kC * ldv);
-#pragma unroll
-            for (int i = 0; i < 2; i++) product<NA, NT, true, MORE>(x[i][0], x[i][1], a, at_kn(state, ld, 16 * d, 16 * (nb + i)), VW * ld);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; i++) add_rows<DK, NP>(acc, nb + i, x[i], f, dots, rows);
-    }
-}
-
-// A side's products with a block of values: X += rows r^T; acc += f rows S0 and (key side) e^{G_C - G} u D; a and z.
-template <int DK, int NP, bool QSIDE>
-__device__ __forceinline__ void with_values(const GradSmem<DK, NP> &sm, float (&X)[8][4], float (&acc)[DK / 8][4], float (&a_dots)[2], float (&z_dots)[2], float scale)
-{
-    using Smem = GradSmem<DK, NP>;
-    constexpr int NT = Smem::NT, NA = QSIDE ? NP : NT, MORE = NT == 2 ? 1 : 0, VW = Smem::VW, ldv = Smem::LDV, ld = DK + kPad;
-    const int w = threadIdx.x / 32 % 4, gr = threadIdx.x % 32 / 4, tc = threadIdx.x % 4 * 2, i0 = 16 * w + gr;
-    const unsigned mine = QSIDE ? smem_addr(sm.v.go[0]) : smem_addr(sm.v.rb[0]), rs = smem_addr(sm.v.r[0]);
-    const bf16 *rows = (QSIDE ? sm.q[0] : sm.k[0]) + i0 * ld + tc;
-    const float sign = QSIDE ? scale : -1.f;
-    const float f[2] = {sign * sm.coef[COEF_EG][i0], sign * sm.coef[COEF_EG][i0 + 8]};
+        for (int e = 0; e < 4; e++) x[n][e] = 0.f;
 #pragma unroll
     for (int d = 0; d < VW / 16; d++) {
+        unsigned a[NA][4], b[2][NT][4];
+        load_left<NA, false>(a, at_kn(left, ldv, 16 * w, 16 * d), kC * ldv);
+#pragma unroll
+        for (int i = 0; i < 2; i++) load_right<NT, true>(b[i], at_kn(state, ld, 16 * d, 16 * (nb + i)), VW * ld);
+        multiply<NA, NT, 2, MORE>(x, a, b);
+    }
+#pragma unroll
+    for (int n = 0; n < 4; n++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const f32x2 y = mul2(f[h], pair(x[n][2 * h], x[n][2 * h + 1]));
+            const bf16 *at = own + 8 * h * ld + 16 * nb + 8 * n;
+            f32x2 z = pair(unpack(*reinterpret_cast<const unsigned *>(at)));
+#pragma unroll
+            for (int i = 1; i < NP; i++) z = add2(z, pair(unpack(*reinterpret_cast<const unsigned *>(at + i * (kC * ld)))));
+            dots[h] = fma2(y, z, dots[h]);
+            x[n][2 * h] = halves(y).x;
+            x[n][2 * h + 1] = halves(y).y;
+        }
+}
+template <int N> __device__ __forceinline__ void add_tiles(float (*acc)[4], const float (&x)[N][4])
+{
+#pragma unroll
+    for (int n = 0; n < N; n++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const float2 y = halves(add2(pair(acc[n][2 * h], acc[n][2 * h + 1]), pair(x[n][2 * h], x[n][2 * h + 1])));
+            acc[n][2 * h] = y.x;
+            acc[n][2 * h + 1] = y.y;
+        }
+}
+
+// A side's products with a block of values: X += rows r^T; acc += f rows S0; a and z.  The query side, which has less to do,
+// also makes the key side's e^{G_C - G} u D and hands it over, two column blocks at a time (all of it on the key side: the
+// kernel of 3072 chunks 209 us).
+enum { BAR_HANDED = 1, BAR_TAKEN = 2 };
+template <int DK, int NP, bool QSIDE>
+__device__ __forceinline__ void with_values(GradSmem<DK, NP> &sm, float (&X)[8][4], float (&acc)[DK / 8][4], f32x2 (&a_dots)[2], f32x2 (&z_dots)[2], float scale)
+{
+    using Smem = GradSmem<DK, NP>;
+    constexpr int NT = Smem::NT, NA = QSIDE ? NP : NT, MORE = NA == 2 ? 1 : 0, ldv = Smem::LDV, ld = DK + kPad;
+    const int lane = threadIdx.x % 32, w = threadIdx.x / 32 % 4, gr = lane / 4, tc = lane % 4 * 2, i0 = 16 * w + gr;
+    const unsigned mine = QSIDE ? smem_addr(sm.v.go[0]) : smem_addr(sm.v.rb[0]), rs = smem_addr(sm.v.r[0]);
+    const unsigned s0s = smem_addr(sm.v.s0[0]), dss = smem_addr(sm.v.ds[0]);
+    const bf16 *own = (QSIDE ? sm.q[0] : sm.k[0]) + i0 * ld + tc, *keys = sm.k[0] + i0 * ld + tc;
+#pragma unroll
+    for (int d = 0; d < Smem::VW / 16; d++) {
         unsigned a[NA][4];
         load_left<NA, false>(a, at_kn(mine, ldv, 16 * w, 16 * d), kC * ldv);
 #pragma unroll
-        for (int nb = 0; nb < 4; nb++)
-            if (nb <= w) product<NA, NT, false, NA == 2 ? MORE : 0>(X[2 * nb], X[2 * nb + 1], a, at_nk(rs, ldv, 16 * nb, 16 * d), kC * ldv);
+        for (int nb = 0; nb < 4; nb += 2) {
+            if (nb + 1 <= w) {
+                unsigned b[2][NT][4];
+                load_right<NT, false>(b[0], at_nk(rs, ldv, 16 * nb, 16 * d), kC * ldv);
+                load_right<NT, false>(b[1], at_nk(rs, ldv, 16 * nb + 16, 16 * d), kC * ldv);
+                multiply<NA, NT, 2, MORE>(reinterpret_cast<float (&)[4][4]>(X[2 * nb]), a, b);
+            } else if (nb == w) {
+                product<NA, NT, false, MORE>(X[2 * nb], X[2 * nb + 1], a, at_nk(rs, ldv, 16 * nb, 16 * d), kC * ldv);
+            }
+        }
     }
-    times_state<DK, NP, NA>(acc, mine, smem_addr(sm.v.s0[0]), f, a_dots, rows);
-    if constexpr (!QSIDE) {
-        const float g[2] = {sm.coef[COEF_LEFT][i0] * sm.coef[COEF_BETA][i0], sm.coef[COEF_LEFT][i0 + 8] * sm.coef[COEF_BETA][i0 + 8]};
-        times_state<DK, NP, NT>(acc, rs, smem_addr(sm.v.ds[0]), g, z_dots, rows);
+    auto twice = [](float v) { return pair(v, v); };
+    const float sign = QSIDE ? scale : -1.f;
+    const f32x2 f[2] = {twice(sign * sm.coef[COEF_EG][i0]), twice(sign * sm.coef[COEF_EG][i0 + 8])};
+    const f32x2 g[2] = {twice(sm.coef[COEF_LEFT][i0] * sm.coef[COEF_BETA][i0]), twice(sm.coef[COEF_LEFT][i0 + 8] * sm.coef[COEF_BETA][i0 + 8])};
+#pragma unroll
+    for (int nb = 0; nb < DK / 16; nb += 2) {
+        float x[4][4];
+        if constexpr (QSIDE) {
+            times_state<DK, NP, NT>(x, nb, rs, dss, g, z_dots, keys);
+            if (nb > 0) bar_sync(BAR_TAKEN, 256);
+#pragma unroll
+            for (int n = 0; n < 4; n++) sm.handed[w][n][lane] = make_float4(x[n][0], x[n][1], x[n][2], x[n][3]);
+            bar_arrive(BAR_HANDED, 256);
+        }
+        times_state<DK, NP, NA>(x, nb, mine, s0s, f, a_dots, own);
+        add_tiles<4>(acc + 2 * nb, x);
+        if constexpr (!QSIDE) {
+            bar_sync(BAR_HANDED, 256);
+#pragma unroll
+            for (int n = 0; n < 4; n++) {
+                const float4 y = sm.handed[w][n][lane];
+                x[n][0] = y.x; x[n][1] = y.y; x[n][2] = y.z; x[n][3] = y.w;
+            }
+            if (nb + 2 < DK / 16) bar_arrive(BAR_TAKEN, 256);
+            add_tiles<4>(acc + 2 * nb, x);
+        }
     }
 }
 
-// For every token t: the sum over this warp's rows i >= t and all j < t of X_ij times rows' scores with the keys.  A row's
-// sums over j < t are a running sum without what lies at t (which may be larger than all of it).
-template <int DK, int NP>
-__device__ __forceinline__ void sum_pairs(const float (&X)[8][4], unsigned rows, unsigned keys, float *to)
+// dP or E from X, as left factors (xa) and as a tile (for dK, transposed), and for every token t the sum over this warp's
+// rows i >= t and all j < t of it times the rows' scores with the keys.  A row's sum over j < t is a running sum without
+// what lies at t (which may be larger than all of it).  Key side: the gradients of beta, which are X's diagonal.
+template <int DK, int NP, bool QSIDE>
+__device__ __forceinline__ void weights(GradSmem<DK, NP> &sm, float (&X)[8][4], unsigned (&xa)[4][GradSmem<DK, NP>::NT][4], float scale, float *gbeta, long long step, int valid)
 {
-    constexpr int ld = DK + kPad;
+    constexpr int ld = DK + kPad, NT = GradSmem<DK, NP>::NT;
     const int lane = threadIdx.x % 32, w = threadIdx.x / 32 % 4, gr = lane / 4, tc = lane % 4 * 2, i0 = 16 * w + gr;
+    const unsigned keys = smem_addr(sm.k[0]), rows = QSIDE ? smem_addr(sm.q[0]) : keys;
+    bf16 *tile = QSIDE ? sm.m.dp[0] : sm.m.e[0];
+    const f32x2 sign = QSIDE ? pair(scale, scale) : pair(-1.f, -1.f);
+    const float hi0 = sm.coef[COEF_GHI][i0], lo0 = sm.coef[COEF_GLO][i0], hi8 = sm.coef[COEF_GHI][i0 + 8], lo8 = sm.coef[COEF_GLO][i0 + 8];
+    const f32x2 hi[2] = {pair(hi0, hi0), pair(hi8, hi8)}, lo[2] = {pair(lo0, lo0), pair(lo8, lo8)}, minus = pair(-1.f, -1.f);
     float run[2] = {0.f, 0.f}, sums[8][2];
 #pragma unroll
     for (int nb = 0; nb < 4; nb++) {
+        sums[2 * nb][0] = sums[2 * nb][1] = sums[2 * nb + 1][0] = sums[2 * nb + 1][1] = 0.f;
+        if (nb > w) continue;
         float s[2][4] = {};
-        if (nb <= w) {
 #pragma unroll
-            for (int d = 0; d < DK / 16; d++) {
-                unsigned a[NP][4];
-                load_left<NP, false>(a, at_kn(rows, ld, 16 * w, 16 * d), kC * ld);
-                product<NP, NP, false>(s[0], s[1], a, at_nk(keys, ld, 16 * nb, 16 * d), kC * ld);
-            }
+        for (int d = 0; d < DK / 16; d++) {
+            unsigned a[NP][4];
+            load_left<NP, false>(a, at_kn(rows, ld, 16 * w, 16 * d), kC * ld);
+            product<NP, NP, false>(s[0], s[1], a, at_nk(keys, ld, 16 * nb, 16 * d), kC * ld);
         }
 #pragma unroll
         for (int m = 0; m < 2; m++) {
-            const int n = 2 * nb + m, t = 8 * n + tc;
-            sums[n][0] = sums[n][1] = 0.f;
-            if (nb > w) continue;
+            const int n = 2 * nb + m, j = 8 * n + tc;
+            auto two = [&](int which) { return *reinterpret_cast<const f32x2 *>(&sm.coef[which][j]); };
+            const f32x2 factor = mul2(sign, two(COEF_BETA)), jhi = two(COEF_GHI), jlo = two(COEF_GLO);
 #pragma unroll
             for (int h = 0; h < 2; h++) {
                 const int i = i0 + 8 * h;
-                const float w0 = X[n][2 * h] * s[m][2 * h], w1 = X[n][2 * h + 1] * s[m][2 * h + 1];
+                float2 x = make_float2(X[n][2 * h], X[n][2 * h + 1]);
+                if (!QSIDE && nb == w && i < valid && (i == j || i == j + 1)) gbeta[i * step] = (i == j ? x.x : x.y) / sm.coef[COEF_BETA][i];
+                const float2 g = halves(add2(fma2(jhi, minus, hi[h]), fma2(jlo, minus, lo[h])));
+                x = halves(mul2(mul2(factor, pair(exp2_fast(g.x), exp2_fast(g.y))), pair(x)));
+                if (nb == w) {
+                    if (QSIDE ? i < j : i <= j) x.x = 0.f;
+                    if (QSIDE ? i < j + 1 : i <= j + 1) x.y = 0.f;
+                }
+                X[n][2 * h] = x.x;
+                X[n][2 * h + 1] = x.y;
+                const float w0 = x.x * s[m][2 * h], w1 = x.y * s[m][2 * h + 1];
                 float upto = w0 + w1;
 #pragma unroll
                 for (int o = 1; o < 4; o *= 2) {
@@ -158,14 +208,20 @@ __device__ __forceinline__ void sum_pairs(const float (&X)[8][4], unsigned rows,
                     if (lane % 4 >= o) upto += other;
                 }
                 const float left = __shfl_up_sync(0xffffffffu, upto, 1, 4), before = run[h] + (lane % 4 > 0 ? left : 0.f);
-                if (t <= i) sums[n][0] += before;
-                if (t + 1 <= i) sums[n][1] += before + w0;
+                if (nb < w || j <= i) sums[n][0] += before;
+                if (nb < w || j + 1 <= i) sums[n][1] += before + w0;
                 run[h] += __shfl_sync(0xffffffffu, upto, 3, 4);
             }
         }
+        as_left(X[2 * nb], X[2 * nb + 1], xa[nb]);
+#pragma unroll
+        for (int m = 0; m < NT; m++)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                *reinterpret_cast<unsigned *>(tile + m * (kC * kLd) + (i0 + e % 2 * 8) * kLd + 16 * nb + e / 2 * 8 + tc) = xa[nb][m][e];
     }
     column_sums(sums);
-    *reinterpret_cast<float2 *>(to + 8 * gr + tc) = make_float2(sums[0][0], sums[0][1]);
+    *reinterpret_cast<float2 *>(&sm.pairs[threadIdx.x / 32][8 * gr + tc]) = make_float2(sums[0][0], sums[0][1]);
 }
 
 template <int DK, int NP, class T>
@@ -200,7 +256,8 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
         if (threadIdx.x < kCoef * 16)
             cp16(smem_addr(&sm.coef[0][0]) + threadIdx.x * 16, P.coef + nc * (kCoef * kC) + threadIdx.x * 4, true);
         float X[8][4] = {};                 // dO.r or rb.r, then dP or E
-        float a_dots[2] = {0.f, 0.f}, z_dots[2] = {0.f, 0.f}, end = 0.f;
+        f32x2 a_dots[2] = {}, z_dots[2] = {};
+        float end = 0.f;
         for (int v0 = 0; v0 < P.Dv; v0 += VW) {
             const int vcols = P.Dv - v0 < VW ? P.Dv - v0 : VW, in = v0 % kC;
             const long long nv = nc * P.vblocks + v0 / kC, here = v_base(P, P.rb, bh, t0) + v0;
@@ -236,35 +293,15 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
             __syncthreads();        // the value tiles are free
         }
 
-        // dP or E, and as tiles (they feed dK transposed)
-        bf16 *tile = qside ? sm.m.dp[0] : sm.m.e[0];
-        const float sign = qside ? P.scale : -1.f;
-#pragma unroll
-        for (int n = 0; n < 8; n++)
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const int i = i0 + 8 * h, j = 8 * n + tc;
-                float x[2];
-#pragma unroll
-                for (int e = 0; e < 2; e++) {
-                    if (!qside && i == j + e && i < rows) P.gbeta[at + (long long)i * P.Hv] = X[n][2 * h + e] / sm.coef[COEF_BETA][i];
-                    const bool on = n / 2 <= w && (qside ? i >= j + e : i > j + e);
-                    x[e] = on ? sign * sm.coef[COEF_BETA][j + e] * X[n][2 * h + e] *
-                                    exp2_fast((sm.coef[COEF_GHI][i] - sm.coef[COEF_GHI][j + e]) + (sm.coef[COEF_GLO][i] - sm.coef[COEF_GLO][j + e])) : 0.f;
-                    X[n][2 * h + e] = x[e];
-                }
-                unsigned y[NT];
-                split(x[0], x[1], y);
-#pragma unroll
-                for (int m = 0; m < NT; m++) *reinterpret_cast<unsigned *>(tile + m * (kC * kLd) + i * kLd + j) = y[m];
-            }
-        // what the gradients of g are summed from
-        sum_pairs<DK, NP>(X, qside ? qs : ks, ks, sm.pairs[warp]);
+        unsigned xa[4][NT][4];              // dP or E as left factors
+        if (qside) weights<DK, NP, true>(sm, X, xa, P.scale, nullptr, 0, 0);
+        else weights<DK, NP, false>(sm, X, xa, P.scale, P.gbeta + at, P.Hv, rows);
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            const float a = row_sum(a_dots[h]), z = row_sum(z_dots[h]);
+            const float2 ah = halves(a_dots[h]), zh = halves(z_dots[h]);
+            const float a = row_sum(ah.x + ah.y), z = row_sum(zh.x + zh.y);
             if (tc == 0) sm.dots[qside ? DOTS_Q : DOTS_K][i0 + 8 * h] = a;
-            if (tc == 0 && !qside) sm.dots[DOTS_Z][i0 + 8 * h] = z;
+            if (tc == 0 && qside) sm.dots[DOTS_Z][i0 + 8 * h] = z;
         }
 #pragma unroll
         for (int o = 16; o > 0; o /= 2) end += __shfl_xor_sync(0xffffffffu, end, o);
@@ -279,8 +316,7 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
             for (int jb = 0; jb < 4; jb++) {
                 unsigned a[NT][4];
                 if (jb <= w) {
-                    as_left(X[2 * jb], X[2 * jb + 1], a);
-                    product<NT, NP, true>(x[0], x[1], a, at_kn(ks, ld, 16 * jb, 16 * nb), kC * ld);
+                    product<NT, NP, true>(x[0], x[1], xa[jb], at_kn(ks, ld, 16 * jb, 16 * nb), kC * ld);
                 }
                 if (!qside && jb >= w) {
                     load_left<NT, true>(a, at_nk(es, kLd, 16 * jb, 16 * w), kC * kLd);

@@ -287,12 +287,12 @@ template <int BP, bool TRANS> __device__ __forceinline__ void load_right(unsigne
 
 // Tiles 2 i, 2 i + 1 += left (AP terms) x right block i (BP terms), N blocks.  Pairs of terms
 // beyond the precision of the longer operand are left out: 2 x 2 terms take three products, 3 x 3 six (MORE: pairs of
-// so many further orders are taken).  Blocks
-// are the inner loop: a product waits 21 cycles for the sum before it but issues every 8.
-template <int AP, int BP, int N>
+// so many further orders are taken).  Blocks are the inner loop: a product waits 21 cycles for the sum before it but
+// issues every 8.
+template <int AP, int BP, int N, int MORE = 0>
 __device__ __forceinline__ void multiply(float (&c)[2 * N][4], const unsigned (&a)[AP][4], const unsigned (&b)[N][BP][4])
 {
-    constexpr int ORDER = AP > BP ? AP : BP;
+    constexpr int ORDER = (AP > BP ? AP : BP) + MORE;
 #pragma unroll
     for (int j = 0; j < BP; j++)
 #pragma unroll
