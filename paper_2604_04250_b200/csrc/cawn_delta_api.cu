@@ -139,7 +139,6 @@ int chunk_params(ChunkParams &C, const cawn_delta_params *p, const DeltaParams &
     C.g = D.g; C.beta = D.beta; C.state_in = D.state_in;
     C.L = p->L; C.B = p->B; C.Hk = p->Hk; C.Hv = p->Hv; C.Dk = p->Dk; C.Dv = p->Dv; C.scale = p->scale;
     C.chunks = w.chunks; C.vblocks = w.vblocks; C.segs = w.segs; C.seg_chunks = w.seg_chunks;
-    C.p_terms = w.terms == 3 ? 3 : grad_o != nullptr ? 2 : 1;   // bfloat16 outputs take one, the backward's dots two
     SplitJobs jobs = {};
     jobs.rows = (long long)p->B * p->L;
     C.q = terms_of(jobs, D.q, D.q_stride, p, p->Hk * p->Dk, w, w.q, ws);

@@ -8,11 +8,12 @@
 //
 // Precision.  Products run on the tensor cores with bfloat16 factors and float sums; a float factor enters
 // as a sum of bfloat16 terms (8 mantissa bits each).  NP: terms of inputs, NT: terms of T and P.
-// bfloat16 storage: inputs are exact as one term (NP 1), T and P take two (NT 2; the forward's P one), the state and R
-// as factors of the chain two in the forward and three in the backward, the state's update three.  The factors of dq, dk
-// and the gradients of g and beta (r, rb, both states, the products' weights) take two, and pairs of those all
-// four products: dq and dk are rounded once, the gradients of g and beta off by 3e-6 .. 8e-6 of their norm.  State, u and
-// P as factors of o are rounded to one term: o is off by 3e-3 where the rounding of the result alone makes 1.7e-3.
+// bfloat16 storage: inputs are exact as one term (NP 1), T and P take two (NT 2), the state and R as factors of the
+// chain two in the forward and three in the backward, the state's update three.  The factors of o (state, u, P) and of
+// dq, dk and the gradients of g and beta (r, rb, both states, the products' weights) take two, in the backward with all
+// four products of a pair: o, dq and dk are rounded to 8 bits once, at the end, the gradients of g and beta off by
+// 1e-6 .. 8e-6 of their norm.  Sixteen bits and not eight for these, because their sums may be differences: where keys
+// overwrite a state 50 times the values, one term each left o off by 6e-2 and dq, dk by more.
 // Float storage: three terms everywhere (NP = NT = 3), inputs by a pass of their own: 1e-6 .. 3e-6.
 // (With two terms throughout the state was off by 5e-6 and the gradient of g by up to 2e-5.)
 //
@@ -67,7 +68,6 @@ struct ChunkParams {
     float *adj_start, *adj_end;
     int segs, seg_chunks;
     int B, Hk, Hv, Dk, Dv, chunks, vblocks;
-    int p_terms;                        // terms of P that the walk will read
     float scale;
 };
 
@@ -260,13 +260,6 @@ template <int N> __device__ __forceinline__ void as_left(const float (&c0)[4], c
 #pragma unroll
         for (int i = 0; i < N; i++) a[i][e] = w[i];
     }
-}
-
-// The first N terms
-template <int N, int M> __device__ __forceinline__ const unsigned (&leading(const unsigned (&a)[M][4]))[N][4]
-{
-    static_assert(N <= M, "no more terms than there are");
-    return reinterpret_cast<const unsigned (&)[N][4]>(a);
 }
 
 // Left operand of AP terms from shared planes `plane` elements apart (TRANS: stored [k][m], at_nk; else at_kn).

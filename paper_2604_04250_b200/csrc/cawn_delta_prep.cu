@@ -24,9 +24,9 @@ template <int DK, int NP> struct PrepSmem {
     float nhi[kC], nlo[kC], beta[kC];   // -G in two parts
 };
 
-// PT: terms of P that are read later.  Each of the four warps owns the 8-row blocks w and 7 - w: below the diagonal that is nine 8 x 8 blocks for
+// Each of the four warps owns the 8-row blocks w and 7 - w: below the diagonal that is nine 8 x 8 blocks for
 // everyone.  (With 16 adjacent rows the last warp had four times the first one's exponentials.)
-template <int DK, int NP, int PT>
+template <int DK, int NP>
 __global__ void __launch_bounds__(128, (DK == 64 && NP == 1 ? 5 : 1)) delta_prep_kernel(const ChunkParams P)
 {
     follow_previous();
@@ -137,14 +137,15 @@ __global__ void __launch_bounds__(128, (DK == 64 && NP == 1 ? 5 : 1)) delta_prep
                 p.x = i >= j ? p.x : 0.f; p.y = i >= j + 1 ? p.y : 0.f;
                 a.x = i > j ? a.x : 0.f; a.y = i > j + 1 ? a.y : 0.f;
             }
-            unsigned pw[PT], aw[NT];
+            unsigned pw[NT], aw[NT];
             split(p.x, p.y, pw);
             split(a.x, a.y, aw);
             const int to = in_triangle(block / 2, n / 2) + (block % 2 * 2 + n % 2) * 64 + lane * 2;
 #pragma unroll
-            for (int m = 0; m < PT; m++) *reinterpret_cast<unsigned *>(pt + m * kTri + to) = pw[m];
-#pragma unroll
-            for (int m = 0; m < NT; m++) *reinterpret_cast<unsigned *>(&sm.a[m][i * kLd + j]) = aw[m];
+            for (int m = 0; m < NT; m++) {
+                *reinterpret_cast<unsigned *>(pt + m * kTri + to) = pw[m];
+                *reinterpret_cast<unsigned *>(&sm.a[m][i * kLd + j]) = aw[m];
+            }
             if (n / 2 == block / 2) *reinterpret_cast<float2 *>(&sm.diag[block / 2][i % 16][j % 16]) = a;
         }
     }
@@ -238,21 +239,20 @@ __global__ void __launch_bounds__(256) delta_split_kernel(const SplitJobs jobs)
     for (int m = 0; m < 3; m++) *reinterpret_cast<uint4 *>(j.dst + m * (words * 8) + i * 8) = make_uint4(w[0][m], w[1][m], w[2][m], w[3][m]);
 }
 
-template <int DK, int NP, int PT> cudaError_t prep(const ChunkParams &P, cudaStream_t st)
+template <int DK, int NP> cudaError_t prep(const ChunkParams &P, cudaStream_t st)
 {
     const size_t smem = sizeof(PrepSmem<DK, NP>);
-    const cudaError_t e = cudaFuncSetAttribute(delta_prep_kernel<DK, NP, PT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = cudaFuncSetAttribute(delta_prep_kernel<DK, NP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    return launch<true>(delta_prep_kernel<DK, NP, PT>, dim3((unsigned)(P.B * P.Hv * (long long)P.chunks)), dim3(128), smem, st, P);
+    return launch<true>(delta_prep_kernel<DK, NP>, dim3((unsigned)(P.B * P.Hv * (long long)P.chunks)), dim3(128), smem, st, P);
 }
 
 }  // namespace
 
 cudaError_t launch_delta_prep(const ChunkParams &P, int dk, int terms, cudaStream_t st)
 {
-    if (terms == 3) return dk == 64 ? prep<64, 3, 3>(P, st) : prep<128, 3, 3>(P, st);
-    if (P.p_terms == 1) return dk == 64 ? prep<64, 1, 1>(P, st) : prep<128, 1, 1>(P, st);
-    return dk == 64 ? prep<64, 1, 2>(P, st) : prep<128, 1, 2>(P, st);
+    if (terms == 3) return dk == 64 ? prep<64, 3>(P, st) : prep<128, 3>(P, st);
+    return dk == 64 ? prep<64, 1>(P, st) : prep<128, 1>(P, st);
 }
 
 cudaError_t launch_delta_split(const SplitJobs &jobs, cudaStream_t st)

@@ -32,13 +32,15 @@ template <int DK, int NP> struct ScanStage {
 };
 // Tiles of the outputs.
 template <int DK, int NP> struct ScanSide {
-    bf16 q[NP][kC * (DK + kPad)], p[NP][kTri];
+    static constexpr int NT = NP == 1 ? 2 : 3;
+    bf16 q[NP][kC * (DK + kPad)], p[NT][kTri];
     bf16 t[kC * (16 * kRowGroups<NP> + kPad)];          // the way out for token rows
     float coef[kCoef][kC];
 };
 // From chain to side warp: terms of the state and of u.
 template <int DK, int NP> struct ScanSwap {
-    uint4 s[NP * DK / 16 * 32], u[NP * 4 * 32];
+    static constexpr int NT = NP == 1 ? 2 : 3;
+    uint4 s[NT * DK / 16 * 32], u[NT * 4 * 32];
 };
 
 template <int DK, int NP, int MODE> struct ScanPlan {
@@ -76,10 +78,9 @@ __device__ __forceinline__ void side_load(const ChunkParams &P, ScanSide<DK, NP>
     const long long t0 = (long long)c * kC, nc = (long long)bh * P.chunks + c;
     const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
 #pragma unroll
-    for (int i = 0; i < NP; i++) {
-        load_tile<kC, DK, TH>(st.q[i], P.q.at + i * P.q.plane + q_base(P, P.q, bh, t0), P.q.stride_t, rows, P.Dk);
-        load_triangle<TH>(st.p[i], P.p + (nc * NT + i) * kTri);
-    }
+    for (int i = 0; i < NP; i++) load_tile<kC, DK, TH>(st.q[i], P.q.at + i * P.q.plane + q_base(P, P.q, bh, t0), P.q.stride_t, rows, P.Dk);
+#pragma unroll
+    for (int i = 0; i < NT; i++) load_triangle<TH>(st.p[i], P.p + (nc * NT + i) * kTri);
     for (int i = threadIdx.x % TH; i < kCoef * kC / 4; i += TH) cp16(smem_addr(&st.coef[0][0]) + i * 16, P.coef + nc * (kCoef * kC) + i * 4, true);
     cp_commit();
 }
@@ -137,15 +138,15 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
                 else cp_commit();               // an empty group keeps the count
             }
             bar_sync(BAR_READY + par, PAIR);
-            // Y = scale e^G S Q^T + u P^T; factors in the output's terms
+            // Y = scale e^G S Q^T + u P^T
             float Y[8][4] = {};
 #pragma unroll
             for (int d = 0; d < DK / 16; d++) {
-                unsigned a[NP][4], b[4][NP][4];
+                unsigned a[NT][4], b[4][NP][4];
                 get_left(a, sw.s, d);
 #pragma unroll
                 for (int i = 0; i < 4; i++) load_right<NP, false>(b[i], at_nk(qs, ld, 16 * i, 16 * d), kC * ld);
-                multiply<NP, NP, 4>(Y, a, b);
+                multiply<NT, NP, 4>(Y, a, b);
             }
 #pragma unroll
             for (int n = 0; n < 8; n++) {
@@ -158,7 +159,7 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
                 if (SS == 2) cp_wait<1>(); else cp_wait<0>();
                 bar_arrive(BAR_FULL + (cs ^ 1), PAIR);
             }
-            triangle<NP, NP, false, false>(Y, [&](unsigned (&a)[NP][4], int tb) { get_left(a, sw.u, tb); },
+            triangle<NT, NT, false, false>(Y, [&](unsigned (&a)[NT][4], int tb) { get_left(a, sw.u, tb); },
                                            [&](int tb, int nb) { return triangle_nk(ps, nb, tb); });
             if (c + WS < c1) bar_arrive(BAR_FREE + par, PAIR);
             if (c + CS >= c1) {
@@ -203,7 +204,6 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
 
     // -------------------------------------------------------------------------- chain warps
     // Two terms of the state are enough for what is read from it; its update takes three.
-    constexpr int NS = NP == 1 ? 2 : 3;
     const int row = r0 + 16 * w + gr;                       // state rows row, row + 8; columns 8 n + tc, +1 of tile n
     float S[DK / 8][4];
     if (ident) {
@@ -230,12 +230,12 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
         float X[8][4] = {};
 #pragma unroll
         for (int d = 0; d < DK / 16; d++) {
-            unsigned a[NS][4], b[4][NP][4];
+            unsigned a[NT][4], b[4][NP][4];
 #pragma unroll
             for (int i = 0; i < 4; i++) load_right<NP, false>(b[i], at_nk(ks, ld, 16 * i, 16 * d), kC * ld);
             as_left(S[2 * d], S[2 * d + 1], a);
-            if constexpr (MODE == MODE_OUT) put_left(sw.s, d, leading<NP>(a));
-            multiply<NS, NP, 4>(X, a, b);
+            if constexpr (MODE == MODE_OUT) put_left(sw.s, d, a);
+            multiply<NT, NP, 4>(X, a, b);
         }
         // R (in X), r = R + R (T - I)^T: tokens t of the result from block t' on
         residual<NP>(X, st.coef, smem_addr(st.v[0]), VLD, 16 * w, vcols > 0);
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__((ScanPlan<DK, NP, MODE>::threads), 1) delta_sc
         if constexpr (MODE == MODE_OUT) {
 #pragma unroll
             for (int tb = 0; tb < 4; tb++) {
-                unsigned a[NP][4];
+                unsigned a[NT][4];
                 as_left(r[2 * tb], r[2 * tb + 1], a);
                 put_left(sw.u, tb, a);
             }

@@ -515,3 +515,27 @@ def test_backward_of_many_heads_does_not_wait_for_another_stream():
     torch.cuda.synchronize()
     for n in outs[0]:
         assert torch.equal(outs[0][n], outs[1][n])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("form", ["step", "chunk"])
+def test_overwritten_state(form, dtype):
+    """As in the backward: 50 x 2^-17 of a few factors beside the rounding of o; float storage 50 x 1e-5."""
+    d = overwritten(dtype)
+    o, so = forward(d, form)
+    want_o, want_s = reference(d)
+    close(o[:, 16:], want_o[:, 16:], 5e-3 if dtype == torch.bfloat16 else 5e-4)
+    close(so, want_s, 5e-4)
+
+
+@pytest.mark.parametrize("shape", [(2, 200, 2, 4, 64, 64), (1, 300, 1, 2, 128, 72)], ids=str)
+def test_bfloat16_outputs_are_rounded_once(shape):
+    """o, dq, dk, dv against the definition rounded to bfloat16: equal but for values next to a rounding boundary.  With
+    factors of 16 bits a result moves by about 1e-5 of its row, and one in a few hundred crosses a boundary by 2^-8 of
+    itself: 2^-8 / sqrt(100) = 4e-4 of the norm."""
+    d = delta_inputs(*shape, torch.bfloat16, seed=33)
+    o, _ = forward(d, "chunk")
+    close(o, reference(d)[0].bfloat16(), 4e-4)
+    got, want = backward(d), reference_grads(d)
+    for n in "qkv":
+        close(got[n], want[n].bfloat16(), 4e-4, n)
