@@ -539,3 +539,91 @@ def test_bfloat16_outputs_are_rounded_once(shape):
     got, want = backward(d), reference_grads(d)
     for n in "qkv":
         close(got[n], want[n].bfloat16(), 4e-4, n)
+
+
+# ------------------------------------------------------------------------------------ resets, bad values, workspaces
+
+def reset(d):
+    """Resets, strong and no decays, beta 0 and almost 2, one key over and over."""
+    L = d["g"].shape[1]
+    d["g"][:, L // 3] = -float("inf")
+    d["g"][:, L // 3 + 1] = -float("inf")
+    d["g"][:, L // 2:L // 2 + 10] = -90.0
+    d["g"][:, L // 2 + 10:L // 2 + 20] = -1000.0
+    d["g"][:, L // 2 + 20:L // 2 + 40] = 0.0
+    d["beta"][:, L // 2 + 40:L // 2 + 50] = 0.0
+    d["beta"][:, L // 2 + 50:L // 2 + 55] = 1.9
+    d["k"][:, L // 4:L // 4 + 20] = d["k"][:, L // 4:L // 4 + 1]
+    return d
+
+
+RESETS = [(1, 200, 2, 2, 64, 64), (2, 230, 1, 2, 128, 72), (1, 1500, 1, 1, 64, 64), (1, 1300, 1, 2, 128, 64)]     # the last two in segments
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("form", ["step", "chunk"])
+@pytest.mark.parametrize("shape", RESETS, ids=str)
+def test_forgetting_in_both_storages_and_in_segments(shape, form, dtype):
+    d = reset(delta_inputs(*shape, dtype, seed=40))
+    o, so = forward(d, form)
+    want_o, want_s = reference(d)
+    close(o, want_o, TOL[dtype])
+    close(so, want_s, STATE_TOL)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", RESETS, ids=str)
+def test_backward_forgetting_in_both_storages_and_in_segments(shape, dtype):
+    d = reset(delta_inputs(*shape, dtype, seed=41))
+    got, want = backward(d), reference_grads(d)
+    forgotten = d["g"] < -104
+    assert (got["g"].cpu()[forgotten] == 0).all()
+    check_grads(got, want, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(2, 130, 1, 1, 64, 64), (1, 1500, 1, 1, 64, 64)], ids=str)
+def test_bad_values_stay_in_their_row_and_behind_their_chunk(shape, dtype):
+    """NaN or infinity in a value: its row of the state from there on, and in the chunk of 64 tokens where it stands; nothing
+    else.  A NaN decay: everything behind."""
+    d = delta_inputs(*shape, dtype, seed=42)
+    L = shape[1]
+    at = L // 2 + 9
+    first = at // 64 * 64
+    clean, clean_s = forward(d, "chunk")
+    for bad in (float("nan"), float("inf")):
+        x = dict(d, v=d["v"].clone())
+        x["v"][0, at, 0, 3] = bad
+        o, so = forward(x, "chunk")
+        assert torch.equal(o[:, :first], clean[:, :first]) and torch.equal(o[1:], clean[1:])
+        assert not torch.isfinite(o[0, at:, 0, 3]).any() and not torch.isfinite(so[0, 0, 3]).any()
+        others = [i for i in range(64) if i != 3]
+        assert torch.equal(o[..., others], clean[..., others]) and torch.equal(so[:, :, others], clean_s[:, :, others])
+    x = dict(d, g=d["g"].clone())
+    x["g"][0, at] = float("nan")
+    o, so = forward(x, "chunk")
+    assert torch.equal(o[:, :first], clean[:, :first]) and torch.isnan(o[0, at:]).all() and torch.isnan(so[0]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(1, 1500, 1, 1, 64, 64), (1, 1300, 1, 2, 128, 72), (12, 130, 4, 8, 64, 64), (3, 100, 2, 2, 40, 104), (1, 33, 1, 1, 8, 8)], ids=str)
+def test_calls_keep_to_their_workspace(shape, dtype):
+    """In segments, with many heads, with values that are no multiple of 64, in both storages: the reported size is enough, and
+    nothing behind it is written."""
+    d = delta_inputs(*shape, dtype, seed=43)
+    c = {n: t.cuda() for n, t in d.items()}
+    prm = params(d)
+    want_o, want_g = forward(d, "chunk"), backward(d)
+    for op in (cb.CAWN_DELTA_FWD, cb.CAWN_DELTA_BWD):
+        n = cb.cawn_delta_rule_workspace_bytes(prm, op)
+        ws = torch.full((n + (1 << 16),), 0xA5, dtype=torch.uint8, device="cuda")
+        if op == cb.CAWN_DELTA_FWD:
+            o, so = torch.empty_like(c["v"]), torch.empty_like(c["state_in"])
+            cb.cawn_delta_rule_fwd(prm, c["q"], c["k"], c["v"], c["g"], c["beta"], o, ws[:n], state_in=c["state_in"], state_out=so)
+            assert torch.equal(o, want_o[0]) and torch.equal(so, want_o[1])
+        else:
+            out = {m: torch.empty_like(c[m]) for m in want_g}
+            cb.cawn_delta_rule_bwd(prm, c["q"], c["k"], c["v"], c["g"], c["beta"], c["grad_o"], out["q"], out["k"], out["v"], out["g"], out["beta"],
+                                   ws[:n], state_in=c["state_in"], grad_state_out=c["grad_state_out"], grad_state_in=out["state_in"])
+            assert all(torch.equal(out[m], want_g[m]) for m in out)
+        assert (ws[n:] == 0xA5).all()

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from paper_2604_04250_b200 import binding as cb
-from delta_ref import close as close64, flags_of, group_norm, philox_bits
+from delta_ref import PHILOX_ANSWERS, close as close64, flags_of, group_norm, philox_bits, philox_words
 
 pytestmark = pytest.mark.gpu
 
@@ -270,3 +270,76 @@ def test_an_independent_input_written_two_calls_before(writer, between):
         outs.append(ys)
     for a, b in zip(*outs):
         assert torch.equal(torch.view_as_real(a), torch.view_as_real(b))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(20, 4, 64), (3, 2, 4096), (9, 5, 37)], ids=str)
+def test_norm_over_its_inputs(shape, dtype):
+    """y may take the place of x or of the gate, grad_x that of grad_y (teams of lanes, whole blocks and odd widths)."""
+    d, prm = norm_case(*shape, dtype, "gate", seed=70)
+    x, gate, gy, w, b = (on_gpu(d[n]) for n in ("x", "gate", "gy", "w", "b"))
+    y = torch.empty_like(x)
+    cb.cawn_group_norm_fwd(prm, x, y, weight=w, bias=b, gate=gate)
+    for n in ("x", "gate"):
+        t = {"x": x.clone(), "gate": gate.clone()}
+        cb.cawn_group_norm_fwd(prm, t["x"], t[n], weight=w, bias=b, gate=t["gate"])
+        assert torch.equal(t[n], y), n
+    gx, gg, over = torch.empty_like(x), torch.empty_like(x), gy.clone()
+    sums = [torch.empty_like(w) for _ in range(4)]
+    cb.cawn_group_norm_bwd(prm, x, gy, gx, cb.new_norm_workspace(prm), weight=w, bias=b, gate=gate, grad_gate=gg, grad_weight=sums[0], grad_bias=sums[1])
+    again = torch.empty_like(gg)
+    cb.cawn_group_norm_bwd(prm, x, over, over, cb.new_norm_workspace(prm), weight=w, bias=b, gate=gate, grad_gate=again, grad_weight=sums[2], grad_bias=sums[3])
+    assert torch.equal(over, gx) and torch.equal(again, gg) and torch.equal(sums[0], sums[2]) and torch.equal(sums[1], sums[3])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(300, 12, 64), (890, 12, 64), (7, 8, 1024), (50, 2, 4096), (5, 5, 37)], ids=str)
+def test_norm_keeps_to_its_workspace(shape, dtype):
+    d, prm = norm_case(*shape, dtype, "silu", seed=71)
+    x, gy, w, b = (on_gpu(d[n]) for n in ("x", "gy", "w", "b"))
+    n = cb.cawn_group_norm_workspace_bytes(prm)
+    ws = torch.full((n + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    gx, gw, gb = torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+    cb.cawn_group_norm_bwd(prm, x, gy, gx, ws[:n], weight=w, bias=b, grad_weight=gw, grad_bias=gb)
+    assert (ws[n:] == 0xA5).all()
+
+
+def test_dropout_over_its_residual():
+    n = 4099
+    rng = torch.Generator().manual_seed(72)
+    x, r = torch.randn(n, generator=rng).cuda(), torch.randn(n, generator=rng).cuda()
+    prm = cb.make_dropout_params(n, 0.3, 9, 2)
+    y = torch.empty_like(x)
+    cb.cawn_dropout(prm, x, y, residual=r)
+    cb.cawn_dropout(prm, x, r, residual=r)
+    assert torch.equal(y, r)
+
+
+def test_dropout_draws_the_published_bits():
+    """Counter and key of zeros: an element is kept while the threshold is at most its bits."""
+    words = PHILOX_ANSWERS[0][2]
+    bits = [half for w in words for half in (w & 0xFFFF, w >> 16)]
+    y = torch.empty(8, device="cuda")
+    for i, b in enumerate(bits):
+        for threshold in (b, b + 1):
+            cb.cawn_dropout(cb.make_dropout_params(8, threshold / 65536, 0), torch.ones(8, device="cuda"), y)
+            assert (y != 0).tolist() == [x >= threshold for x in bits], (i, threshold)
+
+
+def test_dropout_of_more_than_2_35_elements():
+    """The counter's second word is the upper half of element / 8: the last elements of an array of 2^35 + 64 (in place, 69 GB
+    of bfloat16)."""
+    n = (1 << 35) + 64
+    if torch.cuda.mem_get_info()[0] < 90 * (1 << 30):
+        pytest.skip("less than 90 GB of device memory free")
+    x = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    seed, offset = 0x0123456789ABCDEF, 5
+    cb.cawn_dropout(cb.make_dropout_params(n, 0.5, seed, offset, flags=flags_of(x.dtype)), x, x)
+    tail = (x[-128:] != 0).cpu().numpy()
+    del x
+    torch.cuda.empty_cache()
+    bits = []
+    for i in range(n // 8 - 16, n // 8):
+        for w in philox_words((i & 0xFFFFFFFF, i >> 32, offset, 0), (seed & 0xFFFFFFFF, seed >> 32)):
+            bits += [w & 0xFFFF, w >> 16]
+    assert np.array_equal(tail, np.array(bits) >= 32768)

@@ -246,3 +246,11 @@ def test_dropout_refusals():
     assert f(ok, r=A + 2) == cb.CAWN_ERR_MISALIGNED and f(ok, d=A + 4) == cb.CAWN_ERR_MISALIGNED
     assert f(make(1 << 50, 0.1, 0)) == cb.CAWN_ERR_UNSUPPORTED
     assert f(make(0, 0.1, 0), x=None) == cb.CAWN_OK
+
+
+def test_the_tests_generator_gives_the_published_answers():
+    from delta_ref import PHILOX_ANSWERS, philox_bits, philox_words
+    for counter, key, answer in PHILOX_ANSWERS:
+        assert tuple(philox_words(counter, key)) == answer
+    counter, key, answer = PHILOX_ANSWERS[0]
+    assert philox_bits(8, 0, 0).tolist() == [half for w in answer for half in (w & 0xFFFF, w >> 16)]
