@@ -327,9 +327,16 @@ def make_delta_params(B, L, Hk, Hv, Dk, Dv, scale=None, flags=0, q_stride=0, k_s
 
 def _dense(names, *arrays):
     """What the kernels take as dense arrays has to be laid out so."""
-    for i, x in enumerate(arrays):
-        if x is not None and not getattr(x, "is_contiguous", _yes)():
-            raise ValueError(f"{names.split()[i]}: strides {tuple(x.stride())} of shape {tuple(x.shape)}, it has to be dense")
+    try:
+        for x in arrays:
+            if x is not None and not x.is_contiguous():
+                break
+        else:
+            return
+    except AttributeError:              # not a tensor (a numpy array): its owner's business
+        return
+    name = next(n for n, y in zip(names.split(), arrays) if y is x)
+    raise ValueError(f"{name}: strides {tuple(x.stride())} of shape {tuple(x.shape)}, it has to be dense")
 
 
 def _yes():
@@ -366,6 +373,12 @@ def _delta_rows(params, q, k, v, o):
     B, L, p = params.B, params.L, params
     if L < 1:
         return params
+    try:                                # the usual cases at once: whole tensors, with no stride given or none that counts
+        if (q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and o.is_contiguous() and
+                (B * L == 1 or not (p.q_stride or p.k_stride or p.v_stride or p.o_stride))):
+            return params
+    except AttributeError:
+        pass
     qk, vo = p.Hk * p.Dk, p.Hv * p.Dv
     for name, x, width, row in (("q_stride", q, qk, p.q_stride), ("k_stride", k, qk, p.k_stride),
                                 ("v_stride", v, vo, p.v_stride), ("o_stride", o, vo, p.o_stride)):
