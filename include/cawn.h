@@ -441,6 +441,14 @@ CAWN_API int cawn_phase_accumulate_fwd_static(const cawn_params *params,
  * g is the log decay, at most 0: e^{g} in [0, 1]; -infinity forgets the state (a packed document's
  * first token).  beta is usually in [0, 1]; the recurrence is stable while beta |k|^2 < 2, which the
  * caller sees to (unit keys).
+ * Precision.  Sums are float.  Calls by token (see cawn_delta_rule_step) compute in float throughout.  Calls by chunk
+ * multiply on the tensor cores: inputs exactly, computed factors (states, corrections, scores) with 16 or more mantissa
+ * bits in bfloat16 storage and 24 in float storage; results are rounded once.  So an error is a part of the terms of a sum,
+ * not of a result in which they cancel: of |S| |q| for o, about 2^-17 (float storage 2^-21); states and the
+ * gradients of g and beta come out within 1e-5 of their norm (float storage: all results), usually 1e-6 to 8e-6.  The
+ * gradient of g is a sum of terms that all carry e^g, so a head with strong decays has it to the same relative accuracy.
+ * Non-finite inputs stay in their batch row and value head (v: in their row of the state); a call by chunk may also spoil
+ * the tokens before a non-finite one in its chunk of 64, counted from the call's first token.
  * Limits: Hv a multiple of Hk, Dk and Dv multiples of 8 up to 128, strides multiples of 8 elements,
  * B * Hv <= 65535 * 64.
  */
@@ -465,8 +473,6 @@ CAWN_API int cawn_delta_rule_workspace_bytes(const cawn_delta_params *params, in
  * Forward for prompts and training.  state_in NULL = zero; state_out NULL = not wanted, may alias
  * state_in.  o may not alias an input.  Short calls run the recurrence token by token, longer ones
  * chunk by chunk, and with few heads the time axis is cut into segments that run side by side.
- * With bfloat16 storage o is rounded once from a sum whose factors (state, corrections, scores) were
- * rounded to bfloat16; the state and everything that feeds it keep 16 or more mantissa bits.
  */
 CAWN_API int cawn_delta_rule_fwd(const cawn_delta_params *params,
                                  const void *q, const void *k, const void *v,

@@ -47,8 +47,9 @@ int pass_state(const cawn_delta_params *p, const float *from, float *to, cudaStr
 }
 
 // Calls of up to this many tokens run token by token.  Step / chunk, us: bfloat16, 12 heads of 64 x 64, 12 tokens
-// 14 / 15, 16 tokens 16 / 15, 24 tokens 21 / 15; 1024 heads of 128 x 128, 16 tokens 102 / 110.  Float storage, whose
-// chunks multiply three terms: 12 heads, 32 tokens 25 / 28, 64 tokens 43 / 30; 1024 heads, 32 tokens 197 / 359.
+// 14 / 13, 17 tokens 16 / 13, 24 tokens 21 / 13; 1024 heads of 128 x 128, 17 tokens 107 / 110, 24 tokens 143 / 112.  Float
+// storage, whose chunks multiply three terms: 12 heads, 33 tokens 25 / 22, 64 tokens 43 / 22; 1024 heads, 33 tokens 199 / 347,
+// 64 tokens 369 / 378.
 inline int step_tokens(const cawn_delta_params *p) { return p->flags != 0 ? 16 : 32; }
 
 // The workspace, front to back; sizes in bytes, every part a multiple of 256.
@@ -72,10 +73,11 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
     w.chunks = (int)((p->L + kC - 1) / kC);
     w.vblocks = (p->Dv + kC - 1) / kC;
     // Time segments where the heads alone leave SMs without a block.  They cost a second walk over values and keys and
-    // the join, so three pay in a forward for long sequences alone.  Three / one, us, bfloat16 heads of 64 x 64: forward,
-    // 49 / 50 heads x 8192 tokens 329 / 366, 49 heads x 2048 110 / 103, x 1024 69 / 58; backward, 24 / 25 heads x 8192
-    // 603 / 732, 24 heads x 2048 191 / 202, x 1024 120 / 116 (float storage, 12 heads x 1024: 177 / 193).  Four, forward,
-    // 36 / 50 heads x 1024: 56 / 58.
+    // the join, so three pay in a forward for long sequences alone.  Three / one, us: forward, 49 heads of 64 in bfloat16 x
+    // 1024 tokens 65 / 60, x 2048 99 / 108, x 4096 175 / 200; 24 of 128 97 / 75, 146 / 138, 247 / 263; 24 of 64 in
+    // float 103 / 95, 175 / 179, 323 / 349.  Backward, 24 of 64 in bfloat16 x 1024 114 / 112, x 2048 183 / 196; 12 of 128
+    // 196 / 181, 298 / 310; 12 of 64 in float 165 / 173, 261 / 296.  Four / one, forward, 36 of 64 in bfloat16 x 1024 50 / 56;
+    // backward, 18 heads 89 / 99.
     const int vw = 16 * (w.terms == 1 ? kRowGroups<1> : kRowGroups<3>);
     const int64_t blocks = (int64_t)p->B * p->Hv * ((p->Dv + vw - 1) / vw) * (backward ? 2 : 1);
     int64_t segs = sm_count() / blocks;

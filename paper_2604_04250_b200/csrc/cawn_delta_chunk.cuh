@@ -22,8 +22,8 @@
 // factor.  The accumulator layout of mma.m16n8k16 is the layout of that operand: the chain stays in one warp's
 // registers.  The right factors (K, Q, T, P tiles) come from shared memory.  Chain warps do what the next
 // chunk waits for, one per scheduler of the SM.  Other warps fetch all tiles (cp.async); in the forward they also make
-// the outputs, which hang off the chain (8 x 2048 x 12 heads: 91 -> 72 us).  (Two warps sharing a row
-// group's chain were slower, 101 us: handing fragments over doubled the shared-memory traffic.)
+// the outputs, which hang off the chain (8 x 2048 x 12 heads, with outputs of one term: 91 -> 72 us).  (Two warps sharing a
+// row group's chain were slower, 101 us: handing fragments over doubled the shared-memory traffic.)
 #pragma once
 #include "cawn_delta.cuh"
 

@@ -5,15 +5,15 @@
 //   S <- e^{G_C} S + (e^{G_C - G} u) K
 // Bound: the chain of these products, chunk after chunk, on the tensor pipes of the SMs that have a head.  The
 // chain's warps do nothing else; side warps make the outputs from the state and the corrections handed to them.
-// Measured: 96 heads of 64 x 64, 2048 tokens, bfloat16: 71 us, 2.2 us a chunk; the tensor pipes of the 96 SMs are busy 56%
-// of the time (a chain warp issues a product every 14 cycles, the pipe takes one every 8).  64 blocks of 128 x 64,
-// 4096 tokens: 199 us.
+// Measured: 96 heads of 64 x 64, 2048 tokens, bfloat16: 87 us, 2.7 us a chunk; the tensor pipes of the 96 SMs are busy 59%
+// of the time with the chain's 220 products and the outputs' 124 a chunk and row group (with 52 for the outputs, whose
+// factors then had 8 bits, 75 us).  64 blocks of 128 x 64, 4096 tokens: 237 us, pipes busy 69%.
 //
 // Few heads leave SMs idle while the chain is long, so the time axis is cut into segments: a chunk acts on
 // a state row s as s <- s M + l, so a first pass computes each segment's M (the same walk over the rows
 // of the identity with V = 0) and l (from a zero state); a small kernel chains them to every segment's
-// start state, and the output pass runs all segments side by side.  12 heads x 32768 tokens in 12 segments: 132 us for
-// the first pass, 18 for the chaining, 93 for the outputs; in one segment the walk took 1.5 ms.
+// start state, and the output pass runs all segments side by side.  12 heads x 32768 tokens in 12 segments: 137 us for
+// the first pass, 18 for the chaining, 127 for the outputs; in one segment the walk took 1.5 ms.
 #include "cawn_delta_chunk.cuh"
 
 #include <type_traits>
