@@ -57,7 +57,7 @@ struct Plan {
     int dk, terms, chunks, vblocks, segs, seg_chunks;    // terms: of an input
     size_t q, k, v, go;                  // three bfloat16 terms each, float storage only
     size_t coef, tri, p;
-    size_t r, s0, rbt;                  // backward: s0 also for the adjoints
+    size_t r, s0, rbt;                  // backward: r also for D K^T, s0 for the adjoints
     size_t seg_state, seg_map;
     size_t total;
 };
@@ -105,11 +105,11 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
     w.p = w.tri;
     if (backward) {
         const double nv = (double)nc * w.vblocks;
-        w.r = part(nv * nt * kTile * 2);
-        w.s0 = part(nv * nt * kC * w.dk * 2);
+        w.r = part(nv * kTile * 4);
+        w.s0 = part(nv * kC * w.dk * 4);
         w.rbt = w.terms == 3 ? w.v : part((double)rows * p->Hv * p->Dv * 2);     // bfloat16: the first of two terms is dV
     }
-    w.total = w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + w.r + 2 * w.s0 + w.rbt + (backward ? 4 : 2) * w.seg_state + w.seg_map;
+    w.total = w.q + w.k + w.v + w.go + w.coef + w.tri + w.p + 2 * (w.r + w.s0) + w.rbt + (backward ? 4 : 2) * w.seg_state + w.seg_map;
     return w;
 }
 
@@ -239,9 +239,10 @@ extern "C" int cawn_delta_rule_bwd(const cawn_delta_params *params, const void *
     C.adj_start = ws.take<float>(w.seg_state);
     C.adj_end = ws.take<float>(w.seg_state);
     C.adj_in = grad_state_out; C.adj_out = grad_state_in;
-    C.r = ws.take<bf16>(w.r);
-    C.s0 = ws.take<bf16>(w.s0);
-    C.ds = ws.take<bf16>(w.s0);
+    C.r = ws.take<float>(w.r);
+    C.dk = ws.take<float>(w.r);
+    C.s0 = ws.take<float>(w.s0);
+    C.ds = ws.take<float>(w.s0);
     C.rbt = ws.take<bf16>(w.rbt);
     C.o = grad_v;
     const long long vo = (long long)params->Hv * params->Dv;

@@ -11,12 +11,12 @@
 // strong.  (As a suffix sum of dO.o - dV.v, which is cheaper, terms of order one cancelled: heads with g = -8 were off by
 // 7e-3 of their gradient, with g = -12 by half of it.)
 //
-// Precision: with bfloat16 storage r, rb and both states come in two terms and pairs of those take all four products.
+// Precision: with bfloat16 storage r, rb and both states enter products in two terms and pairs of those take all four
+// products; z and <S0, D> are float.
 //
 // Bound: the chains of products within a warp, the barriers between them and the trip to memory at the start of a
-// block; all chunks of all key heads at once, two blocks per SM of 64 keys and values in bfloat16 (3072 chunks: 180 us, tensor
-// pipe 37%, shared memory pipe 56%).  At the 128 registers a thread that two blocks leave 236 bytes are spilled; with 255 and
-// one block the same kernel took 12% longer.
+// block; all chunks of all key heads at once, two blocks per SM of 64 keys and values in bfloat16, at the 128 registers a
+// thread that these leave (3072 chunks: 188 us; an earlier form took 12% longer with one block and 255 registers).
 #include "cawn_delta_chunk.cuh"
 
 #include <type_traits>
@@ -33,7 +33,7 @@ template <int DK, int NP> struct GradSmem {
     bf16 q[NP][kC * (DK + kPad)], k[NP][kC * (DK + kPad)];
     union {
         struct {
-            bf16 go[NP][kC * LDV], r[NT][kC * LDV], rb[NT][kC * LDV];
+            bf16 go[NP][kC * LDV], rb[NT][kC * LDV], r[NT][VW * kLd];      // r as value rows
             bf16 s0[NT][VW * (DK + kPad)], ds[NT][VW * (DK + kPad)];
         } v;
         struct {
@@ -42,11 +42,14 @@ template <int DK, int NP> struct GradSmem {
     };
     float coef[kCoef][kC];
     float pairs[8][kC];                     // per warp: its rows' part of the sum over pairs
-    float dots[3][kC];                      // a of the query rows, a of the key rows, z
+    float dots[2][kC];                      // a of the query rows, a of the key rows
     float ends[8];                          // per warp: its part of <S0, D>
-    float4 handed[4][4][32];                // from a query warp to its key warp: accumulators of two column blocks
+    union {
+        float4 handed[4][4][32];            // from a query warp to its key warp: accumulators of two column blocks
+        float z[8][kC];                     // then, per warp, its part of z
+    };
 };
-enum { DOTS_Q = 0, DOTS_K = 1, DOTS_Z = 2 };
+enum { DOTS_Q = 0, DOTS_K = 1 };
 
 // Sum over the four lanes that share a row
 __device__ __forceinline__ float row_sum(float v)
@@ -54,10 +57,60 @@ __device__ __forceinline__ float row_sum(float v)
     v += __shfl_xor_sync(0xffffffffu, v, 1);
     return v + __shfl_xor_sync(0xffffffffu, v, 2);
 }
+// N words of four floats of a thread's share of two arrays with rows of COLS, zero from row `rows` on.
+template <int COLS, int N> __device__ __forceinline__ void fetch_rows(float4 (&x)[N], float4 (&y)[N], const float *from_x, const float *from_y, int rows)
+{
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const int at = i * 256 + threadIdx.x;
+        x[i] = y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (at / (COLS / 4) < rows) {
+            x[i] = reinterpret_cast<const float4 *>(from_x)[at];
+            y[i] = reinterpret_cast<const float4 *>(from_y)[at];
+        }
+    }
+}
+// a word as terms into a tile, planes `plane` elements apart
+template <int NT> __device__ __forceinline__ void put_terms(bf16 *to, int plane, float4 x)
+{
+    unsigned a[NT], b[NT];
+    split(x.x, x.y, a);
+    split(x.z, x.w, b);
+#pragma unroll
+    for (int n = 0; n < NT; n++) *reinterpret_cast<uint2 *>(to + n * plane) = make_uint2(a[n], b[n]);
+}
+// What the walks left of a block of values, from floats to terms in the tiles; <S0, D> and r.(D K^T) in float on the way.
+// (Those dots make the gradients of g where decays are weak, and are often small differences: from products of two
+// terms the gradients of short sequences were off by up to 2e-5.)
+template <int DK, int NP>
+__device__ __forceinline__ void load_floats(GradSmem<DK, NP> &sm, const ChunkParams &P, long long nv, int in, int rows, float &dot, float4 &z)
+{
+    constexpr int NT = GradSmem<DK, NP>::NT, VW = GradSmem<DK, NP>::VW, ld = DK + kPad;
+    float4 s[VW * DK / 1024], d[VW * DK / 1024], x[VW * kC / 1024], y[VW * kC / 1024];
+    fetch_rows<DK>(s, d, P.s0 + nv * (kC * DK) + in * DK, P.ds + nv * (kC * DK) + in * DK, rows);
+    fetch_rows<kC>(x, y, P.r + nv * kTile + in * kC, P.dk + nv * kTile + in * kC, rows);
+#pragma unroll
+    for (int i = 0; i < VW * DK / 1024; i++) {
+        const int at = i * 256 + threadIdx.x, to = at / (DK / 4) * ld + at % (DK / 4) * 4;
+        dot = fmaf(s[i].x, d[i].x, fmaf(s[i].y, d[i].y, fmaf(s[i].z, d[i].z, fmaf(s[i].w, d[i].w, dot))));
+        put_terms<NT>(sm.v.s0[0] + to, VW * ld, s[i]);
+        put_terms<NT>(sm.v.ds[0] + to, VW * ld, d[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < VW * kC / 1024; i++) {
+        const int at = i * 256 + threadIdx.x, to = at / (kC / 4) * kLd + at % (kC / 4) * 4;
+        z.x = fmaf(x[i].x, y[i].x, z.x);
+        z.y = fmaf(x[i].y, y[i].y, z.y);
+        z.z = fmaf(x[i].z, y[i].z, z.z);
+        z.w = fmaf(x[i].w, y[i].w, z.w);
+        put_terms<NT>(sm.v.r[0] + to, VW * kLd, x[i]);
+    }
+}
+
 // x (column blocks nb, nb + 1 of a side's rows) = f (by row half) rows (NA terms, at `left`) x state; dots += x times this
 // thread's places of a tile (NP planes, its row i0 at `own`).  Two column blocks at a time: the left factors are read
-// again for each two, which leaves the registers to the sums.
-template <int DK, int NP, int NA>
+// again for each two, which leaves the registers to the sums.  OF_R: the rows are r's, stored transposed; no dots.
+template <int DK, int NP, int NA, bool OF_R>
 __device__ __forceinline__ void times_state(float (&x)[4][4], int nb, unsigned left, unsigned state, const f32x2 (&f)[2], f32x2 (&dots)[2], const bf16 *own)
 {
     using Smem = GradSmem<DK, NP>;
@@ -70,7 +123,8 @@ __device__ __forceinline__ void times_state(float (&x)[4][4], int nb, unsigned l
 #pragma unroll
     for (int d = 0; d < VW / 16; d++) {
         unsigned a[NA][4], b[2][NT][4];
-        load_left<NA, false>(a, at_kn(left, ldv, 16 * w, 16 * d), kC * ldv);
+        if (OF_R) load_left<NA, true>(a, at_nk(left, kLd, 16 * d, 16 * w), VW * kLd);
+        else load_left<NA, false>(a, at_kn(left, ldv, 16 * w, 16 * d), kC * ldv);
 #pragma unroll
         for (int i = 0; i < 2; i++) load_right<NT, true>(b[i], at_kn(state, ld, 16 * d, 16 * (nb + i)), VW * ld);
         multiply<NA, NT, 2, MORE>(x, a, b);
@@ -80,13 +134,14 @@ __device__ __forceinline__ void times_state(float (&x)[4][4], int nb, unsigned l
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             const f32x2 y = mul2(f[h], pair(x[n][2 * h], x[n][2 * h + 1]));
-            const bf16 *at = own + 8 * h * ld + 16 * nb + 8 * n;
-            f32x2 z = pair(unpack(*reinterpret_cast<const unsigned *>(at)));
-#pragma unroll
-            for (int i = 1; i < NP; i++) z = add2(z, pair(unpack(*reinterpret_cast<const unsigned *>(at + i * (kC * ld)))));
-            dots[h] = fma2(y, z, dots[h]);
             x[n][2 * h] = halves(y).x;
             x[n][2 * h + 1] = halves(y).y;
+            if (OF_R) continue;
+            const bf16 *at = own + 8 * h * ld + 16 * nb + 8 * n;
+            f32x2 k = pair(unpack(*reinterpret_cast<const unsigned *>(at)));
+#pragma unroll
+            for (int i = 1; i < NP; i++) k = add2(k, pair(unpack(*reinterpret_cast<const unsigned *>(at + i * (kC * ld)))));
+            dots[h] = fma2(y, k, dots[h]);
         }
 }
 template <int N> __device__ __forceinline__ void add_tiles(float (*acc)[4], const float (&x)[N][4])
@@ -101,19 +156,19 @@ template <int N> __device__ __forceinline__ void add_tiles(float (*acc)[4], cons
         }
 }
 
-// A side's products with a block of values: X += rows r^T; acc += f rows S0; a and z.  The query side, which has less to do,
-// also makes the key side's e^{G_C - G} u D and hands it over, two column blocks at a time (all of it on the key side: the
-// kernel of 3072 chunks 209 us).
+// A side's products with a block of values: X += rows r^T; acc += f rows S0; a.  The query side, which has less to do,
+// also makes the key side's e^{G_C - G} u D and hands it over, two column blocks at a time (all of it on the key side: 3072
+// chunks 209 us where they now took 180, before r and the states came as floats).
 enum { BAR_HANDED = 1, BAR_TAKEN = 2 };
 template <int DK, int NP, bool QSIDE>
-__device__ __forceinline__ void with_values(GradSmem<DK, NP> &sm, float (&X)[8][4], float (&acc)[DK / 8][4], f32x2 (&a_dots)[2], f32x2 (&z_dots)[2], float scale)
+__device__ __forceinline__ void with_values(GradSmem<DK, NP> &sm, float (&X)[8][4], float (&acc)[DK / 8][4], f32x2 (&dots)[2], float scale)
 {
     using Smem = GradSmem<DK, NP>;
     constexpr int NT = Smem::NT, NA = QSIDE ? NP : NT, MORE = NA == 2 ? 1 : 0, ldv = Smem::LDV, ld = DK + kPad;
     const int lane = threadIdx.x % 32, w = threadIdx.x / 32 % 4, gr = lane / 4, tc = lane % 4 * 2, i0 = 16 * w + gr;
     const unsigned mine = QSIDE ? smem_addr(sm.v.go[0]) : smem_addr(sm.v.rb[0]), rs = smem_addr(sm.v.r[0]);
     const unsigned s0s = smem_addr(sm.v.s0[0]), dss = smem_addr(sm.v.ds[0]);
-    const bf16 *own = (QSIDE ? sm.q[0] : sm.k[0]) + i0 * ld + tc, *keys = sm.k[0] + i0 * ld + tc;
+    const bf16 *own = (QSIDE ? sm.q[0] : sm.k[0]) + i0 * ld + tc;
 #pragma unroll
     for (int d = 0; d < Smem::VW / 16; d++) {
         unsigned a[NA][4];
@@ -122,11 +177,11 @@ __device__ __forceinline__ void with_values(GradSmem<DK, NP> &sm, float (&X)[8][
         for (int nb = 0; nb < 4; nb += 2) {
             if (nb + 1 <= w) {
                 unsigned b[2][NT][4];
-                load_right<NT, false>(b[0], at_nk(rs, ldv, 16 * nb, 16 * d), kC * ldv);
-                load_right<NT, false>(b[1], at_nk(rs, ldv, 16 * nb + 16, 16 * d), kC * ldv);
+                load_right<NT, true>(b[0], at_kn(rs, kLd, 16 * d, 16 * nb), Smem::VW * kLd);
+                load_right<NT, true>(b[1], at_kn(rs, kLd, 16 * d, 16 * nb + 16), Smem::VW * kLd);
                 multiply<NA, NT, 2, MORE>(reinterpret_cast<float (&)[4][4]>(X[2 * nb]), a, b);
             } else if (nb == w) {
-                product<NA, NT, false, MORE>(X[2 * nb], X[2 * nb + 1], a, at_nk(rs, ldv, 16 * nb, 16 * d), kC * ldv);
+                product<NA, NT, true, MORE>(X[2 * nb], X[2 * nb + 1], a, at_kn(rs, kLd, 16 * d, 16 * nb), Smem::VW * kLd);
             }
         }
     }
@@ -138,13 +193,13 @@ __device__ __forceinline__ void with_values(GradSmem<DK, NP> &sm, float (&X)[8][
     for (int nb = 0; nb < DK / 16; nb += 2) {
         float x[4][4];
         if constexpr (QSIDE) {
-            times_state<DK, NP, NT>(x, nb, rs, dss, g, z_dots, keys);
+            times_state<DK, NP, NT, true>(x, nb, rs, dss, g, dots, nullptr);
             if (nb > 0) bar_sync(BAR_TAKEN, 256);
 #pragma unroll
             for (int n = 0; n < 4; n++) sm.handed[w][n][lane] = make_float4(x[n][0], x[n][1], x[n][2], x[n][3]);
             bar_arrive(BAR_HANDED, 256);
         }
-        times_state<DK, NP, NA>(x, nb, mine, s0s, f, a_dots, own);
+        times_state<DK, NP, NA, false>(x, nb, mine, s0s, f, dots, own);
         add_tiles<4>(acc + 2 * nb, x);
         if constexpr (!QSIDE) {
             bar_sync(BAR_HANDED, 256);
@@ -226,7 +281,9 @@ __device__ __forceinline__ void weights(GradSmem<DK, NP> &sm, float (&X)[8][4], 
     *reinterpret_cast<float2 *>(&sm.pairs[threadIdx.x / 32][8 * gr + tc]) = make_float2(sums[0][0], sums[0][1]);
 }
 
-template <int DK, int NP, class T>
+// ONE: one block of values and one value head per key head, so that all sums begin in the block and the registers are free
+// for what is fetched first (3072 chunks: 188 us, in the general form, which spills 456 bytes, 215).
+template <int DK, int NP, bool ONE, class T>
 __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grads_kernel(const ChunkParams P)
 {
     follow_previous();
@@ -236,7 +293,7 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
     auto &sm = *reinterpret_cast<Smem *>(raw);
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, w = warp % 4, gr = lane / 4, tc = lane % 4 * 2;
     const bool qside = warp < 4;
-    const int c = (int)(blockIdx.x % P.chunks), bk = (int)(blockIdx.x / P.chunks), b = bk / P.Hk, hk = bk % P.Hk, rep = P.Hv / P.Hk;
+    const int c = (int)(blockIdx.x % P.chunks), bk = (int)(blockIdx.x / P.chunks), b = bk / P.Hk, hk = bk % P.Hk, rep = ONE ? 1 : P.Hv / P.Hk;
     const long long t0 = (long long)c * kC;
     const int rows = P.L - t0 < kC ? (int)(P.L - t0) : kC;
     const unsigned qs = smem_addr(sm.q[0]), ks = smem_addr(sm.k[0]);
@@ -258,9 +315,10 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
         if (threadIdx.x < kCoef * 16)
             cp16(smem_addr(&sm.coef[0][0]) + threadIdx.x * 16, P.coef + nc * (kCoef * kC) + threadIdx.x * 4, true);
         float X[8][4] = {};                 // dO.r or rb.r, then dP or E
-        f32x2 a_dots[2] = {}, z_dots[2] = {};
+        f32x2 a_dots[2] = {};
         float end = 0.f;
-        for (int v0 = 0; v0 < P.Dv; v0 += VW) {
+        float4 z4 = make_float4(0.f, 0.f, 0.f, 0.f);       // of tokens 4 (lane % 16) ..
+        for (int v0 = 0; v0 < (ONE ? VW : P.Dv); v0 += VW) {
             const int vcols = P.Dv - v0 < VW ? P.Dv - v0 : VW, in = v0 % kC;
             const long long nv = nc * P.vblocks + v0 / kC, here = v_base(P, P.rb, bh, t0) + v0;
 #pragma unroll
@@ -269,29 +327,13 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
             for (int i = 0; i < NT; i++) {
                 const bf16 *rb = NP == 1 && i == 0 ? static_cast<const bf16 *>(P.o) : P.rbt + (i - (NP == 1 ? 1 : 0)) * P.rb.plane;
                 load_tile<kC, VW, 256>(sm.v.rb[i], rb + here, P.rb.stride_t, rows, vcols);
-                load_tile<kC, VW, 256>(sm.v.r[i], P.r + (nv * NT + i) * kTile + in, kC, kC, vcols);
-                load_tile<VW, DK, 256>(sm.v.s0[i], P.s0 + (nv * NT + i) * (kC * DK) + in * DK, DK, vcols, DK);
-                load_tile<VW, DK, 256>(sm.v.ds[i], P.ds + (nv * NT + i) * (kC * DK) + in * DK, DK, vcols, DK);
             }
             cp_commit();
+            load_floats<DK, NP>(sm, P, nv, in, vcols, end, z4);
             cp_wait<0>();
             __syncthreads();
-            if (qside) with_values<DK, NP, true>(sm, X, acc, a_dots, z_dots, P.scale);
-            else with_values<DK, NP, false>(sm, X, acc, a_dots, z_dots, P.scale);
-            for (int i = threadIdx.x; i < VW * (DK / 8); i += 256) {        // <S0, D>
-                const int place = i / (DK / 8) * ld + i % (DK / 8) * 8;
-                unsigned s[NT][4], d[NT][4];
-#pragma unroll
-                for (int n = 0; n < NT; n++) {
-                    *reinterpret_cast<uint4 *>(s[n]) = *reinterpret_cast<const uint4 *>(&sm.v.s0[n][place]);
-                    *reinterpret_cast<uint4 *>(d[n]) = *reinterpret_cast<const uint4 *>(&sm.v.ds[n][place]);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const float2 x = sum_terms(s, e), y = sum_terms(d, e);
-                    end = fmaf(x.x, y.x, fmaf(x.y, y.y, end));
-                }
-            }
+            if (qside) with_values<DK, NP, true>(sm, X, acc, a_dots, P.scale);
+            else with_values<DK, NP, false>(sm, X, acc, a_dots, P.scale);
             __syncthreads();        // the value tiles are free
         }
 
@@ -300,11 +342,15 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
         else weights<DK, NP, false>(sm, X, xa, P.scale, P.gbeta + at, P.Hv, rows);
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            const float2 ah = halves(a_dots[h]), zh = halves(z_dots[h]);
-            const float a = row_sum(ah.x + ah.y), z = row_sum(zh.x + zh.y);
+            const float2 ah = halves(a_dots[h]);
+            const float a = row_sum(ah.x + ah.y);
             if (tc == 0) sm.dots[qside ? DOTS_Q : DOTS_K][i0 + 8 * h] = a;
-            if (tc == 0 && qside) sm.dots[DOTS_Z][i0 + 8 * h] = z;
         }
+        z4.x += __shfl_xor_sync(0xffffffffu, z4.x, 16);
+        z4.y += __shfl_xor_sync(0xffffffffu, z4.y, 16);
+        z4.z += __shfl_xor_sync(0xffffffffu, z4.z, 16);
+        z4.w += __shfl_xor_sync(0xffffffffu, z4.w, 16);
+        if (lane < 16) *reinterpret_cast<float4 *>(&sm.z[warp][4 * lane]) = z4;
 #pragma unroll
         for (int o = 16; o > 0; o /= 2) end += __shfl_xor_sync(0xffffffffu, end, o);
         if (lane == 0) sm.ends[warp] = end;
@@ -343,7 +389,9 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
                 const int t = 2 * lane + e;
                 for (int i = 0; i < 8; i++) pairs[e] += sm.pairs[i][t];
                 a[e] = sm.dots[DOTS_Q][t] + sm.dots[DOTS_K][t];
-                z[e] = sm.dots[DOTS_Z][t];
+                z[e] = 0.f;
+                for (int i = 0; i < 8; i++) z[e] += sm.z[i][t];
+                z[e] *= sm.coef[COEF_LEFT][t] * sm.coef[COEF_BETA][t];
             }
             float after = a[0] + a[1], before = z[0] + z[1];
 #pragma unroll
@@ -380,12 +428,12 @@ __global__ void __launch_bounds__(256, (DK == 64 && NP == 1 ? 2 : 1)) delta_grad
         }
 }
 
-template <int DK, int NP> cudaError_t grads(const ChunkParams &P, cudaStream_t st)
+template <int DK, int NP, bool ONE> cudaError_t grads(const ChunkParams &P, cudaStream_t st)
 {
     using T = typename std::conditional<NP == 1, bf16, float>::type;
     const size_t smem = sizeof(GradSmem<DK, NP>);
     static_assert(sizeof(GradSmem<DK, NP>) <= 227 * 1024, "fits an SM");
-    auto *kernel = delta_grads_kernel<DK, NP, T>;
+    auto *kernel = delta_grads_kernel<DK, NP, ONE, T>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     return launch(kernel, dim3((unsigned)(P.B * P.Hk * (long long)P.chunks)), dim3(256), smem, st, P);
@@ -395,8 +443,9 @@ template <int DK, int NP> cudaError_t grads(const ChunkParams &P, cudaStream_t s
 
 cudaError_t launch_delta_grads(const ChunkParams &P, int dk, int terms, cudaStream_t st)
 {
-    if (dk == 64) return terms == 1 ? grads<64, 1>(P, st) : grads<64, 3>(P, st);
-    return terms == 1 ? grads<128, 1>(P, st) : grads<128, 3>(P, st);
+    if (dk == 64 && terms == 1) return P.Hk == P.Hv && P.Dv <= kGradVW<64, 1> ? grads<64, 1, true>(P, st) : grads<64, 1, false>(P, st);
+    if (dk == 64) return grads<64, 3, false>(P, st);
+    return terms == 1 ? grads<128, 1, false>(P, st) : grads<128, 3, false>(P, st);
 }
 
 }  // namespace cawn

@@ -50,9 +50,10 @@ struct ChunkParams {
     const float *g, *beta;
     float *coef;                        // [nc][kCoef][64]
     bf16 *tri, *p;                      // [nc][NT][kTri]: T - I, transposed, and P, see in_triangle
-    // What the backward's walks leave for the chunk-local products, NT terms each: r as token rows, the state before the
-    // chunk and the adjoint of the one after it as value rows
-    bf16 *r, *s0, *ds;                  // [nv][NT][64 t][64 v], [nv][NT][64 v][DK] twice
+    // What the backward's walks leave for the chunk-local products, value rows: the state before the chunk, the adjoint D
+    // of the one after it, r and D K^T
+    float *s0, *ds;                     // [nv][64 v][DK]
+    float *r, *dk;                      // [nv][64 v][64 t]
     bf16 *rbt;                          // and rb, laid out like v; with bfloat16 storage the first term is dV itself (o)
     Terms rb;                           // its plane and strides
     const float *state_in;              // [bh][Dv][Dk], may be NULL
@@ -420,19 +421,14 @@ template <int DK> __device__ __forceinline__ void store_state(float *to, const f
             if (r + 8 * h < rows && 8 * n + tc < Dk)
                 *reinterpret_cast<float2 *>(to + (long long)(r + 8 * h) * Dk + 8 * n + tc) = make_float2(S[n][2 * h], S[n][2 * h + 1]);
 }
-// a state's rows in NP terms, rows of DK elements
-template <int NP, int DK> __device__ __forceinline__ void store_rows(bf16 *to, const float (&S)[DK / 8][4])
+// a row group's value rows, 8 N floats each
+template <int N> __device__ __forceinline__ void store_rows(float *to, const float (&x)[N][4])
 {
-    to += threadIdx.x % 32 / 4 * DK + threadIdx.x % 4 * 2;
+    to += threadIdx.x % 32 / 4 * (8 * N) + threadIdx.x % 4 * 2;
 #pragma unroll
-    for (int n = 0; n < DK / 8; n++)
+    for (int n = 0; n < N; n++)
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            unsigned x[NP];
-            split(S[n][2 * h], S[n][2 * h + 1], x);
-#pragma unroll
-            for (int i = 0; i < NP; i++) *reinterpret_cast<unsigned *>(to + i * (kC * DK) + 8 * h * DK + 8 * n) = x[i];
-        }
+        for (int h = 0; h < 2; h++) *reinterpret_cast<float2 *>(to + 8 * h * (8 * N) + 8 * n) = make_float2(x[n][2 * h], x[n][2 * h + 1]);
 }
 // Value head's place
 __device__ __forceinline__ long long q_base(const ChunkParams &P, const Terms &t, int bh, long long t0)

@@ -4,11 +4,11 @@
 //   X = S K^T,  R = V^T - e^G X,  r = R T^T,  u = beta r,  S <- e^{G_C} S + (e^{G_C - G} u) K,
 // and the reverse walk, with D the adjoint of the state after a chunk,
 //   dU = P^T dO + e^{G_C - G} (K D^T),   rb = T^T (beta dU),   D <- e^{G_C} D + (scale e^G dO)^T Q - (e^G rb)^T K.
-// Neither needs the other, and all sums over both are left to the chunk-local kernel.  They leave r, rb and both states
-// in bfloat16 terms.  Bound: each walk is a chain of products and of the instructions between them, on the SMs that
+// Neither needs the other, and all sums over both are left to the chunk-local kernel.  They leave r, D K^T and both
+// states as floats, and rb.  Bound: each walk is a chain of products and of the instructions between them, on the SMs that
 // have a head.  One launch runs both, the reverse ones, which take longer, first: with few heads each walk has an SM of
 // its own, with many the forward walks fill the SMs that the reverse ones leave or come free first (96 heads of 64 x 64,
-// 2048 tokens, bfloat16: 177 us, of which a reverse walk takes 126 and a forward one 88; tensor pipes busy 48%).
+// 2048 tokens, bfloat16: 151 us; with r and the states converted to bfloat16 terms here 177).
 // A block is 16 * row groups of values of one head and one direction.  Warps of their own fetch the tiles (with the
 // chain warps fetching, either walk of 96 heads took 153 us instead of 127), a chunk ahead where shared memory holds
 // two sets; else the tiles that a chunk starts with come a chunk ahead and the others when it starts.
@@ -127,8 +127,8 @@ template <class Plan> __device__ __forceinline__ void late_tiles(bool walks)
     __syncthreads();
 }
 
-// A thread's accumulators as token rows of 16 values per warp: through shared memory (`way`, this warp's own columns), in
-// N terms; `put(term, t, from)`: eight values of token t.
+// A thread's accumulators as token rows of 16 values per warp, in N terms, through shared memory (`way`, this warp's own
+// columns); `put(term, t, v, x)`: eight values of token t, from value v of the warp's on.
 template <int N, class Put> __device__ __forceinline__ void token_rows(const float (&x)[8][4], bf16 *way, int ld, int col, Put put)
 {
     const int lane = threadIdx.x % 32;
@@ -196,7 +196,7 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
         float X[8][4] = {};
         if (walks) {
             rows_times<3, NP, DK>(X, S, ks);
-            if constexpr (!SUMMARY) store_rows<NT, DK>(P.s0 + nv * (NT * kC * DK) + 16 * w4 * DK, S);
+            if constexpr (!SUMMARY) store_rows(P.s0 + nv * (kC * DK) + 16 * w4 * DK, S);
             residual<NP>(X, e.coef, smem_addr(e.v[0]), VLD, 16 * w, vcols > 0);
         }
         late_tiles<Plan>(walks);
@@ -208,10 +208,7 @@ __device__ __forceinline__ void forward_walk(const ChunkParams &P, unsigned char
             for (int j = 0; j < 4; j++) r[n][j] = X[n][j];
         triangle<3, NT, true, false>(r, [&](unsigned (&a)[3][4], int tb) { as_left(X[2 * tb], X[2 * tb + 1], a); },
                                      [&](int tb, int nb) { return triangle_kn(smem_addr(late.tri[0]), nb, tb); });
-        if constexpr (!SUMMARY)             // by way of this warp's own part of the V tile, which is done with
-            token_rows<NT>(r, e.v[0], VLD, 16 * w, [&](int term, int t, int v, uint4 x) {
-                *reinterpret_cast<uint4 *>(P.r + (nv * NT + term) * kTile + t * kC + 16 * w4 + v) = x;
-            });
+        if constexpr (!SUMMARY) store_rows(P.r + nv * kTile + 16 * w4 * kC, r);
         scale_tokens(r, e.coef, COEF_BETA);
         // the update is summed from zero and added once, as in the forward
         const float eC = e.coef[COEF_EG][kC - 1];
@@ -280,7 +277,10 @@ __device__ __forceinline__ void reverse_walk(const ChunkParams &P, unsigned char
         float X[8][4] = {};
         if (walks) {
             rows_times<3, NP, DK>(X, D, ks);
-            if constexpr (!SUMMARY) store_rows<NT, DK>(P.ds + nv * (NT * kC * DK) + 16 * w4 * DK, D);
+            if constexpr (!SUMMARY) {
+                store_rows(P.ds + nv * (kC * DK) + 16 * w4 * DK, D);
+                store_rows(P.dk + nv * kTile + 16 * w4 * kC, X);
+            }
             scale_tokens(X, e.coef, COEF_LEFT);
             triangle<NP, NT, true, true>(X, [&](unsigned (&a)[NP][4], int ib) { load_left<NP, true>(a, at_nk(gs, VLD, 16 * ib, 16 * w), kC * VLD); },
                                          [&](int ib, int nb) { return triangle_kn(smem_addr(e.p[0]), ib, nb); });

@@ -627,3 +627,14 @@ def test_calls_keep_to_their_workspace(shape, dtype):
                                    ws[:n], state_in=c["state_in"], grad_state_out=c["grad_state_out"], grad_state_in=out["state_in"])
             assert all(torch.equal(out[m], want_g[m]) for m in out)
         assert (ws[n:] == 0xA5).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_backward_gradient_of_g_where_little_is_left_of_the_states(dtype):
+    """Many short sequences, each head held to its own size: some have a small <state, adjoint>, a difference of large
+    terms.  With three terms of both a head's error is that of the other sums, 2^-17 of a few."""
+    for seed, shape in ((1, (24, 34, 2, 2, 128, 128)), (2, (16, 63, 4, 4, 64, 64)), (3, (16, 33, 4, 8, 40, 24))):
+        d = delta_inputs(*shape, dtype, seed=seed)
+        got, want = backward(d)["g"], reference_grads(d)["g"]
+        for b in range(shape[0]):
+            close(got[b], want[b], STATE_TOL, (seed, b))
