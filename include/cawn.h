@@ -444,8 +444,8 @@ CAWN_API int cawn_phase_accumulate_fwd_static(const cawn_params *params,
  * Precision.  Sums are float.  Calls by token (see cawn_delta_rule_step) compute in float throughout.  Calls by chunk
  * multiply on the tensor cores: inputs exactly, computed factors (states, corrections, scores) with 16 or more mantissa
  * bits in bfloat16 storage and 24 in float storage; results are rounded once.  So an error is a part of the terms of a sum,
- * not of a result in which they cancel: of |S| |q| for o, about 2^-17 (float storage 2^-21); states and the
- * gradients of g and beta come out within 1e-5 of their norm (float storage: all results), usually 1e-6 to 8e-6.  The
+ * not of a result in which they cancel: of |S| |q| for o, about 2^-17 (float storage 2^-21).  States and the
+ * gradients of g and beta come out within 1e-6 to 9e-6 of their norm (float storage: all results, 1e-6 to 4e-6).  The
  * gradient of g is a sum of terms that all carry e^g, so a head with strong decays has it to the same relative accuracy.
  * Non-finite inputs stay in their batch row and value head (v: in their row of the state); a call by chunk may also spoil
  * the tokens before a non-finite one in its chunk of 64, counted from the call's first token.

@@ -75,9 +75,9 @@ Plan plan_of(const cawn_delta_params *p, bool backward)
     // Time segments where the heads alone leave SMs without a block.  They cost a second walk over values and keys and
     // the join, so three pay in a forward for long sequences alone.  Three / one, us: forward, 49 heads of 64 in bfloat16 x
     // 1024 tokens 65 / 60, x 2048 99 / 108, x 4096 175 / 200; 24 of 128 97 / 75, 146 / 138, 247 / 263; 24 of 64 in
-    // float 103 / 95, 175 / 179, 323 / 349.  Backward, 24 of 64 in bfloat16 x 1024 114 / 112, x 2048 183 / 196; 12 of 128
-    // 196 / 181, 298 / 310; 12 of 64 in float 165 / 173, 261 / 296.  Four / one, forward, 36 of 64 in bfloat16 x 1024 50 / 56;
-    // backward, 18 heads 89 / 99.
+    // float 103 / 95, 175 / 179, 323 / 349.  Backward, 24 of 64 in bfloat16 x 1024 116 / 114, x 2048 183 / 196; 12 of 128
+    // 188 / 171, 290 / 298; 12 of 64 in float 165 / 171, 261 / 290.  Four / one, forward, 36 of 64 in bfloat16 x 1024 50 / 56;
+    // backward, 18 heads 87 / 97.
     const int vw = 16 * (w.terms == 1 ? kRowGroups<1> : kRowGroups<3>);
     const int64_t blocks = (int64_t)p->B * p->Hv * ((p->Dv + vw - 1) / vw) * (backward ? 2 : 1);
     int64_t segs = sm_count() / blocks;
