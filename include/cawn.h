@@ -569,6 +569,184 @@ typedef struct cawn_dropout_params {
 CAWN_API int cawn_dropout(const cawn_dropout_params *params, const void *x, const void *residual,
                           void *y, const uint64_t *offset_device, void *cuda_stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Operators of a selective state space layer: a short causal convolution, the scan behind it, and
+ * the norm in front of both.  The rules above hold (storage flags, float sums and states, 16-byte
+ * aligned pointers unless said otherwise, plain workspaces, no atomics: bitwise repeatable).
+ *
+ * Sequences.  Arrays of rows hold B sequences, either of L rows each (offsets NULL, rows 0), or
+ * packed: `offsets` (device, int64, B + 1 values that do not fall) says that sequence b has the rows
+ * offsets[b] .. offsets[b+1] - 1, `rows` how many rows the arrays have, and L how many tokens the
+ * longest sequence has.  A sequence may be empty.  The device clamps offsets to the arrays' rows and
+ * a sequence to its first L tokens.  Rows that no sequence has are neither read nor written, in no
+ * direction.  States have one entry per sequence; an empty sequence passes its state on.
+ * ------------------------------------------------------------------------------------------ */
+
+/*
+ * Short causal convolution of each channel over time, with its history:
+ *   z_t = bias_c + sum_k weight[c,k] x_{t-(K-1)+k}       bias NULL = 0
+ *   y_t = z_t | z_t sigmoid(z_t)                         by `act`
+ * Rows in front of a sequence are its history state_in [B, K-1, C] float (NULL = 0; the oldest row
+ * first); state_out receives the last K-1 rows of (history, sequence) and may alias state_in.
+ * x: [rows, C], rows x_stride elements apart (0 = dense); y [rows, C] dense, not aliasing x.
+ * weight [C, K], bias [C] float.  Single tokens are calls with L = 1.
+ */
+enum { CAWN_CONV_ACT_NONE = 0, CAWN_CONV_ACT_SILU = 1 };
+
+typedef struct cawn_conv_params {
+    uint32_t struct_size;
+    int32_t  B;              /* sequences >= 1                                                   */
+    int64_t  L;              /* tokens of the longest sequence, >= 0                             */
+    int32_t  C;              /* channels >= 1                                                    */
+    int32_t  K;              /* taps, 1..4                                                       */
+    int32_t  act;            /* CAWN_CONV_ACT_*                                                  */
+    uint32_t flags;          /* 0, or CAWN_FLAG_INPUT_BF16 | CAWN_FLAG_OUTPUT_BF16: x, y and their
+                                gradients are bfloat16                                           */
+    uint32_t reserved[2];    /* 0                                                                */
+    int64_t  x_stride;       /* elements from one row of x to the next; 0 = dense                */
+    int64_t  rows;           /* packed: rows of the arrays; otherwise 0                          */
+} cawn_conv_params;
+
+CAWN_API int cawn_short_conv_fwd(const cawn_conv_params *params, const void *x, const float *weight,
+                                 const float *bias, const float *state_in, const int64_t *offsets,
+                                 void *y, float *state_out, void *cuda_stream);
+
+/* Host-only size query for cawn_short_conv_bwd; enough for every B and L up to the given ones. */
+CAWN_API int cawn_short_conv_workspace_bytes(const cawn_conv_params *params, size_t *bytes);
+
+/* Backward; what the activation needs is recomputed from x.  grad_y, grad_x [rows, C] dense.
+ * grad_state_out: gradient of state_out or NULL (= 0).  grad_weight, grad_bias, grad_state_in: float
+ * or NULL.  The workspace is used for grad_weight and grad_bias only and may be NULL when neither is
+ * wanted.  Outputs may not alias inputs or each other. */
+CAWN_API int cawn_short_conv_bwd(const cawn_conv_params *params, const void *x, const float *weight,
+                                 const float *bias, const float *state_in, const int64_t *offsets,
+                                 const void *grad_y, const float *grad_state_out,
+                                 void *grad_x, float *grad_weight, float *grad_bias, float *grad_state_in,
+                                 void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Selective scan: per channel c a state of N floats whose decay and input depend on the token.
+ *   d_t  = softplus(dt_t + dt_bias), or dt_t + dt_bias with softplus = 0      (dt_bias NULL = 0)
+ *   h_t  = exp(d_t A[c,n]) h_{t-1} + d_t x_t B_t[n]                           h_{-1} = state_in (0 when NULL)
+ *   y_t  = (sum_n C_t[n] h_t[n] + skip_c x_t) silu(z_t)                       skip NULL = 0; z NULL: no gate
+ *   state_out = h_{L-1}
+ * Shapes.  x, dt, z, y [rows, D]; B, C [rows, G, N], channel c reads group c / (D/G); A [D, N] float
+ * (usually negative); skip, dt_bias [D] float; states [B, D, N] float.  Rows of x, dt, z, B and C lie
+ * *_stride elements apart (0 = dense), so that they may be slices of projections; B and C need only be
+ * aligned to their elements (whole words are read where they are aligned to four of them).
+ * Precision.  Everything is computed in float; results are rounded once to their type.  The
+ * backward's sums over channels (gradients of B and C) take terms of 22 bits of mantissa.
+ * Non-finite values stay in their sequence and in the channels of their group; gradients of B and C may
+ * also be spoilt in the 8 tokens (N > 32: 4), counted from the sequence's first, around one.
+ * Limits: N <= 64, G <= 65535.
+ */
+typedef struct cawn_scan_params {
+    uint32_t struct_size;
+    int32_t  B;              /* sequences >= 1                                                   */
+    int64_t  L;              /* tokens of the longest sequence, >= 0                             */
+    int32_t  D;              /* channels >= 1                                                    */
+    int32_t  N;              /* states of a channel, 1..64                                       */
+    int32_t  G;              /* groups that share B and C; divides D                             */
+    int32_t  softplus;       /* 0 or 1                                                           */
+    uint32_t flags;          /* 0, or CAWN_FLAG_INPUT_BF16 | CAWN_FLAG_OUTPUT_BF16: x, dt, z, B, C,
+                                y and their gradients are bfloat16                               */
+    uint32_t reserved;       /* 0                                                                */
+    int64_t  x_stride, dt_stride, z_stride, b_stride, c_stride;
+    int64_t  rows;           /* packed: rows of the arrays; otherwise 0                          */
+} cawn_scan_params;
+
+/* `op` of cawn_selective_scan_workspace_bytes. */
+enum {
+    CAWN_SCAN_FWD = 0,           /* workspace of cawn_selective_scan_fwd (may be 0 bytes)         */
+    CAWN_SCAN_BWD = 1,           /* workspace of cawn_selective_scan_bwd with checkpoints          */
+    CAWN_SCAN_BWD_RECOMPUTE = 2, /* ... without: adds room for states that are found again         */
+    CAWN_SCAN_CHECKPOINTS = 3    /* size of the checkpoints that a forward can leave for it        */
+};
+
+/* Host-only size query; enough for every B, L and rows up to the given ones. */
+CAWN_API int cawn_selective_scan_workspace_bytes(const cawn_scan_params *params, int op, size_t *bytes);
+
+/*
+ * Forward for prompts and training.  With few channels and long sequences the time axis is cut into
+ * segments that run side by side.  state_in NULL = zero; state_out NULL = not wanted, may alias
+ * state_in.  y may not alias an input.  checkpoints: the states of every 16th token, for the backward
+ * of the same params and inputs, or NULL.
+ */
+CAWN_API int cawn_selective_scan_fwd(const cawn_scan_params *params, const void *x, const void *dt, const float *A,
+                                     const void *B, const void *C, const float *skip, const float *dt_bias,
+                                     const void *z, const float *state_in, const int64_t *offsets,
+                                     void *y, float *state_out, float *checkpoints,
+                                     void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * The same operation token by token, for decoding: one token (or a few) of B sequences of L tokens each, with
+ * the states read and written once.  No workspace.  Any L; meant for short ones.
+ */
+CAWN_API int cawn_selective_scan_step(const cawn_scan_params *params, const void *x, const void *dt, const float *A,
+                                      const void *B, const void *C, const float *skip, const float *dt_bias,
+                                      const void *z, const float *state_in,
+                                      void *y, float *state_out, void *cuda_stream);
+
+/*
+ * Backward.  checkpoints: what the forward left, or NULL (the states are then found again, for the time of
+ * about a forward and with the larger workspace).  grad_y [rows, D] dense; grad_state_out: gradient of
+ * state_out or NULL (= 0).  grad_x, grad_dt, grad_z [rows, D] and grad_B, grad_C [rows, G, N] (summed over
+ * the group's channels): dense, the type of the inputs; grad_z goes with z.  grad_A [D, N], grad_skip,
+ * grad_dt_bias [D], grad_state_in [B, D, N]: float; the last three may be NULL.  Outputs may not alias
+ * inputs or each other.
+ */
+CAWN_API int cawn_selective_scan_bwd(const cawn_scan_params *params, const void *x, const void *dt, const float *A,
+                                     const void *B, const void *C, const float *skip, const float *dt_bias,
+                                     const void *z, const float *state_in, const int64_t *offsets,
+                                     const float *checkpoints, const void *grad_y, const float *grad_state_out,
+                                     void *grad_x, void *grad_dt, float *grad_A, void *grad_B, void *grad_C,
+                                     float *grad_skip, float *grad_dt_bias, void *grad_z, float *grad_state_in,
+                                     void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Root-mean-square norm of the stream that a branch is added to:
+ *   s = x + residual (residual NULL = 0), rounded to the stream's type;  sum_out = s (NULL = not wanted)
+ *   y = s / sqrt(mean(s^2) + eps) * weight                               weight [M] float, NULL = 1
+ * x [N, M], rows x_stride elements apart (0 = dense); residual, sum_out: [N, M] dense in the stream's
+ * type, which is that of x, or float with stream_float.  sum_out may alias residual, or x where x is
+ * dense and of the stream's type.  y [N, M] dense, by `out`:
+ *   CAWN_NORM_OUT_SAME   the type of x (may alias x where x is dense; scales NULL)
+ *   CAWN_NORM_OUT_E4M3   8-bit floats (4 bits of exponent, 3 of mantissa, largest value 448) with a
+ *                        scale per scale_block channels of a row (32, 64 or 128; the last may be fewer)
+ *                        or per row (0):  scale = max(max |y|, 1e-30) / 448,  stored = y / scale,
+ *                        rounded to nearest even from the float value.  scales [N, ceil(M/scale_block)]
+ *                        or [N] float.  A NaN in a block makes the block's scale NaN.
+ */
+enum { CAWN_NORM_OUT_SAME = 0, CAWN_NORM_OUT_E4M3 = 1 };
+
+typedef struct cawn_residual_norm_params {
+    uint32_t struct_size;
+    int32_t  M;              /* channels, 1..8192                                                */
+    int64_t  N;              /* rows >= 0                                                        */
+    float    eps;            /* >= 0                                                             */
+    int32_t  out;            /* CAWN_NORM_OUT_*                                                  */
+    int32_t  scale_block;    /* 0, 32, 64 or 128                                                 */
+    int32_t  stream_float;   /* 1: the stream is float though flags say bfloat16                 */
+    uint32_t flags;          /* 0, or CAWN_FLAG_INPUT_BF16 | CAWN_FLAG_OUTPUT_BF16               */
+    uint32_t reserved;       /* 0                                                                */
+    int64_t  x_stride;
+} cawn_residual_norm_params;
+
+CAWN_API int cawn_residual_norm_fwd(const cawn_residual_norm_params *params, const void *x, const void *residual,
+                                    const float *weight, void *sum_out, void *y, float *scales, void *cuda_stream);
+
+/* Host-only size query for cawn_residual_norm_bwd; enough for every N up to the given one. */
+CAWN_API int cawn_residual_norm_workspace_bytes(const cawn_residual_norm_params *params, size_t *bytes);
+
+/* Backward, from the sum that the forward left (`out`, scale_block and x_stride are not looked at: a rounding to 8 bits
+ * is passed straight through).  grad_y [N, M] in the type of x; grad_sum: gradient of sum_out in the stream's type,
+ * or NULL (= 0).  The gradient of x and of the residual is the same: grad_residual in the stream's type, grad_x in
+ * that of x, either may be NULL.  grad_residual may alias grad_sum (and grad_y where the types are the same),
+ * grad_x may alias grad_y.  grad_weight [M] float or NULL; the workspace is used for it only. */
+CAWN_API int cawn_residual_norm_bwd(const cawn_residual_norm_params *params, const void *sum, const float *weight,
+                                    const void *grad_y, const void *grad_sum, void *grad_residual, void *grad_x,
+                                    float *grad_weight, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

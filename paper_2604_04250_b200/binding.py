@@ -35,6 +35,9 @@ CAWN_OP_FWD, CAWN_OP_BWD_SAVED, CAWN_OP_BWD_PUSHES, CAWN_OP_STATE, CAWN_OP_FWD_H
 CAWN_SAVED_STATES, CAWN_SAVED_PUSHES = 0, 1
 CAWN_DELTA_FWD, CAWN_DELTA_BWD = 0, 1
 CAWN_NORM_ACT_NONE, CAWN_NORM_ACT_SILU, CAWN_NORM_ACT_GATE = range(3)
+CAWN_CONV_ACT_NONE, CAWN_CONV_ACT_SILU = range(2)
+CAWN_SCAN_FWD, CAWN_SCAN_BWD, CAWN_SCAN_BWD_RECOMPUTE, CAWN_SCAN_CHECKPOINTS = range(4)
+CAWN_NORM_OUT_SAME, CAWN_NORM_OUT_E4M3 = range(2)
 
 EXPORTS = (
     "cawn_status_string", "cawn_workspace_bytes", "cawn_workspace_init",
@@ -44,6 +47,9 @@ EXPORTS = (
     "cawn_workspace_set_wait_hook", "cawn_mixing_bwd_dynamic",
     "cawn_delta_rule_workspace_bytes", "cawn_delta_rule_fwd", "cawn_delta_rule_step", "cawn_delta_rule_bwd",
     "cawn_group_norm_fwd", "cawn_group_norm_workspace_bytes", "cawn_group_norm_bwd", "cawn_dropout",
+    "cawn_short_conv_fwd", "cawn_short_conv_workspace_bytes", "cawn_short_conv_bwd",
+    "cawn_selective_scan_workspace_bytes", "cawn_selective_scan_fwd", "cawn_selective_scan_step", "cawn_selective_scan_bwd",
+    "cawn_residual_norm_fwd", "cawn_residual_norm_workspace_bytes", "cawn_residual_norm_bwd",
 )
 
 
@@ -109,6 +115,56 @@ class cawn_dropout_params(ctypes.Structure):
     ]
 
 
+class cawn_conv_params(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("B", ctypes.c_int32),
+        ("L", ctypes.c_int64),
+        ("C", ctypes.c_int32),
+        ("K", ctypes.c_int32),
+        ("act", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+        ("reserved", ctypes.c_uint32 * 2),
+        ("x_stride", ctypes.c_int64),
+        ("rows", ctypes.c_int64),
+    ]
+
+
+class cawn_scan_params(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("B", ctypes.c_int32),
+        ("L", ctypes.c_int64),
+        ("D", ctypes.c_int32),
+        ("N", ctypes.c_int32),
+        ("G", ctypes.c_int32),
+        ("softplus", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+        ("reserved", ctypes.c_uint32),
+        ("x_stride", ctypes.c_int64),
+        ("dt_stride", ctypes.c_int64),
+        ("z_stride", ctypes.c_int64),
+        ("b_stride", ctypes.c_int64),
+        ("c_stride", ctypes.c_int64),
+        ("rows", ctypes.c_int64),
+    ]
+
+
+class cawn_residual_norm_params(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("M", ctypes.c_int32),
+        ("N", ctypes.c_int64),
+        ("eps", ctypes.c_float),
+        ("out", ctypes.c_int32),
+        ("scale_block", ctypes.c_int32),
+        ("stream_float", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+        ("reserved", ctypes.c_uint32),
+        ("x_stride", ctypes.c_int64),
+    ]
+
+
 class CawnError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -153,6 +209,17 @@ def lib():
         L.cawn_group_norm_workspace_bytes.argtypes = [np_, ctypes.POINTER(sz)]
         L.cawn_group_norm_bwd.argtypes = [np_, vp, fp, fp, vp, vp, vp, vp, fp, fp, vp, sz, vp]
         L.cawn_dropout.argtypes = [op, vp, vp, vp, vp, vp]
+        cp, sp, rp = ctypes.POINTER(cawn_conv_params), ctypes.POINTER(cawn_scan_params), ctypes.POINTER(cawn_residual_norm_params)
+        L.cawn_short_conv_fwd.argtypes = [cp, vp, fp, fp, fp, vp, vp, fp, vp]
+        L.cawn_short_conv_workspace_bytes.argtypes = [cp, ctypes.POINTER(sz)]
+        L.cawn_short_conv_bwd.argtypes = [cp, vp, fp, fp, fp, vp, vp, fp, vp, fp, fp, fp, vp, sz, vp]
+        L.cawn_selective_scan_workspace_bytes.argtypes = [sp, ctypes.c_int, ctypes.POINTER(sz)]
+        L.cawn_selective_scan_fwd.argtypes = [sp, vp, vp, fp, vp, vp, fp, fp, vp, fp, vp, vp, fp, fp, vp, sz, vp]
+        L.cawn_selective_scan_step.argtypes = [sp, vp, vp, fp, vp, vp, fp, fp, vp, fp, vp, fp, vp]
+        L.cawn_selective_scan_bwd.argtypes = [sp, vp, vp, fp, vp, vp, fp, fp, vp, fp, vp, fp, vp, fp, vp, vp, fp, vp, vp, fp, fp, vp, fp, vp, sz, vp]
+        L.cawn_residual_norm_fwd.argtypes = [rp, vp, vp, fp, vp, vp, fp, vp]
+        L.cawn_residual_norm_workspace_bytes.argtypes = [rp, ctypes.POINTER(sz)]
+        L.cawn_residual_norm_bwd.argtypes = [rp, vp, fp, vp, vp, vp, vp, fp, vp, sz, vp]
         for name in EXPORTS:
             if name != "cawn_status_string":
                 getattr(L, name).restype = ctypes.c_int
@@ -491,3 +558,158 @@ def cawn_dropout(params, x, y, residual=None, offset_device=None, stream=None):
     _dense("x y residual", x, y, residual)
     _check(lib().cawn_dropout(ctypes.byref(params), _dp(x), _dp(residual), _dp(y), _dp(offset_device), _stream(stream)),
            "cawn_dropout")
+
+
+# ---- operators of a selective state space layer
+
+def make_conv_params(B, L, C, K, act=CAWN_CONV_ACT_NONE, flags=0, x_stride=0, rows=0):
+    return cawn_conv_params(ctypes.sizeof(cawn_conv_params), B, L, C, K, act, flags, (0, 0), x_stride, rows)
+
+
+def _sequence_rows(params, offsets, arrays):
+    """Rows of a call's arrays ((name, tensor, width, stride) each), their layout checked, and how many there are.  One row has no step to the
+    next, so torch gives that dimension any stride; one token each of several sequences is as many rows."""
+    packed = offsets is not None
+    if packed:
+        _dense("offsets", offsets)
+        if hasattr(offsets, "dtype") and (str(offsets.dtype) not in ("torch.int64", "int64") or offsets.shape != (params.B + 1,)):
+            raise ValueError(f"offsets: {params.B + 1} values of int64 are needed, got {tuple(offsets.shape)} of {offsets.dtype}")
+    rows = params.rows if packed else params.B * params.L
+    if rows < 1:
+        return
+    for name, x, width, stride in arrays:
+        if x is None:
+            continue
+        stride = stride or width
+        if rows > 1:
+            _check_rows(name, x, width, stride)
+        elif hasattr(x, "stride") and width > 1 and x.shape[-1] > 1 and x.stride(-1) != 1:
+            raise ValueError(f"{name}: strides {tuple(x.stride())} of shape {tuple(x.shape)}, a row has to be dense")
+        if hasattr(x, "numel") and x.numel() != rows * width:
+            raise ValueError(f"{name}: {tuple(x.shape)} is not {rows} rows of {width} elements")
+
+
+def cawn_short_conv_workspace_bytes(params):
+    n = ctypes.c_size_t(0)
+    _check(lib().cawn_short_conv_workspace_bytes(ctypes.byref(params), ctypes.byref(n)), "cawn_short_conv_workspace_bytes")
+    return n.value
+
+
+def new_conv_workspace(params, device="cuda"):
+    """Allocate (with torch, as plain device memory) a workspace for cawn_short_conv_bwd."""
+    return _plain_workspace(cawn_short_conv_workspace_bytes(params), device)
+
+
+def cawn_short_conv_fwd(params, x, weight, y, bias=None, state_in=None, state_out=None, offsets=None, stream=None):
+    _dense("weight y bias state_in state_out", weight, y, bias, state_in, state_out)
+    _sequence_rows(params, offsets, (("x_stride", x, params.C, params.x_stride), ("y", y, params.C, 0)))
+    _check(lib().cawn_short_conv_fwd(ctypes.byref(params), _dp(x), _dp(weight), _dp(bias), _dp(state_in), _dp(offsets), _dp(y),
+                                     _dp(state_out), _stream(stream)), "cawn_short_conv_fwd")
+
+
+def cawn_short_conv_bwd(params, x, weight, grad_y, grad_x, workspace=None, bias=None, state_in=None, offsets=None, grad_state_out=None,
+                        grad_weight=None, grad_bias=None, grad_state_in=None, stream=None):
+    _dense("weight grad_y grad_x bias state_in grad_state_out grad_weight grad_bias grad_state_in",
+           weight, grad_y, grad_x, bias, state_in, grad_state_out, grad_weight, grad_bias, grad_state_in)
+    _sequence_rows(params, offsets, (("x_stride", x, params.C, params.x_stride), ("grad_y", grad_y, params.C, 0), ("grad_x", grad_x, params.C, 0)))
+    n = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().cawn_short_conv_bwd(
+        ctypes.byref(params), _dp(x), _dp(weight), _dp(bias), _dp(state_in), _dp(offsets), _dp(grad_y), _dp(grad_state_out), _dp(grad_x),
+        _dp(grad_weight), _dp(grad_bias), _dp(grad_state_in), _dp(workspace), n, _stream(stream)), "cawn_short_conv_bwd")
+
+
+def make_scan_params(B, L, D, N, G=1, softplus=True, flags=0, x_stride=0, dt_stride=0, z_stride=0, b_stride=0, c_stride=0, rows=0):
+    return cawn_scan_params(ctypes.sizeof(cawn_scan_params), B, L, D, N, G, int(softplus), flags, 0, x_stride, dt_stride, z_stride, b_stride,
+                            c_stride, rows)
+
+
+def cawn_selective_scan_workspace_bytes(params, op):
+    n = ctypes.c_size_t(0)
+    _check(lib().cawn_selective_scan_workspace_bytes(ctypes.byref(params), op, ctypes.byref(n)), "cawn_selective_scan_workspace_bytes")
+    return n.value
+
+
+def new_scan_workspace(params, op, device="cuda"):
+    """Allocate (with torch, as plain device memory) a workspace for CAWN_SCAN_FWD, CAWN_SCAN_BWD or CAWN_SCAN_BWD_RECOMPUTE, or the
+    checkpoints (CAWN_SCAN_CHECKPOINTS) that a forward leaves for its backward."""
+    return _plain_workspace(cawn_selective_scan_workspace_bytes(params, op), device)
+
+
+def _scan_rows(params, offsets, x, dt, z, B, C, **dense):
+    D, bc = params.D, params.G * params.N
+    _sequence_rows(params, offsets, (("x_stride", x, D, params.x_stride), ("dt_stride", dt, D, params.dt_stride), ("z_stride", z, D, params.z_stride),
+                                     ("b_stride", B, bc, params.b_stride), ("c_stride", C, bc, params.c_stride),
+                                     *((name, y, bc if name in ("grad_B", "grad_C") else D, 0) for name, y in dense.items())))
+
+
+def _scan_checkpoints(params, checkpoints):
+    """They carry no size of their own into the call, so it is looked at here."""
+    if checkpoints is not None and hasattr(checkpoints, "numel"):
+        need = cawn_selective_scan_workspace_bytes(params, CAWN_SCAN_CHECKPOINTS)
+        if checkpoints.numel() * checkpoints.element_size() < need:
+            raise ValueError(f"checkpoints: {checkpoints.numel() * checkpoints.element_size()} bytes, {need} are needed")
+
+
+def cawn_selective_scan_fwd(params, x, dt, A, B, C, y, workspace=None, skip=None, dt_bias=None, z=None, state_in=None, state_out=None,
+                            offsets=None, checkpoints=None, stream=None):
+    _dense("A y skip dt_bias state_in state_out checkpoints", A, y, skip, dt_bias, state_in, state_out, checkpoints)
+    _scan_rows(params, offsets, x, dt, z, B, C, y=y)
+    _scan_checkpoints(params, checkpoints)
+    n = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().cawn_selective_scan_fwd(
+        ctypes.byref(params), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(skip), _dp(dt_bias), _dp(z), _dp(state_in), _dp(offsets), _dp(y),
+        _dp(state_out), _dp(checkpoints), _dp(workspace), n, _stream(stream)), "cawn_selective_scan_fwd")
+
+
+def cawn_selective_scan_step(params, x, dt, A, B, C, y, skip=None, dt_bias=None, z=None, state_in=None, state_out=None, stream=None):
+    _dense("A y skip dt_bias state_in state_out", A, y, skip, dt_bias, state_in, state_out)
+    _scan_rows(params, None, x, dt, z, B, C, y=y)
+    _check(lib().cawn_selective_scan_step(
+        ctypes.byref(params), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(skip), _dp(dt_bias), _dp(z), _dp(state_in), _dp(y), _dp(state_out),
+        _stream(stream)), "cawn_selective_scan_step")
+
+
+def cawn_selective_scan_bwd(params, x, dt, A, B, C, grad_y, grad_x, grad_dt, grad_A, grad_B, grad_C, workspace, skip=None, dt_bias=None, z=None,
+                            state_in=None, offsets=None, checkpoints=None, grad_state_out=None, grad_skip=None, grad_dt_bias=None, grad_z=None,
+                            grad_state_in=None, stream=None):
+    _dense("A grad_y grad_x grad_dt grad_A grad_B grad_C skip dt_bias state_in checkpoints grad_state_out grad_skip grad_dt_bias grad_z grad_state_in",
+           A, grad_y, grad_x, grad_dt, grad_A, grad_B, grad_C, skip, dt_bias, state_in, checkpoints, grad_state_out, grad_skip, grad_dt_bias, grad_z,
+           grad_state_in)
+    _scan_rows(params, offsets, x, dt, z, B, C, grad_y=grad_y, grad_x=grad_x, grad_dt=grad_dt, grad_B=grad_B, grad_C=grad_C, grad_z=grad_z)
+    _scan_checkpoints(params, checkpoints)
+    _check(lib().cawn_selective_scan_bwd(
+        ctypes.byref(params), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(skip), _dp(dt_bias), _dp(z), _dp(state_in), _dp(offsets), _dp(checkpoints),
+        _dp(grad_y), _dp(grad_state_out), _dp(grad_x), _dp(grad_dt), _dp(grad_A), _dp(grad_B), _dp(grad_C), _dp(grad_skip), _dp(grad_dt_bias),
+        _dp(grad_z), _dp(grad_state_in), _dp(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "cawn_selective_scan_bwd")
+
+
+def make_residual_norm_params(N, M, eps=1e-5, out=CAWN_NORM_OUT_SAME, scale_block=0, stream_float=False, flags=0, x_stride=0):
+    return cawn_residual_norm_params(ctypes.sizeof(cawn_residual_norm_params), M, N, eps, out, scale_block, int(stream_float), flags, 0, x_stride)
+
+
+def cawn_residual_norm_workspace_bytes(params):
+    n = ctypes.c_size_t(0)
+    _check(lib().cawn_residual_norm_workspace_bytes(ctypes.byref(params), ctypes.byref(n)), "cawn_residual_norm_workspace_bytes")
+    return n.value
+
+
+def new_residual_norm_workspace(params, device="cuda"):
+    """Allocate (with torch, as plain device memory) a workspace for cawn_residual_norm_bwd."""
+    return _plain_workspace(cawn_residual_norm_workspace_bytes(params), device)
+
+
+def cawn_residual_norm_fwd(params, x, y, residual=None, weight=None, sum_out=None, scales=None, stream=None):
+    _dense("y residual weight sum_out scales", y, residual, weight, sum_out, scales)
+    if params.N > 0:
+        _check_rows("x_stride", x, params.M, params.x_stride or params.M)
+    _check(lib().cawn_residual_norm_fwd(ctypes.byref(params), _dp(x), _dp(residual), _dp(weight), _dp(sum_out), _dp(y), _dp(scales),
+                                        _stream(stream)), "cawn_residual_norm_fwd")
+
+
+def cawn_residual_norm_bwd(params, sum, grad_y, workspace=None, weight=None, grad_sum=None, grad_residual=None, grad_x=None, grad_weight=None,
+                           stream=None):
+    _dense("sum grad_y weight grad_sum grad_residual grad_x grad_weight", sum, grad_y, weight, grad_sum, grad_residual, grad_x, grad_weight)
+    n = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().cawn_residual_norm_bwd(
+        ctypes.byref(params), _dp(sum), _dp(weight), _dp(grad_y), _dp(grad_sum), _dp(grad_residual), _dp(grad_x), _dp(grad_weight), _dp(workspace), n,
+        _stream(stream)), "cawn_residual_norm_bwd")

@@ -1,0 +1,201 @@
+// Selective scan: what its translation units share.
+//
+// Mathematics, per channel c with N states:  d = softplus(dt + bias),  h_n <- e^{d A_n} h_n + d x B_n,
+// y = (sum_n C_n h_n + skip x) silu(z).  B and C belong to a token and a group of channels.
+//
+// Layout of the work.  A block has 32 channels of one group and one sequence (or a segment of it) and walks its tokens in
+// tiles; NL lanes share a channel, NS states each (N up to NL * NS), so a block is NL warps.  In a warp lane bits 0-1 are a
+// channel, the next log2 NL bits the lane's states, the rest channels again.  A tile's (d, d x) and rows of B and C are
+// made floats once, in shared memory; the next tile is fetched while one is computed.  Few channels: the time axis is cut
+// into segments that run side by side, behind a pass that finds each segment's own end state and its sum of d (the decay
+// over a segment is e^{A sum d}), so that every exponential is taken twice.
+#pragma once
+#include "cawn_seq.cuh"
+
+namespace cawn {
+
+constexpr int kScanChannels = 32, kCheckpoint = 16;     // tokens between two states that the forward leaves for the backward
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct SelectiveParams {
+    Sequences seq;
+    const void *x, *dt, *z, *bm, *cm, *gy;
+    const float *A, *skip, *dt_bias, *state_in, *gstate_out;
+    void *y, *gx, *gdt, *gz;
+    float *state_out, *gstate_in, *checkpoints;
+    float *seg_state, *seg_time, *first;        // segments' own ends and sums of d; a copy of state_in
+    float *part_bc, *part_param;                // backward: partial sums of a block's channels, of a block's tokens
+    long long xs, dts, zs, bs, cs;              // elements between rows
+    long long param_cols;                       // floats of a row of part_param, a multiple of 4
+    long long per;                              // tokens of a segment, a multiple of 32
+    int D, N, G, Dg, blocks;                    // channels of a group, blocks of channels per group
+    int S;                                      // segments
+    int softplus, whole_x, whole_dt, whole_z, whole_d, whole_b, whole_c;
+};
+
+// log(1 + e^v) without loss where it is small: v^+ + log1p(u), u = e^{-|v|}, log1p(u) = 2 atanh(u / (2 + u)) by its series
+// (u / (2 + u) is at most 1/3, where the first term left out is 2e-9 of the sum).
+__device__ __forceinline__ float softplus_of(float v)
+{
+    const float u = exp2_fast(-kLog2e * fabsf(v)), s = __fdividef(u, 2.f + u), q = s * s;
+    float p = 1.f / 17.f;
+    p = fmaf(p, q, 1.f / 15.f);
+    p = fmaf(p, q, 1.f / 13.f);
+    p = fmaf(p, q, 1.f / 11.f);
+    p = fmaf(p, q, 1.f / 9.f);
+    p = fmaf(p, q, 1.f / 7.f);
+    p = fmaf(p, q, 1.f / 5.f);
+    p = fmaf(p, q, 1.f / 3.f);
+    p = fmaf(p, q, 1.f);
+    return fmaf(2.f * s, p, v > 0.f ? v : v != v ? v : 0.f);
+}
+
+// Four elements as they are stored.
+template <class T> struct Quad;
+template <> struct Quad<bf16> {
+    uint2 w;
+    __device__ __forceinline__ float4 get() const
+    {
+        return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
+    }
+    __device__ __forceinline__ void set(float4 v) { w = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)); }
+    __device__ __forceinline__ void load(const bf16 *p) { w = *reinterpret_cast<const uint2 *>(p); }
+};
+template <> struct Quad<float> {
+    float4 w;
+    __device__ __forceinline__ float4 get() const { return w; }
+    __device__ __forceinline__ void set(float4 v) { w = v; }
+    __device__ __forceinline__ void load(const float *p) { w = *reinterpret_cast<const float4 *>(p); }
+};
+template <class T> __device__ __forceinline__ Quad<T> fetch_quad(const T *p, int n, bool whole)
+{
+    Quad<T> r;
+    if (whole && n >= 4) r.load(p);
+    else r.set(make_float4(n > 0 ? widen(p[0]) : 0.f, n > 1 ? widen(p[1]) : 0.f, n > 2 ? widen(p[2]) : 0.f, n > 3 ? widen(p[3]) : 0.f));
+    return r;
+}
+
+// Where a thread is, and what its states are.
+template <int NL, int NS> struct Place {
+    static constexpr int kThreads = 32 * NL, kPad = NL * NS, kPairs = NS / 2, kTile = NL >= 4 ? 32 : 16;
+    static constexpr int kShift = NL == 1 ? 0 : NL == 2 ? 1 : NL == 4 ? 2 : 3;
+    int nl, ch;                 // lane among a channel's, channel of the block
+    __device__ __forceinline__ Place()
+    {
+        const int lane = threadIdx.x % 32;
+        nl = (lane >> 2) & (NL - 1);
+        ch = threadIdx.x / 32 * (32 / NL) + (lane & 3) + 4 * (lane >> (2 + kShift));
+    }
+};
+
+// This lane's NS of a channel's N floats at p; those past N are zero.
+template <int NS> __device__ __forceinline__ void load_states(f32x2 (&h)[NS / 2], const float *p, int n0, int N, bool in)
+{
+    float f[NS];
+    if (in && N % 4 == 0) {
+#pragma unroll
+        for (int k = 0; k < NS; k += 4) {
+            const float4 v = n0 + k < N ? *reinterpret_cast<const float4 *>(p + n0 + k) : make_float4(0.f, 0.f, 0.f, 0.f);
+            f[k] = v.x; f[k + 1] = v.y; f[k + 2] = v.z; f[k + 3] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < NS; k++) f[k] = in && n0 + k < N ? p[n0 + k] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < NS / 2; k++) h[k] = pair(f[2 * k], f[2 * k + 1]);
+}
+template <int NS> __device__ __forceinline__ void store_states(float *p, const f32x2 (&h)[NS / 2], int n0, int N, bool in)
+{
+    float f[NS];
+#pragma unroll
+    for (int k = 0; k < NS / 2; k++) {
+        const float2 v = halves(h[k]);
+        f[2 * k] = v.x;
+        f[2 * k + 1] = v.y;
+    }
+    if (!in) return;
+    if (N % 4 == 0) {
+#pragma unroll
+        for (int k = 0; k < NS; k += 4)
+            if (n0 + k < N) *reinterpret_cast<float4 *>(p + n0 + k) = make_float4(f[k], f[k + 1], f[k + 2], f[k + 3]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < NS; k++)
+            if (n0 + k < N) p[n0 + k] = f[k];
+    }
+}
+
+__device__ __forceinline__ f32x2 exp2_pair(f32x2 v)
+{
+    const float2 f = halves(v);
+    return pair(exp2_fast(f.x), exp2_fast(f.y));
+}
+__device__ __forceinline__ f32x2 twice(float v) { return pair(v, v); }
+__device__ __forceinline__ float sum_of(f32x2 v)
+{
+    const float2 f = halves(v);
+    return f.x + f.y;
+}
+template <int NS> __device__ __forceinline__ void row_pairs(f32x2 (&r)[NS / 2], const float *p)
+{
+#pragma unroll
+    for (int k = 0; k < NS / 2; k += 2) {
+        const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(p + 2 * k);
+        r[k] = v.x;
+        r[k + 1] = v.y;
+    }
+}
+
+// Four tokens' sums over the NL lanes of a channel, by halving: each exchange sends half of a lane's values away and keeps
+// the other half.  Each sum is then written once, to out[token * stride].
+template <int NL> __device__ __forceinline__ void sum_four(const float (&v)[4], int nl, float *out, int stride)
+{
+    if constexpr (NL == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) out[i * stride] = v[i];
+    } else {
+        const bool odd = nl & 1, high = nl & 2;
+        float a = odd ? v[1] : v[0], b = odd ? v[3] : v[2];
+        a += __shfl_xor_sync(0xffffffffu, odd ? v[0] : v[1], 4);
+        b += __shfl_xor_sync(0xffffffffu, odd ? v[2] : v[3], 4);
+        if constexpr (NL == 2) {
+            out[nl * stride] = a;
+            out[(nl + 2) * stride] = b;
+        } else {
+            float c = high ? b : a;
+            c += __shfl_xor_sync(0xffffffffu, high ? a : b, 8);
+            if constexpr (NL == 8) {
+                c += __shfl_xor_sync(0xffffffffu, c, 16);
+                if (nl < 4) out[nl * stride] = c;
+            } else {
+                out[nl * stride] = c;
+            }
+        }
+    }
+}
+
+// The state (or gradient) that comes into a segment from those before (behind) it.
+template <int NS> __device__ __forceinline__ void fold_segment(f32x2 (&h)[NS / 2], const SelectiveParams &P, const f32x2 (&A2)[NS / 2], long long at, int n0, bool in)
+{
+    f32x2 own[NS / 2];
+    load_states<NS>(own, P.seg_state + at * P.N, n0, P.N, in);
+    const f32x2 time = twice(in ? P.seg_time[at] : 0.f);
+#pragma unroll
+    for (int k = 0; k < NS / 2; k++) h[k] = fma2(exp2_pair(mul2(time, A2[k])), h[k], own[k]);
+}
+
+// First checkpoint of a sequence: those of two sequences never meet, whatever the lengths.
+__device__ __forceinline__ long long checkpoint_of(const Span &s, int b) { return s.begin / kCheckpoint + b; }
+
+using SelectiveKernel = void (*)(SelectiveParams);
+struct Shape { int nl, ns; };
+inline Shape shape_of(int N) { return N <= 4 ? Shape{1, 4} : N <= 8 ? Shape{2, 4} : N <= 16 ? Shape{4, 4} : N <= 32 ? Shape{8, 4} : Shape{8, 8}; }
+
+// One call of each kernel family; the grid is (blocks of channels x sequences, segments).
+int launch_selective_fwd(const SelectiveParams &P, const Shape &s, bool half, bool summary, cudaStream_t st);
+int launch_selective_step(const SelectiveParams &P, bool half, cudaStream_t st);
+int launch_selective_bwd(const SelectiveParams &P, const Shape &s, bool half, bool summary, cudaStream_t st);
+int launch_selective_bc(const SelectiveParams &P, bool half, void *grad_b, void *grad_c, cudaStream_t st);
+
+}  // namespace cawn

@@ -1,0 +1,223 @@
+// Selective scan: argument checks, workspaces and the order of launches.
+#include "cawn_selective.cuh"
+
+namespace cawn {
+namespace {
+
+int check(const cawn_scan_params *p)
+{
+    if (p == nullptr) return CAWN_ERR_NULL_POINTER;
+    if (p->struct_size != sizeof(cawn_scan_params)) return CAWN_ERR_INVALID_ARG;
+    if (p->B < 1 || p->L < 0 || p->D < 1 || p->N < 1 || p->G < 1 || p->D % p->G != 0 || p->rows < 0 || !storage_flags_ok(p->flags) ||
+        (p->softplus != 0 && p->softplus != 1) || p->reserved != 0)
+        return CAWN_ERR_INVALID_ARG;
+    const int64_t bc = (int64_t)p->G * p->N;
+    for (int64_t stride : {p->x_stride, p->dt_stride, p->z_stride})
+        if (stride != 0 && stride < p->D) return CAWN_ERR_INVALID_ARG;
+    for (int64_t stride : {p->b_stride, p->c_stride})
+        if (stride != 0 && stride < bc) return CAWN_ERR_INVALID_ARG;
+    if (p->N > 64 || p->D > (1 << 22) || p->G > 65535) return CAWN_ERR_UNSUPPORTED;
+    int64_t wide = most(p->D, bc);
+    for (int64_t stride : {p->x_stride, p->dt_stride, p->z_stride, p->b_stride, p->c_stride}) wide = most(wide, stride);
+    const double rows = p->rows > 0 ? (double)p->rows : (double)p->B * (double)p->L;
+    if (rows * (double)wide > 1.0e17) return CAWN_ERR_UNSUPPORTED;
+    if ((double)p->B * (p->D / kScanChannels + p->G) * 16.0 > 2.0e9 || (double)p->B * ((double)p->L / 32 + 1) > 2.0e9) return CAWN_ERR_UNSUPPORTED;
+    return CAWN_OK;
+}
+
+int64_t blocks_of(const cawn_scan_params *p) { return p->G * ceil_div(p->D / p->G, kScanChannels); }
+int64_t rows_of(const cawn_scan_params *p) { return p->rows > 0 ? p->rows : (int64_t)p->B * p->L; }
+
+// Segments of the time axis.  Whole sequences when their blocks fill the GPU (`fill` warps a multiprocessor); otherwise
+// as many segments as do, none shorter than 256 tokens.
+constexpr int kFill = 12, kShortest = 256;
+int64_t wanted(const cawn_scan_params *p) { return most((int64_t)sm_count() * kFill / (blocks_of(p) * shape_of(p->N).nl), 1); }    // sequences x segments
+int64_t segments_of(const cawn_scan_params *p)
+{
+    const int64_t want = wanted(p);
+    if (p->B * 2 > want) return 1;
+    const int64_t s = most(want / p->B, 1), longest = most(p->L / kShortest, 1);
+    return s < longest ? (s < 64 ? s : 64) : (longest < 64 ? longest : 64);
+}
+// The most sequences x segments of any call with up to this B and L.
+int64_t most_segments(const cawn_scan_params *p)
+{
+    const int64_t cut = most(wanted(p), p->B), whole = p->B * most(p->L / kShortest, 1);
+    return cut < whole ? cut : whole;
+}
+
+// A workspace in its parts, each on a 256-byte boundary.
+struct Carver {
+    unsigned char *base;
+    size_t used = 0;
+    float *floats(int64_t n)
+    {
+        float *p = base != nullptr ? reinterpret_cast<float *>(base + used) : nullptr;
+        used += ((size_t)n * sizeof(float) + 255) / 256 * 256;
+        return p;
+    }
+};
+
+// Partial sums of grad_A, grad_skip and grad_dt_bias: rows that begin on 16 bytes.
+int64_t param_cols(const cawn_scan_params *p) { return ceil_div((int64_t)p->D * (p->N + 2), 4) * 4; }
+int64_t checkpoint_rows(const cawn_scan_params *p) { return rows_of(p) / kCheckpoint + p->B + 1; }
+
+// `sized`: for any call up to this one (the size query) instead of for this very call.
+void carve_segments(Carver &c, SelectiveParams &P, const cawn_scan_params *p, bool first, bool sized)
+{
+    const int64_t pieces = sized ? most_segments(p) : p->B * segments_of(p);
+    if (pieces <= (sized ? 1 : p->B)) return;
+    P.seg_state = c.floats(pieces * p->D * p->N);
+    P.seg_time = c.floats(pieces * p->D);
+    if (first) P.first = c.floats((int64_t)p->B * p->D * p->N);
+}
+void carve_bwd(Carver &c, SelectiveParams &P, const cawn_scan_params *p, bool sized)
+{
+    P.part_bc = c.floats(blocks_of(p) * rows_of(p) * 2 * p->N);
+    P.part_param = c.floats((sized ? most_segments(p) : p->B * segments_of(p)) * param_cols(p));
+}
+
+SelectiveParams fill(const cawn_scan_params *p, const int64_t *offsets, const void *b, const void *c)
+{
+    SelectiveParams P = {};
+    const int per = p->flags != 0 ? 8 : 4;
+    P.seq = {reinterpret_cast<const long long *>(offsets), p->L, rows_of(p), p->B};
+    P.D = p->D; P.N = p->N; P.G = p->G; P.Dg = p->D / p->G;
+    P.blocks = (int)ceil_div(P.Dg, kScanChannels);
+    auto stride = [](int64_t s, int64_t dense) { return s != 0 ? s : dense; };
+    P.xs = stride(p->x_stride, p->D); P.dts = stride(p->dt_stride, p->D); P.zs = stride(p->z_stride, p->D);
+    P.bs = stride(p->b_stride, (int64_t)p->G * p->N); P.cs = stride(p->c_stride, (int64_t)p->G * p->N);
+    const bool eights = P.Dg % 8 == 0;          // a block's channels begin on a word
+    P.whole_x = eights && P.xs % per == 0; P.whole_dt = eights && P.dts % per == 0; P.whole_z = eights && P.zs % per == 0;
+    P.whole_d = eights && p->D % per == 0;
+    const uintptr_t quad = p->flags != 0 ? 7 : 15;
+    P.whole_b = p->N % 4 == 0 && P.bs % 4 == 0 && (reinterpret_cast<uintptr_t>(b) & quad) == 0;
+    P.whole_c = p->N % 4 == 0 && P.cs % 4 == 0 && (reinterpret_cast<uintptr_t>(c) & quad) == 0;
+    P.softplus = p->softplus;
+    P.S = (int)segments_of(p);
+    P.param_cols = param_cols(p);
+    P.per = most(ceil_div(ceil_div(p->L, P.S), 32), 1) * 32;
+    return P;
+}
+
+// B and C may begin anywhere in a row of theirs: at an element.
+bool elements_aligned(const cawn_scan_params *p, const void *b, const void *c)
+{
+    const uintptr_t mask = p->flags != 0 ? 1 : 3;
+    return ((reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c)) & mask) == 0;
+}
+
+}  // namespace
+}  // namespace cawn
+
+extern "C" int cawn_selective_scan_workspace_bytes(const cawn_scan_params *params, int op, size_t *bytes)
+{
+    using namespace cawn;
+    const int rc = check(params);
+    if (rc != CAWN_OK) return rc;
+    if (bytes == nullptr) return CAWN_ERR_NULL_POINTER;
+    SelectiveParams P = {};
+    Carver c = {nullptr};
+    switch (op) {
+    case CAWN_SCAN_FWD: carve_segments(c, P, params, true, true); break;
+    case CAWN_SCAN_BWD:
+        carve_segments(c, P, params, true, true);
+        carve_bwd(c, P, params, true);
+        break;
+    case CAWN_SCAN_BWD_RECOMPUTE:
+        carve_segments(c, P, params, true, true);
+        carve_bwd(c, P, params, true);
+        c.floats(checkpoint_rows(params) * params->D * params->N);
+        break;
+    case CAWN_SCAN_CHECKPOINTS: c.floats(checkpoint_rows(params) * params->D * params->N); break;
+    default: return CAWN_ERR_INVALID_ARG;
+    }
+    *bytes = c.used;
+    return CAWN_OK;
+}
+
+extern "C" int cawn_selective_scan_fwd(const cawn_scan_params *params, const void *x, const void *dt, const float *A, const void *B,
+                                       const void *C, const float *skip, const float *dt_bias, const void *z, const float *state_in,
+                                       const int64_t *offsets, void *y, float *state_out, float *checkpoints,
+                                       void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    using namespace cawn;
+    int rc = check(params);
+    if (rc == CAWN_OK) rc = check_offsets(offsets, params->B, params->L, params->rows);
+    if (rc != CAWN_OK) return rc;
+    if (A == nullptr || (params->L > 0 && (x == nullptr || dt == nullptr || B == nullptr || C == nullptr || y == nullptr))) return CAWN_ERR_NULL_POINTER;
+    if (!all_aligned16(x, dt, A, skip, dt_bias, z, state_in, y, state_out, checkpoints, workspace) || !elements_aligned(params, B, C))
+        return CAWN_ERR_MISALIGNED;
+    SelectiveParams P = fill(params, offsets, B, C);
+    Carver c = {static_cast<unsigned char *>(workspace)};
+    carve_segments(c, P, params, true, false);
+    if (c.used > 0 && workspace == nullptr) return CAWN_ERR_NULL_POINTER;
+    if (c.used > workspace_bytes) return CAWN_ERR_WORKSPACE_TOO_SMALL;
+    P.x = x; P.dt = dt; P.A = A; P.bm = B; P.cm = C; P.skip = skip; P.dt_bias = dt_bias; P.z = z;
+    P.state_in = state_in; P.y = y; P.state_out = state_out; P.checkpoints = checkpoints;
+    const Shape s = shape_of(params->N);
+    const bool half = params->flags != 0;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (P.S > 1) rc = launch_selective_fwd(P, s, half, true, st);
+    return rc != CAWN_OK ? rc : launch_selective_fwd(P, s, half, false, st);
+}
+
+extern "C" int cawn_selective_scan_step(const cawn_scan_params *params, const void *x, const void *dt, const float *A, const void *B,
+                                        const void *C, const float *skip, const float *dt_bias, const void *z, const float *state_in,
+                                        void *y, float *state_out, void *cuda_stream)
+{
+    using namespace cawn;
+    int rc = check(params);
+    if (rc == CAWN_OK) rc = check_offsets(nullptr, params->B, params->L, params->rows);
+    if (rc != CAWN_OK) return rc;
+    if (A == nullptr || (params->L > 0 && (x == nullptr || dt == nullptr || B == nullptr || C == nullptr || y == nullptr))) return CAWN_ERR_NULL_POINTER;
+    if (!all_aligned16(x, dt, A, skip, dt_bias, z, state_in, y, state_out) || !elements_aligned(params, B, C)) return CAWN_ERR_MISALIGNED;
+    SelectiveParams P = fill(params, nullptr, B, C);
+    P.x = x; P.dt = dt; P.A = A; P.bm = B; P.cm = C; P.skip = skip; P.dt_bias = dt_bias; P.z = z;
+    P.state_in = state_in; P.y = y; P.state_out = state_out;
+    return launch_selective_step(P, params->flags != 0, static_cast<cudaStream_t>(cuda_stream));
+}
+
+extern "C" int cawn_selective_scan_bwd(const cawn_scan_params *params, const void *x, const void *dt, const float *A, const void *B,
+                                       const void *C, const float *skip, const float *dt_bias, const void *z, const float *state_in,
+                                       const int64_t *offsets, const float *checkpoints, const void *grad_y, const float *grad_state_out,
+                                       void *grad_x, void *grad_dt, float *grad_A, void *grad_B, void *grad_C, float *grad_skip,
+                                       float *grad_dt_bias, void *grad_z, float *grad_state_in,
+                                       void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    using namespace cawn;
+    int rc = check(params);
+    if (rc == CAWN_OK) rc = check_offsets(offsets, params->B, params->L, params->rows);
+    if (rc != CAWN_OK) return rc;
+    if (z == nullptr && grad_z != nullptr) return CAWN_ERR_INVALID_ARG;
+    if (A == nullptr || grad_A == nullptr || workspace == nullptr) return CAWN_ERR_NULL_POINTER;
+    if (params->L > 0 && (x == nullptr || dt == nullptr || B == nullptr || C == nullptr || grad_y == nullptr || grad_x == nullptr || grad_dt == nullptr ||
+                          grad_B == nullptr || grad_C == nullptr || (z != nullptr && grad_z == nullptr)))
+        return CAWN_ERR_NULL_POINTER;
+    if (!all_aligned16(x, dt, A, skip, dt_bias, z, state_in, checkpoints, grad_y, grad_state_out, grad_x, grad_dt, grad_A, grad_B, grad_C, grad_skip,
+                       grad_dt_bias, grad_z, grad_state_in, workspace) || !elements_aligned(params, B, C))
+        return CAWN_ERR_MISALIGNED;
+    SelectiveParams P = fill(params, offsets, B, C);
+    Carver c = {static_cast<unsigned char *>(workspace)};
+    carve_segments(c, P, params, true, false);
+    carve_bwd(c, P, params, false);
+    float *own = checkpoints == nullptr && params->L > 0 ? c.floats(checkpoint_rows(params) * params->D * params->N) : nullptr;
+    if (c.used > workspace_bytes) return CAWN_ERR_WORKSPACE_TOO_SMALL;
+    P.x = x; P.dt = dt; P.A = A; P.bm = B; P.cm = C; P.skip = skip; P.dt_bias = dt_bias; P.z = z; P.state_in = state_in;
+    P.gy = grad_y; P.gstate_out = grad_state_out; P.gx = grad_x; P.gdt = grad_dt; P.gz = grad_z; P.gstate_in = grad_state_in;
+    const Shape s = shape_of(params->N);
+    const bool half = params->flags != 0;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    P.checkpoints = own != nullptr ? own : const_cast<float *>(checkpoints);
+    if (own != nullptr) {           // the forward's walk once more, for its states alone
+        if (P.S > 1) rc = launch_selective_fwd(P, s, half, true, st);
+        if (rc == CAWN_OK) rc = launch_selective_fwd(P, s, half, false, st);
+    }
+    if (rc == CAWN_OK && P.S > 1) rc = launch_selective_bwd(P, s, half, true, st);
+    if (rc == CAWN_OK) rc = launch_selective_bwd(P, s, half, false, st);
+    if (rc == CAWN_OK && params->L > 0) rc = launch_selective_bc(P, half, grad_B, grad_C, st);
+    if (rc != CAWN_OK) return rc;
+    const long long D = params->D;
+    PartialSums sums = {P.part_param, (long long)params->B * P.S, P.param_cols, {grad_A, grad_skip, grad_dt_bias}, {D * params->N, D, D}};
+    return sum_partials(sums, st);
+}
