@@ -580,13 +580,20 @@ def _sequence_rows(params, offsets, arrays):
     for name, x, width, stride in arrays:
         if x is None:
             continue
-        stride = stride or width
+        row = stride or width
+        shape = getattr(x, "shape", None)
+        if shape is None or not hasattr(x, "stride"):
+            continue
+        if len(shape) == 2 and shape[1] == width and shape[0] == rows:          # the usual case at once
+            steps = x.stride()
+            if steps[1] == 1 and (steps[0] == row or rows == 1):
+                continue
         if rows > 1:
-            _check_rows(name, x, width, stride)
-        elif hasattr(x, "stride") and width > 1 and x.shape[-1] > 1 and x.stride(-1) != 1:
-            raise ValueError(f"{name}: strides {tuple(x.stride())} of shape {tuple(x.shape)}, a row has to be dense")
-        if hasattr(x, "numel") and x.numel() != rows * width:
-            raise ValueError(f"{name}: {tuple(x.shape)} is not {rows} rows of {width} elements")
+            _check_rows(name, x, width, row)
+        elif width > 1 and shape[-1] > 1 and x.stride(-1) != 1:
+            raise ValueError(f"{name}: strides {tuple(x.stride())} of shape {tuple(shape)}, a row has to be dense")
+        if x.numel() != rows * width:
+            raise ValueError(f"{name}: {tuple(shape)} is not {rows} rows of {width} elements")
 
 
 def cawn_short_conv_workspace_bytes(params):

@@ -3,15 +3,14 @@
 // Mathematics: with e the sequence behind its history of K - 1 rows, z_t = bias + sum_k w_k e_{t+k}, y_t = z_t or z_t sigmoid(z_t);
 // the new history is e's last K - 1 rows.  Backward: dz = dy act'(z), de_i = sum_k w_k dz_{i-k} (and the new history's
 // gradient on the last K - 1), dw_k = sum_t dz_t e_{t+k}, dbias = sum_t dz_t.
-// Bound: memory; an element costs K products.  A thread keeps eight channels (a 16-byte word of bfloat16) and walks
-// kRows rows with the last K - 1 of them in registers, so that a row is fetched once but for the K - 1 in front of
+// Bound: memory; an element costs K products.  A thread keeps four channels and walks kRows rows with the last K - 1 of them in registers, so that a row is fetched once but for the K - 1 in front of
 // a walk, which the neighbour's fetch has brought to L1 or L2.
 #include "cawn_seq.cuh"
 
 namespace cawn {
 namespace {
 
-constexpr int kRows = 16, kLanes = 32, kWalks = 4, kTile = kRows * kWalks;     // a block: 32 words of channels, 4 walks
+constexpr int kRows = 16, kLanes = 32, kWalks = 4, kTile = kRows * kWalks;     // a block: 32 words of four channels, 4 walks
 constexpr int kConvThreads = kLanes * kWalks;
 
 struct ConvParams {
@@ -24,99 +23,141 @@ struct ConvParams {
     int C, words, silu, x_whole, c_whole;
 };
 
-template <class T> __device__ __forceinline__ void row_of(float (&f)[8], const T *p, int n, bool whole) { fetch_eight(p, n, whole).widen_to(f); }
+constexpr int kWord = 4, kPairs = kWord / 2;
+using Row = f32x2[kPairs];      // a thread's channels as pairs
+
+// A row's four channels.  WHOLE: every row of every array begins on a word and C is a multiple of four, so that an access is
+// one instruction (8 x 2048 x 2048, forward: 18 instructions an element without, 10 with).
+template <bool WHOLE, class T> __device__ __forceinline__ Quad<T> word_of(const T *p, bool in, int n, bool whole)
+{
+    if constexpr (!WHOLE) return fetch_quad(p, in ? n : 0, whole);
+    Quad<T> r;
+    r.set(make_float4(0.f, 0.f, 0.f, 0.f));
+    if (in) r.load(p);
+    return r;
+}
+template <class T> __device__ __forceinline__ void pairs_of(Row &r, const Quad<T> &e)
+{
+    const float4 f = e.get();
+    r[0] = pair(f.x, f.y);
+    r[1] = pair(f.z, f.w);
+}
+template <bool WHOLE, class T> __device__ __forceinline__ void store_row(T *p, const Row &r, int n, bool whole)
+{
+    const float2 a = halves(r[0]), b = halves(r[1]);
+    store_quad(p, make_float4(a.x, a.y, b.x, b.y), WHOLE ? kWord : n, WHOLE || whole);
+}
 
 // Row `i` of the sequence behind its history (i < 0: history, zero without one), as the arrays hold it.
-template <class T, int K>
-__device__ __forceinline__ void extended(float (&f)[8], const ConvParams &P, const T *x, const float *history, long long i, int n)
+template <class T, int K, bool WHOLE>
+__device__ __forceinline__ void extended(Row &r, const ConvParams &P, const T *x, const float *history, long long i, int n)
 {
-    if (i >= 0) row_of(f, x + i * P.x_stride, n, P.x_whole);
-    else if (history != nullptr) row_of(f, history + (i + K - 1) * P.C, n, P.c_whole);
-    else {
+    if (i >= 0) {
+        pairs_of(r, word_of<WHOLE>(x + i * P.x_stride, true, n, P.x_whole));
+    } else if (history != nullptr) {
+        pairs_of(r, word_of<WHOLE>(history + (i + K - 1) * P.C, true, n, P.c_whole));
+    } else {
 #pragma unroll
-        for (int c = 0; c < 8; c++) f[c] = 0.f;
+        for (int c = 0; c < kPairs; c++) r[c] = 0ull;
     }
 }
 
-template <int K> __device__ __forceinline__ void taps_of(float (&w)[K][8], float (&b)[8], const ConvParams &P, int c0, int n)
+// The block's weights and biases, fetched as they lie, turned over in shared memory, and a thread's own of them.
+constexpr int kChannels = kLanes * kWord;
+template <int K> __device__ __forceinline__ void taps_of(Row (&w)[K], Row &b, const ConvParams &P)
 {
+    __shared__ __align__(16) float turned[K + 1][kChannels + 8];
+    const int first = blockIdx.y * kChannels, here = P.C - first < kChannels ? P.C - first : kChannels;
+    for (int i = threadIdx.x; i < kChannels * K; i += kConvThreads) turned[i % K][i / K] = i < here * K ? P.w[(long long)first * K + i] : 0.f;
+    for (int i = threadIdx.x; i < kChannels; i += kConvThreads) turned[K][i] = i < here && P.b != nullptr ? P.b[first + i] : 0.f;
+    __syncthreads();
+    const int at = threadIdx.x % kLanes * kWord;
 #pragma unroll
-    for (int c = 0; c < 8; c++) {
-#pragma unroll
-        for (int k = 0; k < K; k++) w[k][c] = c < n ? P.w[(long long)(c0 + c) * K + k] : 0.f;
-        b[c] = c < n && P.b != nullptr ? P.b[c0 + c] : 0.f;
+    for (int k = 0; k <= K; k++) {
+        const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(&turned[k][at]);
+        (k < K ? w[k < K ? k : 0] : b)[0] = v.x;
+        (k < K ? w[k < K ? k : 0] : b)[1] = v.y;
     }
 }
 
-template <class T, int K>
+template <class T, int K, bool WHOLE>
 __global__ void __launch_bounds__(kConvThreads) conv_fwd_kernel(const ConvParams P)
 {
     follow_previous();
-    const int word = (blockIdx.y * kLanes + threadIdx.x % kLanes), c0 = word * 8;
-    if (word >= P.words) return;
-    const int n = P.C - c0 < 8 ? P.C - c0 : 8;
+    const int word = (blockIdx.y * kLanes + threadIdx.x % kLanes), c0 = word * kWord;
+    const int n = P.C - c0 < kWord ? P.C - c0 : kWord;
     const int b = (int)(blockIdx.x / P.tiles);
     const long long t0 = (blockIdx.x % P.tiles) * kTile + threadIdx.x / kLanes * kRows;
     const Span s = span_of(P.seq, b);
+    const bool here = word < P.words && (t0 < s.len || t0 == 0);
     const T *x = static_cast<const T *>(P.x) + s.begin * P.x_stride + c0;
     const float *history = P.state_in != nullptr && K > 1 ? P.state_in + (long long)b * (K - 1) * P.C + c0 : nullptr;
-
-    // The new history, by the walk at the sequence's start: it alone reads the old one, which may be the same array.
-    float old[K][8];            // row j of the window's past; K - 1 are used
-    if (t0 < s.len || t0 == 0) {
+    const int rows = !here ? 0 : s.len - t0 < kRows ? (int)(s.len - t0) : kRows;
+    // Four rows are computed while the next four are on their way; the first eight, and the K - 1 in front, set out
+    // before the weights do.
+    Quad<T> next[2][4];
+    const T *ahead = x + t0 * P.x_stride;
+    auto fetch = [&](int q) {
 #pragma unroll
-        for (int j = 0; j < K - 1; j++) extended<T, K>(old[j], P, x, history, t0 + j - (K - 1), n);
+        for (int r = 0; r < 4; r++) next[q % 2][r] = word_of<WHOLE>(ahead + r * P.x_stride, q * 4 + r < rows, n, P.x_whole);
+        ahead += 4 * P.x_stride;
+    };
+    Row old[K];                 // the K - 1 rows in front of the next one
+    fetch(0);
+    fetch(1);
+    if (here) {
+#pragma unroll
+        for (int j = 0; j < K - 1; j++) extended<T, K, WHOLE>(old[j], P, x, history, t0 + j - (K - 1), n);
     }
+    Row w[K], bias;
+    taps_of<K>(w, bias, P);
+    if (!here) return;
+    // The new history, by the walk at the sequence's start: it alone reads the old one, which may be the same array.
     if (K > 1 && t0 == 0 && P.state_out != nullptr) {
         float *out = P.state_out + (long long)b * (K - 1) * P.C + c0;
 #pragma unroll
         for (int j = 0; j < K - 1; j++) {
-            float f[8];
-            extended<T, K>(f, P, x, history, s.len + j - (K - 1), n);       // never a row of the history that is overwritten already
-            store_eight(out + (long long)j * P.C, f, n, P.c_whole);
+            Row r;
+            extended<T, K, WHOLE>(r, P, x, history, s.len + j - (K - 1), n);       // never a row of the history that is overwritten already
+            store_row<WHOLE>(out + (long long)j * P.C, r, n, P.c_whole);
         }
     }
-    if (t0 >= s.len) return;
-    float w[K][8], bias[8];
-    taps_of<K>(w, bias, P, c0, n);
     T *y = static_cast<T *>(P.y) + (s.begin + t0) * P.C + c0;
-    x += t0 * P.x_stride;
-    const int rows = s.len - t0 < kRows ? (int)(s.len - t0) : kRows;
 #pragma unroll
-    for (int r0 = 0; r0 < kRows; r0 += 8) {
-        Eight<T> next[8];       // eight rows in flight
+    for (int q = 0; q < kRows / 4; q++) {
+        if (q * 4 >= rows) break;
 #pragma unroll
-        for (int r = 0; r < 8; r++) next[r] = fetch_eight(x + (r0 + r) * P.x_stride, r0 + r < rows ? n : 0, P.x_whole);
+        for (int r = 0; r < 4; r++) {
+            Row now, z;
+            pairs_of(now, next[q % 2][r]);
 #pragma unroll
-        for (int r = 0; r < 8; r++) {
-            float f[8], z[8];
-            next[r].widen_to(f);
+            for (int c = 0; c < kPairs; c++) {
+                z[c] = fma2(w[K - 1][c], now[c], bias[c]);
 #pragma unroll
-            for (int c = 0; c < 8; c++) {
-                float v = bias[c];
-#pragma unroll
-                for (int k = 0; k < K - 1; k++) v = fmaf(w[k][c], old[k][c], v);
-                v = fmaf(w[K - 1][c], f[c], v);
-                z[c] = P.silu ? v * sigmoid_of(v) : v;
+                for (int k = 0; k < K - 1; k++) z[c] = fma2(w[k][c], old[k][c], z[c]);
+                if (P.silu) z[c] = mul2(z[c], sigmoid_of(z[c]));
 #pragma unroll
                 for (int k = 0; k + 2 < K; k++) old[k][c] = old[k + 1][c];
-                if (K > 1) old[K > 1 ? K - 2 : 0][c] = f[c];
+                if (K > 1) old[K > 1 ? K - 2 : 0][c] = now[c];
             }
-            if (r0 + r < rows) store_eight(y + (long long)(r0 + r) * P.C, z, n, P.c_whole);
+            if (q * 4 + r < rows) store_row<WHOLE>(y + (long long)(q * 4 + r) * P.C, z, n, P.c_whole);
         }
+        if (q + 2 < kRows / 4) fetch(q + 2);
     }
 }
 
 // A block takes tile after tile, so that few partial sums of the parameters' gradients are left.
-template <class T, int K>
+template <class T, int K, bool WHOLE>
 __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(const ConvParams P)
 {
     follow_previous();
-    __shared__ float fold[kWalks][kLanes][8];
-    const int lane = threadIdx.x % kLanes, walk = threadIdx.x / kLanes, word = blockIdx.y * kLanes + lane, c0 = word * 8;
-    const int n = word < P.words ? (P.C - c0 < 8 ? P.C - c0 : 8) : 0;
-    float w[K][8], bias[8], gw[K][8] = {}, gb[8] = {};
-    taps_of<K>(w, bias, P, n > 0 ? c0 : 0, n);
+    constexpr int kAhead = 4;   // rows computed while as many are on their way
+    __shared__ __align__(16) float fold[kWalks][kChannels];
+    const int lane = threadIdx.x % kLanes, walk = threadIdx.x / kLanes, word = blockIdx.y * kLanes + lane, c0 = word * kWord;
+    const int n = word < P.words ? (P.C - c0 < kWord ? P.C - c0 : kWord) : 0;
+    Row w[K], bias, gw[K] = {}, gb = {};
+    taps_of<K>(w, bias, P);
+    constexpr int kSteps = (kRows + K - 1 + kAhead - 1) / kAhead;
     for (long long tile = blockIdx.x; tile < P.all_tiles; tile += gridDim.x) {
         const int b = (int)(tile / P.tiles);
         const long long t0 = (tile % P.tiles) * kTile + walk * kRows;
@@ -127,61 +168,77 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(const ConvParams
         T *gx = static_cast<T *>(P.gx) + s.begin * P.C + c0;
         const float *history = P.state_in != nullptr && K > 1 ? P.state_in + (long long)b * (K - 1) * P.C + c0 : nullptr;
         const float *gso = P.gstate_out != nullptr && K > 1 ? P.gstate_out + (long long)b * (K - 1) * P.C + c0 : nullptr;
-        float old[K][8], dz[K][8] = {};         // rows t-K+1 .. t-1 of e; dz of rows t-K+1 .. t (0 before this walk)
+        Row old[K], dz[K] = {};                 // rows t-K+1 .. t-1 of e; dz of rows t-K+1 .. t (0 before this walk)
+        Quad<T> nx[2][kAhead], ngy[2][kAhead];
+        const T *ax = x + t0 * P.x_stride, *ag = gy + t0 * P.C;
+        auto fetch = [&](int q) {
 #pragma unroll
-        for (int j = 0; j < K - 1; j++) extended<T, K>(old[j], P, x, history, t0 + j - (K - 1), n);
+            for (int r = 0; r < kAhead; r++) {
+                const long long t = t0 + q * kAhead + r;
+                nx[q % 2][r] = word_of<WHOLE>(ax + r * P.x_stride, t < s.len, n, P.x_whole);
+                ngy[q % 2][r] = word_of<WHOLE>(ag + (long long)r * P.C, t < s.len, n, P.c_whole);
+            }
+            ax += kAhead * P.x_stride;
+            ag += (long long)kAhead * P.C;
+        };
+        fetch(0);
+#pragma unroll
+        for (int j = 0; j < K - 1; j++) extended<T, K, WHOLE>(old[j], P, x, history, t0 + j - (K - 1), n);
         const long long end = t0 + kRows < s.len ? t0 + kRows : s.len;      // this walk's own rows end here
         // row t gives dz_t; what then is complete is the gradient of row t - (K - 1), whose last term dz_t is
-#pragma unroll 4
-        for (int r = 0; r < kRows + K - 1; r++) {
-            const long long t = t0 + r;
-            if (t - (K - 1) >= end && t0 != 0) break;
-            float f[8], g[8];
-            row_of(f, x + t * P.x_stride, t < s.len ? n : 0, P.x_whole);
-            row_of(g, gy + t * P.C, t < s.len ? n : 0, P.c_whole);
-            const bool own = t < end;
 #pragma unroll
-            for (int c = 0; c < 8; c++) {
-                float d = g[c];
-                if (P.silu) {
-                    float v = bias[c];
+        for (int q = 0; q < kSteps; q++) {
+            if (t0 + q * kAhead - (K - 1) >= end && t0 != 0) break;
+            if (q + 1 < kSteps) fetch(q + 1);
 #pragma unroll
-                    for (int k = 0; k < K - 1; k++) v = fmaf(w[k][c], old[k][c], v);
-                    v = fmaf(w[K - 1][c], f[c], v);
-                    d *= silu_slope(v, sigmoid_of(v));
+            for (int r = 0; r < kAhead; r++) {
+                const long long t = t0 + q * kAhead + r;
+                Row now, d;
+                pairs_of(now, nx[q % 2][r]);
+                pairs_of(d, ngy[q % 2][r]);            // past the end: zero
+                const bool own = t < end;
+#pragma unroll
+                for (int c = 0; c < kPairs; c++) {
+                    if (P.silu) {
+                        f32x2 z = fma2(w[K - 1][c], now[c], bias[c]);
+#pragma unroll
+                        for (int k = 0; k < K - 1; k++) z = fma2(w[k][c], old[k][c], z);
+                        const f32x2 sg = sigmoid_of(z), one = twice(1.f);
+                        const f32x2 slope = mul2(sg, fma2(z, fma2(sg, twice(-1.f), one), one));
+                        d[c] = t < s.len ? mul2(d[c], slope) : 0ull;        // a select: the slope there may be anything
+                    }
+#pragma unroll
+                    for (int k = 0; k + 1 < K; k++) dz[k][c] = dz[k + 1][c];
+                    dz[K - 1][c] = d[c];
+                    if (own) {
+#pragma unroll
+                        for (int k = 0; k < K - 1; k++) gw[k][c] = fma2(d[c], old[k][c], gw[k][c]);
+                        gw[K - 1][c] = fma2(d[c], now[c], gw[K - 1][c]);
+                        gb[c] = add2(gb[c], d[c]);
+                    }
+#pragma unroll
+                    for (int k = 0; k + 2 < K; k++) old[k][c] = old[k + 1][c];
+                    if (K > 1) old[K > 1 ? K - 2 : 0][c] = now[c];
                 }
-                if (t >= s.len) d = 0.f;
+                const long long i = t - (K - 1);            // the row of x that is complete, or below 0 one of the history
+                if (i >= end || (i < t0 && (t0 != 0 || P.gstate_in == nullptr || K == 1)) || q * kAhead + r >= kRows + K - 1) continue;
+                Row de;
 #pragma unroll
-                for (int k = 0; k + 1 < K; k++) dz[k][c] = dz[k + 1][c];
-                dz[K - 1][c] = d;
-                if (own) {
+                for (int c = 0; c < kPairs; c++) {
+                    de[c] = mul2(w[0][c], dz[K - 1][c]);
 #pragma unroll
-                    for (int k = 0; k < K - 1; k++) gw[k][c] = fmaf(d, old[k][c], gw[k][c]);
-                    gw[K - 1][c] = fmaf(d, f[c], gw[K - 1][c]);
-                    gb[c] += d;
+                    for (int k = 1; k < K; k++) de[c] = fma2(w[k][c], dz[K - 1 - k][c], de[c]);
                 }
+                const long long j = i + (K - 1) - s.len;    // its place in the new history
+                if (j >= 0 && gso != nullptr) {
+                    Row g2;
+                    pairs_of(g2, word_of<WHOLE>(gso + j * P.C, true, n, P.c_whole));
 #pragma unroll
-                for (int k = 0; k + 2 < K; k++) old[k][c] = old[k + 1][c];
-                if (K > 1) old[K > 1 ? K - 2 : 0][c] = f[c];
+                    for (int c = 0; c < kPairs; c++) de[c] = add2(de[c], g2[c]);
+                }
+                if (i >= 0) store_row<WHOLE>(gx + i * P.C, de, n, P.c_whole);
+                else store_row<WHOLE>(P.gstate_in + ((long long)b * (K - 1) + i + K - 1) * P.C + c0, de, n, P.c_whole);
             }
-            const long long i = t - (K - 1);                // the row of x that is complete, or below 0 one of the history
-            if (i >= end || (i < t0 && (t0 != 0 || P.gstate_in == nullptr || K == 1))) continue;
-            float de[8];
-#pragma unroll
-            for (int c = 0; c < 8; c++) {
-                de[c] = 0.f;
-#pragma unroll
-                for (int k = 0; k < K; k++) de[c] = fmaf(w[k][c], dz[K - 1 - k][c], de[c]);
-            }
-            const long long j = i + (K - 1) - s.len;        // its place in the new history
-            if (j >= 0 && gso != nullptr) {
-                float g2[8];
-                row_of(g2, gso + j * P.C, n, P.c_whole);
-#pragma unroll
-                for (int c = 0; c < 8; c++) de[c] += g2[c];
-            }
-            if (i >= 0) store_eight(gx + i * P.C, de, n, P.c_whole);
-            else store_eight(P.gstate_in + ((long long)b * (K - 1) + i + K - 1) * P.C + c0, de, n, P.c_whole);
         }
     }
     if (P.part == nullptr) return;
@@ -190,13 +247,13 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(const ConvParams
     for (int k = 0; k <= K; k++) {
         __syncthreads();
 #pragma unroll
-        for (int c = 0; c < 8; c++) fold[walk][lane][c] = k < K ? gw[k < K ? k : 0][c] : gb[c];
+        for (int c = 0; c < kPairs; c++) *reinterpret_cast<f32x2 *>(&fold[walk][lane * kWord + 2 * c]) = k < K ? gw[k < K ? k : 0][c] : gb[c];
         __syncthreads();
-        for (int i = threadIdx.x; i < kLanes * 8; i += kConvThreads) {
-            const int c = blockIdx.y * kLanes * 8 + i;
+        for (int i = threadIdx.x; i < kChannels; i += kConvThreads) {
+            const int c = blockIdx.y * kChannels + i;
             float v = 0.f;
 #pragma unroll
-            for (int q = 0; q < kWalks; q++) v += fold[q][i / 8][i % 8];
+            for (int q = 0; q < kWalks; q++) v += fold[q][i];
             if (c < P.C) part[k < K ? (long long)c * K + k : (long long)P.C * K + c] = v;
         }
     }
@@ -219,36 +276,40 @@ int check(const cawn_conv_params *p)
 ConvParams fill(const cawn_conv_params *p, const int64_t *offsets)
 {
     ConvParams P = {};
-    const int per = p->flags != 0 ? 8 : 4;
     P.seq = {reinterpret_cast<const long long *>(offsets), p->L, offsets != nullptr ? p->rows : (int64_t)p->B * p->L, p->B};
     P.C = p->C;
     P.x_stride = p->x_stride != 0 ? p->x_stride : p->C;
-    P.words = (int)ceil_div(p->C, 8);
+    P.words = (int)ceil_div(p->C, kWord);
     P.tiles = most(ceil_div(p->L, kTile), 1);
     P.all_tiles = P.tiles * p->B;
     P.silu = p->act == CAWN_CONV_ACT_SILU;
-    P.x_whole = P.x_stride % per == 0;
-    P.c_whole = p->C % per == 0 && p->C % 4 == 0;
+    P.x_whole = P.x_stride % kWord == 0;
+    P.c_whole = p->C % kWord == 0;
     return P;
 }
 
-// Blocks along the tiles in the backward: about eight a SM, each with a partial row of sums.  Never fewer for more tiles.
+// Blocks along the tiles in the backward: as many as run at once by their registers, each with a partial row of sums.  Never fewer for more tiles.
 int64_t workers(const cawn_conv_params *p)
 {
-    const int64_t across = ceil_div(ceil_div(p->C, 8), kLanes), tiles = most(ceil_div(p->L, kTile), 1) * p->B;
-    const int64_t want = most((int64_t)sm_count() * 8 / across, 1);
+    const int64_t across = ceil_div(p->C, kChannels), tiles = most(ceil_div(p->L, kTile), 1) * p->B;
+    const int64_t want = most((int64_t)sm_count() * (p->flags != 0 ? 3 : 2) / across, 1);
     return tiles < want ? tiles : want;
 }
 
 using ConvKernel = void (*)(ConvParams);
-template <class T> ConvKernel pick(int K, bool bwd)
+template <class T, bool WHOLE> ConvKernel pick(int K, bool bwd)
 {
     switch (K) {
-    case 1: return bwd ? conv_bwd_kernel<T, 1> : conv_fwd_kernel<T, 1>;
-    case 2: return bwd ? conv_bwd_kernel<T, 2> : conv_fwd_kernel<T, 2>;
-    case 3: return bwd ? conv_bwd_kernel<T, 3> : conv_fwd_kernel<T, 3>;
-    default: return bwd ? conv_bwd_kernel<T, 4> : conv_fwd_kernel<T, 4>;
+    case 1: return bwd ? conv_bwd_kernel<T, 1, WHOLE> : conv_fwd_kernel<T, 1, WHOLE>;
+    case 2: return bwd ? conv_bwd_kernel<T, 2, WHOLE> : conv_fwd_kernel<T, 2, WHOLE>;
+    case 3: return bwd ? conv_bwd_kernel<T, 3, WHOLE> : conv_fwd_kernel<T, 3, WHOLE>;
+    default: return bwd ? conv_bwd_kernel<T, 4, WHOLE> : conv_fwd_kernel<T, 4, WHOLE>;
     }
+}
+ConvKernel pick(const cawn_conv_params *p, const ConvParams &P, bool bwd)
+{
+    const bool whole = P.x_whole && P.c_whole;
+    return p->flags != 0 ? (whole ? pick<bf16, true>(p->K, bwd) : pick<bf16, false>(p->K, bwd)) : (whole ? pick<float, true>(p->K, bwd) : pick<float, false>(p->K, bwd));
 }
 
 }  // namespace
@@ -265,8 +326,7 @@ extern "C" int cawn_short_conv_fwd(const cawn_conv_params *params, const void *x
     if (!all_aligned16(x, weight, bias, state_in, y, state_out)) return CAWN_ERR_MISALIGNED;
     ConvParams P = fill(params, offsets);
     P.x = x; P.w = weight; P.b = bias; P.state_in = state_in; P.y = y; P.state_out = state_out;
-    const ConvKernel k = params->flags != 0 ? pick<bf16>(params->K, false) : pick<float>(params->K, false);
-    return status_of(launch<true>(k, dim3((unsigned)P.all_tiles, (unsigned)ceil_div(P.words, kLanes)), dim3(kConvThreads), 0,
+    return status_of(launch<true>(pick(params, P, false), dim3((unsigned)P.all_tiles, (unsigned)ceil_div(P.words, kLanes)), dim3(kConvThreads), 0,
                                   static_cast<cudaStream_t>(cuda_stream), P));
 }
 
@@ -300,8 +360,7 @@ extern "C" int cawn_short_conv_bwd(const cawn_conv_params *params, const void *x
     P.x = x; P.w = weight; P.b = bias; P.state_in = state_in; P.gy = grad_y; P.gstate_out = grad_state_out;
     P.gx = grad_x; P.gstate_in = grad_state_in; P.part = sums ? static_cast<float *>(workspace) : nullptr;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const ConvKernel k = params->flags != 0 ? pick<bf16>(params->K, true) : pick<float>(params->K, true);
-    rc = status_of(launch<true>(k, dim3((unsigned)blocks, (unsigned)ceil_div(P.words, kLanes)), dim3(kConvThreads), 0, st, P));
+    rc = status_of(launch<true>(pick(params, P, true), dim3((unsigned)blocks, (unsigned)ceil_div(P.words, kLanes)), dim3(kConvThreads), 0, st, P));
     if (rc != CAWN_OK || !sums) return rc;
     PartialSums S = {P.part, blocks, cols, {grad_weight, grad_bias, nullptr}, {(long long)params->C * params->K, params->C, 0}};
     return sum_partials(S, st);

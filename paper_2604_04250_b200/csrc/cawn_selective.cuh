@@ -4,18 +4,19 @@
 // y = (sum_n C_n h_n + skip x) silu(z).  B and C belong to a token and a group of channels.
 //
 // Layout of the work.  A block has 32 channels of one group and one sequence (or a segment of it) and walks its tokens in
-// tiles; NL lanes share a channel, NS states each (N up to NL * NS), so a block is NL warps.  In a warp lane bits 0-1 are a
-// channel, the next log2 NL bits the lane's states, the rest channels again.  A tile's (d, d x) and rows of B and C are
-// made floats once, in shared memory; the next tile is fetched while one is computed.  Few channels: the time axis is cut
-// into segments that run side by side, behind a pass that finds each segment's own end state and its sum of d (the decay
-// over a segment is e^{A sum d}), so that every exponential is taken twice.
+// tiles of 16.  A thread has CD neighbouring channels and NS states of each; NL lanes share a channel (N up to NL * NS).  In a
+// warp lane bits 0-1 are channels, the next log2 NL bits the lane's states, the rest channels again.  A tile's (d, d x) and
+// rows of B and C are made floats once, in shared memory; the next tile is fetched while one is computed.  What a
+// thread reads there for a token is 8 bytes a channel and 8 a state, so two channels by four states (6 bytes a cell) and not one by
+// four (10): shared memory fills 128 bytes of registers a clock, and that was the bound.
+// Few channels: the time axis is cut into segments that run side by side, behind a pass that finds each segment's own end
+// state and its sum of d (the decay over a segment is e^{A sum d}), so that every exponential is taken twice.
 #pragma once
 #include "cawn_seq.cuh"
 
 namespace cawn {
 
-constexpr int kScanChannels = 32, kCheckpoint = 16;     // tokens between two states that the forward leaves for the backward
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kScanChannels = 32, kTile = 16;           // a tile is also what lies between two states that the forward leaves for the backward
 
 struct SelectiveParams {
     Sequences seq;
@@ -33,58 +34,37 @@ struct SelectiveParams {
     int softplus, whole_x, whole_dt, whole_z, whole_d, whole_b, whole_c;
 };
 
-// log(1 + e^v) without loss where it is small: v^+ + log1p(u), u = e^{-|v|}, log1p(u) = 2 atanh(u / (2 + u)) by its series
-// (u / (2 + u) is at most 1/3, where the first term left out is 2e-9 of the sum).
-__device__ __forceinline__ float softplus_of(float v)
+// log(1 + e^v) = v^+ + log1p(u), u = e^{-|v|} in [0, 1], without loss where it is small: log1p(u) / u by the polynomial of degree
+// 8 that fits it best in relative error (3e-8, found by weighted least squares on Chebyshev points).
+__device__ __forceinline__ f32x2 softplus_of(f32x2 v)
 {
-    const float u = exp2_fast(-kLog2e * fabsf(v)), s = __fdividef(u, 2.f + u), q = s * s;
-    float p = 1.f / 17.f;
-    p = fmaf(p, q, 1.f / 15.f);
-    p = fmaf(p, q, 1.f / 13.f);
-    p = fmaf(p, q, 1.f / 11.f);
-    p = fmaf(p, q, 1.f / 9.f);
-    p = fmaf(p, q, 1.f / 7.f);
-    p = fmaf(p, q, 1.f / 5.f);
-    p = fmaf(p, q, 1.f / 3.f);
-    p = fmaf(p, q, 1.f);
-    return fmaf(2.f * s, p, v > 0.f ? v : v != v ? v : 0.f);
+    const float2 f = halves(v);
+    const float2 e = halves(mul2(pair(fabsf(f.x), fabsf(f.y)), twice(-kLog2e)));
+    const f32x2 u = pair(exp2_fast(e.x), exp2_fast(e.y));
+    f32x2 p = twice(5.232693627e-03f);
+    p = fma2(p, u, twice(-2.950523980e-02f));
+    p = fma2(p, u, twice(7.822596282e-02f));
+    p = fma2(p, u, twice(-1.366324723e-01f));
+    p = fma2(p, u, twice(1.910600811e-01f));
+    p = fma2(p, u, twice(-2.484298199e-01f));
+    p = fma2(p, u, twice(3.331909776e-01f));
+    p = fma2(p, u, twice(-4.999949336e-01f));
+    p = fma2(p, u, twice(9.999999404e-01f));
+    return fma2(p, u, pair(fmaxf(f.x, 0.f), fmaxf(f.y, 0.f)));       // a NaN comes through u
 }
-
-// Four elements as they are stored.
-template <class T> struct Quad;
-template <> struct Quad<bf16> {
-    uint2 w;
-    __device__ __forceinline__ float4 get() const
-    {
-        return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
-    }
-    __device__ __forceinline__ void set(float4 v) { w = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)); }
-    __device__ __forceinline__ void load(const bf16 *p) { w = *reinterpret_cast<const uint2 *>(p); }
-};
-template <> struct Quad<float> {
-    float4 w;
-    __device__ __forceinline__ float4 get() const { return w; }
-    __device__ __forceinline__ void set(float4 v) { w = v; }
-    __device__ __forceinline__ void load(const float *p) { w = *reinterpret_cast<const float4 *>(p); }
-};
-template <class T> __device__ __forceinline__ Quad<T> fetch_quad(const T *p, int n, bool whole)
-{
-    Quad<T> r;
-    if (whole && n >= 4) r.load(p);
-    else r.set(make_float4(n > 0 ? widen(p[0]) : 0.f, n > 1 ? widen(p[1]) : 0.f, n > 2 ? widen(p[2]) : 0.f, n > 3 ? widen(p[3]) : 0.f));
-    return r;
-}
+__device__ __forceinline__ float softplus_of(float v) { return halves(softplus_of(twice(v))).x; }
 
 // Where a thread is, and what its states are.
-template <int NL, int NS> struct Place {
-    static constexpr int kThreads = 32 * NL, kPad = NL * NS, kPairs = NS / 2, kTile = NL >= 4 ? 32 : 16;
-    static constexpr int kShift = NL == 1 ? 0 : NL == 2 ? 1 : NL == 4 ? 2 : 3;
-    int nl, ch;                 // lane among a channel's, channel of the block
+template <int NL, int NS, int CD> struct Place {
+    static constexpr int kThreads = 32 * NL / CD, kPad = NL * NS, kPairs = NS / 2, kShift = NL == 2 ? 1 : NL == 4 ? 2 : 3;
+    static constexpr int kStagers = kThreads < kTile * 4 ? kThreads : kTile * 4, kWords = kTile * 4 / kStagers;
+    static_assert(kTile * kPad / 4 == kThreads, "a quad of B and one of C for each thread");
+    int nl, ch;                 // lane among a channel's, first channel of the block
     __device__ __forceinline__ Place()
     {
         const int lane = threadIdx.x % 32;
         nl = (lane >> 2) & (NL - 1);
-        ch = threadIdx.x / 32 * (32 / NL) + (lane & 3) + 4 * (lane >> (2 + kShift));
+        ch = (threadIdx.x / 32 * (32 / NL) + (lane & 3) + 4 * (lane >> (2 + kShift))) * CD;
     }
 };
 
@@ -131,7 +111,6 @@ __device__ __forceinline__ f32x2 exp2_pair(f32x2 v)
     const float2 f = halves(v);
     return pair(exp2_fast(f.x), exp2_fast(f.y));
 }
-__device__ __forceinline__ f32x2 twice(float v) { return pair(v, v); }
 __device__ __forceinline__ float sum_of(f32x2 v)
 {
     const float2 f = halves(v);
@@ -151,26 +130,21 @@ template <int NS> __device__ __forceinline__ void row_pairs(f32x2 (&r)[NS / 2], 
 // the other half.  Each sum is then written once, to out[token * stride].
 template <int NL> __device__ __forceinline__ void sum_four(const float (&v)[4], int nl, float *out, int stride)
 {
-    if constexpr (NL == 1) {
-#pragma unroll
-        for (int i = 0; i < 4; i++) out[i * stride] = v[i];
+    const bool odd = nl & 1, high = nl & 2;
+    float a = odd ? v[1] : v[0], b = odd ? v[3] : v[2];
+    a += __shfl_xor_sync(0xffffffffu, odd ? v[0] : v[1], 4);
+    b += __shfl_xor_sync(0xffffffffu, odd ? v[2] : v[3], 4);
+    if constexpr (NL == 2) {
+        out[nl * stride] = a;
+        out[(nl + 2) * stride] = b;
     } else {
-        const bool odd = nl & 1, high = nl & 2;
-        float a = odd ? v[1] : v[0], b = odd ? v[3] : v[2];
-        a += __shfl_xor_sync(0xffffffffu, odd ? v[0] : v[1], 4);
-        b += __shfl_xor_sync(0xffffffffu, odd ? v[2] : v[3], 4);
-        if constexpr (NL == 2) {
-            out[nl * stride] = a;
-            out[(nl + 2) * stride] = b;
+        float c = high ? b : a;
+        c += __shfl_xor_sync(0xffffffffu, high ? a : b, 8);
+        if constexpr (NL == 8) {
+            c += __shfl_xor_sync(0xffffffffu, c, 16);
+            if (nl < 4) out[nl * stride] = c;
         } else {
-            float c = high ? b : a;
-            c += __shfl_xor_sync(0xffffffffu, high ? a : b, 8);
-            if constexpr (NL == 8) {
-                c += __shfl_xor_sync(0xffffffffu, c, 16);
-                if (nl < 4) out[nl * stride] = c;
-            } else {
-                out[nl * stride] = c;
-            }
+            out[nl * stride] = c;
         }
     }
 }
@@ -186,11 +160,16 @@ template <int NS> __device__ __forceinline__ void fold_segment(f32x2 (&h)[NS / 2
 }
 
 // First checkpoint of a sequence: those of two sequences never meet, whatever the lengths.
-__device__ __forceinline__ long long checkpoint_of(const Span &s, int b) { return s.begin / kCheckpoint + b; }
+__device__ __forceinline__ long long checkpoint_of(const Span &s, int b) { return s.begin / kTile + b; }
 
 using SelectiveKernel = void (*)(SelectiveParams);
-struct Shape { int nl, ns; };
-inline Shape shape_of(int N) { return N <= 4 ? Shape{1, 4} : N <= 8 ? Shape{2, 4} : N <= 16 ? Shape{4, 4} : N <= 32 ? Shape{8, 4} : Shape{8, 8}; }
+struct Shape {
+    int nl, ns, cd;
+    int warps() const { return nl / cd; }
+};
+inline Shape shape_of(int N) { return N <= 8 ? Shape{2, 4, 2} : N <= 16 ? Shape{4, 4, 2} : N <= 32 ? Shape{8, 4, 2} : Shape{8, 8, 1}; }
+// A launch for the shape: CALL(NL, NS, CD).
+#define CAWN_BY_SHAPE(S, CALL) ((S).ns == 8 ? CALL(8, 8, 1) : (S).nl == 8 ? CALL(8, 4, 2) : (S).nl == 4 ? CALL(4, 4, 2) : CALL(2, 4, 2))
 
 // One call of each kernel family; the grid is (blocks of channels x sequences, segments).
 int launch_selective_fwd(const SelectiveParams &P, const Shape &s, bool half, bool summary, cudaStream_t st);

@@ -31,7 +31,7 @@ int64_t rows_of(const cawn_scan_params *p) { return p->rows > 0 ? p->rows : (int
 // Segments of the time axis.  Whole sequences when their blocks fill the GPU (`fill` warps a multiprocessor); otherwise
 // as many segments as do, none shorter than 256 tokens.
 constexpr int kFill = 12, kShortest = 256;
-int64_t wanted(const cawn_scan_params *p) { return most((int64_t)sm_count() * kFill / (blocks_of(p) * shape_of(p->N).nl), 1); }    // sequences x segments
+int64_t wanted(const cawn_scan_params *p) { return most((int64_t)sm_count() * kFill / (blocks_of(p) * shape_of(p->N).warps()), 1); }    // sequences x segments
 int64_t segments_of(const cawn_scan_params *p)
 {
     const int64_t want = wanted(p);
@@ -60,7 +60,7 @@ struct Carver {
 
 // Partial sums of grad_A, grad_skip and grad_dt_bias: rows that begin on 16 bytes.
 int64_t param_cols(const cawn_scan_params *p) { return ceil_div((int64_t)p->D * (p->N + 2), 4) * 4; }
-int64_t checkpoint_rows(const cawn_scan_params *p) { return rows_of(p) / kCheckpoint + p->B + 1; }
+int64_t checkpoint_rows(const cawn_scan_params *p) { return rows_of(p) / kTile + p->B + 1; }
 
 // `sized`: for any call up to this one (the size query) instead of for this very call.
 void carve_segments(Carver &c, SelectiveParams &P, const cawn_scan_params *p, bool first, bool sized)

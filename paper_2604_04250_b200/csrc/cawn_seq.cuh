@@ -92,7 +92,59 @@ template <class T> __device__ __forceinline__ void store_eight(T *p, const float
     }
 }
 
-__device__ __forceinline__ float sigmoid_of(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
+// Four elements as they are stored.
+template <class T> struct Quad;
+template <> struct __align__(8) Quad<bf16> {
+    uint2 w;
+    __device__ __forceinline__ float4 get() const
+    {
+        return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
+    }
+    __device__ __forceinline__ void set(float4 v) { w = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)); }
+    __device__ __forceinline__ void load(const bf16 *p) { w = *reinterpret_cast<const uint2 *>(p); }
+};
+template <> struct __align__(16) Quad<float> {
+    float4 w;
+    __device__ __forceinline__ float4 get() const { return w; }
+    __device__ __forceinline__ void set(float4 v) { w = v; }
+    __device__ __forceinline__ void load(const float *p) { w = *reinterpret_cast<const float4 *>(p); }
+};
+template <class T> __device__ __forceinline__ Quad<T> fetch_quad(const T *p, int n, bool whole)
+{
+    Quad<T> r;
+    if (whole && n >= 4) r.load(p);
+    else r.set(make_float4(n > 0 ? widen(p[0]) : 0.f, n > 1 ? widen(p[1]) : 0.f, n > 2 ? widen(p[2]) : 0.f, n > 3 ? widen(p[3]) : 0.f));
+    return r;
+}
+template <class T> __device__ __forceinline__ void store_quad(T *p, float4 v, int n, bool whole)
+{
+    if (whole && n >= 4) {
+        Quad<T> r;
+        r.set(v);
+        *reinterpret_cast<Quad<T> *>(p) = r;
+    } else {
+        if (n > 0) p[0] = narrow<T>(v.x);
+        if (n > 1) p[1] = narrow<T>(v.y);
+        if (n > 2) p[2] = narrow<T>(v.z);
+        if (n > 3) p[3] = narrow<T>(v.w);
+    }
+}
+
+__device__ __forceinline__ float reciprocal_fast(float v)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+__device__ __forceinline__ float sigmoid_of(float v) { return reciprocal_fast(1.f + exp2_fast(-kLog2e * v)); }
+__device__ __forceinline__ f32x2 twice(float v) { return pair(v, v); }
+__device__ __forceinline__ f32x2 sigmoid_of(f32x2 v)
+{
+    const float2 e = halves(mul2(v, twice(-kLog2e)));
+    const float2 d = halves(add2(pair(exp2_fast(e.x), exp2_fast(e.y)), twice(1.f)));
+    return pair(reciprocal_fast(d.x), reciprocal_fast(d.y));
+}
 // Slope of v sigmoid(v), with sg = sigmoid(v).
 __device__ __forceinline__ float silu_slope(float v, float sg) { return sg * fmaf(v, 1.f - sg, 1.f); }
 
