@@ -31,12 +31,13 @@ struct SelectiveParams {
     long long per;                              // tokens of a segment, a multiple of 32
     int D, N, G, Dg, blocks;                    // channels of a group, blocks of channels per group
     int S;                                      // segments
-    int softplus, whole_x, whole_dt, whole_z, whole_d, whole_b, whole_c;
+    int softplus, whole_x, whole_dt, whole_z, whole_d, whole_b, whole_c, whole;     // whole: all of them
 };
 
 // log(1 + e^v) = v^+ + log1p(u), u = e^{-|v|} in [0, 1], without loss where it is small: log1p(u) / u by the polynomial of degree
 // 8 that fits it best in relative error (3e-8, found by weighted least squares on Chebyshev points).
-__device__ __forceinline__ f32x2 softplus_of(f32x2 v)
+// Its slope 1 / (1 + e^{-v}) is 1 / (1 + u), or u times that for v < 0.
+template <bool SLOPE> __device__ __forceinline__ f32x2 softplus_of(f32x2 v, f32x2 &slope)
 {
     const float2 f = halves(v);
     const float2 e = halves(mul2(pair(fabsf(f.x), fabsf(f.y)), twice(-kLog2e)));
@@ -50,9 +51,20 @@ __device__ __forceinline__ f32x2 softplus_of(f32x2 v)
     p = fma2(p, u, twice(3.331909776e-01f));
     p = fma2(p, u, twice(-4.999949336e-01f));
     p = fma2(p, u, twice(9.999999404e-01f));
+    if constexpr (SLOPE) {
+        const float2 d = halves(add2(u, twice(1.f))), w = halves(u);
+        const float x = reciprocal_fast(d.x), y = reciprocal_fast(d.y);
+        slope = pair(f.x > 0.f ? x : x * w.x, f.y > 0.f ? y : y * w.y);
+    }
     return fma2(p, u, pair(fmaxf(f.x, 0.f), fmaxf(f.y, 0.f)));       // a NaN comes through u
 }
+__device__ __forceinline__ f32x2 softplus_of(f32x2 v)
+{
+    f32x2 none;
+    return softplus_of<false>(v, none);
+}
 __device__ __forceinline__ float softplus_of(float v) { return halves(softplus_of(twice(v))).x; }
+__device__ __forceinline__ f32x2 chosen(bool c, f32x2 a, f32x2 b) { return c ? a : b; }
 
 // Where a thread is, and what its states are.
 template <int NL, int NS, int CD> struct Place {
@@ -127,25 +139,47 @@ template <int NS> __device__ __forceinline__ void row_pairs(f32x2 (&r)[NS / 2], 
 }
 
 // Four tokens' sums over the NL lanes of a channel, by halving: each exchange sends half of a lane's values away and keeps
-// the other half.  Each sum is then written once, to out[token * stride].
-template <int NL> __device__ __forceinline__ void sum_four(const float (&v)[4], int nl, float *out, int stride)
+// the other half.  v[q] then holds the sum of token nl % 4 + 2 q of the four (two sums with NL = 2, otherwise one).
+template <int NL> struct Four { static constexpr int kSums = NL == 2 ? 2 : 1; };
+template <int NL> __device__ __forceinline__ void sum_four(float (&v)[4], int nl)
 {
     const bool odd = nl & 1, high = nl & 2;
     float a = odd ? v[1] : v[0], b = odd ? v[3] : v[2];
     a += __shfl_xor_sync(0xffffffffu, odd ? v[0] : v[1], 4);
     b += __shfl_xor_sync(0xffffffffu, odd ? v[2] : v[3], 4);
     if constexpr (NL == 2) {
-        out[nl * stride] = a;
-        out[(nl + 2) * stride] = b;
+        v[0] = a;
+        v[1] = b;
     } else {
         float c = high ? b : a;
         c += __shfl_xor_sync(0xffffffffu, high ? a : b, 8);
-        if constexpr (NL == 8) {
-            c += __shfl_xor_sync(0xffffffffu, c, 16);
-            if (nl < 4) out[nl * stride] = c;
-        } else {
-            out[nl * stride] = c;
+        if constexpr (NL == 8) c += __shfl_xor_sync(0xffffffffu, c, 16);
+        v[0] = c;
+    }
+}
+// A lane's CD neighbouring channels of a row; `n` of them are there.
+template <class T, int CD> __device__ __forceinline__ void store_channels(T *p, const float (&f)[CD], int n, bool whole)
+{
+    if constexpr (CD == 2) {
+        if (whole && n >= 2) {
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<unsigned *>(p) = pack_bf16(f[0], f[1]);
+            else *reinterpret_cast<float2 *>(p) = make_float2(f[0], f[1]);
+            return;
         }
+    }
+#pragma unroll
+    for (int j = 0; j < CD; j++)
+        if (j < n) p[j] = narrow<T>(f[j]);
+}
+// CD neighbouring pairs of floats in shared memory.
+template <int CD> __device__ __forceinline__ void two_of(float2 (&d)[CD], const float2 *p)
+{
+    if constexpr (CD == 2) {
+        const float4 v = *reinterpret_cast<const float4 *>(p);
+        d[0] = make_float2(v.x, v.y);
+        d[CD - 1] = make_float2(v.z, v.w);
+    } else {
+        d[0] = *p;
     }
 }
 
@@ -168,6 +202,24 @@ struct Shape {
     int warps() const { return nl / cd; }
 };
 inline Shape shape_of(int N) { return N <= 8 ? Shape{2, 4, 2} : N <= 16 ? Shape{4, 4, 2} : N <= 32 ? Shape{8, 4, 2} : Shape{8, 8, 1}; }
+// Rows all of whose words are whole are fetched without a branch.
+template <bool WHOLE, class T> __device__ __forceinline__ Eight<T> eight_of(const T *p, int n, bool whole)
+{
+    if constexpr (!WHOLE) return fetch_eight(p, n, whole);
+    Eight<T> r;
+    r.clear();
+    if (n > 0) r.load(p);
+    return r;
+}
+template <bool WHOLE, class T> __device__ __forceinline__ Quad<T> quad_of(const T *p, int n, bool whole)
+{
+    if constexpr (!WHOLE) return fetch_quad(p, n, whole);
+    Quad<T> r;
+    r.set(make_float4(0.f, 0.f, 0.f, 0.f));
+    if (n > 0) r.load(p);
+    return r;
+}
+
 // A launch for the shape: CALL(NL, NS, CD).
 #define CAWN_BY_SHAPE(S, CALL) ((S).ns == 8 ? CALL(8, 8, 1) : (S).nl == 8 ? CALL(8, 4, 2) : (S).nl == 4 ? CALL(4, 4, 2) : CALL(2, 4, 2))
 

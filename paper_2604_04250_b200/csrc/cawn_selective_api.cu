@@ -93,6 +93,7 @@ SelectiveParams fill(const cawn_scan_params *p, const int64_t *offsets, const vo
     const uintptr_t quad = p->flags != 0 ? 7 : 15;
     P.whole_b = p->N % 4 == 0 && P.bs % 4 == 0 && (reinterpret_cast<uintptr_t>(b) & quad) == 0;
     P.whole_c = p->N % 4 == 0 && P.cs % 4 == 0 && (reinterpret_cast<uintptr_t>(c) & quad) == 0;
+    P.whole = P.whole_x && P.whole_dt && P.whole_z && P.whole_d && P.whole_b && P.whole_c;
     P.softplus = p->softplus;
     P.S = (int)segments_of(p);
     P.param_cols = param_cols(p);

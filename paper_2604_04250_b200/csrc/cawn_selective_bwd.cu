@@ -38,17 +38,16 @@ template <> __device__ __forceinline__ void sum_channels<float>(float (&d)[4], u
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(one), "r"(0u), "r"(x), "r"(y));
 }
 
-template <class T, int NL, int NS, int CD> struct BwdShared {
+template <int NL, int NS, int CD> struct BwdShared {
     using At = Place<NL, NS, CD>;
-    static constexpr int kRow = 40, kWarps = At::kThreads / 32;
-    float2 dd[kTile][kScanChannels];
-    float bc[2][kTile][At::kPad];
-    float dy[kTile][kRow];
-    float sums[3][kTile][kRow];             // flow, drift (sum of lam w A log2 e), read-out
+    static constexpr int kWarps = At::kThreads / 32;
+    float2 dd[2][kTile][kScanChannels];     // d, d x
+    float2 dy[2][kTile][kScanChannels];     // dy', x
+    float2 slopes[2][kTile][kScanChannels]; // slope of d by dt; dy silu'(z)
+    float bc[2][2][kTile][At::kPad];
     float red[2][kWarps][NS * 2 * 64];      // [state of a lane][dB, dC][token of eight][group of lanes]
-    float param[2][At::kStagers][8];        // grad_skip, grad_dt_bias of a stager's channels
+    float4 states[kTile / 4 - 1][CD * NS / 4][At::kThreads];        // a thread's own, in front of tokens 4, 8 and 12
     float bias[kScanChannels], skip[kScanChannels];
-    struct { Eight<T> x, dt, z, gy; } words[At::kWords][At::kStagers];      // a stager's own, from staging to output
 };
 
 template <class T, int NL, int NS, int CD, bool GATE>
@@ -56,9 +55,9 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
 {
     follow_previous();
     using At = Place<NL, NS, CD>;
-    using Shared = BwdShared<T, NL, NS, CD>;
-    constexpr int kThreads = At::kThreads, NP = At::kPad, NK = At::kPairs, kRow = Shared::kRow, kWords = At::kWords, kStagers = At::kStagers;
-    constexpr int TS = 4, kSubs = kTile / TS;       // tokens whose decays stay in registers
+    using Shared = BwdShared<NL, NS, CD>;
+    constexpr int kThreads = At::kThreads, NP = At::kPad, NK = At::kPairs, kWords = At::kWords, kStagers = At::kStagers;
+    constexpr int TS = 4, kSums = Four<NL>::kSums;      // tokens whose decays stay in registers
     extern __shared__ __align__(16) unsigned char raw_shared[];
     Shared &sh = *reinterpret_cast<Shared *>(raw_shared);
 
@@ -72,6 +71,7 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
     float *param = P.part_param + ((long long)b * P.S + seg) * P.param_cols;
 
     f32x2 A2[CD][NK], carry[CD][NK], dA[CD][NK];
+    float gskip[CD] = {}, gbias[CD] = {};               // of the tokens whose sums this lane ends up with
 #pragma unroll
     for (int j = 0; j < CD; j++) {
         const bool in = at.ch + j < nch;
@@ -89,15 +89,14 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
         sh.bias[i] = i < nch && P.dt_bias != nullptr ? P.dt_bias[c0 + i] : 0.f;
         sh.skip[i] = i < nch && P.skip != nullptr ? P.skip[c0 + i] : 0.f;
     }
-    for (int i = tid; i < 2 * kStagers * 8; i += kThreads) (&sh.param[0][0][0])[i] = 0.f;
 
     const T *x = static_cast<const T *>(P.x) + s.begin * P.xs + c0, *dt = static_cast<const T *>(P.dt) + s.begin * P.dts + c0;
     const T *z = GATE ? static_cast<const T *>(P.z) + s.begin * P.zs + c0 : nullptr, *gy = static_cast<const T *>(P.gy) + s.begin * P.D + c0;
     const int word = tid % 4 * 8, quad_row = tid / (NP / 4), quad = tid % (NP / 4) * 4;
     const T *bm = static_cast<const T *>(P.bm) + (s.begin + quad_row) * P.bs + g * P.N + quad, *cm = static_cast<const T *>(P.cm) + (s.begin + quad_row) * P.cs + g * P.N + quad;
     const float *marks = P.checkpoints + (checkpoint_of(s, b) * P.D + c0 + at.ch) * P.N;
-    T *gx = static_cast<T *>(P.gx) + s.begin * P.D + c0, *gdt = static_cast<T *>(P.gdt) + s.begin * P.D + c0;
-    T *gz = GATE ? static_cast<T *>(P.gz) + s.begin * P.D + c0 : nullptr;
+    T *gx = static_cast<T *>(P.gx) + s.begin * P.D + c0 + at.ch, *gdt = static_cast<T *>(P.gdt) + s.begin * P.D + c0 + at.ch;
+    T *gz = GATE ? static_cast<T *>(P.gz) + s.begin * P.D + c0 + at.ch : nullptr;
     float *bc_out = P.part_bc + ((long long)cb * P.seq.rows + s.begin) * 2 * P.N;
     Eight<T> nx[kWords], ndt[kWords], nz[kWords], ngy[kWords];
     Quad<T> nb, nc;
@@ -115,15 +114,13 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
         const int left = t0 + quad_row < end ? P.N - quad : 0;
         nb = fetch_quad(bm + t0 * P.bs, left, P.whole_b);
         nc = fetch_quad(cm + t0 * P.cs, left, P.whole_c);
+    };
+    auto fetch_states = [&](long long t0) {
 #pragma unroll
         for (int j = 0; j < CD; j++) load_states<NS>(nh[j], marks + (t0 / kTile * P.D + j) * P.N, n0, P.N, at.ch + j < nch);
     };
-    const long long last = begin + (end - 1 - begin) / kTile * kTile;
-    if (end > begin) fetch(last);
-    int buf = 0;
-    for (long long t0 = last; t0 >= begin && end > begin; t0 -= kTile) {
-        __syncthreads();
-        if (tid < kStagers) {
+    auto stage = [&](long long t0, int to) {
+        if (kStagers == kThreads || tid < kStagers) {
 #pragma unroll
             for (int i = 0; i < kWords; i++) {
                 const int r = tid / 4 + i * (kStagers / 4);
@@ -131,200 +128,213 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
                 nx[i].widen_to(xf);
                 ndt[i].widen_to(df);
                 ngy[i].widen_to(gf);
-                auto &own = sh.words[i][tid];
-                own.x = nx[i];
-                own.dt = ndt[i];
-                own.gy = ngy[i];
-                if (GATE) {
-                    nz[i].widen_to(zf);
-                    own.z = nz[i];
-                }
-                const bool there = t0 + r < end;
+                if (GATE) nz[i].widen_to(zf);
+                const f32x2 there = twice(t0 + r < end ? 1.f : 0.f);
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
-                    const f32x2 raw = add2(pair(df[j], df[j + 1]), *reinterpret_cast<const f32x2 *>(&sh.bias[word + j]));
-                    const float2 d = halves(P.softplus ? softplus_of(raw) : raw);
-                    *reinterpret_cast<float4 *>(&sh.dd[r][word + j]) = there ? make_float4(d.x, d.x * xf[j], d.y, d.y * xf[j + 1]) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    f32x2 dy = pair(gf[j], gf[j + 1]);
-                    if (GATE) dy = mul2(dy, mul2(pair(zf[j], zf[j + 1]), sigmoid_of(pair(zf[j], zf[j + 1]))));
-                    *reinterpret_cast<f32x2 *>(&sh.dy[r][word + j]) = dy;
+                    const f32x2 xx = pair(xf[j], xf[j + 1]), raw = add2(pair(df[j], df[j + 1]), *reinterpret_cast<const f32x2 *>(&sh.bias[word + j]));
+                    f32x2 slope, dy = pair(gf[j], gf[j + 1]), past = 0ull;
+                    f32x2 d = softplus_of<true>(raw, slope);
+                    d = mul2(chosen(P.softplus, d, raw), there);
+                    slope = chosen(P.softplus, slope, twice(1.f));
+                    if constexpr (GATE) {
+                        const f32x2 zz = pair(zf[j], zf[j + 1]), sg = sigmoid_of(zz), one = twice(1.f);
+                        past = mul2(dy, mul2(sg, fma2(zz, fma2(sg, twice(-1.f), one), one)));
+                        dy = mul2(dy, mul2(zz, sg));
+                    }
+                    float2 u = halves(d), v = halves(mul2(d, xx));
+                    *reinterpret_cast<float4 *>(&sh.dd[to][r][word + j]) = make_float4(u.x, v.x, u.y, v.y);
+                    u = halves(dy);
+                    *reinterpret_cast<float4 *>(&sh.dy[to][r][word + j]) = make_float4(u.x, xf[j], u.y, xf[j + 1]);
+                    u = halves(slope);
+                    v = halves(past);
+                    *reinterpret_cast<float4 *>(&sh.slopes[to][r][word + j]) = make_float4(u.x, v.x, u.y, v.y);
                 }
             }
         }
-        *reinterpret_cast<float4 *>(&sh.bc[0][quad_row][quad]) = nb.get();
-        *reinterpret_cast<float4 *>(&sh.bc[1][quad_row][quad]) = nc.get();
-        f32x2 hs[kSubs][CD][NK];                        // the states in front of each four tokens
+        *reinterpret_cast<float4 *>(&sh.bc[to][0][quad_row][quad]) = nb.get();
+        *reinterpret_cast<float4 *>(&sh.bc[to][1][quad_row][quad]) = nc.get();
+    };
+    const long long last = begin + (end - 1 - begin) / kTile * kTile;
+    __syncthreads();            // bias, skip
+    float skip[CD];
+#pragma unroll
+    for (int j = 0; j < CD; j++) skip[j] = sh.skip[at.ch + j];
+    if (end > begin) {
+        fetch(last);
+        fetch_states(last);
+        stage(last, 0);
+        if (last > begin) fetch(last - kTile);
+    }
+    int buf = 0, turn = 0;
+    for (long long t0 = last; t0 >= begin && end > begin; t0 -= kTile, buf ^= 1) {
+        __syncthreads();        // this tile is staged, and the one behind it has been read
+        f32x2 h[CD][NK], h0[CD][NK];
 #pragma unroll
         for (int j = 0; j < CD; j++)
 #pragma unroll
-            for (int k = 0; k < NK; k++) hs[0][j][k] = nh[j][k];
-        __syncthreads();
-        if (t0 > begin) fetch(t0 - kTile);
-        auto token = [&](float2 (&d)[CD], int t) {
-            if constexpr (CD == 2) {
-                const float4 v = *reinterpret_cast<const float4 *>(&sh.dd[t][at.ch]);
-                d[0] = make_float2(v.x, v.y);
-                d[CD - 1] = make_float2(v.z, v.w);
-            } else {
-                d[0] = sh.dd[t][at.ch];
-            }
-        };
+            for (int k = 0; k < NK; k++) h[j][k] = h0[j][k] = nh[j][k];
+        if (t0 > begin) {
+            fetch_states(t0 - kTile);
+            stage(t0 - kTile, buf ^ 1);
+            if (t0 - kTile > begin) fetch(t0 - 2 * kTile);
+        }
+        const float2 (*dds)[kScanChannels] = sh.dd[buf], (*dys)[kScanChannels] = sh.dy[buf];
+        const float (*bs)[NP] = sh.bc[buf][0], (*cs)[NP] = sh.bc[buf][1];
 #pragma unroll
-        for (int u = 0; u + 1 < kSubs; u++) {
-#pragma unroll
-            for (int j = 0; j < CD; j++)
-#pragma unroll
-                for (int k = 0; k < NK; k++) hs[u + 1][j][k] = hs[u][j][k];
+        for (int u = 0; u < kTile / TS - 1; u++) {
 #pragma unroll
             for (int i = 0; i < TS; i++) {
                 float2 d[CD];
                 f32x2 B[NK];
-                token(d, u * TS + i);
-                row_pairs<NS>(B, &sh.bc[0][u * TS + i][n0]);
+                two_of<CD>(d, &dds[u * TS + i][at.ch]);
+                row_pairs<NS>(B, &bs[u * TS + i][n0]);
 #pragma unroll
                 for (int j = 0; j < CD; j++)
 #pragma unroll
-                    for (int k = 0; k < NK; k++)
-                        hs[u + 1][j][k] = fma2(exp2_pair(mul2(twice(d[j].x), A2[j][k])), hs[u + 1][j][k], mul2(twice(d[j].y), B[k]));
+                    for (int k = 0; k < NK; k++) h[j][k] = fma2(exp2_pair(mul2(twice(d[j].x), A2[j][k])), h[j][k], mul2(twice(d[j].y), B[k]));
             }
-        }
-        float sums[NS][4];
-#pragma unroll
-        for (int u = kSubs - 1; u >= 0; u--) {
-            const int t1 = u * TS;
-            f32x2 a[TS][CD][NK], w[TS][CD][NK], h[CD][NK];
 #pragma unroll
             for (int j = 0; j < CD; j++)
 #pragma unroll
-                for (int k = 0; k < NK; k++) h[j][k] = hs[u][j][k];
-            float v[CD][TS];
-#pragma unroll
-            for (int i = 0; i < TS; i++) {
-                float2 d[CD];
-                f32x2 B[NK], C[NK];
-                token(d, t1 + i);
-                row_pairs<NS>(B, &sh.bc[0][t1 + i][n0]);
-                if constexpr (GATE) row_pairs<NS>(C, &sh.bc[1][t1 + i][n0]);
-#pragma unroll
-                for (int j = 0; j < CD; j++) {
-                    f32x2 acc = 0ull;
-#pragma unroll
-                    for (int k = 0; k < NK; k++) {
-                        a[i][j][k] = exp2_pair(mul2(twice(d[j].x), A2[j][k]));
-                        w[i][j][k] = mul2(a[i][j][k], h[j][k]);
-                        h[j][k] = fma2(twice(d[j].y), B[k], w[i][j][k]);
-                        if constexpr (GATE) acc = k == 0 ? mul2(h[j][k], C[k]) : fma2(h[j][k], C[k], acc);
-                    }
-                    if constexpr (GATE) v[j][i] = sum_of(acc);
+                for (int k = 0; k < NK; k += 2) {
+                    const float2 p = halves(h[j][k]), q = halves(h[j][k + 1]);
+                    sh.states[u][(j * NK + k) / 2][tid] = make_float4(p.x, p.y, q.x, q.y);
                 }
-            }
-            if constexpr (GATE) {
-#pragma unroll
-                for (int j = 0; j < CD; j++) sum_four<NL>(v[j], at.nl, &sh.sums[2][t1][at.ch + j], kRow);
-            }
-            if (u % 2 == 1) {
-#pragma unroll
-                for (int k = 0; k < NS; k++) sums[k][0] = sums[k][1] = sums[k][2] = sums[k][3] = 0.f;
-            }
-            float flow[CD][TS], drift[CD][TS];
-#pragma unroll
-            for (int i = TS - 1; i >= 0; i--) {
-                const int t = t1 + i;
-                float2 d[CD];
-                f32x2 B[NK], C[NK], gb[NK], gc[NK];
-                token(d, t);
-                row_pairs<NS>(B, &sh.bc[0][t][n0]);
-                row_pairs<NS>(C, &sh.bc[1][t][n0]);
-#pragma unroll
-                for (int j = 0; j < CD; j++) {
-                    const f32x2 dl = twice(d[j].x), dx = twice(d[j].y), dy = twice(sh.dy[t][at.ch + j]);
-                    f32x2 fl = 0ull, dr = 0ull;
-#pragma unroll
-                    for (int k = 0; k < NK; k++) {
-                        const f32x2 now = fma2(dx, B[k], w[i][j][k]), lam = fma2(C[k], dy, carry[j][k]), m = mul2(lam, w[i][j][k]);
-                        fl = k == 0 ? mul2(lam, B[k]) : fma2(lam, B[k], fl);
-                        dr = k == 0 ? mul2(m, A2[j][k]) : fma2(m, A2[j][k], dr);
-                        dA[j][k] = fma2(m, dl, dA[j][k]);
-                        carry[j][k] = mul2(a[i][j][k], lam);
-                        gb[k] = j == 0 ? mul2(lam, dx) : fma2(lam, dx, gb[k]);
-                        gc[k] = j == 0 ? mul2(now, dy) : fma2(now, dy, gc[k]);
-                    }
-                    flow[j][i] = sum_of(fl);
-                    drift[j][i] = sum_of(dr);
-                }
-                const unsigned one = lane >> 2 == t % 8 ? (sizeof(T) == 2 ? 0x3f803f80u : 0x3f800000u) : 0u;
-#pragma unroll
-                for (int k = 0; k < NK; k++) {
-                    const float2 p = halves(gb[k]), q = halves(gc[k]);
-                    sum_channels<T>(sums[2 * k], one, p.x, q.x);
-                    sum_channels<T>(sums[2 * k + 1], one, p.y, q.y);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < CD; j++) {
-                sum_four<NL>(flow[j], at.nl, &sh.sums[0][t1][at.ch + j], kRow);
-                sum_four<NL>(drift[j], at.nl, &sh.sums[1][t1][at.ch + j], kRow);
-            }
-            if (u % 2 == 0) {
-                // rows of a selection's result: eight tokens; columns: the groups of lanes that a lane / 4 names
-                float *red = sh.red[buf][tid / 32] + lane * 2;
-#pragma unroll
-                for (int k = 0; k < NS; k++) {
-                    *reinterpret_cast<float2 *>(red + k * 128) = make_float2(sums[k][0], sums[k][1]);
-                    *reinterpret_cast<float2 *>(red + k * 128 + 64) = make_float2(sums[k][2], sums[k][3]);
-                }
-                __syncthreads();
-                // warps, and groups of channels in a warp, in their order; neighbours take neighbouring lane groups
-                for (int o = tid; o < 16 * NP; o += kThreads) {
-                    const int nl = o % NL, i = o / NL % 8, m = o / (NL * 8) % 2, k = o / (NL * 16), n = nl * NS + k;
-                    float sum = 0.f;
-#pragma unroll
-                    for (int r = 0; r < Shared::kWarps; r++)
-#pragma unroll
-                        for (int q = 0; q < 8; q += NL) sum += sh.red[buf][r][((k * 2 + m) * 8 + i) * 8 + q + nl];
-                    if (n < P.N && t0 + t1 + i < end) bc_out[((t0 + t1 + i) * 2 + m) * P.N + n] = sum;
-                }
-                buf ^= 1;
-            }
         }
-        if (tid < kStagers) {
+        // Eight tokens, then the eight before them, four at a time.
+#pragma unroll 1
+        for (int half = 1; half >= 0; half--, turn ^= 1) {
+            float sums[NS][4] = {};
 #pragma unroll
-            for (int i = 0; i < kWords; i++) {
-                const int r = tid / 4 + i * (kStagers / 4);
-                if (t0 + r >= end) break;
-                const auto &own = sh.words[i][tid];
-                float xf[8], df[8], gf[8], zf[8], ox[8], od[8], oz[8];
-                own.x.widen_to(xf);
-                own.dt.widen_to(df);
-                own.gy.widen_to(gf);
-                if (GATE) own.z.widen_to(zf);
+            for (int u = 1; u >= 0; u--) {
+                const int t1 = half * 8 + u * TS;
+                f32x2 a[TS][CD][NK], w[TS][CD][NK];
+                if (t1 == 0) {
 #pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    auto two = [&](const float *p) { return *reinterpret_cast<const f32x2 *>(p + word + j); };
-                    const float4 d = *reinterpret_cast<const float4 *>(&sh.dd[r][word + j]);
-                    const f32x2 xx = pair(xf[j], xf[j + 1]), fl = two(sh.sums[0][r]), skip = two(sh.skip), dy = two(sh.dy[r]);
-                    const f32x2 raw = add2(pair(df[j], df[j + 1]), two(sh.bias));
-                    f32x2 o = fma2(pair(d.x, d.z), fl, mul2(skip, dy));
-                    float2 v = halves(o);
-                    ox[j] = v.x; ox[j + 1] = v.y;
-                    o = fma2(two(sh.sums[1][r]), twice(kLn2), mul2(xx, fl));
-                    if (P.softplus) o = mul2(o, sigmoid_of(raw));
-                    v = halves(o);
-                    od[j] = v.x; od[j + 1] = v.y;
-                    if (GATE) {
-                        const f32x2 zz = pair(zf[j], zf[j + 1]), sg = sigmoid_of(zz), one = twice(1.f);
-                        const f32x2 slope = mul2(sg, fma2(zz, fma2(sg, twice(-1.f), one), one));
-                        v = halves(mul2(mul2(pair(gf[j], gf[j + 1]), slope), fma2(skip, xx, two(sh.sums[2][r]))));
-                        oz[j] = v.x; oz[j + 1] = v.y;
-                    }
-                    f32x2 *acc = reinterpret_cast<f32x2 *>(&sh.param[0][tid][j]);
-                    *acc = fma2(dy, xx, *acc);
-                    acc = reinterpret_cast<f32x2 *>(&sh.param[1][tid][j]);
-                    *acc = add2(o, *acc);
+                    for (int j = 0; j < CD; j++)
+#pragma unroll
+                        for (int k = 0; k < NK; k++) h[j][k] = h0[j][k];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < CD; j++)
+#pragma unroll
+                        for (int k = 0; k < NK; k += 2) {
+                            const float4 f = sh.states[t1 / TS - 1][(j * NK + k) / 2][tid];
+                            h[j][k] = pair(f.x, f.y);
+                            h[j][k + 1] = pair(f.z, f.w);
+                        }
                 }
-                store_eight(gx + (t0 + r) * P.D + word, ox, nch - word, P.whole_d);
-                store_eight(gdt + (t0 + r) * P.D + word, od, nch - word, P.whole_d);
-                if (GATE) store_eight(gz + (t0 + r) * P.D + word, oz, nch - word, P.whole_d);
+                float out[CD][TS];
+#pragma unroll
+                for (int i = 0; i < TS; i++) {
+                    float2 d[CD];
+                    f32x2 B[NK], C[NK];
+                    two_of<CD>(d, &dds[t1 + i][at.ch]);
+                    row_pairs<NS>(B, &bs[t1 + i][n0]);
+                    if constexpr (GATE) row_pairs<NS>(C, &cs[t1 + i][n0]);
+#pragma unroll
+                    for (int j = 0; j < CD; j++) {
+                        f32x2 acc = 0ull;
+#pragma unroll
+                        for (int k = 0; k < NK; k++) {
+                            a[i][j][k] = exp2_pair(mul2(twice(d[j].x), A2[j][k]));
+                            w[i][j][k] = mul2(a[i][j][k], h[j][k]);
+                            h[j][k] = fma2(twice(d[j].y), B[k], w[i][j][k]);
+                            if constexpr (GATE) acc = k == 0 ? mul2(h[j][k], C[k]) : fma2(h[j][k], C[k], acc);
+                        }
+                        if constexpr (GATE) out[j][i] = sum_of(acc);
+                    }
+                }
+                if constexpr (GATE) {
+#pragma unroll
+                    for (int j = 0; j < CD; j++) sum_four<NL>(out[j], at.nl);
+                }
+                float flow[CD][TS], drift[CD][TS];
+#pragma unroll
+                for (int i = TS - 1; i >= 0; i--) {
+                    const int t = t1 + i;
+                    float2 d[CD], e[CD];
+                    f32x2 B[NK], C[NK], gb[NK], gc[NK];
+                    two_of<CD>(d, &dds[t][at.ch]);
+                    two_of<CD>(e, &dys[t][at.ch]);
+                    row_pairs<NS>(B, &bs[t][n0]);
+                    row_pairs<NS>(C, &cs[t][n0]);
+#pragma unroll
+                    for (int j = 0; j < CD; j++) {
+                        const f32x2 dl = twice(d[j].x), dx = twice(d[j].y), dy = twice(e[j].x);
+                        f32x2 fl = 0ull, dr = 0ull;
+#pragma unroll
+                        for (int k = 0; k < NK; k++) {
+                            const f32x2 now = fma2(dx, B[k], w[i][j][k]), lam = fma2(C[k], dy, carry[j][k]), m = mul2(lam, w[i][j][k]);
+                            fl = k == 0 ? mul2(lam, B[k]) : fma2(lam, B[k], fl);
+                            dr = k == 0 ? mul2(m, A2[j][k]) : fma2(m, A2[j][k], dr);
+                            dA[j][k] = fma2(m, dl, dA[j][k]);
+                            carry[j][k] = mul2(a[i][j][k], lam);
+                            gb[k] = j == 0 ? mul2(lam, dx) : fma2(lam, dx, gb[k]);
+                            gc[k] = j == 0 ? mul2(now, dy) : fma2(now, dy, gc[k]);
+                        }
+                        flow[j][i] = sum_of(fl);
+                        drift[j][i] = sum_of(dr);
+                    }
+                    const unsigned one = lane >> 2 == u * TS + i ? (sizeof(T) == 2 ? 0x3f803f80u : 0x3f800000u) : 0u;
+#pragma unroll
+                    for (int k = 0; k < NK; k++) {
+                        const float2 p = halves(gb[k]), q = halves(gc[k]);
+                        sum_channels<T>(sums[2 * k], one, p.x, q.x);
+                        sum_channels<T>(sums[2 * k + 1], one, p.y, q.y);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < CD; j++) {
+                    sum_four<NL>(flow[j], at.nl);
+                    sum_four<NL>(drift[j], at.nl);
+                }
+#pragma unroll
+                for (int q = 0; q < kSums; q++) {
+                    const int t = t1 + at.nl % 4 + 2 * q;
+                    float2 d[CD], e[CD], sl[CD];
+                    float ox[CD], od[CD], oz[CD];
+                    two_of<CD>(d, &dds[t][at.ch]);
+                    two_of<CD>(e, &dys[t][at.ch]);
+                    two_of<CD>(sl, &sh.slopes[buf][t][at.ch]);
+                    const bool own = t0 + t < end && at.nl < 4;
+#pragma unroll
+                    for (int j = 0; j < CD; j++) {
+                        ox[j] = fmaf(d[j].x, flow[j][q], skip[j] * e[j].x);
+                        od[j] = fmaf(drift[j][q], kLn2, e[j].y * flow[j][q]) * sl[j].x;
+                        if (GATE) oz[j] = sl[j].y * fmaf(skip[j], e[j].y, out[j][q]);
+                        if (own) {
+                            gskip[j] = fmaf(e[j].x, e[j].y, gskip[j]);
+                            gbias[j] += od[j];
+                        }
+                    }
+                    if (own) {
+                        const long long row = (t0 + t) * P.D;
+                        store_channels<T, CD>(gx + row, ox, nch - at.ch, P.whole_d);
+                        store_channels<T, CD>(gdt + row, od, nch - at.ch, P.whole_d);
+                        if (GATE) store_channels<T, CD>(gz + row, oz, nch - at.ch, P.whole_d);
+                    }
+                }
+            }
+            // rows of a selection's result: eight tokens; columns: the groups of lanes that a lane / 4 names
+            float *red = sh.red[turn][tid / 32] + lane * 2;
+#pragma unroll
+            for (int k = 0; k < NS; k++) {
+                *reinterpret_cast<float2 *>(red + k * 128) = make_float2(sums[k][0], sums[k][1]);
+                *reinterpret_cast<float2 *>(red + k * 128 + 64) = make_float2(sums[k][2], sums[k][3]);
+            }
+            __syncthreads();
+            // warps, and groups of channels in a warp, in their order; neighbours take neighbouring lane groups
+#pragma unroll
+            for (int o = tid; o < 16 * NP; o += kThreads) {
+                const int nl = o % NL, i = o / NL % 8, m = o / (NL * 8) % 2, k = o / (NL * 16), n = nl * NS + k;
+                float sum = 0.f;
+#pragma unroll
+                for (int r = 0; r < Shared::kWarps; r++)
+#pragma unroll
+                    for (int q = 0; q < 8; q += NL) sum += sh.red[turn][r][((k * 2 + m) * 8 + i) * 8 + q + nl];
+                if (n < P.N && t0 + half * 8 + i < end) bc_out[((t0 + half * 8 + i) * 2 + m) * P.N + n] = sum;
             }
         }
     }
@@ -334,13 +344,15 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
         const int c = c0 + at.ch + j;
         if (seg == 0 && P.gstate_in != nullptr) store_states<NS>(P.gstate_in + ((long long)b * P.D + c) * P.N, carry[j], n0, P.N, in);
         store_states<NS>(param + (long long)c * P.N, dA[j], n0, P.N, in);
-    }
-    __syncthreads();
-    for (int i = tid; i < 2 * nch; i += kThreads) {
-        const int m = i / nch, ch = i % nch;
-        float sum = 0.f;
-        for (int r = ch / 8; r < kStagers; r += 4) sum += sh.param[m][r][ch % 8];
-        param[(long long)P.D * (P.N + m) + c0 + ch] = sum;
+#pragma unroll
+        for (int o = 4; o < 4 * NL; o *= 2) {
+            gskip[j] += __shfl_xor_sync(0xffffffffu, gskip[j], o);
+            gbias[j] += __shfl_xor_sync(0xffffffffu, gbias[j], o);
+        }
+        if (in && at.nl == 0) {
+            param[(long long)P.D * P.N + c] = gskip[j];
+            param[(long long)P.D * (P.N + 1) + c] = gbias[j];
+        }
     }
 }
 
@@ -464,7 +476,7 @@ __global__ void __launch_bounds__(256) selective_bc_kernel(const SelectiveParams
 
 template <class T, bool GATE, int NL, int NS, int CD> int run(const SelectiveParams &P, dim3 grid, cudaStream_t st)
 {
-    constexpr size_t bytes = sizeof(BwdShared<T, NL, NS, CD>);
+    constexpr size_t bytes = sizeof(BwdShared<NL, NS, CD>);
     auto k = selective_bwd_kernel<T, NL, NS, CD, GATE>;
     if (bytes > 48 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);

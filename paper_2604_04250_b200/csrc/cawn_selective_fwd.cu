@@ -4,15 +4,15 @@
 namespace cawn {
 namespace {
 
-template <class T, int NL, int NS, int CD, bool SUMMARY>
+template <class T, int NL, int NS, int CD, bool SUMMARY, bool WHOLE>
 __global__ void __launch_bounds__(32 * NL / CD) selective_fwd_kernel(const SelectiveParams P)
 {
     follow_previous();
     using At = Place<NL, NS, CD>;
-    constexpr int kThreads = At::kThreads, NP = At::kPad, NK = At::kPairs, kWords = At::kWords, kStagers = At::kStagers, kRow = 40;
-    __shared__ __align__(16) float2 dd[kTile][kScanChannels];
-    __shared__ __align__(16) float bc[2][kTile][NP];
-    __shared__ __align__(16) float ys[SUMMARY ? 1 : kTile][kRow];
+    constexpr int kThreads = At::kThreads, NP = At::kPad, NK = At::kPairs, kWords = At::kWords, kStagers = At::kStagers;
+    __shared__ __align__(16) float2 dd[2][kTile][kScanChannels];                  // d, d x
+    __shared__ __align__(16) float2 gates[SUMMARY ? 1 : 2][kTile][kScanChannels]; // skip x, silu(z)
+    __shared__ __align__(16) float bc[2][2][kTile][NP];
     __shared__ __align__(16) float bias[kScanChannels], skip[kScanChannels];
 
     const At at;
@@ -63,70 +63,77 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_fwd_kernel(const Selec
     const T *x = static_cast<const T *>(P.x) + s.begin * P.xs + c0, *dt = static_cast<const T *>(P.dt) + s.begin * P.dts + c0;
     const T *z = P.z != nullptr && !SUMMARY && P.y != nullptr ? static_cast<const T *>(P.z) + s.begin * P.zs + c0 : nullptr;
     T *y = !SUMMARY && P.y != nullptr ? static_cast<T *>(P.y) + s.begin * P.D + c0 : nullptr;
-    const int word = tid % 4 * 8;                       // this thread's eight channels of a row, at staging and output
+    const int word = tid % 4 * 8;                       // this thread's eight channels of a row, at staging
     const int quad_row = tid / (NP / 4), quad = tid % (NP / 4) * 4;     // and its four states of a row of B and C
     const T *bm = static_cast<const T *>(P.bm) + (s.begin + quad_row) * P.bs + g * P.N + quad, *cm = static_cast<const T *>(P.cm) + (s.begin + quad_row) * P.cs + g * P.N + quad;
-    Eight<T> nx[kWords], ndt[kWords], nz[kWords], cx[kWords], cz[kWords];
+    Eight<T> nx[kWords], ndt[kWords], nz[kWords];
     Quad<T> nb, nc;
     auto fetch = [&](long long t0) {
 #pragma unroll
         for (int i = 0; i < kWords; i++) {
             const long long r = t0 + tid / 4 + i * (kStagers / 4);
             const int n = tid < kStagers && r < end ? nch - word : 0;
-            nx[i] = fetch_eight(x + r * P.xs + word, n, P.whole_x);
-            ndt[i] = fetch_eight(dt + r * P.dts + word, n, P.whole_dt);
-            if (z != nullptr) nz[i] = fetch_eight(z + r * P.zs + word, n, P.whole_z);
+            nx[i] = eight_of<WHOLE>(x + r * P.xs + word, n, P.whole_x);
+            ndt[i] = eight_of<WHOLE>(dt + r * P.dts + word, n, P.whole_dt);
+            if (!SUMMARY) nz[i] = eight_of<WHOLE>(z + r * P.zs + word, z != nullptr ? n : 0, P.whole_z);
         }
         const int left = t0 + quad_row < end ? P.N - quad : 0;
-        nb = fetch_quad(bm + t0 * P.bs, left, P.whole_b);
-        if (!SUMMARY) nc = fetch_quad(cm + t0 * P.cs, left, P.whole_c);
+        nb = quad_of<WHOLE>(bm + t0 * P.bs, left, P.whole_b);
+        if (!SUMMARY) nc = quad_of<WHOLE>(cm + t0 * P.cs, left, P.whole_c);
     };
-    fetch(begin);
-    float time[CD] = {};
-    float *mark = P.checkpoints + ((checkpoint_of(s, b) + begin / kTile) * P.D + c0 + at.ch) * P.N;
-    for (long long t0 = begin; t0 < end; t0 += kTile, mark += (long long)P.D * P.N) {
-        __syncthreads();
-        if (tid < kStagers) {
+    auto stage = [&](long long t0, int to) {
+        if (kStagers == kThreads || tid < kStagers) {
 #pragma unroll
             for (int i = 0; i < kWords; i++) {
                 const int r = tid / 4 + i * (kStagers / 4);
-                float xf[8], df[8];
-                cx[i] = nx[i];
-                cz[i] = nz[i];
+                float xf[8], df[8], zf[8];
                 nx[i].widen_to(xf);
                 ndt[i].widen_to(df);
-                const bool there = t0 + r < end;        // past the end nothing moves
+                if (!SUMMARY) nz[i].widen_to(zf);
+                const f32x2 there = twice(t0 + r < end ? 1.f : 0.f);        // past the end nothing moves
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
-                    const f32x2 raw = add2(pair(df[j], df[j + 1]), *reinterpret_cast<const f32x2 *>(&bias[word + j]));
-                    const float2 d = halves(P.softplus ? softplus_of(raw) : raw);
-                    *reinterpret_cast<float4 *>(&dd[r][word + j]) = there ? make_float4(d.x, d.x * xf[j], d.y, d.y * xf[j + 1]) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    const f32x2 xx = pair(xf[j], xf[j + 1]), raw = add2(pair(df[j], df[j + 1]), *reinterpret_cast<const f32x2 *>(&bias[word + j]));
+                    const f32x2 d = mul2(chosen(P.softplus, softplus_of(raw), raw), there);
+                    const float2 e = halves(d), f = halves(mul2(d, xx));
+                    *reinterpret_cast<float4 *>(&dd[to][r][word + j]) = make_float4(e.x, f.x, e.y, f.y);
+                    if constexpr (!SUMMARY) {
+                        const f32x2 zz = pair(zf[j], zf[j + 1]);
+                        const float2 v = halves(mul2(*reinterpret_cast<const f32x2 *>(&skip[word + j]), xx));
+                        const float2 w = halves(chosen(z != nullptr, mul2(zz, sigmoid_of(zz)), twice(1.f)));
+                        *reinterpret_cast<float4 *>(&gates[to][r][word + j]) = make_float4(v.x, w.x, v.y, w.y);
+                    }
                 }
             }
         }
-        *reinterpret_cast<float4 *>(&bc[0][quad_row][quad]) = nb.get();
-        if (!SUMMARY) *reinterpret_cast<float4 *>(&bc[1][quad_row][quad]) = nc.get();
-        __syncthreads();
-        if (t0 + kTile < end) fetch(t0 + kTile);
+        *reinterpret_cast<float4 *>(&bc[to][0][quad_row][quad]) = nb.get();
+        if (!SUMMARY) *reinterpret_cast<float4 *>(&bc[to][1][quad_row][quad]) = nc.get();
+    };
+    fetch(begin);
+    __syncthreads();            // bias, skip
+    stage(begin, 0);
+    fetch(begin + kTile);
+    float time[CD] = {};
+    float *mark = P.checkpoints + ((checkpoint_of(s, b) + begin / kTile) * P.D + c0 + at.ch) * P.N;
+    int buf = 0;
+    for (long long t0 = begin; t0 < end; t0 += kTile, mark += (long long)P.D * P.N, buf ^= 1) {
+        __syncthreads();        // this tile is staged, and the one before has been read
         if (!SUMMARY && P.checkpoints != nullptr) {
 #pragma unroll
             for (int j = 0; j < CD; j++) store_states<NS>(mark + j * P.N, h[j], n0, P.N, at.ch + j < nch);
         }
-        // two tokens' decays are found while the two before them move the states
+        // straight on from here: the next tile is staged, the one after it sets out, this one is computed; two tokens' decays
+        // are found while the two before them move the states
+        stage(t0 + kTile, buf ^ 1);
+        fetch(t0 + 2 * kTile);
         f32x2 a[2][2][CD][NK], in[2][2][CD][NK];
         auto decays = [&](int u) {
 #pragma unroll
             for (int i = 0; i < 2; i++) {
                 f32x2 B[NK];
-                row_pairs<NS>(B, &bc[0][2 * u + i][n0]);
                 float2 d[CD];
-                if constexpr (CD == 2) {
-                    const float4 v = *reinterpret_cast<const float4 *>(&dd[2 * u + i][at.ch]);
-                    d[0] = make_float2(v.x, v.y);
-                    d[CD - 1] = make_float2(v.z, v.w);
-                } else {
-                    d[0] = dd[2 * u + i][at.ch];
-                }
+                row_pairs<NS>(B, &bc[buf][0][2 * u + i][n0]);
+                two_of<CD>(d, &dd[buf][2 * u + i][at.ch]);
 #pragma unroll
                 for (int j = 0; j < CD; j++) {
 #pragma unroll
@@ -146,7 +153,7 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_fwd_kernel(const Selec
 #pragma unroll
             for (int i = 0; i < 2; i++) {
                 f32x2 C[NK];
-                if constexpr (!SUMMARY) row_pairs<NS>(C, &bc[1][2 * u + i][n0]);
+                if constexpr (!SUMMARY) row_pairs<NS>(C, &bc[buf][1][2 * u + i][n0]);
 #pragma unroll
                 for (int j = 0; j < CD; j++) {
                     f32x2 acc = 0ull;
@@ -161,35 +168,18 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_fwd_kernel(const Selec
             if constexpr (!SUMMARY) {
                 if (u % 2 == 1) {
 #pragma unroll
-                    for (int j = 0; j < CD; j++) sum_four<NL>(v[j], at.nl, &ys[2 * u - 2][at.ch + j], kRow);
-                }
-            }
-        }
-        if constexpr (!SUMMARY) {
-            __syncthreads();
-            if (y != nullptr && tid < kStagers) {
+                    for (int j = 0; j < CD; j++) sum_four<NL>(v[j], at.nl);
 #pragma unroll
-                for (int i = 0; i < kWords; i++) {
-                    const int r = tid / 4 + i * (kStagers / 4);
-                    if (t0 + r >= end) break;
-                    float xf[8], f[8];
-                    cx[i].widen_to(xf);
+                    for (int q = 0; q < Four<NL>::kSums; q++) {
+                        const int t = 2 * u - 2 + at.nl % 4 + 2 * q;
+                        float2 gate[CD];
+                        float o[CD];
+                        two_of<CD>(gate, &gates[buf][t][at.ch]);
 #pragma unroll
-                    for (int j = 0; j < 8; j += 4) *reinterpret_cast<float4 *>(f + j) = *reinterpret_cast<const float4 *>(&ys[r][word + j]);
-#pragma unroll
-                    for (int j = 0; j < 8; j += 2) {
-                        f32x2 o = fma2(*reinterpret_cast<const f32x2 *>(&skip[word + j]), pair(xf[j], xf[j + 1]), pair(f[j], f[j + 1]));
-                        if (z != nullptr) {
-                            float zf[8];
-                            cz[i].widen_to(zf);
-                            const f32x2 gate = pair(zf[j], zf[j + 1]);
-                            o = mul2(o, mul2(gate, sigmoid_of(gate)));
-                        }
-                        const float2 w = halves(o);
-                        f[j] = w.x;
-                        f[j + 1] = w.y;
+                        for (int j = 0; j < CD; j++) o[j] = (v[j][q] + gate[j].x) * gate[j].y;
+                        if (y != nullptr && t0 + t < end && at.nl < 4)
+                            store_channels<T, CD>(y + (t0 + t) * P.D + at.ch, o, nch - at.ch, WHOLE || P.whole_d);
                     }
-                    store_eight(y + (t0 + r) * P.D + word, f, nch - word, P.whole_d);
                 }
             }
         }
@@ -208,9 +198,9 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_fwd_kernel(const Selec
     }
 }
 
-template <class T, bool SUMMARY> SelectiveKernel pick(const Shape &s)
+template <class T, bool SUMMARY, bool WHOLE> SelectiveKernel pick(const Shape &s)
 {
-#define CAWN_CALL(NL, NS, CD) selective_fwd_kernel<T, NL, NS, CD, SUMMARY>
+#define CAWN_CALL(NL, NS, CD) selective_fwd_kernel<T, NL, NS, CD, SUMMARY, WHOLE>
     return CAWN_BY_SHAPE(s, CAWN_CALL);
 #undef CAWN_CALL
 }
@@ -219,7 +209,8 @@ template <class T, bool SUMMARY> SelectiveKernel pick(const Shape &s)
 
 int launch_selective_fwd(const SelectiveParams &P, const Shape &s, bool half, bool summary, cudaStream_t st)
 {
-    const SelectiveKernel k = half ? (summary ? pick<bf16, true>(s) : pick<bf16, false>(s)) : (summary ? pick<float, true>(s) : pick<float, false>(s));
+    const SelectiveKernel k = half ? (summary ? (P.whole ? pick<bf16, true, true>(s) : pick<bf16, true, false>(s)) : (P.whole ? pick<bf16, false, true>(s) : pick<bf16, false, false>(s)))
+                                   : (summary ? (P.whole ? pick<float, true, true>(s) : pick<float, true, false>(s)) : (P.whole ? pick<float, false, true>(s) : pick<float, false, false>(s)));
     return status_of(launch<true>(k, dim3((unsigned)(P.G * P.blocks * P.seq.B), (unsigned)(summary ? P.S - 1 : P.S)), dim3(32 * s.warps()), 0, st, P));
 }
 
