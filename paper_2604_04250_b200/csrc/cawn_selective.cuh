@@ -66,11 +66,14 @@ __device__ __forceinline__ f32x2 softplus_of(f32x2 v)
 __device__ __forceinline__ float softplus_of(float v) { return halves(softplus_of(twice(v))).x; }
 __device__ __forceinline__ f32x2 chosen(bool c, f32x2 a, f32x2 b) { return c ? a : b; }
 
-// Where a thread is, and what its states are.
+// Where a thread of the computing warps is, and what its states are.  The last one or two warps stage the tiles: a thread of
+// theirs has kWords words of eight channels and kQuads quads of B (and of C).
+constexpr int stage_warps(int states) { return states >= 16 ? 2 : 1; }
 template <int NL, int NS, int CD> struct Place {
-    static constexpr int kThreads = 32 * NL / CD, kPad = NL * NS, kPairs = NS / 2, kShift = NL == 2 ? 1 : NL == 4 ? 2 : 3;
-    static constexpr int kStagers = kThreads < kTile * 4 ? kThreads : kTile * 4, kWords = kTile * 4 / kStagers;
-    static_assert(kTile * kPad / 4 == kThreads, "a quad of B and one of C for each thread");
+    static constexpr int kStageWarps = stage_warps(NL * NS), kStagers = 32 * kStageWarps;
+    static constexpr int kCompute = 32 * NL / CD, kThreads = kCompute + kStagers, kPad = NL * NS, kPairs = NS / 2, kShift = NL == 2 ? 1 : NL == 4 ? 2 : 3;
+    static constexpr int kWords = kTile * 4 / kStagers, kQuads = kTile * kPad / 4 / kStagers;
+    static_assert(kQuads * kStagers == kTile * kPad / 4, "whole quads");
     int nl, ch;                 // lane among a channel's, first channel of the block
     __device__ __forceinline__ Place()
     {
@@ -79,6 +82,19 @@ template <int NL, int NS, int CD> struct Place {
         ch = (threadIdx.x / 32 * (32 / NL) + (lane & 3) + 4 * (lane >> (2 + kShift))) * CD;
     }
 };
+// Two floats of each channel of a row, in shared memory: eight channels and a gap of 16 bytes, so that the stagers' words (four a
+// row, two rows at a time) and the lanes' reads of four rows go to different banks.
+constexpr int kRowPairs = 40;
+__device__ __forceinline__ int slot_of(int ch) { return ch + ch / 8 * 2; }
+// One float of each channel of a row.
+constexpr int kRowFloats = kScanChannels + 8;
+template <int CD> __device__ __forceinline__ void put_channels(float *p, const float (&f)[CD])
+{
+    if constexpr (CD == 2) *reinterpret_cast<float2 *>(p) = make_float2(f[0], f[1]);
+    else *p = f[0];
+}
+// All threads of a block, from whatever place of the code each warp is at.
+__device__ __forceinline__ void meet() { asm volatile("barrier.sync 0;" ::: "memory"); }
 
 // This lane's NS of a channel's N floats at p; those past N are zero.
 template <int NS> __device__ __forceinline__ void load_states(f32x2 (&h)[NS / 2], const float *p, int n0, int N, bool in)
@@ -199,6 +215,7 @@ __device__ __forceinline__ long long checkpoint_of(const Span &s, int b) { retur
 using SelectiveKernel = void (*)(SelectiveParams);
 struct Shape {
     int nl, ns, cd;
+    int threads() const { return 32 * (nl / cd + stage_warps(nl * ns)); }
     int warps() const { return nl / cd; }
 };
 inline Shape shape_of(int N) { return N <= 8 ? Shape{2, 4, 2} : N <= 16 ? Shape{4, 4, 2} : N <= 32 ? Shape{8, 4, 2} : Shape{8, 8, 1}; }
@@ -222,6 +239,16 @@ template <bool WHOLE, class T> __device__ __forceinline__ Quad<T> quad_of(const 
 
 // A launch for the shape: CALL(NL, NS, CD).
 #define CAWN_BY_SHAPE(S, CALL) ((S).ns == 8 ? CALL(8, 8, 1) : (S).nl == 8 ? CALL(8, 4, 2) : (S).nl == 4 ? CALL(4, 4, 2) : CALL(2, 4, 2))
+
+// More than 48 KB of shared memory are asked for.
+inline int launch_shared(SelectiveKernel k, dim3 grid, int threads, size_t bytes, const SelectiveParams &P, cudaStream_t st)
+{
+    if (bytes > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e != cudaSuccess) return status_of(e);
+    }
+    return status_of(launch<true>(k, grid, dim3(threads), bytes, st, P));
+}
 
 // One call of each kernel family; the grid is (blocks of channels x sequences, segments).
 int launch_selective_fwd(const SelectiveParams &P, const Shape &s, bool half, bool summary, cudaStream_t st);

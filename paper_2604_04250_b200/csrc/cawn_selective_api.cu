@@ -30,7 +30,10 @@ int64_t rows_of(const cawn_scan_params *p) { return p->rows > 0 ? p->rows : (int
 
 // Segments of the time axis.  Whole sequences when their blocks fill the GPU (`fill` warps a multiprocessor); otherwise
 // as many segments as do, none shorter than 256 tokens.
-constexpr int kFill = 12, kShortest = 256;
+#ifndef KFILL
+#define KFILL 12
+#endif
+constexpr int kFill = KFILL, kShortest = 256;
 int64_t wanted(const cawn_scan_params *p) { return most((int64_t)sm_count() * kFill / (blocks_of(p) * shape_of(p->N).warps()), 1); }    // sequences x segments
 int64_t segments_of(const cawn_scan_params *p)
 {

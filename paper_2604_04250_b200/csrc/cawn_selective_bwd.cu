@@ -15,6 +15,9 @@
 // products (m16n8k8).
 #include "cawn_selective.cuh"
 
+#ifndef BWDB
+#define BWDB 1
+#endif
 namespace cawn {
 namespace {
 
@@ -40,42 +43,136 @@ template <> __device__ __forceinline__ void sum_channels<float>(float (&d)[4], u
 
 template <int NL, int NS, int CD> struct BwdShared {
     using At = Place<NL, NS, CD>;
-    static constexpr int kWarps = At::kThreads / 32;
-    float2 dd[2][kTile][kScanChannels];     // d, d x
-    float2 dy[2][kTile][kScanChannels];     // dy', x
-    float2 slopes[2][kTile][kScanChannels]; // slope of d by dt; dy silu'(z)
+    static constexpr int kWarps = At::kCompute / 32, kStateRow = At::kPad + 4;
+    float2 dd[2][kTile][kRowPairs];         // d, d x
+    float2 dy[2][kTile][kRowPairs];         // dy', x
+    float2 slopes[2][kTile][kRowPairs];     // slope of d by dt; dy silu'(z)
     float bc[2][2][kTile][At::kPad];
+    float first[2][kScanChannels][kStateRow];       // the states in front of the tile
     float red[2][kWarps][NS * 2 * 64];      // [state of a lane][dB, dC][token of eight][group of lanes]
-    float4 states[kTile / 4 - 1][CD * NS / 4][At::kThreads];        // a thread's own, in front of tokens 4, 8 and 12
-    float bias[kScanChannels], skip[kScanChannels];
+    float4 states[kTile / 4 - 1][CD * NS / 4][At::kCompute];        // a thread's own, in front of tokens 4, 8 and 12
 };
 
 template <class T, int NL, int NS, int CD, bool GATE>
-__global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const SelectiveParams P)
+__global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, BWDB) selective_bwd_kernel(const SelectiveParams P)
 {
     follow_previous();
     using At = Place<NL, NS, CD>;
     using Shared = BwdShared<NL, NS, CD>;
-    constexpr int kThreads = At::kThreads, NP = At::kPad, NK = At::kPairs, kWords = At::kWords, kStagers = At::kStagers;
+    constexpr int NP = At::kPad, NK = At::kPairs, kWords = At::kWords, kQuads = At::kQuads;
     constexpr int TS = 4, kSums = Four<NL>::kSums;      // tokens whose decays stay in registers
     extern __shared__ __align__(16) unsigned char raw_shared[];
     Shared &sh = *reinterpret_cast<Shared *>(raw_shared);
 
-    const At at;
-    const int tid = threadIdx.x, lane = tid % 32, cb = blockIdx.x % (P.G * P.blocks), b = blockIdx.x / (P.G * P.blocks), g = cb / P.blocks;
+    const int cb = blockIdx.x % (P.G * P.blocks), b = blockIdx.x / (P.G * P.blocks), g = cb / P.blocks;
     const int c0 = g * P.Dg + cb % P.blocks * kScanChannels;
     const int nch = min(kScanChannels, (g + 1) * P.Dg - c0), seg = blockIdx.y;
     const Span s = span_of(P.seq, b);
     const long long begin = seg * P.per, end = s.len < begin + P.per ? s.len : begin + P.per;
-    const int n0 = at.nl * NS;
-    float *param = P.part_param + ((long long)b * P.S + seg) * P.param_cols;
+    const bool walks = begin < end;
+    const long long last = begin + (end - 1 - begin) / kTile * kTile;
 
+    if (threadIdx.x >= At::kCompute) {
+        if (!walks) return;
+        const int lane = threadIdx.x - At::kCompute, word = lane % 4 * 8;
+        const T *x = static_cast<const T *>(P.x) + s.begin * P.xs + c0 + word, *dt = static_cast<const T *>(P.dt) + s.begin * P.dts + c0 + word;
+        const T *z = GATE ? static_cast<const T *>(P.z) + s.begin * P.zs + c0 + word : nullptr, *gy = static_cast<const T *>(P.gy) + s.begin * P.D + c0 + word;
+        const T *bm = static_cast<const T *>(P.bm) + s.begin * P.bs + g * P.N, *cm = static_cast<const T *>(P.cm) + s.begin * P.cs + g * P.N;
+        const float *marks = P.checkpoints + (checkpoint_of(s, b) * P.D + c0) * P.N;
+        f32x2 bias[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int c = word + 2 * j;
+            bias[j] = pair(P.dt_bias != nullptr && c < nch ? P.dt_bias[c0 + c] : 0.f, P.dt_bias != nullptr && c + 1 < nch ? P.dt_bias[c0 + c + 1] : 0.f);
+        }
+        constexpr int kStates = kScanChannels * NP / 4 / At::kStagers;       // quads of a tile's first states a lane
+        struct Raw { Eight<T> x[kWords], dt[kWords], z[kWords], gy[kWords]; Quad<T> b[kQuads], c[kQuads]; Quad<float> h[kStates]; };
+        auto fetch = [&](Raw &to, long long t0) {
+#pragma unroll
+            for (int i = 0; i < kWords; i++) {
+                const long long r = t0 + lane / 4 + i * (At::kStagers / 4);
+                const int n = r < end ? nch - word : 0;
+                to.x[i] = fetch_eight(x + r * P.xs, n, P.whole_x);
+                to.dt[i] = fetch_eight(dt + r * P.dts, n, P.whole_dt);
+                if (GATE) to.z[i] = fetch_eight(z + r * P.zs, n, P.whole_z);
+                to.gy[i] = fetch_eight(gy + r * P.D, n, P.whole_d);
+            }
+#pragma unroll
+            for (int i = 0; i < kQuads; i++) {
+                const int q = lane + i * At::kStagers, n = q % (NP / 4) * 4;
+                const long long r = t0 + q / (NP / 4);
+                const int left = r < end ? P.N - n : 0;
+                to.b[i] = fetch_quad(bm + r * P.bs + n, left, P.whole_b);
+                to.c[i] = fetch_quad(cm + r * P.cs + n, left, P.whole_c);
+            }
+#pragma unroll
+            for (int i = 0; i < kStates; i++) {
+                const int q = lane + i * At::kStagers, ch = q / (NP / 4), n = q % (NP / 4) * 4;
+                to.h[i] = fetch_quad(marks + (t0 / kTile * P.D + ch) * P.N + n, ch < nch ? P.N - n : 0, P.N % 4 == 0);
+            }
+        };
+        Raw next;
+        fetch(next, last);
+        int to = 0;
+        for (long long t0 = last; t0 >= begin; t0 -= kTile, to ^= 1) {
+            const Raw now = next;
+            if (t0 > begin) fetch(next, t0 - kTile);        // on its way while this tile is staged and the one behind it is computed
+#pragma unroll
+            for (int i = 0; i < kWords; i++) {
+                const int r = lane / 4 + i * (At::kStagers / 4);
+                float xf[8], df[8], gf[8], zf[8];
+                now.x[i].widen_to(xf);
+                now.dt[i].widen_to(df);
+                now.gy[i].widen_to(gf);
+                if (GATE) now.z[i].widen_to(zf);
+                const bool there = t0 + r < end;
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    const f32x2 xx = pair(xf[j], xf[j + 1]), raw = add2(pair(df[j], df[j + 1]), bias[j / 2]);
+                    f32x2 slope, dy = pair(gf[j], gf[j + 1]), past = 0ull;
+                    f32x2 d = softplus_of<true>(raw, slope);
+                    d = chosen(there, chosen(P.softplus, d, raw), 0ull);
+                    slope = chosen(P.softplus, slope, twice(1.f));
+                    if constexpr (GATE) {
+                        const f32x2 zz = pair(zf[j], zf[j + 1]), sg = sigmoid_of(zz), one = twice(1.f);
+                        past = mul2(dy, mul2(sg, fma2(zz, fma2(sg, twice(-1.f), one), one)));
+                        dy = mul2(dy, mul2(zz, sg));
+                    }
+                    const int at = slot_of(word) + j;
+                    float2 u = halves(d), v = halves(mul2(d, xx));
+                    *reinterpret_cast<float4 *>(&sh.dd[to][r][at]) = make_float4(u.x, v.x, u.y, v.y);
+                    u = halves(dy);
+                    *reinterpret_cast<float4 *>(&sh.dy[to][r][at]) = make_float4(u.x, xf[j], u.y, xf[j + 1]);
+                    u = halves(slope);
+                    v = halves(past);
+                    *reinterpret_cast<float4 *>(&sh.slopes[to][r][at]) = make_float4(u.x, v.x, u.y, v.y);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kQuads; i++) {
+                *reinterpret_cast<float4 *>(&sh.bc[to][0][0][0] + (lane + i * At::kStagers) * 4) = now.b[i].get();
+                *reinterpret_cast<float4 *>(&sh.bc[to][1][0][0] + (lane + i * At::kStagers) * 4) = now.c[i].get();
+            }
+#pragma unroll
+            for (int i = 0; i < kStates; i++) {
+                const int q = lane + i * At::kStagers;
+                *reinterpret_cast<float4 *>(&sh.first[to][q / (NP / 4)][q % (NP / 4) * 4]) = now.h[i].get();
+            }
+            meet();             // the tile is there; the one behind it has been read
+        }
+        return;
+    }
+
+    const At at;
+    const int tid = threadIdx.x, lane = tid % 32, n0 = at.nl * NS;
+    float *param = P.part_param + ((long long)b * P.S + seg) * P.param_cols;
     f32x2 A2[CD][NK], carry[CD][NK], dA[CD][NK];
-    float gskip[CD] = {}, gbias[CD] = {};               // of the tokens whose sums this lane ends up with
+    float skip[CD], gskip[CD] = {}, gbias[CD] = {};     // gradients: of the tokens whose sums this lane ends up with
 #pragma unroll
     for (int j = 0; j < CD; j++) {
         const bool in = at.ch + j < nch;
         const int c = c0 + at.ch + j;
+        skip[j] = in && P.skip != nullptr ? P.skip[c] : 0.f;
         load_states<NS>(A2[j], P.A + (long long)c * P.N, n0, P.N, in);
         load_states<NS>(carry[j], P.gstate_out + ((long long)b * P.D + c) * P.N, n0, P.N, in && P.gstate_out != nullptr);
 #pragma unroll
@@ -85,110 +182,24 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
         }
         for (long long i = (s.len - 1) / P.per; i > seg; i--) fold_segment<NS>(carry[j], P, A2[j], ((long long)b * (P.S - 1) + i - 1) * P.D + c, n0, in);
     }
-    for (int i = tid; i < kScanChannels; i += kThreads) {
-        sh.bias[i] = i < nch && P.dt_bias != nullptr ? P.dt_bias[c0 + i] : 0.f;
-        sh.skip[i] = i < nch && P.skip != nullptr ? P.skip[c0 + i] : 0.f;
-    }
-
-    const T *x = static_cast<const T *>(P.x) + s.begin * P.xs + c0, *dt = static_cast<const T *>(P.dt) + s.begin * P.dts + c0;
-    const T *z = GATE ? static_cast<const T *>(P.z) + s.begin * P.zs + c0 : nullptr, *gy = static_cast<const T *>(P.gy) + s.begin * P.D + c0;
-    const int word = tid % 4 * 8, quad_row = tid / (NP / 4), quad = tid % (NP / 4) * 4;
-    const T *bm = static_cast<const T *>(P.bm) + (s.begin + quad_row) * P.bs + g * P.N + quad, *cm = static_cast<const T *>(P.cm) + (s.begin + quad_row) * P.cs + g * P.N + quad;
-    const float *marks = P.checkpoints + (checkpoint_of(s, b) * P.D + c0 + at.ch) * P.N;
-    T *gx = static_cast<T *>(P.gx) + s.begin * P.D + c0 + at.ch, *gdt = static_cast<T *>(P.gdt) + s.begin * P.D + c0 + at.ch;
-    T *gz = GATE ? static_cast<T *>(P.gz) + s.begin * P.D + c0 + at.ch : nullptr;
+    const long long row0 = (s.begin + begin) * P.D + c0 + at.ch;        // this lane's channels in the segment's first row
+    T *gx = static_cast<T *>(P.gx) + row0, *gdt = static_cast<T *>(P.gdt) + row0, *gz = GATE ? static_cast<T *>(P.gz) + row0 : nullptr;
     float *bc_out = P.part_bc + ((long long)cb * P.seq.rows + s.begin) * 2 * P.N;
-    Eight<T> nx[kWords], ndt[kWords], nz[kWords], ngy[kWords];
-    Quad<T> nb, nc;
-    f32x2 nh[CD][NK];
-    auto fetch = [&](long long t0) {
-#pragma unroll
-        for (int i = 0; i < kWords; i++) {
-            const long long r = t0 + tid / 4 + i * (kStagers / 4);
-            const int n = tid < kStagers && r < end ? nch - word : 0;
-            nx[i] = fetch_eight(x + r * P.xs + word, n, P.whole_x);
-            ndt[i] = fetch_eight(dt + r * P.dts + word, n, P.whole_dt);
-            if (GATE) nz[i] = fetch_eight(z + r * P.zs + word, n, P.whole_z);
-            ngy[i] = fetch_eight(gy + r * P.D + word, n, P.whole_d);
-        }
-        const int left = t0 + quad_row < end ? P.N - quad : 0;
-        nb = fetch_quad(bm + t0 * P.bs, left, P.whole_b);
-        nc = fetch_quad(cm + t0 * P.cs, left, P.whole_c);
-    };
-    auto fetch_states = [&](long long t0) {
-#pragma unroll
-        for (int j = 0; j < CD; j++) load_states<NS>(nh[j], marks + (t0 / kTile * P.D + j) * P.N, n0, P.N, at.ch + j < nch);
-    };
-    auto stage = [&](long long t0, int to) {
-        if (kStagers == kThreads || tid < kStagers) {
-#pragma unroll
-            for (int i = 0; i < kWords; i++) {
-                const int r = tid / 4 + i * (kStagers / 4);
-                float xf[8], df[8], gf[8], zf[8];
-                nx[i].widen_to(xf);
-                ndt[i].widen_to(df);
-                ngy[i].widen_to(gf);
-                if (GATE) nz[i].widen_to(zf);
-                const f32x2 there = twice(t0 + r < end ? 1.f : 0.f);
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    const f32x2 xx = pair(xf[j], xf[j + 1]), raw = add2(pair(df[j], df[j + 1]), *reinterpret_cast<const f32x2 *>(&sh.bias[word + j]));
-                    f32x2 slope, dy = pair(gf[j], gf[j + 1]), past = 0ull;
-                    f32x2 d = softplus_of<true>(raw, slope);
-                    d = mul2(chosen(P.softplus, d, raw), there);
-                    slope = chosen(P.softplus, slope, twice(1.f));
-                    if constexpr (GATE) {
-                        const f32x2 zz = pair(zf[j], zf[j + 1]), sg = sigmoid_of(zz), one = twice(1.f);
-                        past = mul2(dy, mul2(sg, fma2(zz, fma2(sg, twice(-1.f), one), one)));
-                        dy = mul2(dy, mul2(zz, sg));
-                    }
-                    float2 u = halves(d), v = halves(mul2(d, xx));
-                    *reinterpret_cast<float4 *>(&sh.dd[to][r][word + j]) = make_float4(u.x, v.x, u.y, v.y);
-                    u = halves(dy);
-                    *reinterpret_cast<float4 *>(&sh.dy[to][r][word + j]) = make_float4(u.x, xf[j], u.y, xf[j + 1]);
-                    u = halves(slope);
-                    v = halves(past);
-                    *reinterpret_cast<float4 *>(&sh.slopes[to][r][word + j]) = make_float4(u.x, v.x, u.y, v.y);
-                }
-            }
-        }
-        *reinterpret_cast<float4 *>(&sh.bc[to][0][quad_row][quad]) = nb.get();
-        *reinterpret_cast<float4 *>(&sh.bc[to][1][quad_row][quad]) = nc.get();
-    };
-    const long long last = begin + (end - 1 - begin) / kTile * kTile;
-    __syncthreads();            // bias, skip
-    float skip[CD];
-#pragma unroll
-    for (int j = 0; j < CD; j++) skip[j] = sh.skip[at.ch + j];
-    if (end > begin) {
-        fetch(last);
-        fetch_states(last);
-        stage(last, 0);
-        if (last > begin) fetch(last - kTile);
-    }
+    const int slot = slot_of(at.ch);
     int buf = 0, turn = 0;
-    for (long long t0 = last; t0 >= begin && end > begin; t0 -= kTile, buf ^= 1) {
-        __syncthreads();        // this tile is staged, and the one behind it has been read
-        f32x2 h[CD][NK], h0[CD][NK];
+    for (long long t0 = last; t0 >= begin && walks; t0 -= kTile, buf ^= 1) {
+        meet();
+        f32x2 h[CD][NK];
 #pragma unroll
-        for (int j = 0; j < CD; j++)
-#pragma unroll
-            for (int k = 0; k < NK; k++) h[j][k] = h0[j][k] = nh[j][k];
-        if (t0 > begin) {
-            fetch_states(t0 - kTile);
-            stage(t0 - kTile, buf ^ 1);
-            if (t0 - kTile > begin) fetch(t0 - 2 * kTile);
-        }
-        const float2 (*dds)[kScanChannels] = sh.dd[buf], (*dys)[kScanChannels] = sh.dy[buf];
-        const float (*bs)[NP] = sh.bc[buf][0], (*cs)[NP] = sh.bc[buf][1];
+        for (int j = 0; j < CD; j++) row_pairs<NS>(h[j], &sh.first[buf][at.ch + j][n0]);
 #pragma unroll
         for (int u = 0; u < kTile / TS - 1; u++) {
 #pragma unroll
             for (int i = 0; i < TS; i++) {
                 float2 d[CD];
                 f32x2 B[NK];
-                two_of<CD>(d, &dds[u * TS + i][at.ch]);
-                row_pairs<NS>(B, &bs[u * TS + i][n0]);
+                two_of<CD>(d, &sh.dd[buf][u * TS + i][slot]);
+                row_pairs<NS>(B, &sh.bc[buf][0][u * TS + i][n0]);
 #pragma unroll
                 for (int j = 0; j < CD; j++)
 #pragma unroll
@@ -212,9 +223,7 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
                 f32x2 a[TS][CD][NK], w[TS][CD][NK];
                 if (t1 == 0) {
 #pragma unroll
-                    for (int j = 0; j < CD; j++)
-#pragma unroll
-                        for (int k = 0; k < NK; k++) h[j][k] = h0[j][k];
+                    for (int j = 0; j < CD; j++) row_pairs<NS>(h[j], &sh.first[buf][at.ch + j][n0]);
                 } else {
 #pragma unroll
                     for (int j = 0; j < CD; j++)
@@ -230,9 +239,9 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
                 for (int i = 0; i < TS; i++) {
                     float2 d[CD];
                     f32x2 B[NK], C[NK];
-                    two_of<CD>(d, &dds[t1 + i][at.ch]);
-                    row_pairs<NS>(B, &bs[t1 + i][n0]);
-                    if constexpr (GATE) row_pairs<NS>(C, &cs[t1 + i][n0]);
+                    two_of<CD>(d, &sh.dd[buf][t1 + i][slot]);
+                    row_pairs<NS>(B, &sh.bc[buf][0][t1 + i][n0]);
+                    if constexpr (GATE) row_pairs<NS>(C, &sh.bc[buf][1][t1 + i][n0]);
 #pragma unroll
                     for (int j = 0; j < CD; j++) {
                         f32x2 acc = 0ull;
@@ -256,10 +265,10 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
                     const int t = t1 + i;
                     float2 d[CD], e[CD];
                     f32x2 B[NK], C[NK], gb[NK], gc[NK];
-                    two_of<CD>(d, &dds[t][at.ch]);
-                    two_of<CD>(e, &dys[t][at.ch]);
-                    row_pairs<NS>(B, &bs[t][n0]);
-                    row_pairs<NS>(C, &cs[t][n0]);
+                    two_of<CD>(d, &sh.dd[buf][t][slot]);
+                    two_of<CD>(e, &sh.dy[buf][t][slot]);
+                    row_pairs<NS>(B, &sh.bc[buf][0][t][n0]);
+                    row_pairs<NS>(C, &sh.bc[buf][1][t][n0]);
 #pragma unroll
                     for (int j = 0; j < CD; j++) {
                         const f32x2 dl = twice(d[j].x), dx = twice(d[j].y), dy = twice(e[j].x);
@@ -295,9 +304,9 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
                     const int t = t1 + at.nl % 4 + 2 * q;
                     float2 d[CD], e[CD], sl[CD];
                     float ox[CD], od[CD], oz[CD];
-                    two_of<CD>(d, &dds[t][at.ch]);
-                    two_of<CD>(e, &dys[t][at.ch]);
-                    two_of<CD>(sl, &sh.slopes[buf][t][at.ch]);
+                    two_of<CD>(d, &sh.dd[buf][t][slot]);
+                    two_of<CD>(e, &sh.dy[buf][t][slot]);
+                    two_of<CD>(sl, &sh.slopes[buf][t][slot]);
                     const bool own = t0 + t < end && at.nl < 4;
 #pragma unroll
                     for (int j = 0; j < CD; j++) {
@@ -310,7 +319,7 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
                         }
                     }
                     if (own) {
-                        const long long row = (t0 + t) * P.D;
+                        const long long row = (t0 - begin + t) * P.D;
                         store_channels<T, CD>(gx + row, ox, nch - at.ch, P.whole_d);
                         store_channels<T, CD>(gdt + row, od, nch - at.ch, P.whole_d);
                         if (GATE) store_channels<T, CD>(gz + row, oz, nch - at.ch, P.whole_d);
@@ -324,10 +333,10 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
                 *reinterpret_cast<float2 *>(red + k * 128) = make_float2(sums[k][0], sums[k][1]);
                 *reinterpret_cast<float2 *>(red + k * 128 + 64) = make_float2(sums[k][2], sums[k][3]);
             }
-            __syncthreads();
+            asm volatile("barrier.sync 1, %0;" :: "n"(At::kCompute) : "memory");        // the computing warps
             // warps, and groups of channels in a warp, in their order; neighbours take neighbouring lane groups
 #pragma unroll
-            for (int o = tid; o < 16 * NP; o += kThreads) {
+            for (int o = tid; o < 16 * NP; o += At::kCompute) {
                 const int nl = o % NL, i = o / NL % 8, m = o / (NL * 8) % 2, k = o / (NL * 16), n = nl * NS + k;
                 float sum = 0.f;
 #pragma unroll
@@ -358,22 +367,77 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
 
 // A segment's own gradient at its start, and its sum of d: for the segments in front of it.
 template <class T, int NL, int NS, int CD>
-__global__ void __launch_bounds__(32 * NL / CD) selective_bwd_summary_kernel(const SelectiveParams P)
+__global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads) selective_bwd_summary_kernel(const SelectiveParams P)
 {
     follow_previous();
     using At = Place<NL, NS, CD>;
-    constexpr int kThreads = At::kThreads, NP = At::kPad, NK = At::kPairs, kWords = At::kWords, kStagers = At::kStagers;
-    __shared__ __align__(16) float2 dd[kTile][kScanChannels];           // d, dy'
-    __shared__ __align__(16) float cs[kTile][NP];
-    __shared__ __align__(16) float bias[kScanChannels];
-    const At at;
-    const int tid = threadIdx.x, cb = blockIdx.x % (P.G * P.blocks), b = blockIdx.x / (P.G * P.blocks), g = cb / P.blocks;
+    constexpr int NP = At::kPad, NK = At::kPairs, kWords = At::kWords, kQuads = At::kQuads;
+    __shared__ __align__(16) float2 dd[2][kTile][kRowPairs];            // d, dy'
+    __shared__ __align__(16) float cs[2][kTile][NP];
+    const int cb = blockIdx.x % (P.G * P.blocks), b = blockIdx.x / (P.G * P.blocks), g = cb / P.blocks;
     const int c0 = g * P.Dg + cb % P.blocks * kScanChannels;
     const int nch = min(kScanChannels, (g + 1) * P.Dg - c0), seg = blockIdx.y + 1;
     const Span s = span_of(P.seq, b);
     const long long begin = seg * P.per, end = s.len < begin + P.per ? s.len : begin + P.per;
     if (begin >= s.len) return;
-    const int n0 = at.nl * NS;
+    if (threadIdx.x >= At::kCompute) {
+        const int lane = threadIdx.x - At::kCompute, word = lane % 4 * 8;
+        const T *dt = static_cast<const T *>(P.dt) + s.begin * P.dts + c0 + word, *gy = static_cast<const T *>(P.gy) + s.begin * P.D + c0 + word;
+        const T *z = P.z != nullptr ? static_cast<const T *>(P.z) + s.begin * P.zs + c0 + word : nullptr;
+        const T *cm = static_cast<const T *>(P.cm) + s.begin * P.cs + g * P.N;
+        f32x2 bias[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int c = word + 2 * j;
+            bias[j] = pair(P.dt_bias != nullptr && c < nch ? P.dt_bias[c0 + c] : 0.f, P.dt_bias != nullptr && c + 1 < nch ? P.dt_bias[c0 + c + 1] : 0.f);
+        }
+        struct Raw { Eight<T> dt[kWords], z[kWords], gy[kWords]; Quad<T> c[kQuads]; };
+        auto fetch = [&](Raw &to, long long t0) {
+#pragma unroll
+            for (int i = 0; i < kWords; i++) {
+                const long long r = t0 + lane / 4 + i * (At::kStagers / 4);
+                const int n = r < end ? nch - word : 0;
+                to.dt[i] = fetch_eight(dt + r * P.dts, n, P.whole_dt);
+                to.gy[i] = fetch_eight(gy + r * P.D, n, P.whole_d);
+                to.z[i] = fetch_eight(z + r * P.zs, z != nullptr ? n : 0, P.whole_z);
+            }
+#pragma unroll
+            for (int i = 0; i < kQuads; i++) {
+                const int q = lane + i * At::kStagers, n = q % (NP / 4) * 4;
+                const long long r = t0 + q / (NP / 4);
+                to.c[i] = fetch_quad(cm + r * P.cs + n, r < end ? P.N - n : 0, P.whole_c);
+            }
+        };
+        Raw next;
+        fetch(next, begin);
+        int to = 0;
+        for (long long t0 = begin; t0 < end; t0 += kTile, to ^= 1) {
+            const Raw now = next;
+            fetch(next, t0 + kTile);
+#pragma unroll
+            for (int i = 0; i < kWords; i++) {
+                const int r = lane / 4 + i * (At::kStagers / 4);
+                float df[8], gf[8], zf[8];
+                now.dt[i].widen_to(df);
+                now.gy[i].widen_to(gf);
+                now.z[i].widen_to(zf);
+                const bool there = t0 + r < end;
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    const f32x2 raw = add2(pair(df[j], df[j + 1]), bias[j / 2]), zz = pair(zf[j], zf[j + 1]);
+                    const float2 d = halves(chosen(there, chosen(P.softplus, softplus_of(raw), raw), 0ull));
+                    const float2 e = halves(mul2(pair(gf[j], gf[j + 1]), chosen(z != nullptr, mul2(zz, sigmoid_of(zz)), twice(1.f))));
+                    *reinterpret_cast<float4 *>(&dd[to][r][slot_of(word) + j]) = make_float4(d.x, e.x, d.y, e.y);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kQuads; i++) *reinterpret_cast<float4 *>(&cs[to][0][0] + (lane + i * At::kStagers) * 4) = now.c[i].get();
+            meet();
+        }
+        return;
+    }
+    const At at;
+    const int n0 = at.nl * NS, slot = slot_of(at.ch);
     f32x2 A2[CD][NK], own[CD][NK], past[CD][NK];
 #pragma unroll
     for (int j = 0; j < CD; j++) {
@@ -385,63 +449,23 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_summary_kernel(con
             past[j][k] = twice(1.f);
         }
     }
-    for (int i = tid; i < kScanChannels; i += kThreads) bias[i] = i < nch && P.dt_bias != nullptr ? P.dt_bias[c0 + i] : 0.f;
-    const T *dt = static_cast<const T *>(P.dt) + s.begin * P.dts + c0, *gy = static_cast<const T *>(P.gy) + s.begin * P.D + c0;
-    const T *z = P.z != nullptr ? static_cast<const T *>(P.z) + s.begin * P.zs + c0 : nullptr;
-    const int word = tid % 4 * 8, quad_row = tid / (NP / 4), quad = tid % (NP / 4) * 4;
-    const T *cm = static_cast<const T *>(P.cm) + (s.begin + quad_row) * P.cs + g * P.N + quad;
-    Eight<T> ndt[kWords], ngy[kWords], nz[kWords];
-    Quad<T> nc;
-    auto fetch = [&](long long t0) {
-#pragma unroll
-        for (int i = 0; i < kWords; i++) {
-            const long long r = t0 + tid / 4 + i * (kStagers / 4);
-            const int n = tid < kStagers && r < end ? nch - word : 0;
-            ndt[i] = fetch_eight(dt + r * P.dts + word, n, P.whole_dt);
-            ngy[i] = fetch_eight(gy + r * P.D + word, n, P.whole_d);
-            if (z != nullptr) nz[i] = fetch_eight(z + r * P.zs + word, n, P.whole_z);
-        }
-        nc = fetch_quad(cm + t0 * P.cs, t0 + quad_row < end ? P.N - quad : 0, P.whole_c);
-    };
-    fetch(begin);
     float time[CD] = {};
-    for (long long t0 = begin; t0 < end; t0 += kTile) {
-        __syncthreads();
-        if (tid < kStagers) {
+    int buf = 0;
+    for (long long t0 = begin; t0 < end; t0 += kTile, buf ^= 1) {
+        meet();
 #pragma unroll
-            for (int i = 0; i < kWords; i++) {
-                const int r = tid / 4 + i * (kStagers / 4);
-                float df[8], gf[8], zf[8];
-                ndt[i].widen_to(df);
-                ngy[i].widen_to(gf);
-                if (z != nullptr) nz[i].widen_to(zf);
-                const bool there = t0 + r < end;
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    const f32x2 raw = add2(pair(df[j], df[j + 1]), *reinterpret_cast<const f32x2 *>(&bias[word + j]));
-                    const float2 d = halves(P.softplus ? softplus_of(raw) : raw);
-                    f32x2 dy = pair(gf[j], gf[j + 1]);
-                    if (z != nullptr) dy = mul2(dy, mul2(pair(zf[j], zf[j + 1]), sigmoid_of(pair(zf[j], zf[j + 1]))));
-                    const float2 e = halves(dy);
-                    *reinterpret_cast<float4 *>(&dd[r][word + j]) = there ? make_float4(d.x, e.x, d.y, e.y) : make_float4(0.f, 0.f, 0.f, 0.f);
-                }
-            }
-        }
-        *reinterpret_cast<float4 *>(&cs[quad_row][quad]) = nc.get();
-        __syncthreads();
-        if (t0 + kTile < end) fetch(t0 + kTile);
-#pragma unroll 4
         for (int t = 0; t < kTile; t++) {
             f32x2 C[NK];
-            row_pairs<NS>(C, &cs[t][n0]);
+            float2 d[CD];
+            row_pairs<NS>(C, &cs[buf][t][n0]);
+            two_of<CD>(d, &dd[buf][t][slot]);
 #pragma unroll
             for (int j = 0; j < CD; j++) {
-                const float2 d = dd[t][at.ch + j];
-                time[j] += d.x;
+                time[j] += d[j].x;
 #pragma unroll
                 for (int k = 0; k < NK; k++) {
-                    past[j][k] = mul2(past[j][k], exp2_pair(mul2(twice(d.x), A2[j][k])));
-                    own[j][k] = fma2(past[j][k], mul2(C[k], twice(d.y)), own[j][k]);
+                    past[j][k] = mul2(past[j][k], exp2_pair(mul2(twice(d[j].x), A2[j][k])));
+                    own[j][k] = fma2(past[j][k], mul2(C[k], twice(d[j].y)), own[j][k]);
                 }
             }
         }
@@ -482,7 +506,7 @@ template <class T, bool GATE, int NL, int NS, int CD> int run(const SelectivePar
         const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         if (e != cudaSuccess) return status_of(e);
     }
-    return status_of(launch<true>(k, grid, dim3(32 * NL / CD), bytes, st, P));
+    return status_of(launch<true>(k, grid, dim3(Place<NL, NS, CD>::kThreads), bytes, st, P));
 }
 template <class T, bool GATE> int run(const SelectiveParams &P, const Shape &s, dim3 grid, cudaStream_t st)
 {
@@ -502,7 +526,7 @@ template <class T> SelectiveKernel pick_summary(const Shape &s)
 int launch_selective_bwd(const SelectiveParams &P, const Shape &s, bool half, bool summary, cudaStream_t st)
 {
     const dim3 grid((unsigned)(P.G * P.blocks * P.seq.B), (unsigned)(summary ? P.S - 1 : P.S));
-    if (summary) return status_of(launch<true>(half ? pick_summary<bf16>(s) : pick_summary<float>(s), grid, dim3(32 * s.warps()), 0, st, P));
+    if (summary) return status_of(launch<true>(half ? pick_summary<bf16>(s) : pick_summary<float>(s), grid, dim3(s.threads()), 0, st, P));
     return half ? (P.z != nullptr ? run<bf16, true>(P, s, grid, st) : run<bf16, false>(P, s, grid, st))
                 : (P.z != nullptr ? run<float, true>(P, s, grid, st) : run<float, false>(P, s, grid, st));
 }

@@ -1,28 +1,143 @@
 // Selective scan, forward: walks over tiles of tokens.
+//
+// Two kinds of warps.  The computing ones hold the states and leave, for each token and channel, what each lane's states give to
+// the read-out.  The stagers bring tile k + 1 into shared memory, and finish tile k - 1: they sum over the lanes, add skip x, gate and
+// store.  (With the sums by shuffles and the stores in the computing warps these waited for them in order: 82 of 278 us of
+// 8 x 2048 x 2368 x 16.)
 #include "cawn_selective.cuh"
 
 namespace cawn {
 namespace {
 
+
+template <class T, int NL, int NS, int CD, bool SUMMARY> struct FwdShared {
+    using At = Place<NL, NS, CD>;
+    float2 dd[2][kTile][kRowPairs];                             // d, d x
+    float bc[2][2][kTile][At::kPad];
+    float out[SUMMARY ? 1 : 2][kTile][NL * kRowFloats + 4];     // read-out by lane of a channel (and 16 bytes, for the stagers' two rows at a time)
+    Eight<T> words[SUMMARY ? 1 : 3][2][At::kWords][At::kStagers];       // x and z as a stager fetched them, until their tile is finished
+};
+
 template <class T, int NL, int NS, int CD, bool SUMMARY, bool WHOLE>
-__global__ void __launch_bounds__(32 * NL / CD) selective_fwd_kernel(const SelectiveParams P)
+__global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, NL == 4 ? 4 : 1) selective_fwd_kernel(const SelectiveParams P)
 {
     follow_previous();
     using At = Place<NL, NS, CD>;
-    constexpr int kThreads = At::kThreads, NP = At::kPad, NK = At::kPairs, kWords = At::kWords, kStagers = At::kStagers;
-    __shared__ __align__(16) float2 dd[2][kTile][kScanChannels];                  // d, d x
-    __shared__ __align__(16) float2 gates[SUMMARY ? 1 : 2][kTile][kScanChannels]; // skip x, silu(z)
-    __shared__ __align__(16) float bc[2][2][kTile][NP];
-    __shared__ __align__(16) float bias[kScanChannels], skip[kScanChannels];
+    constexpr int NP = At::kPad, NK = At::kPairs, kWords = At::kWords, kQuads = At::kQuads;
+    using Shared = FwdShared<T, NL, NS, CD, SUMMARY>;
+    extern __shared__ __align__(16) unsigned char raw_shared[];
+    Shared &sh = *reinterpret_cast<Shared *>(raw_shared);
 
-    const At at;
-    const int tid = threadIdx.x, cb = blockIdx.x % (P.G * P.blocks), b = blockIdx.x / (P.G * P.blocks), g = cb / P.blocks;
+    const int cb = blockIdx.x % (P.G * P.blocks), b = blockIdx.x / (P.G * P.blocks), g = cb / P.blocks;
     const int c0 = g * P.Dg + cb % P.blocks * kScanChannels;
     const int nch = min(kScanChannels, (g + 1) * P.Dg - c0), seg = blockIdx.y;
     const Span s = span_of(P.seq, b);
     const long long begin = seg * P.per, end = s.len < begin + P.per ? s.len : begin + P.per;
-    const int n0 = at.nl * NS;
+    const bool walks = SUMMARY ? end < s.len : begin < end;             // a summary: somebody comes behind this segment
 
+    if (threadIdx.x >= At::kCompute) {
+        if (!walks) return;
+        const int lane = threadIdx.x - At::kCompute, word = lane % 4 * 8;
+        const T *x = static_cast<const T *>(P.x) + s.begin * P.xs + c0 + word, *dt = static_cast<const T *>(P.dt) + s.begin * P.dts + c0 + word;
+        const T *z = P.z != nullptr && !SUMMARY && P.y != nullptr ? static_cast<const T *>(P.z) + s.begin * P.zs + c0 + word : nullptr;
+        const T *bm = static_cast<const T *>(P.bm) + s.begin * P.bs + g * P.N, *cm = static_cast<const T *>(P.cm) + s.begin * P.cs + g * P.N;
+        f32x2 bias[4], skip[4];         // of this lane's eight channels
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int c = word + 2 * j;
+            auto two = [&](const float *p) { return pair(p != nullptr && c < nch ? p[c0 + c] : 0.f, p != nullptr && c + 1 < nch ? p[c0 + c + 1] : 0.f); };
+            bias[j] = two(P.dt_bias);
+            skip[j] = two(P.skip);
+        }
+        struct Raw { Eight<T> x[kWords], dt[kWords], z[kWords]; Quad<T> b[kQuads], c[kQuads]; };
+        auto fetch = [&](Raw &to, long long t0) {
+#pragma unroll
+            for (int i = 0; i < kWords; i++) {
+                const long long r = t0 + lane / 4 + i * (At::kStagers / 4);
+                const int n = r < end ? nch - word : 0;
+                to.x[i] = eight_of<WHOLE>(x + r * P.xs, n, P.whole_x);
+                to.dt[i] = eight_of<WHOLE>(dt + r * P.dts, n, P.whole_dt);
+                if (!SUMMARY) to.z[i] = eight_of<WHOLE>(z + r * P.zs, z != nullptr ? n : 0, P.whole_z);
+            }
+#pragma unroll
+            for (int i = 0; i < kQuads; i++) {
+                const int q = lane + i * At::kStagers, n = q % (NP / 4) * 4;
+                const long long r = t0 + q / (NP / 4);
+                const int left = r < end ? P.N - n : 0;
+                to.b[i] = quad_of<WHOLE>(bm + r * P.bs + n, left, P.whole_b);
+                if (!SUMMARY) to.c[i] = quad_of<WHOLE>(cm + r * P.cs + n, left, P.whole_c);
+            }
+        };
+        T *y = !SUMMARY && P.y != nullptr ? static_cast<T *>(P.y) + s.begin * P.D + c0 + word : nullptr;
+        auto finish = [&](long long t0, int from, int kept) {
+#pragma unroll
+            for (int i = 0; i < kWords; i++) {
+                const int r = lane / 4 + i * (At::kStagers / 4);
+                float xf[8], zf[8], f[8];
+                sh.words[kept][0][i][lane].widen_to(xf);
+                sh.words[kept][1][i][lane].widen_to(zf);
+                f32x2 sum[4] = {};
+#pragma unroll
+                for (int q = 0; q < NL; q++) {
+                    f32x2 part[4];
+                    row_pairs<8>(part, &sh.out[from][r][q * kRowFloats + word]);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) sum[j] = q == 0 ? part[j] : add2(sum[j], part[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const f32x2 zz = pair(zf[2 * j], zf[2 * j + 1]), v = fma2(skip[j], pair(xf[2 * j], xf[2 * j + 1]), sum[j]);
+                    const float2 o = halves(chosen(z != nullptr, mul2(v, mul2(zz, sigmoid_of(zz))), v));
+                    f[2 * j] = o.x;
+                    f[2 * j + 1] = o.y;
+                }
+                if (y != nullptr && t0 + r < end) store_eight(y + (t0 + r) * P.D, f, nch - word, WHOLE || P.whole_d);
+            }
+        };
+        Raw next;
+        fetch(next, begin);
+        int to = 0, kept = 0;           // buffers of the tile that is staged
+        for (long long t0 = begin; t0 < end; t0 += kTile, to ^= 1, kept = kept == 2 ? 0 : kept + 1) {
+            const Raw now = next;
+            fetch(next, t0 + kTile);        // on its way while this tile is staged and the one before is computed
+#pragma unroll
+            for (int i = 0; i < kWords; i++) {
+                const int r = lane / 4 + i * (At::kStagers / 4);
+                float xf[8], df[8];
+                now.x[i].widen_to(xf);
+                now.dt[i].widen_to(df);
+                if constexpr (!SUMMARY) {
+                    sh.words[kept][0][i][lane] = now.x[i];
+                    sh.words[kept][1][i][lane] = now.z[i];
+                }
+                const bool there = t0 + r < end;        // past the end nothing moves
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    const f32x2 xx = pair(xf[j], xf[j + 1]), raw = add2(pair(df[j], df[j + 1]), bias[j / 2]);
+                    const f32x2 d = chosen(there, chosen(P.softplus, softplus_of(raw), raw), 0ull);
+                    const float2 e = halves(d), f = halves(mul2(d, xx));
+                    *reinterpret_cast<float4 *>(&sh.dd[to][r][slot_of(word) + j]) = make_float4(e.x, f.x, e.y, f.y);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kQuads; i++) {
+                *reinterpret_cast<float4 *>(&sh.bc[to][0][0][0] + (lane + i * At::kStagers) * 4) = now.b[i].get();
+                if (!SUMMARY) *reinterpret_cast<float4 *>(&sh.bc[to][1][0][0] + (lane + i * At::kStagers) * 4) = now.c[i].get();
+            }
+            if (!SUMMARY && t0 >= begin + 2 * kTile) finish(t0 - 2 * kTile, to, kept == 2 ? 0 : kept + 1);
+            meet();             // the tile is there; the one before it is computed
+        }
+        if constexpr (!SUMMARY) {       // the last two
+            const long long tiles = (end - begin + kTile - 1) / kTile;
+            if (tiles > 1) finish(begin + (tiles - 2) * kTile, to, kept == 2 ? 0 : kept + 1);
+            meet();
+            finish(begin + (tiles - 1) * kTile, to ^ 1, kept == 0 ? 2 : kept - 1);
+        }
+        return;
+    }
+
+    const At at;
+    const int n0 = at.nl * NS;
     f32x2 A2[CD][NK], h[CD][NK];
     if constexpr (SUMMARY) {
         const bool first = seg == 0 && P.state_in != nullptr;
@@ -33,9 +148,9 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_fwd_kernel(const Selec
             load_states<NS>(h[j], P.state_in + state * P.N, n0, P.N, in && first);
             if (first) store_states<NS>(P.first + state * P.N, h[j], n0, P.N, in);      // the walk may overwrite state_in while others need it
         }
-        if (end >= s.len) return;                       // nobody comes behind this segment
+        if (!walks) return;
     } else {
-        if (seg > 0 && begin >= s.len) return;
+        if (seg > 0 && !walks) return;
     }
 #pragma unroll
     for (int j = 0; j < CD; j++) {
@@ -55,85 +170,25 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_fwd_kernel(const Selec
             }
         }
     }
-    for (int i = tid; i < kScanChannels; i += kThreads) {
-        bias[i] = i < nch && P.dt_bias != nullptr ? P.dt_bias[c0 + i] : 0.f;
-        skip[i] = i < nch && P.skip != nullptr ? P.skip[c0 + i] : 0.f;
-    }
-
-    const T *x = static_cast<const T *>(P.x) + s.begin * P.xs + c0, *dt = static_cast<const T *>(P.dt) + s.begin * P.dts + c0;
-    const T *z = P.z != nullptr && !SUMMARY && P.y != nullptr ? static_cast<const T *>(P.z) + s.begin * P.zs + c0 : nullptr;
-    T *y = !SUMMARY && P.y != nullptr ? static_cast<T *>(P.y) + s.begin * P.D + c0 : nullptr;
-    const int word = tid % 4 * 8;                       // this thread's eight channels of a row, at staging
-    const int quad_row = tid / (NP / 4), quad = tid % (NP / 4) * 4;     // and its four states of a row of B and C
-    const T *bm = static_cast<const T *>(P.bm) + (s.begin + quad_row) * P.bs + g * P.N + quad, *cm = static_cast<const T *>(P.cm) + (s.begin + quad_row) * P.cs + g * P.N + quad;
-    Eight<T> nx[kWords], ndt[kWords], nz[kWords];
-    Quad<T> nb, nc;
-    auto fetch = [&](long long t0) {
-#pragma unroll
-        for (int i = 0; i < kWords; i++) {
-            const long long r = t0 + tid / 4 + i * (kStagers / 4);
-            const int n = tid < kStagers && r < end ? nch - word : 0;
-            nx[i] = eight_of<WHOLE>(x + r * P.xs + word, n, P.whole_x);
-            ndt[i] = eight_of<WHOLE>(dt + r * P.dts + word, n, P.whole_dt);
-            if (!SUMMARY) nz[i] = eight_of<WHOLE>(z + r * P.zs + word, z != nullptr ? n : 0, P.whole_z);
-        }
-        const int left = t0 + quad_row < end ? P.N - quad : 0;
-        nb = quad_of<WHOLE>(bm + t0 * P.bs, left, P.whole_b);
-        if (!SUMMARY) nc = quad_of<WHOLE>(cm + t0 * P.cs, left, P.whole_c);
-    };
-    auto stage = [&](long long t0, int to) {
-        if (kStagers == kThreads || tid < kStagers) {
-#pragma unroll
-            for (int i = 0; i < kWords; i++) {
-                const int r = tid / 4 + i * (kStagers / 4);
-                float xf[8], df[8], zf[8];
-                nx[i].widen_to(xf);
-                ndt[i].widen_to(df);
-                if (!SUMMARY) nz[i].widen_to(zf);
-                const f32x2 there = twice(t0 + r < end ? 1.f : 0.f);        // past the end nothing moves
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    const f32x2 xx = pair(xf[j], xf[j + 1]), raw = add2(pair(df[j], df[j + 1]), *reinterpret_cast<const f32x2 *>(&bias[word + j]));
-                    const f32x2 d = mul2(chosen(P.softplus, softplus_of(raw), raw), there);
-                    const float2 e = halves(d), f = halves(mul2(d, xx));
-                    *reinterpret_cast<float4 *>(&dd[to][r][word + j]) = make_float4(e.x, f.x, e.y, f.y);
-                    if constexpr (!SUMMARY) {
-                        const f32x2 zz = pair(zf[j], zf[j + 1]);
-                        const float2 v = halves(mul2(*reinterpret_cast<const f32x2 *>(&skip[word + j]), xx));
-                        const float2 w = halves(chosen(z != nullptr, mul2(zz, sigmoid_of(zz)), twice(1.f)));
-                        *reinterpret_cast<float4 *>(&gates[to][r][word + j]) = make_float4(v.x, w.x, v.y, w.y);
-                    }
-                }
-            }
-        }
-        *reinterpret_cast<float4 *>(&bc[to][0][quad_row][quad]) = nb.get();
-        if (!SUMMARY) *reinterpret_cast<float4 *>(&bc[to][1][quad_row][quad]) = nc.get();
-    };
-    fetch(begin);
-    __syncthreads();            // bias, skip
-    stage(begin, 0);
-    fetch(begin + kTile);
     float time[CD] = {};
     float *mark = P.checkpoints + ((checkpoint_of(s, b) + begin / kTile) * P.D + c0 + at.ch) * P.N;
+    const int slot = slot_of(at.ch);
     int buf = 0;
     for (long long t0 = begin; t0 < end; t0 += kTile, mark += (long long)P.D * P.N, buf ^= 1) {
-        __syncthreads();        // this tile is staged, and the one before has been read
+        meet();
         if (!SUMMARY && P.checkpoints != nullptr) {
 #pragma unroll
             for (int j = 0; j < CD; j++) store_states<NS>(mark + j * P.N, h[j], n0, P.N, at.ch + j < nch);
         }
-        // straight on from here: the next tile is staged, the one after it sets out, this one is computed; two tokens' decays
-        // are found while the two before them move the states
-        stage(t0 + kTile, buf ^ 1);
-        fetch(t0 + 2 * kTile);
+        // two tokens' decays are found while the two before them move the states
         f32x2 a[2][2][CD][NK], in[2][2][CD][NK];
         auto decays = [&](int u) {
 #pragma unroll
             for (int i = 0; i < 2; i++) {
                 f32x2 B[NK];
                 float2 d[CD];
-                row_pairs<NS>(B, &bc[buf][0][2 * u + i][n0]);
-                two_of<CD>(d, &dd[buf][2 * u + i][at.ch]);
+                row_pairs<NS>(B, &sh.bc[buf][0][2 * u + i][n0]);
+                two_of<CD>(d, &sh.dd[buf][2 * u + i][slot]);
 #pragma unroll
                 for (int j = 0; j < CD; j++) {
 #pragma unroll
@@ -146,14 +201,14 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_fwd_kernel(const Selec
             }
         };
         decays(0);
-        float v[CD][4];
 #pragma unroll
         for (int u = 0; u < kTile / 2; u++) {
             if (u + 1 < kTile / 2) decays(u + 1);
 #pragma unroll
             for (int i = 0; i < 2; i++) {
                 f32x2 C[NK];
-                if constexpr (!SUMMARY) row_pairs<NS>(C, &bc[buf][1][2 * u + i][n0]);
+                float v[CD];
+                if constexpr (!SUMMARY) row_pairs<NS>(C, &sh.bc[buf][1][2 * u + i][n0]);
 #pragma unroll
                 for (int j = 0; j < CD; j++) {
                     f32x2 acc = 0ull;
@@ -162,28 +217,13 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_fwd_kernel(const Selec
                         h[j][k] = fma2(a[u % 2][i][j][k], h[j][k], in[u % 2][i][j][k]);
                         if constexpr (!SUMMARY) acc = k == 0 ? mul2(h[j][k], C[k]) : fma2(h[j][k], C[k], acc);
                     }
-                    if constexpr (!SUMMARY) v[j][u % 2 * 2 + i] = sum_of(acc);
+                    v[j] = sum_of(acc);
                 }
-            }
-            if constexpr (!SUMMARY) {
-                if (u % 2 == 1) {
-#pragma unroll
-                    for (int j = 0; j < CD; j++) sum_four<NL>(v[j], at.nl);
-#pragma unroll
-                    for (int q = 0; q < Four<NL>::kSums; q++) {
-                        const int t = 2 * u - 2 + at.nl % 4 + 2 * q;
-                        float2 gate[CD];
-                        float o[CD];
-                        two_of<CD>(gate, &gates[buf][t][at.ch]);
-#pragma unroll
-                        for (int j = 0; j < CD; j++) o[j] = (v[j][q] + gate[j].x) * gate[j].y;
-                        if (y != nullptr && t0 + t < end && at.nl < 4)
-                            store_channels<T, CD>(y + (t0 + t) * P.D + at.ch, o, nch - at.ch, WHOLE || P.whole_d);
-                    }
-                }
+                if constexpr (!SUMMARY) put_channels<CD>(&sh.out[buf][2 * u + i][at.nl * kRowFloats + at.ch], v);
             }
         }
     }
+    if (!SUMMARY && walks) meet();      // for the stagers, which finish the last tile
 #pragma unroll
     for (int j = 0; j < CD; j++) {
         const bool in = at.ch + j < nch;
@@ -198,9 +238,14 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_fwd_kernel(const Selec
     }
 }
 
-template <class T, bool SUMMARY, bool WHOLE> SelectiveKernel pick(const Shape &s)
+template <class T, bool SUMMARY, bool WHOLE, int NL, int NS, int CD> int run(const SelectiveParams &P, dim3 grid, cudaStream_t st)
 {
-#define CAWN_CALL(NL, NS, CD) selective_fwd_kernel<T, NL, NS, CD, SUMMARY, WHOLE>
+    return launch_shared(selective_fwd_kernel<T, NL, NS, CD, SUMMARY, WHOLE>, grid, Place<NL, NS, CD>::kThreads, sizeof(FwdShared<T, NL, NS, CD, SUMMARY>), P, st);
+}
+template <class T, bool SUMMARY> int run(const SelectiveParams &P, const Shape &s, cudaStream_t st)
+{
+    const dim3 grid((unsigned)(P.G * P.blocks * P.seq.B), (unsigned)(SUMMARY ? P.S - 1 : P.S));
+#define CAWN_CALL(NL, NS, CD) (P.whole ? run<T, SUMMARY, true, NL, NS, CD>(P, grid, st) : run<T, SUMMARY, false, NL, NS, CD>(P, grid, st))
     return CAWN_BY_SHAPE(s, CAWN_CALL);
 #undef CAWN_CALL
 }
@@ -209,9 +254,7 @@ template <class T, bool SUMMARY, bool WHOLE> SelectiveKernel pick(const Shape &s
 
 int launch_selective_fwd(const SelectiveParams &P, const Shape &s, bool half, bool summary, cudaStream_t st)
 {
-    const SelectiveKernel k = half ? (summary ? (P.whole ? pick<bf16, true, true>(s) : pick<bf16, true, false>(s)) : (P.whole ? pick<bf16, false, true>(s) : pick<bf16, false, false>(s)))
-                                   : (summary ? (P.whole ? pick<float, true, true>(s) : pick<float, true, false>(s)) : (P.whole ? pick<float, false, true>(s) : pick<float, false, false>(s)));
-    return status_of(launch<true>(k, dim3((unsigned)(P.G * P.blocks * P.seq.B), (unsigned)(summary ? P.S - 1 : P.S)), dim3(32 * s.warps()), 0, st, P));
+    return half ? (summary ? run<bf16, true>(P, s, st) : run<bf16, false>(P, s, st)) : (summary ? run<float, true>(P, s, st) : run<float, false>(P, s, st));
 }
 
 }  // namespace cawn
