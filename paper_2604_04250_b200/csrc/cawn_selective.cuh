@@ -36,8 +36,7 @@ struct SelectiveParams {
 
 // log(1 + e^v) = v^+ + log1p(u), u = e^{-|v|} in [0, 1], without loss where it is small: log1p(u) / u by the polynomial of degree
 // 8 that fits it best in relative error (3e-8, found by weighted least squares on Chebyshev points).
-// Its slope 1 / (1 + e^{-v}) is 1 / (1 + u), or u times that for v < 0.
-template <bool SLOPE> __device__ __forceinline__ f32x2 softplus_of(f32x2 v, f32x2 &slope)
+__device__ __forceinline__ f32x2 softplus_of(f32x2 v)
 {
     const float2 f = halves(v);
     const float2 e = halves(mul2(pair(fabsf(f.x), fabsf(f.y)), twice(-kLog2e)));
@@ -51,17 +50,7 @@ template <bool SLOPE> __device__ __forceinline__ f32x2 softplus_of(f32x2 v, f32x
     p = fma2(p, u, twice(3.331909776e-01f));
     p = fma2(p, u, twice(-4.999949336e-01f));
     p = fma2(p, u, twice(9.999999404e-01f));
-    if constexpr (SLOPE) {
-        const float2 d = halves(add2(u, twice(1.f))), w = halves(u);
-        const float x = reciprocal_fast(d.x), y = reciprocal_fast(d.y);
-        slope = pair(f.x > 0.f ? x : x * w.x, f.y > 0.f ? y : y * w.y);
-    }
     return fma2(p, u, pair(fmaxf(f.x, 0.f), fmaxf(f.y, 0.f)));       // a NaN comes through u
-}
-__device__ __forceinline__ f32x2 softplus_of(f32x2 v)
-{
-    f32x2 none;
-    return softplus_of<false>(v, none);
 }
 __device__ __forceinline__ float softplus_of(float v) { return halves(softplus_of(twice(v))).x; }
 __device__ __forceinline__ f32x2 chosen(bool c, f32x2 a, f32x2 b) { return c ? a : b; }
@@ -92,6 +81,16 @@ template <int CD> __device__ __forceinline__ void put_channels(float *p, const f
 {
     if constexpr (CD == 2) *reinterpret_cast<float2 *>(p) = make_float2(f[0], f[1]);
     else *p = f[0];
+}
+template <int CD> __device__ __forceinline__ void get_channels(float (&f)[CD], const float *p)
+{
+    if constexpr (CD == 2) {
+        const float2 v = *reinterpret_cast<const float2 *>(p);
+        f[0] = v.x;
+        f[CD - 1] = v.y;
+    } else {
+        f[0] = *p;
+    }
 }
 // All threads of a block, from whatever place of the code each warp is at.
 __device__ __forceinline__ void meet() { asm volatile("barrier.sync 0;" ::: "memory"); }
@@ -154,39 +153,6 @@ template <int NS> __device__ __forceinline__ void row_pairs(f32x2 (&r)[NS / 2], 
     }
 }
 
-// Four tokens' sums over the NL lanes of a channel, by halving: each exchange sends half of a lane's values away and keeps
-// the other half.  v[q] then holds the sum of token nl % 4 + 2 q of the four (two sums with NL = 2, otherwise one).
-template <int NL> struct Four { static constexpr int kSums = NL == 2 ? 2 : 1; };
-template <int NL> __device__ __forceinline__ void sum_four(float (&v)[4], int nl)
-{
-    const bool odd = nl & 1, high = nl & 2;
-    float a = odd ? v[1] : v[0], b = odd ? v[3] : v[2];
-    a += __shfl_xor_sync(0xffffffffu, odd ? v[0] : v[1], 4);
-    b += __shfl_xor_sync(0xffffffffu, odd ? v[2] : v[3], 4);
-    if constexpr (NL == 2) {
-        v[0] = a;
-        v[1] = b;
-    } else {
-        float c = high ? b : a;
-        c += __shfl_xor_sync(0xffffffffu, high ? a : b, 8);
-        if constexpr (NL == 8) c += __shfl_xor_sync(0xffffffffu, c, 16);
-        v[0] = c;
-    }
-}
-// A lane's CD neighbouring channels of a row; `n` of them are there.
-template <class T, int CD> __device__ __forceinline__ void store_channels(T *p, const float (&f)[CD], int n, bool whole)
-{
-    if constexpr (CD == 2) {
-        if (whole && n >= 2) {
-            if constexpr (sizeof(T) == 2) *reinterpret_cast<unsigned *>(p) = pack_bf16(f[0], f[1]);
-            else *reinterpret_cast<float2 *>(p) = make_float2(f[0], f[1]);
-            return;
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < CD; j++)
-        if (j < n) p[j] = narrow<T>(f[j]);
-}
 // CD neighbouring pairs of floats in shared memory.
 template <int CD> __device__ __forceinline__ void two_of(float2 (&d)[CD], const float2 *p)
 {
@@ -216,7 +182,8 @@ using SelectiveKernel = void (*)(SelectiveParams);
 struct Shape {
     int nl, ns, cd;
     int threads() const { return 32 * (nl / cd + stage_warps(nl * ns)); }
-    int warps() const { return nl / cd; }
+    // blocks that a multiprocessor holds, by the registers and the shared memory that the kernels take
+    int resident(bool bwd) const { return nl == 2 ? (bwd ? 8 : 6) : nl == 4 ? 4 : ns == 4 ? 2 : 1; }
 };
 inline Shape shape_of(int N) { return N <= 8 ? Shape{2, 4, 2} : N <= 16 ? Shape{4, 4, 2} : N <= 32 ? Shape{8, 4, 2} : Shape{8, 8, 1}; }
 // Rows all of whose words are whole are fetched without a branch.

@@ -28,24 +28,23 @@ int check(const cawn_scan_params *p)
 int64_t blocks_of(const cawn_scan_params *p) { return p->G * ceil_div(p->D / p->G, kScanChannels); }
 int64_t rows_of(const cawn_scan_params *p) { return p->rows > 0 ? p->rows : (int64_t)p->B * p->L; }
 
-// Segments of the time axis.  Whole sequences when their blocks fill the GPU (`fill` warps a multiprocessor); otherwise
-// as many segments as do, none shorter than 256 tokens.
-#ifndef KFILL
-#define KFILL 12
-#endif
-constexpr int kFill = KFILL, kShortest = 256;
-int64_t wanted(const cawn_scan_params *p) { return most((int64_t)sm_count() * kFill / (blocks_of(p) * shape_of(p->N).warps()), 1); }    // sequences x segments
-int64_t segments_of(const cawn_scan_params *p)
+// Segments of the time axis, none shorter than 256 tokens.  Where the blocks of whole sequences leave multiprocessors idle, as many
+// segments as are resident at once; otherwise none: 2048 tokens of 16 states take 107 us with one block a multiprocessor, 168 with
+// two and 240 with four, and the pass before it half as much again, so that two segments of 148 blocks do not pay and four do.
+// The backward's pass is a fifth of its walk: two segments pay as soon as they are resident.
+constexpr int kShortest = 256, kMostSegments = 64;
+int64_t slots_of(const cawn_scan_params *p, bool bwd) { return (int64_t)sm_count() * shape_of(p->N).resident(bwd); }
+int64_t segments_of(const cawn_scan_params *p, bool bwd)
 {
-    const int64_t want = wanted(p);
-    if (p->B * 2 > want) return 1;
-    const int64_t s = most(want / p->B, 1), longest = most(p->L / kShortest, 1);
-    return s < longest ? (s < 64 ? s : 64) : (longest < 64 ? longest : 64);
+    const int64_t whole = p->B * blocks_of(p), cut = slots_of(p, bwd) / whole, longest = most(p->L / kShortest, 1);
+    if (cut < 2 || (!bwd && whole > sm_count())) return 1;
+    const int64_t s = cut < longest ? cut : longest;
+    return s < kMostSegments ? s : kMostSegments;
 }
 // The most sequences x segments of any call with up to this B and L.
-int64_t most_segments(const cawn_scan_params *p)
+int64_t most_segments(const cawn_scan_params *p, bool bwd)
 {
-    const int64_t cut = most(wanted(p), p->B), whole = p->B * most(p->L / kShortest, 1);
+    const int64_t cut = most(slots_of(p, bwd) / blocks_of(p), p->B), whole = p->B * most(p->L / kShortest, 1);
     return cut < whole ? cut : whole;
 }
 
@@ -61,23 +60,30 @@ struct Carver {
     }
 };
 
-// Partial sums of grad_A, grad_skip and grad_dt_bias: rows that begin on 16 bytes.
-int64_t param_cols(const cawn_scan_params *p) { return ceil_div((int64_t)p->D * (p->N + 2), 4) * 4; }
-int64_t checkpoint_rows(const cawn_scan_params *p) { return rows_of(p) / kTile + p->B + 1; }
-
 // `sized`: for any call up to this one (the size query) instead of for this very call.
-void carve_segments(Carver &c, SelectiveParams &P, const cawn_scan_params *p, bool first, bool sized)
+void carve_segments(Carver &c, SelectiveParams &P, const cawn_scan_params *p, bool bwd, bool sized)
 {
-    const int64_t pieces = sized ? most_segments(p) : p->B * segments_of(p);
+    const int64_t pieces = sized ? most_segments(p, bwd) : p->B * segments_of(p, bwd);
     if (pieces <= (sized ? 1 : p->B)) return;
     P.seg_state = c.floats(pieces * p->D * p->N);
     P.seg_time = c.floats(pieces * p->D);
-    if (first) P.first = c.floats((int64_t)p->B * p->D * p->N);
+    if (!bwd) P.first = c.floats((int64_t)p->B * p->D * p->N);
 }
+// Partial sums of grad_A, grad_skip and grad_dt_bias: rows that begin on 16 bytes.
+int64_t param_cols(const cawn_scan_params *p) { return ceil_div((int64_t)p->D * (p->N + 2), 4) * 4; }
 void carve_bwd(Carver &c, SelectiveParams &P, const cawn_scan_params *p, bool sized)
 {
+    carve_segments(c, P, p, true, sized);
     P.part_bc = c.floats(blocks_of(p) * rows_of(p) * 2 * p->N);
-    P.part_param = c.floats((sized ? most_segments(p) : p->B * segments_of(p)) * param_cols(p));
+    P.part_param = c.floats((sized ? most_segments(p, true) : p->B * segments_of(p, true)) * param_cols(p));
+}
+int64_t checkpoint_rows(const cawn_scan_params *p) { return rows_of(p) / kTile + p->B + 1; }
+
+// The time axis in segments, for one direction.
+void cut(SelectiveParams &P, const cawn_scan_params *p, bool bwd)
+{
+    P.S = (int)segments_of(p, bwd);
+    P.per = most(ceil_div(ceil_div(p->L, P.S), kTile), 1) * kTile;
 }
 
 SelectiveParams fill(const cawn_scan_params *p, const int64_t *offsets, const void *b, const void *c)
@@ -98,9 +104,7 @@ SelectiveParams fill(const cawn_scan_params *p, const int64_t *offsets, const vo
     P.whole_c = p->N % 4 == 0 && P.cs % 4 == 0 && (reinterpret_cast<uintptr_t>(c) & quad) == 0;
     P.whole = P.whole_x && P.whole_dt && P.whole_z && P.whole_d && P.whole_b && P.whole_c;
     P.softplus = p->softplus;
-    P.S = (int)segments_of(p);
     P.param_cols = param_cols(p);
-    P.per = most(ceil_div(ceil_div(p->L, P.S), 32), 1) * 32;
     return P;
 }
 
@@ -123,15 +127,12 @@ extern "C" int cawn_selective_scan_workspace_bytes(const cawn_scan_params *param
     SelectiveParams P = {};
     Carver c = {nullptr};
     switch (op) {
-    case CAWN_SCAN_FWD: carve_segments(c, P, params, true, true); break;
-    case CAWN_SCAN_BWD:
-        carve_segments(c, P, params, true, true);
-        carve_bwd(c, P, params, true);
-        break;
+    case CAWN_SCAN_FWD: carve_segments(c, P, params, false, true); break;
+    case CAWN_SCAN_BWD: carve_bwd(c, P, params, true); break;
     case CAWN_SCAN_BWD_RECOMPUTE:
-        carve_segments(c, P, params, true, true);
         carve_bwd(c, P, params, true);
         c.floats(checkpoint_rows(params) * params->D * params->N);
+        carve_segments(c, P, params, false, true);
         break;
     case CAWN_SCAN_CHECKPOINTS: c.floats(checkpoint_rows(params) * params->D * params->N); break;
     default: return CAWN_ERR_INVALID_ARG;
@@ -153,8 +154,9 @@ extern "C" int cawn_selective_scan_fwd(const cawn_scan_params *params, const voi
     if (!all_aligned16(x, dt, A, skip, dt_bias, z, state_in, y, state_out, checkpoints, workspace) || !elements_aligned(params, B, C))
         return CAWN_ERR_MISALIGNED;
     SelectiveParams P = fill(params, offsets, B, C);
+    cut(P, params, false);
     Carver c = {static_cast<unsigned char *>(workspace)};
-    carve_segments(c, P, params, true, false);
+    carve_segments(c, P, params, false, false);
     if (c.used > 0 && workspace == nullptr) return CAWN_ERR_NULL_POINTER;
     if (c.used > workspace_bytes) return CAWN_ERR_WORKSPACE_TOO_SMALL;
     P.x = x; P.dt = dt; P.A = A; P.bm = B; P.cm = C; P.skip = skip; P.dt_bias = dt_bias; P.z = z;
@@ -203,20 +205,23 @@ extern "C" int cawn_selective_scan_bwd(const cawn_scan_params *params, const voi
         return CAWN_ERR_MISALIGNED;
     SelectiveParams P = fill(params, offsets, B, C);
     Carver c = {static_cast<unsigned char *>(workspace)};
-    carve_segments(c, P, params, true, false);
+    cut(P, params, true);
     carve_bwd(c, P, params, false);
-    float *own = checkpoints == nullptr && params->L > 0 ? c.floats(checkpoint_rows(params) * params->D * params->N) : nullptr;
-    if (c.used > workspace_bytes) return CAWN_ERR_WORKSPACE_TOO_SMALL;
     P.x = x; P.dt = dt; P.A = A; P.bm = B; P.cm = C; P.skip = skip; P.dt_bias = dt_bias; P.z = z; P.state_in = state_in;
-    P.gy = grad_y; P.gstate_out = grad_state_out; P.gx = grad_x; P.gdt = grad_dt; P.gz = grad_z; P.gstate_in = grad_state_in;
     const Shape s = shape_of(params->N);
-    const bool half = params->flags != 0;
+    const bool half = params->flags != 0, again = checkpoints == nullptr && params->L > 0;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    P.checkpoints = own != nullptr ? own : const_cast<float *>(checkpoints);
-    if (own != nullptr) {           // the forward's walk once more, for its states alone
-        if (P.S > 1) rc = launch_selective_fwd(P, s, half, true, st);
-        if (rc == CAWN_OK) rc = launch_selective_fwd(P, s, half, false, st);
+    P.checkpoints = const_cast<float *>(checkpoints);
+    SelectiveParams F = P;          // the forward's walk once more, for its states alone
+    if (again) {
+        P.checkpoints = F.checkpoints = c.floats(checkpoint_rows(params) * params->D * params->N);
+        cut(F, params, false);
+        carve_segments(c, F, params, false, false);
     }
+    if (c.used > workspace_bytes) return CAWN_ERR_WORKSPACE_TOO_SMALL;
+    P.gy = grad_y; P.gstate_out = grad_state_out; P.gx = grad_x; P.gdt = grad_dt; P.gz = grad_z; P.gstate_in = grad_state_in;
+    if (again && F.S > 1) rc = launch_selective_fwd(F, s, half, true, st);
+    if (rc == CAWN_OK && again) rc = launch_selective_fwd(F, s, half, false, st);
     if (rc == CAWN_OK && P.S > 1) rc = launch_selective_bwd(P, s, half, true, st);
     if (rc == CAWN_OK) rc = launch_selective_bwd(P, s, half, false, st);
     if (rc == CAWN_OK && params->L > 0) rc = launch_selective_bc(P, half, grad_B, grad_C, st);

@@ -4,20 +4,18 @@
 //   lam_t = C_t dy'_t + e^{d_{t+1} A} lam_{t+1},   dB_t = sum_c lam d x,  dC_t = sum_c dy' h_t,  flow = sum_n lam B,
 //   dx = d flow + skip dy',   dd = sum_n lam w A + x flow,   ddt = dd sigmoid(dt + bias),   dA = sum_t lam w d,
 //   dz = dy (sum_n C h + skip x) silu'(z).
-// A walk takes tiles of 16 tokens from the last to the first.  A tile's first state is a checkpoint; the states in front of
-// each four tokens are found from it, and then w and the decays of four tokens stay in registers while the walk turns
-// round.  So a decay's exponential is taken 1.75 times; the bound is what shared memory and the issue slots give.
-// Sums over states go by shuffles.  Sums over channels (dB, dC) go through the tensor cores: the left factor is a selection,
-// ones in row t (and 8 + t) and zeros elsewhere, so that one product adds four lanes' lam d x to row t and their dy' h to
-// row 8 + t, for eight groups of lanes at once.  Operands: with bfloat16 storage the leading 8 and the next 8 bits of a term
-// side by side (m16n8k16; the rest, 2^-16 of a term, is an eighth of a percent of the result's own rounding; with one operand of 11
-// bits, gradients of rows that a few channels cancel in were off by twice their rounding); with float storage 11 and 11 bits in two
-// products (m16n8k8).
+// A walk takes tiles of 16 tokens from the last to the first, a tile as two halves.  A tile's first state is a checkpoint; the
+// states in front of each four tokens are found from it, and then w and the decays of four tokens stay in registers while
+// the walk turns round.  So a decay's exponential is taken 1.75 times.  Those registers (some 220 a thread) are why every warp here
+// does all of the work, two a scheduler, where the forward has warps of two kinds: lanes leave sums over their own states in
+// shared memory, and when half a tile is done all threads add them up, finish and store.
+// Sums over channels (dB, dC) go through the tensor cores: the left factor is a selection, ones in row t (and 8 + t) and
+// zeros elsewhere, so that one product adds four lanes' lam d x to row t and their dy' h to row 8 + t, for eight groups of
+// lanes at once.  Operands: with bfloat16 storage the leading 8 and the next 8 bits of a term side by side (m16n8k16; the rest,
+// 2^-16 of a term, is less than a hundredth of the result's own rounding; with one operand of 11 bits, gradients of rows that a few
+// channels cancel in were off by twice their rounding); with float storage 11 and 11 bits in two products (m16n8k8).
 #include "cawn_selective.cuh"
 
-#ifndef BWDB
-#define BWDB 1
-#endif
 namespace cawn {
 namespace {
 
@@ -41,138 +39,51 @@ template <> __device__ __forceinline__ void sum_channels<float>(float (&d)[4], u
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(one), "r"(0u), "r"(x), "r"(y));
 }
 
-template <int NL, int NS, int CD> struct BwdShared {
+// Where a thread is: as in the forward's computing warps, and for staging and finishing.
+template <int NL, int NS, int CD> struct Walker : Place<NL, NS, CD> {
     using At = Place<NL, NS, CD>;
-    static constexpr int kWarps = At::kCompute / 32, kStateRow = At::kPad + 4;
+    static constexpr int kThreads = At::kCompute, kWarps = kThreads / 32;
+    static constexpr int kStagers = kThreads < 64 ? kThreads : 64, kWords = 64 / kStagers;     // words of eight channels of a tile
+    static constexpr int kFinishers = kThreads < 64 ? kThreads : 64, kTurns = 64 / kFinishers;  // quads of channels of half a tile
+    static_assert(kTile * At::kPad / 4 == kThreads, "a quad of B and one of C for each thread");
+};
+
+template <class T, int NL, int NS, int CD> struct BwdShared {
+    using At = Walker<NL, NS, CD>;
     float2 dd[2][kTile][kRowPairs];         // d, d x
-    float2 dy[2][kTile][kRowPairs];         // dy', x
-    float2 slopes[2][kTile][kRowPairs];     // slope of d by dt; dy silu'(z)
+    float dy[2][kTile][kRowFloats];         // dy'
     float bc[2][2][kTile][At::kPad];
-    float first[2][kScanChannels][kStateRow];       // the states in front of the tile
-    float red[2][kWarps][NS * 2 * 64];      // [state of a lane][dB, dC][token of eight][group of lanes]
-    float4 states[kTile / 4 - 1][CD * NS / 4][At::kCompute];        // a thread's own, in front of tokens 4, 8 and 12
+    float parts[3][8][NL * kRowFloats + 8]; // flow, drift (sum of lam w A log2 e) and read-out, by lane of a channel
+    float red[At::kWarps][NS * 2 * 64];     // [state of a lane][dB, dC][token of eight][group of lanes]
+    float4 states[kTile / 4][CD * NS / 4][At::kThreads];    // a thread's own, in front of each four tokens
+    Eight<T> words[2][4][kTile][4];         // x, dt, z, dy as they were fetched
+    float bias[kScanChannels], skip[kScanChannels];
 };
 
 template <class T, int NL, int NS, int CD, bool GATE>
-__global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, BWDB) selective_bwd_kernel(const SelectiveParams P)
+__global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const SelectiveParams P)
 {
     follow_previous();
-    using At = Place<NL, NS, CD>;
-    using Shared = BwdShared<NL, NS, CD>;
-    constexpr int NP = At::kPad, NK = At::kPairs, kWords = At::kWords, kQuads = At::kQuads;
-    constexpr int TS = 4, kSums = Four<NL>::kSums;      // tokens whose decays stay in registers
+    using At = Walker<NL, NS, CD>;
+    using Shared = BwdShared<T, NL, NS, CD>;
+    constexpr int NP = At::kPad, NK = At::kPairs, kThreads = At::kThreads;
+    constexpr int TS = 4;       // tokens whose decays stay in registers
     extern __shared__ __align__(16) unsigned char raw_shared[];
     Shared &sh = *reinterpret_cast<Shared *>(raw_shared);
 
-    const int cb = blockIdx.x % (P.G * P.blocks), b = blockIdx.x / (P.G * P.blocks), g = cb / P.blocks;
+    const At at;
+    const int tid = threadIdx.x, lane = tid % 32, cb = blockIdx.x % (P.G * P.blocks), b = blockIdx.x / (P.G * P.blocks), g = cb / P.blocks;
     const int c0 = g * P.Dg + cb % P.blocks * kScanChannels;
     const int nch = min(kScanChannels, (g + 1) * P.Dg - c0), seg = blockIdx.y;
     const Span s = span_of(P.seq, b);
     const long long begin = seg * P.per, end = s.len < begin + P.per ? s.len : begin + P.per;
-    const bool walks = begin < end;
-    const long long last = begin + (end - 1 - begin) / kTile * kTile;
+    const int n0 = at.nl * NS;
 
-    if (threadIdx.x >= At::kCompute) {
-        if (!walks) return;
-        const int lane = threadIdx.x - At::kCompute, word = lane % 4 * 8;
-        const T *x = static_cast<const T *>(P.x) + s.begin * P.xs + c0 + word, *dt = static_cast<const T *>(P.dt) + s.begin * P.dts + c0 + word;
-        const T *z = GATE ? static_cast<const T *>(P.z) + s.begin * P.zs + c0 + word : nullptr, *gy = static_cast<const T *>(P.gy) + s.begin * P.D + c0 + word;
-        const T *bm = static_cast<const T *>(P.bm) + s.begin * P.bs + g * P.N, *cm = static_cast<const T *>(P.cm) + s.begin * P.cs + g * P.N;
-        const float *marks = P.checkpoints + (checkpoint_of(s, b) * P.D + c0) * P.N;
-        f32x2 bias[4];
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int c = word + 2 * j;
-            bias[j] = pair(P.dt_bias != nullptr && c < nch ? P.dt_bias[c0 + c] : 0.f, P.dt_bias != nullptr && c + 1 < nch ? P.dt_bias[c0 + c + 1] : 0.f);
-        }
-        constexpr int kStates = kScanChannels * NP / 4 / At::kStagers;       // quads of a tile's first states a lane
-        struct Raw { Eight<T> x[kWords], dt[kWords], z[kWords], gy[kWords]; Quad<T> b[kQuads], c[kQuads]; Quad<float> h[kStates]; };
-        auto fetch = [&](Raw &to, long long t0) {
-#pragma unroll
-            for (int i = 0; i < kWords; i++) {
-                const long long r = t0 + lane / 4 + i * (At::kStagers / 4);
-                const int n = r < end ? nch - word : 0;
-                to.x[i] = fetch_eight(x + r * P.xs, n, P.whole_x);
-                to.dt[i] = fetch_eight(dt + r * P.dts, n, P.whole_dt);
-                if (GATE) to.z[i] = fetch_eight(z + r * P.zs, n, P.whole_z);
-                to.gy[i] = fetch_eight(gy + r * P.D, n, P.whole_d);
-            }
-#pragma unroll
-            for (int i = 0; i < kQuads; i++) {
-                const int q = lane + i * At::kStagers, n = q % (NP / 4) * 4;
-                const long long r = t0 + q / (NP / 4);
-                const int left = r < end ? P.N - n : 0;
-                to.b[i] = fetch_quad(bm + r * P.bs + n, left, P.whole_b);
-                to.c[i] = fetch_quad(cm + r * P.cs + n, left, P.whole_c);
-            }
-#pragma unroll
-            for (int i = 0; i < kStates; i++) {
-                const int q = lane + i * At::kStagers, ch = q / (NP / 4), n = q % (NP / 4) * 4;
-                to.h[i] = fetch_quad(marks + (t0 / kTile * P.D + ch) * P.N + n, ch < nch ? P.N - n : 0, P.N % 4 == 0);
-            }
-        };
-        Raw next;
-        fetch(next, last);
-        int to = 0;
-        for (long long t0 = last; t0 >= begin; t0 -= kTile, to ^= 1) {
-            const Raw now = next;
-            if (t0 > begin) fetch(next, t0 - kTile);        // on its way while this tile is staged and the one behind it is computed
-#pragma unroll
-            for (int i = 0; i < kWords; i++) {
-                const int r = lane / 4 + i * (At::kStagers / 4);
-                float xf[8], df[8], gf[8], zf[8];
-                now.x[i].widen_to(xf);
-                now.dt[i].widen_to(df);
-                now.gy[i].widen_to(gf);
-                if (GATE) now.z[i].widen_to(zf);
-                const bool there = t0 + r < end;
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    const f32x2 xx = pair(xf[j], xf[j + 1]), raw = add2(pair(df[j], df[j + 1]), bias[j / 2]);
-                    f32x2 slope, dy = pair(gf[j], gf[j + 1]), past = 0ull;
-                    f32x2 d = softplus_of<true>(raw, slope);
-                    d = chosen(there, chosen(P.softplus, d, raw), 0ull);
-                    slope = chosen(P.softplus, slope, twice(1.f));
-                    if constexpr (GATE) {
-                        const f32x2 zz = pair(zf[j], zf[j + 1]), sg = sigmoid_of(zz), one = twice(1.f);
-                        past = mul2(dy, mul2(sg, fma2(zz, fma2(sg, twice(-1.f), one), one)));
-                        dy = mul2(dy, mul2(zz, sg));
-                    }
-                    const int at = slot_of(word) + j;
-                    float2 u = halves(d), v = halves(mul2(d, xx));
-                    *reinterpret_cast<float4 *>(&sh.dd[to][r][at]) = make_float4(u.x, v.x, u.y, v.y);
-                    u = halves(dy);
-                    *reinterpret_cast<float4 *>(&sh.dy[to][r][at]) = make_float4(u.x, xf[j], u.y, xf[j + 1]);
-                    u = halves(slope);
-                    v = halves(past);
-                    *reinterpret_cast<float4 *>(&sh.slopes[to][r][at]) = make_float4(u.x, v.x, u.y, v.y);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kQuads; i++) {
-                *reinterpret_cast<float4 *>(&sh.bc[to][0][0][0] + (lane + i * At::kStagers) * 4) = now.b[i].get();
-                *reinterpret_cast<float4 *>(&sh.bc[to][1][0][0] + (lane + i * At::kStagers) * 4) = now.c[i].get();
-            }
-#pragma unroll
-            for (int i = 0; i < kStates; i++) {
-                const int q = lane + i * At::kStagers;
-                *reinterpret_cast<float4 *>(&sh.first[to][q / (NP / 4)][q % (NP / 4) * 4]) = now.h[i].get();
-            }
-            meet();             // the tile is there; the one behind it has been read
-        }
-        return;
-    }
-
-    const At at;
-    const int tid = threadIdx.x, lane = tid % 32, n0 = at.nl * NS;
-    float *param = P.part_param + ((long long)b * P.S + seg) * P.param_cols;
     f32x2 A2[CD][NK], carry[CD][NK], dA[CD][NK];
-    float skip[CD], gskip[CD] = {}, gbias[CD] = {};     // gradients: of the tokens whose sums this lane ends up with
 #pragma unroll
     for (int j = 0; j < CD; j++) {
         const bool in = at.ch + j < nch;
         const int c = c0 + at.ch + j;
-        skip[j] = in && P.skip != nullptr ? P.skip[c] : 0.f;
         load_states<NS>(A2[j], P.A + (long long)c * P.N, n0, P.N, in);
         load_states<NS>(carry[j], P.gstate_out + ((long long)b * P.D + c) * P.N, n0, P.N, in && P.gstate_out != nullptr);
 #pragma unroll
@@ -182,18 +93,169 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, BWDB) selective_b
         }
         for (long long i = (s.len - 1) / P.per; i > seg; i--) fold_segment<NS>(carry[j], P, A2[j], ((long long)b * (P.S - 1) + i - 1) * P.D + c, n0, in);
     }
-    const long long row0 = (s.begin + begin) * P.D + c0 + at.ch;        // this lane's channels in the segment's first row
-    T *gx = static_cast<T *>(P.gx) + row0, *gdt = static_cast<T *>(P.gdt) + row0, *gz = GATE ? static_cast<T *>(P.gz) + row0 : nullptr;
+    for (int i = tid; i < kScanChannels; i += kThreads) {
+        sh.bias[i] = i < nch && P.dt_bias != nullptr ? P.dt_bias[c0 + i] : 0.f;
+        sh.skip[i] = i < nch && P.skip != nullptr ? P.skip[c0 + i] : 0.f;
+    }
+
+    const T *x = static_cast<const T *>(P.x) + s.begin * P.xs + c0, *dt = static_cast<const T *>(P.dt) + s.begin * P.dts + c0;
+    const T *z = GATE ? static_cast<const T *>(P.z) + s.begin * P.zs + c0 : nullptr, *gy = static_cast<const T *>(P.gy) + s.begin * P.D + c0;
+    const int word = tid % 4 * 8, quad_row = tid / (NP / 4), quad = tid % (NP / 4) * 4;
+    const T *bm = static_cast<const T *>(P.bm) + (s.begin + quad_row) * P.bs + g * P.N + quad, *cm = static_cast<const T *>(P.cm) + (s.begin + quad_row) * P.cs + g * P.N + quad;
+    const float *marks = P.checkpoints + (checkpoint_of(s, b) * P.D + c0 + at.ch) * P.N;
+    Eight<T> nx[At::kWords], ndt[At::kWords], nz[At::kWords], ngy[At::kWords];
+    Quad<T> nb, nc;
+    f32x2 nh[CD][NK];
+    auto fetch = [&](long long t0) {
+#pragma unroll
+        for (int i = 0; i < At::kWords; i++) {
+            const long long r = t0 + tid / 4 + i * (At::kStagers / 4);
+            const int n = tid < At::kStagers && r < end ? nch - word : 0;
+            nx[i] = fetch_eight(x + r * P.xs + word, n, P.whole_x);
+            ndt[i] = fetch_eight(dt + r * P.dts + word, n, P.whole_dt);
+            if (GATE) nz[i] = fetch_eight(z + r * P.zs + word, n, P.whole_z);
+            ngy[i] = fetch_eight(gy + r * P.D + word, n, P.whole_d);
+        }
+        const int left = t0 + quad_row < end ? P.N - quad : 0;
+        nb = fetch_quad(bm + t0 * P.bs, left, P.whole_b);
+        nc = fetch_quad(cm + t0 * P.cs, left, P.whole_c);
+    };
+    auto fetch_states = [&](long long t0) {
+#pragma unroll
+        for (int j = 0; j < CD; j++) load_states<NS>(nh[j], marks + (t0 / kTile * P.D + j) * P.N, n0, P.N, at.ch + j < nch);
+    };
+    auto stage = [&](long long t0, int to) {
+        if (At::kStagers == kThreads || tid < At::kStagers) {
+#pragma unroll
+            for (int i = 0; i < At::kWords; i++) {
+                const int r = tid / 4 + i * (At::kStagers / 4);
+                float xf[8], df[8], gf[8], zf[8];
+                nx[i].widen_to(xf);
+                ndt[i].widen_to(df);
+                ngy[i].widen_to(gf);
+                sh.words[to][0][r][tid % 4] = nx[i];
+                sh.words[to][1][r][tid % 4] = ndt[i];
+                sh.words[to][3][r][tid % 4] = ngy[i];
+                if constexpr (GATE) {
+                    nz[i].widen_to(zf);
+                    sh.words[to][2][r][tid % 4] = nz[i];
+                }
+                const bool there = t0 + r < end;
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    const f32x2 xx = pair(xf[j], xf[j + 1]), raw = add2(pair(df[j], df[j + 1]), *reinterpret_cast<const f32x2 *>(&sh.bias[word + j]));
+                    const f32x2 d = chosen(there, chosen(P.softplus, softplus_of(raw), raw), 0ull);
+                    const float2 u = halves(d), v = halves(mul2(d, xx));
+                    *reinterpret_cast<float4 *>(&sh.dd[to][r][slot_of(word) + j]) = make_float4(u.x, v.x, u.y, v.y);
+                    f32x2 dy = pair(gf[j], gf[j + 1]);
+                    if constexpr (GATE) dy = mul2(dy, mul2(pair(zf[j], zf[j + 1]), sigmoid_of(pair(zf[j], zf[j + 1]))));
+                    *reinterpret_cast<f32x2 *>(&sh.dy[to][r][word + j]) = dy;
+                }
+            }
+        }
+        *reinterpret_cast<float4 *>(&sh.bc[to][0][quad_row][quad]) = nb.get();
+        *reinterpret_cast<float4 *>(&sh.bc[to][1][quad_row][quad]) = nc.get();
+    };
+    // Half a tile: a thread has four channels of one row (or two rows).
+    const int four = tid % 8 * 4;
+    f32x2 gskip[2] = {}, gbias[2] = {};
+    T *gx = static_cast<T *>(P.gx) + s.begin * P.D + c0 + four, *gdt = static_cast<T *>(P.gdt) + s.begin * P.D + c0 + four;
+    T *gz = GATE ? static_cast<T *>(P.gz) + s.begin * P.D + c0 + four : nullptr;
     float *bc_out = P.part_bc + ((long long)cb * P.seq.rows + s.begin) * 2 * P.N;
+    auto finish = [&](long long t0, int from, int half) {
+        if (At::kFinishers == kThreads || tid < At::kFinishers) {
+#pragma unroll
+            for (int i = 0; i < At::kTurns; i++) {
+                const int r8 = tid / 8 + i * (At::kFinishers / 8), r = half * 8 + r8;
+                f32x2 sum[3][2];
+#pragma unroll
+                for (int m = 0; m < (GATE ? 3 : 2); m++)
+#pragma unroll
+                    for (int q = 0; q < NL; q++) {
+                        const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(&sh.parts[m][r8][q * kRowFloats + four]);
+                        sum[m][0] = q == 0 ? v.x : add2(sum[m][0], v.x);
+                        sum[m][1] = q == 0 ? v.y : add2(sum[m][1], v.y);
+                    }
+                auto row = [&](int m) { return reinterpret_cast<const Quad<T> *>(&sh.words[from][m][r][0])[tid % 8].get(); };
+                const float4 xf = row(0), df = row(1), gf = row(3), zf = GATE ? row(2) : xf;
+                float ox[4], od[4], oz[4];
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    const f32x2 xx = j == 0 ? pair(xf.x, xf.y) : pair(xf.z, xf.w), raw = add2(j == 0 ? pair(df.x, df.y) : pair(df.z, df.w), *reinterpret_cast<const f32x2 *>(&sh.bias[four + 2 * j]));
+                    const f32x2 skip = *reinterpret_cast<const f32x2 *>(&sh.skip[four + 2 * j]), dy = *reinterpret_cast<const f32x2 *>(&sh.dy[from][r][four + 2 * j]);
+                    const float4 d = *reinterpret_cast<const float4 *>(&sh.dd[from][r][slot_of(four) + 2 * j]);
+                    float2 v = halves(fma2(pair(d.x, d.z), sum[0][j], mul2(skip, dy)));
+                    ox[2 * j] = v.x;
+                    ox[2 * j + 1] = v.y;
+                    f32x2 o = fma2(sum[1][j], twice(kLn2), mul2(xx, sum[0][j]));
+                    o = chosen(P.softplus, mul2(o, sigmoid_of(raw)), o);
+                    v = halves(o);
+                    od[2 * j] = v.x;
+                    od[2 * j + 1] = v.y;
+                    if (t0 + r < end) {
+                        gskip[j] = fma2(dy, xx, gskip[j]);
+                        gbias[j] = add2(gbias[j], o);
+                    }
+                    if constexpr (GATE) {
+                        const f32x2 zz = j == 0 ? pair(zf.x, zf.y) : pair(zf.z, zf.w), gg = j == 0 ? pair(gf.x, gf.y) : pair(gf.z, gf.w), sg = sigmoid_of(zz), one = twice(1.f);
+                        const f32x2 slope = mul2(sg, fma2(zz, fma2(sg, twice(-1.f), one), one));
+                        v = halves(mul2(mul2(gg, slope), fma2(skip, xx, sum[2][j])));
+                        oz[2 * j] = v.x;
+                        oz[2 * j + 1] = v.y;
+                    }
+                }
+                if (t0 + r < end) {
+                    store_quad(gx + (t0 + r) * P.D, make_float4(ox[0], ox[1], ox[2], ox[3]), nch - four, P.whole_d);
+                    store_quad(gdt + (t0 + r) * P.D, make_float4(od[0], od[1], od[2], od[3]), nch - four, P.whole_d);
+                    if (GATE) store_quad(gz + (t0 + r) * P.D, make_float4(oz[0], oz[1], oz[2], oz[3]), nch - four, P.whole_d);
+                }
+            }
+        }
+        // dB, dC: warps, and groups of channels in a warp, in their order; neighbours take neighbouring groups of lanes
+#pragma unroll
+        for (int o = tid; o < 16 * NP; o += kThreads) {
+            const int nl = o % NL, i = o / NL % 8, m = o / (NL * 8) % 2, k = o / (NL * 16), n = nl * NS + k;
+            const long long t = t0 + half * 8 + i;
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < At::kWarps; r++)
+#pragma unroll
+                for (int q = 0; q < 8; q += NL) sum += sh.red[r][((k * 2 + m) * 8 + i) * 8 + q + nl];
+            if (n < P.N && t < end) bc_out[(t * 2 + m) * P.N + n] = sum;
+        }
+    };
+    const long long last = begin + (end - 1 - begin) / kTile * kTile;
+    __syncthreads();            // bias, skip
+    if (end > begin) {
+        fetch(last);
+        fetch_states(last);
+        stage(last, 0);
+        if (last > begin) fetch(last - kTile);
+    }
     const int slot = slot_of(at.ch);
-    int buf = 0, turn = 0;
-    for (long long t0 = last; t0 >= begin && walks; t0 -= kTile, buf ^= 1) {
-        meet();
+    int buf = 0;
+    for (long long t0 = last; t0 >= begin && end > begin; t0 -= kTile, buf ^= 1) {
+        __syncthreads();        // this tile is staged, and the one behind it is finished
         f32x2 h[CD][NK];
 #pragma unroll
-        for (int j = 0; j < CD; j++) row_pairs<NS>(h[j], &sh.first[buf][at.ch + j][n0]);
+        for (int j = 0; j < CD; j++)
 #pragma unroll
-        for (int u = 0; u < kTile / TS - 1; u++) {
+            for (int k = 0; k < NK; k++) h[j][k] = nh[j][k];
+        if (t0 > begin) {
+            fetch_states(t0 - kTile);
+            stage(t0 - kTile, buf ^ 1);
+            if (t0 - kTile > begin) fetch(t0 - 2 * kTile);
+        }
+#pragma unroll 1
+        for (int u = 0; u < kTile / TS; u++) {
+#pragma unroll
+            for (int j = 0; j < CD; j++)
+#pragma unroll
+                for (int k = 0; k < NK; k += 2) {
+                    const float2 p = halves(h[j][k]), q = halves(h[j][k + 1]);
+                    sh.states[u][(j * NK + k) / 2][tid] = make_float4(p.x, p.y, q.x, q.y);
+                }
+            if (u == kTile / TS - 1) break;
 #pragma unroll
             for (int i = 0; i < TS; i++) {
                 float2 d[CD];
@@ -205,38 +267,26 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, BWDB) selective_b
 #pragma unroll
                     for (int k = 0; k < NK; k++) h[j][k] = fma2(exp2_pair(mul2(twice(d[j].x), A2[j][k])), h[j][k], mul2(twice(d[j].y), B[k]));
             }
-#pragma unroll
-            for (int j = 0; j < CD; j++)
-#pragma unroll
-                for (int k = 0; k < NK; k += 2) {
-                    const float2 p = halves(h[j][k]), q = halves(h[j][k + 1]);
-                    sh.states[u][(j * NK + k) / 2][tid] = make_float4(p.x, p.y, q.x, q.y);
-                }
         }
         // Eight tokens, then the eight before them, four at a time.
 #pragma unroll 1
-        for (int half = 1; half >= 0; half--, turn ^= 1) {
+        for (int half = 1; half >= 0; half--) {
             float sums[NS][4] = {};
-#pragma unroll
+#pragma unroll 1
             for (int u = 1; u >= 0; u--) {
                 const int t1 = half * 8 + u * TS;
                 f32x2 a[TS][CD][NK], w[TS][CD][NK];
-                if (t1 == 0) {
 #pragma unroll
-                    for (int j = 0; j < CD; j++) row_pairs<NS>(h[j], &sh.first[buf][at.ch + j][n0]);
-                } else {
+                for (int j = 0; j < CD; j++)
 #pragma unroll
-                    for (int j = 0; j < CD; j++)
-#pragma unroll
-                        for (int k = 0; k < NK; k += 2) {
-                            const float4 f = sh.states[t1 / TS - 1][(j * NK + k) / 2][tid];
-                            h[j][k] = pair(f.x, f.y);
-                            h[j][k + 1] = pair(f.z, f.w);
-                        }
-                }
-                float out[CD][TS];
+                    for (int k = 0; k < NK; k += 2) {
+                        const float4 f = sh.states[t1 / TS][(j * NK + k) / 2][tid];
+                        h[j][k] = pair(f.x, f.y);
+                        h[j][k + 1] = pair(f.z, f.w);
+                    }
 #pragma unroll
                 for (int i = 0; i < TS; i++) {
+                    float out[CD];
                     float2 d[CD];
                     f32x2 B[NK], C[NK];
                     two_of<CD>(d, &sh.dd[buf][t1 + i][slot]);
@@ -252,26 +302,23 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, BWDB) selective_b
                             h[j][k] = fma2(twice(d[j].y), B[k], w[i][j][k]);
                             if constexpr (GATE) acc = k == 0 ? mul2(h[j][k], C[k]) : fma2(h[j][k], C[k], acc);
                         }
-                        if constexpr (GATE) out[j][i] = sum_of(acc);
+                        if constexpr (GATE) out[j] = sum_of(acc);
                     }
+                    if constexpr (GATE) put_channels<CD>(&sh.parts[2][u * TS + i][at.nl * kRowFloats + at.ch], out);
                 }
-                if constexpr (GATE) {
-#pragma unroll
-                    for (int j = 0; j < CD; j++) sum_four<NL>(out[j], at.nl);
-                }
-                float flow[CD][TS], drift[CD][TS];
 #pragma unroll
                 for (int i = TS - 1; i >= 0; i--) {
                     const int t = t1 + i;
-                    float2 d[CD], e[CD];
+                    float2 d[CD];
+                    float e[CD], flow[CD], drift[CD];
                     f32x2 B[NK], C[NK], gb[NK], gc[NK];
                     two_of<CD>(d, &sh.dd[buf][t][slot]);
-                    two_of<CD>(e, &sh.dy[buf][t][slot]);
+                    get_channels<CD>(e, &sh.dy[buf][t][at.ch]);
                     row_pairs<NS>(B, &sh.bc[buf][0][t][n0]);
                     row_pairs<NS>(C, &sh.bc[buf][1][t][n0]);
 #pragma unroll
                     for (int j = 0; j < CD; j++) {
-                        const f32x2 dl = twice(d[j].x), dx = twice(d[j].y), dy = twice(e[j].x);
+                        const f32x2 dl = twice(d[j].x), dx = twice(d[j].y), dy = twice(e[j]);
                         f32x2 fl = 0ull, dr = 0ull;
 #pragma unroll
                         for (int k = 0; k < NK; k++) {
@@ -283,9 +330,11 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, BWDB) selective_b
                             gb[k] = j == 0 ? mul2(lam, dx) : fma2(lam, dx, gb[k]);
                             gc[k] = j == 0 ? mul2(now, dy) : fma2(now, dy, gc[k]);
                         }
-                        flow[j][i] = sum_of(fl);
-                        drift[j][i] = sum_of(dr);
+                        flow[j] = sum_of(fl);
+                        drift[j] = sum_of(dr);
                     }
+                    put_channels<CD>(&sh.parts[0][u * TS + i][at.nl * kRowFloats + at.ch], flow);
+                    put_channels<CD>(&sh.parts[1][u * TS + i][at.nl * kRowFloats + at.ch], drift);
                     const unsigned one = lane >> 2 == u * TS + i ? (sizeof(T) == 2 ? 0x3f803f80u : 0x3f800000u) : 0u;
 #pragma unroll
                     for (int k = 0; k < NK; k++) {
@@ -294,74 +343,50 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, BWDB) selective_b
                         sum_channels<T>(sums[2 * k + 1], one, p.y, q.y);
                     }
                 }
-#pragma unroll
-                for (int j = 0; j < CD; j++) {
-                    sum_four<NL>(flow[j], at.nl);
-                    sum_four<NL>(drift[j], at.nl);
-                }
-#pragma unroll
-                for (int q = 0; q < kSums; q++) {
-                    const int t = t1 + at.nl % 4 + 2 * q;
-                    float2 d[CD], e[CD], sl[CD];
-                    float ox[CD], od[CD], oz[CD];
-                    two_of<CD>(d, &sh.dd[buf][t][slot]);
-                    two_of<CD>(e, &sh.dy[buf][t][slot]);
-                    two_of<CD>(sl, &sh.slopes[buf][t][slot]);
-                    const bool own = t0 + t < end && at.nl < 4;
-#pragma unroll
-                    for (int j = 0; j < CD; j++) {
-                        ox[j] = fmaf(d[j].x, flow[j][q], skip[j] * e[j].x);
-                        od[j] = fmaf(drift[j][q], kLn2, e[j].y * flow[j][q]) * sl[j].x;
-                        if (GATE) oz[j] = sl[j].y * fmaf(skip[j], e[j].y, out[j][q]);
-                        if (own) {
-                            gskip[j] = fmaf(e[j].x, e[j].y, gskip[j]);
-                            gbias[j] += od[j];
-                        }
-                    }
-                    if (own) {
-                        const long long row = (t0 - begin + t) * P.D;
-                        store_channels<T, CD>(gx + row, ox, nch - at.ch, P.whole_d);
-                        store_channels<T, CD>(gdt + row, od, nch - at.ch, P.whole_d);
-                        if (GATE) store_channels<T, CD>(gz + row, oz, nch - at.ch, P.whole_d);
-                    }
-                }
             }
             // rows of a selection's result: eight tokens; columns: the groups of lanes that a lane / 4 names
-            float *red = sh.red[turn][tid / 32] + lane * 2;
+            float *red = sh.red[tid / 32] + lane * 2;
 #pragma unroll
             for (int k = 0; k < NS; k++) {
                 *reinterpret_cast<float2 *>(red + k * 128) = make_float2(sums[k][0], sums[k][1]);
                 *reinterpret_cast<float2 *>(red + k * 128 + 64) = make_float2(sums[k][2], sums[k][3]);
             }
-            asm volatile("barrier.sync 1, %0;" :: "n"(At::kCompute) : "memory");        // the computing warps
-            // warps, and groups of channels in a warp, in their order; neighbours take neighbouring lane groups
-#pragma unroll
-            for (int o = tid; o < 16 * NP; o += At::kCompute) {
-                const int nl = o % NL, i = o / NL % 8, m = o / (NL * 8) % 2, k = o / (NL * 16), n = nl * NS + k;
-                float sum = 0.f;
-#pragma unroll
-                for (int r = 0; r < Shared::kWarps; r++)
-#pragma unroll
-                    for (int q = 0; q < 8; q += NL) sum += sh.red[turn][r][((k * 2 + m) * 8 + i) * 8 + q + nl];
-                if (n < P.N && t0 + half * 8 + i < end) bc_out[((t0 + half * 8 + i) * 2 + m) * P.N + n] = sum;
-            }
+            __syncthreads();
+            finish(t0, buf, half);
+            if (half == 1) __syncthreads();
         }
     }
+    float *param = P.part_param + ((long long)b * P.S + seg) * P.param_cols;
 #pragma unroll
     for (int j = 0; j < CD; j++) {
         const bool in = at.ch + j < nch;
         const int c = c0 + at.ch + j;
         if (seg == 0 && P.gstate_in != nullptr) store_states<NS>(P.gstate_in + ((long long)b * P.D + c) * P.N, carry[j], n0, P.N, in);
         store_states<NS>(param + (long long)c * P.N, dA[j], n0, P.N, in);
+    }
+    // a channel's sums: over the rows of a warp (lanes of the same four), then over the warps
 #pragma unroll
-        for (int o = 4; o < 4 * NL; o *= 2) {
-            gskip[j] += __shfl_xor_sync(0xffffffffu, gskip[j], o);
-            gbias[j] += __shfl_xor_sync(0xffffffffu, gbias[j], o);
+    for (int j = 0; j < 2; j++)
+#pragma unroll
+        for (int o = 8; o < 32; o *= 2) {
+            gskip[j] = add2(gskip[j], __shfl_xor_sync(0xffffffffu, gskip[j], o));
+            gbias[j] = add2(gbias[j], __shfl_xor_sync(0xffffffffu, gbias[j], o));
         }
-        if (in && at.nl == 0) {
-            param[(long long)P.D * P.N + c] = gskip[j];
-            param[(long long)P.D * (P.N + 1) + c] = gbias[j];
+    __syncthreads();
+    float (*sums)[2][kScanChannels] = reinterpret_cast<float (*)[2][kScanChannels]>(&sh.dd[0][0][0]);
+    if (lane < 8) {
+#pragma unroll
+        for (int j = 0; j < 2; j++) {
+            *reinterpret_cast<f32x2 *>(&sums[tid / 32][0][four + 2 * j]) = gskip[j];
+            *reinterpret_cast<f32x2 *>(&sums[tid / 32][1][four + 2 * j]) = gbias[j];
         }
+    }
+    __syncthreads();
+    for (int i = tid; i < 2 * nch; i += kThreads) {
+        const int m = i / nch, ch = i % nch;
+        float sum = 0.f;
+        for (int w = 0; w < At::kWarps; w++) sum += sums[w][m][ch];
+        param[(long long)P.D * (P.N + m) + c0 + ch] = sum;
     }
 }
 
@@ -479,34 +504,46 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads) selective_bwd_sum
     }
 }
 
-// Gradients of B and C: the sums over a group's blocks of channels, in their order.
+// Gradients of B and C: the sums over a group's blocks of channels, in their order; four neighbours a thread, eight blocks' on their way.
 template <class T>
-__global__ void __launch_bounds__(256) selective_bc_kernel(const SelectiveParams P, T *gb, T *gc, long long tiles)
+__global__ void __launch_bounds__(128) selective_bc_kernel(const SelectiveParams P, T *gb, T *gc, long long tiles)
 {
     follow_previous();
     const int b = (int)(blockIdx.x / tiles), g = blockIdx.y, cols = 2 * P.N;
     const Span s = span_of(P.seq, b);
-    const long long t0 = blockIdx.x % tiles * 32, rows = s.len - t0 < 32 ? s.len - t0 : 32, step = P.seq.rows * cols;
+    const long long t0 = blockIdx.x % tiles * kTile, rows = s.len - t0 < kTile ? s.len - t0 : kTile, step = P.seq.rows * cols;
     const float *part = P.part_bc + (long long)g * P.blocks * step + (s.begin + t0) * cols;
-    for (long long i = threadIdx.x; i < rows * cols; i += blockDim.x) {
-        float sum = 0.f;
-        for (int k = 0; k < P.blocks; k++) sum += part[k * step + i];
+    auto put = [&](long long i, float sum) {
         const long long row = s.begin + t0 + i / cols;
         const int n = (int)(i % cols);
         T *out = n < P.N ? gb + row * P.G * P.N + g * P.N + n : gc + row * P.G * P.N + g * P.N + n - P.N;
         *out = narrow<T>(sum);
+    };
+    if (P.N % 2 == 0) {         // rows of whole 16-byte words
+        for (long long i = threadIdx.x * 4; i < rows * cols; i += 4 * blockDim.x) {
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+            for (int k = 0; k < P.blocks; k++) {
+                const float4 v = *reinterpret_cast<const float4 *>(part + k * step + i);
+                sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+            }
+            put(i, sum.x);
+            put(i + 1, sum.y);
+            put(i + 2, sum.z);
+            put(i + 3, sum.w);
+        }
+    } else {
+        for (long long i = threadIdx.x; i < rows * cols; i += blockDim.x) {
+            float sum = 0.f;
+            for (int k = 0; k < P.blocks; k++) sum += part[k * step + i];
+            put(i, sum);
+        }
     }
 }
 
 template <class T, bool GATE, int NL, int NS, int CD> int run(const SelectiveParams &P, dim3 grid, cudaStream_t st)
 {
-    constexpr size_t bytes = sizeof(BwdShared<NL, NS, CD>);
-    auto k = selective_bwd_kernel<T, NL, NS, CD, GATE>;
-    if (bytes > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-        if (e != cudaSuccess) return status_of(e);
-    }
-    return status_of(launch<true>(k, grid, dim3(Place<NL, NS, CD>::kThreads), bytes, st, P));
+    return launch_shared(selective_bwd_kernel<T, NL, NS, CD, GATE>, grid, Walker<NL, NS, CD>::kThreads, sizeof(BwdShared<T, NL, NS, CD>), P, st);
 }
 template <class T, bool GATE> int run(const SelectiveParams &P, const Shape &s, dim3 grid, cudaStream_t st)
 {
@@ -533,10 +570,10 @@ int launch_selective_bwd(const SelectiveParams &P, const Shape &s, bool half, bo
 
 int launch_selective_bc(const SelectiveParams &P, bool half, void *grad_b, void *grad_c, cudaStream_t st)
 {
-    const long long tiles = ceil_div(P.seq.L, 32);
+    const long long tiles = ceil_div(P.seq.L, kTile);
     const dim3 grid((unsigned)(tiles * P.seq.B), (unsigned)P.G);
-    return half ? status_of(launch<true>(selective_bc_kernel<bf16>, grid, dim3(256), 0, st, P, static_cast<bf16 *>(grad_b), static_cast<bf16 *>(grad_c), tiles))
-                : status_of(launch<true>(selective_bc_kernel<float>, grid, dim3(256), 0, st, P, static_cast<float *>(grad_b), static_cast<float *>(grad_c), tiles));
+    return half ? status_of(launch<true>(selective_bc_kernel<bf16>, grid, dim3(128), 0, st, P, static_cast<bf16 *>(grad_b), static_cast<bf16 *>(grad_c), tiles))
+                : status_of(launch<true>(selective_bc_kernel<float>, grid, dim3(128), 0, st, P, static_cast<float *>(grad_b), static_cast<float *>(grad_c), tiles));
 }
 
 }  // namespace cawn
