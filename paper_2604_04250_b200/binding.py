@@ -567,33 +567,38 @@ def make_conv_params(B, L, C, K, act=CAWN_CONV_ACT_NONE, flags=0, x_stride=0, ro
 
 
 def _sequence_rows(params, offsets, arrays):
-    """Rows of a call's arrays ((name, tensor, width, stride) each), their layout checked, and how many there are.  One row has no step to the
-    next, so torch gives that dimension any stride; one token each of several sequences is as many rows."""
-    packed = offsets is not None
-    if packed:
+    """The arrays of a call, (name, tensor, width, stride) each, have to be the rows that the params say.  One row has no step to the
+    next, so torch gives that dimension any stride."""
+    if offsets is None:
+        rows = params.B * params.L
+    else:
+        rows = params.rows
         _dense("offsets", offsets)
-        if hasattr(offsets, "dtype") and (str(offsets.dtype) not in ("torch.int64", "int64") or offsets.shape != (params.B + 1,)):
+        if hasattr(offsets, "dtype") and (str(offsets.dtype) not in ("torch.int64", "int64") or tuple(offsets.shape) != (params.B + 1,)):
             raise ValueError(f"offsets: {params.B + 1} values of int64 are needed, got {tuple(offsets.shape)} of {offsets.dtype}")
-    rows = params.rows if packed else params.B * params.L
     if rows < 1:
         return
     for name, x, width, stride in arrays:
         if x is None:
             continue
-        row = stride or width
-        shape = getattr(x, "shape", None)
-        if shape is None or not hasattr(x, "stride"):
-            continue
-        if len(shape) == 2 and shape[1] == width and shape[0] == rows:          # the usual case at once
-            steps = x.stride()
-            if steps[1] == 1 and (steps[0] == row or rows == 1):
+        try:                            # the usual case at once
+            if (stride == 0 or stride == width or rows == 1) and x.is_contiguous() and x.numel() == rows * width:
                 continue
-        if rows > 1:
-            _check_rows(name, x, width, row)
-        elif width > 1 and shape[-1] > 1 and x.stride(-1) != 1:
-            raise ValueError(f"{name}: strides {tuple(x.stride())} of shape {tuple(shape)}, a row has to be dense")
-        if x.numel() != rows * width:
-            raise ValueError(f"{name}: {tuple(shape)} is not {rows} rows of {width} elements")
+        except AttributeError:          # not a tensor (a numpy array): its owner's business
+            continue
+        _check_sequence_rows(name, x, rows, width, stride or width)
+
+
+def _check_sequence_rows(name, x, rows, width, row):
+    shape, steps = x.shape, x.stride()
+    if len(shape) == 2 and shape[1] == width and shape[0] == rows and steps[1] == 1 and (steps[0] == row or rows == 1):
+        return
+    if rows > 1:
+        _check_rows(name, x, width, row)
+    elif width > 1 and shape[-1] > 1 and steps[-1] != 1:
+        raise ValueError(f"{name}: strides {tuple(steps)} of shape {tuple(shape)}, a row has to be dense")
+    if x.numel() != rows * width:
+        raise ValueError(f"{name}: {tuple(shape)} is not {rows} rows of {width} elements")
 
 
 def cawn_short_conv_workspace_bytes(params):
@@ -642,11 +647,10 @@ def new_scan_workspace(params, op, device="cuda"):
     return _plain_workspace(cawn_selective_scan_workspace_bytes(params, op), device)
 
 
-def _scan_rows(params, offsets, x, dt, z, B, C, **dense):
+def _scan_rows(params, offsets, x, dt, z, B, C, *more):
     D, bc = params.D, params.G * params.N
     _sequence_rows(params, offsets, (("x_stride", x, D, params.x_stride), ("dt_stride", dt, D, params.dt_stride), ("z_stride", z, D, params.z_stride),
-                                     ("b_stride", B, bc, params.b_stride), ("c_stride", C, bc, params.c_stride),
-                                     *((name, y, bc if name in ("grad_B", "grad_C") else D, 0) for name, y in dense.items())))
+                                     ("b_stride", B, bc, params.b_stride), ("c_stride", C, bc, params.c_stride), *more))
 
 
 def _scan_checkpoints(params, checkpoints):
@@ -660,7 +664,7 @@ def _scan_checkpoints(params, checkpoints):
 def cawn_selective_scan_fwd(params, x, dt, A, B, C, y, workspace=None, skip=None, dt_bias=None, z=None, state_in=None, state_out=None,
                             offsets=None, checkpoints=None, stream=None):
     _dense("A y skip dt_bias state_in state_out checkpoints", A, y, skip, dt_bias, state_in, state_out, checkpoints)
-    _scan_rows(params, offsets, x, dt, z, B, C, y=y)
+    _scan_rows(params, offsets, x, dt, z, B, C, ("y", y, params.D, 0))
     _scan_checkpoints(params, checkpoints)
     n = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib().cawn_selective_scan_fwd(
@@ -670,7 +674,7 @@ def cawn_selective_scan_fwd(params, x, dt, A, B, C, y, workspace=None, skip=None
 
 def cawn_selective_scan_step(params, x, dt, A, B, C, y, skip=None, dt_bias=None, z=None, state_in=None, state_out=None, stream=None):
     _dense("A y skip dt_bias state_in state_out", A, y, skip, dt_bias, state_in, state_out)
-    _scan_rows(params, None, x, dt, z, B, C, y=y)
+    _scan_rows(params, None, x, dt, z, B, C, ("y", y, params.D, 0))
     _check(lib().cawn_selective_scan_step(
         ctypes.byref(params), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(skip), _dp(dt_bias), _dp(z), _dp(state_in), _dp(y), _dp(state_out),
         _stream(stream)), "cawn_selective_scan_step")
@@ -682,7 +686,9 @@ def cawn_selective_scan_bwd(params, x, dt, A, B, C, grad_y, grad_x, grad_dt, gra
     _dense("A grad_y grad_x grad_dt grad_A grad_B grad_C skip dt_bias state_in checkpoints grad_state_out grad_skip grad_dt_bias grad_z grad_state_in",
            A, grad_y, grad_x, grad_dt, grad_A, grad_B, grad_C, skip, dt_bias, state_in, checkpoints, grad_state_out, grad_skip, grad_dt_bias, grad_z,
            grad_state_in)
-    _scan_rows(params, offsets, x, dt, z, B, C, grad_y=grad_y, grad_x=grad_x, grad_dt=grad_dt, grad_B=grad_B, grad_C=grad_C, grad_z=grad_z)
+    D, bc = params.D, params.G * params.N
+    _scan_rows(params, offsets, x, dt, z, B, C, ("grad_y", grad_y, D, 0), ("grad_x", grad_x, D, 0), ("grad_dt", grad_dt, D, 0), ("grad_B", grad_B, bc, 0),
+               ("grad_C", grad_C, bc, 0), ("grad_z", grad_z, D, 0))
     _scan_checkpoints(params, checkpoints)
     _check(lib().cawn_selective_scan_bwd(
         ctypes.byref(params), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(skip), _dp(dt_bias), _dp(z), _dp(state_in), _dp(offsets), _dp(checkpoints),

@@ -10,8 +10,11 @@
 namespace cawn {
 namespace {
 
-constexpr int kRows = 16, kLanes = 32, kWalks = 4, kTile = kRows * kWalks;     // a block: 32 words of four channels, 4 walks
+constexpr int kLanes = 32, kWalks = 4, kStep = 8;        // a block: 32 words of four channels, 4 walks of a multiple of 8 rows
 constexpr int kConvThreads = kLanes * kWalks;
+// Blocks that a multiprocessor holds.
+constexpr int fwd_blocks(size_t element) { return element == 2 ? 5 : 4; }
+constexpr int kBwdBlocks = 4;
 
 struct ConvParams {
     Sequences seq;
@@ -19,7 +22,8 @@ struct ConvParams {
     void *y, *gx;
     const float *w, *b, *state_in, *gstate_out;
     float *state_out, *gstate_in, *part;
-    long long x_stride, tiles, all_tiles;       // tiles of a sequence of L rows, of all sequences
+    int rows;                                   // of a walk
+    long long x_stride, tiles, all_tiles;       // tiles (kWalks walks) of a sequence of L rows, of all sequences
     int C, words, silu, x_whole, c_whole;
 };
 
@@ -81,30 +85,32 @@ template <int K> __device__ __forceinline__ void taps_of(Row (&w)[K], Row &b, co
 }
 
 template <class T, int K, bool WHOLE>
-__global__ void __launch_bounds__(kConvThreads) conv_fwd_kernel(const ConvParams P)
+__global__ void __launch_bounds__(kConvThreads, fwd_blocks(sizeof(T))) conv_fwd_kernel(const ConvParams P)
 {
     follow_previous();
     const int word = (blockIdx.y * kLanes + threadIdx.x % kLanes), c0 = word * kWord;
     const int n = P.C - c0 < kWord ? P.C - c0 : kWord;
     const int b = (int)(blockIdx.x / P.tiles);
-    const long long t0 = (blockIdx.x % P.tiles) * kTile + threadIdx.x / kLanes * kRows;
+    const long long t0 = (blockIdx.x % P.tiles * kWalks + threadIdx.x / kLanes) * (long long)P.rows;
     const Span s = span_of(P.seq, b);
     const bool here = word < P.words && (t0 < s.len || t0 == 0);
     const T *x = static_cast<const T *>(P.x) + s.begin * P.x_stride + c0;
     const float *history = P.state_in != nullptr && K > 1 ? P.state_in + (long long)b * (K - 1) * P.C + c0 : nullptr;
-    const int rows = !here ? 0 : s.len - t0 < kRows ? (int)(s.len - t0) : kRows;
-    // Four rows are computed while the next four are on their way; the first eight, and the K - 1 in front, set out
-    // before the weights do.
+    const int rows = !here ? 0 : s.len - t0 < P.rows ? (int)(s.len - t0) : P.rows;
+    // Four rows are computed while the next four are on their way; the first eight, and the K - 1 in front, set out before
+    // the weights do.
     Quad<T> next[2][4];
     const T *ahead = x + t0 * P.x_stride;
-    auto fetch = [&](int q) {
+    int left = rows;            // of what is still to set out
+    auto fetch = [&](Quad<T> (&to)[4]) {
 #pragma unroll
-        for (int r = 0; r < 4; r++) next[q % 2][r] = word_of<WHOLE>(ahead + r * P.x_stride, q * 4 + r < rows, n, P.x_whole);
+        for (int r = 0; r < 4; r++) to[r] = word_of<WHOLE>(ahead + r * P.x_stride, r < left, n, P.x_whole);
         ahead += 4 * P.x_stride;
+        left -= 4;
     };
     Row old[K];                 // the K - 1 rows in front of the next one
-    fetch(0);
-    fetch(1);
+#pragma unroll
+    for (int q = 0; q < 2; q++) fetch(next[q]);
     if (here) {
 #pragma unroll
         for (int j = 0; j < K - 1; j++) extended<T, K, WHOLE>(old[j], P, x, history, t0 + j - (K - 1), n);
@@ -123,44 +129,46 @@ __global__ void __launch_bounds__(kConvThreads) conv_fwd_kernel(const ConvParams
         }
     }
     T *y = static_cast<T *>(P.y) + (s.begin + t0) * P.C + c0;
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += kStep) {
 #pragma unroll
-    for (int q = 0; q < kRows / 4; q++) {
-        if (q * 4 >= rows) break;
+        for (int q = 0; q < 2; q++) {
 #pragma unroll
-        for (int r = 0; r < 4; r++) {
-            Row now, z;
-            pairs_of(now, next[q % 2][r]);
+            for (int r = 0; r < 4; r++) {
+                Row now, z;
+                pairs_of(now, next[q][r]);
 #pragma unroll
-            for (int c = 0; c < kPairs; c++) {
-                z[c] = fma2(w[K - 1][c], now[c], bias[c]);
+                for (int c = 0; c < kPairs; c++) {
+                    z[c] = fma2(w[K - 1][c], now[c], bias[c]);
 #pragma unroll
-                for (int k = 0; k < K - 1; k++) z[c] = fma2(w[k][c], old[k][c], z[c]);
-                if (P.silu) z[c] = mul2(z[c], sigmoid_of(z[c]));
+                    for (int k = 0; k < K - 1; k++) z[c] = fma2(w[k][c], old[k][c], z[c]);
+                    if (P.silu) z[c] = mul2(z[c], sigmoid_of(z[c]));
 #pragma unroll
-                for (int k = 0; k + 2 < K; k++) old[k][c] = old[k + 1][c];
-                if (K > 1) old[K > 1 ? K - 2 : 0][c] = now[c];
+                    for (int k = 0; k + 2 < K; k++) old[k][c] = old[k + 1][c];
+                    if (K > 1) old[K > 1 ? K - 2 : 0][c] = now[c];
+                }
+                if (r0 + q * 4 + r < rows) store_row<WHOLE>(y + (q * 4 + r) * (long long)P.C, z, n, P.c_whole);
             }
-            if (q * 4 + r < rows) store_row<WHOLE>(y + (long long)(q * 4 + r) * P.C, z, n, P.c_whole);
+            fetch(next[q]);
         }
-        if (q + 2 < kRows / 4) fetch(q + 2);
+        y += (long long)kStep * P.C;
     }
 }
 
 // A block takes tile after tile, so that few partial sums of the parameters' gradients are left.
 template <class T, int K, bool WHOLE>
-__global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(const ConvParams P)
+__global__ void __launch_bounds__(kConvThreads, kBwdBlocks) conv_bwd_kernel(const ConvParams P)
 {
     follow_previous();
-    constexpr int kAhead = 4;   // rows computed while as many are on their way
+    constexpr int kAhead = 2;   // rows computed while as many are on their way
     __shared__ __align__(16) float fold[kWalks][kChannels];
     const int lane = threadIdx.x % kLanes, walk = threadIdx.x / kLanes, word = blockIdx.y * kLanes + lane, c0 = word * kWord;
     const int n = word < P.words ? (P.C - c0 < kWord ? P.C - c0 : kWord) : 0;
     Row w[K], bias, gw[K] = {}, gb = {};
     taps_of<K>(w, bias, P);
-    constexpr int kSteps = (kRows + K - 1 + kAhead - 1) / kAhead;
     for (long long tile = blockIdx.x; tile < P.all_tiles; tile += gridDim.x) {
         const int b = (int)(tile / P.tiles);
-        const long long t0 = (tile % P.tiles) * kTile + walk * kRows;
+        const long long t0 = (tile % P.tiles * kWalks + walk) * P.rows;
         const Span s = span_of(P.seq, b);
         if (n == 0 || (t0 >= s.len && t0 != 0)) continue;
         const T *x = static_cast<const T *>(P.x) + s.begin * P.x_stride + c0;
@@ -169,75 +177,83 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(const ConvParams
         const float *history = P.state_in != nullptr && K > 1 ? P.state_in + (long long)b * (K - 1) * P.C + c0 : nullptr;
         const float *gso = P.gstate_out != nullptr && K > 1 ? P.gstate_out + (long long)b * (K - 1) * P.C + c0 : nullptr;
         Row old[K], dz[K] = {};                 // rows t-K+1 .. t-1 of e; dz of rows t-K+1 .. t (0 before this walk)
+        const int own = (int)(s.len - t0 < P.rows ? s.len - t0 : P.rows);            // rows of this walk
+        const int all = own + K - 1, have = (int)(s.len - t0 < all ? s.len - t0 : all);  // those gone through, and of them in the sequence
         Quad<T> nx[2][kAhead], ngy[2][kAhead];
         const T *ax = x + t0 * P.x_stride, *ag = gy + t0 * P.C;
-        auto fetch = [&](int q) {
+        int left = have;            // of what is still to set out
+        auto fetch = [&](Quad<T> (&to)[kAhead], Quad<T> (&tog)[kAhead]) {
 #pragma unroll
             for (int r = 0; r < kAhead; r++) {
-                const long long t = t0 + q * kAhead + r;
-                nx[q % 2][r] = word_of<WHOLE>(ax + r * P.x_stride, t < s.len, n, P.x_whole);
-                ngy[q % 2][r] = word_of<WHOLE>(ag + (long long)r * P.C, t < s.len, n, P.c_whole);
+                to[r] = word_of<WHOLE>(ax + r * P.x_stride, r < left, n, P.x_whole);
+                tog[r] = word_of<WHOLE>(ag + (long long)r * P.C, r < left, n, P.c_whole);
             }
             ax += kAhead * P.x_stride;
             ag += (long long)kAhead * P.C;
+            left -= kAhead;
         };
-        fetch(0);
+        fetch(nx[0], ngy[0]);
+        fetch(nx[1], ngy[1]);
 #pragma unroll
         for (int j = 0; j < K - 1; j++) extended<T, K, WHOLE>(old[j], P, x, history, t0 + j - (K - 1), n);
-        const long long end = t0 + kRows < s.len ? t0 + kRows : s.len;      // this walk's own rows end here
-        // row t gives dz_t; what then is complete is the gradient of row t - (K - 1), whose last term dz_t is
+        T *out = gx + (t0 - (K - 1)) * P.C;         // of the row that the next one completes
+        // row r gives dz_r; what then is complete is the gradient of row r - (K - 1), whose last term dz_r is (in front of the
+        // first walk of a sequence: of the history)
+#pragma unroll 1
+        for (int r0 = 0; r0 < all; r0 += 2 * kAhead) {
 #pragma unroll
-        for (int q = 0; q < kSteps; q++) {
-            if (t0 + q * kAhead - (K - 1) >= end && t0 != 0) break;
-            if (q + 1 < kSteps) fetch(q + 1);
+            for (int q = 0; q < 2; q++) {
 #pragma unroll
-            for (int r = 0; r < kAhead; r++) {
-                const long long t = t0 + q * kAhead + r;
-                Row now, d;
-                pairs_of(now, nx[q % 2][r]);
-                pairs_of(d, ngy[q % 2][r]);            // past the end: zero
-                const bool own = t < end;
+                for (int k0 = 0; k0 < kAhead; k0++) {
+                    const int r = r0 + q * kAhead + k0;
+                    Row now, d;
+                    pairs_of(now, nx[q][k0]);
+                    pairs_of(d, ngy[q][k0]);        // past the end: zero
 #pragma unroll
-                for (int c = 0; c < kPairs; c++) {
-                    if (P.silu) {
-                        f32x2 z = fma2(w[K - 1][c], now[c], bias[c]);
+                    for (int c = 0; c < kPairs; c++) {
+                        if (P.silu) {
+                            f32x2 z = fma2(w[K - 1][c], now[c], bias[c]);
 #pragma unroll
-                        for (int k = 0; k < K - 1; k++) z = fma2(w[k][c], old[k][c], z);
-                        const f32x2 sg = sigmoid_of(z), one = twice(1.f);
-                        const f32x2 slope = mul2(sg, fma2(z, fma2(sg, twice(-1.f), one), one));
-                        d[c] = t < s.len ? mul2(d[c], slope) : 0ull;        // a select: the slope there may be anything
+                            for (int k = 0; k < K - 1; k++) z = fma2(w[k][c], old[k][c], z);
+                            const f32x2 sg = sigmoid_of(z), one = twice(1.f);
+                            const f32x2 slope = mul2(sg, fma2(z, fma2(sg, twice(-1.f), one), one));
+                            d[c] = r < have ? mul2(d[c], slope) : 0ull;     // a select: the slope there may be anything
+                        }
+#pragma unroll
+                        for (int k = 0; k + 1 < K; k++) dz[k][c] = dz[k + 1][c];
+                        dz[K - 1][c] = d[c];
                     }
+                    if (r < own) {
 #pragma unroll
-                    for (int k = 0; k + 1 < K; k++) dz[k][c] = dz[k + 1][c];
-                    dz[K - 1][c] = d[c];
-                    if (own) {
+                        for (int c = 0; c < kPairs; c++) {
 #pragma unroll
-                        for (int k = 0; k < K - 1; k++) gw[k][c] = fma2(d[c], old[k][c], gw[k][c]);
-                        gw[K - 1][c] = fma2(d[c], now[c], gw[K - 1][c]);
-                        gb[c] = add2(gb[c], d[c]);
+                            for (int k = 0; k < K - 1; k++) gw[k][c] = fma2(d[c], old[k][c], gw[k][c]);
+                            gw[K - 1][c] = fma2(d[c], now[c], gw[K - 1][c]);
+                            gb[c] = add2(gb[c], d[c]);
+                        }
                     }
+                    Row de;
 #pragma unroll
-                    for (int k = 0; k + 2 < K; k++) old[k][c] = old[k + 1][c];
-                    if (K > 1) old[K > 1 ? K - 2 : 0][c] = now[c];
+                    for (int c = 0; c < kPairs; c++) {
+#pragma unroll
+                        for (int k = 0; k + 2 < K; k++) old[k][c] = old[k + 1][c];
+                        if (K > 1) old[K > 1 ? K - 2 : 0][c] = now[c];
+                        de[c] = mul2(w[0][c], dz[K - 1][c]);
+#pragma unroll
+                        for (int k = 1; k < K; k++) de[c] = fma2(w[k][c], dz[K - 1 - k][c], de[c]);
+                    }
+                    if (gso != nullptr && t0 + r >= s.len && r < all) {     // in the new history as well
+                        Row g2;
+                        pairs_of(g2, word_of<WHOLE>(gso + (t0 + r - s.len) * P.C, true, n, P.c_whole));
+#pragma unroll
+                        for (int c = 0; c < kPairs; c++) de[c] = add2(de[c], g2[c]);
+                    }
+                    if (r >= K - 1 && r < all) store_row<WHOLE>(out, de, n, P.c_whole);
+                    if (K > 1 && r < K - 1 && r < all && t0 == 0 && P.gstate_in != nullptr)
+                        store_row<WHOLE>(P.gstate_in + ((long long)b * (K - 1) + r) * P.C + c0, de, n, P.c_whole);
+                    out += P.C;
                 }
-                const long long i = t - (K - 1);            // the row of x that is complete, or below 0 one of the history
-                if (i >= end || (i < t0 && (t0 != 0 || P.gstate_in == nullptr || K == 1)) || q * kAhead + r >= kRows + K - 1) continue;
-                Row de;
-#pragma unroll
-                for (int c = 0; c < kPairs; c++) {
-                    de[c] = mul2(w[0][c], dz[K - 1][c]);
-#pragma unroll
-                    for (int k = 1; k < K; k++) de[c] = fma2(w[k][c], dz[K - 1 - k][c], de[c]);
-                }
-                const long long j = i + (K - 1) - s.len;    // its place in the new history
-                if (j >= 0 && gso != nullptr) {
-                    Row g2;
-                    pairs_of(g2, word_of<WHOLE>(gso + j * P.C, true, n, P.c_whole));
-#pragma unroll
-                    for (int c = 0; c < kPairs; c++) de[c] = add2(de[c], g2[c]);
-                }
-                if (i >= 0) store_row<WHOLE>(gx + i * P.C, de, n, P.c_whole);
-                else store_row<WHOLE>(P.gstate_in + ((long long)b * (K - 1) + i + K - 1) * P.C + c0, de, n, P.c_whole);
+                fetch(nx[q], ngy[q]);
             }
         }
     }
@@ -269,18 +285,28 @@ int check(const cawn_conv_params *p)
     if (p->K > 4 || p->C > (1 << 22)) return CAWN_ERR_UNSUPPORTED;
     const double rows = p->rows > 0 ? (double)p->rows : (double)p->B * (double)p->L;
     if (rows * (double)(p->x_stride > p->C ? p->x_stride : p->C) > 1.0e17) return CAWN_ERR_UNSUPPORTED;
-    if ((double)p->B * (double)(p->L / kTile + 1) > 2.0e9) return CAWN_ERR_UNSUPPORTED;
+    if ((double)p->B * (double)(p->L / (kWalks * kStep) + 1) > 2.0e9) return CAWN_ERR_UNSUPPORTED;
     return CAWN_OK;
 }
 
-ConvParams fill(const cawn_conv_params *p, const int64_t *offsets)
+// Tiles that run at once by the kernels' registers, for each of the blocks across the channels.
+int64_t room(const cawn_conv_params *p, bool bwd)
+{
+    return most((int64_t)sm_count() * (bwd ? kBwdBlocks : fwd_blocks(p->flags != 0 ? 2 : 4)) / ceil_div(p->C, kChannels), 1);
+}
+
+ConvParams fill(const cawn_conv_params *p, const int64_t *offsets, bool bwd)
 {
     ConvParams P = {};
     P.seq = {reinterpret_cast<const long long *>(offsets), p->L, offsets != nullptr ? p->rows : (int64_t)p->B * p->L, p->B};
     P.C = p->C;
     P.x_stride = p->x_stride != 0 ? p->x_stride : p->C;
     P.words = (int)ceil_div(p->C, kWord);
-    P.tiles = most(ceil_div(p->L, kTile), 1);
+    // as many tiles of each sequence as there is room for at once; twice as many where lengths differ
+    const int64_t each = most((offsets != nullptr ? 2 : 1) * room(p, bwd) / p->B, 1);
+    const int64_t steps = most(ceil_div(ceil_div(p->L, each), kWalks * kStep), 1);
+    P.rows = (int)(steps < 1 << 16 ? steps : 1 << 16) * kStep;
+    P.tiles = most(ceil_div(p->L, P.rows * kWalks), 1);
     P.all_tiles = P.tiles * p->B;
     P.silu = p->act == CAWN_CONV_ACT_SILU;
     P.x_whole = P.x_stride % kWord == 0;
@@ -288,11 +314,10 @@ ConvParams fill(const cawn_conv_params *p, const int64_t *offsets)
     return P;
 }
 
-// Blocks along the tiles in the backward: as many as run at once by their registers, each with a partial row of sums.  Never fewer for more tiles.
-int64_t workers(const cawn_conv_params *p)
+// Blocks along the tiles in the backward, each with a partial row of sums; what a workspace is sized for never falls as a call grows.
+int64_t most_workers(const cawn_conv_params *p)
 {
-    const int64_t across = ceil_div(p->C, kChannels), tiles = most(ceil_div(p->L, kTile), 1) * p->B;
-    const int64_t want = most((int64_t)sm_count() * (p->flags != 0 ? 3 : 2) / across, 1);
+    const int64_t tiles = most(ceil_div(p->L, kWalks * kStep), 1) * p->B, want = room(p, true);
     return tiles < want ? tiles : want;
 }
 
@@ -324,7 +349,7 @@ extern "C" int cawn_short_conv_fwd(const cawn_conv_params *params, const void *x
     if (rc != CAWN_OK) return rc;
     if (weight == nullptr || (params->L > 0 && (x == nullptr || y == nullptr))) return CAWN_ERR_NULL_POINTER;
     if (!all_aligned16(x, weight, bias, state_in, y, state_out)) return CAWN_ERR_MISALIGNED;
-    ConvParams P = fill(params, offsets);
+    ConvParams P = fill(params, offsets, false);
     P.x = x; P.w = weight; P.b = bias; P.state_in = state_in; P.y = y; P.state_out = state_out;
     return status_of(launch<true>(pick(params, P, false), dim3((unsigned)P.all_tiles, (unsigned)ceil_div(P.words, kLanes)), dim3(kConvThreads), 0,
                                   static_cast<cudaStream_t>(cuda_stream), P));
@@ -336,7 +361,7 @@ extern "C" int cawn_short_conv_workspace_bytes(const cawn_conv_params *params, s
     const int rc = check(params);
     if (rc != CAWN_OK) return rc;
     if (bytes == nullptr) return CAWN_ERR_NULL_POINTER;
-    *bytes = (size_t)workers(params) * params->C * (params->K + 1) * sizeof(float);
+    *bytes = (size_t)most_workers(params) * params->C * (params->K + 1) * sizeof(float);
     return CAWN_OK;
 }
 
@@ -354,9 +379,9 @@ extern "C" int cawn_short_conv_bwd(const cawn_conv_params *params, const void *x
         return CAWN_ERR_NULL_POINTER;
     if (!all_aligned16(x, weight, bias, state_in, grad_y, grad_state_out, grad_x, grad_weight, grad_bias, grad_state_in, workspace))
         return CAWN_ERR_MISALIGNED;
-    const int64_t blocks = workers(params), cols = (int64_t)params->C * (params->K + 1);
+    ConvParams P = fill(params, offsets, true);
+    const int64_t want = room(params, true), blocks = P.all_tiles < want ? P.all_tiles : want, cols = (int64_t)params->C * (params->K + 1);
     if (sums && workspace_bytes < (size_t)blocks * cols * sizeof(float)) return CAWN_ERR_WORKSPACE_TOO_SMALL;
-    ConvParams P = fill(params, offsets);
     P.x = x; P.w = weight; P.b = bias; P.state_in = state_in; P.gy = grad_y; P.gstate_out = grad_state_out;
     P.gx = grad_x; P.gstate_in = grad_state_in; P.part = sums ? static_cast<float *>(workspace) : nullptr;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

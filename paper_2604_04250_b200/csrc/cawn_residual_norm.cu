@@ -25,6 +25,19 @@ struct ResidualNormParams {
 
 constexpr int kWarps = 8, kNormBlock = 32 * kWarps;
 
+template <class T> __device__ __forceinline__ void pairs_of(f32x2 (&r)[4], const Eight<T> &e)
+{
+    float f[8];
+    e.widen_to(f);
+#pragma unroll
+    for (int i = 0; i < 4; i++) r[i] = pair(f[2 * i], f[2 * i + 1]);
+}
+template <bool WHOLE, class T> __device__ __forceinline__ void put_eight(T *p, const float (&f)[8], int n, bool whole)
+{
+    if constexpr (!WHOLE) store_eight(p, f, n, whole);
+    else if (n > 0) store_vec(p, f);
+}
+
 // Sum (or maximum) over a team: a warp, or the block's eight.  `turn` tells one use of the block's exchange from the next.
 template <int TEAM, bool MAX> __device__ __forceinline__ float over_team(float v, float (*red)[kWarps], int turn)
 {
@@ -54,7 +67,7 @@ __device__ __forceinline__ uint2 to_e4m3(const float (&f)[8])
     return make_uint2(u[0] | u[1] << 16, u[2] | u[3] << 16);
 }
 
-template <class T, class S, int TEAM, int NV, bool E4M3>
+template <class T, class S, int TEAM, int NV, bool E4M3, bool WHOLE>
 __global__ void __launch_bounds__(kNormBlock) residual_norm_fwd_kernel(const ResidualNormParams P)
 {
     follow_previous();
@@ -71,9 +84,8 @@ __global__ void __launch_bounds__(kNormBlock) residual_norm_fwd_kernel(const Res
 #pragma unroll
     for (int j = 0; j < NV; j++) {
         const int c = (j * TEAM + lane) * 8;
-        xs[j] = fetch_eight(x + c, P.M - c, P.x_whole);
-        if (res != nullptr) rs[j] = fetch_eight(res + c, P.M - c, P.m_whole);
-        else rs[j].clear();
+        xs[j] = eight_of<WHOLE>(x + c, P.M - c, P.x_whole);
+        rs[j] = eight_of<WHOLE>(res + c, res != nullptr ? P.M - c : 0, P.m_whole);
     }
 #pragma unroll
     for (int j = 0; j < NV; j++) {
@@ -86,14 +98,14 @@ __global__ void __launch_bounds__(kNormBlock) residual_norm_fwd_kernel(const Res
             v[j][i] = widen(narrow<S>(v[j][i] + b[i]));         // the stream's own value is what is normed
             q = fmaf(v[j][i], v[j][i], q);
         }
-        if (sum != nullptr) store_eight(sum + c, v[j], P.M - c, P.m_whole);
+        if (sum != nullptr) put_eight<WHOLE>(sum + c, v[j], P.M - c, P.m_whole);
     }
     const float rstd = __frsqrt_rn(over_team<TEAM, false>(q, red, 0) * P.inv_m + P.eps);
     float top = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; j++) {
         const int c = (j * TEAM + lane) * 8;
-        const Eight<float> wt = P.w != nullptr ? fetch_eight(P.w + c, P.M - c, P.M % 4 == 0) : Eight<float>();
+        const Eight<float> wt = eight_of<WHOLE>(P.w + c, P.w != nullptr ? P.M - c : 0, P.M % 4 == 0);
         float w[8];
         wt.widen_to(w);
 #pragma unroll
@@ -119,7 +131,7 @@ __global__ void __launch_bounds__(kNormBlock) residual_norm_fwd_kernel(const Res
                 top = m > top || m != m ? m : top;
             }
         } else {
-            store_eight(static_cast<T *>(P.y) + r * P.M + c, v[j], P.M - c, P.m_whole);
+            put_eight<WHOLE>(static_cast<T *>(P.y) + r * P.M + c, v[j], P.M - c, P.m_whole);
         }
     }
     if constexpr (E4M3) {
@@ -148,23 +160,23 @@ __global__ void __launch_bounds__(kNormBlock) residual_norm_fwd_kernel(const Res
     }
 }
 
-template <class T, class S, int TEAM, int NV>
-__global__ void __launch_bounds__(kNormBlock) residual_norm_bwd_kernel(const ResidualNormParams P)
+template <class T, class S, int TEAM, int NV, bool WHOLE>
+__global__ void __launch_bounds__(kNormBlock, NV <= 3 ? 2 : 1) residual_norm_bwd_kernel(const ResidualNormParams P)
 {
     follow_previous();
     __shared__ float red[2][kWarps];
     __shared__ float fold[TEAM == 32 ? kNormBlock * 8 : 1];
     const int lane = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
     constexpr int kTeams = kNormBlock / TEAM;
-    float w[NV][8], gw[NV][8] = {};
+    f32x2 w[NV][4], gw[NV][4] = {};
 #pragma unroll
     for (int j = 0; j < NV; j++) {
         const int c = (j * TEAM + lane) * 8;
         if (P.w != nullptr) {
-            fetch_eight(P.w + c, P.M - c, P.M % 4 == 0).widen_to(w[j]);
+            pairs_of(w[j], eight_of<WHOLE>(P.w + c, P.M - c, P.M % 4 == 0));
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; i++) w[j][i] = 1.f;
+            for (int i = 0; i < 4; i++) w[j][i] = twice(1.f);
         }
     }
     for (long long r = (long long)blockIdx.x * kTeams + team; r < P.N; r += (long long)gridDim.x * kTeams) {
@@ -173,41 +185,44 @@ __global__ void __launch_bounds__(kNormBlock) residual_norm_bwd_kernel(const Res
 #pragma unroll
         for (int j = 0; j < NV; j++) {
             const int c = (j * TEAM + lane) * 8;
-            ss[j] = fetch_eight(static_cast<const S *>(P.sum) + r * P.M + c, P.M - c, P.m_whole);
-            gy[j] = fetch_eight(static_cast<const T *>(P.gy) + r * P.M + c, P.M - c, P.m_whole);
-            if (P.gsum != nullptr) gs[j] = fetch_eight(static_cast<const S *>(P.gsum) + r * P.M + c, P.M - c, P.m_whole);
-            else gs[j].clear();
+            ss[j] = eight_of<WHOLE>(static_cast<const S *>(P.sum) + r * P.M + c, P.M - c, P.m_whole);
+            gy[j] = eight_of<WHOLE>(static_cast<const T *>(P.gy) + r * P.M + c, P.M - c, P.m_whole);
+            gs[j] = eight_of<WHOLE>(static_cast<const S *>(P.gsum) + r * P.M + c, P.gsum != nullptr ? P.M - c : 0, P.m_whole);
         }
-        float q = 0.f, p = 0.f;
+        f32x2 qq = 0ull, pp = 0ull;
 #pragma unroll
         for (int j = 0; j < NV; j++) {
-            float s[8], g[8];
-            ss[j].widen_to(s);
-            gy[j].widen_to(g);
+            f32x2 s[4], g[4];
+            pairs_of(s, ss[j]);
+            pairs_of(g, gy[j]);
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                q = fmaf(s[i], s[i], q);
-                p = fmaf(g[i] * w[j][i], s[i], p);
+            for (int i = 0; i < 4; i++) {
+                qq = fma2(s[i], s[i], qq);
+                pp = fma2(mul2(g[i], w[j][i]), s[i], pp);
             }
         }
-        q = over_team<TEAM, false>(q, red, 0);
-        p = over_team<TEAM, false>(p, red, 1);
+        const float2 qh = halves(qq), ph = halves(pp);
+        const float q = over_team<TEAM, false>(qh.x + qh.y, red, 0), p = over_team<TEAM, false>(ph.x + ph.y, red, 1);
         // r (d - s k) with k = mean(d s) / (mean(s^2) + eps): the two terms may cancel, so k is rounded as few times as it can be
         const float var = q * P.inv_m + P.eps, rstd = __frsqrt_rn(var), k = p * P.inv_m / var;
+        const f32x2 r2 = twice(rstd), k2 = twice(-k);
 #pragma unroll
         for (int j = 0; j < NV; j++) {
             const int c = (j * TEAM + lane) * 8;
-            float s[8], g[8], past[8], d[8];
-            ss[j].widen_to(s);
-            gy[j].widen_to(g);
-            gs[j].widen_to(past);
+            f32x2 s[4], g[4], past[4];
+            float d[8];
+            pairs_of(s, ss[j]);
+            pairs_of(g, gy[j]);
+            pairs_of(past, gs[j]);
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                gw[j][i] = fmaf(g[i], s[i] * rstd, gw[j][i]);
-                d[i] = fmaf(rstd, fmaf(-s[i], k, g[i] * w[j][i]), past[i]);
+            for (int i = 0; i < 4; i++) {
+                gw[j][i] = fma2(g[i], mul2(s[i], r2), gw[j][i]);
+                const float2 o = halves(fma2(r2, fma2(s[i], k2, mul2(g[i], w[j][i])), past[i]));
+                d[2 * i] = o.x;
+                d[2 * i + 1] = o.y;
             }
-            if (P.gresidual != nullptr) store_eight(static_cast<S *>(P.gresidual) + r * P.M + c, d, P.M - c, P.m_whole);
-            if (P.gx != nullptr) store_eight(static_cast<T *>(P.gx) + r * P.M + c, d, P.M - c, P.m_whole);
+            if (P.gresidual != nullptr) put_eight<WHOLE>(static_cast<S *>(P.gresidual) + r * P.M + c, d, P.M - c, P.m_whole);
+            if (P.gx != nullptr) put_eight<WHOLE>(static_cast<T *>(P.gx) + r * P.M + c, d, P.M - c, P.m_whole);
         }
         if constexpr (TEAM > 32) __syncthreads();               // red is written again in the next row
     }
@@ -218,12 +233,19 @@ __global__ void __launch_bounds__(kNormBlock) residual_norm_bwd_kernel(const Res
         if constexpr (TEAM > 32) {
             const int c = (j * TEAM + lane) * 8;
 #pragma unroll
-            for (int i = 0; i < 8; i++)
-                if (c + i < P.M) part[c + i] = gw[j][i];
+            for (int i = 0; i < 4; i++) {
+                const float2 v = halves(gw[j][i]);
+                if (c + 2 * i < P.M) part[c + 2 * i] = v.x;
+                if (c + 2 * i + 1 < P.M) part[c + 2 * i + 1] = v.y;
+            }
         } else {
             __syncthreads();
 #pragma unroll
-            for (int i = 0; i < 8; i++) fold[(team * 8 + i) * 32 + lane] = gw[j][i];
+            for (int i = 0; i < 4; i++) {
+                const float2 v = halves(gw[j][i]);
+                fold[(team * 8 + 2 * i) * 32 + lane] = v.x;
+                fold[(team * 8 + 2 * i + 1) * 32 + lane] = v.y;
+            }
             __syncthreads();
             // one channel a thread: 256 of the word row j
             float v = 0.f;
@@ -261,7 +283,7 @@ Team team_of(int M)
 int64_t workers(const cawn_residual_norm_params *p)
 {
     const Team t = team_of(p->M);
-    const int64_t blocks = ceil_div(p->N, kNormBlock / t.size), want = (int64_t)sm_count() * (t.nv <= 1 ? 4 : t.nv <= 3 ? 2 : 1);
+    const int64_t blocks = ceil_div(p->N, kNormBlock / t.size), want = (int64_t)sm_count() * (t.nv <= 3 ? 2 : 1);
     return blocks < want ? blocks : want;
 }
 
@@ -280,22 +302,28 @@ ResidualNormParams fill(const cawn_residual_norm_params *p)
 }
 
 using Kernel = void (*)(ResidualNormParams);
-template <class T, class S, int KIND> Kernel pick(const Team &t)       // KIND: 0 forward, 1 forward to e4m3, 2 backward
+// KIND: 0 forward, 1 forward to e4m3, 2 backward.  WHOLE: all rows are whole 16-byte words of eight channels.
+template <class T, class S, int KIND, bool WHOLE> Kernel pick(const Team &t)
 {
 #define CAWN_PICK(TEAM, NV)                                                                                           \
     if (t.size == TEAM && t.nv == NV) {                                                                               \
-        if constexpr (KIND == 2) return residual_norm_bwd_kernel<T, S, TEAM, NV>;                                     \
-        else return residual_norm_fwd_kernel<T, S, TEAM, NV, KIND == 1>;                                              \
+        if constexpr (KIND == 2) return residual_norm_bwd_kernel<T, S, TEAM, NV, WHOLE>;                              \
+        else return residual_norm_fwd_kernel<T, S, TEAM, NV, KIND == 1, WHOLE>;                                       \
     }
     CAWN_PICK(32, 1) CAWN_PICK(32, 2) CAWN_PICK(32, 3) CAWN_PICK(32, 4)
     CAWN_PICK(kNormBlock, 1) CAWN_PICK(kNormBlock, 2) CAWN_PICK(kNormBlock, 3) CAWN_PICK(kNormBlock, 4)
 #undef CAWN_PICK
     return nullptr;
 }
-template <int KIND> Kernel pick(const cawn_residual_norm_params *p, const Team &t)
+template <int KIND, bool WHOLE> Kernel pick(const cawn_residual_norm_params *p, const Team &t)
 {
-    if (p->flags == 0) return pick<float, float, KIND>(t);
-    return p->stream_float ? pick<bf16, float, KIND>(t) : pick<bf16, bf16, KIND>(t);
+    if (p->flags == 0) return pick<float, float, KIND, WHOLE>(t);
+    return p->stream_float ? pick<bf16, float, KIND, WHOLE>(t) : pick<bf16, bf16, KIND, WHOLE>(t);
+}
+template <int KIND> Kernel pick(const cawn_residual_norm_params *p, const ResidualNormParams &P, const Team &t)
+{
+    const bool whole = P.m_whole && (KIND == 2 || P.x_whole) && p->M % 8 == 0;
+    return whole ? pick<KIND, true>(p, t) : pick<KIND, false>(p, t);
 }
 
 }  // namespace
@@ -315,7 +343,7 @@ extern "C" int cawn_residual_norm_fwd(const cawn_residual_norm_params *params, c
     ResidualNormParams P = fill(params);
     P.x = x; P.residual = residual; P.w = weight; P.sum_out = sum_out; P.y = y; P.scales = scales;
     const Team t = team_of(params->M);
-    return status_of(launch<true>(e4m3 ? pick<1>(params, t) : pick<0>(params, t), dim3((unsigned)ceil_div(P.N, kNormBlock / t.size)), dim3(kNormBlock), 0,
+    return status_of(launch<true>(e4m3 ? pick<1>(params, P, t) : pick<0>(params, P, t), dim3((unsigned)ceil_div(P.N, kNormBlock / t.size)), dim3(kNormBlock), 0,
                                   static_cast<cudaStream_t>(cuda_stream), P));
 }
 
@@ -347,7 +375,7 @@ extern "C" int cawn_residual_norm_bwd(const cawn_residual_norm_params *params, c
     ResidualNormParams P = fill(params);
     P.sum = sum; P.w = weight; P.gy = grad_y; P.gsum = grad_sum; P.gresidual = grad_residual; P.gx = grad_x;
     P.part = grad_weight != nullptr ? static_cast<float *>(workspace) : nullptr;
-    const int first = status_of(launch<true>(pick<2>(params, team_of(params->M)), dim3((unsigned)blocks), dim3(kNormBlock), 0, st, P));
+    const int first = status_of(launch<true>(pick<2>(params, P, team_of(params->M)), dim3((unsigned)blocks), dim3(kNormBlock), 0, st, P));
     if (first != CAWN_OK || grad_weight == nullptr) return first;
     PartialSums S = {P.part, blocks, params->M, {grad_weight, nullptr, nullptr}, {params->M, 0, 0}};
     return sum_partials(S, st);

@@ -186,24 +186,6 @@ struct Shape {
     int resident(bool bwd) const { return nl == 2 ? (bwd ? 8 : 6) : nl == 4 ? 4 : ns == 4 ? 2 : 1; }
 };
 inline Shape shape_of(int N) { return N <= 8 ? Shape{2, 4, 2} : N <= 16 ? Shape{4, 4, 2} : N <= 32 ? Shape{8, 4, 2} : Shape{8, 8, 1}; }
-// Rows all of whose words are whole are fetched without a branch.
-template <bool WHOLE, class T> __device__ __forceinline__ Eight<T> eight_of(const T *p, int n, bool whole)
-{
-    if constexpr (!WHOLE) return fetch_eight(p, n, whole);
-    Eight<T> r;
-    r.clear();
-    if (n > 0) r.load(p);
-    return r;
-}
-template <bool WHOLE, class T> __device__ __forceinline__ Quad<T> quad_of(const T *p, int n, bool whole)
-{
-    if constexpr (!WHOLE) return fetch_quad(p, n, whole);
-    Quad<T> r;
-    r.set(make_float4(0.f, 0.f, 0.f, 0.f));
-    if (n > 0) r.load(p);
-    return r;
-}
-
 // A launch for the shape: CALL(NL, NS, CD).
 #define CAWN_BY_SHAPE(S, CALL) ((S).ns == 8 ? CALL(8, 8, 1) : (S).nl == 8 ? CALL(8, 4, 2) : (S).nl == 4 ? CALL(4, 4, 2) : CALL(2, 4, 2))
 

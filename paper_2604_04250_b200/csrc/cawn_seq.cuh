@@ -130,6 +130,24 @@ template <class T> __device__ __forceinline__ void store_quad(T *p, float4 v, in
     }
 }
 
+// Rows all of whose words are whole are fetched without a branch.
+template <bool WHOLE, class T> __device__ __forceinline__ Eight<T> eight_of(const T *p, int n, bool whole)
+{
+    if constexpr (!WHOLE) return fetch_eight(p, n, whole);
+    Eight<T> r;
+    r.clear();
+    if (n > 0) r.load(p);
+    return r;
+}
+template <bool WHOLE, class T> __device__ __forceinline__ Quad<T> quad_of(const T *p, int n, bool whole)
+{
+    if constexpr (!WHOLE) return fetch_quad(p, n, whole);
+    Quad<T> r;
+    r.set(make_float4(0.f, 0.f, 0.f, 0.f));
+    if (n > 0) r.load(p);
+    return r;
+}
+
 __device__ __forceinline__ float reciprocal_fast(float v)
 {
     float r;
