@@ -12,9 +12,10 @@ namespace {
 
 constexpr int kLanes = 32, kWalks = 4, kStep = 8;        // a block: 32 words of four channels, 4 walks of a multiple of 8 rows
 constexpr int kConvThreads = kLanes * kWalks;
+constexpr int kBatch = 4;       // rows that are computed at a time
 // Blocks that a multiprocessor holds.
-constexpr int fwd_blocks(size_t element) { return element == 2 ? 5 : 4; }
-constexpr int kBwdBlocks = 4;
+constexpr int fwd_blocks(size_t element) { return element == 2 ? 8 : 5; }
+constexpr int kBwdBlocks = 3, kPackedTurns = 3;        // packed sequences differ, so their blocks come in that many waves
 
 struct ConvParams {
     Sequences seq;
@@ -51,6 +52,30 @@ template <bool WHOLE, class T> __device__ __forceinline__ void store_row(T *p, c
     const float2 a = halves(r[0]), b = halves(r[1]);
     store_quad(p, make_float4(a.x, a.y, b.x, b.y), WHOLE ? kWord : n, WHOLE || whole);
 }
+
+// A thread's rows on their way: DEPTH batches in shared memory, each thread's own words, so that no one waits for another
+// and none of them takes registers (with eight rows in registers the forward of 8 x 2048 x 2048 took 36 us, the backward 91).
+template <class T, int DEPTH, bool WHOLE> struct Ring {
+    Quad<T> words[DEPTH][kBatch][kConvThreads];
+    // Four rows set out, `left` of them there; as one group even where there is none.
+    __device__ __forceinline__ void fetch(int slot, const T *p, long long stride, int left, int n, bool whole)
+    {
+#pragma unroll
+        for (int r = 0; r < kBatch; r++) {
+            Quad<T> *to = &words[slot][r][threadIdx.x];
+            if constexpr (WHOLE) {
+                const unsigned at = (unsigned)__cvta_generic_to_shared(to);
+                const int bytes = r < left ? (int)sizeof(Quad<T>) : 0;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" :: "r"(at), "l"(p + r * stride), "n"(sizeof(Quad<T>)), "r"(bytes) : "memory");
+            } else {
+                *to = fetch_quad(p + r * stride, r < left ? n : 0, whole);
+            }
+        }
+    }
+    __device__ __forceinline__ void row(Row &r, int slot, int i) const { pairs_of(r, words[slot][i][threadIdx.x]); }
+};
+__device__ __forceinline__ void close_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int NEWER> __device__ __forceinline__ void wait_group() { asm volatile("cp.async.wait_group %0;" :: "n"(NEWER) : "memory"); }
 
 // Row `i` of the sequence behind its history (i < 0: history, zero without one), as the arrays hold it.
 template <class T, int K, bool WHOLE>
@@ -97,20 +122,20 @@ __global__ void __launch_bounds__(kConvThreads, fwd_blocks(sizeof(T))) conv_fwd_
     const T *x = static_cast<const T *>(P.x) + s.begin * P.x_stride + c0;
     const float *history = P.state_in != nullptr && K > 1 ? P.state_in + (long long)b * (K - 1) * P.C + c0 : nullptr;
     const int rows = !here ? 0 : s.len - t0 < P.rows ? (int)(s.len - t0) : P.rows;
-    // Four rows are computed while the next four are on their way; the first eight, and the K - 1 in front, set out before
-    // the weights do.
-    Quad<T> next[2][4];
+    // The first batches, and the K - 1 rows in front, set out before the weights do.
+    constexpr int kDepth = 4;
+    __shared__ __align__(16) Ring<T, kDepth, WHOLE> ring;
     const T *ahead = x + t0 * P.x_stride;
     int left = rows;            // of what is still to set out
-    auto fetch = [&](Quad<T> (&to)[4]) {
-#pragma unroll
-        for (int r = 0; r < 4; r++) to[r] = word_of<WHOLE>(ahead + r * P.x_stride, r < left, n, P.x_whole);
-        ahead += 4 * P.x_stride;
-        left -= 4;
+    auto fetch = [&](int slot) {
+        ring.fetch(slot, ahead, P.x_stride, left, n, P.x_whole);
+        close_group();
+        ahead += kBatch * P.x_stride;
+        left -= kBatch;
     };
     Row old[K];                 // the K - 1 rows in front of the next one
 #pragma unroll
-    for (int q = 0; q < 2; q++) fetch(next[q]);
+    for (int q = 0; q < kDepth; q++) fetch(q);
     if (here) {
 #pragma unroll
         for (int j = 0; j < K - 1; j++) extended<T, K, WHOLE>(old[j], P, x, history, t0 + j - (K - 1), n);
@@ -129,29 +154,84 @@ __global__ void __launch_bounds__(kConvThreads, fwd_blocks(sizeof(T))) conv_fwd_
         }
     }
     T *y = static_cast<T *>(P.y) + (s.begin + t0) * P.C + c0;
+    int slot = 0;
 #pragma unroll 1
-    for (int r0 = 0; r0 < rows; r0 += kStep) {
+    for (int r0 = 0; r0 < rows; r0 += kBatch, slot = slot + 1 == kDepth ? 0 : slot + 1) {
+        wait_group<kDepth - 1>();
 #pragma unroll
-        for (int q = 0; q < 2; q++) {
+        for (int r = 0; r < kBatch; r++) {
+            Row now, z;
+            ring.row(now, slot, r);
 #pragma unroll
-            for (int r = 0; r < 4; r++) {
-                Row now, z;
-                pairs_of(now, next[q][r]);
+            for (int c = 0; c < kPairs; c++) {
+                z[c] = fma2(w[K - 1][c], now[c], bias[c]);
 #pragma unroll
-                for (int c = 0; c < kPairs; c++) {
-                    z[c] = fma2(w[K - 1][c], now[c], bias[c]);
+                for (int k = 0; k < K - 1; k++) z[c] = fma2(w[k][c], old[k][c], z[c]);
+                if (P.silu) z[c] = mul2(z[c], sigmoid_of(z[c]));
 #pragma unroll
-                    for (int k = 0; k < K - 1; k++) z[c] = fma2(w[k][c], old[k][c], z[c]);
-                    if (P.silu) z[c] = mul2(z[c], sigmoid_of(z[c]));
-#pragma unroll
-                    for (int k = 0; k + 2 < K; k++) old[k][c] = old[k + 1][c];
-                    if (K > 1) old[K > 1 ? K - 2 : 0][c] = now[c];
-                }
-                if (r0 + q * 4 + r < rows) store_row<WHOLE>(y + (q * 4 + r) * (long long)P.C, z, n, P.c_whole);
+                for (int k = 0; k + 2 < K; k++) old[k][c] = old[k + 1][c];
+                if (K > 1) old[K > 1 ? K - 2 : 0][c] = now[c];
             }
-            fetch(next[q]);
+            if (r0 + r < rows) store_row<WHOLE>(y + r * (long long)P.C, z, n, P.c_whole);
         }
-        y += (long long)kStep * P.C;
+        y += (long long)kBatch * P.C;
+        fetch(slot);
+    }
+}
+
+// Single tokens: a thread has four channels of kTokens sequences, which share their weights.
+constexpr int kTokens = 4;
+template <class T, int K>
+__global__ void __launch_bounds__(kConvThreads) conv_step_kernel(const ConvParams P)
+{
+    follow_previous();
+    const int word = blockIdx.x * kConvThreads + threadIdx.x, c0 = word * kWord;
+    if (word >= P.words) return;
+    const int n = P.C - c0 < kWord ? P.C - c0 : kWord;
+    const long long b0 = (long long)blockIdx.y * kTokens;
+    Quad<T> x[kTokens];
+    Quad<float> old[kTokens][K], w[K];          // rows of the history; the four channels' K weights as they lie
+#pragma unroll
+    for (int r = 0; r < kTokens; r++) {
+        const bool in = b0 + r < P.seq.B;
+        x[r] = fetch_quad(static_cast<const T *>(P.x) + (b0 + r) * P.x_stride + c0, in ? n : 0, P.x_whole);
+#pragma unroll
+        for (int k = 0; k < K - 1; k++)
+            old[r][k] = fetch_quad(P.state_in + ((b0 + r) * (K - 1) + k) * P.C + c0, in && P.state_in != nullptr ? n : 0, P.c_whole);
+    }
+#pragma unroll
+    for (int i = 0; i < K; i++) w[i] = fetch_quad(P.w + (long long)c0 * K + i * 4, n * K - i * 4, true);
+    const Quad<float> bias = fetch_quad(P.b + c0, P.b != nullptr ? n : 0, true);
+    float ws[K * 4];
+#pragma unroll
+    for (int i = 0; i < K; i++) {
+        const float4 v = w[i].get();
+        ws[4 * i] = v.x; ws[4 * i + 1] = v.y; ws[4 * i + 2] = v.z; ws[4 * i + 3] = v.w;
+    }
+#pragma unroll
+    for (int r = 0; r < kTokens; r++) {
+        if (b0 + r >= P.seq.B) break;
+        const float4 now = x[r].get(), bv = bias.get();
+        float xs[4] = {now.x, now.y, now.z, now.w}, z[4] = {bv.x, bv.y, bv.z, bv.w};
+#pragma unroll
+        for (int c = 0; c < 4; c++) z[c] = fmaf(ws[c * K + K - 1], xs[c], z[c]);
+#pragma unroll
+        for (int k = 0; k < K - 1; k++) {
+            const float4 o = old[r][k].get();
+            const float os[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+            for (int c = 0; c < 4; c++) z[c] = fmaf(ws[c * K + k], os[c], z[c]);
+        }
+        if (P.silu) {
+#pragma unroll
+            for (int c = 0; c < 4; c++) z[c] *= sigmoid_of(z[c]);
+        }
+        store_quad(static_cast<T *>(P.y) + (b0 + r) * P.C + c0, make_float4(z[0], z[1], z[2], z[3]), n, P.c_whole);
+        if (K > 1 && P.state_out != nullptr) {
+            float *out = P.state_out + (b0 + r) * (K - 1) * P.C + c0;
+#pragma unroll
+            for (int k = 0; k < K - 1; k++) store_quad(out + (long long)k * P.C, k + 2 < K ? old[r][k + 2 < K ? k + 1 : 0].get() : now, n, P.c_whole);
+        }
     }
 }
 
@@ -160,7 +240,8 @@ template <class T, int K, bool WHOLE>
 __global__ void __launch_bounds__(kConvThreads, kBwdBlocks) conv_bwd_kernel(const ConvParams P)
 {
     follow_previous();
-    constexpr int kAhead = 2;   // rows computed while as many are on their way
+    constexpr int kDepth = sizeof(T) == 2 ? 4 : 2;
+    __shared__ __align__(16) Ring<T, kDepth, WHOLE> ring, ringg;        // x; grad_y
     __shared__ __align__(16) float fold[kWalks][kChannels];
     const int lane = threadIdx.x % kLanes, walk = threadIdx.x / kLanes, word = blockIdx.y * kLanes + lane, c0 = word * kWord;
     const int n = word < P.words ? (P.C - c0 < kWord ? P.C - c0 : kWord) : 0;
@@ -179,36 +260,34 @@ __global__ void __launch_bounds__(kConvThreads, kBwdBlocks) conv_bwd_kernel(cons
         Row old[K], dz[K] = {};                 // rows t-K+1 .. t-1 of e; dz of rows t-K+1 .. t (0 before this walk)
         const int own = (int)(s.len - t0 < P.rows ? s.len - t0 : P.rows);            // rows of this walk
         const int all = own + K - 1, have = (int)(s.len - t0 < all ? s.len - t0 : all);  // those gone through, and of them in the sequence
-        Quad<T> nx[2][kAhead], ngy[2][kAhead];
         const T *ax = x + t0 * P.x_stride, *ag = gy + t0 * P.C;
         int left = have;            // of what is still to set out
-        auto fetch = [&](Quad<T> (&to)[kAhead], Quad<T> (&tog)[kAhead]) {
-#pragma unroll
-            for (int r = 0; r < kAhead; r++) {
-                to[r] = word_of<WHOLE>(ax + r * P.x_stride, r < left, n, P.x_whole);
-                tog[r] = word_of<WHOLE>(ag + (long long)r * P.C, r < left, n, P.c_whole);
-            }
-            ax += kAhead * P.x_stride;
-            ag += (long long)kAhead * P.C;
-            left -= kAhead;
+        auto fetch = [&](int slot) {
+            ring.fetch(slot, ax, P.x_stride, left, n, P.x_whole);
+            ringg.fetch(slot, ag, P.C, left, n, P.c_whole);
+            close_group();
+            ax += kBatch * P.x_stride;
+            ag += (long long)kBatch * P.C;
+            left -= kBatch;
         };
-        fetch(nx[0], ngy[0]);
-        fetch(nx[1], ngy[1]);
+        wait_group<0>();            // nothing of the tile before is on its way
+#pragma unroll
+        for (int q = 0; q < kDepth; q++) fetch(q);
 #pragma unroll
         for (int j = 0; j < K - 1; j++) extended<T, K, WHOLE>(old[j], P, x, history, t0 + j - (K - 1), n);
         T *out = gx + (t0 - (K - 1)) * P.C;         // of the row that the next one completes
         // row r gives dz_r; what then is complete is the gradient of row r - (K - 1), whose last term dz_r is (in front of the
         // first walk of a sequence: of the history)
+        int slot = 0;
 #pragma unroll 1
-        for (int r0 = 0; r0 < all; r0 += 2 * kAhead) {
+        for (int r0 = 0; r0 < all; r0 += kBatch, slot = slot + 1 == kDepth ? 0 : slot + 1) {
+            wait_group<kDepth - 1>();
 #pragma unroll
-            for (int q = 0; q < 2; q++) {
-#pragma unroll
-                for (int k0 = 0; k0 < kAhead; k0++) {
-                    const int r = r0 + q * kAhead + k0;
+            for (int k0 = 0; k0 < kBatch; k0++) {
+                    const int r = r0 + k0;
                     Row now, d;
-                    pairs_of(now, nx[q][k0]);
-                    pairs_of(d, ngy[q][k0]);        // past the end: zero
+                    ring.row(now, slot, k0);
+                    ringg.row(d, slot, k0);         // past the end: zero
 #pragma unroll
                     for (int c = 0; c < kPairs; c++) {
                         if (P.silu) {
@@ -252,9 +331,8 @@ __global__ void __launch_bounds__(kConvThreads, kBwdBlocks) conv_bwd_kernel(cons
                     if (K > 1 && r < K - 1 && r < all && t0 == 0 && P.gstate_in != nullptr)
                         store_row<WHOLE>(P.gstate_in + ((long long)b * (K - 1) + r) * P.C + c0, de, n, P.c_whole);
                     out += P.C;
-                }
-                fetch(nx[q], ngy[q]);
             }
+            fetch(slot);
         }
     }
     if (P.part == nullptr) return;
@@ -302,9 +380,9 @@ ConvParams fill(const cawn_conv_params *p, const int64_t *offsets, bool bwd)
     P.C = p->C;
     P.x_stride = p->x_stride != 0 ? p->x_stride : p->C;
     P.words = (int)ceil_div(p->C, kWord);
-    // as many tiles of each sequence as there is room for at once; twice as many where lengths differ
-    const int64_t each = most((offsets != nullptr ? 2 : 1) * room(p, bwd) / p->B, 1);
-    const int64_t steps = most(ceil_div(ceil_div(p->L, each), kWalks * kStep), 1);
+    // as many tiles as there is room for at once
+    const int64_t rows = offsets != nullptr ? ceil_div(p->rows, kPackedTurns * room(p, bwd)) : ceil_div(p->L, most(room(p, bwd) / p->B, 1));
+    const int64_t steps = most(ceil_div(rows, kWalks * kStep), 1);
     P.rows = (int)(steps < 1 << 16 ? steps : 1 << 16) * kStep;
     P.tiles = most(ceil_div(p->L, P.rows * kWalks), 1);
     P.all_tiles = P.tiles * p->B;
@@ -317,7 +395,7 @@ ConvParams fill(const cawn_conv_params *p, const int64_t *offsets, bool bwd)
 // Blocks along the tiles in the backward, each with a partial row of sums; what a workspace is sized for never falls as a call grows.
 int64_t most_workers(const cawn_conv_params *p)
 {
-    const int64_t tiles = most(ceil_div(p->L, kWalks * kStep), 1) * p->B, want = room(p, true);
+    const int64_t tiles = most(ceil_div(p->L, kWalks * kStep), 1) * p->B, want = kPackedTurns * room(p, true);
     return tiles < want ? tiles : want;
 }
 
@@ -330,6 +408,10 @@ template <class T, bool WHOLE> ConvKernel pick(int K, bool bwd)
     case 3: return bwd ? conv_bwd_kernel<T, 3, WHOLE> : conv_fwd_kernel<T, 3, WHOLE>;
     default: return bwd ? conv_bwd_kernel<T, 4, WHOLE> : conv_fwd_kernel<T, 4, WHOLE>;
     }
+}
+template <class T> ConvKernel pick_step(int K)
+{
+    return K == 1 ? conv_step_kernel<T, 1> : K == 2 ? conv_step_kernel<T, 2> : K == 3 ? conv_step_kernel<T, 3> : conv_step_kernel<T, 4>;
 }
 ConvKernel pick(const cawn_conv_params *p, const ConvParams &P, bool bwd)
 {
@@ -351,6 +433,10 @@ extern "C" int cawn_short_conv_fwd(const cawn_conv_params *params, const void *x
     if (!all_aligned16(x, weight, bias, state_in, y, state_out)) return CAWN_ERR_MISALIGNED;
     ConvParams P = fill(params, offsets, false);
     P.x = x; P.w = weight; P.b = bias; P.state_in = state_in; P.y = y; P.state_out = state_out;
+    if (params->L == 1 && offsets == nullptr && ceil_div(params->B, kTokens) <= 65535)
+        return status_of(launch<true>(params->flags != 0 ? pick_step<bf16>(params->K) : pick_step<float>(params->K),
+                                      dim3((unsigned)ceil_div(P.words, kConvThreads), (unsigned)ceil_div(params->B, kTokens)), dim3(kConvThreads), 0,
+                                      static_cast<cudaStream_t>(cuda_stream), P));
     return status_of(launch<true>(pick(params, P, false), dim3((unsigned)P.all_tiles, (unsigned)ceil_div(P.words, kLanes)), dim3(kConvThreads), 0,
                                   static_cast<cudaStream_t>(cuda_stream), P));
 }
@@ -380,7 +466,7 @@ extern "C" int cawn_short_conv_bwd(const cawn_conv_params *params, const void *x
     if (!all_aligned16(x, weight, bias, state_in, grad_y, grad_state_out, grad_x, grad_weight, grad_bias, grad_state_in, workspace))
         return CAWN_ERR_MISALIGNED;
     ConvParams P = fill(params, offsets, true);
-    const int64_t want = room(params, true), blocks = P.all_tiles < want ? P.all_tiles : want, cols = (int64_t)params->C * (params->K + 1);
+    const int64_t want = (offsets != nullptr ? kPackedTurns : 1) * room(params, true), blocks = P.all_tiles < want ? P.all_tiles : want, cols = (int64_t)params->C * (params->K + 1);
     if (sums && workspace_bytes < (size_t)blocks * cols * sizeof(float)) return CAWN_ERR_WORKSPACE_TOO_SMALL;
     P.x = x; P.w = weight; P.b = bias; P.state_in = state_in; P.gy = grad_y; P.gstate_out = grad_state_out;
     P.gx = grad_x; P.gstate_in = grad_state_in; P.part = sums ? static_cast<float *>(workspace) : nullptr;
