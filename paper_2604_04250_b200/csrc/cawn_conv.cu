@@ -15,7 +15,7 @@ constexpr int kConvThreads = kLanes * kWalks;
 constexpr int kBatch = 4;       // rows that are computed at a time
 // Blocks that a multiprocessor holds.
 constexpr int fwd_blocks(size_t element) { return element == 2 ? 8 : 5; }
-constexpr int kBwdBlocks = 3, kPackedTurns = 3;        // packed sequences differ, so their blocks come in that many waves
+constexpr int kBwdBlocks = 3;
 
 struct ConvParams {
     Sequences seq;
@@ -242,7 +242,6 @@ __global__ void __launch_bounds__(kConvThreads, kBwdBlocks) conv_bwd_kernel(cons
     follow_previous();
     constexpr int kDepth = sizeof(T) == 2 ? 4 : 2;
     __shared__ __align__(16) Ring<T, kDepth, WHOLE> ring, ringg;        // x; grad_y
-    __shared__ __align__(16) float fold[kWalks][kChannels];
     const int lane = threadIdx.x % kLanes, walk = threadIdx.x / kLanes, word = blockIdx.y * kLanes + lane, c0 = word * kWord;
     const int n = word < P.words ? (P.C - c0 < kWord ? P.C - c0 : kWord) : 0;
     Row w[K], bias, gw[K] = {}, gb = {};
@@ -336,20 +335,24 @@ __global__ void __launch_bounds__(kConvThreads, kBwdBlocks) conv_bwd_kernel(cons
         }
     }
     if (P.part == nullptr) return;
+    // sums of the block's walks, in their order
+    float (*fold)[K + 1][kChannels] = reinterpret_cast<float (*)[K + 1][kChannels]>(&ring);
+    static_assert(sizeof(ring) >= sizeof(float) * kWalks * (K + 1) * kChannels, "the rows' words serve again");
+    wait_group<0>();
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k <= K; k++)
+#pragma unroll
+        for (int c = 0; c < kPairs; c++) *reinterpret_cast<f32x2 *>(&fold[walk][k][lane * kWord + 2 * c]) = k < K ? gw[k < K ? k : 0][c] : gb[c];
+    __syncthreads();
     float *part = P.part + (long long)blockIdx.x * P.C * (K + 1);
+    const int first = blockIdx.y * kChannels, here = P.C - first < kChannels ? P.C - first : kChannels;
+    for (int i = threadIdx.x; i < here * (K + 1); i += kConvThreads) {
+        const int k = i < here * K ? i % K : K, c = i < here * K ? i / K : i - here * K;
+        float v = 0.f;
 #pragma unroll
-    for (int k = 0; k <= K; k++) {
-        __syncthreads();
-#pragma unroll
-        for (int c = 0; c < kPairs; c++) *reinterpret_cast<f32x2 *>(&fold[walk][lane * kWord + 2 * c]) = k < K ? gw[k < K ? k : 0][c] : gb[c];
-        __syncthreads();
-        for (int i = threadIdx.x; i < kChannels; i += kConvThreads) {
-            const int c = blockIdx.y * kChannels + i;
-            float v = 0.f;
-#pragma unroll
-            for (int q = 0; q < kWalks; q++) v += fold[q][i];
-            if (c < P.C) part[k < K ? (long long)c * K + k : (long long)P.C * K + c] = v;
-        }
+        for (int q = 0; q < kWalks; q++) v += fold[q][k][c];
+        part[k < K ? (long long)first * K + i : (long long)P.C * K + first + c] = v;
     }
 }
 
@@ -381,7 +384,7 @@ ConvParams fill(const cawn_conv_params *p, const int64_t *offsets, bool bwd)
     P.x_stride = p->x_stride != 0 ? p->x_stride : p->C;
     P.words = (int)ceil_div(p->C, kWord);
     // as many tiles as there is room for at once
-    const int64_t rows = offsets != nullptr ? ceil_div(p->rows, kPackedTurns * room(p, bwd)) : ceil_div(p->L, most(room(p, bwd) / p->B, 1));
+    const int64_t rows = offsets != nullptr ? ceil_div(p->rows, room(p, bwd)) : ceil_div(p->L, most(room(p, bwd) / p->B, 1));
     const int64_t steps = most(ceil_div(rows, kWalks * kStep), 1);
     P.rows = (int)(steps < 1 << 16 ? steps : 1 << 16) * kStep;
     P.tiles = most(ceil_div(p->L, P.rows * kWalks), 1);
@@ -395,7 +398,7 @@ ConvParams fill(const cawn_conv_params *p, const int64_t *offsets, bool bwd)
 // Blocks along the tiles in the backward, each with a partial row of sums; what a workspace is sized for never falls as a call grows.
 int64_t most_workers(const cawn_conv_params *p)
 {
-    const int64_t tiles = most(ceil_div(p->L, kWalks * kStep), 1) * p->B, want = kPackedTurns * room(p, true);
+    const int64_t tiles = most(ceil_div(p->L, kWalks * kStep), 1) * p->B, want = room(p, true);
     return tiles < want ? tiles : want;
 }
 
@@ -466,7 +469,7 @@ extern "C" int cawn_short_conv_bwd(const cawn_conv_params *params, const void *x
     if (!all_aligned16(x, weight, bias, state_in, grad_y, grad_state_out, grad_x, grad_weight, grad_bias, grad_state_in, workspace))
         return CAWN_ERR_MISALIGNED;
     ConvParams P = fill(params, offsets, true);
-    const int64_t want = (offsets != nullptr ? kPackedTurns : 1) * room(params, true), blocks = P.all_tiles < want ? P.all_tiles : want, cols = (int64_t)params->C * (params->K + 1);
+    const int64_t want = room(params, true), blocks = P.all_tiles < want ? P.all_tiles : want, cols = (int64_t)params->C * (params->K + 1);
     if (sums && workspace_bytes < (size_t)blocks * cols * sizeof(float)) return CAWN_ERR_WORKSPACE_TOO_SMALL;
     P.x = x; P.w = weight; P.b = bias; P.state_in = state_in; P.gy = grad_y; P.gstate_out = grad_state_out;
     P.gx = grad_x; P.gstate_in = grad_state_in; P.part = sums ? static_cast<float *>(workspace) : nullptr;
