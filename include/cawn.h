@@ -588,7 +588,8 @@ CAWN_API int cawn_dropout(const cawn_dropout_params *params, const void *x, cons
  *   y_t = z_t | z_t sigmoid(z_t)                         by `act`
  * Rows in front of a sequence are its history state_in [B, K-1, C] float (NULL = 0; the oldest row
  * first); state_out receives the last K-1 rows of (history, sequence) and may alias state_in.
- * x: [rows, C], rows x_stride elements apart (0 = dense); y [rows, C] dense, not aliasing x.
+ * x: [rows, C], rows x_stride elements apart (0 = dense), aligned to its elements (whole words are read where
+ * rows begin on four of them); y [rows, C] dense, not aliasing x.
  * weight [C, K], bias [C] float.  Single tokens are calls with L = 1.
  */
 enum { CAWN_CONV_ACT_NONE = 0, CAWN_CONV_ACT_SILU = 1 };
@@ -632,8 +633,8 @@ CAWN_API int cawn_short_conv_bwd(const cawn_conv_params *params, const void *x, 
  *   state_out = h_{L-1}
  * Shapes.  x, dt, z, y [rows, D]; B, C [rows, G, N], channel c reads group c / (D/G); A [D, N] float
  * (usually negative); skip, dt_bias [D] float; states [B, D, N] float.  Rows of x, dt, z, B and C lie
- * *_stride elements apart (0 = dense), so that they may be slices of projections; B and C need only be
- * aligned to their elements (whole words are read where they are aligned to four of them).
+ * *_stride elements apart (0 = dense), so that they may be slices of projections, and need only be aligned to
+ * their elements (whole words are read where rows begin on 16 bytes; of B and C, on four elements).
  * Precision.  Everything is computed in float; results are rounded once to their type.  The
  * backward's sums over channels (gradients of B and C) take terms of 22 bits of mantissa.
  * Non-finite values stay in their sequence and in the channels of their group; gradients of B and C may
@@ -707,7 +708,7 @@ CAWN_API int cawn_selective_scan_bwd(const cawn_scan_params *params, const void 
  * Root-mean-square norm of the stream that a branch is added to:
  *   s = x + residual (residual NULL = 0), rounded to the stream's type;  sum_out = s (NULL = not wanted)
  *   y = s / sqrt(mean(s^2) + eps) * weight                               weight [M] float, NULL = 1
- * x [N, M], rows x_stride elements apart (0 = dense); residual, sum_out: [N, M] dense in the stream's
+ * x [N, M], rows x_stride elements apart (0 = dense), aligned to its elements; residual, sum_out: [N, M] dense in the stream's
  * type, which is that of x, or float with stream_float.  sum_out may alias residual, or x where x is
  * dense and of the stream's type.  y [N, M] dense, by `out`:
  *   CAWN_NORM_OUT_SAME   the type of x (may alias x where x is dense; scales NULL)

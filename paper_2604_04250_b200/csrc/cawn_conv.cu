@@ -376,7 +376,7 @@ int64_t room(const cawn_conv_params *p, bool bwd)
     return most((int64_t)sm_count() * (bwd ? kBwdBlocks : fwd_blocks(p->flags != 0 ? 2 : 4)) / ceil_div(p->C, kChannels), 1);
 }
 
-ConvParams fill(const cawn_conv_params *p, const int64_t *offsets, bool bwd)
+ConvParams fill(const cawn_conv_params *p, const void *x, const int64_t *offsets, bool bwd)
 {
     ConvParams P = {};
     P.seq = {reinterpret_cast<const long long *>(offsets), p->L, offsets != nullptr ? p->rows : (int64_t)p->B * p->L, p->B};
@@ -390,7 +390,8 @@ ConvParams fill(const cawn_conv_params *p, const int64_t *offsets, bool bwd)
     P.tiles = most(ceil_div(p->L, P.rows * kWalks), 1);
     P.all_tiles = P.tiles * p->B;
     P.silu = p->act == CAWN_CONV_ACT_SILU;
-    P.x_whole = P.x_stride % kWord == 0;
+    P.x = x;
+    P.x_whole = P.x_stride % kWord == 0 && begins_on(x, p->flags != 0 ? 8 : 16);
     P.c_whole = p->C % kWord == 0;
     return P;
 }
@@ -433,9 +434,9 @@ extern "C" int cawn_short_conv_fwd(const cawn_conv_params *params, const void *x
     if (rc == CAWN_OK) rc = check_offsets(offsets, params->B, params->L, params->rows);
     if (rc != CAWN_OK) return rc;
     if (weight == nullptr || (params->L > 0 && (x == nullptr || y == nullptr))) return CAWN_ERR_NULL_POINTER;
-    if (!all_aligned16(x, weight, bias, state_in, y, state_out)) return CAWN_ERR_MISALIGNED;
-    ConvParams P = fill(params, offsets, false);
-    P.x = x; P.w = weight; P.b = bias; P.state_in = state_in; P.y = y; P.state_out = state_out;
+    if (!all_aligned16(weight, bias, state_in, y, state_out) || !elements_aligned(params->flags, x)) return CAWN_ERR_MISALIGNED;
+    ConvParams P = fill(params, x, offsets, false);
+    P.w = weight; P.b = bias; P.state_in = state_in; P.y = y; P.state_out = state_out;
     if (params->L == 1 && offsets == nullptr && ceil_div(params->B, kTokens) <= 65535)
         return status_of(launch<true>(params->flags != 0 ? pick_step<bf16>(params->K) : pick_step<float>(params->K),
                                       dim3((unsigned)ceil_div(P.words, kConvThreads), (unsigned)ceil_div(params->B, kTokens)), dim3(kConvThreads), 0,
@@ -466,12 +467,12 @@ extern "C" int cawn_short_conv_bwd(const cawn_conv_params *params, const void *x
     const bool sums = grad_weight != nullptr || grad_bias != nullptr;
     if (weight == nullptr || (params->L > 0 && (x == nullptr || grad_y == nullptr || grad_x == nullptr)) || (sums && workspace == nullptr))
         return CAWN_ERR_NULL_POINTER;
-    if (!all_aligned16(x, weight, bias, state_in, grad_y, grad_state_out, grad_x, grad_weight, grad_bias, grad_state_in, workspace))
+    if (!all_aligned16(weight, bias, state_in, grad_y, grad_state_out, grad_x, grad_weight, grad_bias, grad_state_in, workspace) || !elements_aligned(params->flags, x))
         return CAWN_ERR_MISALIGNED;
-    ConvParams P = fill(params, offsets, true);
+    ConvParams P = fill(params, x, offsets, true);
     const int64_t want = room(params, true), blocks = P.all_tiles < want ? P.all_tiles : want, cols = (int64_t)params->C * (params->K + 1);
     if (sums && workspace_bytes < (size_t)blocks * cols * sizeof(float)) return CAWN_ERR_WORKSPACE_TOO_SMALL;
-    P.x = x; P.w = weight; P.b = bias; P.state_in = state_in; P.gy = grad_y; P.gstate_out = grad_state_out;
+    P.w = weight; P.b = bias; P.state_in = state_in; P.gy = grad_y; P.gstate_out = grad_state_out;
     P.gx = grad_x; P.gstate_in = grad_state_in; P.part = sums ? static_cast<float *>(workspace) : nullptr;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     rc = status_of(launch<true>(pick(params, P, true), dim3((unsigned)blocks, (unsigned)ceil_div(P.words, kLanes)), dim3(kConvThreads), 0, st, P));

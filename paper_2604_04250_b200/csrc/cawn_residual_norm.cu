@@ -339,9 +339,9 @@ extern "C" int cawn_residual_norm_fwd(const cawn_residual_norm_params *params, c
     if (!e4m3 && scales != nullptr) return CAWN_ERR_INVALID_ARG;
     if (params->N == 0) return CAWN_OK;
     if (x == nullptr || y == nullptr || (e4m3 && scales == nullptr)) return CAWN_ERR_NULL_POINTER;
-    if (!all_aligned16(x, residual, weight, sum_out, y, scales)) return CAWN_ERR_MISALIGNED;
+    if (!all_aligned16(residual, weight, sum_out, y, scales) || !elements_aligned(params->flags, x)) return CAWN_ERR_MISALIGNED;
     ResidualNormParams P = fill(params);
-    P.x = x; P.residual = residual; P.w = weight; P.sum_out = sum_out; P.y = y; P.scales = scales;
+    P.x = x; P.x_whole = P.x_whole && begins_on(x, 16); P.residual = residual; P.w = weight; P.sum_out = sum_out; P.y = y; P.scales = scales;
     const Team t = team_of(params->M);
     return status_of(launch<true>(e4m3 ? pick<1>(params, P, t) : pick<0>(params, P, t), dim3((unsigned)ceil_div(P.N, kNormBlock / t.size)), dim3(kNormBlock), 0,
                                   static_cast<cudaStream_t>(cuda_stream), P));

@@ -86,7 +86,7 @@ void cut(SelectiveParams &P, const cawn_scan_params *p, bool bwd)
     P.per = most(ceil_div(ceil_div(p->L, P.S), kTile), 1) * kTile;
 }
 
-SelectiveParams fill(const cawn_scan_params *p, const int64_t *offsets, const void *b, const void *c)
+SelectiveParams fill(const cawn_scan_params *p, const int64_t *offsets, const void *x, const void *dt, const void *z, const void *b, const void *c)
 {
     SelectiveParams P = {};
     const int per = p->flags != 0 ? 8 : 4;
@@ -97,22 +97,18 @@ SelectiveParams fill(const cawn_scan_params *p, const int64_t *offsets, const vo
     P.xs = stride(p->x_stride, p->D); P.dts = stride(p->dt_stride, p->D); P.zs = stride(p->z_stride, p->D);
     P.bs = stride(p->b_stride, (int64_t)p->G * p->N); P.cs = stride(p->c_stride, (int64_t)p->G * p->N);
     const bool eights = P.Dg % 8 == 0;          // a block's channels begin on a word
-    P.whole_x = eights && P.xs % per == 0; P.whole_dt = eights && P.dts % per == 0; P.whole_z = eights && P.zs % per == 0;
+    P.x = x; P.dt = dt; P.z = z; P.bm = b; P.cm = c;
+    P.whole_x = eights && P.xs % per == 0 && begins_on(x, 16);
+    P.whole_dt = eights && P.dts % per == 0 && begins_on(dt, 16);
+    P.whole_z = eights && P.zs % per == 0 && begins_on(z, 16);
     P.whole_d = eights && p->D % per == 0;
-    const uintptr_t quad = p->flags != 0 ? 7 : 15;
-    P.whole_b = p->N % 4 == 0 && P.bs % 4 == 0 && (reinterpret_cast<uintptr_t>(b) & quad) == 0;
-    P.whole_c = p->N % 4 == 0 && P.cs % 4 == 0 && (reinterpret_cast<uintptr_t>(c) & quad) == 0;
+    const uintptr_t quad = p->flags != 0 ? 8 : 16;
+    P.whole_b = p->N % 4 == 0 && P.bs % 4 == 0 && begins_on(b, quad);
+    P.whole_c = p->N % 4 == 0 && P.cs % 4 == 0 && begins_on(c, quad);
     P.whole = P.whole_x && P.whole_dt && P.whole_z && P.whole_d && P.whole_b && P.whole_c;
     P.softplus = p->softplus;
     P.param_cols = param_cols(p);
     return P;
-}
-
-// B and C may begin anywhere in a row of theirs: at an element.
-bool elements_aligned(const cawn_scan_params *p, const void *b, const void *c)
-{
-    const uintptr_t mask = p->flags != 0 ? 1 : 3;
-    return ((reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c)) & mask) == 0;
 }
 
 }  // namespace
@@ -151,15 +147,15 @@ extern "C" int cawn_selective_scan_fwd(const cawn_scan_params *params, const voi
     if (rc == CAWN_OK) rc = check_offsets(offsets, params->B, params->L, params->rows);
     if (rc != CAWN_OK) return rc;
     if (A == nullptr || (params->L > 0 && (x == nullptr || dt == nullptr || B == nullptr || C == nullptr || y == nullptr))) return CAWN_ERR_NULL_POINTER;
-    if (!all_aligned16(x, dt, A, skip, dt_bias, z, state_in, y, state_out, checkpoints, workspace) || !elements_aligned(params, B, C))
+    if (!all_aligned16(A, skip, dt_bias, state_in, y, state_out, checkpoints, workspace) || !elements_aligned(params->flags, x, dt, z, B, C))
         return CAWN_ERR_MISALIGNED;
-    SelectiveParams P = fill(params, offsets, B, C);
+    SelectiveParams P = fill(params, offsets, x, dt, z, B, C);
     cut(P, params, false);
     Carver c = {static_cast<unsigned char *>(workspace)};
     carve_segments(c, P, params, false, false);
     if (c.used > 0 && workspace == nullptr) return CAWN_ERR_NULL_POINTER;
     if (c.used > workspace_bytes) return CAWN_ERR_WORKSPACE_TOO_SMALL;
-    P.x = x; P.dt = dt; P.A = A; P.bm = B; P.cm = C; P.skip = skip; P.dt_bias = dt_bias; P.z = z;
+    P.A = A; P.skip = skip; P.dt_bias = dt_bias;
     P.state_in = state_in; P.y = y; P.state_out = state_out; P.checkpoints = checkpoints;
     const Shape s = shape_of(params->N);
     const bool half = params->flags != 0;
@@ -177,9 +173,9 @@ extern "C" int cawn_selective_scan_step(const cawn_scan_params *params, const vo
     if (rc == CAWN_OK) rc = check_offsets(nullptr, params->B, params->L, params->rows);
     if (rc != CAWN_OK) return rc;
     if (A == nullptr || (params->L > 0 && (x == nullptr || dt == nullptr || B == nullptr || C == nullptr || y == nullptr))) return CAWN_ERR_NULL_POINTER;
-    if (!all_aligned16(x, dt, A, skip, dt_bias, z, state_in, y, state_out) || !elements_aligned(params, B, C)) return CAWN_ERR_MISALIGNED;
-    SelectiveParams P = fill(params, nullptr, B, C);
-    P.x = x; P.dt = dt; P.A = A; P.bm = B; P.cm = C; P.skip = skip; P.dt_bias = dt_bias; P.z = z;
+    if (!all_aligned16(A, skip, dt_bias, state_in, y, state_out) || !elements_aligned(params->flags, x, dt, z, B, C)) return CAWN_ERR_MISALIGNED;
+    SelectiveParams P = fill(params, nullptr, x, dt, z, B, C);
+    P.A = A; P.skip = skip; P.dt_bias = dt_bias;
     P.state_in = state_in; P.y = y; P.state_out = state_out;
     return launch_selective_step(P, params->flags != 0, static_cast<cudaStream_t>(cuda_stream));
 }
@@ -200,14 +196,14 @@ extern "C" int cawn_selective_scan_bwd(const cawn_scan_params *params, const voi
     if (params->L > 0 && (x == nullptr || dt == nullptr || B == nullptr || C == nullptr || grad_y == nullptr || grad_x == nullptr || grad_dt == nullptr ||
                           grad_B == nullptr || grad_C == nullptr || (z != nullptr && grad_z == nullptr)))
         return CAWN_ERR_NULL_POINTER;
-    if (!all_aligned16(x, dt, A, skip, dt_bias, z, state_in, checkpoints, grad_y, grad_state_out, grad_x, grad_dt, grad_A, grad_B, grad_C, grad_skip,
-                       grad_dt_bias, grad_z, grad_state_in, workspace) || !elements_aligned(params, B, C))
+    if (!all_aligned16(A, skip, dt_bias, state_in, checkpoints, grad_y, grad_state_out, grad_x, grad_dt, grad_A, grad_B, grad_C, grad_skip,
+                       grad_dt_bias, grad_z, grad_state_in, workspace) || !elements_aligned(params->flags, x, dt, z, B, C))
         return CAWN_ERR_MISALIGNED;
-    SelectiveParams P = fill(params, offsets, B, C);
+    SelectiveParams P = fill(params, offsets, x, dt, z, B, C);
     Carver c = {static_cast<unsigned char *>(workspace)};
     cut(P, params, true);
     carve_bwd(c, P, params, false);
-    P.x = x; P.dt = dt; P.A = A; P.bm = B; P.cm = C; P.skip = skip; P.dt_bias = dt_bias; P.z = z; P.state_in = state_in;
+    P.A = A; P.skip = skip; P.dt_bias = dt_bias; P.state_in = state_in;
     const Shape s = shape_of(params->N);
     const bool half = params->flags != 0, again = checkpoints == nullptr && params->L > 0;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

@@ -183,6 +183,14 @@ inline int check_offsets(const int64_t *offsets, int64_t B, int64_t L, int64_t r
     return (reinterpret_cast<uintptr_t>(offsets) & 7) != 0 ? CAWN_ERR_MISALIGNED : CAWN_OK;
 }
 
+// Slices may begin at any element; whole words are read where rows begin on `bytes`.
+template <class... P> inline bool elements_aligned(uint32_t flags, P... p)
+{
+    const uintptr_t mask = flags != 0 ? 1 : 3;
+    return (((reinterpret_cast<uintptr_t>(p) & mask) == 0) && ...);
+}
+inline bool begins_on(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
 inline int64_t most(int64_t a, int64_t b) { return a > b ? a : b; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 

@@ -10,7 +10,7 @@ import torch
 
 from delta_ref import close as close64
 from paper_2604_04250_b200 import binding as cb
-from selective_ref import flags_of, residual_norm, to_e4m3
+from selective_ref import flags_of, residual_norm, slices, to_e4m3
 
 pytestmark = pytest.mark.gpu
 TOL = {torch.float32: 1e-6, torch.bfloat16: 2.0 ** -9}
@@ -125,6 +125,11 @@ def test_in_place_strides_and_absent_arrays():
             wide[:, :M] = c["x"]
             y2 = torch.empty_like(y)
             cb.cawn_residual_norm_fwd(params(N, M, kind, x_stride=M + pad), wide[:, :M], y2, residual=c["residual"], weight=c["weight"])
+            assert torch.equal(y2, y)
+        for pad in (8, 3):                      # the middle of wider rows
+            x = slices(d["x"], pad)
+            y2 = torch.empty_like(y)
+            cb.cawn_residual_norm_fwd(params(N, M, kind, x_stride=M + 2 * pad), x, y2, residual=c["residual"], weight=c["weight"])
             assert torch.equal(y2, y)
         y3 = torch.empty_like(y)
         cb.cawn_residual_norm_fwd(params(N, M, kind), c["x"], y3)

@@ -134,7 +134,7 @@ def test_packed(D, N, G, saved, lengths, first, behind, dtype):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("absent", [("z",), ("skip", "dt_bias"), ("state_in",), ("z", "skip", "dt_bias", "state_in")])
-@pytest.mark.parametrize("pad", [0, 8, 24])
+@pytest.mark.parametrize("pad", [0, 8, 24, 4, 3, 1])
 def test_slices_and_absent_arrays(pad, absent, dtype):
     check([0, 40, 80], 48, 16, 1, dtype, pad=pad, absent=absent)
 
@@ -178,9 +178,10 @@ def test_longer_sequences_than_said_and_offsets_outside():
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("D, N, G", [(40, 16, 1), (7, 5, 1), (64, 64, 2), (33, 24, 1), (16, 1, 1), (20, 37, 2)])
-def test_tokens_one_by_one(D, N, G, dtype):
+@pytest.mark.parametrize("B", [3, 5])
+def test_tokens_one_by_one(B, D, N, G, dtype):
     """Single tokens with the states in place, several at a time, and the whole sequence: against the definition each."""
-    B, L = 3, 12
+    L = 12
     offsets = [i * L for i in range(B + 1)]
     d, c = case(offsets, D, N, G, dtype, seed=D + N)
     w = {n: t.double() for n, t in d.items()}
@@ -195,10 +196,32 @@ def test_tokens_one_by_one(D, N, G, dtype):
             parts.append(y)
         close(torch.cat(parts, 1).view(B * L, D), want, TOL[dtype], "y")
         close(state, want_state, FLOAT, "state")
+    for pad in (1, 8):                              # slices, whose strides the params name
+        s = {n: slices(d[n].flatten(1), pad) for n in DENSE}
+        prm = cb.make_scan_params(B, L, D, N, G, True, flags_of(dtype), *(s[n].stride(0) for n in ("x", "dt", "z", "B", "C")))
+        y, state = torch.empty(B * L, D, dtype=dtype, device="cuda"), c["state_in"].clone()
+        cb.cawn_selective_scan_step(prm, s["x"], s["dt"], c["A"], s["B"], s["C"], y, skip=c["skip"], dt_bias=c["dt_bias"], z=s["z"], state_in=state, state_out=state)
+        close(y, want, TOL[dtype], "y of slices")
+        close(state, want_state, FLOAT, "state of slices")
     y = torch.empty(B * L, D, dtype=dtype, device="cuda")
     cb.cawn_selective_scan_step(cb.make_scan_params(B, L, D, N, G, flags=flags_of(dtype)), c["x"], c["dt"], c["A"], c["B"], c["C"], y)
     want, _ = selective_scan(*(w[n] for n in ("x", "dt", "A", "B", "C")), None, None, None, torch.zeros(B, D, N, dtype=torch.double), offsets, L)
     close(y, want, TOL[dtype], "y from no state")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B, D, N", [(70, 300, 16), (61, 1100, 5), (40, 512, 24), (33, 5000, 2), (66, 130, 64)])
+def test_single_tokens_of_a_batch(B, D, N, dtype):
+    """Enough of them that a thread takes four sequences, the last of which may be fewer."""
+    offsets = list(range(B + 1))
+    d, c = case(offsets, D, N, 1, dtype, seed=B)
+    w = {n: t.double() for n, t in d.items()}
+    want, want_state = selective_scan(*(w[n] for n in LEAVES), offsets, 1)
+    y, state = torch.empty(B, D, dtype=dtype, device="cuda"), c["state_in"].clone()
+    cb.cawn_selective_scan_step(cb.make_scan_params(B, 1, D, N, flags=flags_of(dtype)), c["x"], c["dt"], c["A"], c["B"], c["C"], y, skip=c["skip"], dt_bias=c["dt_bias"],
+                                z=c["z"], state_in=state, state_out=state)
+    close(y, want, TOL[dtype], "y")
+    close(state, want_state, FLOAT, "state")
 
 
 def test_state_in_place_and_prompts_in_pieces():

@@ -100,21 +100,8 @@ def test_packed(C, K, lengths, first, behind, dtype):
 @pytest.mark.parametrize("pad", [8, 3, 1])
 @pytest.mark.parametrize("bias, state", [(True, False), (False, True), (False, False)])
 def test_slices_and_absent_arrays(bias, state, pad, dtype):
-    if (pad * torch.finfo(dtype).bits) % 128 == 0:
-        check([0, 70, 140], 48, 4, dtype, "silu", pad=pad, bias=bias, state=state)
-        return
-    # a pointer off the 16-byte boundary is refused; the same stride from an aligned start is not
-    d, c = case([0, 70, 140], 48, 4, dtype, pad=pad)
-    prm = params([0, 70, 140], 48, 4, "silu", dtype, False, 140, pad=pad)
-    y = torch.empty(140, 48, dtype=dtype, device="cuda")
-    with pytest.raises(cb.CawnError, match="align"):
-        cb.cawn_short_conv_fwd(prm, c["x"], c["weight"], y)
-    wide = torch.zeros(140, 48 + 2 * pad, dtype=dtype, device="cuda")
-    wide[:, :48] = d["x"].cuda()
-    cb.cawn_short_conv_fwd(prm, wide[:, :48], c["weight"], y, bias=c["bias"] if bias else None, state_in=c["state_in"] if state else None)
-    want, _ = short_conv(d["x"].double(), d["weight"].double(), d["bias"].double() if bias else None, True,
-                         d["state_in"].double() if state else torch.zeros(2, 3, 48, dtype=torch.double), [0, 70, 140], 70)
-    close(y, want, TOL[dtype])
+    check([0, 70, 140], 48, 4, dtype, "silu", pad=pad, bias=bias, state=state)
+    check([0, 1, 2, 3], 48, 4, dtype, "silu", pad=pad, bias=bias, state=state)
 
 
 def test_longer_sequences_than_said_and_offsets_outside():

@@ -104,8 +104,9 @@ def test_conv(entry_point):
     assert entry_point(conv(rows=300), offsets=A + 4) == cb.CAWN_ERR_MISALIGNED
     for name in ("x", "weight"):
         assert entry_point(conv(), **{name: None}) == cb.CAWN_ERR_NULL_POINTER, name
-    for name in ("x", "weight", "bias", "state_in"):
+    for name in ("weight", "bias", "state_in"):
         assert entry_point(conv(), **{name: A + 8}) == cb.CAWN_ERR_MISALIGNED, name
+    assert entry_point(conv(), x=A + 2) == cb.CAWN_ERR_MISALIGNED and entry_point(conv(flags=BF16), x=A + 1) == cb.CAWN_ERR_MISALIGNED
 
 
 def test_conv_pointers_of_one_direction():
@@ -126,11 +127,12 @@ def test_scan(entry_point):
         assert entry_point(scan(**kw)) == cb.CAWN_ERR_UNSUPPORTED, kw
     for name in ("x", "dt", "A", "B", "C"):
         assert entry_point(scan(), **{name: None}) == cb.CAWN_ERR_NULL_POINTER, name
-    for name in ("x", "dt", "A", "skip", "dt_bias", "z", "state_in"):
-        assert entry_point(scan(), **{name: A + 8, **({"grad_z": A} if name == "z" and entry_point is scan_bwd else {})}) == cb.CAWN_ERR_MISALIGNED, name
-    for name in ("B", "C"):         # aligned to their elements is enough
-        assert entry_point(scan(), **{name: A + 2}) == cb.CAWN_ERR_MISALIGNED, name
-        assert entry_point(scan(flags=BF16), **{name: A + 1}) == cb.CAWN_ERR_MISALIGNED, name
+    for name in ("A", "skip", "dt_bias", "state_in"):
+        assert entry_point(scan(), **{name: A + 8}) == cb.CAWN_ERR_MISALIGNED, name
+    for name in ("x", "dt", "z", "B", "C"):         # aligned to their elements is enough
+        more = {"grad_z": A} if name == "z" and entry_point is scan_bwd else {}
+        assert entry_point(scan(), **{name: A + 2, **more}) == cb.CAWN_ERR_MISALIGNED, name
+        assert entry_point(scan(flags=BF16), **{name: A + 1, **more}) == cb.CAWN_ERR_MISALIGNED, name
     if entry_point is not scan_step:
         assert entry_point(scan(), offsets=A) == cb.CAWN_ERR_INVALID_ARG
         assert entry_point(scan(rows=300), offsets=A + 4) == cb.CAWN_ERR_MISALIGNED
@@ -170,8 +172,9 @@ def test_residual_norm():
     assert norm_fwd(norm(), scales=A) == cb.CAWN_ERR_INVALID_ARG and norm_fwd(norm(out=1)) == cb.CAWN_ERR_NULL_POINTER
     for name in ("x", "y"):
         assert norm_fwd(norm(), **{name: None}) == cb.CAWN_ERR_NULL_POINTER
-    for name in ("x", "y", "residual", "weight", "sum_out"):
+    for name in ("y", "residual", "weight", "sum_out"):
         assert norm_fwd(norm(), **{name: A + 4}) == cb.CAWN_ERR_MISALIGNED, name
+    assert norm_fwd(norm(), x=A + 2) == cb.CAWN_ERR_MISALIGNED
     assert norm_fwd(norm(out=1), scales=A + 4) == cb.CAWN_ERR_MISALIGNED
     for name in ("sum", "grad_y"):
         assert norm_bwd(norm(), **{name: None}) == cb.CAWN_ERR_NULL_POINTER
