@@ -178,12 +178,15 @@ template <int NS> __device__ __forceinline__ void fold_segment(f32x2 (&h)[NS / 2
 // First checkpoint of a sequence: those of two sequences never meet, whatever the lengths.
 __device__ __forceinline__ long long checkpoint_of(const Span &s, int b) { return s.begin / kTile + b; }
 
+// Blocks that a multiprocessor holds at once: the forward's by the registers it is given, the backward's (of the walk) by shared
+// memory and 255 registers.
+constexpr int resident_blocks(int nl, int ns, bool bwd) { return nl == 2 ? (bwd ? 4 : 6) : nl == 4 ? 4 : ns == 4 ? 2 : 1; }
+
 using SelectiveKernel = void (*)(SelectiveParams);
 struct Shape {
     int nl, ns, cd;
     int threads() const { return 32 * (nl / cd + stage_warps(nl * ns)); }
-    // blocks that a multiprocessor holds, by the registers and the shared memory that the kernels take
-    int resident(bool bwd) const { return nl == 2 ? (bwd ? 8 : 6) : nl == 4 ? 4 : ns == 4 ? 2 : 1; }
+    int resident(bool bwd) const { return resident_blocks(nl, ns, bwd); }
 };
 inline Shape shape_of(int N) { return N <= 8 ? Shape{2, 4, 2} : N <= 16 ? Shape{4, 4, 2} : N <= 32 ? Shape{8, 4, 2} : Shape{8, 8, 1}; }
 // A launch for the shape: CALL(NL, NS, CD).

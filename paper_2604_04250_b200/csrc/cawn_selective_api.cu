@@ -28,23 +28,27 @@ int check(const cawn_scan_params *p)
 int64_t blocks_of(const cawn_scan_params *p) { return p->G * ceil_div(p->D / p->G, kScanChannels); }
 int64_t rows_of(const cawn_scan_params *p) { return p->rows > 0 ? p->rows : (int64_t)p->B * p->L; }
 
-// Segments of the time axis, none shorter than 256 tokens.  Where the blocks of whole sequences leave multiprocessors idle, as many
+// Segments of the time axis, none shorter than 128 tokens.  Where the blocks of whole sequences leave multiprocessors idle, as many
 // segments as are resident at once; otherwise none: 2048 tokens of 16 states take 107 us with one block a multiprocessor, 168 with
 // two and 240 with four, and the pass before it half as much again, so that two segments of 148 blocks do not pay and four do.
-// The backward's pass is a fifth of its walk: two segments pay as soon as they are resident.
-constexpr int kShortest = 256, kMostSegments = 64;
+// The backward's pass is a fifth of its walk: two segments pay as soon as they are resident.  Packed sequences count by their
+// rows, as so many of the longest one's length: blocks of short ones end early.
+constexpr int kShortest = 128, kMostSegments = 64;
 int64_t slots_of(const cawn_scan_params *p, bool bwd) { return (int64_t)sm_count() * shape_of(p->N).resident(bwd); }
 int64_t segments_of(const cawn_scan_params *p, bool bwd)
 {
-    const int64_t whole = p->B * blocks_of(p), cut = slots_of(p, bwd) / whole, longest = most(p->L / kShortest, 1);
+    const int64_t sequences = p->rows > 0 && p->L > 0 && p->rows / p->L < p->B ? p->rows / p->L + 1 : p->B;
+    const int64_t whole = sequences * blocks_of(p), cut = slots_of(p, bwd) / whole, longest = most(p->L / kShortest, 1);
     if (cut < 2 || (!bwd && whole > sm_count())) return 1;
     const int64_t s = cut < longest ? cut : longest;
     return s < kMostSegments ? s : kMostSegments;
 }
-// The most sequences x segments of any call with up to this B and L.
+// The most sequences x segments of any call with up to this B, L and rows.
 int64_t most_segments(const cawn_scan_params *p, bool bwd)
 {
-    const int64_t cut = most(slots_of(p, bwd) / blocks_of(p), p->B), whole = p->B * most(p->L / kShortest, 1);
+    const int64_t each = most(slots_of(p, bwd) / blocks_of(p), 1), longest = most(p->L / kShortest, 1), of_one = each < longest ? each : longest;
+    if (p->rows > 0) return p->B * (of_one < kMostSegments ? of_one : kMostSegments);       // one of them may have nearly all rows
+    const int64_t cut = most(each, p->B), whole = p->B * longest;
     return cut < whole ? cut : whole;
 }
 

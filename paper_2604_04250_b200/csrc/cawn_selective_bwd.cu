@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
 
 // A segment's own gradient at its start, and its sum of d: for the segments in front of it.
 template <class T, int NL, int NS, int CD>
-__global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads) selective_bwd_summary_kernel(const SelectiveParams P)
+__global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(NL, NS, false)) selective_bwd_summary_kernel(const SelectiveParams P)
 {
     follow_previous();
     using At = Place<NL, NS, CD>;

@@ -19,7 +19,7 @@ template <class T, int NL, int NS, int CD, bool SUMMARY> struct FwdShared {
 };
 
 template <class T, int NL, int NS, int CD, bool SUMMARY, bool WHOLE>
-__global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, NL == 4 ? 4 : 1) selective_fwd_kernel(const SelectiveParams P)
+__global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(NL, NS, false)) selective_fwd_kernel(const SelectiveParams P)
 {
     follow_previous();
     using At = Place<NL, NS, CD>;
