@@ -636,9 +636,10 @@ CAWN_API int cawn_short_conv_bwd(const cawn_conv_params *params, const void *x, 
  * *_stride elements apart (0 = dense), so that they may be slices of projections, and need only be aligned to
  * their elements (whole words are read where rows begin on 16 bytes; of B and C, on four elements).
  * Precision.  Everything is computed in float; results are rounded once to their type.  The
- * backward's sums over channels (gradients of B and C) take terms of 22 bits of mantissa.
+ * backward's sums over channels (gradients of B and C) take terms of 16 bits of mantissa with bfloat16
+ * storage, of 22 with float storage.
  * Non-finite values stay in their sequence and in the channels of their group; gradients of B and C may
- * also be spoilt in the 8 tokens (N > 32: 4), counted from the sequence's first, around one.
+ * also be spoilt in the eight tokens, counted from the sequence's first, around one.
  * Limits: N <= 64, G <= 65535.
  */
 typedef struct cawn_scan_params {
@@ -664,7 +665,8 @@ enum {
     CAWN_SCAN_CHECKPOINTS = 3    /* size of the checkpoints that a forward can leave for it        */
 };
 
-/* Host-only size query; enough for every B, L and rows up to the given ones. */
+/* Host-only size query; enough for every B, L and rows up to the given ones, packed where they are packed
+ * and dense where they are dense. */
 CAWN_API int cawn_selective_scan_workspace_bytes(const cawn_scan_params *params, int op, size_t *bytes);
 
 /*

@@ -21,7 +21,7 @@ int check(const cawn_scan_params *p)
     for (int64_t stride : {p->x_stride, p->dt_stride, p->z_stride, p->b_stride, p->c_stride}) wide = most(wide, stride);
     const double rows = p->rows > 0 ? (double)p->rows : (double)p->B * (double)p->L;
     if (rows * (double)wide > 1.0e17) return CAWN_ERR_UNSUPPORTED;
-    if ((double)p->B * (p->D / kScanChannels + p->G) * 16.0 > 2.0e9 || (double)p->B * ((double)p->L / 32 + 1) > 2.0e9) return CAWN_ERR_UNSUPPORTED;
+    if ((double)p->B * (p->D / kScanChannels + p->G) * 16.0 > 2.0e9 || (double)p->B * ((double)p->L / kTile + 1) > 2.0e9) return CAWN_ERR_UNSUPPORTED;
     return CAWN_OK;
 }
 

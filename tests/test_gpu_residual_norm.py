@@ -189,3 +189,20 @@ def test_gradient_against_differences():
     slope = (loss(1e-2) - loss(-1e-2)) / 2e-2
     want = (gr.norm() + gw.norm()).item()
     assert abs(slope - want) < 1e-3 * want
+
+
+def test_more_than_32_bits_of_elements():
+    N, M, dtype = 1_100_000, 2000, torch.bfloat16
+    x, s, y = torch.randn(N, M, device="cuda", dtype=dtype), None, None
+    assert x.numel() > 2 ** 31
+    s, y, scales = torch.empty_like(x), torch.empty(N, M, device="cuda", dtype=torch.uint8), torch.empty(N, 16, device="cuda")
+    prm = params(N, M, KINDS[1], out=cb.CAWN_NORM_OUT_E4M3, scale_block=128)
+    cb.cawn_residual_norm_fwd(prm, x, y, residual=x, sum_out=s, scales=scales)
+    some = params(100, M, KINDS[1], out=cb.CAWN_NORM_OUT_E4M3, scale_block=128)
+    s2, y2, scales2 = torch.empty_like(s[:100]), torch.empty_like(y[:100]), torch.empty_like(scales[:100])
+    cb.cawn_residual_norm_fwd(some, x[-100:], y2, residual=x[-100:], sum_out=s2, scales=scales2)
+    assert torch.equal(s2, s[-100:]) and torch.equal(y2, y[-100:]) and torch.equal(scales2, scales[-100:])
+    g, g2 = torch.empty_like(x), torch.empty_like(s2)
+    cb.cawn_residual_norm_bwd(prm, s, x, grad_residual=g)
+    cb.cawn_residual_norm_bwd(some, s2, x[-100:], grad_residual=g2)
+    assert torch.equal(g2, g[-100:])

@@ -396,3 +396,30 @@ def test_gradient_against_differences():
     for n in LEAVES:
         slope, want = (loss(n, 1e-2) - loss(n, -1e-2)) / 2e-2, g[n].norm().item()
         assert abs(slope - want) < 2e-3 * want, n
+
+
+def test_more_than_32_bits_of_elements():
+    """2.2e9 elements an array: the second half alone, from the first half's state, gives the same as the whole call."""
+    L, D, N = 1_100_000, 2000, 2
+    half, dtype = 560_000, torch.bfloat16
+    rng = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(L, D, generator=rng, device="cuda", dtype=dtype)
+    dt = torch.full((L, D), -2.0, device="cuda", dtype=dtype)
+    dt[:, ::3] = -5.0
+    BC = torch.randn(L, 2 * N, generator=rng, device="cuda", dtype=dtype)
+    A = -torch.rand(D, N, generator=rng, device="cuda") - 0.1
+    y, so = torch.empty(L, D, device="cuda", dtype=dtype), torch.empty(1, D, N, device="cuda")
+    assert x.numel() > 2 ** 31
+
+    def forward(a, e, y, state_in, state_out):
+        prm = cb.make_scan_params(1, e - a, D, N, flags=flags_of(dtype), b_stride=2 * N, c_stride=2 * N)
+        cb.cawn_selective_scan_fwd(prm, x[a:e], dt[a:e], A, BC[a:e, :N], BC[a:e, N:], y[a:e], cb.new_scan_workspace(prm, cb.CAWN_SCAN_FWD), state_in=state_in, state_out=state_out)
+
+    forward(0, L, y, None, so)
+    mid, end = torch.empty_like(so), torch.empty_like(so)
+    z = torch.empty_like(y)
+    forward(0, half, z, None, mid)
+    forward(half, L, z, mid, end)
+    close(end, so.cpu(), FLOAT, "state")
+    close(z[-2000:], y[-2000:].cpu(), 2.0 ** -9, "the last rows")
+    close(z[half - 1000:half + 1000], y[half - 1000:half + 1000].cpu(), 2.0 ** -9, "the rows around the middle")

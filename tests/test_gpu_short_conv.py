@@ -212,3 +212,19 @@ def test_gradient_against_differences():
     slope = (loss(1e-2) - loss(-1e-2)) / 2e-2
     want = sum(t.norm().item() for t in g.values())
     assert abs(slope - want) < 1e-3 * want
+
+
+def test_more_than_32_bits_of_elements():
+    L, C, dtype = 1_100_000, 2000, torch.bfloat16
+    x = torch.randn(L, C, device="cuda", dtype=dtype)
+    w, b, y, gx = torch.randn(C, 4, device="cuda"), torch.randn(C, device="cuda"), torch.empty_like(x), torch.empty_like(x)
+    prm = cb.make_conv_params(1, L, C, 4, act=cb.CAWN_CONV_ACT_SILU, flags=flags_of(dtype))
+    assert x.numel() > 2 ** 31
+    cb.cawn_short_conv_fwd(prm, x, w, y, bias=b)
+    want, _ = short_conv(x[-203:].cpu().double(), w.cpu().double(), b.cpu().double(), True, torch.zeros(1, 3, C, dtype=torch.double), [0, 203], 203)
+    close(y[-200:], want[-200:], TOL[dtype])
+    cb.cawn_short_conv_bwd(prm, x, w, y, gx, bias=b)
+    tail, gt = x[-203:].contiguous(), torch.empty(203, C, device="cuda", dtype=dtype)
+    some = cb.make_conv_params(1, 203, C, 4, act=cb.CAWN_CONV_ACT_SILU, flags=flags_of(dtype))
+    cb.cawn_short_conv_bwd(some, tail, w, y[-203:].contiguous(), gt, bias=b)
+    assert torch.equal(gx[-200:], gt[-200:])
