@@ -4,11 +4,14 @@
 // y = (sum_n C_n h_n + skip x) silu(z).  B and C belong to a token and a group of channels.
 //
 // Layout of the work.  A block has 32 channels of one group and one sequence (or a segment of it) and walks its tokens in
-// tiles of 16.  A thread has CD neighbouring channels and NS states of each; NL lanes share a channel (N up to NL * NS).  In a
+// tiles of 16 (blocks of 16 channels would spread more evenly over the multiprocessors, but 8 x 2048 x 2048 x 16 then takes 311 us
+// instead of 234: each stages B and C for itself).  A thread has CD neighbouring channels and NS states of each; NL lanes share a channel (N up to NL * NS).  In a
 // warp lane bits 0-1 are channels, the next log2 NL bits the lane's states, the rest channels again.  A tile's (d, d x) and
 // rows of B and C are made floats once, in shared memory; the next tile is fetched while one is computed.  What a
 // thread reads there for a token is 8 bytes a channel and 8 a state, so two channels by four states (6 bytes a cell) and not one by
 // four (10): shared memory fills 128 bytes of registers a clock, and that was the bound.
+// Bound: a decay is an exponential a cell, and a multiprocessor takes 16 a clock: 119 us for 8 x 2048 x 2048 x 16, whose
+// arrays take 42 us of memory's time.
 // Few channels: the time axis is cut into segments that run side by side, behind a pass that finds each segment's own end
 // state and its sum of d (the decay over a segment is e^{A sum d}), so that every exponential is taken twice.
 #pragma once
@@ -28,7 +31,7 @@ struct SelectiveParams {
     float *part_bc, *part_param;                // backward: partial sums of a block's channels, of a block's tokens
     long long xs, dts, zs, bs, cs;              // elements between rows
     long long param_cols;                       // floats of a row of part_param, a multiple of 4
-    long long per;                              // tokens of a segment, a multiple of 32
+    long long per;                              // tokens of a segment, a multiple of kTile
     int D, N, G, Dg, blocks;                    // channels of a group, blocks of channels per group
     int S;                                      // segments
     int softplus, whole_x, whole_dt, whole_z, whole_d, whole_b, whole_c, whole;     // whole: all of them

@@ -14,6 +14,8 @@
 // lanes at once.  Operands: with bfloat16 storage the leading 8 and the next 8 bits of a term side by side (m16n8k16; the rest,
 // 2^-16 of a term, is less than a hundredth of the result's own rounding; with one operand of 11 bits, gradients of rows that a few
 // channels cancel in were off by twice their rounding); with float storage 11 and 11 bits in two products (m16n8k8).
+// Bound: the latency of those chains with eight warps a multiprocessor.  8 x 2048 x 1024 x 16 bfloat16 with the gate: walk 545 us
+// (issue 38%, shared memory 48%, exponentials 26%), the pass before its two segments 92, the sums of dB and dC 18.
 #include "cawn_selective.cuh"
 
 namespace cawn {

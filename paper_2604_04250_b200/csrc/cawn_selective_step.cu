@@ -13,7 +13,7 @@ constexpr int kStepThreads = 128;
 
 // NL lanes a channel; R sequences a thread.  With R = 4 a lane finds the step and the gate of one sequence and hands them to the
 // others, and their sums are scattered back to it, so that they are found once and not by each lane; A is shared
-// (256 sequences of 2048 channels of 16: R = 1 30 us, R = 4 without that 48).
+// (256 sequences of 2048 channels of 16, bfloat16: 16 us, memory's time 11; R = 1 30, R = 4 without the handing over 48).
 template <class T, int NL, int R, bool WHOLE>
 __global__ void __launch_bounds__(kStepThreads) selective_step_kernel(const SelectiveParams P)
 {
