@@ -29,8 +29,9 @@ int64_t blocks_of(const cawn_scan_params *p) { return p->G * ceil_div(p->D / p->
 int64_t rows_of(const cawn_scan_params *p) { return p->rows > 0 ? p->rows : (int64_t)p->B * p->L; }
 
 // Segments of the time axis, none shorter than 128 tokens.  Where the blocks of whole sequences leave multiprocessors idle, as many
-// segments as are resident at once; otherwise none: 2048 tokens of 16 states take 107 us with one block a multiprocessor, 168 with
-// two and 240 with four, and the pass before it half as much again, so that two segments of 148 blocks do not pay and four do.
+// segments as are resident at once; otherwise none: 2048 tokens of 16 states take 107 us with one block a multiprocessor, 127 with
+// two and 236 with four, and the pass before it half as much again (74 blocks: 107 us whole, 103 in two segments, 78 in four; 148
+// blocks of 32 states: 123 us whole, 160 in two).
 // The backward's pass is a fifth of its walk: two segments pay as soon as they are resident.  Packed sequences count by their
 // rows, as so many of the longest one's length: blocks of short ones end early.
 constexpr int kShortest = 128, kMostSegments = 64;
@@ -39,7 +40,7 @@ int64_t segments_of(const cawn_scan_params *p, bool bwd)
 {
     const int64_t sequences = p->rows > 0 && p->L > 0 && p->rows / p->L < p->B ? p->rows / p->L + 1 : p->B;
     const int64_t whole = sequences * blocks_of(p), cut = slots_of(p, bwd) / whole, longest = most(p->L / kShortest, 1);
-    if (cut < 2 || (!bwd && whole > sm_count())) return 1;
+    if (cut < (bwd ? 2 : 3) || (!bwd && whole > sm_count())) return 1;
     const int64_t s = cut < longest ? cut : longest;
     return s < kMostSegments ? s : kMostSegments;
 }

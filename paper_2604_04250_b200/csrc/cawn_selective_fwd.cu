@@ -20,8 +20,10 @@ template <class T, int NL, int NS, int CD, bool SUMMARY> struct FwdShared {
     Eight<T> words[SUMMARY ? 1 : 3][2][At::kWords][At::kStagers];       // x and z as a stager fetched them, until their tile is finished
 };
 
-template <class T, int NL, int NS, int CD, bool SUMMARY, bool WHOLE>
-__global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(NL, NS, false)) selective_fwd_kernel(const SelectiveParams P)
+// SPLIT: the finishing has warps of its own and the computing warps look four tokens ahead, not two.  For calls of so few blocks that
+// half of a multiprocessor's places are enough, and with them half of the registers: 8 x 2048 x 1024 x 16 in 127 instead of 160 us.
+template <class T, int NL, int NS, int CD, bool SUMMARY, bool WHOLE, bool SPLIT>
+__global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads + (SPLIT ? Place<NL, NS, CD>::kStagers : 0), resident_blocks(NL, NS, false) / (SPLIT ? 2 : 1)) selective_fwd_kernel(const SelectiveParams P)
 {
     follow_previous();
     using At = Place<NL, NS, CD>;
@@ -39,7 +41,7 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(N
 
     if (threadIdx.x >= At::kCompute) {
         if (!walks) return;
-        const int lane = threadIdx.x - At::kCompute, word = lane % 4 * 8;
+        const int lane = (threadIdx.x - At::kCompute) % At::kStagers, word = lane % 4 * 8;
         const T *x = static_cast<const T *>(P.x) + s.begin * P.xs + c0 + word, *dt = static_cast<const T *>(P.dt) + s.begin * P.dts + c0 + word;
         const T *z = P.z != nullptr && !SUMMARY && P.y != nullptr ? static_cast<const T *>(P.z) + s.begin * P.zs + c0 + word : nullptr;
         const T *bm = static_cast<const T *>(P.bm) + s.begin * P.bs + g * P.N, *cm = static_cast<const T *>(P.cm) + s.begin * P.cs + g * P.N;
@@ -96,13 +98,29 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(N
                 if (there && y != nullptr && t0 + r < end) store_eight(y + (t0 + r) * P.D, f, nch - word, WHOLE || P.whole_d);
             }
         };
+        int to = 0, kept = 0;           // buffers of the tile that is staged
+        auto finish_last_two = [&] {
+            const long long tiles = (end - begin + kTile - 1) / kTile;
+            if (tiles > 1) finish(begin + (tiles - 2) * kTile, to, kept == 2 ? 0 : kept + 1, true);
+            meet();
+            finish(begin + (tiles - 1) * kTile, to ^ 1, kept == 0 ? 2 : kept - 1, true);
+        };
+        if (SPLIT && threadIdx.x >= At::kCompute + At::kStagers) {
+            for (long long t0 = begin; t0 < end; t0 += kTile, to ^= 1, kept = kept == 2 ? 0 : kept + 1) {
+                finish(t0 - 2 * kTile, to, kept == 2 ? 0 : kept + 1, t0 >= begin + 2 * kTile);
+                meet();
+            }
+            finish_last_two();
+            return;
+        }
+        // Finished among the staging, or behind it: floats have no registers left for the first (8 x 2048 x 2368 x 8: 276 us, 205).
+        constexpr bool kEarly = sizeof(T) == 2;
         Raw next;
         fetch(next, begin);
-        int to = 0, kept = 0;           // buffers of the tile that is staged
         for (long long t0 = begin; t0 < end; t0 += kTile, to ^= 1, kept = kept == 2 ? 0 : kept + 1) {
             const Raw now = next;
             fetch(next, t0 + kTile);        // on its way while this tile is staged and the one before is computed
-            if constexpr (!SUMMARY) finish(t0 - 2 * kTile, to, kept == 2 ? 0 : kept + 1, t0 >= begin + 2 * kTile);
+            if constexpr (!SUMMARY && !SPLIT && kEarly) finish(t0 - 2 * kTile, to, kept == 2 ? 0 : kept + 1, t0 >= begin + 2 * kTile);
 #pragma unroll
             for (int i = 0; i < kWords; i++) {
                 const int r = lane / 4 + i * (At::kStagers / 4);
@@ -127,14 +145,11 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(N
                 *reinterpret_cast<float4 *>(&sh.bc[to][0][0][0] + (lane + i * At::kStagers) * 4) = now.b[i].get();
                 if (!SUMMARY) *reinterpret_cast<float4 *>(&sh.bc[to][1][0][0] + (lane + i * At::kStagers) * 4) = now.c[i].get();
             }
+            if constexpr (!SUMMARY && !SPLIT && !kEarly) finish(t0 - 2 * kTile, to, kept == 2 ? 0 : kept + 1, t0 >= begin + 2 * kTile);
             meet();             // the tile is there; the one before it is computed
         }
-        if constexpr (!SUMMARY) {       // the last two
-            const long long tiles = (end - begin + kTile - 1) / kTile;
-            if (tiles > 1) finish(begin + (tiles - 2) * kTile, to, kept == 2 ? 0 : kept + 1, true);
-            meet();
-            finish(begin + (tiles - 1) * kTile, to ^ 1, kept == 0 ? 2 : kept - 1, true);
-        }
+        if constexpr (SPLIT) meet();
+        else if constexpr (!SUMMARY) finish_last_two();
         return;
     }
 
@@ -182,15 +197,16 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(N
 #pragma unroll
             for (int j = 0; j < CD; j++) store_states<NS>(mark + j * P.N, h[j], n0, P.N, at.ch + j < nch);
         }
-        // two tokens' decays are found while the two before them move the states
-        f32x2 a[2][2][CD][NK], in[2][2][CD][NK];
+        // some tokens' decays are found while those before them move the states
+        constexpr int kSome = SPLIT ? 4 : 2;
+        f32x2 a[2][kSome][CD][NK], in[2][kSome][CD][NK];
         auto decays = [&](int u) {
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
+            for (int i = 0; i < kSome; i++) {
                 f32x2 B[NK];
                 float2 d[CD];
-                row_pairs<NS>(B, &sh.bc[buf][0][2 * u + i][n0]);
-                two_of<CD>(d, &sh.dd[buf][2 * u + i][slot]);
+                row_pairs<NS>(B, &sh.bc[buf][0][kSome * u + i][n0]);
+                two_of<CD>(d, &sh.dd[buf][kSome * u + i][slot]);
 #pragma unroll
                 for (int j = 0; j < CD; j++) {
 #pragma unroll
@@ -204,13 +220,13 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(N
         };
         decays(0);
 #pragma unroll
-        for (int u = 0; u < kTile / 2; u++) {
-            if (u + 1 < kTile / 2) decays(u + 1);
+        for (int u = 0; u < kTile / kSome; u++) {
+            if (u + 1 < kTile / kSome) decays(u + 1);
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
+            for (int i = 0; i < kSome; i++) {
                 f32x2 C[NK];
                 float v[CD];
-                if constexpr (!SUMMARY) row_pairs<NS>(C, &sh.bc[buf][1][2 * u + i][n0]);
+                if constexpr (!SUMMARY) row_pairs<NS>(C, &sh.bc[buf][1][kSome * u + i][n0]);
 #pragma unroll
                 for (int j = 0; j < CD; j++) {
                     f32x2 acc = 0ull;
@@ -221,7 +237,7 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(N
                     }
                     v[j] = sum_of(acc);
                 }
-                if constexpr (!SUMMARY) put_channels<CD>(&sh.out[buf][2 * u + i][at.nl * kRowFloats + at.ch], v);
+                if constexpr (!SUMMARY) put_channels<CD>(&sh.out[buf][kSome * u + i][at.nl * kRowFloats + at.ch], v);
             }
         }
     }
@@ -240,16 +256,25 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(N
     }
 }
 
-template <class T, bool SUMMARY, bool WHOLE, int NL, int NS, int CD> int run(const SelectiveParams &P, dim3 grid, cudaStream_t st)
+template <class T, bool SUMMARY, bool WHOLE, bool SPLIT, int NL, int NS, int CD> int run(const SelectiveParams &P, dim3 grid, cudaStream_t st)
 {
-    return launch_shared(selective_fwd_kernel<T, NL, NS, CD, SUMMARY, WHOLE>, grid, Place<NL, NS, CD>::kThreads, sizeof(FwdShared<T, NL, NS, CD, SUMMARY>), P, st);
+    using At = Place<NL, NS, CD>;
+    return launch_shared(selective_fwd_kernel<T, NL, NS, CD, SUMMARY, WHOLE, SPLIT>, grid, At::kThreads + (SPLIT ? At::kStagers : 0), sizeof(FwdShared<T, NL, NS, CD, SUMMARY>), P, st);
+}
+template <class T, bool SUMMARY, bool SPLIT> int run(const SelectiveParams &P, const Shape &s, dim3 grid, cudaStream_t st)
+{
+#define CAWN_CALL(NL, NS, CD)                                                                                  \
+    (P.whole ? run<T, SUMMARY, true, SPLIT && NS == 4, NL, NS, CD>(P, grid, st)                                \
+             : run<T, SUMMARY, false, SPLIT && NS == 4, NL, NS, CD>(P, grid, st))
+    return CAWN_BY_SHAPE(s, CAWN_CALL);
+#undef CAWN_CALL
 }
 template <class T, bool SUMMARY> int run(const SelectiveParams &P, const Shape &s, cudaStream_t st)
 {
     const dim3 grid((unsigned)(P.G * P.blocks * P.seq.B), (unsigned)(SUMMARY ? P.S - 1 : P.S));
-#define CAWN_CALL(NL, NS, CD) (P.whole ? run<T, SUMMARY, true, NL, NS, CD>(P, grid, st) : run<T, SUMMARY, false, NL, NS, CD>(P, grid, st))
-    return CAWN_BY_SHAPE(s, CAWN_CALL);
-#undef CAWN_CALL
+    const bool few = s.ns == 4 && (int64_t)grid.x * grid.y <= (int64_t)sm_count() * (s.resident(false) / 2);
+    if constexpr (!SUMMARY) return few ? run<T, false, true>(P, s, grid, st) : run<T, false, false>(P, s, grid, st);
+    else return run<T, true, false>(P, s, grid, st);
 }
 
 }  // namespace
