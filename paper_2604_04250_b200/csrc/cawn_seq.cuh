@@ -167,7 +167,7 @@ __device__ __forceinline__ f32x2 sigmoid_of(f32x2 v)
 __device__ __forceinline__ float silu_slope(float v, float sg) { return sg * fmaf(v, 1.f - sg, 1.f); }
 
 // Sums of `rows` partial rows of `cols` floats each, in double and in a fixed order, into up to three arrays that the
-// columns belong to one after the other (NULL: not wanted).  32 columns a block, 32 row lanes of two sums.
+// columns belong to one after the other (NULL: not wanted).
 struct PartialSums {
     const float *part;
     long long rows, cols;
