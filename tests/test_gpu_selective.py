@@ -114,6 +114,14 @@ def test_dense(B, L, D, N, G, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D, N, lengths", [(224, 8, 70 * (37,)), (221, 3, 71 * (34,)), (224, 16, 46 * (33,)), (221, 16, 46 * (50,)), (224, 16, 46 * (1,)), (200, 24, 26 * (49,)),
+                                           (203, 29, 26 * (17,)), (224, 16, 12 * (37, 0, 50, 16, 1)), (221, 13, 12 * (2, 33, 0, 47, 15)), (200, 32, 6 * (31, 0, 32, 5, 48))])
+def test_more_blocks_than_half_of_the_places(D, N, lengths, dtype):
+    """Calls that fill the device; those of few blocks have warps of their own for finishing."""
+    check(packed_offsets(lengths, 0), D, N, 1, dtype, packed=len(set(lengths)) > 1, seed=D + N)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("B, L, D, N", [(1, 700, 40, 16), (2, 1100, 24, 4), (1, 800, 16, 64), (1, 523, 33, 24), (1, 1030, 8, 8)])
 @pytest.mark.parametrize("saved", [True, False])
 def test_segments(B, L, D, N, saved, dtype):
