@@ -70,8 +70,9 @@ void carve_segments(Carver &c, SelectiveParams &P, const cawn_scan_params *p, bo
 {
     const int64_t pieces = sized ? most_segments(p, bwd) : p->B * segments_of(p, bwd);
     if (pieces <= (sized ? 1 : p->B)) return;
-    P.seg_state = c.floats(pieces * p->D * p->N);
-    P.seg_time = c.floats(pieces * p->D);
+    const int64_t ends = bwd ? 2 * pieces : pieces;         // the backward may have one per half
+    P.seg_state = c.floats(ends * p->D * p->N);
+    P.seg_time = c.floats(ends * p->D);
     if (!bwd) P.first = c.floats((int64_t)p->B * p->D * p->N);
 }
 // Partial sums of grad_A, grad_skip and grad_dt_bias: rows that begin on 16 bytes.
@@ -89,6 +90,7 @@ void cut(SelectiveParams &P, const cawn_scan_params *p, bool bwd)
 {
     P.S = (int)segments_of(p, bwd);
     P.per = most(ceil_div(ceil_div(p->L, P.S), kTile), 1) * kTile;
+    P.halves = bwd && 2 * (P.S - 1) * p->B * blocks_of(p) <= slots_of(p, false) ? 2 : 1;
 }
 
 SelectiveParams fill(const cawn_scan_params *p, const int64_t *offsets, const void *x, const void *dt, const void *z, const void *b, const void *c)

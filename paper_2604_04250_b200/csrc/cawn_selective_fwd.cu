@@ -183,8 +183,7 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads + (SPLIT ? Place<N
             } else {
                 const long long segment = (long long)b * (P.S - 1) * P.D + c;
                 load_states<NS>(h[j], P.seg_state + segment * P.N, n0, P.N, in);
-#pragma unroll 4
-                for (int i = 1; i < seg; i++) fold_segment<NS>(h[j], P, A2[j], segment + (long long)i * P.D, n0, in);
+                fold_segments<NS>(h[j], P, A2[j], segment + P.D, P.D, seg - 1, n0, in);
             }
         }
     }

@@ -132,6 +132,14 @@ def test_segments(B, L, D, N, saved, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lengths, G, N", [((600,), 148, 9), ((600, 3, 0, 40), 90, 12), ((523,), 70, 16), ((1040,), 37, 5), ((385, 385), 30, 20)])
+@pytest.mark.parametrize("saved", [True, False])
+def test_segments_of_many_blocks(lengths, G, N, saved, dtype):
+    """A block a channel: segments that fill the device, so that the backward's pass before them takes them whole."""
+    check(packed_offsets(lengths, 0), G, N, G, dtype, packed=len(lengths) > 1, seed=G, saved=saved)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("lengths, first, behind", [((5, 0, 1, 70, 2), 0, 0), ((0, 0), 3, 4), ((130, 1, 64), 2, 5), ((1,), 0, 1), ((0, 90, 0, 33, 16), 0, 0),
                                                     ((600, 0, 300, 5), 7, 3)])
 @pytest.mark.parametrize("D, N, G, saved", [(40, 16, 1, True), (26, 5, 2, False)])
