@@ -32,7 +32,7 @@ int64_t rows_of(const cawn_scan_params *p) { return p->rows > 0 ? p->rows : (int
 // segments as are resident at once; otherwise none: 2048 tokens of 16 states take 107 us with one block a multiprocessor, 127 with
 // two and 236 with four, and the pass before it half as much again (74 blocks: 107 us whole, 103 in two segments, 78 in four; 148
 // blocks of 32 states: 123 us whole, 160 in two).
-// The backward's pass is a fifth of its walk: two segments pay as soon as they are resident.  Packed sequences count by their
+// The backward's pass is an eighth of its walk: two segments pay as soon as they are resident.  Packed sequences count by their
 // rows, as so many of the longest one's length: blocks of short ones end early.
 constexpr int kShortest = 128, kMostSegments = 64;
 int64_t slots_of(const cawn_scan_params *p, bool bwd) { return (int64_t)sm_count() * shape_of(p->N).resident(bwd); }

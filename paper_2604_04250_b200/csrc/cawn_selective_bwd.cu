@@ -15,7 +15,7 @@
 // 2^-16 of a term, is less than a hundredth of the result's own rounding; with one operand of 11 bits, gradients of rows that a few
 // channels cancel in were off by twice their rounding); with float storage 11 and 11 bits in two products (m16n8k8).
 // Bound: the latency of those chains with eight warps a multiprocessor.  8 x 2048 x 1024 x 16 bfloat16 with the gate: walk 545 us
-// (issue 38%, shared memory 48%, exponentials 26%), the pass before its two segments 92, the sums of dB and dC 18.
+// (issue 38%, shared memory 48%, exponentials 26%), the pass before its two segments 65, the sums of dB and dC 17.
 #include "cawn_selective.cuh"
 
 namespace cawn {
