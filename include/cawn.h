@@ -635,9 +635,7 @@ CAWN_API int cawn_short_conv_bwd(const cawn_conv_params *params, const void *x, 
  * (usually negative); skip, dt_bias [D] float; states [B, D, N] float.  Rows of x, dt, z, B and C lie
  * *_stride elements apart (0 = dense), so that they may be slices of projections, and need only be aligned to
  * their elements (whole words are read where rows begin on 16 bytes; of B and C, on four elements).
- * Precision.  Everything is computed in float; results are rounded once to their type.  The
- * backward's sums over channels (gradients of B and C) take terms of 16 bits of mantissa with bfloat16
- * storage, of 22 with float storage.
+ * Precision.  Everything is computed in float; results are rounded once to their type.
  * Non-finite values stay in their sequence and in the channels of their group; gradients of B and C may
  * also be spoilt in the eight tokens, counted from the sequence's first, around one.
  * Limits: N <= 64, G <= 65535.

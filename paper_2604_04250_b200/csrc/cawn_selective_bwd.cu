@@ -11,9 +11,8 @@
 // shared memory, and when half a tile is done all threads add them up, finish and store.
 // Sums over channels (dB, dC) go through the tensor cores: the left factor is a selection, ones in row t (and 8 + t) and
 // zeros elsewhere, so that one product adds four lanes' lam d x to row t and their dy' h to row 8 + t, for eight groups of
-// lanes at once.  Operands: with bfloat16 storage the leading 8 and the next 8 bits of a term side by side (m16n8k16; the rest,
-// 2^-16 of a term, is less than a hundredth of the result's own rounding; with one operand of 11 bits, gradients of rows that a few
-// channels cancel in were off by twice their rounding); with float storage 11 and 11 bits in two products (m16n8k8).
+// lanes at once.  Operands: a term in three bfloat16 parts of eight bits, which hold all of a float's 24; two of them in one product
+// (m16n8k16), the third in another (m16n8k8).  (With two parts, 16 bits, results in bfloat16 were off by 2e-4 of their norm.)
 // Bound: the latency of those chains with eight warps a multiprocessor.  8 x 2048 x 1024 x 16 bfloat16 with the gate: walk 545 us
 // (issue 38%, shared memory 48%, exponentials 26%), the pass before its two segments 65, the sums of dB and dC 17.
 #include "cawn_selective.cuh"
@@ -21,24 +20,26 @@
 namespace cawn {
 namespace {
 
-// d: rows t and 8 + t gain u and v of four lanes; `one`: what a lane holds of the selection of t.
-template <class T> __device__ __forceinline__ void sum_channels(float (&d)[4], unsigned one, float u, float v);
-template <> __device__ __forceinline__ void sum_channels<bf16>(float (&d)[4], unsigned one, float u, float v)
+// Rows t and 8 + t of d0 gain u.x and v.x of four lanes, those of d1 u.y and v.y; `here`: this lane's row of the selection is t.
+__device__ __forceinline__ void sum_channels(float (&d0)[4], float (&d1)[4], bool here, f32x2 u, f32x2 v)
 {
-    // upper half of a register: the leading bits; lower half: those of what is left
-    const unsigned a = __float_as_uint(u) & 0xffff0000u, b = __float_as_uint(v) & 0xffff0000u;
-    const unsigned x = __byte_perm(__float_as_uint(u - __uint_as_float(a)), a, 0x7632), y = __byte_perm(__float_as_uint(v - __uint_as_float(b)), b, 0x7632);
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%5,%4}, {%6,%7}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(one), "r"(0u), "r"(x), "r"(y));
-}
-template <> __device__ __forceinline__ void sum_channels<float>(float (&d)[4], unsigned one, float u, float v)
-{
-    const unsigned a = __float_as_uint(u) & 0xffffe000u, b = __float_as_uint(v) & 0xffffe000u;
-    const unsigned x = __float_as_uint(u - __uint_as_float(a)) & 0xffffe000u, y = __float_as_uint(v - __uint_as_float(b)) & 0xffffe000u;
-    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%5,%4}, {%6,%7}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(one), "r"(0u), "r"(a), "r"(b));
-    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%5,%4}, {%6,%7}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(one), "r"(0u), "r"(x), "r"(y));
+    // What a term is beyond its first eight bits, and beyond those the next eight: what is left then has no more than eight.
+    auto lead = [](f32x2 a) { return a & 0xffff0000ffff0000ull; };
+    auto rest = [&](f32x2 a) { return fma2(lead(a), twice(-1.f), a); };
+    const f32x2 ur = rest(u), vr = rest(v), ul = rest(ur), vl = rest(vr);
+    const unsigned both = here ? 0x3f803f80u : 0u, low = both & 0xffffu, high = both & 0xffff0000u;
+    auto add = [&](float (&d)[4], float u0, float v0, float u1, float v1, float u2, float v2) {
+        // upper half of a register: the leading bits; lower half: the next ones
+        const unsigned x = __byte_perm(__float_as_uint(u1), __float_as_uint(u0), 0x7632), y = __byte_perm(__float_as_uint(v1), __float_as_uint(v0), 0x7632);
+        const unsigned z = __byte_perm(__float_as_uint(u2), __float_as_uint(v2), 0x7632);           // the last bits: u's, and v's above
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%5,%4}, {%6,%7}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(both), "r"(0u), "r"(x), "r"(y));
+        asm("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(low), "r"(high), "r"(z));
+    };
+    const float2 a = halves(u), b = halves(v), ar = halves(ur), br = halves(vr), al = halves(ul), bl = halves(vl);
+    add(d0, a.x, b.x, ar.x, br.x, al.x, bl.x);
+    add(d1, a.y, b.y, ar.y, br.y, al.y, bl.y);
 }
 
 // Where a thread is: as in the forward's computing warps, and for staging and finishing.
@@ -342,13 +343,9 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
                     }
                     put_channels<CD>(&sh.parts[0][u * TS + i][at.nl * kRowFloats + at.ch], flow);
                     put_channels<CD>(&sh.parts[1][u * TS + i][at.nl * kRowFloats + at.ch], drift);
-                    const unsigned one = lane >> 2 == u * TS + i ? (sizeof(T) == 2 ? 0x3f803f80u : 0x3f800000u) : 0u;
+                    const bool here = lane >> 2 == u * TS + i;
 #pragma unroll
-                    for (int k = 0; k < NK; k++) {
-                        const float2 p = halves(gb[k]), q = halves(gc[k]);
-                        sum_channels<T>(sums[2 * k], one, p.x, q.x);
-                        sum_channels<T>(sums[2 * k + 1], one, p.y, q.y);
-                    }
+                    for (int k = 0; k < NK; k++) sum_channels(sums[2 * k], sums[2 * k + 1], here, gb[k], gc[k]);
                 }
             }
             // rows of a selection's result: eight tokens; columns: the groups of lanes that a lane / 4 names

@@ -439,3 +439,28 @@ def test_more_than_32_bits_of_elements():
     close(end, so.cpu(), FLOAT, "state")
     close(z[-2000:], y[-2000:].cpu(), 2.0 ** -9, "the last rows")
     close(z[half - 1000:half + 1000], y[half - 1000:half + 1000].cpu(), 2.0 ** -9, "the rows around the middle")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N", [4, 16, 32, 64])
+@pytest.mark.parametrize("other", [1, 2, 7, 31, 45])
+def test_terms_of_sums_over_channels_keep_their_bits(other, N, dtype):
+    """Channel 0 has steps of s + k 2^-23, another one steps of s = 1.3333332539 (all 24 bits in use) and the opposite x; every other channel
+    has x = 0, B = C = 1 and decays are 0.  So the terms of dB and dC are these steps with a sign (lam = dy' = 1: dB = sum d x, and h = d x:
+    dC = sum d x), and their sums k 2^-23: whole numbers of up to 8 bits times a power of two, which every storage holds and sums of 24
+    bits give exactly in any order."""
+    D, L = 64, 21
+    offsets = [0, L]
+    for k in (1, 3, 77, 255, 0x540000):
+        d, c = case(offsets, D, N, 1, dtype, softplus=False)
+        sign = 1.0 - 2.0 * (torch.arange(L) % 2)
+        new = {"x": torch.zeros(L, D), "dt": torch.ones(L, D), "A": torch.full((D, N), -200.0), "B": torch.ones(L, 1, N), "C": torch.ones(L, 1, N),
+               "dt_bias": torch.zeros(D), "grad_y": torch.zeros(L, D), "grad_state_out": torch.zeros(1, D, N)}
+        new["x"][:, 0], new["x"][:, other] = sign, -sign
+        new["grad_y"][:, 0] = new["grad_y"][:, other] = 1.0
+        new["dt_bias"][0], new["dt_bias"][other] = (0x2AAAAA + k) * 2.0 ** -23, 0x2AAAAA * 2.0 ** -23
+        c.update({n: t.to(c[n].dtype).cuda() for n, t in new.items()})
+        g = backward(params(offsets, D, N, 1, dtype, softplus=False, z=False), c, absent=("z", "state_in"))
+        want = (sign * k * 2.0 ** -23)[:, None, None].expand(L, 1, N).to(dtype)
+        assert torch.equal(g["B"].cpu(), want), (k, (g["B"].cpu().float() - want).abs().max())
+        assert torch.equal(g["C"].cpu(), want), (k, (g["C"].cpu().float() - want).abs().max())
