@@ -197,15 +197,17 @@ template <int NS> __device__ __forceinline__ void fold_segments(f32x2 (&h)[NS / 
 // First checkpoint of a sequence: those of two sequences never meet, whatever the lengths.
 __device__ __forceinline__ long long checkpoint_of(const Span &s, int b) { return s.begin / kTile + b; }
 
-// Blocks that a multiprocessor holds at once: the forward's by the registers it is given, the backward's (of the walk) by shared
-// memory and 255 registers.
-constexpr int resident_blocks(int nl, int ns, bool bwd) { return nl == 2 ? (bwd ? 4 : 6) : nl == 4 ? 4 : ns == 4 ? 2 : 1; }
+// Blocks that a multiprocessor holds at once: the forward's by the registers it is given, the backward's (of the walk, of which the
+// type of the arrays decides too) by shared memory and 255 registers, as is asserted there.
+constexpr int resident_blocks(int nl, int ns) { return nl == 2 ? 6 : nl == 4 ? 4 : ns == 4 ? 2 : 1; }
+constexpr int resident_walks(int nl, int ns, bool half) { return nl == 2 ? (half ? 5 : 4) : nl == 4 ? (half ? 4 : 3) : ns == 4 ? 2 : 1; }
 
 using SelectiveKernel = void (*)(SelectiveParams);
 struct Shape {
     int nl, ns, cd;
     int threads() const { return 32 * (nl / cd + stage_warps(nl * ns)); }
-    int resident(bool bwd) const { return resident_blocks(nl, ns, bwd); }
+    int resident() const { return resident_blocks(nl, ns); }
+    int resident_bwd(bool half) const { return resident_walks(nl, ns, half); }
 };
 inline Shape shape_of(int N) { return N <= 8 ? Shape{2, 4, 2} : N <= 16 ? Shape{4, 4, 2} : N <= 32 ? Shape{8, 4, 2} : Shape{8, 8, 1}; }
 // A launch for the shape: CALL(NL, NS, CD).

@@ -32,14 +32,23 @@ int64_t rows_of(const cawn_scan_params *p) { return p->rows > 0 ? p->rows : (int
 // segments as are resident at once; otherwise none: 2048 tokens of 16 states take 107 us with one block a multiprocessor, 127 with
 // two and 236 with four, and the pass before it half as much again (74 blocks: 107 us whole, 103 in two segments, 78 in four; 148
 // blocks of 32 states: 123 us whole, 160 in two).
-// The backward's pass is an eighth of its walk: two segments pay as soon as they are resident.  Packed sequences count by their
-// rows, as so many of the longest one's length: blocks of short ones end early.
+// The backward's pass is an eighth of its walk: two segments pay as soon as they are resident, with 9 to 16 states up to seven tenths of
+// the places (1024 tokens of 16 states, float: 288 blocks 669 us whole, 575 in two, 352 blocks 692 and 687, 384 blocks 694 and 742; bfloat16:
+// 416 blocks 709 and 679, 448 blocks 729 and 781; with 8 states, float, 320 blocks 669 and 687, with 24 224 blocks 742 and 790).
+// Packed sequences count by their rows, as so many of the longest one's length: blocks of short ones end early.
 constexpr int kShortest = 128, kMostSegments = 64;
-int64_t slots_of(const cawn_scan_params *p, bool bwd) { return (int64_t)sm_count() * shape_of(p->N).resident(bwd); }
+int64_t slots_of(const cawn_scan_params *p, bool bwd)
+{
+    const Shape s = shape_of(p->N);
+    return (int64_t)sm_count() * (bwd ? s.resident_bwd(p->flags != 0) : s.resident());
+}
+// The most blocks that the backward takes in two segments each.
+int64_t most_in_two(const cawn_scan_params *p) { return shape_of(p->N).nl == 4 ? slots_of(p, true) * 7 / 10 : slots_of(p, true) / 2; }
 int64_t segments_of(const cawn_scan_params *p, bool bwd)
 {
     const int64_t sequences = p->rows > 0 && p->L > 0 && p->rows / p->L < p->B ? p->rows / p->L + 1 : p->B;
-    const int64_t whole = sequences * blocks_of(p), cut = slots_of(p, bwd) / whole, longest = most(p->L / kShortest, 1);
+    const int64_t whole = sequences * blocks_of(p), room = slots_of(p, bwd) / whole, longest = most(p->L / kShortest, 1);
+    const int64_t cut = bwd && whole <= most_in_two(p) ? most(room, 2) : room;
     if (cut < (bwd ? 2 : 3) || (!bwd && whole > sm_count())) return 1;
     const int64_t s = cut < longest ? cut : longest;
     return s < kMostSegments ? s : kMostSegments;
@@ -47,7 +56,8 @@ int64_t segments_of(const cawn_scan_params *p, bool bwd)
 // The most sequences x segments of any call with up to this B, L and rows.
 int64_t most_segments(const cawn_scan_params *p, bool bwd)
 {
-    const int64_t each = most(slots_of(p, bwd) / blocks_of(p), 1), longest = most(p->L / kShortest, 1), of_one = each < longest ? each : longest;
+    const int64_t room = most(slots_of(p, bwd) / blocks_of(p), 1), longest = most(p->L / kShortest, 1);
+    const int64_t each = bwd ? most(room, 2 * (most_in_two(p) / blocks_of(p))) : room, of_one = each < longest ? each : longest;
     if (p->rows > 0) return p->B * (of_one < kMostSegments ? of_one : kMostSegments);       // one of them may have nearly all rows
     const int64_t cut = most(each, p->B), whole = p->B * longest;
     return cut < whole ? cut : whole;

@@ -397,7 +397,7 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
 // A segment's own gradient at its start, and its sum of d: for the segments in front of it.  In halves where there is room for as many
 // blocks at once, since there is one segment less than in the walk (8 x 2048 x 1024 x 16: 90 us whole, 65 in halves).
 template <class T, int NL, int NS, int CD>
-__global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(NL, NS, false)) selective_bwd_summary_kernel(const SelectiveParams P)
+__global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(NL, NS)) selective_bwd_summary_kernel(const SelectiveParams P)
 {
     follow_previous();
     using At = Place<NL, NS, CD>;
@@ -549,6 +549,9 @@ __global__ void __launch_bounds__(128) selective_bc_kernel(const SelectiveParams
 
 template <class T, bool GATE, int NL, int NS, int CD> int run(const SelectiveParams &P, dim3 grid, cudaStream_t st)
 {
+    // 228 KB of shared memory, of which a block takes 1 KB more than it asks for, and 65,536 registers, 256 a thread
+    constexpr int shared = 228 * 1024 / (int)(sizeof(BwdShared<T, NL, NS, CD>) + 1024), registers = 65536 / (256 * Walker<NL, NS, CD>::kThreads);
+    static_assert(resident_walks(NL, NS, sizeof(T) == 2) == (shared < registers ? shared : registers), "the time axis is cut for this many blocks");
     return launch_shared(selective_bwd_kernel<T, NL, NS, CD, GATE>, grid, Walker<NL, NS, CD>::kThreads, sizeof(BwdShared<T, NL, NS, CD>), P, st);
 }
 template <class T, bool GATE> int run(const SelectiveParams &P, const Shape &s, dim3 grid, cudaStream_t st)

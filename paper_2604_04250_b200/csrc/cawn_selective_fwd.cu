@@ -23,7 +23,7 @@ template <class T, int NL, int NS, int CD, bool SUMMARY> struct FwdShared {
 // SPLIT: the finishing has warps of its own and the computing warps look four tokens ahead, not two.  For calls of so few blocks that
 // half of a multiprocessor's places are enough, and with them half of the registers: 8 x 2048 x 1024 x 16 in 127 instead of 160 us.
 template <class T, int NL, int NS, int CD, bool SUMMARY, bool WHOLE, bool SPLIT>
-__global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads + (SPLIT ? Place<NL, NS, CD>::kStagers : 0), resident_blocks(NL, NS, false) / (SPLIT ? 2 : 1)) selective_fwd_kernel(const SelectiveParams P)
+__global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads + (SPLIT ? Place<NL, NS, CD>::kStagers : 0), resident_blocks(NL, NS) / (SPLIT ? 2 : 1)) selective_fwd_kernel(const SelectiveParams P)
 {
     follow_previous();
     using At = Place<NL, NS, CD>;
@@ -272,7 +272,7 @@ template <class T, bool SUMMARY, bool SPLIT> int run(const SelectiveParams &P, c
 template <class T, bool SUMMARY> int run(const SelectiveParams &P, const Shape &s, cudaStream_t st)
 {
     const dim3 grid((unsigned)(P.G * P.blocks * P.seq.B), (unsigned)(SUMMARY ? P.S - 1 : P.S));
-    const bool few = s.ns == 4 && (int64_t)grid.x * grid.y <= (int64_t)sm_count() * (s.resident(false) / 2);
+    const bool few = s.ns == 4 && (int64_t)grid.x * grid.y <= (int64_t)sm_count() * (s.resident() / 2);
     if constexpr (!SUMMARY) return few ? run<T, false, true>(P, s, grid, st) : run<T, false, false>(P, s, grid, st);
     else return run<T, true, false>(P, s, grid, st);
 }

@@ -262,3 +262,12 @@ def test_every_dense_array_of_every_call_is_looked_at():
             kw.update(params=prm, **{name: halves})
             with pytest.raises(ValueError, match=name):
                 f(**kw)
+
+
+@pytest.mark.parametrize("N, fewer", [(5, True), (8, True), (9, True), (16, True), (24, False), (64, False)])
+def test_the_backward_is_cut_for_the_blocks_that_are_resident(N, fewer):
+    """A block of the walk keeps fetched rows as they are stored, so with up to 16 states fewer blocks of float are resident than of bfloat16
+    (4 and 5, with 9 or more states 3 and 4): fewer segments, whose states and sums are the workspace of this call but for parts
+    that are float in both."""
+    of = lambda flags: cb.cawn_selective_scan_workspace_bytes(scan(B=1, L=8192, D=60, N=N, G=60, flags=flags), cb.CAWN_SCAN_BWD)
+    assert (of(0) < of(BF16)) if fewer else (of(0) == of(BF16))
