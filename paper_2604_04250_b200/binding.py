@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcawn.so")
@@ -409,7 +410,6 @@ def _dense(names, *arrays):
 def _yes():
     return True
 
-
 def _check_rows(name, x, width, row):
     """x's elements, in order, have to be rows of `width` neighbours that start `row` apart (the shape may be any that
     has whole rows: [B, L, H, D], [B, L, H * D], [B * L, H * D])."""
@@ -562,31 +562,74 @@ def cawn_dropout(params, x, y, residual=None, offset_device=None, stream=None):
 
 # ---- operators of a selective state space layer
 
+# The params' fields as they lie (filling a Structure field by field takes twice as long, a fifth of what checking a call does).
+_CONV, _SCAN, _RESIDUAL_NORM = struct.Struct("@IiqiiiIIIqq"), struct.Struct("@IiqiiiiIIqqqqqq"), struct.Struct("@IiqfiiiIIq")
+
+
 def make_conv_params(B, L, C, K, act=CAWN_CONV_ACT_NONE, flags=0, x_stride=0, rows=0):
-    return cawn_conv_params(ctypes.sizeof(cawn_conv_params), B, L, C, K, act, flags, (0, 0), x_stride, rows)
+    try:
+        return cawn_conv_params.from_buffer_copy(_CONV.pack(_CONV.size, B, L, C, K, act, flags, 0, 0, x_stride, rows))
+    except struct.error:                # a value that does not fit
+        return cawn_conv_params(_CONV.size, B, L, C, K, act, flags, (0, 0), x_stride, rows)
 
 
-def _sequence_rows(params, offsets, arrays):
-    """The arrays of a call, (name, tensor, width, stride) each, have to be the rows that the params say.  One row has no step to the
-    next, so torch gives that dimension any stride."""
-    if offsets is None:
-        rows = params.B * params.L
-    else:
-        rows = params.rows
-        _dense("offsets", offsets)
-        if hasattr(offsets, "dtype") and (str(offsets.dtype) not in ("torch.int64", "int64") or tuple(offsets.shape) != (params.B + 1,)):
-            raise ValueError(f"offsets: {params.B + 1} values of int64 are needed, got {tuple(offsets.shape)} of {offsets.dtype}")
-    if rows < 1:
-        return
-    for name, x, width, stride in arrays:
-        if x is None:
-            continue
-        try:                            # the usual case at once
-            if (stride == 0 or stride == width or rows == 1) and x.is_contiguous() and x.numel() == rows * width:
-                continue
-        except AttributeError:          # not a tensor (a numpy array): its owner's business
-            continue
+_types = None
+
+
+def _torch_types():
+    """torch's float32 and bfloat16, asked for once."""
+    global _types
+    import torch
+    _types = torch.float32, torch.bfloat16
+    return _types
+
+
+def _array(late, name, x, n, kind):
+    """Pointer of an array that has to be dense, of one type, and to hold n elements at least.  A layout is refused at once, a type or size
+    after all layouts have been looked at: what is wrong goes into `late`."""
+    if x is None:
+        return None
+    try:
+        if x.dtype is kind and x.numel() >= n and x.is_contiguous():
+            return x.data_ptr()
+        if not x.is_contiguous():
+            raise ValueError(f"{name}: strides {tuple(x.stride())} of shape {tuple(x.shape)}, it has to be dense")
+    except AttributeError:              # not a tensor (a numpy array): its owner's business
+        return _dp(x)
+    late.append(f"{name}: {tuple(x.shape)} of {x.dtype}, but {n} elements of {kind} are needed")
+
+
+def _rows(name, x, rows, width, stride, kind):
+    """Pointer of an array that has to be so many rows of one type, `stride` (0: width) elements apart.  One row has no step to the next,
+    so torch gives that dimension any stride."""
+    if x is None:
+        return None
+    try:                                # the usual cases at once: whole arrays, and slices of a projection
+        if x.dtype is kind and (x.is_contiguous() and x.numel() == rows * width if stride == 0 or stride == width
+                                else x.stride() == (stride, 1) and x.shape == (rows, width)):
+            return x.data_ptr()
+        x.is_contiguous
+    except AttributeError:
+        return _dp(x)
+    if rows > 0:
+        if x.dtype is not kind:
+            raise ValueError(f"{name}: {x.dtype}, but the flags say {kind}")
         _check_sequence_rows(name, x, rows, width, stride or width)
+    return x.data_ptr()
+
+
+def _refuse(late):
+    raise ValueError(late[0])
+
+
+def _row_count(params, offsets):
+    """Rows that the arrays of a call have."""
+    if offsets is None:
+        return params.B * params.L
+    _dense("offsets", offsets)
+    if hasattr(offsets, "dtype") and (str(offsets.dtype) not in ("torch.int64", "int64") or tuple(offsets.shape) != (params.B + 1,)):
+        raise ValueError(f"offsets: {params.B + 1} values of int64 are needed, got {tuple(offsets.shape)} of {offsets.dtype}")
+    return params.rows
 
 
 def _check_sequence_rows(name, x, rows, width, row):
@@ -613,26 +656,36 @@ def new_conv_workspace(params, device="cuda"):
 
 
 def cawn_short_conv_fwd(params, x, weight, y, bias=None, state_in=None, state_out=None, offsets=None, stream=None):
-    _dense("weight y bias state_in state_out", weight, y, bias, state_in, state_out)
-    _sequence_rows(params, offsets, (("x_stride", x, params.C, params.x_stride), ("y", y, params.C, 0)))
-    _check(lib().cawn_short_conv_fwd(ctypes.byref(params), _dp(x), _dp(weight), _dp(bias), _dp(state_in), _dp(offsets), _dp(y),
-                                     _dp(state_out), _stream(stream)), "cawn_short_conv_fwd")
+    C, K, rows, types, late = params.C, params.K, _row_count(params, offsets), _types or _torch_types(), []
+    f, kind, history = types[0], types[params.flags != 0], params.B * (K - 1) * C
+    arrays = (_rows("x_stride", x, rows, C, params.x_stride, kind), _array(late, "weight", weight, C * K, f), _array(late, "bias", bias, C, f),
+              _array(late, "state_in", state_in, history, f), _dp(offsets), _rows("y", y, rows, C, 0, kind), _array(late, "state_out", state_out, history, f))
+    if late:
+        _refuse(late)
+    _check(lib().cawn_short_conv_fwd(ctypes.byref(params), *arrays, _stream(stream)), "cawn_short_conv_fwd")
 
 
 def cawn_short_conv_bwd(params, x, weight, grad_y, grad_x, workspace=None, bias=None, state_in=None, offsets=None, grad_state_out=None,
                         grad_weight=None, grad_bias=None, grad_state_in=None, stream=None):
-    _dense("weight grad_y grad_x bias state_in grad_state_out grad_weight grad_bias grad_state_in",
-           weight, grad_y, grad_x, bias, state_in, grad_state_out, grad_weight, grad_bias, grad_state_in)
-    _sequence_rows(params, offsets, (("x_stride", x, params.C, params.x_stride), ("grad_y", grad_y, params.C, 0), ("grad_x", grad_x, params.C, 0)))
+    C, K, rows, types, late = params.C, params.K, _row_count(params, offsets), _types or _torch_types(), []
+    f, kind, history = types[0], types[params.flags != 0], params.B * (K - 1) * C
+    arrays = (_rows("x_stride", x, rows, C, params.x_stride, kind), _array(late, "weight", weight, C * K, f), _array(late, "bias", bias, C, f),
+              _array(late, "state_in", state_in, history, f), _dp(offsets), _rows("grad_y", grad_y, rows, C, 0, kind),
+              _array(late, "grad_state_out", grad_state_out, history, f), _rows("grad_x", grad_x, rows, C, 0, kind),
+              _array(late, "grad_weight", grad_weight, C * K, f), _array(late, "grad_bias", grad_bias, C, f),
+              _array(late, "grad_state_in", grad_state_in, history, f))
+    if late:
+        _refuse(late)
     n = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().cawn_short_conv_bwd(
-        ctypes.byref(params), _dp(x), _dp(weight), _dp(bias), _dp(state_in), _dp(offsets), _dp(grad_y), _dp(grad_state_out), _dp(grad_x),
-        _dp(grad_weight), _dp(grad_bias), _dp(grad_state_in), _dp(workspace), n, _stream(stream)), "cawn_short_conv_bwd")
+    _check(lib().cawn_short_conv_bwd(ctypes.byref(params), *arrays, _dp(workspace), n, _stream(stream)), "cawn_short_conv_bwd")
 
 
 def make_scan_params(B, L, D, N, G=1, softplus=True, flags=0, x_stride=0, dt_stride=0, z_stride=0, b_stride=0, c_stride=0, rows=0):
-    return cawn_scan_params(ctypes.sizeof(cawn_scan_params), B, L, D, N, G, int(softplus), flags, 0, x_stride, dt_stride, z_stride, b_stride,
-                            c_stride, rows)
+    values = _SCAN.size, B, L, D, N, G, int(softplus), flags, 0, x_stride, dt_stride, z_stride, b_stride, c_stride, rows
+    try:
+        return cawn_scan_params.from_buffer_copy(_SCAN.pack(*values))
+    except struct.error:
+        return cawn_scan_params(*values)
 
 
 def cawn_selective_scan_workspace_bytes(params, op):
@@ -648,14 +701,17 @@ def new_scan_workspace(params, op, device="cuda"):
 
 
 def _scan_rows(params, offsets, x, dt, z, B, C, *more):
-    D, bc = params.D, params.G * params.N
-    _sequence_rows(params, offsets, (("x_stride", x, D, params.x_stride), ("dt_stride", dt, D, params.dt_stride), ("z_stride", z, D, params.z_stride),
-                                     ("b_stride", B, bc, params.b_stride), ("c_stride", C, bc, params.c_stride), *more))
+    """Pointers of the rows of a call, `more`, (name, tensor, width) each, being dense."""
+    rows, D, bc, kind = _row_count(params, offsets), params.D, params.G * params.N, (_types or _torch_types())[params.flags != 0]
+    return (_rows("x_stride", x, rows, D, params.x_stride, kind), _rows("dt_stride", dt, rows, D, params.dt_stride, kind),
+            _rows("z_stride", z, rows, D, params.z_stride, kind), _rows("b_stride", B, rows, bc, params.b_stride, kind),
+            _rows("c_stride", C, rows, bc, params.c_stride, kind), *[_rows(name, t, rows, width, 0, kind) for name, t, width in more])
 
 
 def _scan_checkpoints(params, checkpoints):
     """They carry no size of their own into the call, so it is looked at here."""
     if checkpoints is not None and hasattr(checkpoints, "numel"):
+        _dense("checkpoints", checkpoints)
         need = cawn_selective_scan_workspace_bytes(params, CAWN_SCAN_CHECKPOINTS)
         if checkpoints.numel() * checkpoints.element_size() < need:
             raise ValueError(f"checkpoints: {checkpoints.numel() * checkpoints.element_size()} bytes, {need} are needed")
@@ -663,41 +719,58 @@ def _scan_checkpoints(params, checkpoints):
 
 def cawn_selective_scan_fwd(params, x, dt, A, B, C, y, workspace=None, skip=None, dt_bias=None, z=None, state_in=None, state_out=None,
                             offsets=None, checkpoints=None, stream=None):
-    _dense("A y skip dt_bias state_in state_out checkpoints", A, y, skip, dt_bias, state_in, state_out, checkpoints)
-    _scan_rows(params, offsets, x, dt, z, B, C, ("y", y, params.D, 0))
     _scan_checkpoints(params, checkpoints)
+    D, f, late = params.D, (_types or _torch_types())[0], []
+    rates = D * params.N
+    states = params.B * rates
+    x, dt, z, B, C, y = _scan_rows(params, offsets, x, dt, z, B, C, ("y", y, D))
+    arrays = (x, dt, _array(late, "A", A, rates, f), B, C, _array(late, "skip", skip, D, f), _array(late, "dt_bias", dt_bias, D, f), z,
+              _array(late, "state_in", state_in, states, f), _dp(offsets), y, _array(late, "state_out", state_out, states, f))
+    if late:
+        _refuse(late)
     n = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().cawn_selective_scan_fwd(
-        ctypes.byref(params), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(skip), _dp(dt_bias), _dp(z), _dp(state_in), _dp(offsets), _dp(y),
-        _dp(state_out), _dp(checkpoints), _dp(workspace), n, _stream(stream)), "cawn_selective_scan_fwd")
+    _check(lib().cawn_selective_scan_fwd(ctypes.byref(params), *arrays, _dp(checkpoints), _dp(workspace), n, _stream(stream)), "cawn_selective_scan_fwd")
 
 
 def cawn_selective_scan_step(params, x, dt, A, B, C, y, skip=None, dt_bias=None, z=None, state_in=None, state_out=None, stream=None):
-    _dense("A y skip dt_bias state_in state_out", A, y, skip, dt_bias, state_in, state_out)
-    _scan_rows(params, None, x, dt, z, B, C, ("y", y, params.D, 0))
-    _check(lib().cawn_selective_scan_step(
-        ctypes.byref(params), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(skip), _dp(dt_bias), _dp(z), _dp(state_in), _dp(y), _dp(state_out),
-        _stream(stream)), "cawn_selective_scan_step")
+    types, late, batch, D, N = _types or _torch_types(), [], params.B, params.D, params.N
+    f, kind, rows, bc, states = types[0], types[params.flags != 0], batch * params.L, params.G * N, batch * D * N
+    # as _scan_rows, without the calls in between: a single token's call is half as long as its checks
+    arrays = (_rows("x_stride", x, rows, D, params.x_stride, kind), _rows("dt_stride", dt, rows, D, params.dt_stride, kind), _array(late, "A", A, D * N, f),
+              _rows("b_stride", B, rows, bc, params.b_stride, kind), _rows("c_stride", C, rows, bc, params.c_stride, kind), _array(late, "skip", skip, D, f),
+              _array(late, "dt_bias", dt_bias, D, f), _rows("z_stride", z, rows, D, params.z_stride, kind), _array(late, "state_in", state_in, states, f),
+              _rows("y", y, rows, D, 0, kind), _array(late, "state_out", state_out, states, f))
+    if late:
+        _refuse(late)
+    _check(lib().cawn_selective_scan_step(ctypes.byref(params), *arrays, _stream(stream)), "cawn_selective_scan_step")
 
 
 def cawn_selective_scan_bwd(params, x, dt, A, B, C, grad_y, grad_x, grad_dt, grad_A, grad_B, grad_C, workspace, skip=None, dt_bias=None, z=None,
                             state_in=None, offsets=None, checkpoints=None, grad_state_out=None, grad_skip=None, grad_dt_bias=None, grad_z=None,
                             grad_state_in=None, stream=None):
-    _dense("A grad_y grad_x grad_dt grad_A grad_B grad_C skip dt_bias state_in checkpoints grad_state_out grad_skip grad_dt_bias grad_z grad_state_in",
-           A, grad_y, grad_x, grad_dt, grad_A, grad_B, grad_C, skip, dt_bias, state_in, checkpoints, grad_state_out, grad_skip, grad_dt_bias, grad_z,
-           grad_state_in)
-    D, bc = params.D, params.G * params.N
-    _scan_rows(params, offsets, x, dt, z, B, C, ("grad_y", grad_y, D, 0), ("grad_x", grad_x, D, 0), ("grad_dt", grad_dt, D, 0), ("grad_B", grad_B, bc, 0),
-               ("grad_C", grad_C, bc, 0), ("grad_z", grad_z, D, 0))
     _scan_checkpoints(params, checkpoints)
-    _check(lib().cawn_selective_scan_bwd(
-        ctypes.byref(params), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(skip), _dp(dt_bias), _dp(z), _dp(state_in), _dp(offsets), _dp(checkpoints),
-        _dp(grad_y), _dp(grad_state_out), _dp(grad_x), _dp(grad_dt), _dp(grad_A), _dp(grad_B), _dp(grad_C), _dp(grad_skip), _dp(grad_dt_bias),
-        _dp(grad_z), _dp(grad_state_in), _dp(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "cawn_selective_scan_bwd")
+    D, bc, f, late = params.D, params.G * params.N, (_types or _torch_types())[0], []
+    rates = D * params.N
+    states = params.B * rates
+    x, dt, z, B, C, grad_y, grad_x, grad_dt, grad_B, grad_C, grad_z = _scan_rows(
+        params, offsets, x, dt, z, B, C, ("grad_y", grad_y, D), ("grad_x", grad_x, D), ("grad_dt", grad_dt, D), ("grad_B", grad_B, bc), ("grad_C", grad_C, bc),
+        ("grad_z", grad_z, D))
+    arrays = (x, dt, _array(late, "A", A, rates, f), B, C, _array(late, "skip", skip, D, f), _array(late, "dt_bias", dt_bias, D, f), z,
+              _array(late, "state_in", state_in, states, f), _dp(offsets), _dp(checkpoints), grad_y, _array(late, "grad_state_out", grad_state_out, states, f),
+              grad_x, grad_dt, _array(late, "grad_A", grad_A, rates, f), grad_B, grad_C, _array(late, "grad_skip", grad_skip, D, f),
+              _array(late, "grad_dt_bias", grad_dt_bias, D, f), grad_z, _array(late, "grad_state_in", grad_state_in, states, f))
+    if late:
+        _refuse(late)
+    _check(lib().cawn_selective_scan_bwd(ctypes.byref(params), *arrays, _dp(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+           "cawn_selective_scan_bwd")
 
 
 def make_residual_norm_params(N, M, eps=1e-5, out=CAWN_NORM_OUT_SAME, scale_block=0, stream_float=False, flags=0, x_stride=0):
-    return cawn_residual_norm_params(ctypes.sizeof(cawn_residual_norm_params), M, N, eps, out, scale_block, int(stream_float), flags, 0, x_stride)
+    values = _RESIDUAL_NORM.size, M, N, eps, out, scale_block, int(stream_float), flags, 0, x_stride
+    try:
+        return cawn_residual_norm_params.from_buffer_copy(_RESIDUAL_NORM.pack(*values))
+    except (struct.error, OverflowError):
+        return cawn_residual_norm_params(*values)
 
 
 def cawn_residual_norm_workspace_bytes(params):
@@ -711,18 +784,51 @@ def new_residual_norm_workspace(params, device="cuda"):
     return _plain_workspace(cawn_residual_norm_workspace_bytes(params), device)
 
 
+def _norm_types(params):
+    """float32, and the types of the rows and of the stream."""
+    f, b = _types or _torch_types()
+    return (f, b, f if params.stream_float else b) if params.flags else (f, f, f)
+
+
+def _norm_rows_in(late, x, rows, M, stride, kind):
+    """Pointer of the norm's input: at least so many rows, `stride` (0: M) elements apart."""
+    n = rows * M
+    try:
+        if x.dtype is kind and x.numel() >= n and (stride == 0 or stride == M) and x.is_contiguous():
+            return x.data_ptr()
+        if n > 0:
+            _check_rows("x_stride", x, M, stride or M)
+            if x.dtype is not kind or x.numel() < n:
+                late.append(f"x: {tuple(x.shape)} of {x.dtype}, but {n} elements of {kind} are needed")
+    except AttributeError:
+        pass
+    return _dp(x)
+
+
 def cawn_residual_norm_fwd(params, x, y, residual=None, weight=None, sum_out=None, scales=None, stream=None):
-    _dense("y residual weight sum_out scales", y, residual, weight, sum_out, scales)
-    if params.N > 0:
-        _check_rows("x_stride", x, params.M, params.x_stride or params.M)
-    _check(lib().cawn_residual_norm_fwd(ctypes.byref(params), _dp(x), _dp(residual), _dp(weight), _dp(sum_out), _dp(y), _dp(scales),
-                                        _stream(stream)), "cawn_residual_norm_fwd")
+    f, kind, of_stream = _norm_types(params)
+    rows, M, late = params.N, params.M, []
+    n, out, cols = rows * M, kind, 1
+    if params.out == CAWN_NORM_OUT_E4M3:
+        out = getattr(y, "dtype", None)             # any type of one byte
+        if hasattr(y, "element_size") and y.element_size() != 1:
+            raise ValueError(f"y: {out}, but values of 8 bits are written")
+        cols = -(-M // params.scale_block) if params.scale_block > 0 else 1
+    arrays = (_norm_rows_in(late, x, rows, M, params.x_stride, kind), _array(late, "residual", residual, n, of_stream), _array(late, "weight", weight, M, f),
+              _array(late, "sum_out", sum_out, n, of_stream), _array(late, "y", y, n, out), _array(late, "scales", scales, rows * cols, f))
+    if late:
+        _refuse(late)
+    _check(lib().cawn_residual_norm_fwd(ctypes.byref(params), *arrays, _stream(stream)), "cawn_residual_norm_fwd")
 
 
 def cawn_residual_norm_bwd(params, sum, grad_y, workspace=None, weight=None, grad_sum=None, grad_residual=None, grad_x=None, grad_weight=None,
                            stream=None):
-    _dense("sum grad_y weight grad_sum grad_residual grad_x grad_weight", sum, grad_y, weight, grad_sum, grad_residual, grad_x, grad_weight)
+    f, kind, of_stream = _norm_types(params)
+    M, n, late = params.M, params.N * params.M, []
+    arrays = (_array(late, "sum", sum, n, of_stream), _array(late, "weight", weight, M, f), _array(late, "grad_y", grad_y, n, kind),
+              _array(late, "grad_sum", grad_sum, n, of_stream), _array(late, "grad_residual", grad_residual, n, of_stream),
+              _array(late, "grad_x", grad_x, n, kind), _array(late, "grad_weight", grad_weight, M, f))
+    if late:
+        _refuse(late)
     n = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().cawn_residual_norm_bwd(
-        ctypes.byref(params), _dp(sum), _dp(weight), _dp(grad_y), _dp(grad_sum), _dp(grad_residual), _dp(grad_x), _dp(grad_weight), _dp(workspace), n,
-        _stream(stream)), "cawn_residual_norm_bwd")
+    _check(lib().cawn_residual_norm_bwd(ctypes.byref(params), *arrays, _dp(workspace), n, _stream(stream)), "cawn_residual_norm_bwd")

@@ -271,3 +271,72 @@ def test_the_backward_is_cut_for_the_blocks_that_are_resident(N, fewer):
     that are float in both."""
     of = lambda flags: cb.cawn_selective_scan_workspace_bytes(scan(B=1, L=8192, D=60, N=N, G=60, flags=flags), cb.CAWN_SCAN_BWD)
     assert (of(0) < of(BF16)) if fewer else (of(0) == of(BF16))
+
+
+B_, L_, D_, N_, G_, K_ = 2, 3, 48, 8, 2, 4
+
+
+def arrays_of(f, dtype, wide=False):
+    """Arguments of a call with every array it takes, of the sizes and types that its params say."""
+    rows, z = B_ * L_, lambda n, t: torch.zeros(n, dtype=t)
+    flags = BF16 if dtype == torch.bfloat16 else 0
+    if "norm" in f.__name__:
+        stream = torch.float32 if wide else dtype
+        prm = cb.make_residual_norm_params(rows, D_, flags=flags, stream_float=wide)
+        of = {"x": dtype, "y": dtype, "grad_y": dtype, "grad_x": dtype, "residual": stream, "sum_out": stream, "sum": stream, "grad_sum": stream, "grad_residual": stream}
+        sizes = {**{n: (rows * D_, t) for n, t in of.items()}, "weight": (D_, torch.float32), "grad_weight": (D_, torch.float32)}
+    elif "conv" in f.__name__:
+        prm = cb.make_conv_params(B_, L_, D_, K_, flags=flags)
+        sizes = {**{n: (rows * D_, dtype) for n in ("x", "y", "grad_y", "grad_x")}, "weight": (D_ * K_, torch.float32), "bias": (D_, torch.float32)}
+        sizes.update({"grad_" + n: sizes[n] for n in ("weight", "bias")})
+        sizes.update({n: (B_ * (K_ - 1) * D_, torch.float32) for n in ("state_in", "state_out", "grad_state_out", "grad_state_in")})
+    else:
+        prm = cb.make_scan_params(B_, L_, D_, N_, G_, flags=flags)
+        sizes = {**{n: (rows * D_, dtype) for n in ("x", "dt", "z", "y")}, **{n: (rows * G_ * N_, dtype) for n in ("B", "C")}, "A": (D_ * N_, torch.float32),
+                 "skip": (D_, torch.float32), "dt_bias": (D_, torch.float32), "state_in": (B_ * D_ * N_, torch.float32)}
+        sizes.update({"grad_" + n: s for n, s in sizes.items()})
+        sizes.update({n: sizes["state_in"] for n in ("state_out", "grad_state_out")})
+    takes = inspect.signature(f).parameters
+    return {"params": prm, **{n: z(*s) for n, s in sizes.items() if n in takes}, **({"workspace": torch.zeros(4096, dtype=torch.uint8)} if "workspace" in takes else {})}
+
+
+@pytest.mark.parametrize("dtype, wide", [(torch.float32, False), (torch.bfloat16, False), (torch.bfloat16, True)])
+@pytest.mark.parametrize("f", [cb.cawn_short_conv_fwd, cb.cawn_short_conv_bwd, cb.cawn_selective_scan_fwd, cb.cawn_selective_scan_step, cb.cawn_selective_scan_bwd,
+                               cb.cawn_residual_norm_fwd, cb.cawn_residual_norm_bwd])
+def test_arrays_that_are_short_or_of_another_type(f, dtype, wide, monkeypatch):
+    """Each array one element short, and of each other type: refused before the library is called, which would read or write past it."""
+    class Reached(Exception):
+        pass
+
+    def lib():
+        raise Reached
+
+    good = arrays_of(f, dtype, wide)
+    checked = [n for n, t in good.items() if isinstance(t, torch.Tensor) and n != "workspace"]
+    assert len(checked) >= 5
+    monkeypatch.setattr(cb, "lib", lib)
+    with pytest.raises(Reached):
+        f(**good)
+    for n in checked:
+        t = good[n]
+        for bad in (t[:-1], *(t.to(k) for k in (torch.float32, torch.bfloat16, torch.float16, torch.float64) if k != t.dtype)):
+            with pytest.raises(ValueError, match="(?i)^" + n):         # B's rows go by the name of their stride
+                f(**{**good, n: bad})
+
+
+def test_scales_and_8_bit_rows(monkeypatch):
+    def lib():
+        raise KeyError
+    monkeypatch.setattr(cb, "lib", lib)
+    x, rows = torch.zeros(6, 200), torch.zeros(6, 200, dtype=torch.uint8)
+    for block, cols in ((0, 1), (32, 7), (64, 4), (128, 2)):
+        prm = norm(N=6, M=200, out=cb.CAWN_NORM_OUT_E4M3, scale_block=block)
+        for y in (rows, rows.view(torch.float8_e4m3fn)):
+            with pytest.raises(KeyError):
+                cb.cawn_residual_norm_fwd(prm, x, y, scales=torch.zeros(6, cols))
+        for y, scales, name in ((rows, torch.zeros(6 * cols - 1), "scales"), (rows, torch.zeros(6, cols, dtype=torch.float64), "scales"), (rows[:5], torch.zeros(6, cols), "y"),
+                                (x, torch.zeros(6, cols), "y"), (x.bfloat16(), torch.zeros(6, cols), "y")):
+            with pytest.raises(ValueError, match=name):
+                cb.cawn_residual_norm_fwd(prm, x, y, scales=scales)
+    with pytest.raises(ValueError, match="x"):          # a slice of rows, one of them missing
+        cb.cawn_residual_norm_fwd(norm(N=6, M=200, x_stride=400), torch.zeros(5, 400)[:, :200], x)
