@@ -632,9 +632,10 @@ CAWN_API int cawn_short_conv_bwd(const cawn_conv_params *params, const void *x, 
  *   y_t  = (sum_n C_t[n] h_t[n] + skip_c x_t) silu(z_t)                       skip NULL = 0; z NULL: no gate
  *   state_out = h_{L-1}
  * Shapes.  x, dt, z, y [rows, D]; B, C [rows, G, N], channel c reads group c / (D/G); A [D, N] float
- * (usually negative); skip, dt_bias [D] float; states [B, D, N] float.  Rows of x, dt, z, B and C lie
- * *_stride elements apart (0 = dense), so that they may be slices of projections, and need only be aligned to
- * their elements (whole words are read where rows begin on 16 bytes; of B and C, on four elements).
+ * (usually negative; with -infinity a state forgets all, but a step of 0 leaves it as it is); skip, dt_bias [D]
+ * float; states [B, D, N] float.  Rows of x, dt, z, B and C lie *_stride elements apart (0 = dense), so that they
+ * may be slices of projections, and need only be aligned to their elements (whole words are read where rows begin
+ * on 16 bytes; of B and C, on four elements).
  * Precision.  Everything is computed in float; results are rounded once to their type.
  * Non-finite values stay in their sequence and in the channels of their group; gradients of B and C may
  * also be spoilt in the eight tokens, counted from the sequence's first, around one.

@@ -137,6 +137,20 @@ template <int NS> __device__ __forceinline__ void store_states(float *p, const f
     }
 }
 
+// Rates for exponentials of base two.  They are finite (a NaN stays), so that a step of zero, as tokens past the end have, leaves a
+// state as it is whatever its rate.
+__device__ __forceinline__ float rate_of(float a)
+{
+    constexpr float most = 3.402823466e38f;
+    const float v = a * kLog2e;
+    return v < -most ? -most : v > most ? most : v;
+}
+__device__ __forceinline__ f32x2 rate_of(f32x2 a)
+{
+    const float2 f = halves(a);
+    return pair(rate_of(f.x), rate_of(f.y));
+}
+
 __device__ __forceinline__ f32x2 exp2_pair(f32x2 v)
 {
     const float2 f = halves(v);

@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
         load_states<NS>(carry[j], P.gstate_out + ((long long)b * P.D + c) * P.N, n0, P.N, in && P.gstate_out != nullptr);
 #pragma unroll
         for (int k = 0; k < NK; k++) {
-            A2[j][k] = mul2(A2[j][k], twice(kLog2e));
+            A2[j][k] = rate_of(A2[j][k]);
             dA[j][k] = 0ull;
         }
         const long long behind = (s.len - 1) / P.per;           // the sequence's last segment
@@ -475,7 +475,7 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(N
         load_states<NS>(A2[j], P.A + (long long)(c0 + at.ch + j) * P.N, n0, P.N, at.ch + j < nch);
 #pragma unroll
         for (int k = 0; k < NK; k++) {
-            A2[j][k] = mul2(A2[j][k], twice(kLog2e));
+            A2[j][k] = rate_of(A2[j][k]);
             own[j][k] = 0ull;
             past[j][k] = twice(1.f);
         }

@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads + (SPLIT ? Place<N
         const int c = c0 + at.ch + j;
         load_states<NS>(A2[j], P.A + (long long)c * P.N, n0, P.N, in);
 #pragma unroll
-        for (int k = 0; k < NK; k++) A2[j][k] = mul2(A2[j][k], twice(kLog2e));
+        for (int k = 0; k < NK; k++) A2[j][k] = rate_of(A2[j][k]);
         if constexpr (!SUMMARY) {
             if (seg == 0) {
                 const float *from = P.S > 1 ? P.first : P.state_in;

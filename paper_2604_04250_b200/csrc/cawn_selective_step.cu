@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(kStepThreads) selective_step_kernel(const Sele
     const float bias = P.dt_bias != nullptr ? P.dt_bias[c] : 0.f, skip = P.skip != nullptr ? P.skip[c] : 0.f;
     Token now = {};
     if (L > 0) now = token(0);
-    f32x2 A2[2] = {mul2(pair(rawA.get().x, rawA.get().y), twice(kLog2e)), mul2(pair(rawA.get().z, rawA.get().w), twice(kLog2e))}, h[R][2];
+    f32x2 A2[2] = {rate_of(pair(rawA.get().x, rawA.get().y)), rate_of(pair(rawA.get().z, rawA.get().w))}, h[R][2];
 #pragma unroll
     for (int r = 0; r < R; r++) {
         h[r][0] = pair(raw[r].get().x, raw[r].get().y);

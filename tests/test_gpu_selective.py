@@ -464,3 +464,32 @@ def test_terms_of_sums_over_channels_keep_their_bits(other, N, dtype):
         want = (sign * k * 2.0 ** -23)[:, None, None].expand(L, 1, N).to(dtype)
         assert torch.equal(g["B"].cpu(), want), (k, (g["B"].cpu().float() - want).abs().max())
         assert torch.equal(g["C"].cpu(), want), (k, (g["C"].cpu().float() - want).abs().max())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("L, D, N", [(21, 40, 16), (16, 40, 16), (3, 33, 5), (50, 24, 24), (40, 16, 64), (700, 40, 16), (523, 24, 7)])
+def test_rates_that_forget_everything(L, D, N, dtype):
+    """A of -infinity, and of a size that its product with log2 e does not hold: such a state is its own token's term alone, also behind the last
+    token of a tile that is not full.  (The definition's gradient of dt is 0 times infinity there, so that one and dt_bias's are left out.)"""
+    offsets = [0, L, 2 * L]
+    d, c = case(offsets, D, N, 1, dtype, seed=L)
+    d["A"][:, ::3], d["A"][::2, 1] = float("-inf"), -3e38
+    c["A"] = d["A"].cuda()
+    prm = params(offsets, D, N, 1, dtype)
+    marks = cb.new_scan_workspace(prm, cb.CAWN_SCAN_CHECKPOINTS)
+    y, so = forward(prm, c, checkpoints=marks)
+    w = {n: t.double().requires_grad_() for n, t in d.items()}
+    want, state = selective_scan(*(w[n] for n in LEAVES), offsets, L)
+    close(y, want, TOL[dtype], "y")
+    close(so, state, FLOAT, "state_out")
+    names = [n for n in LEAVES if n not in ("dt", "dt_bias")]
+    leaves = torch.autograd.grad([want, state], [w[n] for n in names], [d["grad_y"].double(), d["grad_state_out"].double()])
+    for saved in (marks, None):
+        g = backward(prm, c, checkpoints=saved)
+        for n, t in zip(names, leaves):
+            close(g[n], t, TOL[dtype] if n in DENSE else FLOAT, "grad_" + n)
+    if L < 60:
+        y, so = torch.empty_like(y), torch.empty_like(so)
+        cb.cawn_selective_scan_step(prm, c["x"], c["dt"], c["A"], c["B"], c["C"], y, skip=c["skip"], dt_bias=c["dt_bias"], z=c["z"], state_in=c["state_in"], state_out=so)
+        close(y, want, TOL[dtype], "y of single tokens")
+        close(so, state, FLOAT, "state of single tokens")
