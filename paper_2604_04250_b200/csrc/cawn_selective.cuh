@@ -32,8 +32,10 @@ struct SelectiveParams {
     long long xs, dts, zs, bs, cs;              // elements between rows
     long long param_cols;                       // floats of a row of part_param, a multiple of 4
     long long per;                              // tokens of a segment, a multiple of kTile
+    long long param_rows;                       // rows of part_param
     int D, N, G, Dg, blocks;                    // channels of a group, blocks of channels per group
     int S;                                      // segments
+    int by_rows;                                // segments' ends, and rows of part_param, are numbered by rows and not by sequences
     int halves;                                 // 2: the backward's first pass takes segments in halves
     int softplus, whole_x, whole_dt, whole_z, whole_d, whole_b, whole_c, whole;     // whole: all of them
 };
@@ -207,6 +209,10 @@ template <int NS> __device__ __forceinline__ void fold_segments(f32x2 (&h)[NS / 
         }
     }
 }
+
+// A sequence's first segment among those that keep an end, and its segments' rows of part_param.
+__device__ __forceinline__ long long first_end(const SelectiveParams &P, const Span &s, int b) { return P.by_rows ? s.begin / P.per : (long long)b * (P.S - 1); }
+__device__ __forceinline__ long long param_row(const SelectiveParams &P, const Span &s, int b, int seg) { return (P.by_rows ? s.begin / P.per + b : (long long)b * P.S) + seg; }
 
 // First checkpoint of a sequence: those of two sequences never meet, whatever the lengths.
 __device__ __forceinline__ long long checkpoint_of(const Span &s, int b) { return s.begin / kTile + b; }

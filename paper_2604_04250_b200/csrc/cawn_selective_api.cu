@@ -53,14 +53,15 @@ int64_t segments_of(const cawn_scan_params *p, bool bwd)
     const int64_t s = cut < longest ? cut : longest;
     return s < kMostSegments ? s : kMostSegments;
 }
-// The most sequences x segments of any call with up to this B, L and rows.
-int64_t most_segments(const cawn_scan_params *p, bool bwd)
+// For a size query: the most segments of one sequence, and of all sequences together (counted by the rows where they are packed: see
+// carve_segments), in any call with up to this B, L and rows.
+struct Most { int64_t of_one, of_all; };
+Most most_segments(const cawn_scan_params *p, bool bwd)
 {
     const int64_t room = most(slots_of(p, bwd) / blocks_of(p), 1), longest = most(p->L / kShortest, 1);
     const int64_t each = bwd ? most(room, 2 * (most_in_two(p) / blocks_of(p))) : room, of_one = each < longest ? each : longest;
-    if (p->rows > 0) return p->B * (of_one < kMostSegments ? of_one : kMostSegments);       // one of them may have nearly all rows
-    const int64_t cut = most(each, p->B), whole = p->B * longest;
-    return cut < whole ? cut : whole;
+    const int64_t whole = p->rows > 0 ? p->rows / kShortest : p->B * longest;
+    return {of_one < kMostSegments ? of_one : kMostSegments, each < whole ? each : whole};
 }
 
 // A workspace in its parts, each on a 256-byte boundary.
@@ -75,23 +76,33 @@ struct Carver {
     }
 };
 
+// The parts of a call whose time axis is cut.  All segments of a sequence but one keep an end.  These are numbered by sequences or, where
+// that are fewer (packed, many sequences shorter than L), by rows: a sequence of n rows from row r has floor((n - 1) / per) of them from
+// floor(r / per) on, so those of two sequences never meet, and all lie below rows / per.  That is no more than what is resident at once: by
+// segments_of, rows / L sequences of S segments are, and per >= L / S.
 // `sized`: for any call up to this one (the size query) instead of for this very call.
 void carve_segments(Carver &c, SelectiveParams &P, const cawn_scan_params *p, bool bwd, bool sized)
 {
-    const int64_t pieces = sized ? most_segments(p, bwd) : p->B * segments_of(p, bwd);
-    if (pieces <= (sized ? 1 : p->B)) return;
-    const int64_t ends = bwd ? 2 * pieces : pieces;         // the backward may have one per half
+    const Most m = most_segments(p, bwd);
+    if ((sized ? m.of_one : P.S) < 2) return;
+    const int64_t by_sequence = p->B * ((sized ? m.of_one : P.S) - 1);
+    const int64_t by_rows = sized ? m.of_all : P.seq.offsets != nullptr ? P.seq.rows / P.per : by_sequence;
+    P.by_rows = by_rows < by_sequence;
+    const int64_t ends = (bwd ? 2 : 1) * (P.by_rows ? by_rows : by_sequence);       // the backward may have one per half
     P.seg_state = c.floats(ends * p->D * p->N);
     P.seg_time = c.floats(ends * p->D);
     if (!bwd) P.first = c.floats((int64_t)p->B * p->D * p->N);
 }
-// Partial sums of grad_A, grad_skip and grad_dt_bias: rows that begin on 16 bytes.
+// Partial sums of grad_A, grad_skip and grad_dt_bias: rows that begin on 16 bytes, one a segment, numbered as the ends are with one more for
+// each sequence.
 int64_t param_cols(const cawn_scan_params *p) { return ceil_div((int64_t)p->D * (p->N + 2), 4) * 4; }
 void carve_bwd(Carver &c, SelectiveParams &P, const cawn_scan_params *p, bool sized)
 {
     carve_segments(c, P, p, true, sized);
     P.part_bc = c.floats(blocks_of(p) * rows_of(p) * 2 * p->N);
-    P.part_param = c.floats((sized ? most_segments(p, true) : p->B * segments_of(p, true)) * param_cols(p));
+    const Most m = most_segments(p, true);
+    P.param_rows = P.by_rows ? p->B + (sized ? m.of_all : P.seq.rows / P.per) : p->B * (sized ? m.of_one : P.S);
+    P.part_param = c.floats(P.param_rows * param_cols(p));
 }
 int64_t checkpoint_rows(const cawn_scan_params *p) { return rows_of(p) / kTile + p->B + 1; }
 
@@ -240,6 +251,6 @@ extern "C" int cawn_selective_scan_bwd(const cawn_scan_params *params, const voi
     if (rc == CAWN_OK && params->L > 0) rc = launch_selective_bc(P, half, grad_B, grad_C, st);
     if (rc != CAWN_OK) return rc;
     const long long D = params->D;
-    PartialSums sums = {P.part_param, (long long)params->B * P.S, P.param_cols, {grad_A, grad_skip, grad_dt_bias}, {D * params->N, D, D}};
+    PartialSums sums = {P.part_param, P.param_rows, P.param_cols, {grad_A, grad_skip, grad_dt_bias}, {D * params->N, D, D}};
     return sum_partials(sums, st);
 }

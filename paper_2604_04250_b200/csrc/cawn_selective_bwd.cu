@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
         }
         const long long behind = (s.len - 1) / P.per;           // the sequence's last segment
         const int end_of_all = (int)(behind - 1) * P.halves + (P.halves == 2 && s.len - 1 - behind * P.per >= half_of(P.per));
-        fold_segments<NS>(carry[j], P, A2[j], ((long long)b * (P.S - 1) * P.halves + end_of_all) * P.D + c, -P.D, end_of_all - seg * P.halves + 1, n0, in);
+        fold_segments<NS>(carry[j], P, A2[j], (first_end(P, s, b) * P.halves + end_of_all) * P.D + c, -P.D, end_of_all - seg * P.halves + 1, n0, in);
     }
     for (int i = tid; i < kScanChannels; i += kThreads) {
         sh.bias[i] = i < nch && P.dt_bias != nullptr ? P.dt_bias[c0 + i] : 0.f;
@@ -360,7 +360,8 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
             if (half == 1) __syncthreads();
         }
     }
-    float *param = P.part_param + ((long long)b * P.S + seg) * P.param_cols;
+    if (P.by_rows && seg > 0 && begin >= end) return;        // no row is theirs
+    float *param = P.part_param + param_row(P, s, b, seg) * P.param_cols;
 #pragma unroll
     for (int j = 0; j < CD; j++) {
         const bool in = at.ch + j < nch;
@@ -404,6 +405,10 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(N
     constexpr int NP = At::kPad, NK = At::kPairs, kWords = At::kWords, kQuads = At::kQuads;
     __shared__ __align__(16) float2 dd[2][kTile][kRowPairs];            // d, dy'
     __shared__ __align__(16) float cs[2][kTile][NP];
+    if (P.by_rows) {            // rows of part_param that no segment has
+        const long long all = P.param_rows * P.param_cols, step = (long long)gridDim.x * gridDim.y * blockDim.x;
+        for (long long i = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * blockDim.x + threadIdx.x; i < all; i += step) P.part_param[i] = 0.f;
+    }
     const int cb = blockIdx.x % (P.G * P.blocks), b = blockIdx.x / (P.G * P.blocks), g = cb / P.blocks;
     const int c0 = g * P.Dg + cb % P.blocks * kScanChannels;
     const int nch = min(kScanChannels, (g + 1) * P.Dg - c0), seg = blockIdx.y / P.halves + 1, half = blockIdx.y % P.halves;
@@ -504,7 +509,7 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(N
 #pragma unroll
     for (int j = 0; j < CD; j++) {
         const bool in = at.ch + j < nch;
-        const long long segment = (((long long)b * (P.S - 1) + seg - 1) * P.halves + half) * P.D + c0 + at.ch + j;
+        const long long segment = ((first_end(P, s, b) + seg - 1) * P.halves + half) * P.D + c0 + at.ch + j;
         store_states<NS>(P.seg_state + segment * P.N, own[j], n0, P.N, in);
         if (in && at.nl == 0) P.seg_time[segment] = time[j];
     }

@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads + (SPLIT ? Place<N
                 const float *from = P.S > 1 ? P.first : P.state_in;
                 load_states<NS>(h[j], from + ((long long)b * P.D + c) * P.N, n0, P.N, in && P.state_in != nullptr);
             } else {
-                const long long segment = (long long)b * (P.S - 1) * P.D + c;
+                const long long segment = first_end(P, s, b) * P.D + c;
                 load_states<NS>(h[j], P.seg_state + segment * P.N, n0, P.N, in);
                 fold_segments<NS>(h[j], P, A2[j], segment + P.D, P.D, seg - 1, n0, in);
             }
@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads + (SPLIT ? Place<N
         const bool in = at.ch + j < nch;
         const int c = c0 + at.ch + j;
         if constexpr (SUMMARY) {
-            const long long segment = ((long long)b * (P.S - 1) + seg) * P.D + c;
+            const long long segment = (first_end(P, s, b) + seg) * P.D + c;
             store_states<NS>(P.seg_state + segment * P.N, h[j], n0, P.N, in);
             if (in && at.nl == 0) P.seg_time[segment] = time[j];
         } else {

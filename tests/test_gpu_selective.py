@@ -493,3 +493,49 @@ def test_rates_that_forget_everything(L, D, N, dtype):
         cb.cawn_selective_scan_step(prm, c["x"], c["dt"], c["A"], c["B"], c["C"], y, skip=c["skip"], dt_bias=c["dt_bias"], z=c["z"], state_in=c["state_in"], state_out=so)
         close(y, want, TOL[dtype], "y of single tokens")
         close(so, state, FLOAT, "state of single tokens")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("saved", [True, False])
+@pytest.mark.parametrize("lengths, first, behind", [((*(30 * (3, 0, 17)), 900, *(20 * (5,))), 0, 0), ((520, *(60 * (1,)), 700, 0, 40), 77, 300), ((*(50 * (0,)), 1100, 16, *(40 * (0,))), 3, 0),
+                                                    ((130, 257, 128, 129, 400, 127, 600, 1, 255, 256), 0, 1)])
+@pytest.mark.parametrize("D, N, G", [(40, 16, 1), (10, 5, 5), (33, 24, 1)])
+def test_many_short_sequences_and_a_long_one(D, N, G, lengths, first, behind, saved, dtype):
+    """Cut for the long one: what segments leave is numbered by rows."""
+    offsets = packed_offsets(lengths, first)
+    check(offsets, D, N, G, dtype, packed=True, rows=offsets[-1] + behind, seed=len(lengths) + D, saved=saved)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D, N, G", [(8, 16, 1), (96, 8, 3), (1000, 16, 1), (33, 64, 1), (70, 24, 70)])
+def test_calls_take_the_workspace_that_the_query_names(D, N, G, dtype):
+    """Each call with as many bytes as the query says, and nothing written behind them; and with those of the largest of the calls."""
+    dense = [[i * L for i in range(B + 1)] for B, L in ((1, 1), (1, 300), (3, 600), (7, 130), (1, 2100), (40, 257))]
+    packed = [packed_offsets(lengths, first) for lengths, first in (((600, 0, 300, 5), 7), (90 * (3,) + (900,), 0), (20 * (0, 1), 4), ((256, 129) * 9, 0))]
+    ops = (cb.CAWN_SCAN_FWD, cb.CAWN_SCAN_BWD, cb.CAWN_SCAN_BWD_RECOMPUTE, cb.CAWN_SCAN_CHECKPOINTS)
+    guard, pattern = 4096, 0x5A
+
+    def call(offsets, is_packed, sizes):
+        """y, states and gradients (with and without checkpoints) of a call with workspaces of these sizes."""
+        rows = offsets[-1]
+        _, c = case(offsets, D, N, G, dtype, seed=rows)
+        prm = params(offsets, D, N, G, dtype, is_packed, rows)
+        off = torch.tensor(offsets, device="cuda") if is_packed else None
+        spaces = [torch.full((n + guard,), pattern, dtype=torch.uint8, device="cuda") for n in sizes(prm)]
+        wf, wb, wr, marks = (w[:w.numel() - guard] for w in spaces)
+        for w in (wf, wb, wr, marks):
+            w.fill_(0xFF)
+        y, so = torch.full_like(c["grad_y"], 7), torch.empty_like(c["state_in"])
+        same = {n: c[n] for n in ("skip", "dt_bias", "z", "state_in")}
+        cb.cawn_selective_scan_fwd(prm, c["x"], c["dt"], c["A"], c["B"], c["C"], y, wf, state_out=so, offsets=off, checkpoints=marks, **same)
+        saved, again = backward(prm, c, off, checkpoints=marks, workspace=wb), backward(prm, c, off, workspace=wr)
+        assert all((w[-guard:] == pattern).all() for w in spaces)
+        return [y, so, *saved.values(), *again.values()]
+
+    for calls, is_packed in ((dense, False), (packed, True)):
+        of = lambda p: [cb.cawn_selective_scan_workspace_bytes(p, op) for op in ops]
+        biggest = cb.make_scan_params(max(len(o) - 1 for o in calls), max(b - a for o in calls for a, b in zip(o, o[1:])), D, N, G, flags=flags_of(dtype),
+                                      rows=max(o[-1] for o in calls) if is_packed else 0)
+        for offsets in calls:
+            got, want = call(offsets, is_packed, of), call(offsets, is_packed, lambda p: of(biggest))
+            assert all(torch.equal(a, b) for a, b in zip(got, want))

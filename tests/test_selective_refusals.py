@@ -340,3 +340,13 @@ def test_scales_and_8_bit_rows(monkeypatch):
                 cb.cawn_residual_norm_fwd(prm, x, y, scales=scales)
     with pytest.raises(ValueError, match="x"):          # a slice of rows, one of them missing
         cb.cawn_residual_norm_fwd(norm(N=6, M=200, x_stride=400), torch.zeros(5, 400)[:, :200], x)
+
+
+@pytest.mark.parametrize("B, rows, L, D, N", [(256, 65536, 2048, 2048, 16), (1000, 30000, 4000, 512, 8), (64, 100000, 20000, 64, 24)])
+def test_packed_workspaces_are_counted_by_their_rows(B, rows, L, D, N):
+    """Many sequences shorter than the longest: what the dense call of as many rows in sequences of L takes, and for each sequence a state (forward)
+    or a row of parameters' gradients (backward) more."""
+    packed, dense = cb.make_scan_params(B, L, D, N, rows=rows), cb.make_scan_params(-(-rows // L), L, D, N)
+    size = cb.cawn_selective_scan_workspace_bytes
+    assert size(packed, cb.CAWN_SCAN_FWD) <= size(dense, cb.CAWN_SCAN_FWD) + B * D * N * 4 + 1024
+    assert size(packed, cb.CAWN_SCAN_BWD) <= size(dense, cb.CAWN_SCAN_BWD) + B * D * (N + 2) * 4 + 1024
