@@ -539,3 +539,36 @@ def test_calls_take_the_workspace_that_the_query_names(D, N, G, dtype):
         for offsets in calls:
             got, want = call(offsets, is_packed, of), call(offsets, is_packed, lambda p: of(biggest))
             assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("saved", [True, False])
+@pytest.mark.parametrize("absent, pad, softplus", [(("z",), 0, True), (("state_in",), 8, True), (("skip", "dt_bias"), 3, True), (("z", "skip", "dt_bias", "state_in"), 8, True),
+                                                   ((), 3, False), (("z", "state_in"), 0, False)])
+def test_segments_of_slices_and_without_arrays(absent, pad, softplus, saved, dtype):
+    check([0, 690, 1380], 40, 16, 2, dtype, pad=pad, absent=absent, softplus=softplus, saved=saved)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("absent", [(), ("z", "state_in")])
+def test_segments_of_longer_sequences_than_said(absent, dtype):
+    """Cut by the L of the params: the rows behind are neither read nor written."""
+    check([3, 903, 1203, 1203, 1960], 24, 16, 1, dtype, packed=True, L=600, rows=1965, absent=absent, pad=8)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("absent", [(), ("z",), ("state_in",), ("z", "skip", "dt_bias", "state_in")])
+@pytest.mark.parametrize("B, D, N, G, L", [(70, 300, 16, 2, 4), (61, 1100, 5, 2, 3), (40, 512, 24, 4, 2), (33, 5000, 2, 5, 2), (66, 130, 64, 2, 4)])
+def test_tokens_of_a_batch_in_groups(B, D, N, G, L, absent, dtype):
+    """A thread takes four sequences, several tokens of each, with groups and without what may be absent."""
+    offsets = [i * L for i in range(B + 1)]
+    d, c = case(offsets, D, N, G, dtype, seed=B + L, pad=8)
+    w = {n: t.double() for n, t in d.items()}
+    a = [None if n in absent and n != "state_in" else w[n] for n in LEAVES[:-1]]
+    want, want_state = selective_scan(*a, torch.zeros_like(w["state_in"]) if "state_in" in absent else w["state_in"], offsets, L)
+    y, state = torch.empty(B * L, D, dtype=dtype, device="cuda"), torch.full_like(c["state_in"], float("nan"))
+    opt = {n: None if n in absent else c[n] for n in ("skip", "dt_bias", "z", "state_in")}
+    prm = cb.make_scan_params(B, L, D, N, G, True, flags_of(dtype), *(c[n].stride(0) for n in ("x", "dt", "z", "B", "C")))
+    cb.cawn_selective_scan_step(prm, c["x"], c["dt"], c["A"], c["B"], c["C"], y, state_out=state, **opt)
+    close(y, want, TOL[dtype], "y")
+    close(state, want_state, FLOAT, "state")
