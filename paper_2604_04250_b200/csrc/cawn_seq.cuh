@@ -163,8 +163,6 @@ __device__ __forceinline__ f32x2 sigmoid_of(f32x2 v)
     const float2 d = halves(add2(pair(exp2_fast(e.x), exp2_fast(e.y)), twice(1.f)));
     return pair(reciprocal_fast(d.x), reciprocal_fast(d.y));
 }
-// Slope of v sigmoid(v), with sg = sigmoid(v).
-__device__ __forceinline__ float silu_slope(float v, float sg) { return sg * fmaf(v, 1.f - sg, 1.f); }
 
 // Sums of `rows` partial rows of `cols` floats each, in double and in a fixed order, into up to three arrays that the
 // columns belong to one after the other (NULL: not wanted).
