@@ -32,6 +32,7 @@ struct SelectiveParams {
     long long xs, dts, zs, bs, cs;              // elements between rows
     long long param_cols;                       // floats of a row of part_param, a multiple of 4
     long long per;                              // tokens of a segment, a multiple of kTile
+    double per_inverse;
     long long param_rows;                       // rows of part_param
     int D, N, G, Dg, blocks;                    // channels of a group, blocks of channels per group
     int S;                                      // segments
@@ -211,9 +212,17 @@ template <int NS> __device__ __forceinline__ void fold_segments(f32x2 (&h)[NS / 
     }
 }
 
+// floor(row / per).  The product is off by less than one; a division of long integers is a call, whose registers cost the walk of
+// 1 x 32768 x 768 x 16 2% (294 -> 300 us) though it does not come here.
+__device__ __forceinline__ long long over_per(const SelectiveParams &P, long long row)
+{
+    long long q = (long long)((double)row * P.per_inverse);
+    q -= q * P.per > row;
+    return q + ((q + 1) * P.per <= row);
+}
 // A sequence's first segment among those that keep an end, and its segments' rows of part_param.
-__device__ __forceinline__ long long first_end(const SelectiveParams &P, const Span &s, int b) { return P.by_rows ? s.begin / P.per : (long long)b * (P.S - 1); }
-__device__ __forceinline__ long long param_row(const SelectiveParams &P, const Span &s, int b, int seg) { return (P.by_rows ? s.begin / P.per + b : (long long)b * P.S) + seg; }
+__device__ __forceinline__ long long first_end(const SelectiveParams &P, const Span &s, int b) { return P.by_rows ? over_per(P, s.begin) : (long long)b * (P.S - 1); }
+__device__ __forceinline__ long long param_row(const SelectiveParams &P, const Span &s, int b, int seg) { return (P.by_rows ? over_per(P, s.begin) + b : (long long)b * P.S) + seg; }
 
 // First checkpoint of a sequence: those of two sequences never meet, whatever the lengths.
 __device__ __forceinline__ long long checkpoint_of(const Span &s, int b) { return s.begin / kTile + b; }

@@ -111,6 +111,7 @@ void cut(SelectiveParams &P, const cawn_scan_params *p, bool bwd)
 {
     P.S = (int)segments_of(p, bwd);
     P.per = most(ceil_div(ceil_div(p->L, P.S), kTile), 1) * kTile;
+    P.per_inverse = 1.0 / (double)P.per;
     P.halves = bwd && 2 * (P.S - 1) * p->B * blocks_of(p) <= slots_of(p, false) ? 2 : 1;
 }
 
