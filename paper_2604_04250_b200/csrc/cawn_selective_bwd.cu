@@ -408,6 +408,7 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(N
     constexpr int NP = At::kPad, NK = At::kPairs, kWords = At::kWords, kQuads = At::kQuads;
     __shared__ __align__(16) float2 dd[2][kTile][kRowPairs];            // d, dy'
     __shared__ __align__(16) float cs[2][kTile][NP];
+    __shared__ long long own_end;           // its place; a stager finds it, since the walk needs every register
     if (P.by_rows) {            // rows of part_param that no segment has
         const long long all = P.param_rows * P.param_cols, step = (long long)gridDim.x * gridDim.y * blockDim.x;
         for (long long i = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * blockDim.x + threadIdx.x; i < all; i += step) P.part_param[i] = 0.f;
@@ -420,6 +421,7 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(N
     const long long end = s.len < behind ? s.len : behind;
     if (begin >= end) return;
     if (threadIdx.x >= At::kCompute) {
+        if (threadIdx.x == At::kCompute) own_end = (first_end(P, s, b) + seg - 1) * P.halves + half;
         const int lane = threadIdx.x - At::kCompute, word = lane % 4 * 8;
         const T *dt = static_cast<const T *>(P.dt) + s.begin * P.dts + c0 + word, *gy = static_cast<const T *>(P.gy) + s.begin * P.D + c0 + word;
         const T *z = P.z != nullptr ? static_cast<const T *>(P.z) + s.begin * P.zs + c0 + word : nullptr;
@@ -512,7 +514,7 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(N
 #pragma unroll
     for (int j = 0; j < CD; j++) {
         const bool in = at.ch + j < nch;
-        const long long segment = ((first_end(P, s, b) + seg - 1) * P.halves + half) * P.D + c0 + at.ch + j;
+        const long long segment = own_end * P.D + c0 + at.ch + j;
         store_states<NS>(P.seg_state + segment * P.N, own[j], n0, P.N, in);
         if (in && at.nl == 0) P.seg_time[segment] = time[j];
     }

@@ -17,6 +17,7 @@ template <class T, int NL, int NS, int CD, bool SUMMARY> struct FwdShared {
     float2 dd[2][kTile][kRowPairs];                             // d, d x
     float bc[2][2][kTile][At::kPad];
     float out[SUMMARY ? 1 : 2][kTile][NL * kRowFloats + 4];     // read-out by lane of a channel (and 16 bytes, for the stagers' two rows at a time)
+    long long own_end;                                          // of a summary: its place.  A stager finds it, since the walk needs every register
     Eight<T> words[SUMMARY ? 1 : 3][2][At::kWords][At::kStagers];       // x and z as a stager fetched them, until their tile is finished
 };
 
@@ -41,6 +42,7 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads + (SPLIT ? Place<N
 
     if (threadIdx.x >= At::kCompute) {
         if (!walks) return;
+        if (SUMMARY && threadIdx.x == At::kCompute) sh.own_end = first_end(P, s, b) + seg;
         const int lane = (threadIdx.x - At::kCompute) % At::kStagers, word = lane % 4 * 8;
         const T *x = static_cast<const T *>(P.x) + s.begin * P.xs + c0 + word, *dt = static_cast<const T *>(P.dt) + s.begin * P.dts + c0 + word;
         const T *z = P.z != nullptr && !SUMMARY && P.y != nullptr ? static_cast<const T *>(P.z) + s.begin * P.zs + c0 + word : nullptr;
@@ -247,7 +249,7 @@ __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads + (SPLIT ? Place<N
         const bool in = at.ch + j < nch;
         const int c = c0 + at.ch + j;
         if constexpr (SUMMARY) {
-            const long long segment = (first_end(P, s, b) + seg) * P.D + c;
+            const long long segment = sh.own_end * P.D + c;
             store_states<NS>(P.seg_state + segment * P.N, h[j], n0, P.N, in);
             if (in && at.nl == 0) P.seg_time[segment] = time[j];
         } else {
