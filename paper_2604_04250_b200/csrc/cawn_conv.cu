@@ -5,8 +5,9 @@
 // gradient on the last K - 1), dw_k = sum_t dz_t e_{t+k}, dbias = sum_t dz_t.
 // Bound: memory; an element costs K products.  A thread keeps four channels and walks rows with the last K - 1 of them in
 // registers, so that a row is fetched once but for the K - 1 in front of a walk, which the neighbour's fetch has brought to L1 or L2.
-// Measured with SiLU, K = 4: 8 x 2048 x 2048 bfloat16 forward 30 us (4.5 TB/s; memory's time 21, the exponentials and reciprocals of
-// the sigmoid 15), backward 78, float backward 88 (4.6 TB/s).
+// Measured with SiLU, K = 4: 8 x 2048 x 2048 bfloat16 forward 30 us (4.4 TB/s; memory's time 21, the exponentials and reciprocals of
+// the sigmoid 15), backward 71 (2.9 TB/s; memory's time 31: issue 51% with 12 warps a multiprocessor of 152 registers, which wait for
+// their own arithmetic), float 52 (5.2 TB/s) and 80 (5.1 TB/s).
 #include "cawn_seq.cuh"
 
 namespace cawn {

@@ -5,8 +5,8 @@
 // Backward with d = w dL/dy, sh = s r:  ds = r (d - sh mean(d sh)) + dL/ds from past the norm;  dw = sum of dL/dy sh.
 // Bound: memory.  A row is held in the registers of a team (a warp up to 1024 channels, a block of eight above), eight
 // neighbours a lane and word, and read once.
-// Measured, 32768 x 768 bfloat16: a float stream with its sum, to 8 bits with a scale per 128 channels, 52 us (5.3 TB/s); the
-// backward with a bfloat16 stream 38 us (5.2 TB/s).
+// Measured, 32768 x 768 bfloat16: a float stream with its sum, to 8 bits with a scale per 128 channels, 54 us (5.1 TB/s); the
+// backward with a bfloat16 stream 39 us (5.2 TB/s).
 #include "cawn_seq.cuh"
 
 #include <cuda_fp8.h>

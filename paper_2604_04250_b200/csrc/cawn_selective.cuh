@@ -4,8 +4,8 @@
 // y = (sum_n C_n h_n + skip x) silu(z).  B and C belong to a token and a group of channels.
 //
 // Layout of the work.  A block has 32 channels of one group and one sequence (or a segment of it) and walks its tokens in
-// tiles of 16 (blocks of 16 channels would spread more evenly over the multiprocessors, but 8 x 2048 x 2048 x 16 then takes 311 us
-// instead of 234: each stages B and C for itself).  A thread has CD neighbouring channels and NS states of each; NL lanes share a channel (N up to NL * NS).  In a
+// tiles of 16 (blocks of 16 channels would spread more evenly over the multiprocessors, but 8 x 2048 x 2048 x 16 then took 311 us
+// instead of 235: each stages B and C for itself).  A thread has CD neighbouring channels and NS states of each; NL lanes share a channel (N up to NL * NS).  In a
 // warp lane bits 0-1 are channels, the next log2 NL bits the lane's states, the rest channels again.  A tile's (d, d x) and
 // rows of B and C are made floats once, in shared memory; the next tile is fetched while one is computed.  What a
 // thread reads there for a token is 8 bytes a channel and 8 a state, so two channels by four states (6 bytes a cell) and not one by

@@ -29,9 +29,9 @@ int64_t blocks_of(const cawn_scan_params *p) { return p->G * ceil_div(p->D / p->
 int64_t rows_of(const cawn_scan_params *p) { return p->rows > 0 ? p->rows : (int64_t)p->B * p->L; }
 
 // Segments of the time axis, none shorter than 128 tokens.  Where the blocks of whole sequences leave multiprocessors idle, as many
-// segments as are resident at once; otherwise none: 2048 tokens of 16 states take 107 us with one block a multiprocessor, 127 with
-// two and 236 with four, and the pass before it half as much again (74 blocks: 107 us whole, 103 in two segments, 78 in four; 148
-// blocks of 32 states: 123 us whole, 160 in two).
+// segments as are resident at once; otherwise none: 2048 tokens of 16 states take 112 us with one block a multiprocessor, 131 with
+// two and 233 with four, and the pass before it half as much again (74 blocks: 112 us whole, 67 in four segments; 148 blocks of 32
+// states: 125 us whole, 164 in two).
 // The backward's pass is an eighth of its walk: two segments pay as soon as they are resident, with 9 to 16 states up to seven tenths of
 // the places (1024 tokens of 16 states, float: 288 blocks 669 us whole, 575 in two, 352 blocks 692 and 687, 384 blocks 694 and 742; bfloat16:
 // 416 blocks 709 and 679, 448 blocks 729 and 781; with 8 states, float, 320 blocks 669 and 687, with 24 224 blocks 742 and 790).

@@ -6,15 +6,16 @@
 //   dz = dy (sum_n C h + skip x) silu'(z).
 // A walk takes tiles of 16 tokens from the last to the first, a tile as two halves.  A tile's first state is a checkpoint; the
 // states in front of each four tokens are found from it, and then w and the decays of four tokens stay in registers while
-// the walk turns round.  So a decay's exponential is taken 1.75 times.  Those registers (some 220 a thread) are why every warp here
+// the walk turns round.  So a decay's exponential is taken 1.75 times.  Those registers (some 250 a thread) are why every warp here
 // does all of the work, two a scheduler, where the forward has warps of two kinds: lanes leave sums over their own states in
 // shared memory, and when half a tile is done all threads add them up, finish and store.
 // Sums over channels (dB, dC) go through the tensor cores: the left factor is a selection, ones in row t (and 8 + t) and
 // zeros elsewhere, so that one product adds four lanes' lam d x to row t and their dy' h to row 8 + t, for eight groups of
 // lanes at once.  Operands: a term in three bfloat16 parts of eight bits, which hold all of a float's 24; two of them in one product
 // (m16n8k16), the third in another (m16n8k8).  (With two parts, 16 bits, results in bfloat16 were off by 2e-4 of their norm.)
-// Bound: the latency of those chains with eight warps a multiprocessor.  8 x 2048 x 1024 x 16 bfloat16 with the gate: walk 545 us
-// (issue 38%, shared memory 48%, exponentials 26%), the pass before its two segments 65, the sums of dB and dC 17.
+// Bound: the latency of those chains with eight warps a multiprocessor.  8 x 2048 x 1024 x 16 bfloat16 with the gate: walk 581 us
+// (issue 39%, shared memory 45%, exponentials 24%, tensor cores 11%; with two parts a term 545), the pass before its two segments 63, the
+// sums of dB and dC 18.  In float, six warps a multiprocessor by shared memory: walk 862.
 #include "cawn_selective.cuh"
 
 namespace cawn {
@@ -399,7 +400,7 @@ __global__ void __launch_bounds__(32 * NL / CD) selective_bwd_kernel(const Selec
 }
 
 // A segment's own gradient at its start, and its sum of d: for the segments in front of it.  In halves where there is room for as many
-// blocks at once, since there is one segment less than in the walk (8 x 2048 x 1024 x 16: 90 us whole, 65 in halves).
+// blocks at once, since there is one segment less than in the walk (8 x 2048 x 1024 x 16: 90 us whole, 63 in halves).
 template <class T, int NL, int NS, int CD>
 __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads, resident_blocks(NL, NS)) selective_bwd_summary_kernel(const SelectiveParams P)
 {

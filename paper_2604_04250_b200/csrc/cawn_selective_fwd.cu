@@ -4,9 +4,9 @@
 // the read-out.  The stagers bring tile k + 1 into shared memory, and finish tile k - 1: they sum over the lanes, add skip x, gate and
 // store.  (With the sums by shuffles and the stores in the computing warps these waited for them in order: 82 of 278 us of
 // 8 x 2048 x 2368 x 16.)
-// Measured, bfloat16 with the gate: 8 x 2048 x 2048 x 16 in 226 us, 1.9 times the decays' exponentials: their unit is busy 67% of
+// Measured, bfloat16 with the gate: 8 x 2048 x 2048 x 16 in 224 us, 1.9 times the decays' exponentials: their unit is busy 68% of
 // the time (the step's and the gate's are a quarter more), issue 48%, and 80 of 148 multiprocessors have three blocks where the
-// others have four.  1 x 32768 x 768 x 16, 24 segments behind a pass: 284 us (exponentials 176, each taken twice).
+// others have four.  1 x 32768 x 768 x 16, 24 segments behind a pass: 283 us (exponentials 176, each taken twice).
 #include "cawn_selective.cuh"
 
 namespace cawn {
@@ -22,7 +22,7 @@ template <class T, int NL, int NS, int CD, bool SUMMARY> struct FwdShared {
 };
 
 // SPLIT: the finishing has warps of its own and the computing warps look four tokens ahead, not two.  For calls of so few blocks that
-// half of a multiprocessor's places are enough, and with them half of the registers: 8 x 2048 x 1024 x 16 in 127 instead of 160 us.
+// half of a multiprocessor's places are enough, and with them half of the registers: 8 x 2048 x 1024 x 16 in 131 instead of 166 us.
 template <class T, int NL, int NS, int CD, bool SUMMARY, bool WHOLE, bool SPLIT>
 __global__ void __launch_bounds__(Place<NL, NS, CD>::kThreads + (SPLIT ? Place<NL, NS, CD>::kStagers : 0), resident_blocks(NL, NS) / (SPLIT ? 2 : 1)) selective_fwd_kernel(const SelectiveParams P)
 {
