@@ -637,6 +637,8 @@ CAWN_API int cawn_short_conv_bwd(const cawn_conv_params *params, const void *x, 
  * may be slices of projections, and need only be aligned to their elements (whole words are read where rows begin
  * on 16 bytes; of B and C, on four elements).
  * Precision.  Everything is computed in float; results are rounded once to their type.
+ * Where the time axis is cut (see the forward), the product of the decays of a segment's tokens is a float of its own:
+ * states that grow (A > 0, or negative steps) by more than 3e38 within one become infinite or NaN, whatever they hold.
  * Non-finite values stay in their sequence and in the channels of their group; gradients of B and C may
  * also be spoilt in the eight tokens, counted from the sequence's first, around one.
  * Limits: N <= 64, G <= 65535.
